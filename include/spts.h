@@ -380,6 +380,117 @@ spts_status spts_decode_step(spts_ctx* ctx, const spts_model_weights* mw, spts_k
                              const void* x_in, int32_t token_in, int32_t pos, void* x_out,
                              float* logits_out, int32_t* token_out);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Generation with 4-bit weights and a 4-bit KV cache (the paper's decode phase reads every weight and every cached
+ * row once per token; these calls are the same phase with both held in 4 bits, and the rules a generation puts on
+ * its logits).
+ *
+ * A 4-bit group is 32, 64 or 128 elements that share a bf16 pair (scale, mid); a code c in 0..15 stands for
+ *   scale * (c - 8) + mid.
+ * Quantising a group x (all in 64 bits, every stored number rounded once to bf16):
+ *   scale = bf16((max x - min x) / 15),  mid = bf16((max x + min x) / 2 + scale / 2),
+ *   c = clamp(rint((x - mid) / scale) + 8, 0, 15), ties to even;  scale == 0: c = 8.
+ * A group with a NaN or an infinity in it is stored as scale 0, mid NaN, and SPTS_ERR_NONFINITE goes to the device
+ * status word.
+ *
+ * None of these calls reads anything back or depends on the host's view of a length, so all of them can be captured
+ * into a CUDA graph; like every call they use the context's workspace, so two captured graphs of one context must
+ * not run at the same time.  They take either storage type; SPTS_REFERENCE_KERNELS selects the plain kernels. */
+
+/* A weight matrix [out, in] in 4 bits: byte i of a row holds element 2i in its low and 2i + 1 in its high nibble. */
+typedef struct {
+  const void* codes;      /* [out, in / 2] bytes, 16-byte aligned          */
+  const void* params;     /* [out, in / group, 2] bf16 (scale, mid)        */
+  int32_t out_features;
+  int32_t in_features;    /* a multiple of group                           */
+  int32_t group;          /* 32, 64 or 128                                 */
+} spts_w4;
+
+/* Quantises W [out, in] (storage type) into codes and params as above. */
+spts_status spts_w4_quantize(spts_ctx* ctx, const void* W, int out_features, int in_features, int group, void* codes,
+                             void* params);
+
+enum {
+  SPTS_W4_NORM = 1u,      /* x is RMS-normalised first (rms_eps of the context; gains folded into W): y *= 1 / rms(x) */
+  SPTS_W4_FP32_OUT = 2u   /* Y is fp32 whatever the storage type (logits) */
+};
+#define SPTS_W4_MAX_N 32
+
+/* Y[t] = X[t] W^T for n tokens, 0 <= n <= SPTS_W4_MAX_N (the codes are read once for all of them).
+ *   w2 given: Y[t] = silu(X[t] W^T) * (X[t] W2^T) (gate and up projection; same shape and group)
+ *   residual given: Y[t] = residual[t] + X[t] W^T (Y may be the residual itself; not with w2 or SPTS_W4_FP32_OUT)
+ * X [n, in], residual and Y [n, out] in the storage type with row strides ldx, ldr, ldy in elements; X 16-byte aligned,
+ * ldx a multiple of 8 (n > 1).  Sums in fp32, one rounding at the end. */
+spts_status spts_w4_gemv(spts_ctx* ctx, const spts_w4* w, const spts_w4* w2, const void* X, int64_t ldx, int n,
+                         const void* residual, int64_t ldr, uint32_t flags, void* Y, int64_t ldy);
+
+/* One layer's KV cache of n_seq sequences in 4 bits, head-major: the rows of one KV head of one sequence are
+ * contiguous.  Inside a row of d codes (two to a byte, low nibble first) storage position p holds
+ *   keys    dim 32 t + 8 c + j at p = (c * d / 32 + t) * 8 + j   (c < 4, j < 8)
+ *   values  dim 32 t + 4 g + j at p = (g * d / 32 + t) * 4 + j   (g < 8, j < 4)
+ * (the order in which the attention kernel's matrix fragments want them).  Groups run along the dims of a head.
+ * Rows at and behind len[b] are never read as data: they may hold anything. */
+typedef struct {
+  void* k_codes;          /* [n_seq, Hkv, capacity, d / 2] bytes              */
+  void* v_codes;
+  void* k_params;         /* [n_seq, Hkv, capacity, d / group, 2] bf16        */
+  void* v_params;
+  int32_t* pos;           /* [n_seq, capacity] original positions, optional   */
+  int32_t* len;           /* DEVICE [n_seq]: rows held by each sequence       */
+  int32_t n_seq;
+  int32_t capacity;       /* a multiple of 32                                 */
+  int32_t group;          /* 32, 64 or 128, at most d                         */
+} spts_kv4_cache;
+
+/* Quantises n_rows rows of K and V [n_rows, Hkv, d] (K after RoPE; row strides ldk, ldv in elements) into the cache.
+ * Sequence b owns rows [row_start[b], row_start[b + 1]) (device [n_seq + 1]; NULL: n_rows == n_seq, one row each);
+ * they go to slots at[b], at[b] + 1, ... (device [n_seq]; NULL: behind the rows held, at = len), and len[b] becomes
+ * at[b] + the sequence's number of rows.  Rows behind row_start[n_seq] (padding) are ignored.  A slot outside
+ * [0, capacity) is not written, len is clipped to the capacity, and SPTS_ERR_WORKSPACE goes to the device status word.
+ * pos [n_rows] is stored where the cache has positions.  K_read, V_read [n_rows, Hkv, d] (storage type, optional):
+ * the values that the cache now stands for; padding rows of them are left as they were. */
+spts_status spts_kv4_append(spts_ctx* ctx, const spts_kv4_cache* cache, const void* K, int64_t ldk, const void* V,
+                            int64_t ldv, const int32_t* pos, const int32_t* row_start, const int32_t* at, int n_rows,
+                            void* K_read, void* V_read);
+
+/* Attention of one query per sequence over what its cache holds: O[b, h] = softmax_j(Q[b, h] . K[b, j] / sqrt(d))
+ * V[b, j], j < len[b], KV head h / (H / Hkv).  Q [n_seq, H, d] and O [n_seq, H * d] in the storage type, row strides
+ * ldq, ldo in elements.  A sequence with len[b] <= 0 gets zeros; len[b] beyond the capacity counts as the capacity.
+ * n_seq <= SPTS_KV4_MAX_SEQ. */
+#define SPTS_KV4_MAX_SEQ 1024
+spts_status spts_kv4_attention(spts_ctx* ctx, const spts_kv4_cache* cache, const void* Q, int64_t ldq, void* O_out,
+                               int64_t ldo);
+
+/* Rules for the logits of n rows.  Every pointer is a device pointer and may be NULL (the rule is off).
+ * The lists are packed: row b's tokens are history[history_start[b]] .. history[history_start[b + 1] - 1] and of them
+ * those from index generated_start[b] on were generated (NULL: all); its biases are the entries bias_start[b] ..
+ * bias_start[b + 1] - 1.  Tokens outside [0, vocab) are ignored. */
+typedef struct {
+  const int32_t* history;          /* [n_history]  */
+  const int32_t* history_start;    /* [n + 1]      */
+  const int32_t* generated_start;  /* [n]          */
+  const float* repetition;         /* [n] > 0      */
+  const float* presence;           /* [n]          */
+  const float* frequency;          /* [n]          */
+  const int32_t* bias_token;       /* [n_bias]     */
+  const float* bias_value;         /* [n_bias]     */
+  const int32_t* bias_start;       /* [n + 1]      */
+  const uint32_t* mask;            /* [n, ld_mask] words; bit (v % 32) of word v / 32 set: token v is allowed */
+  int64_t ld_mask;
+  int32_t n_history;
+  int32_t n_bias;
+} spts_logits_rules;
+
+/* For every row b and token v, each step one fp32 operation:
+ *   a token of the history:  l = l > 0 ? l / repetition[b] : l * repetition[b]
+ *   a generated token:       l = l - frequency[b] * (times generated);  l = l - presence[b]
+ *   l = l + bias (of several entries for one token the last one counts)
+ *   l = -inf where the mask does not allow the token
+ * out [n, vocab] (row stride ldo; may be the logits themselves; NULL: not written) and token_out [n] (optional) = the
+ * lowest index of the largest l; NaN never wins; -1 where no token is left above -inf. */
+spts_status spts_process_logits(spts_ctx* ctx, const float* logits, int64_t ld, int n, int vocab,
+                                const spts_logits_rules* rules, float* out, int64_t ldo, int32_t* token_out);
+
 #ifdef __cplusplus
 }
 #endif

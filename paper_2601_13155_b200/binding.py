@@ -22,6 +22,7 @@ OPT_REFERENCE_KERNELS = 2
 OPT_PAP_WINDOW = 8
 OPT_FFN_SCORE_PAP_ONLY = 16
 OPT_DEBUG_CHECKS = 32
+W4_NORM, W4_FP32_OUT, W4_MAX_N = 1, 2, 32
 
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "SHAPE", 3: "WORKSPACE", 4: "CUDA", 5: "TIMEOUT",
                 6: "NONFINITE", 7: "UNSUPPORTED", 8: "INDEX"}
@@ -60,6 +61,25 @@ class MsdpStageC(C.Structure):
                 ("n_next", C.c_int32)]
 
 
+class W4C(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("params", C.c_void_p), ("out_features", C.c_int32), ("in_features", C.c_int32),
+                ("group", C.c_int32)]
+
+
+class Kv4CacheC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k_codes", "v_codes", "k_params", "v_params", "pos", "len")] + \
+               [(n, C.c_int32) for n in ("n_seq", "capacity", "group")]
+
+
+LOGITS_RULES = ("history", "history_start", "generated_start", "repetition", "presence", "frequency", "bias_token",
+                "bias_value", "bias_start", "mask")
+
+
+class LogitsRulesC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in LOGITS_RULES] + \
+               [("ld_mask", C.c_int64), ("n_history", C.c_int32), ("n_bias", C.c_int32)]
+
+
 class ModelWeightsC(C.Structure):
     _fields_ = [("layers", C.POINTER(LayerWeightsC)), ("lm_head", C.c_void_p), ("embed", C.c_void_p)]
 
@@ -70,7 +90,8 @@ EXPORTS = ("spts_workspace_bytes", "spts_create", "spts_destroy", "spts_set_opti
            "spts_first_token", "spts_prefill", "spts_decode_step", "spts_profile_begin", "spts_profile_end",
            "spts_topk_select_static", "spts_proxy_scratch_bytes", "spts_proxy_build",
            "spts_layer_prefill_skip_batch", "spts_msdp_plan", "spts_check_guards", "spts_selftest_wait_timeout",
-           "spts_debug_check_index_list", "spts_reduced_attention", "spts_prepared_bytes", "spts_prepare_layer")
+           "spts_debug_check_index_list", "spts_reduced_attention", "spts_prepared_bytes", "spts_prepare_layer",
+           "spts_w4_quantize", "spts_w4_gemv", "spts_kv4_append", "spts_kv4_attention", "spts_process_logits")
 
 OP_NAMES = {1: "prep", 2: "kproj_pap", 3: "pap_softmax", 4: "topk", 5: "kv_gather", 6: "qv_proj", 7: "attention",
             8: "o_proj", 9: "ltp", 10: "gate_up", 11: "down", 12: "compact", 13: "head", 14: "decode"}
@@ -124,6 +145,12 @@ def load_library() -> C.CDLL:
     lib.spts_profile_begin.argtypes = [vp, i32]
     lib.spts_profile_end.argtypes = [vp, C.POINTER(C.c_float), C.POINTER(C.c_int64), C.POINTER(C.c_double),
                                      C.POINTER(C.c_double)]
+    i64 = C.c_int64
+    lib.spts_w4_quantize.argtypes = [vp, vp, i32, i32, i32, vp, vp]
+    lib.spts_w4_gemv.argtypes = [vp, C.POINTER(W4C), C.POINTER(W4C), vp, i64, i32, vp, i64, u32, vp, i64]
+    lib.spts_kv4_append.argtypes = [vp, C.POINTER(Kv4CacheC), vp, i64, vp, i64, vp, vp, vp, i32, vp, vp]
+    lib.spts_kv4_attention.argtypes = [vp, C.POINTER(Kv4CacheC), vp, i64, vp, i64]
+    lib.spts_process_logits.argtypes = [vp, vp, i64, i32, i32, C.POINTER(LogitsRulesC), vp, i64, vp]
     for n in EXPORTS:
         if n not in ("spts_workspace_bytes", "spts_destroy", "spts_launch_count", "spts_proxy_scratch_bytes",
                      "spts_prepared_bytes"):
@@ -210,6 +237,117 @@ class KvCache:
             e.len = 0
 
 
+def _rows(t: torch.Tensor, width: int, dtype, what: str):
+    """Pointer and row stride of a [n, ...] tensor whose rows of `width` elements are contiguous (a view into wider
+    rows is fine)."""
+    if not t.is_cuda or t.dtype != dtype:
+        raise ValueError(f"{what}: a CUDA tensor of {dtype} is needed, got {t.dtype} on {t.device}")
+    if t.dim() < 2 or t[0:1].numel() != (width if t.shape[0] else 0):
+        raise ValueError(f"{what}: rows of {width} elements are needed, got {tuple(t.shape)}")
+    inner = 1
+    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if size != 1 and stride != inner:
+            raise ValueError(f"{what}: the elements of a row must be contiguous")
+        inner *= size
+    return C.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else width)
+
+
+def _vec(t: Optional[torch.Tensor], n: Optional[int], dtype, what: str, device=None):
+    if t is None:
+        return None
+    if not t.is_cuda or not t.is_contiguous() or t.dtype != dtype or (n is not None and t.numel() != n):
+        raise ValueError(f"{what}: a contiguous CUDA tensor of {dtype}" + (f" with {n} elements" if n is not None else "") + " is needed")
+    if device is not None and t.device != device:
+        raise ValueError(f"{what}: on {t.device}, the context is on {device}")
+    return C.c_void_p(t.data_ptr())
+
+
+class W4Weight:
+    """A weight matrix [out, in] in 4 bits: codes uint8 [out, in / 2], params bf16 [out, in / group, 2] = (scale, mid)."""
+
+    def __init__(self, codes: torch.Tensor, params: torch.Tensor):
+        if codes.dim() != 2 or params.dim() != 3 or params.shape[0] != codes.shape[0] or params.shape[2] != 2 or params.shape[1] < 1:
+            raise ValueError(f"codes [out, in / 2] and params [out, in / group, 2] are needed, got {tuple(codes.shape)}, {tuple(params.shape)}")
+        _vec(codes, None, torch.uint8, "codes")
+        _vec(params, None, torch.bfloat16, "params", codes.device)
+        self.codes, self.params = codes, params
+        self.out_features, self.in_features = codes.shape[0], 2 * codes.shape[1]
+        if self.in_features % params.shape[1] != 0:
+            raise ValueError("params do not divide the rows into equal groups")
+        self.group = self.in_features // params.shape[1]
+        self.c = W4C(codes.data_ptr(), params.data_ptr(), self.out_features, self.in_features, self.group)
+
+
+class Kv4Cache:
+    """One layer's 4-bit cache of n_seq sequences (layouts in include/spts.h).  `length` is a device int32 [n_seq]; the
+    capacity is rounded up to a multiple of 32.  Existing buffers can be handed in."""
+
+    def __init__(self, shape, n_seq: int, capacity: int, group: int = 64, device="cuda:0", k_codes=None, v_codes=None,
+                 k_params=None, v_params=None, length=None, pos=None, positions: bool = False):
+        cap = (capacity + 31) // 32 * 32
+        hkv, d = shape.n_kv_heads, shape.head_dim
+        if group not in (32, 64, 128) or group > d:
+            raise ValueError(f"groups of 32, 64 or 128 within {d} dims, got {group}")
+
+        def buf(t, size, dtype, what):
+            if t is None:
+                return torch.zeros(size, dtype=dtype, device=device)
+            _vec(t, None, dtype, what)
+            if tuple(t.shape) != size:
+                raise ValueError(f"{what}: {size} is needed, got {tuple(t.shape)}")
+            return t
+        self.k_codes = buf(k_codes, (n_seq, hkv, cap, d // 2), torch.uint8, "k_codes")
+        self.v_codes = buf(v_codes, (n_seq, hkv, cap, d // 2), torch.uint8, "v_codes")
+        self.k_params = buf(k_params, (n_seq, hkv, cap, d // group, 2), torch.bfloat16, "k_params")
+        self.v_params = buf(v_params, (n_seq, hkv, cap, d // group, 2), torch.bfloat16, "v_params")
+        self.length = buf(length, (n_seq,), torch.int32, "length")
+        self.pos = buf(pos, (n_seq, cap), torch.int32, "pos") if pos is not None or positions else None
+        for t in (self.v_codes, self.k_params, self.v_params, self.length) + ((self.pos,) if self.pos is not None else ()):
+            if t.device != self.k_codes.device:
+                raise ValueError("the buffers of a cache are on one device")
+        self.n_seq, self.capacity, self.group = n_seq, cap, group
+        self.c = Kv4CacheC(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_params.data_ptr(),
+                           self.v_params.data_ptr(), self.pos.data_ptr() if self.pos is not None else None,
+                           self.length.data_ptr(), n_seq, cap, group)
+
+
+class LogitsRules:
+    """The device lists of spts_logits_rules; every one is optional."""
+
+    def __init__(self, history=None, history_start=None, generated_start=None, repetition=None, presence=None, frequency=None,
+                 bias_token=None, bias_value=None, bias_start=None, mask=None):
+        i32, f32 = torch.int32, torch.float32
+        given = dict(history=(history, i32), history_start=(history_start, i32), generated_start=(generated_start, i32),
+                     repetition=(repetition, f32), presence=(presence, f32), frequency=(frequency, f32),
+                     bias_token=(bias_token, i32), bias_value=(bias_value, f32), bias_start=(bias_start, i32))
+        self.t = {}
+        for name, (t, dtype) in given.items():
+            _vec(t, None, dtype, name)
+            self.t[name] = t
+        if mask is not None and (mask.dim() != 2 or mask.dtype != i32 or not mask.is_cuda or mask.stride(1) != 1):
+            raise ValueError("mask: a CUDA int32 tensor [n, words] is needed")
+        if (history is None) != (history_start is None) or len({t is None for t in (bias_token, bias_value, bias_start)}) > 1:
+            raise ValueError("a history needs its history_start; biases need bias_token, bias_value and bias_start")
+        if bias_token is not None and bias_token.numel() != bias_value.numel():
+            raise ValueError("as many bias tokens as values are needed")
+        self.t["mask"] = mask
+        self.c = LogitsRulesC(*[self.t[n].data_ptr() if self.t[n] is not None else None for n in LOGITS_RULES],
+                              mask.stride(0) if mask is not None else 0, history.numel() if history is not None else 0,
+                              bias_token.numel() if bias_token is not None else 0)
+
+    def check(self, n: int, vocab: int, device):
+        for name, want in (("history_start", n + 1), ("generated_start", n), ("repetition", n), ("presence", n),
+                           ("frequency", n), ("bias_start", n + 1)):
+            if self.t[name] is not None and self.t[name].numel() != want:
+                raise ValueError(f"{name}: {want} entries are needed for {n} rows, got {self.t[name].numel()}")
+        m = self.t["mask"]
+        if m is not None and (m.shape[0] != n or m.shape[1] < (vocab + 31) // 32):
+            raise ValueError(f"mask: [{n}, {(vocab + 31) // 32}] words are needed, got {tuple(m.shape)}")
+        for name, t in self.t.items():
+            if t is not None and t.device != device:
+                raise ValueError(f"{name}: on {t.device}, the context is on {device}")
+
+
 class Spts:
     """One library context bound to a device and a stream."""
 
@@ -224,6 +362,7 @@ class Spts:
                               shape.ltp_dlow, shape.ltp_rank, shape.n_layers, shape.vocab, shape.rms_eps,
                               shape.rope_theta, SPTS_BF16 if shape.dtype == "bf16" else SPTS_FP32)
         torch.cuda.set_device(self.device)
+        self.k_device = torch.device("cuda", self.device.index if self.device.index is not None else torch.cuda.current_device())
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
         nbytes = self.lib.spts_workspace_bytes(C.byref(self.desc), max_seq)
         if nbytes == 0:
@@ -417,6 +556,100 @@ class Spts:
                     logits_out=None, token_out=None):
         self._check(self.lib.spts_decode_step(self.h, C.byref(model.c), cache.c, _ptr(x_in), token_in, pos,
                                               _ptr(x_out), _ptr(logits_out), _ptr(token_out)), "spts_decode_step")
+
+    # ------------------------------------------------------------------ generation with 4-bit weights and caches
+    def _here(self, *tensors):
+        for t in tensors:
+            if t is not None and t.device != self.k_device:
+                raise ValueError(f"a tensor on {t.device}, the context is on {self.k_device}")
+
+    def w4_quantize(self, W: torch.Tensor, group: int = 128) -> W4Weight:
+        """spts_w4_quantize: the 4-bit form of W [out, in] (storage type)."""
+        out, k = W.shape
+        if group not in (32, 64, 128) or k % group:
+            raise ValueError(f"groups of 32, 64 or 128 that divide {k} are needed, got {group}")
+        self._here(W)
+        codes = torch.empty(out, k // 2, dtype=torch.uint8, device=self.device)
+        params = torch.empty(out, k // group, 2, dtype=torch.bfloat16, device=self.device)
+        with torch.cuda.device(self.device):
+            self._check(self.lib.spts_w4_quantize(self.h, _vec(W, out * k, self.dtype, "W"), out, k, group, _ptr(codes), _ptr(params)),
+                        "spts_w4_quantize")
+        return W4Weight(codes, params)
+
+    def w4_gemv(self, w: W4Weight, X: torch.Tensor, w2: Optional[W4Weight] = None, norm: bool = False, residual=None,
+                fp32_out: bool = False, out=None):
+        """spts_w4_gemv: X [n, in] W^T for up to 32 tokens; w2: silu(X W^T) * (X W2^T); residual is added."""
+        n = X.shape[0]
+        odt = torch.float32 if fp32_out else self.dtype
+        if out is None:
+            out = torch.empty(n, w.out_features, dtype=odt, device=self.device)
+        self._here(X, residual, out, w.codes, w2.codes if w2 is not None else None)
+        xp, ldx = _rows(X, w.in_features, self.dtype, "X")
+        yp, ldy = _rows(out, w.out_features, odt, "out")
+        rp, ldr = (None, 0) if residual is None else _rows(residual, w.out_features, self.dtype, "residual")
+        if out.shape[0] != n or (residual is not None and residual.shape[0] != n):
+            raise ValueError("X, residual and out have the same number of rows")
+        with torch.cuda.device(self.device):
+            self._check(self.lib.spts_w4_gemv(self.h, C.byref(w.c), C.byref(w2.c) if w2 is not None else None, xp, ldx, n, rp,
+                                              ldr, (W4_NORM if norm else 0) | (W4_FP32_OUT if fp32_out else 0), yp, ldy),
+                        "spts_w4_gemv")
+        return out
+
+    def _kv4_shape(self, cache: Kv4Cache):
+        if tuple(cache.k_codes.shape[1::2]) != (self.shape.n_kv_heads, self.shape.head_dim // 2):
+            raise ValueError("the cache was made for other heads than this context's")
+        self._here(cache.k_codes)
+
+    def kv4_append(self, cache: Kv4Cache, K: torch.Tensor, V: torch.Tensor, pos=None, row_start=None, at=None, K_out=None,
+                   V_out=None):
+        """spts_kv4_append: rows of K, V [n, Hkv, d] (K after RoPE) into the cache; row_start [n_seq + 1] and at [n_seq]
+        are device int32.  K_out, V_out: the values that the cache then stands for."""
+        n, w = K.shape[0], self.shape.n_kv_heads * self.shape.head_dim
+        self._kv4_shape(cache)
+        self._here(K, V, pos, row_start, at, K_out, V_out)
+        if V.shape[0] != n:
+            raise ValueError("as many rows of V as of K are needed")
+        kp, ldk = _rows(K, w, self.dtype, "K")
+        vp, ldv = _rows(V, w, self.dtype, "V")
+        with torch.cuda.device(self.device):
+            self._check(self.lib.spts_kv4_append(self.h, C.byref(cache.c), kp, ldk, vp, ldv, _vec(pos, n, torch.int32, "pos"),
+                                                 _vec(row_start, cache.n_seq + 1, torch.int32, "row_start"),
+                                                 _vec(at, cache.n_seq, torch.int32, "at"), n, _vec(K_out, n * w, self.dtype, "K_out"),
+                                                 _vec(V_out, n * w, self.dtype, "V_out")), "spts_kv4_append")
+
+    def kv4_attention(self, cache: Kv4Cache, Q: torch.Tensor, O_out=None):
+        """spts_kv4_attention: one query per sequence, Q [n_seq, H, d] (or [n_seq, H * d]) -> [n_seq, H * d]."""
+        w = self.shape.n_q_heads * self.shape.head_dim
+        self._kv4_shape(cache)
+        if O_out is None:
+            O_out = torch.empty(cache.n_seq, w, dtype=self.dtype, device=self.device)
+        self._here(Q, O_out)
+        if Q.shape[0] != cache.n_seq or O_out.shape[0] != cache.n_seq:
+            raise ValueError(f"one query per sequence of the cache: {cache.n_seq} rows are needed")
+        qp, ldq = _rows(Q, w, self.dtype, "Q")
+        op, ldo = _rows(O_out, w, self.dtype, "O_out")
+        with torch.cuda.device(self.device):
+            self._check(self.lib.spts_kv4_attention(self.h, C.byref(cache.c), qp, ldq, op, ldo), "spts_kv4_attention")
+        return O_out
+
+    def process_logits(self, logits: torch.Tensor, rules: LogitsRules, out=None, token_out=None, want_logits: bool = True):
+        """spts_process_logits: (logits under the rules, token).  out may be the logits themselves; with
+        want_logits=False only the token is computed."""
+        n, v = logits.shape
+        rules.check(n, v, self.k_device)
+        if out is None and want_logits:
+            out = torch.empty(n, v, dtype=torch.float32, device=self.device)
+        if token_out is None:
+            token_out = torch.empty(n, dtype=torch.int32, device=self.device)
+        self._here(logits, out, token_out)
+        lp, ld = _rows(logits, v, torch.float32, "logits")
+        op, ldo = (None, 0) if out is None else _rows(out, v, torch.float32, "out")
+        if out is not None and out.shape[0] != n:
+            raise ValueError("as many rows of out as of logits are needed")
+        with torch.cuda.device(self.device):
+            self._check(self.lib.spts_process_logits(self.h, lp, ld, n, v, C.byref(rules.c), op, ldo,
+                                                     _vec(token_out, n, torch.int32, "token_out")), "spts_process_logits")
+        return out, token_out
 
 
 class Model:

@@ -1,0 +1,91 @@
+// 4-bit groups: value = scale * (code - 8) + mid, bf16 (scale, mid) per 32, 64 or 128 elements (include/spts.h has the
+// quantiser's definition).  Shared by the weight and the KV-cache kernels.
+#pragma once
+
+#include "spts_common.cuh"
+
+namespace spts {
+namespace q4 {
+
+__device__ __forceinline__ float lo_bf16(uint32_t w) { return __uint_as_float(w << 16); }            // scale of a params word
+__device__ __forceinline__ float hi_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }    // mid
+
+__device__ __forceinline__ void load8(const float* p, float* x) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+__device__ __forceinline__ void load8(const bf16* p, float* x) {
+  const uint4 v = *reinterpret_cast<const uint4*>(p);
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[2 * i] = lo_bf16(w[i]); x[2 * i + 1] = hi_bf16(w[i]); }
+}
+__device__ __forceinline__ void store8(float* p, const float* x) {
+  *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+  *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+}
+__device__ __forceinline__ void store8(bf16* p, const float* x) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+    w[i] = *reinterpret_cast<const uint32_t*>(&v);
+  }
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Quantises the eight elements of this lane; the group is `lanes` (4, 8 or 16) neighbouring lanes of the warp, aligned
+// to their number, and every lane of the warp calls.  Returns the eight codes, element i in bits 4i .. 4i + 3; `params`
+// = scale | mid << 16; read (if not null) the values that the codes stand for.
+// The code is the exact quotient's rounding: the fp32 quotient is off by less than 3 * 2^-24 * 9 = 1.7e-6 steps (three
+// roundings, at most nine steps from the middle), so wherever it lies farther than 1e-5 from a border it gives the exact
+// quotient's code, and the rest (about one in 50,000 of smooth data) is divided in 64 bits.
+__device__ __forceinline__ uint32_t quantize8(const float* x, int lanes, uint32_t& params, float* read, bool& nonfinite) {
+  float hi = x[0], lo = x[0];
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    hi = fmaxf(hi, x[i]); lo = fminf(lo, x[i]);
+    bad = bad || !(fabsf(x[i]) <= 3.402823466e38f);
+  }
+  for (int o = 1; o < lanes; o <<= 1) {
+    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+  }
+  const uint32_t votes = __ballot_sync(0xffffffffu, bad);
+  const int lane = threadIdx.x & 31;
+  const uint32_t mine = ((1u << lanes) - 1u) << (lane & ~(lanes - 1));
+  nonfinite = (votes & mine) != 0;
+  if (nonfinite) {
+    params = 0x7FC00000u;                       // scale 0, mid NaN
+    if (read)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) read[i] = __uint_as_float(0x7FC00000u);
+    return 0x88888888u;
+  }
+  const double dh = (double)hi, dl = (double)lo;
+  const bf16 sb = __float2bfloat16_rn((float)((dh - dl) / 15.0));
+  const float s = __bfloat162float(sb);
+  const bf16 mb = __float2bfloat16_rn((float)(0.5 * (dh + dl) + 0.5 * (double)s));
+  const float m = __bfloat162float(mb);
+  params = (uint32_t)__bfloat16_as_ushort(sb) | ((uint32_t)__bfloat16_as_ushort(mb) << 16);
+  uint32_t word = 0;
+  const bool tiny = s < 1e-30f;                 // 1 / s would overflow
+  const float inv = tiny ? 0.f : 1.0f / s;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float t = (x[i] - m) * inv;
+    float r = rintf(t);
+    if (tiny || fabsf(fabsf(t - r) - 0.5f) < 1e-5f) {
+      if (s == 0.f) r = 0.f;
+      else r = (float)fmin(8.0, fmax(-9.0, rint(((double)x[i] - (double)m) / (double)s)));
+    }
+    const int c = (int)fminf(7.f, fmaxf(-8.f, r));
+    word |= (uint32_t)(c + 8) << (4 * i);
+    if (read) read[i] = fmaf(s, (float)c, m);
+  }
+  return word;
+}
+
+}  // namespace q4
+}  // namespace spts

@@ -1109,4 +1109,117 @@ spts_status spts_decode_step(spts_ctx* ctx, const spts_model_weights* mw, spts_k
   return SPTS_OK;
 }
 
+// ---- generation with 4-bit weights and caches
+namespace {
+bool group_ok(int group) { return group == 32 || group == 64 || group == 128; }
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
+// rows of 16-byte loads: aligned base, stride a multiple of 16 bytes where there is more than one row
+bool rows_ok(const void* p, int64_t ld, int64_t width, int64_t n, size_t es) {
+  return aligned16(p) && (n < 2 || (ld >= width && (ld * (int64_t)es) % 16 == 0));
+}
+spts_status check_w4(const spts_w4* w) {
+  if (w->codes == nullptr || w->params == nullptr || !aligned16(w->codes) || !aligned4(w->params)) return SPTS_ERR_INVALID_ARG;
+  if (!group_ok(w->group) || w->out_features < 1 || w->in_features < 1 || w->in_features % w->group != 0) return SPTS_ERR_SHAPE;
+  return SPTS_OK;
+}
+spts_status check_kv4(const spts_ctx* ctx, const spts_kv4_cache* c) {
+  if (c == nullptr) return SPTS_ERR_INVALID_ARG;
+  if (c->n_seq < 0 || c->n_seq > SPTS_KV4_MAX_SEQ || c->capacity < 32 || c->capacity % 32 != 0 || !group_ok(c->group) ||
+      c->group > ctx->desc.head_dim)
+    return SPTS_ERR_SHAPE;
+  if (c->n_seq == 0) return SPTS_OK;
+  if (c->k_codes == nullptr || c->v_codes == nullptr || c->k_params == nullptr || c->v_params == nullptr || c->len == nullptr)
+    return SPTS_ERR_INVALID_ARG;
+  if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || !aligned16(c->k_params) || !aligned16(c->v_params))
+    return SPTS_ERR_INVALID_ARG;
+  return SPTS_OK;
+}
+}  // namespace
+
+spts_status spts_w4_quantize(spts_ctx* ctx, const void* W, int out_features, int in_features, int group, void* codes, void* params) {
+  TRY(check_ctx(ctx));
+  if (W == nullptr || codes == nullptr || params == nullptr) return SPTS_ERR_INVALID_ARG;
+  if (!group_ok(group) || out_features < 1 || in_features < 1 || in_features % group != 0) return SPTS_ERR_SHAPE;
+  if (!aligned16(W) || !aligned16(codes) || !aligned4(params)) return SPTS_ERR_INVALID_ARG;
+  return launch_w4_quantize(ctx, W, out_features, in_features, group, codes, params);
+}
+
+spts_status spts_w4_gemv(spts_ctx* ctx, const spts_w4* w, const spts_w4* w2, const void* X, int64_t ldx, int n,
+                         const void* residual, int64_t ldr, uint32_t flags, void* Y, int64_t ldy) {
+  TRY(check_ctx(ctx));
+  if (w == nullptr || (flags & ~(uint32_t)(SPTS_W4_NORM | SPTS_W4_FP32_OUT)) != 0) return SPTS_ERR_INVALID_ARG;
+  TRY(check_w4(w));
+  if (w2 != nullptr) {
+    TRY(check_w4(w2));
+    if (w2->out_features != w->out_features || w2->in_features != w->in_features || w2->group != w->group) return SPTS_ERR_SHAPE;
+  }
+  if (residual != nullptr && (w2 != nullptr || (flags & SPTS_W4_FP32_OUT))) return SPTS_ERR_INVALID_ARG;
+  if (n < 0 || n > SPTS_W4_MAX_N) return SPTS_ERR_SHAPE;
+  if (n == 0) return SPTS_OK;
+  if (X == nullptr || Y == nullptr) return SPTS_ERR_INVALID_ARG;
+  if (!rows_ok(X, ldx, w->in_features, n, elt_size(ctx->desc))) return SPTS_ERR_INVALID_ARG;
+  if (n > 1 && (ldy < w->out_features || (residual != nullptr && ldr < w->out_features))) return SPTS_ERR_INVALID_ARG;
+  if (Y == X || (residual == Y && ldr != ldy && n > 1)) return SPTS_ERR_INVALID_ARG;
+  W4GemvArgs a;
+  memset(&a, 0, sizeof(a));
+  a.codes = w->codes; a.params = w->params;
+  if (w2 != nullptr) { a.codes2 = w2->codes; a.params2 = w2->params; }
+  a.out = w->out_features; a.in = w->in_features; a.group = w->group;
+  a.X = X; a.ldx = ldx; a.n = n; a.residual = residual; a.ldr = ldr;
+  a.norm = (flags & SPTS_W4_NORM) != 0; a.fp32_out = (flags & SPTS_W4_FP32_OUT) != 0;
+  a.Y = Y; a.ldy = ldy;
+  return launch_w4_gemv(ctx, a);
+}
+
+spts_status spts_kv4_append(spts_ctx* ctx, const spts_kv4_cache* cache, const void* K, int64_t ldk, const void* V,
+                            int64_t ldv, const int32_t* pos, const int32_t* row_start, const int32_t* at, int n_rows,
+                            void* K_read, void* V_read) {
+  TRY(check_ctx(ctx));
+  TRY(check_kv4(ctx, cache));
+  if (n_rows < 0) return SPTS_ERR_INVALID_ARG;
+  if (cache->n_seq == 0) return n_rows == 0 || row_start != nullptr ? SPTS_OK : SPTS_ERR_INVALID_ARG;
+  if (row_start == nullptr && n_rows != cache->n_seq) return SPTS_ERR_INVALID_ARG;
+  const int64_t width = (int64_t)ctx->desc.n_kv_heads * ctx->desc.head_dim;
+  const size_t es = elt_size(ctx->desc);
+  if (n_rows > 0) {
+    if (K == nullptr || V == nullptr) return SPTS_ERR_INVALID_ARG;
+    if (!rows_ok(K, ldk, width, n_rows, es) || !rows_ok(V, ldv, width, n_rows, es)) return SPTS_ERR_INVALID_ARG;
+    if (!aligned16(K_read) || !aligned16(V_read) || (K_read != nullptr && K_read == V_read)) return SPTS_ERR_INVALID_ARG;
+  }
+  if (at == cache->len) at = nullptr;
+  return launch_kv4_append(ctx, cache, K, ldk, V, ldv, pos, row_start, at, n_rows, K_read, V_read);
+}
+
+spts_status spts_kv4_attention(spts_ctx* ctx, const spts_kv4_cache* cache, const void* Q, int64_t ldq, void* O_out, int64_t ldo) {
+  TRY(check_ctx(ctx));
+  TRY(check_kv4(ctx, cache));
+  if (cache->n_seq == 0) return SPTS_OK;
+  if (Q == nullptr || O_out == nullptr || Q == O_out) return SPTS_ERR_INVALID_ARG;
+  const int64_t width = (int64_t)ctx->desc.n_q_heads * ctx->desc.head_dim;
+  const size_t es = elt_size(ctx->desc);
+  if (!rows_ok(Q, ldq, width, cache->n_seq, es) || !rows_ok(O_out, ldo, width, cache->n_seq, es)) return SPTS_ERR_INVALID_ARG;
+  return launch_kv4_attention(ctx, cache, Q, ldq, O_out, ldo);
+}
+
+spts_status spts_process_logits(spts_ctx* ctx, const float* logits, int64_t ld, int n, int vocab, const spts_logits_rules* rules,
+                                float* out, int64_t ldo, int32_t* token_out) {
+  TRY(check_ctx(ctx));
+  if (rules == nullptr || n < 0) return SPTS_ERR_INVALID_ARG;
+  if (vocab < 1 || n > 65535) return SPTS_ERR_SHAPE;
+  if (n == 0) return SPTS_OK;
+  if (out == nullptr && token_out == nullptr) return SPTS_ERR_INVALID_ARG;
+  if (logits == nullptr || !aligned4(logits) || !aligned4(out)) return SPTS_ERR_INVALID_ARG;
+  if (n > 1 && (ld < vocab || (out != nullptr && ldo < vocab))) return SPTS_ERR_INVALID_ARG;
+  if (out == logits && n > 1 && ld != ldo) return SPTS_ERR_INVALID_ARG;
+  spts_logits_rules r = *rules;
+  if (r.n_history < 0 || r.n_bias < 0) return SPTS_ERR_INVALID_ARG;
+  if (r.history != nullptr && r.history_start == nullptr) return SPTS_ERR_INVALID_ARG;
+  if (r.bias_token != nullptr && (r.bias_value == nullptr || r.bias_start == nullptr)) return SPTS_ERR_INVALID_ARG;
+  if (r.mask != nullptr && n > 1 && r.ld_mask < (vocab + 31) / 32) return SPTS_ERR_INVALID_ARG;
+  if (r.repetition == nullptr && r.presence == nullptr && r.frequency == nullptr) r.history = nullptr;   // nothing to count for
+  if (r.n_history == 0) r.history = nullptr;
+  if (r.n_bias == 0) r.bias_token = nullptr;
+  return launch_process_logits(ctx, logits, ld, n, vocab, r, out, ldo, token_out);
+}
+
 }  // extern "C"

@@ -247,6 +247,24 @@ spts_status launch_tc_attention_packed(spts_ctx* ctx, const bf16* Q, const bf16*
 spts_status tc_init(spts_ctx* ctx);          // resolves the tensor-map encoder, sets kernel attributes
 int tc_sumsq_parts(int n_out);               // partial sums per row written by TC_SUMSQ
 
+// ---- kernels_w4.cu, kernels_kv4.cu, kernels_logits.cu : generation with 4-bit weights and caches
+struct W4GemvArgs {
+  const void* codes; const void* params; const void* codes2; const void* params2;   // [out, in / 2], [out, in / group, 2]
+  int out, in, group;
+  const void* X; int64_t ldx; int n;
+  const void* residual; int64_t ldr;
+  int norm, fp32_out;
+  void* Y; int64_t ldy;
+};
+spts_status launch_w4_gemv(spts_ctx* ctx, const W4GemvArgs& a);
+spts_status launch_w4_quantize(spts_ctx* ctx, const void* W, int out, int in, int group, void* codes, void* params);
+spts_status launch_kv4_append(spts_ctx* ctx, const spts_kv4_cache* cache, const void* K, int64_t ldk, const void* V,
+                              int64_t ldv, const int32_t* pos, const int32_t* row_start, const int32_t* at, int n_rows,
+                              void* K_read, void* V_read);
+spts_status launch_kv4_attention(spts_ctx* ctx, const spts_kv4_cache* cache, const void* Q, int64_t ldq, void* O, int64_t ldo);
+spts_status launch_process_logits(spts_ctx* ctx, const float* logits, int64_t ld, int n, int vocab,
+                                  const spts_logits_rules& rules, float* out, int64_t ldo, int32_t* token);
+
 // Programmatic dependent launch for chains of short kernels (the decode step, the passes of a top-k): a kernel
 // lets its successor start early (dep_launch), does whatever does not depend on its predecessor (prefetching
 // weights, loading keys) and only then waits for the predecessor's results (dep_wait = predecessor complete,
