@@ -1,5 +1,7 @@
 // The 4-bit KV cache: rows are quantised into it (kv4_append_kernel) and single tokens attend to it.
 //
+// kv4_attn_kernel (bf16): one persistent CTA per SM, its warps streaming 16-row steps of the cache through shared memory
+// into warp-level matrix instructions; see there.
 // kv4_attn_plain_kernel: one CTA per query head and sequence, CUDA cores, fp32 arithmetic, online softmax per warp.
 // fp32 storage and SPTS_REFERENCE_KERNELS.
 #include "q4_common.cuh"
@@ -159,6 +161,505 @@ kv4_attn_plain_kernel(Kv4Dev c, const T* __restrict__ Q, int64_t ldq, int H, T* 
   }
 }
 
+// ---------------------------------------------------------------------------------------------------------------------
+// Attention of single tokens on matrix instructions (m16n8k16, fp32 accumulation).
+//
+// A warp takes 16 cached rows of one KV head at a time and all query heads that read it (up to 8 NB):
+//   S[row, q] = K Q^T    M = 16 rows, N = queries, K = dims        O[dim, q] += V^T P    M = 16 dims, N = queries, K = 16 rows
+// so that the codes are always the A operand and no lane is spent on absent queries beyond eight.
+// Codes become bf16 without arithmetic: code << 3 in the mantissa of 16.0 is exactly 16 + code, one shift and one logic
+// operation per two codes (the storage orders put the two codes of a register 16 bits apart).  Scales and mids stay in fp32:
+//   S = sum_groups scale_g (sum_i (16 + c_i) q_i) + sum_g (mid_g - 24 scale_g) (sum_i q_i)
+// where the second sum is one more matrix step whose A registers are the params words as they lie in memory, and whose B
+// holds -24 sum q and sum q in two bf16 pieces each (16 bits; the term is off by 2^-17 relative).
+//   O = sum_rows (16 + c) p'_g - 24 sum_rows p'_g + sum_rows p mid_g,   p'_g = bf16(p scale_g), p in the last sum bf16(p)
+// (both roundings half a bf16 step, like the rounding of p in the bf16 kernels); the -24 multiplies the rounded p' by a
+// matrix step with a constant A, so the bias cancels exactly up to fp32 sums.  P changes from the accumulator's layout to
+// the B operand's by 8 x 8 transposes between lanes.
+// The running maximum is a reference, not the maximum: it moves only when a score exceeds it by 2^10 (weights are then at
+// most 1024, far inside bf16 and fp32), which after the first rows is rare, so the steps carry no reduction.
+//
+// Work split: the 16-row steps of all (sequence, KV head) units form one line that is cut into equal pieces, one per CTA
+// (persistent, one per SM), and a CTA deals its steps to its warps.  A unit that lies in one CTA is finished there; a unit
+// cut between CTAs leaves one partial result (maximum, sum, O) per CTA, and the CTA that arrives last adds them in the
+// order of the CTAs, so results do not depend on the order of arrival.  One launch, lengths read on the device.
+constexpr float KV4_LOG2E = 1.4426950408889634f;
+constexpr float KV4_SLACK = 10.0f;
+
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ float round_bf16(float v) { return __bfloat162float(__float2bfloat16_rn(v)); }
+// (16 + code j, 16 + code j + 4) of a word of eight codes / of two rows' halfwords
+template <int J> __device__ __forceinline__ uint32_t codes2(uint32_t w) {
+  const uint32_t s = J == 0 ? w << 3 : w >> (4 * J - 3);
+  return (s & 0x00780078u) | 0x41804180u;
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+template <int D, int NG, int NB>
+struct Kv4Tile {
+  static constexpr int WARPS = NB == 1 ? 16 : 8;
+  static constexpr int NQ = 8 * NB;
+  static constexpr int STAGES = 3;
+  // one step of 16 rows in shared memory; the rows of V are 16 bytes apart so that a fragment's four rows lie in distinct banks
+  static constexpr int KC = 0, VC = KC + 16 * (D / 2), VSTRIDE = D / 2 + 16, KP = VC + 16 * VSTRIDE, VP = KP + 16 * NG * 4;
+  static constexpr int STAGE_BYTES = VP + 16 * NG * 4;
+  static constexpr int RING_BYTES = WARPS * STAGES * STAGE_BYTES;
+  static constexpr int OSTRIDE = D + 4;            // floats between the queries of a warp's partial O
+  static constexpr int O_BYTES = WARPS * NQ * OSTRIDE * 4;
+  static constexpr int SMEM = RING_BYTES + O_BYTES;
+};
+
+// A position on the line of steps: sequence b, head unit h, step s of n.  Units are ordered by sequence, then head.
+struct Kv4Unit { int b, h, n; };
+struct Kv4Line {
+  const int* pre;        // [n_seq + 1] steps of one head before each sequence (shared memory)
+  int n_seq, heads;      // head units per sequence
+  __device__ __forceinline__ Kv4Unit find(long x, int& s) const {
+    int lo = 0, hi = n_seq;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if ((long)pre[mid] * heads <= x) lo = mid; else hi = mid;
+    }
+    Kv4Unit u;
+    u.b = lo;
+    u.n = pre[lo + 1] - pre[lo];
+    const long r = x - (long)pre[lo] * heads;
+    u.h = (int)(r / u.n);
+    s = (int)(r - (long)u.h * u.n);
+    return u;
+  }
+  __device__ __forceinline__ Kv4Unit next(Kv4Unit u) const {     // only called while steps are left
+    if (++u.h < heads) return u;
+    u.h = 0;
+    do { ++u.b; u.n = pre[u.b + 1] - pre[u.b]; } while (u.n == 0);
+    return u;
+  }
+};
+
+// The steps of one warp within its CTA's piece of the line: every WARPS-th step of each unit's stretch.
+struct Kv4Walk {
+  Kv4Unit u;
+  int s, end;            // the warp's step, and the end of the stretch in this unit
+  long left;             // steps of the piece behind this stretch
+  __device__ __forceinline__ bool more(const Kv4Line& line, int warp) {      // settles on the next step; false: none left
+    while (s >= end) {
+      if (left == 0) return false;
+      u = line.next(u);
+      end = (int)min((long)u.n, left);
+      left -= end;
+      s = warp;
+    }
+    return true;
+  }
+};
+
+template <int D, int NG, int NB>
+__global__ void __launch_bounds__(Kv4Tile<D, NG, NB>::WARPS * 32, 1)
+kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qblocks, bf16* __restrict__ O, int64_t ldo,
+                float* __restrict__ part, int* __restrict__ arrived) {
+  using T = Kv4Tile<D, NG, NB>;
+  constexpr int WARPS = T::WARPS, NQ = T::NQ, NT = D / 32;
+  constexpr int GT = NT / NG;                      // 32-dim blocks of a group
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ int pre[SPTS_KV4_MAX_SEQ + 1];
+  __shared__ int warp_sums[32];
+  __shared__ float sm_m[WARPS][NQ], sm_l[WARPS][NQ], sm_f[WARPS][NQ], sm_L[NQ], sm_M[NQ];
+  __shared__ int last_flag;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, cc = lane & 3;
+  const int G = H / c.Hkv, heads = c.Hkv * qblocks, per_block = NB == 1 ? G : 16;
+
+  // ---- the line of steps
+  auto steps_of = [&](int b) { return b < c.n_seq ? (max(0, min(__ldg(&c.len[b]), c.capacity)) + 15) >> 4 : 0; };
+  {
+    int carry = 0;
+    if (tid == 0) pre[0] = 0;
+    for (int b0 = 0; b0 < c.n_seq; b0 += WARPS * 32) {
+      int v = steps_of(b0 + tid);
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += up;
+      }
+      if (lane == 31) warp_sums[warp] = v;
+      __syncthreads();
+      int before = carry, all = carry;
+      for (int w = 0; w < WARPS; ++w) { if (w < warp) before += warp_sums[w]; all += warp_sums[w]; }
+      if (b0 + tid < c.n_seq) pre[b0 + tid + 1] = before + v;
+      carry = all;
+      __syncthreads();
+    }
+  }
+  const Kv4Line line{pre, c.n_seq, heads};
+  const long total = (long)pre[c.n_seq] * heads;
+  const long ctas = max(1L, min((long)gridDim.x, (total + WARPS - 1) / WARPS));
+  // sequences without rows
+  for (int b = blockIdx.x; b < c.n_seq; b += gridDim.x)
+    if (pre[b + 1] == pre[b])
+      for (int i = tid; i < H * D; i += WARPS * 32) O[(size_t)b * ldo + i] = __float2bfloat16_rn(0.f);
+  if (total == 0 || blockIdx.x >= ctas) return;
+  const long x0 = total * blockIdx.x / ctas, x1 = total * (blockIdx.x + 1) / ctas;
+
+  unsigned char* ring = smem + warp * (T::STAGES * T::STAGE_BYTES);
+  const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
+  float* sm_o = reinterpret_cast<float*>(smem + T::RING_BYTES);
+  auto fetch = [&](const Kv4Walk& w, int stage) {
+    const int kvh = w.u.h / qblocks;
+    const size_t row = ((size_t)w.u.b * c.Hkv + kvh) * c.capacity + 16 * (size_t)w.s;
+    const uint32_t dst = ring_s + stage * T::STAGE_BYTES;
+    const char* kc = c.k_codes + row * (D / 2);
+    const char* vc = c.v_codes + row * (D / 2);
+#pragma unroll
+    for (int i = lane; i < D / 2; i += 32) {       // 16 rows x D / 32 pieces of 16 bytes
+      cp_async16(dst + T::KC + 16 * i, kc + 16 * i);
+      cp_async16(dst + T::VC + (i / (D / 32)) * T::VSTRIDE + (i % (D / 32)) * 16, vc + 16 * i);
+    }
+    if (lane < 8 * NG) {
+      const int i = lane < 4 * NG ? lane : lane - 4 * NG;
+      const uint32_t* p = (lane < 4 * NG ? c.k_params : c.v_params) + row * NG + 4 * i;
+      cp_async16(dst + (lane < 4 * NG ? T::KP : T::VP) + 16 * i, p);
+    }
+  };
+
+  Kv4Walk ahead, now;
+  {
+    int s;
+    now.u = line.find(x0, s);
+    now.end = (int)min((long)now.u.n, (long)s + (x1 - x0));
+    now.left = (x1 - x0) - (now.end - s);
+    now.s = s + warp;
+    ahead = now;
+  }
+  int first_s;                                     // the stretch of the current unit begins here
+  line.find(x0, first_s);
+  int fetch_stage = 0, use_stage = 0;
+  bool fetching = ahead.more(line, warp);
+#pragma unroll
+  for (int i = 0; i < T::STAGES - 1; ++i) {
+    if (fetching) {
+      fetch(ahead, fetch_stage);
+      ahead.s += WARPS;
+      fetching = ahead.more(line, warp);
+    }
+    cp_async_commit();
+    fetch_stage = fetch_stage + 1 == T::STAGES ? 0 : fetch_stage + 1;
+  }
+
+  const float sl = rsqrtf((float)D) * KV4_LOG2E;
+  while (true) {
+    // ---- one unit's stretch [first_s, now.end)
+    const Kv4Unit u = now.u;
+    const int b = u.b, kvh = u.h / qblocks, hb = kvh * G + (u.h % qblocks) * per_block;
+    const int nq = min(per_block, G - (u.h % qblocks) * per_block);
+    const int len = max(0, min(__ldg(&c.len[b]), c.capacity));
+    const int end = now.end;
+    // Q as B fragments, and (-24 sum q, sum q) of every group in two bf16 pieces
+    uint32_t qf[NB][NT][4], qm[NB][2];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      float sums[NG];
+#pragma unroll
+      for (int i = 0; i < NG; ++i) sums[i] = 0.f;
+      const int qi = 8 * nb + g;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (qi < nq) load8(Q + (size_t)b * ldq + (size_t)(hb + qi) * D + 32 * t + 8 * cc, x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) qf[nb][t][j] = pack2(x[j], x[j + 4]);
+        float s8 = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+        s8 += __shfl_xor_sync(0xffffffffu, s8, 1);
+        s8 += __shfl_xor_sync(0xffffffffu, s8, 2);
+        sums[t / GT] += s8;
+      }
+      float mine = 0.f;
+#pragma unroll
+      for (int i = 0; i < NG; ++i) if (cc == i) mine = sums[i];
+      const float a = -24.f * mine, ah = round_bf16(a), mh = round_bf16(mine);
+      qm[nb][0] = pack2(ah, mh);
+      qm[nb][1] = pack2(a - ah, mine - mh);
+    }
+    float o[NB][NT][2][4], oz[NB][NG][4], om[NB][4], m[NB][2], l[NB][2];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        om[nb][i] = 0.f;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) { o[nb][t][0][i] = 0.f; o[nb][t][1][i] = 0.f; }
+#pragma unroll
+        for (int t = 0; t < NG; ++t) oz[nb][t][i] = 0.f;
+      }
+      m[nb][0] = m[nb][1] = -INFINITY;
+      l[nb][0] = l[nb][1] = 0.f;
+    }
+    for (; now.s < end; now.s += WARPS) {
+      if (fetching) {
+        fetch(ahead, fetch_stage);
+        ahead.s += WARPS;
+        fetching = ahead.more(line, warp);
+      }
+      cp_async_commit();
+      fetch_stage = fetch_stage + 1 == T::STAGES ? 0 : fetch_stage + 1;
+      cp_async_wait<T::STAGES - 1>();
+      __syncwarp();
+      unsigned char* st = ring + use_stage * T::STAGE_BYTES;
+      use_stage = use_stage + 1 == T::STAGES ? 0 : use_stage + 1;
+      const int valid = len - 16 * now.s;          // rows of this step that are held
+      if (valid < 16) {
+        // what lies behind the last row may be anything: its params become zero (its codes are finite whatever they are)
+        for (int i = valid * NG + lane; i < 16 * NG; i += 32) {
+          reinterpret_cast<uint32_t*>(st + T::KP)[i] = 0u;
+          reinterpret_cast<uint32_t*>(st + T::VP)[i] = 0u;
+        }
+        __syncwarp();
+      }
+      // ---- S
+      uint32_t kw0[NT], kw1[NT];
+      if (NT == 4) {
+        *reinterpret_cast<uint4*>(kw0) = *reinterpret_cast<const uint4*>(st + T::KC + g * (D / 2) + cc * 16);
+        *reinterpret_cast<uint4*>(kw1) = *reinterpret_cast<const uint4*>(st + T::KC + (g + 8) * (D / 2) + cc * 16);
+      } else {
+        *reinterpret_cast<uint2*>(kw0) = *reinterpret_cast<const uint2*>(st + T::KC + g * (D / 2) + cc * 8);
+        *reinterpret_cast<uint2*>(kw1) = *reinterpret_cast<const uint2*>(st + T::KC + (g + 8) * (D / 2) + cc * 8);
+      }
+      float sc[NB][4];
+      const uint32_t* kp0 = reinterpret_cast<const uint32_t*>(st + T::KP) + g * NG;
+      const uint32_t* kp1 = kp0 + 8 * NG;
+      const uint32_t pw0 = cc < NG ? kp0[cc < NG ? cc : 0] : 0u, pw1 = cc < NG ? kp1[cc < NG ? cc : 0] : 0u;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[nb][i] = 0.f;
+        mma16816(sc[nb], pw0, pw1, pw0, pw1, qm[nb][0], qm[nb][1]);
+      }
+#pragma unroll
+      for (int gr = 0; gr < NG; ++gr) {
+        float acc[NB][4];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[nb][i] = 0.f;
+#pragma unroll
+        for (int tt = 0; tt < GT; ++tt) {
+          const int t = gr * GT + tt;
+          const uint32_t a0 = codes2<0>(kw0[t]), a1 = codes2<0>(kw1[t]), a2 = codes2<1>(kw0[t]), a3 = codes2<1>(kw1[t]);
+          const uint32_t b0 = codes2<2>(kw0[t]), b1 = codes2<2>(kw1[t]), b2 = codes2<3>(kw0[t]), b3 = codes2<3>(kw1[t]);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            mma16816(acc[nb], a0, a1, a2, a3, qf[nb][t][0], qf[nb][t][1]);
+            mma16816(acc[nb], b0, b1, b2, b3, qf[nb][t][2], qf[nb][t][3]);
+          }
+        }
+        const float s0 = lo_bf16(kp0[gr]), s1 = lo_bf16(kp1[gr]);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          sc[nb][0] = fmaf(s0, acc[nb][0], sc[nb][0]); sc[nb][1] = fmaf(s0, acc[nb][1], sc[nb][1]);
+          sc[nb][2] = fmaf(s1, acc[nb][2], sc[nb][2]); sc[nb][3] = fmaf(s1, acc[nb][3], sc[nb][3]);
+        }
+      }
+      // ---- weights (in powers of two)
+      if (valid < 16) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          if (g >= valid) { sc[nb][0] = -INFINITY; sc[nb][1] = -INFINITY; }
+          if (g + 8 >= valid) { sc[nb][2] = -INFINITY; sc[nb][3] = -INFINITY; }
+        }
+      }
+      bool over = false;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          sc[nb][i] *= sl; sc[nb][2 + i] *= sl;
+          over = over || fmaxf(sc[nb][i], sc[nb][2 + i]) > m[nb][i] + KV4_SLACK;
+        }
+      if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            float x = fmaxf(sc[nb][i], sc[nb][2 + i]);
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+            const float mn = fmaxf(m[nb][i], x);
+            const float f = m[nb][i] == mn ? 1.f : exp2f(m[nb][i] - mn);
+            m[nb][i] = mn;
+            l[nb][i] *= f;
+            om[nb][i] *= f; om[nb][2 + i] *= f;
+#pragma unroll
+            for (int t = 0; t < NG; ++t) { oz[nb][t][i] *= f; oz[nb][t][2 + i] *= f; }
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int j = 0; j < 2; ++j) { o[nb][t][j][i] *= f; o[nb][t][j][2 + i] *= f; }
+          }
+      }
+      const uint32_t* vp0 = reinterpret_cast<const uint32_t*>(st + T::VP) + g * NG;
+      const uint32_t* vp1 = vp0 + 8 * NG;
+      uint32_t pb[NB][NG][2], pu[NB][2];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = exp2f(sc[nb][i] - m[nb][i & 1]);
+        l[nb][0] += p[0] + p[2];
+        l[nb][1] += p[1] + p[3];
+        pu[nb][0] = transpose8x8(pack2(p[0], p[1]));
+        pu[nb][1] = transpose8x8(pack2(p[2], p[3]));
+#pragma unroll
+        for (int gr = 0; gr < NG; ++gr) {
+          const float s0 = lo_bf16(vp0[gr]), s1 = lo_bf16(vp1[gr]);
+          pb[nb][gr][0] = transpose8x8(pack2(p[0] * s0, p[1] * s0));
+          pb[nb][gr][1] = transpose8x8(pack2(p[2] * s1, p[3] * s1));
+        }
+      }
+      // ---- O
+      {
+        // mids: A row r holds group r % NG
+        const uint32_t* vm = reinterpret_cast<const uint32_t*>(st + T::VP) + (g % NG);
+        const uint32_t a0 = __byte_perm(vm[2 * cc * NG], vm[(2 * cc + 1) * NG], 0x7632);
+        const uint32_t a2 = __byte_perm(vm[(2 * cc + 8) * NG], vm[(2 * cc + 9) * NG], 0x7632);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) mma16816(om[nb], a0, 0u, a2, 0u, pu[nb][0], pu[nb][1]);
+      }
+      uint32_t vw[4][NT / 2];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const unsigned char* r = st + T::VC + (8 * (i >> 1) + 2 * cc + (i & 1)) * T::VSTRIDE + g * (D / 16);
+        if (NT == 4) *reinterpret_cast<uint2*>(vw[i]) = *reinterpret_cast<const uint2*>(r);
+        else vw[i][0] = *reinterpret_cast<const uint32_t*>(r);
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const uint32_t sel = (t & 1) ? 0x7632u : 0x5410u;
+        const uint32_t x01 = __byte_perm(vw[0][t / 2], vw[1][t / 2], sel), x23 = __byte_perm(vw[2][t / 2], vw[3][t / 2], sel);
+        const uint32_t a0 = codes2<0>(x01), a1 = codes2<1>(x01), a2 = codes2<0>(x23), a3 = codes2<1>(x23);
+        const uint32_t b0 = codes2<2>(x01), b1 = codes2<3>(x01), b2 = codes2<2>(x23), b3 = codes2<3>(x23);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          mma16816(o[nb][t][0], a0, a1, a2, a3, pb[nb][t / GT][0], pb[nb][t / GT][1]);
+          mma16816(o[nb][t][1], b0, b1, b2, b3, pb[nb][t / GT][0], pb[nb][t / GT][1]);
+        }
+      }
+#pragma unroll
+      for (int gr = 0; gr < NG; ++gr)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+          mma16816(oz[nb][gr], 0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u, pb[nb][gr][0], pb[nb][gr][1]);   // -24
+      __syncwarp();                                // the stage may be filled again
+    }
+    // ---- the warps' results meet
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float s = l[nb][i];
+        s += __shfl_xor_sync(0xffffffffu, s, 4);
+        s += __shfl_xor_sync(0xffffffffu, s, 8);
+        s += __shfl_xor_sync(0xffffffffu, s, 16);
+        if (g == 0) { sm_m[warp][8 * nb + 2 * cc + i] = m[nb][i]; sm_l[warp][8 * nb + 2 * cc + i] = s; }
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        // lane (group, cc) of the mids' tile holds queries 2 cc, 2 cc + 1
+        const float z0 = __shfl_sync(0xffffffffu, om[nb][0], (t / GT) * 4 + cc) + oz[nb][t / GT][0];
+        const float z1 = __shfl_sync(0xffffffffu, om[nb][1], (t / GT) * 4 + cc) + oz[nb][t / GT][1];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float* dst = sm_o + (size_t)(warp * NQ + 8 * nb + 2 * cc) * T::OSTRIDE + 32 * t + 4 * g + 2 * j;
+          *reinterpret_cast<float2*>(dst) = make_float2(o[nb][t][j][0] + z0, o[nb][t][j][2] + z0);
+          *reinterpret_cast<float2*>(dst + T::OSTRIDE) = make_float2(o[nb][t][j][1] + z1, o[nb][t][j][3] + z1);
+        }
+      }
+    }
+    __syncthreads();
+    if (tid < NQ) {
+      float M = -INFINITY, L = 0.f;
+      bool nan = false;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) M = fmaxf(M, sm_m[w][tid]);
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) {
+        // a warp without rows has sum 0 and O = 0; one whose scores were NaN has sum NaN
+        const float f = sm_m[w][tid] == -INFINITY ? 0.f : exp2f(sm_m[w][tid] - M);
+        nan = nan || sm_l[w][tid] != sm_l[w][tid];
+        sm_f[w][tid] = f;
+        L += sm_l[w][tid] * f;
+      }
+      sm_M[tid] = M;
+      sm_L[tid] = nan ? NAN : L;
+    }
+    __syncthreads();
+    const bool whole = first_s == 0 && end == u.n;
+    const int slot = 2 * (int)blockIdx.x + (first_s == 0 ? 1 : 0);
+    for (int i = tid; i < nq * D; i += WARPS * 32) {
+      const int q = i / D, dim = i - q * D;
+      float a = 0.f;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) a = fmaf(sm_o[(size_t)(w * NQ + q) * T::OSTRIDE + dim], sm_f[w][q], a);
+      if (whole) O[(size_t)b * ldo + (size_t)(hb + q) * D + dim] = __float2bfloat16_rn(a / sm_L[q]);
+      else {
+        float* pp = part + ((size_t)slot * 16 + q) * (D + 2);
+        if (dim == 0) { pp[0] = sm_M[q]; pp[1] = sm_L[q]; }
+        pp[2 + dim] = a;
+      }
+    }
+    if (!whole) {
+      // CTAs of this unit: the one with its first step to the one with its last
+      const long ux = (long)pre[b] * heads + (long)u.h * u.n;
+      const int c0 = (int)(((ux + 1) * ctas - 1) / total), c1 = (int)(((ux + u.n) * ctas - 1) / total);
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) last_flag = atomicAdd(&arrived[c0], 1) == c1 - c0;
+      __syncthreads();
+      if (last_flag) {
+        __threadfence();
+        for (int i = tid; i < nq * D; i += WARPS * 32) {
+          const int q = i / D, dim = i - q * D;
+          float M = -INFINITY, L = 0.f, a = 0.f;
+          for (int x = c0; x <= c1; ++x) M = fmaxf(M, __ldcg(part + ((size_t)(2 * x + (x == c0 ? 1 : 0)) * 16 + q) * (D + 2)));
+          for (int x = c0; x <= c1; ++x) {
+            const float* pp = part + ((size_t)(2 * x + (x == c0 ? 1 : 0)) * 16 + q) * (D + 2);
+            const float mx = __ldcg(pp), lx = __ldcg(pp + 1);
+            const float f = mx == -INFINITY ? (lx != lx ? NAN : 0.f) : exp2f(mx - M);
+            L = fmaf(lx, f, L);
+            a = fmaf(__ldcg(pp + 2 + dim), f, a);
+          }
+          O[(size_t)b * ldo + (size_t)(hb + q) * D + dim] = __float2bfloat16_rn(a / L);
+        }
+        if (tid == 0) arrived[c0] = 0;             // for the next call
+      }
+    }
+    // ---- the next unit of the piece
+    if (now.left == 0) break;
+    now.u = line.next(now.u);
+    now.end = (int)min((long)now.u.n, now.left);
+    now.left -= now.end;
+    now.s = warp;
+    first_s = 0;
+    __syncthreads();                               // sm_m, sm_l and sm_o are free again
+  }
+  cp_async_wait<0>();
+}
+
 Kv4Dev kv4_dev(const spts_ctx* ctx, const spts_kv4_cache* c) {
   return Kv4Dev{(char*)c->k_codes, (char*)c->v_codes, (uint32_t*)c->k_params, (uint32_t*)c->v_params, c->pos, c->len,
                 c->n_seq, c->capacity, c->group, ctx->desc.n_kv_heads};
@@ -189,6 +690,25 @@ spts_status attn_plain_t(spts_ctx* ctx, const spts_kv4_cache* cache, const void*
   return SPTS_OK;
 }
 
+template <int D, int NG, int NB>
+spts_status attn_t(spts_ctx* ctx, const spts_kv4_cache* cache, const void* Q, int64_t ldq, void* O, int64_t ldo) {
+  using T = Kv4Tile<D, NG, NB>;
+  const Kv4Dev c = kv4_dev(ctx, cache);
+  const int H = ctx->desc.n_q_heads, G = H / c.Hkv;
+  const int grid = ctx->sm_count < KV4_MAX_CTAS ? ctx->sm_count : KV4_MAX_CTAS;
+  if (cudaFuncSetAttribute(kv4_attn_kernel<D, NG, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, T::SMEM) != cudaSuccess)
+    return SPTS_ERR_CUDA;
+  kv4_attn_kernel<D, NG, NB><<<grid, T::WARPS * 32, T::SMEM, ctx->stream>>>(c, (const bf16*)Q, ldq, H, NB == 1 ? 1 : ceil_div(G, 16),
+                                                                            (bf16*)O, ldo, ctx->ws.kv4_part, ctx->ws.kv4_arrived);
+  SPTS_CUDA_OK(ctx);
+  return SPTS_OK;
+}
+template <int D, int NG>
+spts_status attn_heads(spts_ctx* ctx, const spts_kv4_cache* cache, const void* Q, int64_t ldq, void* O, int64_t ldo) {
+  return ctx->desc.n_q_heads / ctx->desc.n_kv_heads <= 8 ? attn_t<D, NG, 1>(ctx, cache, Q, ldq, O, ldo)
+                                                         : attn_t<D, NG, 2>(ctx, cache, Q, ldq, O, ldo);
+}
+
 }  // namespace
 
 spts_status launch_kv4_append(spts_ctx* ctx, const spts_kv4_cache* cache, const void* K, int64_t ldk, const void* V,
@@ -204,6 +724,12 @@ spts_status launch_kv4_append(spts_ctx* ctx, const spts_kv4_cache* cache, const 
 
 spts_status launch_kv4_attention(spts_ctx* ctx, const spts_kv4_cache* cache, const void* Q, int64_t ldq, void* O, int64_t ldo) {
   const bool wide = ctx->desc.head_dim == 128;
+  if (!plain4(ctx)) {
+    const int ng = ctx->desc.head_dim / cache->group;
+    if (!wide) return ng == 2 ? attn_heads<64, 2>(ctx, cache, Q, ldq, O, ldo) : attn_heads<64, 1>(ctx, cache, Q, ldq, O, ldo);
+    if (ng == 4) return attn_heads<128, 4>(ctx, cache, Q, ldq, O, ldo);
+    return ng == 2 ? attn_heads<128, 2>(ctx, cache, Q, ldq, O, ldo) : attn_heads<128, 1>(ctx, cache, Q, ldq, O, ldo);
+  }
   if (ctx->desc.dtype == SPTS_BF16)
     return wide ? attn_plain_t<bf16, 128>(ctx, cache, Q, ldq, O, ldo) : attn_plain_t<bf16, 64>(ctx, cache, Q, ldq, O, ldo);
   return wide ? attn_plain_t<float, 128>(ctx, cache, Q, ldq, O, ldo) : attn_plain_t<float, 64>(ctx, cache, Q, ldq, O, ldo);

@@ -104,6 +104,8 @@ size_t carve(const spts_model_desc& d, int Nmax, void* base, Workspace* ws, std:
   w.acc32_elems = N * KD;
   if (Npad * HD * es >= w.acc32_elems * sizeof(float)) w.acc32 = reinterpret_cast<float*>(w.o_att);
   else w.acc32 = c.take<float>(w.acc32_elems);
+  w.kv4_part = c.take<float>((size_t)2 * KV4_MAX_CTAS * 16 * (d.head_dim + 2));
+  w.kv4_arrived = c.take<int>(KV4_MAX_CTAS);
   w.dec = c.take<float>(decode_scratch_floats(d));
   w.logits_v = c.take<float>((size_t)(d.vocab > 0 ? d.vocab : 1));
   w.xrow = c.take<char>((size_t)d.hidden * es);
@@ -575,6 +577,7 @@ spts_status spts_create(const spts_model_desc* desc, int max_seq, void* workspac
   ctx->rope_pos = nullptr;
   ctx->rope_n = 0;
   ctx->pap_window = 1;
+  ctx->reference_option = false;
   ctx->debug_checks = false;
   ctx->prof = new (std::nothrow) Profiler;
   ctx->ws_base = reinterpret_cast<char*>(workspace);
@@ -591,6 +594,10 @@ spts_status spts_create(const spts_model_desc* desc, int max_seq, void* workspac
   }
   if (cudaMemsetAsync(ctx->ws.status, 0, 64 * sizeof(int), ctx->stream) != cudaSuccess) { spts_destroy(ctx); return SPTS_ERR_CUDA; }
   if (cudaMemsetAsync(ctx->ws.topk_scratch, 0, TOPK_SCRATCH_WORDS * sizeof(uint32_t), ctx->stream) != cudaSuccess) {
+    spts_destroy(ctx);
+    return SPTS_ERR_CUDA;
+  }
+  if (cudaMemsetAsync(ctx->ws.kv4_arrived, 0, KV4_MAX_CTAS * sizeof(int), ctx->stream) != cudaSuccess) {
     spts_destroy(ctx);
     return SPTS_ERR_CUDA;
   }
@@ -638,6 +645,7 @@ spts_status spts_set_option(spts_ctx* ctx, uint32_t option, int value) {
   TRY(check_ctx(ctx));
   if (option == SPTS_REFERENCE_KERNELS) {
     if (ctx->desc.dtype == SPTS_FP32 || !tc_shape_ok(ctx->desc)) return value ? SPTS_OK : SPTS_ERR_UNSUPPORTED;
+    ctx->reference_option = value != 0;
     if (!value && ctx->encode_tiled == nullptr) TRY(tc_init(ctx));
     ctx->reference_kernels = value != 0;
     return SPTS_OK;

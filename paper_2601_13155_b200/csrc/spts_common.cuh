@@ -90,6 +90,8 @@ struct Workspace {
   int32_t* row_seq;     // [Nmax]
   int32_t* vt_col;      // [Nmax]
   int vt_ld_max;        // columns of v_t
+  float* kv4_part;      // [2 * KV4_MAX_CTAS, 16, d + 2] partial results of the attention over a 4-bit cache
+  int* kv4_arrived;     // [KV4_MAX_CTAS] CTAs that have left theirs; zero between calls
   int4* attn_tiles;     // [Nmax / 128 + BATCH_MAX_SEQ] query tiles of a packed batch's attention launch
 };
 
@@ -100,6 +102,7 @@ struct spts_ctx {
   int max_seq;
   cudaStream_t stream;
   spts::Workspace ws;
+  bool reference_option;    // SPTS_REFERENCE_KERNELS was set by the caller
   bool reference_kernels;   // plain CUDA-core kernels (always true in fp32 mode)
   bool ffn_score_pap_only;   // T_f from S_mha alone (no proxy FFN)
   bool debug_checks;        // every selected index list is checked on the device (SPTS_ERR_INDEX in the status word)
@@ -122,6 +125,7 @@ struct spts_ctx {
 namespace spts {
 
 static const int BATCH_MAX_SEQ = 1024;        // sequences per packed batch that take the one-launch-per-step route
+static const int KV4_MAX_CTAS = 160;          // CTAs of the attention over a 4-bit cache: one per SM
 static const int PAP_MAX_WINDOW = 64;         // largest query window of the probe (the paper ablates 1, 4 and 64)
 
 // top-k scratch size in uint32 words
@@ -256,6 +260,8 @@ struct W4GemvArgs {
   int norm, fp32_out;
   void* Y; int64_t ldy;
 };
+// fp32 storage, or the plain kernels were asked for
+inline bool plain4(const spts_ctx* ctx) { return ctx->desc.dtype != SPTS_BF16 || ctx->reference_option; }
 spts_status launch_w4_gemv(spts_ctx* ctx, const W4GemvArgs& a);
 spts_status launch_w4_quantize(spts_ctx* ctx, const void* W, int out, int in, int group, void* codes, void* params);
 spts_status launch_kv4_append(spts_ctx* ctx, const spts_kv4_cache* cache, const void* K, int64_t ldk, const void* V,
