@@ -7,6 +7,7 @@ module without the built library raises.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from typing import Dict, List, Optional, Sequence
 
@@ -237,29 +238,32 @@ class KvCache:
             e.len = 0
 
 
-def _rows(t: torch.Tensor, width: int, dtype, what: str):
-    """Pointer and row stride of a [n, ...] tensor whose rows of `width` elements are contiguous (a view into wider
+def _rows(t: torch.Tensor, width: int, dtype, what: str, dev: int):
+    """Address and row stride of a [n, ...] tensor whose rows of `width` elements are contiguous (a view into wider
     rows is fine)."""
-    if not t.is_cuda or t.dtype != dtype:
-        raise ValueError(f"{what}: a CUDA tensor of {dtype} is needed, got {t.dtype} on {t.device}")
-    if t.dim() < 2 or t[0:1].numel() != (width if t.shape[0] else 0):
-        raise ValueError(f"{what}: rows of {width} elements are needed, got {tuple(t.shape)}")
+    if t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{what}: a tensor of {dtype} on cuda:{dev} is needed, got {t.dtype} on {t.device}")
+    shape = t.shape
+    if len(shape) == 2 and shape[1] == width and t.stride(1) == 1:
+        return t.data_ptr(), (t.stride(0) if shape[0] > 1 else width)
+    if len(shape) < 2 or math.prod(shape[1:]) != width:
+        raise ValueError(f"{what}: rows of {width} elements are needed, got {tuple(shape)}")
     inner = 1
-    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+    for size, stride in zip(reversed(shape[1:]), reversed(t.stride()[1:])):
         if size != 1 and stride != inner:
             raise ValueError(f"{what}: the elements of a row must be contiguous")
         inner *= size
-    return C.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else width)
+    return t.data_ptr(), (t.stride(0) if shape[0] > 1 else width)
 
 
-def _vec(t: Optional[torch.Tensor], n: Optional[int], dtype, what: str, device=None):
+def _vec(t: Optional[torch.Tensor], n: Optional[int], dtype, what: str, dev: Optional[int] = None):
     if t is None:
         return None
-    if not t.is_cuda or not t.is_contiguous() or t.dtype != dtype or (n is not None and t.numel() != n):
+    if not t.is_cuda or not t.is_contiguous() or t.dtype is not dtype or (n is not None and t.numel() != n):
         raise ValueError(f"{what}: a contiguous CUDA tensor of {dtype}" + (f" with {n} elements" if n is not None else "") + " is needed")
-    if device is not None and t.device != device:
-        raise ValueError(f"{what}: on {t.device}, the context is on {device}")
-    return C.c_void_p(t.data_ptr())
+    if dev is not None and t.get_device() != dev:
+        raise ValueError(f"{what}: on {t.device}, cuda:{dev} is needed")
+    return t.data_ptr()
 
 
 class W4Weight:
@@ -269,12 +273,13 @@ class W4Weight:
         if codes.dim() != 2 or params.dim() != 3 or params.shape[0] != codes.shape[0] or params.shape[2] != 2 or params.shape[1] < 1:
             raise ValueError(f"codes [out, in / 2] and params [out, in / group, 2] are needed, got {tuple(codes.shape)}, {tuple(params.shape)}")
         _vec(codes, None, torch.uint8, "codes")
-        _vec(params, None, torch.bfloat16, "params", codes.device)
+        _vec(params, None, torch.bfloat16, "params", codes.get_device())
         self.codes, self.params = codes, params
         self.out_features, self.in_features = codes.shape[0], 2 * codes.shape[1]
         if self.in_features % params.shape[1] != 0:
             raise ValueError("params do not divide the rows into equal groups")
         self.group = self.in_features // params.shape[1]
+        self.device_index = codes.get_device()
         self.c = W4C(codes.data_ptr(), params.data_ptr(), self.out_features, self.in_features, self.group)
 
 
@@ -306,6 +311,7 @@ class Kv4Cache:
             if t.device != self.k_codes.device:
                 raise ValueError("the buffers of a cache are on one device")
         self.n_seq, self.capacity, self.group = n_seq, cap, group
+        self.heads, self.device_index = (hkv, d), self.k_codes.get_device()
         self.c = Kv4CacheC(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_params.data_ptr(),
                            self.v_params.data_ptr(), self.pos.data_ptr() if self.pos is not None else None,
                            self.length.data_ptr(), n_seq, cap, group)
@@ -335,17 +341,19 @@ class LogitsRules:
                               mask.stride(0) if mask is not None else 0, history.numel() if history is not None else 0,
                               bias_token.numel() if bias_token is not None else 0)
 
-    def check(self, n: int, vocab: int, device):
-        for name, want in (("history_start", n + 1), ("generated_start", n), ("repetition", n), ("presence", n),
-                           ("frequency", n), ("bias_start", n + 1)):
-            if self.t[name] is not None and self.t[name].numel() != want:
-                raise ValueError(f"{name}: {want} entries are needed for {n} rows, got {self.t[name].numel()}")
+        self.sizes = [(name, t.numel(), 1 if name.endswith("_start") and name != "generated_start" else 0) for name, t in self.t.items()
+                      if t is not None and name in ("history_start", "generated_start", "repetition", "presence", "frequency", "bias_start")]
+        self.devices = {t.get_device() for t in self.t.values() if t is not None}
+
+    def check(self, n: int, vocab: int, dev: int):
+        for name, size, more in self.sizes:
+            if size != n + more:
+                raise ValueError(f"{name}: {n + more} entries are needed for {n} rows, got {size}")
         m = self.t["mask"]
         if m is not None and (m.shape[0] != n or m.shape[1] < (vocab + 31) // 32):
             raise ValueError(f"mask: [{n}, {(vocab + 31) // 32}] words are needed, got {tuple(m.shape)}")
-        for name, t in self.t.items():
-            if t is not None and t.device != device:
-                raise ValueError(f"{name}: on {t.device}, the context is on {device}")
+        if self.devices - {dev}:
+            raise ValueError(f"the rules' tensors are on cuda:{self.devices}, the context is on cuda:{dev}")
 
 
 class Spts:
@@ -362,7 +370,7 @@ class Spts:
                               shape.ltp_dlow, shape.ltp_rank, shape.n_layers, shape.vocab, shape.rms_eps,
                               shape.rope_theta, SPTS_BF16 if shape.dtype == "bf16" else SPTS_FP32)
         torch.cuda.set_device(self.device)
-        self.k_device = torch.device("cuda", self.device.index if self.device.index is not None else torch.cuda.current_device())
+        self.dev = self.device.index if self.device.index is not None else torch.cuda.current_device()
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
         nbytes = self.lib.spts_workspace_bytes(C.byref(self.desc), max_seq)
         if nbytes == 0:
@@ -558,97 +566,91 @@ class Spts:
                                               _ptr(x_out), _ptr(logits_out), _ptr(token_out)), "spts_decode_step")
 
     # ------------------------------------------------------------------ generation with 4-bit weights and caches
-    def _here(self, *tensors):
-        for t in tensors:
-            if t is not None and t.device != self.k_device:
-                raise ValueError(f"a tensor on {t.device}, the context is on {self.k_device}")
-
     def w4_quantize(self, W: torch.Tensor, group: int = 128) -> W4Weight:
         """spts_w4_quantize: the 4-bit form of W [out, in] (storage type)."""
         out, k = W.shape
         if group not in (32, 64, 128) or k % group:
             raise ValueError(f"groups of 32, 64 or 128 that divide {k} are needed, got {group}")
-        self._here(W)
         codes = torch.empty(out, k // 2, dtype=torch.uint8, device=self.device)
         params = torch.empty(out, k // group, 2, dtype=torch.bfloat16, device=self.device)
-        with torch.cuda.device(self.device):
-            self._check(self.lib.spts_w4_quantize(self.h, _vec(W, out * k, self.dtype, "W"), out, k, group, _ptr(codes), _ptr(params)),
-                        "spts_w4_quantize")
+        self._check(self.lib.spts_w4_quantize(self.h, _vec(W, out * k, self.dtype, "W", self.dev), out, k, group, _ptr(codes),
+                                              _ptr(params)), "spts_w4_quantize")
         return W4Weight(codes, params)
 
     def w4_gemv(self, w: W4Weight, X: torch.Tensor, w2: Optional[W4Weight] = None, norm: bool = False, residual=None,
                 fp32_out: bool = False, out=None):
         """spts_w4_gemv: X [n, in] W^T for up to 32 tokens; w2: silu(X W^T) * (X W2^T); residual is added."""
-        n = X.shape[0]
+        n, width, dev = X.shape[0], w.out_features, self.dev
         odt = torch.float32 if fp32_out else self.dtype
         if out is None:
-            out = torch.empty(n, w.out_features, dtype=odt, device=self.device)
-        self._here(X, residual, out, w.codes, w2.codes if w2 is not None else None)
-        xp, ldx = _rows(X, w.in_features, self.dtype, "X")
-        yp, ldy = _rows(out, w.out_features, odt, "out")
-        rp, ldr = (None, 0) if residual is None else _rows(residual, w.out_features, self.dtype, "residual")
+            out = torch.empty((n, width), dtype=odt, device=self.device)
+        if w.device_index != dev or (w2 is not None and w2.device_index != dev):
+            raise ValueError(f"the weights are not on cuda:{dev}")
+        xp, ldx = _rows(X, w.in_features, self.dtype, "X", dev)
+        yp, ldy = _rows(out, width, odt, "out", dev)
+        rp, ldr = (None, 0) if residual is None else _rows(residual, width, self.dtype, "residual", dev)
         if out.shape[0] != n or (residual is not None and residual.shape[0] != n):
             raise ValueError("X, residual and out have the same number of rows")
-        with torch.cuda.device(self.device):
-            self._check(self.lib.spts_w4_gemv(self.h, C.byref(w.c), C.byref(w2.c) if w2 is not None else None, xp, ldx, n, rp,
-                                              ldr, (W4_NORM if norm else 0) | (W4_FP32_OUT if fp32_out else 0), yp, ldy),
-                        "spts_w4_gemv")
+        code = self.lib.spts_w4_gemv(self.h, w.c, w2.c if w2 is not None else None, xp, ldx, n, rp, ldr,
+                                     (W4_NORM if norm else 0) | (W4_FP32_OUT if fp32_out else 0), yp, ldy)
+        if code:
+            raise SptsError(code, "spts_w4_gemv")
         return out
 
     def _kv4_shape(self, cache: Kv4Cache):
-        if tuple(cache.k_codes.shape[1::2]) != (self.shape.n_kv_heads, self.shape.head_dim // 2):
+        if cache.heads != (self.shape.n_kv_heads, self.shape.head_dim):
             raise ValueError("the cache was made for other heads than this context's")
-        self._here(cache.k_codes)
+        if cache.device_index != self.dev:
+            raise ValueError(f"the cache is not on cuda:{self.dev}")
 
     def kv4_append(self, cache: Kv4Cache, K: torch.Tensor, V: torch.Tensor, pos=None, row_start=None, at=None, K_out=None,
                    V_out=None):
         """spts_kv4_append: rows of K, V [n, Hkv, d] (K after RoPE) into the cache; row_start [n_seq + 1] and at [n_seq]
         are device int32.  K_out, V_out: the values that the cache then stands for."""
-        n, w = K.shape[0], self.shape.n_kv_heads * self.shape.head_dim
+        n, w, dev = K.shape[0], self.shape.n_kv_heads * self.shape.head_dim, self.dev
         self._kv4_shape(cache)
-        self._here(K, V, pos, row_start, at, K_out, V_out)
         if V.shape[0] != n:
             raise ValueError("as many rows of V as of K are needed")
-        kp, ldk = _rows(K, w, self.dtype, "K")
-        vp, ldv = _rows(V, w, self.dtype, "V")
-        with torch.cuda.device(self.device):
-            self._check(self.lib.spts_kv4_append(self.h, C.byref(cache.c), kp, ldk, vp, ldv, _vec(pos, n, torch.int32, "pos"),
-                                                 _vec(row_start, cache.n_seq + 1, torch.int32, "row_start"),
-                                                 _vec(at, cache.n_seq, torch.int32, "at"), n, _vec(K_out, n * w, self.dtype, "K_out"),
-                                                 _vec(V_out, n * w, self.dtype, "V_out")), "spts_kv4_append")
+        kp, ldk = _rows(K, w, self.dtype, "K", dev)
+        vp, ldv = _rows(V, w, self.dtype, "V", dev)
+        i32 = torch.int32
+        code = self.lib.spts_kv4_append(self.h, cache.c, kp, ldk, vp, ldv, _vec(pos, n, i32, "pos", dev),
+                                        _vec(row_start, cache.n_seq + 1, i32, "row_start", dev), _vec(at, cache.n_seq, i32, "at", dev),
+                                        n, _vec(K_out, n * w, self.dtype, "K_out", dev), _vec(V_out, n * w, self.dtype, "V_out", dev))
+        if code:
+            raise SptsError(code, "spts_kv4_append")
 
     def kv4_attention(self, cache: Kv4Cache, Q: torch.Tensor, O_out=None):
         """spts_kv4_attention: one query per sequence, Q [n_seq, H, d] (or [n_seq, H * d]) -> [n_seq, H * d]."""
-        w = self.shape.n_q_heads * self.shape.head_dim
+        n, w = cache.n_seq, self.shape.n_q_heads * self.shape.head_dim
         self._kv4_shape(cache)
         if O_out is None:
-            O_out = torch.empty(cache.n_seq, w, dtype=self.dtype, device=self.device)
-        self._here(Q, O_out)
-        if Q.shape[0] != cache.n_seq or O_out.shape[0] != cache.n_seq:
-            raise ValueError(f"one query per sequence of the cache: {cache.n_seq} rows are needed")
-        qp, ldq = _rows(Q, w, self.dtype, "Q")
-        op, ldo = _rows(O_out, w, self.dtype, "O_out")
-        with torch.cuda.device(self.device):
-            self._check(self.lib.spts_kv4_attention(self.h, C.byref(cache.c), qp, ldq, op, ldo), "spts_kv4_attention")
+            O_out = torch.empty((n, w), dtype=self.dtype, device=self.device)
+        if Q.shape[0] != n or O_out.shape[0] != n:
+            raise ValueError(f"one query per sequence of the cache: {n} rows are needed")
+        qp, ldq = _rows(Q, w, self.dtype, "Q", self.dev)
+        op, ldo = _rows(O_out, w, self.dtype, "O_out", self.dev)
+        code = self.lib.spts_kv4_attention(self.h, cache.c, qp, ldq, op, ldo)
+        if code:
+            raise SptsError(code, "spts_kv4_attention")
         return O_out
 
     def process_logits(self, logits: torch.Tensor, rules: LogitsRules, out=None, token_out=None, want_logits: bool = True):
         """spts_process_logits: (logits under the rules, token).  out may be the logits themselves; with
         want_logits=False only the token is computed."""
         n, v = logits.shape
-        rules.check(n, v, self.k_device)
+        rules.check(n, v, self.dev)
         if out is None and want_logits:
-            out = torch.empty(n, v, dtype=torch.float32, device=self.device)
+            out = torch.empty((n, v), dtype=torch.float32, device=self.device)
         if token_out is None:
             token_out = torch.empty(n, dtype=torch.int32, device=self.device)
-        self._here(logits, out, token_out)
-        lp, ld = _rows(logits, v, torch.float32, "logits")
-        op, ldo = (None, 0) if out is None else _rows(out, v, torch.float32, "out")
+        lp, ld = _rows(logits, v, torch.float32, "logits", self.dev)
+        op, ldo = (None, 0) if out is None else _rows(out, v, torch.float32, "out", self.dev)
         if out is not None and out.shape[0] != n:
             raise ValueError("as many rows of out as of logits are needed")
-        with torch.cuda.device(self.device):
-            self._check(self.lib.spts_process_logits(self.h, lp, ld, n, v, C.byref(rules.c), op, ldo,
-                                                     _vec(token_out, n, torch.int32, "token_out")), "spts_process_logits")
+        code = self.lib.spts_process_logits(self.h, lp, ld, n, v, rules.c, op, ldo, _vec(token_out, n, torch.int32, "token_out", self.dev))
+        if code:
+            raise SptsError(code, "spts_process_logits")
         return out, token_out
 
 

@@ -186,32 +186,11 @@ kv4_attn_plain_kernel(Kv4Dev c, const T* __restrict__ Q, int64_t ldq, int H, T* 
 constexpr float KV4_LOG2E = 1.4426950408889634f;
 constexpr float KV4_SLACK = 10.0f;
 
-__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
   uint32_t d;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
   return d;
 }
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ float round_bf16(float v) { return __bfloat162float(__float2bfloat16_rn(v)); }
-// (16 + code j, 16 + code j + 4) of a word of eight codes / of two rows' halfwords
-template <int J> __device__ __forceinline__ uint32_t codes2(uint32_t w) {
-  const uint32_t s = J == 0 ? w << 3 : w >> (4 * J - 3);
-  return (s & 0x00780078u) | 0x41804180u;
-}
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 template <int D, int NG, int NB>
 struct Kv4Tile {
   static constexpr int WARPS = NB == 1 ? 16 : 8;
@@ -391,7 +370,7 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
       float mine = 0.f;
 #pragma unroll
       for (int i = 0; i < NG; ++i) if (cc == i) mine = sums[i];
-      const float a = -24.f * mine, ah = round_bf16(a), mh = round_bf16(mine);
+      const float a = -CODE_BIAS * mine, ah = round_bf16(a), mh = round_bf16(mine);
       qm[nb][0] = pack2(ah, mh);
       qm[nb][1] = pack2(a - ah, mine - mh);
     }
@@ -459,8 +438,8 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
 #pragma unroll
         for (int tt = 0; tt < GT; ++tt) {
           const int t = gr * GT + tt;
-          const uint32_t a0 = codes2<0>(kw0[t]), a1 = codes2<0>(kw1[t]), a2 = codes2<1>(kw0[t]), a3 = codes2<1>(kw1[t]);
-          const uint32_t b0 = codes2<2>(kw0[t]), b1 = codes2<2>(kw1[t]), b2 = codes2<3>(kw0[t]), b3 = codes2<3>(kw1[t]);
+          const uint32_t a0 = code_pair<0>(kw0[t]), a1 = code_pair<0>(kw1[t]), a2 = code_pair<1>(kw0[t]), a3 = code_pair<1>(kw1[t]);
+          const uint32_t b0 = code_pair<2>(kw0[t]), b1 = code_pair<2>(kw1[t]), b2 = code_pair<3>(kw0[t]), b3 = code_pair<3>(kw1[t]);
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) {
             mma16816(acc[nb], a0, a1, a2, a3, qf[nb][t][0], qf[nb][t][1]);
@@ -551,8 +530,8 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
       for (int t = 0; t < NT; ++t) {
         const uint32_t sel = (t & 1) ? 0x7632u : 0x5410u;
         const uint32_t x01 = __byte_perm(vw[0][t / 2], vw[1][t / 2], sel), x23 = __byte_perm(vw[2][t / 2], vw[3][t / 2], sel);
-        const uint32_t a0 = codes2<0>(x01), a1 = codes2<1>(x01), a2 = codes2<0>(x23), a3 = codes2<1>(x23);
-        const uint32_t b0 = codes2<2>(x01), b1 = codes2<3>(x01), b2 = codes2<2>(x23), b3 = codes2<3>(x23);
+        const uint32_t a0 = code_pair<0>(x01), a1 = code_pair<1>(x01), a2 = code_pair<0>(x23), a3 = code_pair<1>(x23);
+        const uint32_t b0 = code_pair<2>(x01), b1 = code_pair<3>(x01), b2 = code_pair<2>(x23), b3 = code_pair<3>(x23);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           mma16816(o[nb][t][0], a0, a1, a2, a3, pb[nb][t / GT][0], pb[nb][t / GT][1]);
@@ -563,7 +542,8 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
       for (int gr = 0; gr < NG; ++gr)
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
-          mma16816(oz[nb][gr], 0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u, pb[nb][gr][0], pb[nb][gr][1]);   // -24
+          mma16816(oz[nb][gr], MINUS_BIAS_BF16X2, MINUS_BIAS_BF16X2, MINUS_BIAS_BF16X2, MINUS_BIAS_BF16X2, pb[nb][gr][0],
+                   pb[nb][gr][1]);
       __syncwarp();                                // the stage may be filled again
     }
     // ---- the warps' results meet

@@ -34,6 +34,37 @@ __device__ __forceinline__ void store8(bf16* p, const float* x) {
   *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// ---- matrix instructions on codes
+// Codes become bf16 without arithmetic: code << 3 in the mantissa of 16.0 is exactly 16 + code, one shift and one logic
+// operation per two codes.  J-th codes of the two halves of a word: (16 + low, 16 + high).
+template <int J> __device__ __forceinline__ uint32_t code_pair(uint32_t w) {
+  const uint32_t s = J == 0 ? w << 3 : w >> (4 * J - 3);
+  return (s & 0x00780078u) | 0x41804180u;
+}
+constexpr float CODE_BIAS = 24.f;               // 16 of the mantissa trick + 8 of the format
+constexpr uint32_t MINUS_BIAS_BF16X2 = 0xC1C0C1C0u;
+constexpr uint32_t ONE_BF16X2 = 0x3F803F80u;
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ float round_bf16(float v) { return __bfloat162float(__float2bfloat16_rn(v)); }
+
+// ---- asynchronous copies into shared memory
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, bool in) {       // zero where not `in`
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(in ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // Quantises the eight elements of this lane; the group is `lanes` (4, 8 or 16) neighbouring lanes of the warp, aligned
 // to their number, and every lane of the warp calls.  Returns the eight codes, element i in bits 4i .. 4i + 3; `params`
 // = scale | mid << 16; read (if not null) the values that the codes stand for.

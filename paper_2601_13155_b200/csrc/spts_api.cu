@@ -560,16 +560,19 @@ spts_status spts_create(const spts_model_desc* desc, int max_seq, void* workspac
   if (carve(*desc, max_seq, nullptr, nullptr) > workspace_bytes) return SPTS_ERR_WORKSPACE;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return SPTS_ERR_CUDA;
-  cudaDeviceProp prop;
-  if (cudaGetDeviceProperties(&prop, dev) != cudaSuccess) return SPTS_ERR_CUDA;
-  if (desc->dtype == SPTS_BF16 && prop.major != 10) return SPTS_ERR_UNSUPPORTED;   // sm_100a only
+  int major = 0, sms = 0;
+  if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return SPTS_ERR_CUDA;
+  if (desc->dtype == SPTS_BF16 && major != 10) return SPTS_ERR_UNSUPPORTED;   // sm_100a only
   spts_ctx* ctx = new (std::nothrow) spts_ctx;
   if (ctx == nullptr) return SPTS_ERR_INVALID_ARG;
   ctx->desc = *desc;
   ctx->max_seq = max_seq;
   ctx->stream = reinterpret_cast<cudaStream_t>(cuda_stream);
   ctx->launches = 0;
-  ctx->sm_count = prop.multiProcessorCount;
+  ctx->sm_count = sms;
+  ctx->device = dev;
   ctx->encode_tiled = nullptr;
   ctx->ffn_score_pap_only = false;
   ctx->rstd_rows = nullptr;
@@ -1119,6 +1122,18 @@ spts_status spts_decode_step(spts_ctx* ctx, const spts_model_weights* mw, spts_k
 
 // ---- generation with 4-bit weights and caches
 namespace {
+// The calls of this part may be made while another device is current.
+struct DeviceScope {
+  int back = -1;
+  bool ok;
+  explicit DeviceScope(const spts_ctx* ctx) {
+    int cur = -1;
+    ok = cudaGetDevice(&cur) == cudaSuccess;
+    if (ok && cur != ctx->device) { back = cur; ok = cudaSetDevice(ctx->device) == cudaSuccess; }
+  }
+  ~DeviceScope() { if (back >= 0) cudaSetDevice(back); }
+};
+#define ON_DEVICE(ctx) DeviceScope device_scope__(ctx); if (!device_scope__.ok) return SPTS_ERR_CUDA
 bool group_ok(int group) { return group == 32 || group == 64 || group == 128; }
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
 // rows of 16-byte loads: aligned base, stride a multiple of 16 bytes where there is more than one row
@@ -1149,6 +1164,7 @@ spts_status spts_w4_quantize(spts_ctx* ctx, const void* W, int out_features, int
   if (W == nullptr || codes == nullptr || params == nullptr) return SPTS_ERR_INVALID_ARG;
   if (!group_ok(group) || out_features < 1 || in_features < 1 || in_features % group != 0) return SPTS_ERR_SHAPE;
   if (!aligned16(W) || !aligned16(codes) || !aligned4(params)) return SPTS_ERR_INVALID_ARG;
+  ON_DEVICE(ctx);
   return launch_w4_quantize(ctx, W, out_features, in_features, group, codes, params);
 }
 
@@ -1176,6 +1192,7 @@ spts_status spts_w4_gemv(spts_ctx* ctx, const spts_w4* w, const spts_w4* w2, con
   a.X = X; a.ldx = ldx; a.n = n; a.residual = residual; a.ldr = ldr;
   a.norm = (flags & SPTS_W4_NORM) != 0; a.fp32_out = (flags & SPTS_W4_FP32_OUT) != 0;
   a.Y = Y; a.ldy = ldy;
+  ON_DEVICE(ctx);
   return launch_w4_gemv(ctx, a);
 }
 
@@ -1195,6 +1212,7 @@ spts_status spts_kv4_append(spts_ctx* ctx, const spts_kv4_cache* cache, const vo
     if (!aligned16(K_read) || !aligned16(V_read) || (K_read != nullptr && K_read == V_read)) return SPTS_ERR_INVALID_ARG;
   }
   if (at == cache->len) at = nullptr;
+  ON_DEVICE(ctx);
   return launch_kv4_append(ctx, cache, K, ldk, V, ldv, pos, row_start, at, n_rows, K_read, V_read);
 }
 
@@ -1206,6 +1224,7 @@ spts_status spts_kv4_attention(spts_ctx* ctx, const spts_kv4_cache* cache, const
   const int64_t width = (int64_t)ctx->desc.n_q_heads * ctx->desc.head_dim;
   const size_t es = elt_size(ctx->desc);
   if (!rows_ok(Q, ldq, width, cache->n_seq, es) || !rows_ok(O_out, ldo, width, cache->n_seq, es)) return SPTS_ERR_INVALID_ARG;
+  ON_DEVICE(ctx);
   return launch_kv4_attention(ctx, cache, Q, ldq, O_out, ldo);
 }
 
@@ -1227,6 +1246,7 @@ spts_status spts_process_logits(spts_ctx* ctx, const float* logits, int64_t ld, 
   if (r.repetition == nullptr && r.presence == nullptr && r.frequency == nullptr) r.history = nullptr;   // nothing to count for
   if (r.n_history == 0) r.history = nullptr;
   if (r.n_bias == 0) r.bias_token = nullptr;
+  ON_DEVICE(ctx);
   return launch_process_logits(ctx, logits, ld, n, vocab, r, out, ldo, token_out);
 }
 

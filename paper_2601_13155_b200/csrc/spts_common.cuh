@@ -118,6 +118,7 @@ struct spts_ctx {
   int pap_window;           // number of trailing queries the probe averages over (1 = the paper's default)
   int64_t launches;
   int sm_count;
+  int device;               // the device the context was created on
   void* encode_tiled;       // cuTensorMapEncodeTiled entry point (tensor-core mode)
   void* prof;               // per-operation CUDA-event timing (host state)
 };
