@@ -164,41 +164,58 @@ kv4_attn_plain_kernel(Kv4Dev c, const T* __restrict__ Q, int64_t ldq, int H, T* 
 // ---------------------------------------------------------------------------------------------------------------------
 // Attention of single tokens on matrix instructions (m16n8k16, fp32 accumulation).
 //
-// A warp takes 16 cached rows of one KV head at a time and all query heads that read it (up to 8 NB):
+// A warp takes tiles of 16 cached rows of one KV head and all query heads that read it (up to 8 NB):
 //   S[row, q] = K Q^T    M = 16 rows, N = queries, K = dims        O[dim, q] += V^T P    M = 16 dims, N = queries, K = 16 rows
-// so that the codes are always the A operand and no lane is spent on absent queries beyond eight.
-// Codes become bf16 without arithmetic: code << 3 in the mantissa of 16.0 is exactly 16 + code, one shift and one logic
-// operation per two codes (the storage orders put the two codes of a register 16 bits apart).  Scales and mids stay in fp32:
-//   S = sum_groups scale_g (sum_i (16 + c_i) q_i) + sum_g (mid_g - 24 scale_g) (sum_i q_i)
-// where the second sum is one more matrix step whose A registers are the params words as they lie in memory, and whose B
-// holds -24 sum q and sum q in two bf16 pieces each (16 bits; the term is off by 2^-17 relative).
-//   O = sum_rows (16 + c) p'_g - 24 sum_rows p'_g + sum_rows p mid_g,   p'_g = bf16(p scale_g), p in the last sum bf16(p)
-// (both roundings half a bf16 step, like the rounding of p in the bf16 kernels); the -24 multiplies the rounded p' by a
-// matrix step with a constant A, so the bias cancels exactly up to fp32 sums.  P changes from the accumulator's layout to
-// the B operand's by 8 x 8 transposes between lanes.
-// The running maximum is a reference, not the maximum: it moves only when a score exceeds it by 2^10 (weights are then at
-// most 1024, far inside bf16 and fp32), which after the first rows is rare, so the steps carry no reduction.
+// so that the codes are always the A operand and no lane is spent on absent queries beyond eight.  What bounds the kernel is
+// the instructions between the codes and the matrix units, so they are few: codes enter as fp16 by masks alone (code_pair),
+// scales and mids stay outside in fp32:
+//   S = sum_groups scale_g (sum_i c_i q_i) + sum_g (mid_g - 8 scale_g) (sum_i q_i)
+// q is brought to fp16 by a power of two per query (exact: bf16 has fewer bits, and what falls below fp16's range is 2^-35 of
+// the query's largest element).  The second sum is one more matrix step, in bf16, whose A registers are the params words as
+// they lie in memory and whose B holds -8 sum q and sum q in two bf16 pieces each (off by 2^-17 relative).
+//   O = sum_rows c p'_g - 8 sum_rows p'_g + sum_rows p mid_g,   p'_g = fp16(p scale_g / r), p in the last sum bf16(p)
+// r is a power of two near the largest scale met, so p' uses fp16's eleven bits down to 2^-20 of the largest weight, and its
+// absolute error below that is 2^-31; the -8 multiplies the rounded p' by a matrix step with a constant A, so it cancels up
+// to fp32 sums.  P changes from the accumulator's layout to the B operand's by 8 x 8 transposes between lanes.
+// The running maximum is a reference, not the maximum: it moves only when a score exceeds it by 2^6 (r likewise by 2), which
+// after the first rows is rare, so the steps carry no reduction.
 //
-// Work split: the 16-row steps of all (sequence, KV head) units form one line that is cut into equal pieces, one per CTA
+// Work split: the steps (one or two tiles) of all (sequence, KV head) units form one line that is cut into equal pieces, one per CTA
 // (persistent, one per SM), and a CTA deals its steps to its warps.  A unit that lies in one CTA is finished there; a unit
 // cut between CTAs leaves one partial result (maximum, sum, O) per CTA, and the CTA that arrives last adds them in the
 // order of the CTAs, so results do not depend on the order of arrival.  One launch, lengths read on the device.
 constexpr float KV4_LOG2E = 1.4426950408889634f;
-constexpr float KV4_SLACK = 10.0f;
+constexpr float KV4_SLACK = 6.0f;       // weights stay below 2^6 ...
+constexpr float KV4_BOOST = 64.f;       // ... and meet the scale 2^6 higher: p' below 2^13, normal fp16 down to 2^-20 of the largest
 
+// 2^x to two units in the last place (results below the normal range become zero)
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
   uint32_t d;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
   return d;
 }
+template <int NG> __device__ __forceinline__ void load_params(const unsigned char* p, uint32_t (&w)[NG]) {
+  if (NG == 4) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(p);
+  else if (NG == 2) *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(p);
+  else w[0] = *reinterpret_cast<const uint32_t*>(p);
+}
+
 template <int D, int NG, int NB>
 struct Kv4Tile {
-  static constexpr int WARPS = NB == 1 ? 16 : 8;
+  static constexpr int WARPS = 8;
+  // row tiles of a step: with one, the dependent chain of a step leaves the issue slots half empty at two warps per
+  // scheduler (more warps would need the registers that the accumulators hold)
+  static constexpr int RT = NB == 1 ? 2 : 1, ROWS = 16 * RT;
   static constexpr int NQ = 8 * NB;
   static constexpr int STAGES = 3;
-  // one step of 16 rows in shared memory; the rows of V are 16 bytes apart so that a fragment's four rows lie in distinct banks
-  static constexpr int KC = 0, VC = KC + 16 * (D / 2), VSTRIDE = D / 2 + 16, KP = VC + 16 * VSTRIDE, VP = KP + 16 * NG * 4;
-  static constexpr int STAGE_BYTES = VP + 16 * NG * 4;
+  // one step in shared memory; the rows of V are 16 bytes apart so that a fragment's four rows lie in distinct banks
+  static constexpr int KC = 0, VC = KC + ROWS * (D / 2), VSTRIDE = D / 2 + 16, KP = VC + ROWS * VSTRIDE, VP = KP + ROWS * NG * 4;
+  static constexpr int STAGE_BYTES = VP + ROWS * NG * 4;
   static constexpr int RING_BYTES = WARPS * STAGES * STAGE_BYTES;
   static constexpr int OSTRIDE = D + 4;            // floats between the queries of a warp's partial O
   static constexpr int O_BYTES = WARPS * NQ * OSTRIDE * 4;
@@ -254,7 +271,7 @@ __global__ void __launch_bounds__(Kv4Tile<D, NG, NB>::WARPS * 32, 1)
 kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qblocks, bf16* __restrict__ O, int64_t ldo,
                 float* __restrict__ part, int* __restrict__ arrived) {
   using T = Kv4Tile<D, NG, NB>;
-  constexpr int WARPS = T::WARPS, NQ = T::NQ, NT = D / 32;
+  constexpr int WARPS = T::WARPS, NQ = T::NQ, NT = D / 32, RT = T::RT, ROWS = T::ROWS;
   constexpr int GT = NT / NG;                      // 32-dim blocks of a group
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ int pre[SPTS_KV4_MAX_SEQ + 1];
@@ -265,7 +282,7 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
   const int G = H / c.Hkv, heads = c.Hkv * qblocks, per_block = NB == 1 ? G : 16;
 
   // ---- the line of steps
-  auto steps_of = [&](int b) { return b < c.n_seq ? (max(0, min(__ldg(&c.len[b]), c.capacity)) + 15) >> 4 : 0; };
+  auto steps_of = [&](int b) { return b < c.n_seq ? (max(0, min(__ldg(&c.len[b]), c.capacity)) + ROWS - 1) / ROWS : 0; };
   {
     int carry = 0;
     if (tid == 0) pre[0] = 0;
@@ -296,23 +313,30 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
   const long x0 = total * blockIdx.x / ctas, x1 = total * (blockIdx.x + 1) / ctas;
 
   unsigned char* ring = smem + warp * (T::STAGES * T::STAGE_BYTES);
-  const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
   float* sm_o = reinterpret_cast<float*>(smem + T::RING_BYTES);
-  auto fetch = [&](const Kv4Walk& w, int stage) {
-    const int kvh = w.u.h / qblocks;
-    const size_t row = ((size_t)w.u.b * c.Hkv + kvh) * c.capacity + 16 * (size_t)w.s;
-    const uint32_t dst = ring_s + stage * T::STAGE_BYTES;
-    const char* kc = c.k_codes + row * (D / 2);
-    const char* vc = c.v_codes + row * (D / 2);
+  // a lane's share of a step's copies: D / 64 pieces of 16 bytes of either code block, one of the params (K's, then V's)
+  const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
+  const uint32_t dst_k = ring_s + T::KC + 16 * lane, dst_v = ring_s + T::VC + (lane / (D / 32)) * T::VSTRIDE + (lane % (D / 32)) * 16;
+  const bool lane_p = lane < 4 * NG * RT;
+  const uint32_t dst_p = ring_s + T::KP + 16 * lane;
+  const char* src_k = nullptr; const char* src_v = nullptr; const char* src_kp = nullptr; const char* src_vp = nullptr;
+  auto point = [&](const Kv4Walk& w) {             // at the lane's share of the walk's step
+    const size_t row = ((size_t)w.u.b * c.Hkv + w.u.h / qblocks) * c.capacity + ROWS * (size_t)w.s;
+    src_k = c.k_codes + row * (D / 2) + 16 * lane;
+    src_v = c.v_codes + row * (D / 2) + 16 * lane;
+    src_kp = (const char*)(c.k_params + row * NG) + 16 * lane;
+    src_vp = (const char*)(c.v_params + row * NG) + 16 * lane;
+  };
+  uint32_t fetch_at = 0;                           // byte offset of the stage to fill
+  auto fetch = [&]() {
 #pragma unroll
-    for (int i = lane; i < D / 2; i += 32) {       // 16 rows x D / 32 pieces of 16 bytes
-      cp_async16(dst + T::KC + 16 * i, kc + 16 * i);
-      cp_async16(dst + T::VC + (i / (D / 32)) * T::VSTRIDE + (i % (D / 32)) * 16, vc + 16 * i);
+    for (int i = 0; i < D / 64 * RT; ++i) {
+      cp_async16(dst_k + fetch_at + 512 * i, src_k + 512 * i);
+      cp_async16(dst_v + fetch_at + 512 / (D / 2) * i * T::VSTRIDE, src_v + 512 * i);
     }
-    if (lane < 8 * NG) {
-      const int i = lane < 4 * NG ? lane : lane - 4 * NG;
-      const uint32_t* p = (lane < 4 * NG ? c.k_params : c.v_params) + row * NG + 4 * i;
-      cp_async16(dst + (lane < 4 * NG ? T::KP : T::VP) + 16 * i, p);
+    if (lane_p) {
+      cp_async16(dst_p + fetch_at, src_kp);
+      cp_async16(dst_p + fetch_at + (T::VP - T::KP), src_vp);
     }
   };
 
@@ -327,20 +351,31 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
   }
   int first_s;                                     // the stretch of the current unit begins here
   line.find(x0, first_s);
-  int fetch_stage = 0, use_stage = 0;
   bool fetching = ahead.more(line, warp);
-#pragma unroll
-  for (int i = 0; i < T::STAGES - 1; ++i) {
+  if (fetching) point(ahead);
+  auto fetch_next = [&]() {
     if (fetching) {
-      fetch(ahead, fetch_stage);
+      fetch();
       ahead.s += WARPS;
-      fetching = ahead.more(line, warp);
+      if (ahead.s < ahead.end) {
+        src_k += WARPS * ROWS * (D / 2);
+        src_v += WARPS * ROWS * (D / 2);
+        src_kp += WARPS * ROWS * NG * 4;
+        src_vp += WARPS * ROWS * NG * 4;
+      } else {
+        fetching = ahead.more(line, warp);
+        if (fetching) point(ahead);
+      }
     }
     cp_async_commit();
-    fetch_stage = fetch_stage + 1 == T::STAGES ? 0 : fetch_stage + 1;
-  }
+    fetch_at = fetch_at + T::STAGE_BYTES == T::STAGES * T::STAGE_BYTES ? 0 : fetch_at + T::STAGE_BYTES;
+  };
+#pragma unroll
+  for (int i = 0; i < T::STAGES - 1; ++i) fetch_next();
 
-  const float sl = rsqrtf((float)D) * KV4_LOG2E;
+  // scores stay as they come out of the products; sl brings them to powers of two inside the exponential's argument
+  const float sl = rsqrtf((float)D) * KV4_LOG2E, slack = KV4_SLACK / sl;
+  uint32_t use_at = 0;
   while (true) {
     // ---- one unit's stretch [first_s, now.end)
     const Kv4Unit u = now.u;
@@ -348,33 +383,48 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
     const int nq = min(per_block, G - (u.h % qblocks) * per_block);
     const int len = max(0, min(__ldg(&c.len[b]), c.capacity));
     const int end = now.end;
-    // Q as B fragments, and (-24 sum q, sum q) of every group in two bf16 pieces
+    // Q as B fragments, and (-8 sum q, sum q) of every group in two bf16 pieces, all times the query's power of two; slq
+    // brings a score in those units to a power of two's exponent
     uint32_t qf[NB][NT][4], qm[NB][2];
+    float slq[NB][2];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      float sums[NG];
-#pragma unroll
-      for (int i = 0; i < NG; ++i) sums[i] = 0.f;
       const int qi = 8 * nb + g;
+      float x[NT][8], top = 0.f;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (qi < nq) load8(Q + (size_t)b * ldq + (size_t)(hb + qi) * D + 32 * t + 8 * cc, x);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) qf[nb][t][j] = pack2(x[j], x[j + 4]);
-        float s8 = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+        for (int j = 0; j < 8; ++j) x[t][j] = 0.f;
+        if (qi < nq) load8(Q + (size_t)b * ldq + (size_t)(hb + qi) * D + 32 * t + 8 * cc, x[t]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[t][j]));
+      }
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const float qs = scale_to_2_13(top);
+      float mine = 0.f, sum = 0.f;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float f = (j & 1) ? qs * ODD : qs;
+          qf[nb][t][j] = pack2_f16(x[t][j] * f, x[t][j + 4] * f);
+        }
+        float s8 = ((x[t][0] + x[t][1]) + (x[t][2] + x[t][3])) + ((x[t][4] + x[t][5]) + (x[t][6] + x[t][7]));
         s8 += __shfl_xor_sync(0xffffffffu, s8, 1);
         s8 += __shfl_xor_sync(0xffffffffu, s8, 2);
-        sums[t / GT] += s8;
+        sum = t % GT == 0 ? s8 : sum + s8;
+        if (cc == t / GT) mine = sum;
       }
-      float mine = 0.f;
-#pragma unroll
-      for (int i = 0; i < NG; ++i) if (cc == i) mine = sums[i];
-      const float a = -CODE_BIAS * mine, ah = round_bf16(a), mh = round_bf16(mine);
+      const float u = qs * CODE_UNIT, a = -8.f * mine * u, ah = round_bf16(a), sm = mine * u, mh = round_bf16(sm);
       qm[nb][0] = pack2(ah, mh);
-      qm[nb][1] = pack2(a - ah, mine - mh);
+      qm[nb][1] = pack2(a - ah, sm - mh);
+      const float mysl = sl / u;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) slq[nb][i] = __shfl_sync(0xffffffffu, mysl, 4 * (2 * cc + i));
     }
-    float o[NB][NT][2][4], oz[NB][NG][4], om[NB][4], m[NB][2], l[NB][2];
+    float o[NB][NT][2][4], oz[NB][NG][4], om[NB][4], thr[NB][2], msl[NB][2], l[NB][2];    // thr: where the reference moves
+    float r_inv = KV4_BOOST, r_lim = 0.f;         // 2^6 / r, and the scale where r moves
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
@@ -385,165 +435,193 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
 #pragma unroll
         for (int t = 0; t < NG; ++t) oz[nb][t][i] = 0.f;
       }
-      m[nb][0] = m[nb][1] = -INFINITY;
+      thr[nb][0] = thr[nb][1] = msl[nb][0] = msl[nb][1] = -INFINITY;
       l[nb][0] = l[nb][1] = 0.f;
     }
     for (; now.s < end; now.s += WARPS) {
-      if (fetching) {
-        fetch(ahead, fetch_stage);
-        ahead.s += WARPS;
-        fetching = ahead.more(line, warp);
-      }
-      cp_async_commit();
-      fetch_stage = fetch_stage + 1 == T::STAGES ? 0 : fetch_stage + 1;
+      fetch_next();
       cp_async_wait<T::STAGES - 1>();
       __syncwarp();
-      unsigned char* st = ring + use_stage * T::STAGE_BYTES;
-      use_stage = use_stage + 1 == T::STAGES ? 0 : use_stage + 1;
-      const int valid = len - 16 * now.s;          // rows of this step that are held
-      if (valid < 16) {
+      unsigned char* st = ring + use_at;
+      use_at = use_at + T::STAGE_BYTES == T::STAGES * T::STAGE_BYTES ? 0 : use_at + T::STAGE_BYTES;
+      const int valid = len - ROWS * now.s;        // rows of this step that are held
+      if (valid < ROWS) {
         // what lies behind the last row may be anything: its params become zero (its codes are finite whatever they are)
-        for (int i = valid * NG + lane; i < 16 * NG; i += 32) {
+        for (int i = valid * NG + lane; i < ROWS * NG; i += 32) {
           reinterpret_cast<uint32_t*>(st + T::KP)[i] = 0u;
           reinterpret_cast<uint32_t*>(st + T::VP)[i] = 0u;
         }
         __syncwarp();
       }
       // ---- S
-      uint32_t kw0[NT], kw1[NT];
-      if (NT == 4) {
-        *reinterpret_cast<uint4*>(kw0) = *reinterpret_cast<const uint4*>(st + T::KC + g * (D / 2) + cc * 16);
-        *reinterpret_cast<uint4*>(kw1) = *reinterpret_cast<const uint4*>(st + T::KC + (g + 8) * (D / 2) + cc * 16);
-      } else {
-        *reinterpret_cast<uint2*>(kw0) = *reinterpret_cast<const uint2*>(st + T::KC + g * (D / 2) + cc * 8);
-        *reinterpret_cast<uint2*>(kw1) = *reinterpret_cast<const uint2*>(st + T::KC + (g + 8) * (D / 2) + cc * 8);
-      }
-      float sc[NB][4];
-      const uint32_t* kp0 = reinterpret_cast<const uint32_t*>(st + T::KP) + g * NG;
-      const uint32_t* kp1 = kp0 + 8 * NG;
-      const uint32_t pw0 = cc < NG ? kp0[cc < NG ? cc : 0] : 0u, pw1 = cc < NG ? kp1[cc < NG ? cc : 0] : 0u;
+      float sc[RT][NB][4];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sc[nb][i] = 0.f;
-        mma16816(sc[nb], pw0, pw1, pw0, pw1, qm[nb][0], qm[nb][1]);
-      }
-#pragma unroll
-      for (int gr = 0; gr < NG; ++gr) {
-        float acc[NB][4];
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[nb][i] = 0.f;
-#pragma unroll
-        for (int tt = 0; tt < GT; ++tt) {
-          const int t = gr * GT + tt;
-          const uint32_t a0 = code_pair<0>(kw0[t]), a1 = code_pair<0>(kw1[t]), a2 = code_pair<1>(kw0[t]), a3 = code_pair<1>(kw1[t]);
-          const uint32_t b0 = code_pair<2>(kw0[t]), b1 = code_pair<2>(kw1[t]), b2 = code_pair<3>(kw0[t]), b3 = code_pair<3>(kw1[t]);
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-            mma16816(acc[nb], a0, a1, a2, a3, qf[nb][t][0], qf[nb][t][1]);
-            mma16816(acc[nb], b0, b1, b2, b3, qf[nb][t][2], qf[nb][t][3]);
-          }
+      for (int rt = 0; rt < RT; ++rt) {
+        const int r0 = 16 * rt + g, r1 = r0 + 8;
+        uint32_t kw0[NT], kw1[NT], kp0[NG], kp1[NG];
+        if (NT == 4) {
+          *reinterpret_cast<uint4*>(kw0) = *reinterpret_cast<const uint4*>(st + T::KC + r0 * (D / 2) + cc * 16);
+          *reinterpret_cast<uint4*>(kw1) = *reinterpret_cast<const uint4*>(st + T::KC + r1 * (D / 2) + cc * 16);
+        } else {
+          *reinterpret_cast<uint2*>(kw0) = *reinterpret_cast<const uint2*>(st + T::KC + r0 * (D / 2) + cc * 8);
+          *reinterpret_cast<uint2*>(kw1) = *reinterpret_cast<const uint2*>(st + T::KC + r1 * (D / 2) + cc * 8);
         }
-        const float s0 = lo_bf16(kp0[gr]), s1 = lo_bf16(kp1[gr]);
+        load_params<NG>(st + T::KP + r0 * NG * 4, kp0);
+        load_params<NG>(st + T::KP + r1 * NG * 4, kp1);
+        uint32_t pw0 = 0u, pw1 = 0u;
+        if (cc < NG) {
+          pw0 = *reinterpret_cast<const uint32_t*>(st + T::KP + (r0 * NG + cc) * 4);
+          pw1 = *reinterpret_cast<const uint32_t*>(st + T::KP + (r1 * NG + cc) * 4);
+        }
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          sc[nb][0] = fmaf(s0, acc[nb][0], sc[nb][0]); sc[nb][1] = fmaf(s0, acc[nb][1], sc[nb][1]);
-          sc[nb][2] = fmaf(s1, acc[nb][2], sc[nb][2]); sc[nb][3] = fmaf(s1, acc[nb][3], sc[nb][3]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sc[rt][nb][i] = 0.f;
+          mma16816(sc[rt][nb], pw0, pw1, pw0, pw1, qm[nb][0], qm[nb][1]);
+        }
+#pragma unroll
+        for (int gr = 0; gr < NG; ++gr) {
+          float acc[NB][4];
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[nb][i] = 0.f;
+#pragma unroll
+          for (int tt = 0; tt < GT; ++tt) {
+            const int t = gr * GT + tt;
+            const uint32_t a0 = code_pair<0>(kw0[t]), a1 = code_pair<0>(kw1[t]), a2 = code_pair<1>(kw0[t]), a3 = code_pair<1>(kw1[t]);
+            const uint32_t b0 = code_pair<2>(kw0[t]), b1 = code_pair<2>(kw1[t]), b2 = code_pair<3>(kw0[t]), b3 = code_pair<3>(kw1[t]);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+              mma_f16(acc[nb], a0, a1, a2, a3, qf[nb][t][0], qf[nb][t][1]);
+              mma_f16(acc[nb], b0, b1, b2, b3, qf[nb][t][2], qf[nb][t][3]);
+            }
+          }
+          const float s0 = lo_bf16(kp0[gr]), s1 = lo_bf16(kp1[gr]);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            float (&x)[4] = sc[rt][nb];
+            x[0] = fmaf(s0, acc[nb][0], x[0]); x[1] = fmaf(s0, acc[nb][1], x[1]);
+            x[2] = fmaf(s1, acc[nb][2], x[2]); x[3] = fmaf(s1, acc[nb][3], x[3]);
+          }
         }
       }
       // ---- weights (in powers of two)
-      if (valid < 16) {
+      if (valid < ROWS) {
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          if (g >= valid) { sc[nb][0] = -INFINITY; sc[nb][1] = -INFINITY; }
-          if (g + 8 >= valid) { sc[nb][2] = -INFINITY; sc[nb][3] = -INFINITY; }
-        }
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            if (16 * rt + g >= valid) { sc[rt][nb][0] = -INFINITY; sc[rt][nb][1] = -INFINITY; }
+            if (16 * rt + g + 8 >= valid) { sc[rt][nb][2] = -INFINITY; sc[rt][nb][3] = -INFINITY; }
+          }
       }
-      bool over = false;
+      uint32_t vp0[RT][NG], vp1[RT][NG];
+      float top_s = 0.f, top[NB][2];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
+      for (int nb = 0; nb < NB; ++nb) top[nb][0] = top[nb][1] = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          sc[nb][i] *= sl; sc[nb][2 + i] *= sl;
-          over = over || fmaxf(sc[nb][i], sc[nb][2 + i]) > m[nb][i] + KV4_SLACK;
-        }
+      for (int rt = 0; rt < RT; ++rt) {
+        load_params<NG>(st + T::VP + (16 * rt + g) * NG * 4, vp0[rt]);
+        load_params<NG>(st + T::VP + (16 * rt + g + 8) * NG * 4, vp1[rt]);
+#pragma unroll
+        for (int gr = 0; gr < NG; ++gr) top_s = fmaxf(top_s, fmaxf(lo_bf16(vp0[rt][gr]), lo_bf16(vp1[rt][gr])));
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) top[nb][i] = fmaxf(top[nb][i], fmaxf(sc[rt][nb][i], sc[rt][nb][2 + i]));
+      }
+      bool over = top_s > r_lim;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) over = over || top[nb][0] > thr[nb][0] || top[nb][1] > thr[nb][1];
       if (__any_sync(0xffffffffu, over)) {
+        top_s = warp_max(top_s);
+        float fr = 1.f;
+        if (top_s > r_lim) {
+          const float inv = scale_to_2_13(top_s) * (KV4_BOOST / 8192.f);       // 2^6 / r with r in (top_s / 2, top_s]
+          fr = r_lim == 0.f ? 0.f : inv / r_inv;
+          r_inv = inv;
+          r_lim = 2.f * top_s;
+        }
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            float x = fmaxf(sc[nb][i], sc[nb][2 + i]);
+            float x = top[nb][i];
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-            const float mn = fmaxf(m[nb][i], x);
-            const float f = m[nb][i] == mn ? 1.f : exp2f(m[nb][i] - mn);
-            m[nb][i] = mn;
+            x *= slq[nb][i];
+            const float mn = fmaxf(msl[nb][i], x);
+            const float f = msl[nb][i] == mn ? 1.f : exp2f(msl[nb][i] - mn), fo = f * fr;
+            msl[nb][i] = mn;
+            thr[nb][i] = (mn + KV4_SLACK) / slq[nb][i];
             l[nb][i] *= f;
             om[nb][i] *= f; om[nb][2 + i] *= f;
 #pragma unroll
-            for (int t = 0; t < NG; ++t) { oz[nb][t][i] *= f; oz[nb][t][2 + i] *= f; }
+            for (int t = 0; t < NG; ++t) { oz[nb][t][i] *= fo; oz[nb][t][2 + i] *= fo; }
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-              for (int j = 0; j < 2; ++j) { o[nb][t][j][i] *= f; o[nb][t][j][2 + i] *= f; }
+              for (int j = 0; j < 2; ++j) { o[nb][t][j][i] *= fo; o[nb][t][j][2 + i] *= fo; }
           }
       }
-      const uint32_t* vp0 = reinterpret_cast<const uint32_t*>(st + T::VP) + g * NG;
-      const uint32_t* vp1 = vp0 + 8 * NG;
-      uint32_t pb[NB][NG][2], pu[NB][2];
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        float p[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = exp2f(sc[nb][i] - m[nb][i & 1]);
-        l[nb][0] += p[0] + p[2];
-        l[nb][1] += p[1] + p[3];
-        pu[nb][0] = transpose8x8(pack2(p[0], p[1]));
-        pu[nb][1] = transpose8x8(pack2(p[2], p[3]));
-#pragma unroll
-        for (int gr = 0; gr < NG; ++gr) {
-          const float s0 = lo_bf16(vp0[gr]), s1 = lo_bf16(vp1[gr]);
-          pb[nb][gr][0] = transpose8x8(pack2(p[0] * s0, p[1] * s0));
-          pb[nb][gr][1] = transpose8x8(pack2(p[2] * s1, p[3] * s1));
-        }
-      }
       // ---- O
-      {
-        // mids: A row r holds group r % NG
-        const uint32_t* vm = reinterpret_cast<const uint32_t*>(st + T::VP) + (g % NG);
-        const uint32_t a0 = __byte_perm(vm[2 * cc * NG], vm[(2 * cc + 1) * NG], 0x7632);
-        const uint32_t a2 = __byte_perm(vm[(2 * cc + 8) * NG], vm[(2 * cc + 9) * NG], 0x7632);
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) mma16816(om[nb], a0, 0u, a2, 0u, pu[nb][0], pu[nb][1]);
-      }
-      uint32_t vw[4][NT / 2];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const unsigned char* r = st + T::VC + (8 * (i >> 1) + 2 * cc + (i & 1)) * T::VSTRIDE + g * (D / 16);
-        if (NT == 4) *reinterpret_cast<uint2*>(vw[i]) = *reinterpret_cast<const uint2*>(r);
-        else vw[i][0] = *reinterpret_cast<const uint32_t*>(r);
-      }
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const uint32_t sel = (t & 1) ? 0x7632u : 0x5410u;
-        const uint32_t x01 = __byte_perm(vw[0][t / 2], vw[1][t / 2], sel), x23 = __byte_perm(vw[2][t / 2], vw[3][t / 2], sel);
-        const uint32_t a0 = code_pair<0>(x01), a1 = code_pair<1>(x01), a2 = code_pair<0>(x23), a3 = code_pair<1>(x23);
-        const uint32_t b0 = code_pair<2>(x01), b1 = code_pair<3>(x01), b2 = code_pair<2>(x23), b3 = code_pair<3>(x23);
+      for (int rt = 0; rt < RT; ++rt) {
+        uint32_t pb[NB][NG][2], pu[NB][2];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          mma16816(o[nb][t][0], a0, a1, a2, a3, pb[nb][t / GT][0], pb[nb][t / GT][1]);
-          mma16816(o[nb][t][1], b0, b1, b2, b3, pb[nb][t / GT][0], pb[nb][t / GT][1]);
+          float p[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[i] = exp2_fast(fmaf(sc[rt][nb][i], slq[nb][i & 1], -msl[nb][i & 1]));
+          l[nb][0] += p[0] + p[2];
+          l[nb][1] += p[1] + p[3];
+          pu[nb][0] = transpose8x8(pack2(p[0], p[1]));
+          pu[nb][1] = transpose8x8(pack2(p[2], p[3]));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[i] *= r_inv;
+#pragma unroll
+          for (int gr = 0; gr < NG; ++gr) {
+            const float s0 = lo_bf16(vp0[rt][gr]), s1 = lo_bf16(vp1[rt][gr]);
+            pb[nb][gr][0] = transpose8x8(pack2_f16(p[0] * s0, p[1] * s0));
+            pb[nb][gr][1] = transpose8x8(pack2_f16(p[2] * s1, p[3] * s1));
+          }
         }
+        {
+          // mids: A row r holds group r % NG
+          const uint32_t* vm = reinterpret_cast<const uint32_t*>(st + T::VP) + 16 * rt * NG + (g % NG);
+          const uint32_t a0 = __byte_perm(vm[2 * cc * NG], vm[(2 * cc + 1) * NG], 0x7632);
+          const uint32_t a2 = __byte_perm(vm[(2 * cc + 8) * NG], vm[(2 * cc + 9) * NG], 0x7632);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) mma16816(om[nb], a0, 0u, a2, 0u, pu[nb][0], pu[nb][1]);
+        }
+        uint32_t vw[4][NT / 2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const unsigned char* r = st + T::VC + (16 * rt + 8 * (i >> 1) + 2 * cc + (i & 1)) * T::VSTRIDE + g * (D / 16);
+          if (NT == 4) *reinterpret_cast<uint2*>(vw[i]) = *reinterpret_cast<const uint2*>(r);
+          else vw[i][0] = *reinterpret_cast<const uint32_t*>(r);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const uint32_t sel = (t & 1) ? 0x7632u : 0x5410u;
+          const uint32_t x01 = __byte_perm(vw[0][t / 2], vw[1][t / 2], sel), x23 = __byte_perm(vw[2][t / 2], vw[3][t / 2], sel);
+          const uint32_t a0 = code_pair<0>(x01), a1 = code_pair<1>(x01), a2 = code_pair<0>(x23), a3 = code_pair<1>(x23);
+          const uint32_t b0 = code_pair<2>(x01), b1 = code_pair<3>(x01), b2 = code_pair<2>(x23), b3 = code_pair<3>(x23);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            mma_f16(o[nb][t][0], a0, a1, a2, a3, pb[nb][t / GT][0], pb[nb][t / GT][1]);
+            mma_f16(o[nb][t][1], b0, b1, b2, b3, pb[nb][t / GT][0], pb[nb][t / GT][1]);
+          }
+        }
+        // -8 in the units of the even (A rows 0..7) and the odd codes (rows 8..15)
+#pragma unroll
+        for (int gr = 0; gr < NG; ++gr)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+            mma_f16(oz[nb][gr], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, pb[nb][gr][0], pb[nb][gr][1]);
       }
-#pragma unroll
-      for (int gr = 0; gr < NG; ++gr)
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-          mma16816(oz[nb][gr], MINUS_BIAS_BF16X2, MINUS_BIAS_BF16X2, MINUS_BIAS_BF16X2, MINUS_BIAS_BF16X2, pb[nb][gr][0],
-                   pb[nb][gr][1]);
       __syncwarp();                                // the stage may be filled again
     }
     // ---- the warps' results meet
@@ -555,18 +633,20 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
         s += __shfl_xor_sync(0xffffffffu, s, 4);
         s += __shfl_xor_sync(0xffffffffu, s, 8);
         s += __shfl_xor_sync(0xffffffffu, s, 16);
-        if (g == 0) { sm_m[warp][8 * nb + 2 * cc + i] = m[nb][i]; sm_l[warp][8 * nb + 2 * cc + i] = s; }
+        if (g == 0) { sm_m[warp][8 * nb + 2 * cc + i] = msl[nb][i]; sm_l[warp][8 * nb + 2 * cc + i] = s; }
       }
+      const float even = CODE_UNIT_INV / r_inv, odd = even * ODD;       // back from the codes' units; r_inv holds the boost
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         // lane (group, cc) of the mids' tile holds queries 2 cc, 2 cc + 1
-        const float z0 = __shfl_sync(0xffffffffu, om[nb][0], (t / GT) * 4 + cc) + oz[nb][t / GT][0];
-        const float z1 = __shfl_sync(0xffffffffu, om[nb][1], (t / GT) * 4 + cc) + oz[nb][t / GT][1];
+        const float z0 = __shfl_sync(0xffffffffu, om[nb][0], (t / GT) * 4 + cc), z1 = __shfl_sync(0xffffffffu, om[nb][1], (t / GT) * 4 + cc);
+        const float* oz_t = oz[nb][t / GT];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
+          const float* ov = o[nb][t][j];
           float* dst = sm_o + (size_t)(warp * NQ + 8 * nb + 2 * cc) * T::OSTRIDE + 32 * t + 4 * g + 2 * j;
-          *reinterpret_cast<float2*>(dst) = make_float2(o[nb][t][j][0] + z0, o[nb][t][j][2] + z0);
-          *reinterpret_cast<float2*>(dst + T::OSTRIDE) = make_float2(o[nb][t][j][1] + z1, o[nb][t][j][3] + z1);
+          *reinterpret_cast<float2*>(dst) = make_float2(fmaf(ov[0] + oz_t[0], even, z0), fmaf(ov[2] + oz_t[2], odd, z0));
+          *reinterpret_cast<float2*>(dst + T::OSTRIDE) = make_float2(fmaf(ov[1] + oz_t[1], even, z1), fmaf(ov[3] + oz_t[3], odd, z1));
         }
       }
     }

@@ -124,6 +124,10 @@ spts_status launch_plain(spts_ctx* ctx, const W4GemvArgs& a) {
 // ring of asynchronous copies runs on across tiles, so the memory system never drains at a tile's end.
 // Order of k inside a 32-block: any order serves a dot product, so lane (g, c) takes the eight consecutive codes 8c .. 8c + 7
 // of its row (one word) and the eight consecutive x of its token (one 16-byte load).
+template <int J> __device__ __forceinline__ uint32_t code_pair16(uint32_t w) {
+  const uint32_t s = J == 0 ? w << 3 : w >> (4 * J - 3);
+  return (s & 0x00780078u) | 0x41804180u;
+}
 constexpr int W4_WARPS = 8;
 constexpr int W4_CHUNK = 128;
 
@@ -234,8 +238,8 @@ w4_gemv_kernel(const char* __restrict__ codes, const uint32_t* __restrict__ para
             const uint4 v = xw[nb][t];
             b[nb][0] = __byte_perm(v.x, v.z, 0x5410); b[nb][1] = __byte_perm(v.x, v.z, 0x7632);
             b[nb][2] = __byte_perm(v.y, v.w, 0x5410); b[nb][3] = __byte_perm(v.y, v.w, 0x7632);
-            mma16816(xs[nb], ONE_BF16X2, ONE_BF16X2, ONE_BF16X2, ONE_BF16X2, b[nb][0], b[nb][1]);
-            mma16816(xs[nb], ONE_BF16X2, ONE_BF16X2, ONE_BF16X2, ONE_BF16X2, b[nb][2], b[nb][3]);
+            mma16816(xs[nb], 0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u, b[nb][0], b[nb][1]);
+            mma16816(xs[nb], 0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u, b[nb][2], b[nb][3]);
             if (first && norm) {
               const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -247,8 +251,8 @@ w4_gemv_kernel(const char* __restrict__ codes, const uint32_t* __restrict__ para
             const unsigned char* base = st + mt * T::SUB + 16 * t + 4 * cc;
             const uint32_t w0 = *reinterpret_cast<const uint32_t*>(base + g * T::CSTRIDE);
             const uint32_t w1 = *reinterpret_cast<const uint32_t*>(base + (g + 8) * T::CSTRIDE);
-            const uint32_t a0 = code_pair<0>(w0), a1 = code_pair<0>(w1), a2 = code_pair<1>(w0), a3 = code_pair<1>(w1);
-            const uint32_t c0 = code_pair<2>(w0), c1 = code_pair<2>(w1), c2 = code_pair<3>(w0), c3 = code_pair<3>(w1);
+            const uint32_t a0 = code_pair16<0>(w0), a1 = code_pair16<0>(w1), a2 = code_pair16<1>(w0), a3 = code_pair16<1>(w1);
+            const uint32_t c0 = code_pair16<2>(w0), c1 = code_pair16<2>(w1), c2 = code_pair16<3>(w0), c3 = code_pair16<3>(w1);
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
               mma16816(acc[nb][mt], a0, a1, a2, a3, b[nb][0], b[nb][1]);
@@ -261,7 +265,7 @@ w4_gemv_kernel(const char* __restrict__ codes, const uint32_t* __restrict__ para
           const uint32_t* pw = reinterpret_cast<const uint32_t*>(st + mt * T::SUB + T::PARAMS) + gr;
           const uint32_t p0 = pw[g * NGC], p1 = pw[(g + 8) * NGC];
           const float s0 = lo_bf16(p0), s1 = lo_bf16(p1);
-          const float m0 = fmaf(-CODE_BIAS, s0, hi_bf16(p0)), m1 = fmaf(-CODE_BIAS, s1, hi_bf16(p1));
+          const float m0 = fmaf(-24.f, s0, hi_bf16(p0)), m1 = fmaf(-24.f, s1, hi_bf16(p1));
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll

@@ -2,6 +2,8 @@
 // quantiser's definition).  Shared by the weight and the KV-cache kernels.
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include "spts_common.cuh"
 
 namespace spts {
@@ -35,15 +37,32 @@ __device__ __forceinline__ void store8(bf16* p, const float* x) {
 }
 
 // ---- matrix instructions on codes
-// Codes become bf16 without arithmetic: code << 3 in the mantissa of 16.0 is exactly 16 + code, one shift and one logic
-// operation per two codes.  J-th codes of the two halves of a word: (16 + low, 16 + high).
+// A nibble in the low mantissa bits of an fp16 whose other bits are zero IS a number: code * 2^-24 in bits 0..3 and
+// code * 2^-20 in bits 4..7 (subnormals, and exact; the matrix units take them as they are).  So the eight codes of a word
+// become four registers of two fp16 with four masks and one shift, without a bias or a conversion.  J-th codes of the two
+// 16-bit halves, times 2^-24 (J even) or 2^-20 (J odd):
 template <int J> __device__ __forceinline__ uint32_t code_pair(uint32_t w) {
-  const uint32_t s = J == 0 ? w << 3 : w >> (4 * J - 3);
-  return (s & 0x00780078u) | 0x41804180u;
+  const uint32_t s = J < 2 ? w : w >> 8;
+  return s & ((J & 1) ? 0x00F000F0u : 0x000F000Fu);
 }
-constexpr float CODE_BIAS = 24.f;               // 16 of the mantissa trick + 8 of the format
-constexpr uint32_t MINUS_BIAS_BF16X2 = 0xC1C0C1C0u;
-constexpr uint32_t ONE_BF16X2 = 0x3F803F80u;
+constexpr float CODE_UNIT = 5.9604644775390625e-08f;        // 2^-24
+constexpr float CODE_UNIT_INV = 16777216.f;                 // 2^24
+constexpr float ODD = 0.0625f;                              // what a factor of an odd J is multiplied by to be in the same unit
+// The power of two that brings `top` (>= 0) to [2^13, 2^14), held within 2^-100 .. 2^120; 1 for zero, infinity and NaN.
+__device__ __forceinline__ float scale_to_2_13(float top) {
+  const int e = (int)(__float_as_uint(top) >> 23);          // biased exponent
+  if (e == 0 || e >= 255) return e == 0 && top > 0.f ? 1.329227995784916e36f : 1.f;
+  return __uint_as_float((uint32_t)(127 + max(-100, min(120, 13 + 127 - e))) << 23);
+}
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack2_f16(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
