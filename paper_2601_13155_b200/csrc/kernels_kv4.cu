@@ -18,27 +18,33 @@ struct Kv4Dev {
   int n_seq, capacity, group, Hkv;
 };
 
-// One unit = one (row, KV head, K or V): D / 8 lanes, eight dims each; quantised, its words stored in the cache's order.
-template <typename T, int D>
+// One unit = one (row, KV head) of K or of V: D / 8 lanes, eight dims each, 256 / D units to a warp pass; quantised, its words
+// stored in the cache's order.  A warp takes up to `per` passes of one row (blockIdx.y: which, and of K or V), so that the row's
+// sequence is looked up once and the pointers only move.
+// Memory asks for 27 us at 24,600 rows of 8 heads x 128 (each element read once, codes, params and values written once); the
+// quantiser's instructions bound it instead.
+template <typename T, int D, int LANES>
 __global__ void __launch_bounds__(256)
 kv4_append_kernel(Kv4Dev c, const T* __restrict__ K, int64_t ldk, const T* __restrict__ V, int64_t ldv,
                   const int32_t* __restrict__ pos, const int32_t* __restrict__ row_start, const int32_t* __restrict__ at,
-                  int n_rows, T* __restrict__ K_read, T* __restrict__ V_read, int* status) {
-  constexpr int LPR = D / 8;                       // lanes per unit
-  const int sub = threadIdx.x % LPR;
-  const int units = 2 * c.Hkv;
-  const long total = (long)n_rows * units;
-  const long u0 = ((long)blockIdx.x * 256 + threadIdx.x) / LPR, stride = (long)gridDim.x * 256 / LPR;
-  const long first = ((long)blockIdx.x * 256 + (threadIdx.x & ~31)) / LPR;      // the warp's first unit
-  for (long step = 0; first + step < total; step += stride) {
-    const long u = u0 + step;
-    const int row = u < total ? (int)(u / units) : 0;
-    const int which = (int)(u % units);
-    const int kvh = which >> 1;
-    const bool is_v = which & 1;
+                  int n_rows, int per, T* __restrict__ K_read, T* __restrict__ V_read, int* status) {
+  constexpr int LPR = D / 8, UPW = 32 / LPR;       // lanes per unit, units per warp pass
+  const int lane = threadIdx.x & 31, sub = lane % LPR;
+  const int passes = (c.Hkv + UPW - 1) / UPW, parts = (passes + per - 1) / per;
+  const bool is_v = (int)blockIdx.y >= parts;
+  const int p0 = ((int)blockIdx.y - (is_v ? parts : 0)) * per, p1 = min(passes, p0 + per);
+  const T* src0 = (is_v ? V : K) + p0 * 256 + 8 * lane;
+  T* read0 = is_v ? V_read : K_read;
+  const int64_t ld = is_v ? ldv : ldk;
+  char* codes0 = is_v ? c.v_codes : c.k_codes;
+  uint32_t* params0 = is_v ? c.v_params : c.k_params;
+  // dims 32 t + 8 q .. of a row are word q D / 32 + t of a key; of a value they are two halfwords D / 16 bytes apart, and the
+  // lanes of blocks t and t ^ 1 exchange one each to store whole words
+  const int t = sub >> 2, q = sub & 3;
+  const int at_word = is_v ? (2 * q + (t & 1)) * (D / 64) + (t >> 1) : q * (D / 32) + t;
+  for (int row = blockIdx.x * 8 + (threadIdx.x >> 5); row < n_rows; row += gridDim.x * 8) {
     // the sequence that owns the row: the last b with row_start[b] <= row
     int b = row, first_row = row;
-    bool in = u < total;
     if (row_start != nullptr) {
       int lo = 0, hi = c.n_seq;
       while (hi - lo > 1) {
@@ -47,37 +53,49 @@ kv4_append_kernel(Kv4Dev c, const T* __restrict__ K, int64_t ldk, const T* __res
       }
       b = lo;
       first_row = __ldg(&row_start[b]);
-      in = in && row >= first_row && row < __ldg(&row_start[b + 1]);
+      if (row < first_row || row >= __ldg(&row_start[b + 1])) continue;
     }
-    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (in) load8((is_v ? V + (size_t)row * ldv : K + (size_t)row * ldk) + kvh * D + 8 * sub, x);
-    uint32_t p;
-    bool bad;
-    float read[8];
-    const uint32_t w = quantize8(x, c.group / 8, p, read, bad);
-    if (!in) continue;
-    if (K_read != nullptr || V_read != nullptr) {
-      T* dst = is_v ? V_read : K_read;
-      if (dst != nullptr) store8(dst + ((size_t)row * c.Hkv + kvh) * D + 8 * sub, read);
+    const long slot = (long)(at != nullptr ? __ldg(&at[b]) : __ldg(&c.len[b])) + (row - first_row);
+    const bool room = slot >= 0 && slot < c.capacity;
+    if (!room && lane == 0) set_status(status, SPTS_ERR_WORKSPACE);
+    if (pos != nullptr && c.pos != nullptr && room && blockIdx.y == 0 && lane == 0) c.pos[(size_t)b * c.capacity + slot] = pos[row];
+    int kvh = p0 * UPW + lane / LPR;
+    const T* src = src0 + (size_t)row * ld;
+    T* read_to = read0 != nullptr ? read0 + (size_t)row * c.Hkv * D + p0 * 256 + 8 * lane : nullptr;
+    const size_t r = ((size_t)b * c.Hkv + kvh) * c.capacity + (room ? slot : 0);
+    uint32_t* codes = reinterpret_cast<uint32_t*>(codes0 + r * (D / 2)) + at_word;
+    uint32_t* params = params0 + r * (LPR / LANES) + sub / LANES;
+    Raw8<T> next;                                  // the next pass's elements are on their way while this one's are quantised
+    next.zero();
+    if (kvh < c.Hkv) next.load(src);
+    for (int p = p0; p < p1; ++p) {
+      const bool in = kvh < c.Hkv;
+      float x[8];
+      next.get(x);
+      if (p + 1 < p1 && kvh + UPW < c.Hkv) next.load(src + 256);
+      else next.zero();
+      uint32_t prm;
+      bool bad;
+      float read[8];
+      uint32_t w = quantize8<LANES>(K, x, prm, read, bad);
+      if (is_v) {
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, (t & 1) ? w : w >> 16, 4);
+        w = (t & 1) ? __byte_perm(other, w, 0x7610) : __byte_perm(w, other, 0x5410);
+      }
+      if (in) {
+        if (bad) set_status(status, SPTS_ERR_NONFINITE);
+        if (read_to != nullptr) store8(read_to, read);
+        if (room) {
+          *codes = w;
+          if (sub % LANES == 0) *params = prm;
+        }
+      }
+      kvh += UPW;
+      src += 256;
+      if (read_to != nullptr) read_to += 256;
+      codes += (size_t)UPW * c.capacity * (D / 8);
+      params += (size_t)UPW * c.capacity * (LPR / LANES);
     }
-    const long slot = (long)(at != nullptr ? __ldg(&at[b]) : c.len[b]) + (row - first_row);
-    if (bad) set_status(status, SPTS_ERR_NONFINITE);
-    if (slot < 0 || slot >= c.capacity) {
-      if (sub == 0) set_status(status, SPTS_ERR_WORKSPACE);
-      continue;
-    }
-    const size_t r = ((size_t)b * c.Hkv + kvh) * c.capacity + slot;
-    const int t = sub >> 2, q = sub & 3;           // dims 32 t + 8 q .. + 7
-    if (!is_v) {
-      reinterpret_cast<uint32_t*>(c.k_codes + r * (D / 2))[q * (D / 32) + t] = w;
-    } else {
-      uint16_t* v = reinterpret_cast<uint16_t*>(c.v_codes + r * (D / 2));
-      v[2 * q * (D / 32) + t] = (uint16_t)w;
-      v[(2 * q + 1) * (D / 32) + t] = (uint16_t)(w >> 16);
-    }
-    const int lanes = c.group / 8;
-    if (sub % lanes == 0) (is_v ? c.v_params : c.k_params)[r * (D / c.group) + sub / lanes] = p;
-    if (pos != nullptr && c.pos != nullptr && which == 0 && sub == 0) c.pos[(size_t)b * c.capacity + slot] = pos[row];
   }
 }
 
@@ -759,10 +777,14 @@ spts_status append_t(spts_ctx* ctx, const spts_kv4_cache* cache, const void* K, 
                      const int32_t* pos, const int32_t* row_start, const int32_t* at, int n_rows, void* K_read, void* V_read) {
   const Kv4Dev c = kv4_dev(ctx, cache);
   if (n_rows > 0) {
-    long blocks = ((long)n_rows * 2 * c.Hkv * (D / 8) + 255) / 256;
-    if (blocks > 8L * ctx->sm_count) blocks = 8L * ctx->sm_count;
-    kv4_append_kernel<T, D><<<(int)blocks, 256, 0, ctx->stream>>>(c, (const T*)K, ldk, (const T*)V, ldv, pos, row_start, at, n_rows,
-                                                                  (T*)K_read, (T*)V_read, ctx->ws.status);
+    // many rows: four passes to a warp; few: one, so that they spread over the SMs
+    const int passes = ceil_div(c.Hkv, 256 / D);
+    const int per = (long)n_rows * passes >= 16L * 8 * ctx->sm_count ? 4 : 1, parts = 2 * ceil_div(passes, per);
+    int blocks = ceil_div(n_rows, 8);
+    if (blocks > ceil_div(16 * ctx->sm_count, parts)) blocks = ceil_div(16 * ctx->sm_count, parts);
+    auto kernel = c.group == 32 ? kv4_append_kernel<T, D, 4> : c.group == 64 || D == 64 ? kv4_append_kernel<T, D, 8> : kv4_append_kernel<T, D, D / 8>;
+    kernel<<<dim3(blocks, parts), 256, 0, ctx->stream>>>(c, (const T*)K, ldk, (const T*)V, ldv, pos, row_start, at, n_rows, per,
+                                                         (T*)K_read, (T*)V_read, ctx->ws.status);
     SPTS_CUDA_OK(ctx);
   }
   kv4_len_kernel<<<ceil_div(c.n_seq, 256), 256, 0, ctx->stream>>>(c.len, at, row_start, c.n_seq, c.capacity);

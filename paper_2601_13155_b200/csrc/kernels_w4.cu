@@ -12,23 +12,23 @@ namespace {
 
 using namespace q4;
 
-template <typename T>
+template <typename T, int LANES>
 __global__ void __launch_bounds__(256)
-w4_quantize_kernel(const T* __restrict__ W, long n_words, int lanes, uint32_t* __restrict__ codes,
+w4_quantize_kernel(const T* __restrict__ W, long n_words, uint32_t* __restrict__ codes,
                    uint32_t* __restrict__ params, int* status) {
   const long i0 = (long)blockIdx.x * 256 + threadIdx.x, stride = (long)gridDim.x * 256;
   // every lane of a warp takes the same number of steps (the group's shuffles need all of them)
   for (long i = i0; (i & ~31L) < n_words; i += stride) {
-    const bool in = i < n_words;                   // whole groups: n_words is a multiple of the lanes of a group
+    const bool in = i < n_words;                   // whole groups: n_words is a multiple of LANES
     float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (in) load8(W + 8 * i, x);
     uint32_t p;
     bool bad;
-    const uint32_t w = quantize8(x, lanes, p, nullptr, bad);
+    const uint32_t w = quantize8<LANES>(W, x, p, nullptr, bad);
     if (in) {
       codes[i] = w;
-      if (i % lanes == 0) {
-        params[i / lanes] = p;
+      if (i % LANES == 0) {
+        params[i / LANES] = p;
         if (bad) set_status(status, SPTS_ERR_NONFINITE);
       }
     }
@@ -355,16 +355,19 @@ spts_status launch_w4_gemv(spts_ctx* ctx, const W4GemvArgs& a) {
   return a.n == 1 ? launch_plain<bf16, 1>(ctx, a) : launch_plain<bf16, 4>(ctx, a);
 }
 
+template <typename T>
+static void quantize_t(spts_ctx* ctx, const void* W, long n_words, int blocks, int group, void* codes, void* params) {
+  void (*kernel)(const T*, long, uint32_t*, uint32_t*, int*) =
+      group == 32 ? w4_quantize_kernel<T, 4> : group == 64 ? w4_quantize_kernel<T, 8> : w4_quantize_kernel<T, 16>;
+  kernel<<<blocks, 256, 0, ctx->stream>>>((const T*)W, n_words, (uint32_t*)codes, (uint32_t*)params, ctx->ws.status);
+}
+
 spts_status launch_w4_quantize(spts_ctx* ctx, const void* W, int out, int in, int group, void* codes, void* params) {
   const long n_words = (long)out * (in / 8);
   long blocks = (n_words + 255) / 256;
   if (blocks > 16L * ctx->sm_count) blocks = 16L * ctx->sm_count;
-  if (ctx->desc.dtype == SPTS_BF16)
-    w4_quantize_kernel<bf16><<<(int)blocks, 256, 0, ctx->stream>>>((const bf16*)W, n_words, group / 8, (uint32_t*)codes,
-                                                                   (uint32_t*)params, ctx->ws.status);
-  else
-    w4_quantize_kernel<float><<<(int)blocks, 256, 0, ctx->stream>>>((const float*)W, n_words, group / 8, (uint32_t*)codes,
-                                                                    (uint32_t*)params, ctx->ws.status);
+  if (ctx->desc.dtype == SPTS_BF16) quantize_t<bf16>(ctx, W, n_words, (int)blocks, group, codes, params);
+  else quantize_t<float>(ctx, W, n_words, (int)blocks, group, codes, params);
   SPTS_CUDA_OK(ctx);
   return SPTS_OK;
 }

@@ -22,6 +22,24 @@ __device__ __forceinline__ void load8(const bf16* p, float* x) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) { x[2 * i] = lo_bf16(w[i]); x[2 * i + 1] = hi_bf16(w[i]); }
 }
+// Eight elements as they lie in memory.
+template <typename T> struct Raw8;
+template <> struct Raw8<float> {
+  float4 a, b;
+  __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const float4*>(p); b = *reinterpret_cast<const float4*>(p + 4); }
+  __device__ __forceinline__ void get(float* x) const { x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w; }
+};
+template <> struct Raw8<bf16> {
+  uint4 v;
+  __device__ __forceinline__ void zero() { v = make_uint4(0u, 0u, 0u, 0u); }
+  __device__ __forceinline__ void load(const bf16* p) { v = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void get(float* x) const {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = lo_bf16(w[i]); x[2 * i + 1] = hi_bf16(w[i]); }
+  }
+};
 __device__ __forceinline__ void store8(float* p, const float* x) {
   *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
   *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
@@ -84,28 +102,64 @@ __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, bool in
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// Quantises the eight elements of this lane; the group is `lanes` (4, 8 or 16) neighbouring lanes of the warp, aligned
+// Quantises the eight elements of this lane; the group is LANES (4, 8 or 16) neighbouring lanes of the warp, aligned
 // to their number, and every lane of the warp calls.  Returns the eight codes, element i in bits 4i .. 4i + 3; `params`
 // = scale | mid << 16; read (if not null) the values that the codes stand for.
-// The code is the exact quotient's rounding: the fp32 quotient is off by less than 3 * 2^-24 * 9 = 1.7e-6 steps (three
-// roundings, at most nine steps from the middle), so wherever it lies farther than 1e-5 from a border it gives the exact
-// quotient's code, and the rest (about one in 50,000 of smooth data) is divided in 64 bits.
-__device__ __forceinline__ uint32_t quantize8(const float* x, int lanes, uint32_t& params, float* read, bool& nonfinite) {
-  float hi = x[0], lo = x[0];
-  bool bad = false;
+// The stored numbers are those of 64-bit arithmetic, at the price of 32-bit arithmetic: each is computed in fp32 with a
+// bound on its error, and only where the bound reaches a border between two results the border is decided exactly.  Borders
+// are common, not rare: differences of bf16 numbers have few bits, so a quotient that ends in exactly one half turns up in
+// every other warp, and a mid that needs nine bits in every group; both are decided in fp32 with error-free sums.
+//   scale  three roundings, off by less than 4 in the 16 bits that bf16 drops: near their middle, 64 bits (rare)
+//   mid    fp32 sums with their errors: without error it is exact; with one it is off by less than 2^-22 (|hi| + |lo| + scale),
+//          and where that reaches a border, 64 bits (rare)
+//   code   the quotient has error below 4 * 2^-23 * 9 steps = 4.3e-6; within 1e-5 of a border the residual d - border * scale
+//          decides, which a fused multiply-add gives exactly there (d = x - mid with its own error)
+__device__ __forceinline__ __nv_bfloat162 as_bf162(uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); }
+__device__ __forceinline__ uint32_t as_word(__nv_bfloat162 v) { return *reinterpret_cast<const uint32_t*>(&v); }
+
+// Largest and smallest of the group; a NaN in it makes `hi` NaN.
+template <int LANES> __device__ __forceinline__ void group_range(const float* p, const float* x, float& hi, float& lo) {
+  hi = lo = x[0];
+  bool nan = x[0] != x[0];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 1; i < 8; ++i) {
     hi = fmaxf(hi, x[i]); lo = fminf(lo, x[i]);
-    bad = bad || !(fabsf(x[i]) <= 3.402823466e38f);
+    nan = nan || x[i] != x[i];
   }
-  for (int o = 1; o < lanes; o <<= 1) {
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+  if (nan) hi = __uint_as_float(0x7FFFFFFFu);
+#pragma unroll
+  for (int o = 1; o < LANES; o <<= 1) {
+    const float h = __shfl_xor_sync(0xffffffffu, hi, o);
+    hi = hi != hi || h != h ? __uint_as_float(0x7FFFFFFFu) : fmaxf(hi, h);
     lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
   }
-  const uint32_t votes = __ballot_sync(0xffffffffu, bad);
-  const int lane = threadIdx.x & 31;
-  const uint32_t mine = ((1u << lanes) - 1u) << (lane & ~(lanes - 1));
-  nonfinite = (votes & mine) != 0;
+}
+// The same for bf16, on pairs as they lie in memory: (largest, largest of the negatives) travel in one register.
+template <int LANES> __device__ __forceinline__ void group_range(const bf16* p, const float* x, float& hi, float& lo) {
+  const uint32_t w[4] = {__byte_perm(__float_as_uint(x[0]), __float_as_uint(x[1]), 0x7632), __byte_perm(__float_as_uint(x[2]), __float_as_uint(x[3]), 0x7632),
+                         __byte_perm(__float_as_uint(x[4]), __float_as_uint(x[5]), 0x7632), __byte_perm(__float_as_uint(x[6]), __float_as_uint(x[7]), 0x7632)};
+  const __nv_bfloat162 h = __hmax2_nan(__hmax2_nan(as_bf162(w[0]), as_bf162(w[1])), __hmax2_nan(as_bf162(w[2]), as_bf162(w[3])));
+  const __nv_bfloat162 l = __hmin2_nan(__hmin2_nan(as_bf162(w[0]), as_bf162(w[1])), __hmin2_nan(as_bf162(w[2]), as_bf162(w[3])));
+  const uint32_t hw = as_word(h), lw = as_word(l) ^ 0x80008000u;
+  uint32_t v = as_word(__hmax2_nan(as_bf162(__byte_perm(hw, lw, 0x5410)), as_bf162(__byte_perm(hw, lw, 0x7632))));
+#pragma unroll
+  for (int o = 1; o < LANES; o <<= 1) v = as_word(__hmax2_nan(as_bf162(v), as_bf162(__shfl_xor_sync(0xffffffffu, v, o))));
+  hi = lo_bf16(v);
+  lo = -hi_bf16(v);
+}
+
+// a + b - s, exactly, where s is the rounded sum
+__device__ __forceinline__ float sum_error(float a, float b, float s) {
+  const float bb = __fsub_rn(s, a);
+  return __fadd_rn(__fsub_rn(a, __fsub_rn(s, bb)), __fsub_rn(b, bb));
+}
+
+template <int LANES, typename T>
+__device__ __forceinline__ uint32_t quantize8(const T* type, const float* x, uint32_t& params, float* read, bool& nonfinite) {
+  float hi, lo;
+  group_range<LANES>(type, x, hi, lo);
+  const float big = fmaxf(fabsf(hi), fabsf(lo));
+  nonfinite = hi != hi || !(big <= 3.402823466e38f);
   if (nonfinite) {
     params = 0x7FC00000u;                       // scale 0, mid NaN
     if (read)
@@ -113,27 +167,68 @@ __device__ __forceinline__ uint32_t quantize8(const float* x, int lanes, uint32_
       for (int i = 0; i < 8; ++i) read[i] = __uint_as_float(0x7FC00000u);
     return 0x88888888u;
   }
-  const double dh = (double)hi, dl = (double)lo;
-  const bf16 sb = __float2bfloat16_rn((float)((dh - dl) / 15.0));
+  // (small ranges, where fp32 loses bits to underflow, and ranges that overflow it go the long way)
+  float sf = (hi - lo) * (1.0f / 15.0f);
+  const uint32_t low = __float_as_uint(sf) & 0xFFFFu;
+  bf16 sb = __float2bfloat16_rn(sf);
+  if (!(sf > 1e-30f && sf < 1e37f) || (low - 0x7FFCu) <= 8u) sb = __float2bfloat16_rn((float)(((double)hi - (double)lo) / 15.0));
   const float s = __bfloat162float(sb);
-  const bf16 mb = __float2bfloat16_rn((float)(0.5 * (dh + dl) + 0.5 * (double)s));
+  const float sum = hi + lo, m2 = sum + s;      // twice the mid
+  const bool exact = sum - hi == lo && sum - lo == hi && m2 - sum == s && m2 - s == sum;
+  const float mf = 0.5f * m2;
+  bf16 mb = __float2bfloat16_rn(mf);
+  if (!(big < 1e37f && s > 1e-30f)) mb = __float2bfloat16_rn((float)(0.5 * ((double)hi + (double)lo) + 0.5 * (double)s));
+  else if (!exact) {
+    const float me = 2.4e-7f * (fabsf(hi) + fabsf(lo) + s);
+    if (__bfloat16_as_ushort(__float2bfloat16_rn(mf - me)) != __bfloat16_as_ushort(__float2bfloat16_rn(mf + me)))
+      mb = __float2bfloat16_rn((float)(0.5 * ((double)hi + (double)lo) + 0.5 * (double)s));
+  }
   const float m = __bfloat162float(mb);
   params = (uint32_t)__bfloat16_as_ushort(sb) | ((uint32_t)__bfloat16_as_ushort(mb) << 16);
-  uint32_t word = 0;
-  const bool tiny = s < 1e-30f;                 // 1 / s would overflow
-  const float inv = tiny ? 0.f : 1.0f / s;
+  float xs[8], ss = s, ms = m;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float t = (x[i] - m) * inv;
-    float r = rintf(t);
-    if (tiny || fabsf(fabsf(t - r) - 0.5f) < 1e-5f) {
-      if (s == 0.f) r = 0.f;
-      else r = (float)fmin(8.0, fmax(-9.0, rint(((double)x[i] - (double)m) / (double)s)));
-    }
-    const int c = (int)fminf(7.f, fmaxf(-8.f, r));
-    word |= (uint32_t)(c + 8) << (4 * i);
-    if (read) read[i] = fmaf(s, (float)c, m);
+  for (int i = 0; i < 8; ++i) xs[i] = x[i];
+  if (s < 1e-37f) {                             // a scale near the end of fp32's range (all elements lie below 2^-90 then)
+    const float up = s == 0.f ? 0.f : 1.8446744073709552e19f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) xs[i] = s == 0.f ? 0.f : x[i] * up;
+    ss = s == 0.f ? 1.f : s * up;
+    ms = m * up;
   }
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(ss));
+  // adding 1.5 * 2^23 + 8 leaves the code in a float's last bits (round to nearest, ties to even) under a constant, which
+  // the sum of all eight carries off at once
+  constexpr float MAGIC = 12582920.f;
+  constexpr uint32_t MAGIC_BITS = 0x4B400000u;
+  uint32_t word = 0;
+  float r[8], far = 0.f;                        // far: the largest distance of an element from its code's value
+#pragma unroll
+  for (int i = 7; i >= 0; --i) {
+    const float d = xs[i] - ms, y = fminf(fmaxf(fmaf(d, inv, MAGIC), MAGIC - 8.f), MAGIC + 7.f);
+    r[i] = y - MAGIC;
+    far = fmaxf(far, fabsf(fmaf(-r[i], ss, d)));
+    word = word * 16u + __float_as_uint(y);
+  }
+  word -= MAGIC_BITS * 0x11111111u;
+  if (far > 0.49999f * ss) {
+    word = 0;
+#pragma unroll
+    for (int i = 7; i >= 0; --i) {
+      const float d = xs[i] - ms, off = fmaf(-r[i], ss, d);
+      if (fabsf(off) > 0.49999f * ss) {
+        const float border = r[i] + copysignf(0.5f, off);
+        const float side = fmaf(-border, ss, d) + sum_error(xs[i], -ms, d);
+        const float below = border - 0.5f, even = (__float_as_uint(below + MAGIC) & 1u) ? below + 1.f : below;
+        const float c = side > 0.f ? below + 1.f : side < 0.f ? below : even;
+        r[i] = fminf(fmaxf(c, -8.f), 7.f);
+      }
+      word = word * 16u + (__float_as_uint(r[i] + MAGIC) & 15u);
+    }
+  }
+  if (read)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) read[i] = fmaf(s, r[i], m);
   return word;
 }
 
