@@ -400,7 +400,7 @@ spts_status spts_decode_step(spts_ctx* ctx, const spts_model_weights* mw, spts_k
 /* A weight matrix [out, in] in 4 bits: byte i of a row holds element 2i in its low and 2i + 1 in its high nibble. */
 typedef struct {
   const void* codes;      /* [out, in / 2] bytes, 16-byte aligned          */
-  const void* params;     /* [out, in / group, 2] bf16 (scale, mid)        */
+  const void* params;     /* [out, in / group, 2] bf16 (scale, mid), 16-byte aligned */
   int32_t out_features;
   int32_t in_features;    /* a multiple of group                           */
   int32_t group;          /* 32, 64 or 128                                 */
@@ -415,8 +415,10 @@ enum {
   SPTS_W4_FP32_OUT = 2u   /* Y is fp32 whatever the storage type (logits) */
 };
 #define SPTS_W4_MAX_N 32
+#define SPTS_W4_MAX_IN 131072
 
-/* Y[t] = X[t] W^T for n tokens, 0 <= n <= SPTS_W4_MAX_N (the codes are read once for all of them).
+/* Y[t] = X[t] W^T for n tokens, 0 <= n <= SPTS_W4_MAX_N, in_features <= SPTS_W4_MAX_IN (the codes are read once for all
+ * tokens up to 32768 features, beyond that once for every 24, 16 or 8).
  *   w2 given: Y[t] = silu(X[t] W^T) * (X[t] W2^T) (gate and up projection; same shape and group)
  *   residual given: Y[t] = residual[t] + X[t] W^T (Y may be the residual itself; not with w2 or SPTS_W4_FP32_OUT)
  * X [n, in], residual and Y [n, out] in the storage type with row strides ldx, ldr, ldy in elements; X 16-byte aligned,

@@ -217,12 +217,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
   return d;
 }
-template <int NG> __device__ __forceinline__ void load_params(const unsigned char* p, uint32_t (&w)[NG]) {
-  if (NG == 4) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(p);
-  else if (NG == 2) *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(p);
-  else w[0] = *reinterpret_cast<const uint32_t*>(p);
-}
-
 template <int D, int NG, int NB>
 struct Kv4Tile {
   static constexpr int WARPS = 8;
@@ -484,8 +478,8 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
           *reinterpret_cast<uint2*>(kw0) = *reinterpret_cast<const uint2*>(st + T::KC + r0 * (D / 2) + cc * 8);
           *reinterpret_cast<uint2*>(kw1) = *reinterpret_cast<const uint2*>(st + T::KC + r1 * (D / 2) + cc * 8);
         }
-        load_params<NG>(st + T::KP + r0 * NG * 4, kp0);
-        load_params<NG>(st + T::KP + r1 * NG * 4, kp1);
+        load_words<NG>(st + T::KP + r0 * NG * 4, kp0);
+        load_words<NG>(st + T::KP + r1 * NG * 4, kp1);
         uint32_t pw0 = 0u, pw1 = 0u;
         if (cc < NG) {
           pw0 = *reinterpret_cast<const uint32_t*>(st + T::KP + (r0 * NG + cc) * 4);
@@ -540,8 +534,8 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
       for (int nb = 0; nb < NB; ++nb) top[nb][0] = top[nb][1] = -INFINITY;
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-        load_params<NG>(st + T::VP + (16 * rt + g) * NG * 4, vp0[rt]);
-        load_params<NG>(st + T::VP + (16 * rt + g + 8) * NG * 4, vp1[rt]);
+        load_words<NG>(st + T::VP + (16 * rt + g) * NG * 4, vp0[rt]);
+        load_words<NG>(st + T::VP + (16 * rt + g + 8) * NG * 4, vp1[rt]);
 #pragma unroll
         for (int gr = 0; gr < NG; ++gr) top_s = fmaxf(top_s, fmaxf(lo_bf16(vp0[rt][gr]), lo_bf16(vp1[rt][gr])));
 #pragma unroll

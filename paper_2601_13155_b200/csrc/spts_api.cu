@@ -104,6 +104,10 @@ size_t carve(const spts_model_desc& d, int Nmax, void* base, Workspace* ws, std:
   w.acc32_elems = N * KD;
   if (Npad * HD * es >= w.acc32_elems * sizeof(float)) w.acc32 = reinterpret_cast<float*>(w.o_att);
   else w.acc32 = c.take<float>(w.acc32_elems);
+  // fragments 2 bytes an element; sums 16 bytes per 32; factors
+  w.w4_x = c.take<char>(W4_X_ELEMENTS * 2 + W4_X_ELEMENTS / 2 + 256);
+  w.w4_part = c.take<float>((size_t)W4_MAX_ITEMS * 32 * 256);
+  w.w4_arrived = c.take<int>(W4_MAX_ITEMS);
   w.kv4_part = c.take<float>((size_t)2 * KV4_MAX_CTAS * 16 * (d.head_dim + 2));
   w.kv4_arrived = c.take<int>(KV4_MAX_CTAS);
   w.dec = c.take<float>(decode_scratch_floats(d));
@@ -600,7 +604,8 @@ spts_status spts_create(const spts_model_desc* desc, int max_seq, void* workspac
     spts_destroy(ctx);
     return SPTS_ERR_CUDA;
   }
-  if (cudaMemsetAsync(ctx->ws.kv4_arrived, 0, KV4_MAX_CTAS * sizeof(int), ctx->stream) != cudaSuccess) {
+  if (cudaMemsetAsync(ctx->ws.kv4_arrived, 0, KV4_MAX_CTAS * sizeof(int), ctx->stream) != cudaSuccess ||
+      cudaMemsetAsync(ctx->ws.w4_arrived, 0, W4_MAX_ITEMS * sizeof(int), ctx->stream) != cudaSuccess) {
     spts_destroy(ctx);
     return SPTS_ERR_CUDA;
   }
@@ -1141,8 +1146,10 @@ bool rows_ok(const void* p, int64_t ld, int64_t width, int64_t n, size_t es) {
   return aligned16(p) && (n < 2 || (ld >= width && (ld * (int64_t)es) % 16 == 0));
 }
 spts_status check_w4(const spts_w4* w) {
-  if (w->codes == nullptr || w->params == nullptr || !aligned16(w->codes) || !aligned4(w->params)) return SPTS_ERR_INVALID_ARG;
-  if (!group_ok(w->group) || w->out_features < 1 || w->in_features < 1 || w->in_features % w->group != 0) return SPTS_ERR_SHAPE;
+  if (w->codes == nullptr || w->params == nullptr || !aligned16(w->codes) || !aligned16(w->params)) return SPTS_ERR_INVALID_ARG;
+  if (!group_ok(w->group) || w->out_features < 1 || w->in_features < 1 || w->in_features % w->group != 0 ||
+      w->in_features > SPTS_W4_MAX_IN)
+    return SPTS_ERR_SHAPE;
   return SPTS_OK;
 }
 spts_status check_kv4(const spts_ctx* ctx, const spts_kv4_cache* c) {
@@ -1163,7 +1170,7 @@ spts_status spts_w4_quantize(spts_ctx* ctx, const void* W, int out_features, int
   TRY(check_ctx(ctx));
   if (W == nullptr || codes == nullptr || params == nullptr) return SPTS_ERR_INVALID_ARG;
   if (!group_ok(group) || out_features < 1 || in_features < 1 || in_features % group != 0) return SPTS_ERR_SHAPE;
-  if (!aligned16(W) || !aligned16(codes) || !aligned4(params)) return SPTS_ERR_INVALID_ARG;
+  if (!aligned16(W) || !aligned16(codes) || !aligned16(params)) return SPTS_ERR_INVALID_ARG;
   ON_DEVICE(ctx);
   return launch_w4_quantize(ctx, W, out_features, in_features, group, codes, params);
 }
