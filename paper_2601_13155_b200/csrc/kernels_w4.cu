@@ -120,19 +120,22 @@ spts_status launch_plain(spts_ctx* ctx, const W4GemvArgs& a) {
 // has its second part in one more matrix step per four groups, in bf16, whose A registers are the params words as they lie in
 // memory and whose B holds -8 sum x and sum x in bf16 pieces (two of them, 2^-17 relative; three for fp32 outputs).
 //
-// x is laid out for that once per call by w4_prepare_kernel (a CTA per token): brought to fp16 by a power of two (exact: bf16
-// has fewer bits, and what falls below fp16's range is 2^-35 of the token's largest element), in the order of the B fragments,
-// with the groups' sums and the factor that takes the power of two back (and the row norm with it).  The product kernel is its
-// programmatic dependent: it fills its rings with weights while x is prepared.
+// x is laid out for that once per call: brought to fp16 by a power of two (exact: bf16 has fewer bits, and what falls below
+// fp16's range is 2^-35 of the token's largest element), in the order of the B fragments, with the groups' sums and the factor
+// that takes the power of two back (and the row norm with it).  Few elements (LOCAL) every CTA lays out for itself in shared
+// memory while its first weights are on their way; more are laid out once by w4_prepare_kernel (a CTA per token), whose
+// programmatic dependent the product kernel is: it fills its rings with weights meanwhile.
 //
-// Work split.  A warp takes 16 MT rows (gate and up rows alternating in MT when there are two matrices).  With at most eight
-// tokens the WK = 8 warps of a CTA split the input axis in chunks of 128 (the CTA reads 512 contiguous bytes of each row at a
-// time); with more, x is what is read most, so the warps take different rows and the same chunks (WK = 1), and seven of eight
-// reads of x hit L1.  Where that leaves SMs without work, the input axis is also cut between CTAs (`slices`), and the CTA that
-// arrives last adds their shares in order.  The grid is persistent, and every warp's ring of asynchronous copies runs on across
-// tiles.
+// Work split.  A warp takes 16 MT rows (gate and up rows alternating in MT when there are two matrices), a CTA's WR x WK warps
+// a tile of WR such blocks and WK chunks of 128 of the input axis at a time.  The steps (WK chunks of a tile) of all tiles form
+// one line that is cut into equal pieces, one per CTA (persistent); a tile that lies in one piece is finished there, of a tile
+// cut between CTAs each leaves its share, and w4_join_kernel adds them in the order of the CTAs.  (The CTA that arrives last
+// added them at first: one CTA's loads for 21 tokens x 256 rows x 21 shares took 50 us.)  Every warp's ring of asynchronous
+// copies runs on across tiles.
 constexpr int W4_WARPS = 8;
 constexpr int W4_CHUNK = 128;
+constexpr int W4_WK = 1;
+constexpr int W4_LOCAL = 16384;            // elements of x that a CTA lays out for itself
 
 // The order of k inside a chunk: step t of the chunk's four, lane c, eight consecutive codes (one word).  A lane's words lie
 // side by side within a group, so that they are one shared-memory load.
@@ -140,17 +143,16 @@ template <int NGC> __host__ __device__ constexpr int w4_k(int t, int c) {
   return NGC == 1 ? 32 * c + 8 * t : NGC == 2 ? 64 * (t >> 1) + 16 * c + 8 * (t & 1) : 32 * t + 8 * c;
 }
 
-// x [n, in] -> frag [chunk][t][tokens][c] (16 bytes: four fp16 pairs), sums [chunk][tokens][c] (three pairs of pieces), factor [n]
-template <int NGC>
-__global__ void __launch_bounds__(512)
-w4_prepare_kernel(const bf16* __restrict__ X, int64_t ldx, int in, int tokens, int norm, float eps, uint4* __restrict__ frag,
-                  uint4* __restrict__ sums, float* __restrict__ factor) {
-  __shared__ float red[2][16];
-  const int token = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
-  const bf16* x = X + (size_t)token * ldx;
-  dep_launch();
+// x [n, in] -> frag [chunk][t][n][c] (16 bytes: four fp16 pairs), sums [chunk][n][c] (three pairs of pieces), factor [n];
+// one token, by a CTA of THREADS
+template <int NGC, int THREADS>
+__device__ __forceinline__ void w4_prepare(const bf16* __restrict__ x, int token, int n, int in, int norm, float eps, uint4* frag,
+                                           uint4* sums, float* factor) {
+  constexpr int WARPS = THREADS / 32;
+  __shared__ float red[2][WARPS];
+  const int tid = threadIdx.x, lane = tid & 31;
   float top = 0.f, ss = 0.f;
-  for (int k = 8 * tid; k < in; k += 8 * 512) {
+  for (int k = 8 * tid; k < in; k += 8 * THREADS) {
     float v[8];
     load8(x + k, v);
 #pragma unroll
@@ -158,15 +160,16 @@ w4_prepare_kernel(const bf16* __restrict__ X, int64_t ldx, int in, int tokens, i
   }
   top = warp_max(top);
   ss = warp_sum(ss);
+  __syncthreads();                                 // (the token before has been read)
   if (lane == 0) { red[0][tid >> 5] = top; red[1][tid >> 5] = ss; }
   __syncthreads();
   top = red[0][0]; ss = red[1][0];
 #pragma unroll
-  for (int w = 1; w < 16; ++w) { top = fmaxf(top, red[0][w]); ss += red[1][w]; }
+  for (int w = 1; w < WARPS; ++w) { top = fmaxf(top, red[0][w]); ss += red[1][w]; }
   const float xs = scale_to_2_13(top), u = xs * CODE_UNIT;
   if (tid == 0) factor[token] = (norm ? 1.0f / sqrtf(ss / (float)in + eps) : 1.0f) / u;
   const int chunks = (in + W4_CHUNK - 1) / W4_CHUNK, total = chunks * 16;
-  for (int i0 = tid & ~31; i0 < total; i0 += 512) {
+  for (int i0 = tid & ~31; i0 < total; i0 += THREADS) {
     const int i = i0 + lane, chunk = i >> 4, t = (i >> 2) & 3, c = i & 3;
     const int k = chunk * W4_CHUNK + w4_k<NGC>(t, c);
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -174,7 +177,7 @@ w4_prepare_kernel(const bf16* __restrict__ X, int64_t ldx, int in, int tokens, i
     float s = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
     if (i < total) {
       const float xo = xs * ODD;
-      frag[((size_t)(chunk * 4 + t) * tokens + token) * 4 + c] =
+      frag[((size_t)(chunk * 4 + t) * n + token) * 4 + c] =
           make_uint4(pack2_f16(v[0] * xs, v[4] * xs), pack2_f16(v[1] * xo, v[5] * xo), pack2_f16(v[2] * xs, v[6] * xs),
                      pack2_f16(v[3] * xo, v[7] * xo));
     }
@@ -184,74 +187,106 @@ w4_prepare_kernel(const bf16* __restrict__ X, int64_t ldx, int in, int tokens, i
     if (i < total && i % LANES == 0) {
       const float sm = s * u, a = -8.f * sm;
       const float ah = round_bf16(a), mh = round_bf16(sm), am = round_bf16(a - ah), mm = round_bf16(sm - mh);
-      sums[((size_t)chunk * tokens + token) * 4 + (i % 16) / LANES] =
+      sums[((size_t)chunk * n + token) * 4 + (i % 16) / LANES] =
           make_uint4(pack2(ah, mh), pack2(am, mm), pack2((a - ah) - am, (sm - mh) - mm), 0u);
     }
   }
+}
+template <int NGC>
+__global__ void __launch_bounds__(512)
+w4_prepare_kernel(const bf16* __restrict__ X, int64_t ldx, int in, int n, int norm, float eps, uint4* __restrict__ frag,
+                  uint4* __restrict__ sums, float* __restrict__ factor) {
+  dep_launch();
+  w4_prepare<NGC, 512>(X + (size_t)blockIdx.x * ldx, blockIdx.x, n, in, norm, eps, frag, sums, factor);
 }
 
 template <int NB, int MT, int NGC, int WK>
 struct W4Tile {
   static constexpr int WR = W4_WARPS / WK;
-  static constexpr int STAGES = 4;
+  static constexpr int STAGES = 3;
   static constexpr int CSTRIDE = NGC == 1 ? 64 : NGC == 2 ? 96 : 80;      // bytes between rows: a load's lanes lie in distinct banks
   static constexpr int PARAMS = 16 * MT * CSTRIDE, STAGE = PARAMS + 16 * MT * NGC * 4;
   static constexpr int RING = W4_WARPS * STAGES * STAGE;
-  static constexpr int RED = WK * 8 * NB * WR * MT * 16 * 4;              // [wk][token][wr][mt][row]
-  static constexpr int SMEM = RING + RED;
+  static constexpr int RED = W4_WARPS * MT * 16 * 4;                      // a token's [wk][wr][mt][row]
 };
 
 struct W4Mat { const char* codes; const uint32_t* params; };
 
-template <int NB, int MT, int NGC, bool TWO, int WK>
-__global__ void __launch_bounds__(W4_WARPS * 32, 2)
-w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, int slices, const uint4* __restrict__ frag, const uint4* __restrict__ sums,
-               const float* __restrict__ factor, float* __restrict__ part, int* __restrict__ arrived, W4Out o) {
+// The line of steps: tiles x steps, cut into `ctas` pieces.  A share is [token][a tile's rows in the order wr, mt, row]; a CTA
+// has at most two: 2 cta + 1 of a tile that begins in its piece, 2 cta of one that began before.
+struct W4Line {
+  int tiles, steps, ctas;
+  __device__ __forceinline__ long total() const { return (long)tiles * steps; }
+  __device__ __forceinline__ long begin(int cta) const { return total() * cta / ctas; }
+  __device__ __forceinline__ int cta_of(long x) const { return (int)(((x + 1) * ctas - 1) / total()); }
+};
+
+// where output r of a tile lies in a share (two matrices: the up row 16 behind the gate row)
+template <int MT, bool TWO> __device__ __forceinline__ int w4_place(int r) {
+  constexpr int WROWS = TWO ? 8 * MT : 16 * MT;
+  const int w = r / WROWS, rw = r - w * WROWS;
+  return w * MT * 16 + (TWO ? (rw >> 4) * 32 + (rw & 15) : rw);
+}
+
+template <int NB, int MT, int NGC, bool TWO, int WK, bool LOCAL>
+__global__ void __launch_bounds__(W4_WARPS * 32, NB > 2 ? 1 : 2)
+w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf16* __restrict__ X, int64_t ldx, int norm, float eps,
+               const uint4* __restrict__ frag_g, const uint4* __restrict__ sums_g, const float* __restrict__ factor_g,
+               float* __restrict__ part, W4Out o) {
   using T = W4Tile<NB, MT, NGC, WK>;
   constexpr int WR = T::WR, WROWS = TWO ? 8 * MT : 16 * MT, ROWS = WR * WROWS;      // output features of a warp, of a tile
-  constexpr int TOKENS = 8 * NB, RSTRIDE = WR * MT * 16;
+  constexpr int RSTRIDE = WR * MT * 16;
   constexpr int GT = 4 / NGC;                                 // steps of a group
   extern __shared__ __align__(128) unsigned char smem[];
-  __shared__ int last_flag;
+  __shared__ float sm_factor[8 * NB];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, cc = lane & 3;
   const int wk = warp % WK, wr = warp / WK;
-  const int chunks = (in + W4_CHUNK - 1) / W4_CHUNK, tiles = (out + ROWS - 1) / ROWS, groups = in / (128 / NGC);
-  const int items = tiles * slices;
+  const int chunks = (in + W4_CHUNK - 1) / W4_CHUNK, groups = in / (128 / NGC);
   const size_t row_bytes = in / 2;
   float* red = reinterpret_cast<float*>(smem + T::RING);
+  uint4* x_local = reinterpret_cast<uint4*>(smem + T::RING + n * T::RED);
   unsigned char* ring = smem + warp * (T::STAGES * T::STAGE);
   const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
-  const bool whole = groups % NGC == 0;                       // every chunk is: a row's params of a chunk are one copy
+  const bool whole_chunks = groups % NGC == 0;                // a row's params of a chunk are one aligned copy
+  const long u0 = line.begin(blockIdx.x), u1 = line.begin(blockIdx.x + 1);
 
-  // the walk of the copies: item, chunk, the warp's row pointers in that item
-  int f_item = blockIdx.x, f_chunk = 0, f_end = 0;
+  // the walk of the copies: tile, chunk, the warp's row pointers in that tile
+  int f_tile = (int)(u0 / line.steps), f_step = (int)(u0 - (long)f_tile * line.steps);
+  long f_left = u1 - u0;                                      // steps from here on
+  int f_chunk = 0, f_end = 0;
+  bool fetching = true;
   const char* f_codes[MT][2];
   const uint32_t* f_params = nullptr;                         // lane r: row r of the warp's 16 MT rows
   uint32_t fetch_at = 0, use_at = 0;
-  auto f_open = [&]() {                                       // settles on the next item in which this warp has a chunk
-    for (; f_item < items; f_item += gridDim.x) {
-      const int tile = f_item / slices, slice = f_item - tile * slices;
-      f_chunk = (int)((long)chunks * slice / slices) + wk;
-      f_end = (int)((long)chunks * (slice + 1) / slices);
+  auto f_open = [&]() {                                       // settles on the next tile in which this warp has a chunk
+    while (f_left > 0) {
+      const int here = (int)min((long)(line.steps - f_step), f_left);
+      const int tile = f_tile;
+      f_chunk = f_step * WK + wk;
+      f_end = min(chunks, (f_step + here) * WK);
+      f_left -= here;
+      ++f_tile;
+      f_step = 0;
       if (f_chunk >= f_end) continue;
       const int r0 = tile * ROWS + wr * WROWS;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
         const bool second = TWO && (mt & 1);
-        const W4Mat& m = second ? m2 : m1;
         const int rm = r0 + 16 * (TWO ? mt >> 1 : mt);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) f_codes[mt][i] = m.codes + min(rm + 8 * i + g, out - 1) * row_bytes + (size_t)f_chunk * 64 + 16 * cc;
+        for (int i = 0; i < 2; ++i)
+          f_codes[mt][i] = (second ? m2.codes : m1.codes) + min(rm + 8 * i + g, out - 1) * row_bytes + (size_t)f_chunk * 64 + 16 * cc;
       }
       const int mt = lane >> 4;
       const bool second = TWO && (mt & 1);
       f_params = (second ? m2.params : m1.params) + (size_t)min(r0 + 16 * (TWO ? mt >> 1 : mt) + (lane & 15), out - 1) * groups;
       return;
     }
+    fetching = false;
   };
   f_open();
   auto fetch_next = [&]() {
-    if (f_item < items) {
+    if (fetching) {
       const uint32_t dst = ring_s + fetch_at;
       if (f_chunk * W4_CHUNK + 32 * cc < in) {                // codes behind the end meet x = 0: any bits are finite numbers
 #pragma unroll
@@ -262,8 +297,8 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, int slices, const uin
       if (lane < 16 * MT) {
         const uint32_t* p = f_params + f_chunk * NGC;
         const uint32_t pd = dst + T::PARAMS + lane * NGC * 4;
-        if (NGC == 4 && whole) cp_async16(pd, p);
-        else if (NGC == 2 && whole) cp_async8(pd, p);
+        if (NGC == 4 && whole_chunks) cp_async16(pd, p);
+        else if (NGC == 2 && whole_chunks) cp_async8(pd, p);
         else {
 #pragma unroll
           for (int i = 0; i < NGC; ++i) {
@@ -279,7 +314,6 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, int slices, const uin
 #pragma unroll
           for (int i = 0; i < 2; ++i) f_codes[mt][i] += 64 * WK;
       } else {
-        f_item += gridDim.x;
         f_open();
       }
     }
@@ -288,11 +322,24 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, int slices, const uin
   };
 #pragma unroll
   for (int i = 0; i < T::STAGES - 1; ++i) fetch_next();
-  dep_wait();                                                 // x is prepared
+  const uint4* frag = frag_g;
+  const uint4* sums = sums_g;
+  if (LOCAL) {
+    uint4* sums_l = x_local + (size_t)chunks * 16 * n;
+    for (int t = 0; t < n; ++t)
+      w4_prepare<NGC, W4_WARPS * 32>(X + (size_t)t * ldx, t, n, in, norm, eps, x_local, sums_l, sm_factor);
+    frag = x_local;
+    sums = sums_l;
+  } else {
+    dep_wait();                                               // x is prepared
+    if (threadIdx.x < n) sm_factor[threadIdx.x] = __ldg(factor_g + threadIdx.x);
+  }
+  __syncthreads();
+  dep_launch();
 
-  for (int item = blockIdx.x; item < items; item += gridDim.x) {
-    const int tile = item / slices, slice = item - tile * slices;
-    const int c1 = (int)((long)chunks * (slice + 1) / slices);
+  int tile = (int)(u0 / line.steps), step = (int)(u0 - (long)tile * line.steps);
+  for (long left = u1 - u0; left > 0;) {
+    const int here = (int)min((long)(line.steps - step), left), c1 = min(chunks, (step + here) * WK);
     float y[NB][MT][4];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
@@ -300,18 +347,19 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, int slices, const uin
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[nb][mt][i] = 0.f;
-    for (int chunk = (int)((long)chunks * slice / slices) + wk; chunk < c1; chunk += WK) {
+    for (int chunk = step * WK + wk; chunk < c1; chunk += WK) {
       uint4 xf[NB][4], xs[NB];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         const bool has = 8 * nb + g < n;
+        const uint4* fp = frag + ((size_t)chunk * 4 * n + 8 * nb + g) * 4 + cc;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           xf[nb][t] = make_uint4(0u, 0u, 0u, 0u);
-          if (has) xf[nb][t] = __ldg(frag + ((size_t)(chunk * 4 + t) * TOKENS + 8 * nb + g) * 4 + cc);
+          if (has) xf[nb][t] = fp[(size_t)t * 4 * n];
         }
         xs[nb] = make_uint4(0u, 0u, 0u, 0u);
-        if (has && cc < NGC) xs[nb] = __ldg(sums + ((size_t)chunk * TOKENS + 8 * nb + g) * 4 + cc);
+        if (has && cc < NGC) xs[nb] = sums[((size_t)chunk * n + 8 * nb + g) * 4 + cc];
       }
       fetch_next();
       cp_async_wait<T::STAGES - 1>();
@@ -376,7 +424,7 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, int slices, const uin
       for (int i = 0; i < 2; ++i) {
         const int token = 8 * nb + 2 * cc + i;
         if (token < n) {
-          float* r = red + (size_t)(wk * TOKENS + token) * RSTRIDE + wr * MT * 16 + g;
+          float* r = red + (size_t)(wk * n + token) * RSTRIDE + wr * MT * 16 + g;
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt) { r[16 * mt] = y[nb][mt][i]; r[16 * mt + 8] = y[nb][mt][2 + i]; }
         }
@@ -385,92 +433,122 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, int slices, const uin
     auto sum_wk = [&](int t, int r) {
       float v = 0.f;
 #pragma unroll
-      for (int w = 0; w < WK; ++w) v += red[(size_t)(w * TOKENS + t) * RSTRIDE + r];
+      for (int w = 0; w < WK; ++w) v += red[(size_t)(w * n + t) * RSTRIDE + r];
       return v;
     };
-    bool finish = true;
-    if (slices > 1) {
-      float* mine = part + (size_t)item * TOKENS * RSTRIDE;
-      for (int i = threadIdx.x; i < n * RSTRIDE; i += W4_WARPS * 32) mine[i] = sum_wk(i / RSTRIDE, i % RSTRIDE);
-      __threadfence();
-      __syncthreads();
-      if (threadIdx.x == 0) last_flag = atomicAdd(&arrived[tile], 1) == slices - 1;
-      __syncthreads();
-      finish = last_flag;
-      if (finish) {
-        __threadfence();
-        if (threadIdx.x == 0) arrived[tile] = 0;              // for the next call
-      }
-    }
-    if (finish) {
+    if (here == line.steps) {
       for (int i = threadIdx.x; i < n * ROWS; i += W4_WARPS * 32) {
-        const int t = i / ROWS, r = i - t * ROWS, row = tile * ROWS + r;
+        const int t = i / ROWS, r = i - t * ROWS, row = tile * ROWS + r, at = w4_place<MT, TWO>(r);
         if (row >= out) continue;
-        // where the row's value lies: the warp's, then its tile of 16 (with two matrices gate and up tiles alternate)
-        const int w = r / WROWS, rw = r - w * WROWS, at = w * MT * 16 + (TWO ? (rw >> 4) * 32 + (rw & 15) : rw);
-        float v = 0.f, v2 = 0.f;
-        if (slices == 1) {
-          v = sum_wk(t, at);
-          if (TWO) v2 = sum_wk(t, at + 16);
-        } else {
-          const float* p = part + (size_t)tile * slices * TOKENS * RSTRIDE + (size_t)t * RSTRIDE + at;
-#pragma unroll 4
-          for (int s = 0; s < slices; ++s) {
-            v += __ldcg(p + (size_t)s * TOKENS * RSTRIDE);
-            if (TWO) v2 += __ldcg(p + (size_t)s * TOKENS * RSTRIDE + 16);
-          }
-        }
-        const float f = __ldg(factor + t);
-        v *= f;
-        w4_store<bf16>(o, t, row, TWO ? silu_mul(v, v2 * f) : v);
+        const float f = sm_factor[t], v = sum_wk(t, at) * f;
+        w4_store<bf16>(o, t, row, TWO ? silu_mul(v, sum_wk(t, at + 16) * f) : v);
       }
+    } else {
+      float* mine = part + (size_t)(2 * blockIdx.x + (step == 0 ? 1 : 0)) * n * RSTRIDE;
+      for (int i = threadIdx.x; i < n * RSTRIDE; i += W4_WARPS * 32) mine[i] = sum_wk(i / RSTRIDE, i % RSTRIDE);
     }
+    left -= here;
+    ++tile;
+    step = 0;
     __syncthreads();
   }
   cp_async_wait<0>();
 }
 
-template <int NB, int MT, int NGC, bool TWO, int WK>
-spts_status launch_tile(spts_ctx* ctx, const W4GemvArgs& a) {
-  using T = W4Tile<NB, MT, NGC, WK>;
-  const W4Out o{a.residual, a.ldr, a.Y, a.ldy, a.fp32_out};
-  const int rows = T::WR * (TWO ? 8 * MT : 16 * MT), tiles = ceil_div(a.out, rows), chunks = ceil_div(a.in, W4_CHUNK);
-  const int most = 2 * ctx->sm_count < W4_MAX_ITEMS ? 2 * ctx->sm_count : W4_MAX_ITEMS;
-  // the input axis is cut where there are fewer tiles than SMs, to two CTAs per SM but not below one chunk per warp
-  int slices = tiles < ctx->sm_count ? most / tiles : 1;
-  if (slices > chunks / WK) slices = chunks / WK > 1 ? chunks / WK : 1;
-  const int grid = tiles * slices < most ? tiles * slices : most;
-  uint4* frag = (uint4*)ctx->ws.w4_x;
-  uint4* sums = frag + (size_t)chunks * 16 * 8 * NB;
-  float* factor = (float*)(sums + (size_t)chunks * 4 * 8 * NB);
-  w4_prepare_kernel<NGC><<<a.n, 512, 0, ctx->stream>>>((const bf16*)a.X, a.ldx, a.in, 8 * NB, a.norm, ctx->desc.rms_eps, frag, sums, factor);
-  SPTS_CUDA_OK(ctx);
-  auto kernel = w4_gemv_kernel<NB, MT, NGC, TWO, WK>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, T::SMEM) != cudaSuccess) return SPTS_ERR_CUDA;
+// Outputs of tiles that were cut between CTAs: the sum of their shares.
+template <int MT, bool TWO, int WR>
+__global__ void __launch_bounds__(128)
+w4_join_kernel(int out, int n, W4Line line, const float* __restrict__ part, const float* __restrict__ factor, W4Out o) {
+  constexpr int ROWS = WR * (TWO ? 8 * MT : 16 * MT), RSTRIDE = WR * MT * 16;
+  const int row = blockIdx.x * 128 + threadIdx.x, t = blockIdx.y;
+  const int tile = row / ROWS, at = w4_place<MT, TWO>(row - tile * ROWS);
+  const int c0 = line.cta_of((long)tile * line.steps), c1 = line.cta_of((long)(tile + 1) * line.steps - 1);
+  dep_wait();
+  if (row >= out || c0 == c1) return;
+  const size_t share = (size_t)n * RSTRIDE;
+  const float* p = part + (size_t)t * RSTRIDE + at;
+  float v = __ldcg(p + (2 * c0 + 1) * share), v2 = TWO ? __ldcg(p + (2 * c0 + 1) * share + 16) : 0.f;
+#pragma unroll 8
+  for (int c = c0 + 1; c <= c1; ++c) {
+    v += __ldcg(p + 2 * c * share);
+    if (TWO) v2 += __ldcg(p + 2 * c * share + 16);
+  }
+  const float f = __ldg(factor + t);
+  w4_store<bf16>(o, t, row, TWO ? silu_mul(v * f, v2 * f) : v * f);
+}
+
+template <typename... KArgs, typename... Args>
+cudaError_t launch_dep_smem(void (*kernel)(KArgs...), dim3 grid, int threads, size_t smem, cudaStream_t st, Args... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(W4_WARPS * 32);
-  cfg.dynamicSmemBytes = T::SMEM;
-  cfg.stream = ctx->stream;
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, kernel, W4Mat{(const char*)a.codes, (const uint32_t*)a.params},
-                         W4Mat{(const char*)a.codes2, (const uint32_t*)a.params2}, a.out, a.in, a.n, slices, (const uint4*)frag,
-                         (const uint4*)sums, (const float*)factor, ctx->ws.w4_part, ctx->ws.w4_arrived, o) != cudaSuccess)
-    return SPTS_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+}
+
+template <int NB, int MT, int NGC, bool TWO, int WK, bool LOCAL>
+spts_status launch_tile(spts_ctx* ctx, const W4GemvArgs& a) {
+  using T = W4Tile<NB, MT, NGC, WK>;
+  const W4Out o{a.residual, a.ldr, a.Y, a.ldy, a.fp32_out};
+  const int rows = T::WR * (TWO ? 8 * MT : 16 * MT), chunks = ceil_div(a.in, W4_CHUNK);
+  W4Line line;
+  line.tiles = ceil_div(a.out, rows);
+  line.steps = ceil_div(chunks, WK);
+  const int most = (NB > 2 ? 1 : 2) * (ctx->sm_count < W4_MAX_CTAS / 2 ? ctx->sm_count : W4_MAX_CTAS / 2);
+  const long total = (long)line.tiles * line.steps;
+  // a CTA per tile where that fills the SMs once and no more than the resident CTAs, or where tiles are too short for two more
+  // launches to pay (16 steps take about 8 us); else equal pieces of the line
+  const bool tile_each = line.tiles <= most && (line.tiles >= ctx->sm_count || (LOCAL && line.steps <= 16));
+  line.ctas = tile_each ? line.tiles : total < most ? (int)total : most;
+  const bool cut = !(line.tiles % line.ctas == 0);
+  uint4* frag = (uint4*)ctx->ws.w4_x;
+  uint4* sums = frag + (size_t)chunks * 16 * a.n;
+  float* factor = (float*)(sums + (size_t)chunks * 4 * a.n);
+  const bool local = LOCAL && !cut;
+  if (!local) {
+    w4_prepare_kernel<NGC><<<a.n, 512, 0, ctx->stream>>>((const bf16*)a.X, a.ldx, a.in, a.n, a.norm, ctx->desc.rms_eps, frag, sums, factor);
+    SPTS_CUDA_OK(ctx);
+  }
+  auto kernel = local ? w4_gemv_kernel<NB, MT, NGC, TWO, WK, LOCAL> : w4_gemv_kernel<NB, MT, NGC, TWO, WK, false>;
+  const size_t smem = T::RING + (size_t)a.n * T::RED + (local ? (size_t)chunks * a.n * (16 + 4) * 16 : 0);
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return SPTS_ERR_CUDA;
+  const W4Mat m1{(const char*)a.codes, (const uint32_t*)a.params}, m2{(const char*)a.codes2, (const uint32_t*)a.params2};
+  const cudaError_t e = [&]() {
+    if (!local)
+      return launch_dep_smem(kernel, dim3(line.ctas), W4_WARPS * 32, smem, ctx->stream, m1, m2, a.out, a.in, a.n, line, (const bf16*)a.X, a.ldx,
+                             a.norm, ctx->desc.rms_eps, (const uint4*)frag, (const uint4*)sums, (const float*)factor, ctx->ws.w4_part, o);
+    kernel<<<line.ctas, W4_WARPS * 32, smem, ctx->stream>>>(m1, m2, a.out, a.in, a.n, line, (const bf16*)a.X, a.ldx, a.norm,
+                                                            ctx->desc.rms_eps, frag, sums, factor, ctx->ws.w4_part, o);
+    return cudaGetLastError();
+  }();
+  if (e != cudaSuccess) return SPTS_ERR_CUDA;
   SPTS_CUDA_OK(ctx);
+  if (cut) {
+    if (launch_dep_smem(w4_join_kernel<MT, TWO, T::WR>, dim3(ceil_div(a.out, 128), a.n), 128, 0, ctx->stream, a.out, a.n, line,
+                        (const float*)ctx->ws.w4_part, (const float*)factor, o) != cudaSuccess)
+      return SPTS_ERR_CUDA;
+    SPTS_CUDA_OK(ctx);
+  }
   return SPTS_OK;
 }
 template <int NB, int NGC>
 spts_status launch_rows(spts_ctx* ctx, const W4GemvArgs& a) {
-  constexpr int WK = NB == 1 ? 8 : 1;
-  if (a.codes2 != nullptr) return launch_tile<NB, 2, NGC, true, WK>(ctx, a);
-  // one tile of 16 rows to a warp where two would leave SMs without a CTA
-  if (NB == 1 && ceil_div(a.out, 32) < 2 * ctx->sm_count) return launch_tile<NB, NB == 1 ? 1 : 2, NGC, false, WK>(ctx, a);
-  return launch_tile<NB, 2, NGC, false, WK>(ctx, a);
+  if constexpr (NB > 1) {
+    if (a.codes2 != nullptr) return launch_tile<NB, 2, NGC, true, 1, false>(ctx, a);
+    return launch_tile<NB, 2, NGC, false, 1, false>(ctx, a);
+  } else {
+    // few rows: all eight warps on one tile of 16, and few elements of x are laid out in the kernel itself
+    if (a.codes2 != nullptr) return launch_tile<1, 2, NGC, true, W4_WK, false>(ctx, a);
+    if (ceil_div(a.out, 16) <= 2 * ctx->sm_count)
+      return (long)a.n * a.in <= W4_LOCAL ? launch_tile<1, 1, NGC, false, 8, true>(ctx, a) : launch_tile<1, 1, NGC, false, 8, false>(ctx, a);
+    return launch_tile<1, 2, NGC, false, W4_WK, false>(ctx, a);
+  }
 }
 template <int NB>
 spts_status launch_group(spts_ctx* ctx, const W4GemvArgs& a) {

@@ -106,8 +106,7 @@ size_t carve(const spts_model_desc& d, int Nmax, void* base, Workspace* ws, std:
   else w.acc32 = c.take<float>(w.acc32_elems);
   // fragments 2 bytes an element; sums 16 bytes per 32; factors
   w.w4_x = c.take<char>(W4_X_ELEMENTS * 2 + W4_X_ELEMENTS / 2 + 256);
-  w.w4_part = c.take<float>((size_t)W4_MAX_ITEMS * 32 * 256);
-  w.w4_arrived = c.take<int>(W4_MAX_ITEMS);
+  w.w4_part = c.take<float>((size_t)2 * W4_MAX_CTAS * 16 * 256);
   w.kv4_part = c.take<float>((size_t)2 * KV4_MAX_CTAS * 16 * (d.head_dim + 2));
   w.kv4_arrived = c.take<int>(KV4_MAX_CTAS);
   w.dec = c.take<float>(decode_scratch_floats(d));
@@ -604,8 +603,7 @@ spts_status spts_create(const spts_model_desc* desc, int max_seq, void* workspac
     spts_destroy(ctx);
     return SPTS_ERR_CUDA;
   }
-  if (cudaMemsetAsync(ctx->ws.kv4_arrived, 0, KV4_MAX_CTAS * sizeof(int), ctx->stream) != cudaSuccess ||
-      cudaMemsetAsync(ctx->ws.w4_arrived, 0, W4_MAX_ITEMS * sizeof(int), ctx->stream) != cudaSuccess) {
+  if (cudaMemsetAsync(ctx->ws.kv4_arrived, 0, KV4_MAX_CTAS * sizeof(int), ctx->stream) != cudaSuccess) {
     spts_destroy(ctx);
     return SPTS_ERR_CUDA;
   }

@@ -91,8 +91,7 @@ struct Workspace {
   int32_t* vt_col;      // [Nmax]
   int vt_ld_max;        // columns of v_t
   void* w4_x;           // tokens prepared for a 4-bit product: fragments, group sums, factors
-  float* w4_part;       // [W4_MAX_ITEMS, 32, 256] shares of CTAs that split a product's input axis
-  int* w4_arrived;      // [W4_MAX_ITEMS] of them have left theirs; zero between calls
+  float* w4_part;       // [2 W4_MAX_CTAS, 32, 256] shares of CTAs that split a product's input axis
   float* kv4_part;      // [2 * KV4_MAX_CTAS, 16, d + 2] partial results of the attention over a 4-bit cache
   int* kv4_arrived;     // [KV4_MAX_CTAS] CTAs that have left theirs; zero between calls
   int4* attn_tiles;     // [Nmax / 128 + BATCH_MAX_SEQ] query tiles of a packed batch's attention launch
@@ -129,7 +128,7 @@ struct spts_ctx {
 namespace spts {
 
 static const int BATCH_MAX_SEQ = 1024;        // sequences per packed batch that take the one-launch-per-step route
-static const int W4_MAX_ITEMS = 320;          // CTAs of a 4-bit product: two per SM
+static const int W4_MAX_CTAS = 320;           // CTAs of a 4-bit product: two per SM
 static const size_t W4_X_ELEMENTS = 1 << 20;  // tokens x features that are prepared at a time
 static const int KV4_MAX_CTAS = 160;          // CTAs of the attention over a 4-bit cache: one per SM
 static const int PAP_MAX_WINDOW = 64;         // largest query window of the probe (the paper ablates 1, 4 and 64)
