@@ -135,7 +135,8 @@ spts_status launch_plain(spts_ctx* ctx, const W4GemvArgs& a) {
 constexpr int W4_WARPS = 8;
 constexpr int W4_CHUNK = 128;
 constexpr int W4_WK = 1;
-constexpr int W4_LOCAL = 16384;            // elements of x that a CTA lays out for itself
+// elements of x that a CTA lays out for itself: 2.5 bytes each beside a ring of up to 80 KB, two CTAs to an SM
+constexpr int W4_LOCAL = 12288;
 
 // The order of k inside a chunk: step t of the chunk's four, lane c, eight consecutive codes (one word).  A lane's words lie
 // side by side within a group, so that they are one shared-memory load.
@@ -231,8 +232,7 @@ template <int MT, bool TWO> __device__ __forceinline__ int w4_place(int r) {
 template <int NB, int MT, int NGC, bool TWO, int WK, bool LOCAL>
 __global__ void __launch_bounds__(W4_WARPS * 32, NB > 2 ? 1 : 2)
 w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf16* __restrict__ X, int64_t ldx, int norm, float eps,
-               const uint4* __restrict__ frag_g, const uint4* __restrict__ sums_g, const float* __restrict__ factor_g,
-               float* __restrict__ part, W4Out o) {
+               const uint4* frag_g, const uint4* sums_g, float* factor_g, float* __restrict__ part, W4Out o) {
   using T = W4Tile<NB, MT, NGC, WK>;
   constexpr int WR = T::WR, WROWS = TWO ? 8 * MT : 16 * MT, ROWS = WR * WROWS;      // output features of a warp, of a tile
   constexpr int RSTRIDE = WR * MT * 16;
@@ -330,11 +330,13 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
       w4_prepare<NGC, W4_WARPS * 32>(X + (size_t)t * ldx, t, n, in, norm, eps, x_local, sums_l, sm_factor);
     frag = x_local;
     sums = sums_l;
+    __syncthreads();
+    if (blockIdx.x == 0 && threadIdx.x < n) factor_g[threadIdx.x] = sm_factor[threadIdx.x];      // for the join
   } else {
     dep_wait();                                               // x is prepared
-    if (threadIdx.x < n) sm_factor[threadIdx.x] = __ldg(factor_g + threadIdx.x);
+    if (threadIdx.x < n) sm_factor[threadIdx.x] = __ldcg(factor_g + threadIdx.x);
+    __syncthreads();
   }
-  __syncthreads();
   dep_launch();
 
   int tile = (int)(u0 / line.steps), step = (int)(u0 - (long)tile * line.steps);
@@ -347,19 +349,35 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[nb][mt][i] = 0.f;
-    for (int chunk = step * WK + wk; chunk < c1; chunk += WK) {
-      uint4 xf[NB][4], xs[NB];
+    // a chunk's x: one chunk ahead of its use where it comes from L1 or L2 and the registers allow
+    constexpr bool AHEAD = !LOCAL && NB == 1;
+    uint4 xf[NB][4], xs[NB], xf2[NB][4], xs2[NB];
+    auto load_x = [&](int chunk, uint4 (&f)[NB][4], uint4 (&sm)[NB]) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         const bool has = 8 * nb + g < n;
         const uint4* fp = frag + ((size_t)chunk * 4 * n + 8 * nb + g) * 4 + cc;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          xf[nb][t] = make_uint4(0u, 0u, 0u, 0u);
-          if (has) xf[nb][t] = fp[(size_t)t * 4 * n];
+          f[nb][t] = make_uint4(0u, 0u, 0u, 0u);
+          if (has) f[nb][t] = fp[(size_t)t * 4 * n];
         }
-        xs[nb] = make_uint4(0u, 0u, 0u, 0u);
-        if (has && cc < NGC) xs[nb] = sums[((size_t)chunk * n + 8 * nb + g) * 4 + cc];
+        sm[nb] = make_uint4(0u, 0u, 0u, 0u);
+        if (has && cc < NGC) sm[nb] = sums[((size_t)chunk * n + 8 * nb + g) * 4 + cc];
+      }
+    };
+    if (AHEAD && step * WK + wk < c1) load_x(step * WK + wk, xf2, xs2);
+    for (int chunk = step * WK + wk; chunk < c1; chunk += WK) {
+      if (AHEAD) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          xs[nb] = xs2[nb];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) xf[nb][t] = xf2[nb][t];
+        }
+        if (chunk + WK < c1) load_x(chunk + WK, xf2, xs2);
+      } else {
+        load_x(chunk, xf, xs);
       }
       fetch_next();
       cp_async_wait<T::STAGES - 1>();
@@ -510,19 +528,18 @@ spts_status launch_tile(spts_ctx* ctx, const W4GemvArgs& a) {
   uint4* frag = (uint4*)ctx->ws.w4_x;
   uint4* sums = frag + (size_t)chunks * 16 * a.n;
   float* factor = (float*)(sums + (size_t)chunks * 4 * a.n);
-  const bool local = LOCAL && !cut;
-  if (!local) {
+  if (!LOCAL) {
     w4_prepare_kernel<NGC><<<a.n, 512, 0, ctx->stream>>>((const bf16*)a.X, a.ldx, a.in, a.n, a.norm, ctx->desc.rms_eps, frag, sums, factor);
     SPTS_CUDA_OK(ctx);
   }
-  auto kernel = local ? w4_gemv_kernel<NB, MT, NGC, TWO, WK, LOCAL> : w4_gemv_kernel<NB, MT, NGC, TWO, WK, false>;
-  const size_t smem = T::RING + (size_t)a.n * T::RED + (local ? (size_t)chunks * a.n * (16 + 4) * 16 : 0);
+  auto kernel = w4_gemv_kernel<NB, MT, NGC, TWO, WK, LOCAL>;
+  const size_t smem = T::RING + (size_t)a.n * T::RED + (LOCAL ? (size_t)chunks * a.n * (16 + 4) * 16 : 0);
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return SPTS_ERR_CUDA;
   const W4Mat m1{(const char*)a.codes, (const uint32_t*)a.params}, m2{(const char*)a.codes2, (const uint32_t*)a.params2};
   const cudaError_t e = [&]() {
-    if (!local)
+    if (!LOCAL)
       return launch_dep_smem(kernel, dim3(line.ctas), W4_WARPS * 32, smem, ctx->stream, m1, m2, a.out, a.in, a.n, line, (const bf16*)a.X, a.ldx,
-                             a.norm, ctx->desc.rms_eps, (const uint4*)frag, (const uint4*)sums, (const float*)factor, ctx->ws.w4_part, o);
+                             a.norm, ctx->desc.rms_eps, (const uint4*)frag, (const uint4*)sums, factor, ctx->ws.w4_part, o);
     kernel<<<line.ctas, W4_WARPS * 32, smem, ctx->stream>>>(m1, m2, a.out, a.in, a.n, line, (const bf16*)a.X, a.ldx, a.norm,
                                                             ctx->desc.rms_eps, frag, sums, factor, ctx->ws.w4_part, o);
     return cudaGetLastError();
@@ -543,11 +560,12 @@ spts_status launch_rows(spts_ctx* ctx, const W4GemvArgs& a) {
     if (a.codes2 != nullptr) return launch_tile<NB, 2, NGC, true, 1, false>(ctx, a);
     return launch_tile<NB, 2, NGC, false, 1, false>(ctx, a);
   } else {
-    // few rows: all eight warps on one tile of 16, and few elements of x are laid out in the kernel itself
-    if (a.codes2 != nullptr) return launch_tile<1, 2, NGC, true, W4_WK, false>(ctx, a);
+    // few elements of x are laid out in the kernel itself; few rows: all eight warps on one tile of 16
+    const bool local = (long)a.n * align_up((size_t)a.in, W4_CHUNK) <= W4_LOCAL;
+    if (a.codes2 != nullptr) return local ? launch_tile<1, 2, NGC, true, W4_WK, true>(ctx, a) : launch_tile<1, 2, NGC, true, W4_WK, false>(ctx, a);
     if (ceil_div(a.out, 16) <= 2 * ctx->sm_count)
-      return (long)a.n * a.in <= W4_LOCAL ? launch_tile<1, 1, NGC, false, 8, true>(ctx, a) : launch_tile<1, 1, NGC, false, 8, false>(ctx, a);
-    return launch_tile<1, 2, NGC, false, W4_WK, false>(ctx, a);
+      return local ? launch_tile<1, 1, NGC, false, 8, true>(ctx, a) : launch_tile<1, 1, NGC, false, 8, false>(ctx, a);
+    return local ? launch_tile<1, 2, NGC, false, W4_WK, true>(ctx, a) : launch_tile<1, 2, NGC, false, W4_WK, false>(ctx, a);
   }
 }
 template <int NB>
