@@ -134,7 +134,7 @@ spts_status launch_plain(spts_ctx* ctx, const W4GemvArgs& a) {
 // copies runs on across tiles.
 constexpr int W4_WARPS = 8;
 constexpr int W4_CHUNK = 128;
-constexpr int W4_WK = 1;
+constexpr int W4_WK = 4;
 // elements of x that a CTA lays out for itself: 2.5 bytes each beside a ring of up to 80 KB, two CTAs to an SM
 constexpr int W4_LOCAL = 12288;
 
@@ -144,15 +144,17 @@ template <int NGC> __host__ __device__ constexpr int w4_k(int t, int c) {
   return NGC == 1 ? 32 * c + 8 * t : NGC == 2 ? 64 * (t >> 1) + 16 * c + 8 * (t & 1) : 32 * t + 8 * c;
 }
 
-// x [n, in] -> frag [chunk][t][n][c] (16 bytes: four fp16 pairs), sums [chunk][n][c] (three pairs of pieces), factor [n];
-// one token, by a CTA of THREADS
+// x [n, in] -> blocks [chunk][n] of W4_BLOCK bytes: fragments [t][c] (16 bytes: four fp16 pairs), then sums [c] (three pairs of
+// pieces; zero where there is no c-th group); factor [n].  One token, by a CTA of THREADS.
+constexpr int W4_BLOCK = 320;
 template <int NGC, int THREADS>
-__device__ __forceinline__ void w4_prepare(const bf16* __restrict__ x, int token, int n, int in, int norm, float eps, uint4* frag,
-                                           uint4* sums, float* factor) {
+__device__ __forceinline__ void w4_prepare(const bf16* __restrict__ x, int token, int n, int in, int norm, float eps,
+                                           unsigned char* blocks, float* factor) {
   constexpr int WARPS = THREADS / 32;
   __shared__ float red[2][WARPS];
   const int tid = threadIdx.x, lane = tid & 31;
   float top = 0.f, ss = 0.f;
+#pragma unroll 4
   for (int k = 8 * tid; k < in; k += 8 * THREADS) {
     float v[8];
     load8(x + k, v);
@@ -170,15 +172,17 @@ __device__ __forceinline__ void w4_prepare(const bf16* __restrict__ x, int token
   const float xs = scale_to_2_13(top), u = xs * CODE_UNIT;
   if (tid == 0) factor[token] = (norm ? 1.0f / sqrtf(ss / (float)in + eps) : 1.0f) / u;
   const int chunks = (in + W4_CHUNK - 1) / W4_CHUNK, total = chunks * 16;
+#pragma unroll 2
   for (int i0 = tid & ~31; i0 < total; i0 += THREADS) {
     const int i = i0 + lane, chunk = i >> 4, t = (i >> 2) & 3, c = i & 3;
     const int k = chunk * W4_CHUNK + w4_k<NGC>(t, c);
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (i < total && k < in) load8(x + k, v);
     float s = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+    uint4* block = reinterpret_cast<uint4*>(blocks + ((size_t)chunk * n + token) * W4_BLOCK);
     if (i < total) {
       const float xo = xs * ODD;
-      frag[((size_t)(chunk * 4 + t) * n + token) * 4 + c] =
+      block[t * 4 + c] =
           make_uint4(pack2_f16(v[0] * xs, v[4] * xs), pack2_f16(v[1] * xo, v[5] * xo), pack2_f16(v[2] * xs, v[6] * xs),
                      pack2_f16(v[3] * xo, v[7] * xo));
     }
@@ -188,17 +192,17 @@ __device__ __forceinline__ void w4_prepare(const bf16* __restrict__ x, int token
     if (i < total && i % LANES == 0) {
       const float sm = s * u, a = -8.f * sm;
       const float ah = round_bf16(a), mh = round_bf16(sm), am = round_bf16(a - ah), mm = round_bf16(sm - mh);
-      sums[((size_t)chunk * n + token) * 4 + (i % 16) / LANES] =
-          make_uint4(pack2(ah, mh), pack2(am, mm), pack2((a - ah) - am, (sm - mh) - mm), 0u);
+      block[16 + (i % 16) / LANES] = make_uint4(pack2(ah, mh), pack2(am, mm), pack2((a - ah) - am, (sm - mh) - mm), 0u);
     }
+    if (NGC < 4 && i < total && i % 16 < 4 - NGC) block[16 + NGC + i % 16] = make_uint4(0u, 0u, 0u, 0u);
   }
 }
 template <int NGC>
-__global__ void __launch_bounds__(512)
-w4_prepare_kernel(const bf16* __restrict__ X, int64_t ldx, int in, int n, int norm, float eps, uint4* __restrict__ frag,
-                  uint4* __restrict__ sums, float* __restrict__ factor) {
+__global__ void __launch_bounds__(1024)
+w4_prepare_kernel(const bf16* __restrict__ X, int64_t ldx, int in, int n, int norm, float eps, unsigned char* __restrict__ blocks,
+                  float* __restrict__ factor) {
   dep_launch();
-  w4_prepare<NGC, 512>(X + (size_t)blockIdx.x * ldx, blockIdx.x, n, in, norm, eps, frag, sums, factor);
+  w4_prepare<NGC, 1024>(X + (size_t)blockIdx.x * ldx, blockIdx.x, n, in, norm, eps, blocks, factor);
 }
 
 template <int NB, int MT, int NGC, int WK>
@@ -215,10 +219,13 @@ struct W4Mat { const char* codes; const uint32_t* params; };
 
 // The line of steps: tiles x steps, cut into `ctas` pieces.  A share is [token][a tile's rows in the order wr, mt, row]; a CTA
 // has at most two: 2 cta + 1 of a tile that begins in its piece, 2 cta of one that began before.
+// With `whole` the cuts fall between tiles.
 struct W4Line {
-  int tiles, steps, ctas;
+  int tiles, steps, ctas, whole;
   __device__ __forceinline__ long total() const { return (long)tiles * steps; }
-  __device__ __forceinline__ long begin(int cta) const { return total() * cta / ctas; }
+  __device__ __forceinline__ long begin(int cta) const {
+    return whole ? (long)steps * (int)((long)tiles * cta / ctas) : total() * cta / ctas;
+  }
   __device__ __forceinline__ int cta_of(long x) const { return (int)(((x + 1) * ctas - 1) / total()); }
 };
 
@@ -232,7 +239,7 @@ template <int MT, bool TWO> __device__ __forceinline__ int w4_place(int r) {
 template <int NB, int MT, int NGC, bool TWO, int WK, bool LOCAL>
 __global__ void __launch_bounds__(W4_WARPS * 32, NB > 2 ? 1 : 2)
 w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf16* __restrict__ X, int64_t ldx, int norm, float eps,
-               const uint4* frag_g, const uint4* sums_g, float* factor_g, float* __restrict__ part, W4Out o) {
+               const unsigned char* blocks_g, float* factor_g, float* __restrict__ part, W4Out o) {
   using T = W4Tile<NB, MT, NGC, WK>;
   constexpr int WR = T::WR, WROWS = TWO ? 8 * MT : 16 * MT, ROWS = WR * WROWS;      // output features of a warp, of a tile
   constexpr int RSTRIDE = WR * MT * 16;
@@ -244,7 +251,7 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
   const int chunks = (in + W4_CHUNK - 1) / W4_CHUNK, groups = in / (128 / NGC);
   const size_t row_bytes = in / 2;
   float* red = reinterpret_cast<float*>(smem + T::RING);
-  uint4* x_local = reinterpret_cast<uint4*>(smem + T::RING + n * T::RED);
+  unsigned char* x_local = smem + T::RING + n * T::RED;       // a block of zeros, then LOCAL's blocks
   unsigned char* ring = smem + warp * (T::STAGES * T::STAGE);
   const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
   const bool whole_chunks = groups % NGC == 0;                // a row's params of a chunk are one aligned copy
@@ -322,14 +329,12 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
   };
 #pragma unroll
   for (int i = 0; i < T::STAGES - 1; ++i) fetch_next();
-  const uint4* frag = frag_g;
-  const uint4* sums = sums_g;
+  if (threadIdx.x < W4_BLOCK / 16) reinterpret_cast<uint4*>(x_local)[threadIdx.x] = make_uint4(0u, 0u, 0u, 0u);
+  const unsigned char* blocks = blocks_g;
   if (LOCAL) {
-    uint4* sums_l = x_local + (size_t)chunks * 16 * n;
     for (int t = 0; t < n; ++t)
-      w4_prepare<NGC, W4_WARPS * 32>(X + (size_t)t * ldx, t, n, in, norm, eps, x_local, sums_l, sm_factor);
-    frag = x_local;
-    sums = sums_l;
+      w4_prepare<NGC, W4_WARPS * 32>(X + (size_t)t * ldx, t, n, in, norm, eps, x_local + W4_BLOCK, sm_factor);
+    blocks = x_local + W4_BLOCK;
     __syncthreads();
     if (blockIdx.x == 0 && threadIdx.x < n) factor_g[threadIdx.x] = sm_factor[threadIdx.x];      // for the join
   } else {
@@ -349,24 +354,27 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[nb][mt][i] = 0.f;
-    // a chunk's x: one chunk ahead of its use where it comes from L1 or L2 and the registers allow
+    // a chunk's x: one chunk ahead of its use where it comes from L1 or L2 and the registers allow.  Lanes of absent tokens read
+    // the block of zeros.
     constexpr bool AHEAD = !LOCAL && NB == 1;
     uint4 xf[NB][4], xs[NB], xf2[NB][4], xs2[NB];
-    auto load_x = [&](int chunk, uint4 (&f)[NB][4], uint4 (&sm)[NB]) {
+    const unsigned char* xp[NB];
+    const size_t x_step = (size_t)WK * n * W4_BLOCK;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int token = 8 * nb + g;
+      xp[nb] = (token < n ? blocks + ((size_t)(step * WK + wk) * n + token) * W4_BLOCK : x_local) + 16 * cc;
+    }
+    auto load_x = [&](uint4 (&f)[NB][4], uint4 (&sm)[NB]) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        const bool has = 8 * nb + g < n;
-        const uint4* fp = frag + ((size_t)chunk * 4 * n + 8 * nb + g) * 4 + cc;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          f[nb][t] = make_uint4(0u, 0u, 0u, 0u);
-          if (has) f[nb][t] = fp[(size_t)t * 4 * n];
-        }
-        sm[nb] = make_uint4(0u, 0u, 0u, 0u);
-        if (has && cc < NGC) sm[nb] = sums[((size_t)chunk * n + 8 * nb + g) * 4 + cc];
+        for (int t = 0; t < 4; ++t) f[nb][t] = *reinterpret_cast<const uint4*>(xp[nb] + 64 * t);
+        sm[nb] = *reinterpret_cast<const uint4*>(xp[nb] + 256);
+        if (8 * nb + g < n) xp[nb] += x_step;
       }
     };
-    if (AHEAD && step * WK + wk < c1) load_x(step * WK + wk, xf2, xs2);
+    if (AHEAD && step * WK + wk < c1) load_x(xf2, xs2);
     for (int chunk = step * WK + wk; chunk < c1; chunk += WK) {
       if (AHEAD) {
 #pragma unroll
@@ -375,62 +383,76 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
 #pragma unroll
           for (int t = 0; t < 4; ++t) xf[nb][t] = xf2[nb][t];
         }
-        if (chunk + WK < c1) load_x(chunk + WK, xf2, xs2);
+        if (chunk + WK < c1) load_x(xf2, xs2);
       } else {
-        load_x(chunk, xf, xs);
+        load_x(xf, xs);
       }
       fetch_next();
       cp_async_wait<T::STAGES - 1>();
       __syncwarp();
       const unsigned char* st = ring + use_at;
       use_at = use_at + T::STAGE == T::STAGES * T::STAGE ? 0 : use_at + T::STAGE;
+      const unsigned char* row = st + g * T::CSTRIDE + 4 * GT * cc;
+      const unsigned char* prm = st + T::PARAMS + g * NGC * 4;
+      // params words of groups that there are not meet zeros in x's sums (a NaN among them makes the row NaN, as it is)
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
-        const unsigned char* row0 = st + (16 * mt + g) * T::CSTRIDE;
-        const unsigned char* row1 = row0 + 8 * T::CSTRIDE;
-        const unsigned char* prm0 = st + T::PARAMS + (16 * mt + g) * NGC * 4;
-        const unsigned char* prm1 = prm0 + 8 * NGC * 4;
-        {
-          uint32_t p0 = 0u, p1 = 0u;
-          if (cc < NGC) { p0 = *reinterpret_cast<const uint32_t*>(prm0 + 4 * cc); p1 = *reinterpret_cast<const uint32_t*>(prm1 + 4 * cc); }
+        const uint32_t p0 = *reinterpret_cast<const uint32_t*>(prm + 16 * mt * NGC * 4 + 4 * (cc % NGC));
+        const uint32_t p1 = *reinterpret_cast<const uint32_t*>(prm + (16 * mt + 8) * NGC * 4 + 4 * (cc % NGC));
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-            mma16816(y[nb][mt], p0, p1, p0, p1, xs[nb].x, xs[nb].y);
-            if (o.fp32_out) mma16816(y[nb][mt], p0, p1, 0u, 0u, xs[nb].z, 0u);
+        for (int nb = 0; nb < NB; ++nb) {
+          mma16816(y[nb][mt], p0, p1, p0, p1, xs[nb].x, xs[nb].y);
+          if (o.fp32_out) mma16816(y[nb][mt], p0, p1, 0u, 0u, xs[nb].z, 0u);
+        }
+      }
+      uint32_t q[MT][2][NGC];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) load_words<NGC>(prm + (16 * mt + 8 * h) * NGC * 4, q[mt][h]);
+#pragma unroll
+      for (int gr = 0; gr < NGC; ++gr) {
+        uint32_t w[MT][2][GT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) load_words<GT>(row + (16 * mt + 8 * h) * T::CSTRIDE + (64 / NGC) * gr, w[mt][h]);
+        float acc[NB][MT][4];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[nb][mt][i] = 0.f;
+        // the row tiles take turns, so that a product does not wait for the one before it
+#pragma unroll
+        for (int tt = 0; tt < GT; ++tt) {
+          const int t = gr * GT + tt;
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            const uint32_t a0 = code_pair<0>(w[mt][0][tt]), a1 = code_pair<0>(w[mt][1][tt]);
+            const uint32_t a2 = code_pair<1>(w[mt][0][tt]), a3 = code_pair<1>(w[mt][1][tt]);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) mma_f16(acc[nb][mt], a0, a1, a2, a3, xf[nb][t].x, xf[nb][t].y);
+          }
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            const uint32_t a0 = code_pair<2>(w[mt][0][tt]), a1 = code_pair<2>(w[mt][1][tt]);
+            const uint32_t a2 = code_pair<3>(w[mt][0][tt]), a3 = code_pair<3>(w[mt][1][tt]);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) mma_f16(acc[nb][mt], a0, a1, a2, a3, xf[nb][t].z, xf[nb][t].w);
           }
         }
-        uint32_t w0[4], w1[4], q0[NGC], q1[NGC];
-        load_words<NGC>(prm0, q0);
-        load_words<NGC>(prm1, q1);
 #pragma unroll
-        for (int gr = 0; gr < NGC; ++gr) {
-          load_words<GT>(row0 + (64 / NGC) * gr + 4 * GT * cc, *reinterpret_cast<uint32_t (*)[GT]>(w0 + gr * GT));
-          load_words<GT>(row1 + (64 / NGC) * gr + 4 * GT * cc, *reinterpret_cast<uint32_t (*)[GT]>(w1 + gr * GT));
-        }
-#pragma unroll
-        for (int gr = 0; gr < NGC; ++gr) {
-          float acc[NB][4];
+        for (int mt = 0; mt < MT; ++mt) {
+          const float s0 = lo_bf16(q[mt][0][gr]), s1 = lo_bf16(q[mt][1][gr]);
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[nb][i] = 0.f;
-#pragma unroll
-          for (int tt = 0; tt < GT; ++tt) {
-            const int t = gr * GT + tt;
-            const uint32_t a0 = code_pair<0>(w0[t]), a1 = code_pair<0>(w1[t]), a2 = code_pair<1>(w0[t]), a3 = code_pair<1>(w1[t]);
-            const uint32_t b0 = code_pair<2>(w0[t]), b1 = code_pair<2>(w1[t]), b2 = code_pair<3>(w0[t]), b3 = code_pair<3>(w1[t]);
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-              mma_f16(acc[nb], a0, a1, a2, a3, xf[nb][t].x, xf[nb][t].y);
-              mma_f16(acc[nb], b0, b1, b2, b3, xf[nb][t].z, xf[nb][t].w);
+            for (int i = 0; i < 2; ++i) {
+              y[nb][mt][i] = fmaf(s0, acc[nb][mt][i], y[nb][mt][i]);
+              y[nb][mt][2 + i] = fmaf(s1, acc[nb][mt][2 + i], y[nb][mt][2 + i]);
             }
-          }
-          const float s0 = lo_bf16(q0[gr]), s1 = lo_bf16(q1[gr]);
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-            y[nb][mt][0] = fmaf(s0, acc[nb][0], y[nb][mt][0]); y[nb][mt][1] = fmaf(s0, acc[nb][1], y[nb][mt][1]);
-            y[nb][mt][2] = fmaf(s1, acc[nb][2], y[nb][mt][2]); y[nb][mt][3] = fmaf(s1, acc[nb][3], y[nb][mt][3]);
-          }
         }
       }
       __syncwarp();                                           // the stage may be filled again
@@ -520,28 +542,27 @@ spts_status launch_tile(spts_ctx* ctx, const W4GemvArgs& a) {
   line.steps = ceil_div(chunks, WK);
   const int most = (NB > 2 ? 1 : 2) * (ctx->sm_count < W4_MAX_CTAS / 2 ? ctx->sm_count : W4_MAX_CTAS / 2);
   const long total = (long)line.tiles * line.steps;
-  // a CTA per tile where that fills the SMs once and no more than the resident CTAs, or where tiles are too short for two more
-  // launches to pay (16 steps take about 8 us); else equal pieces of the line
-  const bool tile_each = line.tiles <= most && (line.tiles >= ctx->sm_count || (LOCAL && line.steps <= 16));
-  line.ctas = tile_each ? line.tiles : total < most ? (int)total : most;
-  const bool cut = !(line.tiles % line.ctas == 0);
-  uint4* frag = (uint4*)ctx->ws.w4_x;
-  uint4* sums = frag + (size_t)chunks * 16 * a.n;
-  float* factor = (float*)(sums + (size_t)chunks * 4 * a.n);
+  // Whole tiles where there are three for every resident CTA, or between one and two for every SM, or where tiles are too
+  // short for two more launches to pay (16 steps take about 8 us); else equal pieces of the line, whose cut tiles are joined.
+  line.whole = line.tiles >= 3 * most || (line.tiles <= most && (line.tiles >= ctx->sm_count || (LOCAL && line.steps <= 16)));
+  line.ctas = line.whole ? (line.tiles < most ? line.tiles : most) : total < most ? (int)total : most;
+  const bool cut = !line.whole;
+  unsigned char* blocks = (unsigned char*)ctx->ws.w4_x;
+  float* factor = (float*)(blocks + (size_t)chunks * a.n * W4_BLOCK);
   if (!LOCAL) {
-    w4_prepare_kernel<NGC><<<a.n, 512, 0, ctx->stream>>>((const bf16*)a.X, a.ldx, a.in, a.n, a.norm, ctx->desc.rms_eps, frag, sums, factor);
+    w4_prepare_kernel<NGC><<<a.n, 1024, 0, ctx->stream>>>((const bf16*)a.X, a.ldx, a.in, a.n, a.norm, ctx->desc.rms_eps, blocks, factor);
     SPTS_CUDA_OK(ctx);
   }
   auto kernel = w4_gemv_kernel<NB, MT, NGC, TWO, WK, LOCAL>;
-  const size_t smem = T::RING + (size_t)a.n * T::RED + (LOCAL ? (size_t)chunks * a.n * (16 + 4) * 16 : 0);
+  const size_t smem = T::RING + (size_t)a.n * T::RED + W4_BLOCK + (LOCAL ? (size_t)chunks * a.n * W4_BLOCK : 0);
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return SPTS_ERR_CUDA;
   const W4Mat m1{(const char*)a.codes, (const uint32_t*)a.params}, m2{(const char*)a.codes2, (const uint32_t*)a.params2};
   const cudaError_t e = [&]() {
     if (!LOCAL)
       return launch_dep_smem(kernel, dim3(line.ctas), W4_WARPS * 32, smem, ctx->stream, m1, m2, a.out, a.in, a.n, line, (const bf16*)a.X, a.ldx,
-                             a.norm, ctx->desc.rms_eps, (const uint4*)frag, (const uint4*)sums, factor, ctx->ws.w4_part, o);
+                             a.norm, ctx->desc.rms_eps, (const unsigned char*)blocks, factor, ctx->ws.w4_part, o);
     kernel<<<line.ctas, W4_WARPS * 32, smem, ctx->stream>>>(m1, m2, a.out, a.in, a.n, line, (const bf16*)a.X, a.ldx, a.norm,
-                                                            ctx->desc.rms_eps, frag, sums, factor, ctx->ws.w4_part, o);
+                                                            ctx->desc.rms_eps, blocks, factor, ctx->ws.w4_part, o);
     return cudaGetLastError();
   }();
   if (e != cudaSuccess) return SPTS_ERR_CUDA;
