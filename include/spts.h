@@ -493,6 +493,35 @@ typedef struct {
 spts_status spts_process_logits(spts_ctx* ctx, const float* logits, int64_t ld, int n, int vocab,
                                 const spts_logits_rules* rules, float* out, int64_t ldo, int32_t* token_out);
 
+/* One layer's weights in 4 bits: the projections of q, k and v stacked row after row, the others as in spts_layer_weights.
+ * RMSNorm gains are folded into the columns (spts_fold_norm_gain) before quantising. */
+typedef struct {
+  spts_w4 wqkv;    /* [(H + 2 Hkv) * d, D] */
+  spts_w4 wo;      /* [D, H * d]           */
+  spts_w4 w_gate;  /* [Dff, D]             */
+  spts_w4 w_up;    /* [Dff, D], the group of w_gate */
+  spts_w4 w_down;  /* [D, Dff]             */
+} spts_layer_weights4;
+
+typedef struct {
+  const spts_layer_weights4* layers; /* host array [n_layers] */
+  spts_w4 lm_head;                   /* [vocab, D]            */
+  const void* embed;                 /* [vocab, D] in the storage type, used with token_in */
+} spts_model_weights4;
+
+/* One decode step with 4-bit weights and caches for all sequences of the caches (Algorithm 1 outside the prefill phase: no
+ * skipping): one new token each, at most SPTS_W4_MAX_N and max_seq sequences.  `caches` is a host array [n_layers] with the
+ * same n_seq.  The tokens' rows are x_in [n_seq, D], or, if that is NULL, rows token_in[b] (DEVICE [n_seq]) of mw->embed (a
+ * token outside the vocabulary gives a row of zeros and SPTS_ERR_INDEX in the device status word).  pos (DEVICE [n_seq]) are
+ * their original positions.  Every layer appends the token's K / V to its cache (len grows on the device) and attends to what
+ * the cache then holds.  x_out [n_seq, D] optional.  logits_out [n_seq, vocab] fp32 receives the head's logits, with the rules
+ * applied where there are any; token_out [n_seq] (optional, needs logits_out) the largest one's token as in
+ * spts_process_logits.  Everything that changes from step to step lies on the device, so one captured step can be replayed:
+ * token_out may be the next step's token_in. */
+spts_status spts_decode_step4(spts_ctx* ctx, const spts_model_weights4* mw, const spts_kv4_cache* caches, const void* x_in,
+                              const int32_t* token_in, const int32_t* pos, const spts_logits_rules* rules, void* x_out,
+                              float* logits_out, int32_t* token_out);
+
 #ifdef __cplusplus
 }
 #endif

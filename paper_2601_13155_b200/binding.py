@@ -72,6 +72,14 @@ class Kv4CacheC(C.Structure):
                [(n, C.c_int32) for n in ("n_seq", "capacity", "group")]
 
 
+class LayerWeights4C(C.Structure):
+    _fields_ = [(n, W4C) for n in ("wqkv", "wo", "w_gate", "w_up", "w_down")]
+
+
+class ModelWeights4C(C.Structure):
+    _fields_ = [("layers", C.POINTER(LayerWeights4C)), ("lm_head", W4C), ("embed", C.c_void_p)]
+
+
 LOGITS_RULES = ("history", "history_start", "generated_start", "repetition", "presence", "frequency", "bias_token",
                 "bias_value", "bias_start", "mask")
 
@@ -92,7 +100,8 @@ EXPORTS = ("spts_workspace_bytes", "spts_create", "spts_destroy", "spts_set_opti
            "spts_topk_select_static", "spts_proxy_scratch_bytes", "spts_proxy_build",
            "spts_layer_prefill_skip_batch", "spts_msdp_plan", "spts_check_guards", "spts_selftest_wait_timeout",
            "spts_debug_check_index_list", "spts_reduced_attention", "spts_prepared_bytes", "spts_prepare_layer",
-           "spts_w4_quantize", "spts_w4_gemv", "spts_kv4_append", "spts_kv4_attention", "spts_process_logits")
+           "spts_w4_quantize", "spts_w4_gemv", "spts_kv4_append", "spts_kv4_attention", "spts_process_logits",
+           "spts_decode_step4")
 
 OP_NAMES = {1: "prep", 2: "kproj_pap", 3: "pap_softmax", 4: "topk", 5: "kv_gather", 6: "qv_proj", 7: "attention",
             8: "o_proj", 9: "ltp", 10: "gate_up", 11: "down", 12: "compact", 13: "head", 14: "decode"}
@@ -151,6 +160,8 @@ def load_library() -> C.CDLL:
     lib.spts_w4_gemv.argtypes = [vp, C.POINTER(W4C), C.POINTER(W4C), vp, i64, i32, vp, i64, u32, vp, i64]
     lib.spts_kv4_append.argtypes = [vp, C.POINTER(Kv4CacheC), vp, i64, vp, i64, vp, vp, vp, i32, vp, vp]
     lib.spts_kv4_attention.argtypes = [vp, C.POINTER(Kv4CacheC), vp, i64, vp, i64]
+    lib.spts_decode_step4.argtypes = [vp, C.POINTER(ModelWeights4C), C.POINTER(Kv4CacheC), vp, vp, vp, C.POINTER(LogitsRulesC),
+                                      vp, vp, vp]
     lib.spts_process_logits.argtypes = [vp, vp, i64, i32, i32, C.POINTER(LogitsRulesC), vp, i64, vp]
     for n in EXPORTS:
         if n not in ("spts_workspace_bytes", "spts_destroy", "spts_launch_count", "spts_proxy_scratch_bytes",
@@ -652,6 +663,52 @@ class Spts:
         if code:
             raise SptsError(code, "spts_process_logits")
         return out, token_out
+
+    def quantize_layer4(self, tensors: Dict[str, torch.Tensor], group: int = 128) -> Dict[str, W4Weight]:
+        """The 4-bit form of one layer's matrices (wq, wk, wv, wo, w_gate, w_up, w_down in the storage type)."""
+        qkv = torch.cat([tensors["wq"], tensors["wk"], tensors["wv"]], 0).contiguous()
+        out = {"wqkv": self.w4_quantize(qkv, group)}
+        for name in ("wo", "w_gate", "w_up", "w_down"):
+            out[name] = self.w4_quantize(tensors[name], group)
+        self.stream.synchronize()                                  # qkv is released on return
+        return out
+
+    def decode_step4(self, model: "Model4", caches: "Kv4Caches", pos, x_in=None, token_in=None, rules: Optional[LogitsRules] = None,
+                     x_out=None, logits_out=None, token_out=None):
+        """spts_decode_step4: one token for every sequence of the caches; pos, token_in, token_out are device int32 [n_seq]."""
+        n, s, dev, i32 = caches.n_seq, self.shape, self.dev, torch.int32
+        if len(model.layers) != s.n_layers or len(caches.layers) != s.n_layers:
+            raise ValueError(f"{s.n_layers} layers of weights and caches are needed")
+        for cache in caches.layers:
+            self._kv4_shape(cache)
+        if rules is not None:
+            rules.check(n, s.vocab, dev)
+        code = self.lib.spts_decode_step4(self.h, model.c, caches.c, _vec(x_in, n * s.hidden, self.dtype, "x_in", dev),
+                                          _vec(token_in, n, i32, "token_in", dev), _vec(pos, n, i32, "pos", dev),
+                                          rules.c if rules is not None else None, _vec(x_out, n * s.hidden, self.dtype, "x_out", dev),
+                                          _vec(logits_out, n * s.vocab, torch.float32, "logits_out", dev),
+                                          _vec(token_out, n, i32, "token_out", dev))
+        if code:
+            raise SptsError(code, "spts_decode_step4")
+
+
+class Kv4Caches:
+    """The 4-bit caches of all layers, n_seq sequences each."""
+
+    def __init__(self, shape, n_layers: int, n_seq: int, capacity: int, group: int = 64, device="cuda:0", positions: bool = True):
+        self.layers = [Kv4Cache(shape, n_seq, capacity, group, device, positions=positions) for _ in range(n_layers)]
+        self.n_seq = n_seq
+        self.c = (Kv4CacheC * n_layers)(*[cache.c for cache in self.layers])
+
+
+class Model4:
+    """All layers' weights in 4 bits (dicts as Spts.quantize_layer4 gives them), the LM head and the embedding table."""
+
+    def __init__(self, layers: List[Dict[str, W4Weight]], lm_head: Optional[W4Weight] = None, embed: Optional[torch.Tensor] = None):
+        self.layers, self.lm_head, self.embed = layers, lm_head, embed
+        self._arr = (LayerWeights4C * len(layers))(*[LayerWeights4C(*[w[n].c for n in ("wqkv", "wo", "w_gate", "w_up", "w_down")])
+                                                     for w in layers])
+        self.c = ModelWeights4C(self._arr, lm_head.c if lm_head is not None else W4C(), embed.data_ptr() if embed is not None else None)
 
 
 class Model:

@@ -104,6 +104,14 @@ size_t carve(const spts_model_desc& d, int Nmax, void* base, Workspace* ws, std:
   w.acc32_elems = N * KD;
   if (Npad * HD * es >= w.acc32_elems * sizeof(float)) w.acc32 = reinterpret_cast<float*>(w.o_att);
   else w.acc32 = c.take<float>(w.acc32_elems);
+  {
+    const size_t Q = HD + 2 * KD, n = SPTS_W4_MAX_N;
+    w.s4_x = c.take<char>(n * d.hidden * es);
+    w.s4_qkv32 = c.take<float>(n * Q);
+    w.s4_qkv = c.take<char>(n * Q * es);
+    w.s4_att = c.take<char>(n * HD * es);
+    w.s4_hm = c.take<char>(n * d.ffn_dim * es);
+  }
   // fragments 2 bytes an element; sums 16 bytes per 32; factors
   w.w4_x = c.take<char>(W4_X_ELEMENTS * 2 + W4_X_ELEMENTS / 2 + 256);
   w.w4_part = c.take<float>((size_t)2 * W4_MAX_CTAS * 16 * 256);
@@ -1253,6 +1261,66 @@ spts_status spts_process_logits(spts_ctx* ctx, const float* logits, int64_t ld, 
   if (r.n_bias == 0) r.bias_token = nullptr;
   ON_DEVICE(ctx);
   return launch_process_logits(ctx, logits, ld, n, vocab, r, out, ldo, token_out);
+}
+
+
+spts_status spts_decode_step4(spts_ctx* ctx, const spts_model_weights4* mw, const spts_kv4_cache* caches, const void* x_in,
+                              const int32_t* token_in, const int32_t* pos, const spts_logits_rules* rules, void* x_out,
+                              float* logits_out, int32_t* token_out) {
+  TRY(check_ctx(ctx));
+  if (mw == nullptr || mw->layers == nullptr || caches == nullptr) return SPTS_ERR_INVALID_ARG;
+  const auto& d = ctx->desc;
+  const int n = caches[0].n_seq, D = d.hidden, HD = d.n_q_heads * d.head_dim, KD = d.n_kv_heads * d.head_dim, Q = HD + 2 * KD;
+  const auto fits = [&](const spts_w4& w, int out, int in) { return w.out_features == out && w.in_features == in; };
+  for (int l = 0; l < d.n_layers; ++l) {
+    TRY(check_kv4(ctx, &caches[l]));
+    const spts_layer_weights4& w = mw->layers[l];
+    TRY(check_w4(&w.wqkv)); TRY(check_w4(&w.wo)); TRY(check_w4(&w.w_gate)); TRY(check_w4(&w.w_up)); TRY(check_w4(&w.w_down));
+    if (caches[l].n_seq != n || !fits(w.wqkv, Q, D) || !fits(w.wo, D, HD) || !fits(w.w_gate, d.ffn_dim, D) || !fits(w.w_up, d.ffn_dim, D) ||
+        !fits(w.w_down, D, d.ffn_dim) || w.w_gate.group != w.w_up.group)
+      return SPTS_ERR_SHAPE;
+  }
+  if (n > SPTS_W4_MAX_N || n > ctx->max_seq) return SPTS_ERR_SHAPE;
+  if (n == 0) return SPTS_OK;
+  if (pos == nullptr || (x_in == nullptr && (token_in == nullptr || mw->embed == nullptr))) return SPTS_ERR_INVALID_ARG;
+  if (!aligned16(x_in) || !aligned16(x_out) || !aligned16(mw->embed)) return SPTS_ERR_INVALID_ARG;
+  const bool head = logits_out != nullptr || token_out != nullptr;
+  if (head) {
+    if (logits_out == nullptr || d.vocab < 1) return SPTS_ERR_INVALID_ARG;
+    TRY(check_w4(&mw->lm_head));
+    if (!fits(mw->lm_head, d.vocab, D)) return SPTS_ERR_SHAPE;
+  }
+  ON_DEVICE(ctx);
+  Workspace& ws = ctx->ws;
+  const size_t es = elt_size(d);
+  char* qkv = (char*)ws.s4_qkv;
+  TRY(launch_rope_table(ctx, pos, n, ws.rope_cs));
+  ctx->rope_pos = nullptr;
+  if (x_in != nullptr) {
+    if (cudaMemcpyAsync(ws.s4_x, x_in, (size_t)n * D * es, cudaMemcpyDeviceToDevice, ctx->stream) != cudaSuccess) return SPTS_ERR_CUDA;
+  } else {
+    TRY(launch_embed_rows(ctx, mw->embed, token_in, n, ws.s4_x));
+  }
+  for (int l = 0; l < d.n_layers; ++l) {
+    const spts_layer_weights4& w = mw->layers[l];
+    const int64_t q = Q;
+    TRY(spts_w4_gemv(ctx, &w.wqkv, nullptr, ws.s4_x, D, n, nullptr, 0, SPTS_W4_NORM | SPTS_W4_FP32_OUT, ws.s4_qkv32, q));
+    TRY(launch_rope_rows(ctx, ws.s4_qkv32, ws.rope_cs, n, qkv));
+    TRY(spts_kv4_append(ctx, &caches[l], qkv + (size_t)HD * es, q, qkv + (size_t)(HD + KD) * es, q, pos, nullptr, nullptr, n, nullptr, nullptr));
+    TRY(spts_kv4_attention(ctx, &caches[l], qkv, q, ws.s4_att, HD));
+    TRY(spts_w4_gemv(ctx, &w.wo, nullptr, ws.s4_att, HD, n, ws.s4_x, D, 0, ws.s4_x, D));
+    TRY(spts_w4_gemv(ctx, &w.w_gate, &w.w_up, ws.s4_x, D, n, nullptr, 0, SPTS_W4_NORM, ws.s4_hm, d.ffn_dim));
+    TRY(spts_w4_gemv(ctx, &w.w_down, nullptr, ws.s4_hm, d.ffn_dim, n, ws.s4_x, D, 0, ws.s4_x, D));
+  }
+  if (x_out != nullptr &&
+      cudaMemcpyAsync(x_out, ws.s4_x, (size_t)n * D * es, cudaMemcpyDeviceToDevice, ctx->stream) != cudaSuccess)
+    return SPTS_ERR_CUDA;
+  if (!head) return SPTS_OK;
+  TRY(spts_w4_gemv(ctx, &mw->lm_head, nullptr, ws.s4_x, D, n, nullptr, 0, SPTS_W4_NORM | SPTS_W4_FP32_OUT, logits_out, d.vocab));
+  if (rules == nullptr && token_out == nullptr) return SPTS_OK;
+  spts_logits_rules none;
+  memset(&none, 0, sizeof(none));
+  return spts_process_logits(ctx, logits_out, d.vocab, n, d.vocab, rules != nullptr ? rules : &none, logits_out, d.vocab, token_out);
 }
 
 }  // extern "C"

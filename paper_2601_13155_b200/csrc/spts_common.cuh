@@ -90,6 +90,11 @@ struct Workspace {
   int32_t* row_seq;     // [Nmax]
   int32_t* vt_col;      // [Nmax]
   int vt_ld_max;        // columns of v_t
+  void* s4_x;           // [SPTS_W4_MAX_N, D] the residual rows of a 4-bit decode step
+  float* s4_qkv32;      // [SPTS_W4_MAX_N, (H + 2 Hkv) d] projections before the rotation
+  void* s4_qkv;         // the same behind it
+  void* s4_att;         // [SPTS_W4_MAX_N, H d]
+  void* s4_hm;          // [SPTS_W4_MAX_N, Dff]
   void* w4_x;           // tokens prepared for a 4-bit product: fragments, group sums, factors
   float* w4_part;       // [2 W4_MAX_CTAS, 32, 256] shares of CTAs that split a product's input axis
   float* kv4_part;      // [2 * KV4_MAX_CTAS, 16, d + 2] partial results of the attention over a 4-bit cache
@@ -275,6 +280,10 @@ spts_status launch_kv4_append(spts_ctx* ctx, const spts_kv4_cache* cache, const 
 spts_status launch_kv4_attention(spts_ctx* ctx, const spts_kv4_cache* cache, const void* Q, int64_t ldq, void* O, int64_t ldo);
 spts_status launch_process_logits(spts_ctx* ctx, const float* logits, int64_t ld, int n, int vocab,
                                   const spts_logits_rules& rules, float* out, int64_t ldo, int32_t* token);
+
+// ---- kernels_step4.cu
+spts_status launch_embed_rows(spts_ctx* ctx, const void* embed, const int32_t* token, int n, void* x);
+spts_status launch_rope_rows(spts_ctx* ctx, const float* in, const float2* cs, int n, void* out);
 
 // Programmatic dependent launch for chains of short kernels (the decode step, the passes of a top-k): a kernel
 // lets its successor start early (dep_launch), does whatever does not depend on its predecessor (prefetching
