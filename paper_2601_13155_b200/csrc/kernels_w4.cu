@@ -127,29 +127,35 @@ spts_status launch_plain(spts_ctx* ctx, const W4GemvArgs& a) {
 // programmatic dependent the product kernel is: it fills its rings with weights meanwhile.
 //
 // Work split.  A warp takes 16 MT rows (gate and up rows alternating in MT when there are two matrices), a CTA's WR x WK warps
-// a tile of WR such blocks and WK chunks of 128 of the input axis at a time.  The steps (WK chunks of a tile) of all tiles form
+// a tile of WR such blocks and WK chunks of 256 of the input axis at a time.  The steps (WK chunks of a tile) of all tiles form
 // one line that is cut into equal pieces, one per CTA (persistent); a tile that lies in one piece is finished there, of a tile
 // cut between CTAs each leaves its share, and w4_join_kernel adds them in the order of the CTAs.  (The CTA that arrives last
 // added them at first: one CTA's loads for 21 tokens x 256 rows x 21 shares took 50 us.)  Every warp's ring of asynchronous
 // copies runs on across tiles.
 constexpr int W4_WARPS = 8;
-constexpr int W4_CHUNK = 128;
+// 256 features: a row's codes of a chunk are one line of 128 bytes, its params 8 to 32 bytes.  (With chunks of 128 the copies
+// spend twice as many line accesses per byte, and the loop's own instructions weigh twice as much.)
+constexpr int W4_CHUNK = 256;
 constexpr int W4_WK = 4;
-// elements of x that a CTA lays out for itself: 2.5 bytes each beside a ring of up to 80 KB, two CTAs to an SM
-constexpr int W4_LOCAL = 12288;
+// elements of x that a CTA lays out for itself: 2.5 bytes each beside a ring of up to 82 KB, two CTAs to an SM
+constexpr int W4_LOCAL = 8192;
 
-// The order of k inside a chunk: step t of the chunk's four, lane c, eight consecutive codes (one word).  A lane's words lie
-// side by side within a group, so that they are one shared-memory load.
-template <int NGC> __host__ __device__ constexpr int w4_k(int t, int c) {
-  return NGC == 1 ? 32 * c + 8 * t : NGC == 2 ? 64 * (t >> 1) + 16 * c + 8 * (t & 1) : 32 * t + 8 * c;
-}
+// NG groups to a chunk (2, 4 or 8): a lane c holds GT = 8 / NG neighbouring words (of eight codes) of a row's group, one
+// shared-memory load; any order of k serves a dot product, so x's fragments follow: step t of the chunk's eight is word t % GT
+// of group t / GT.
+template <int NG> struct W4Order {
+  static constexpr int GT = 8 / NG, LANES = 4 * GT;              // LANES of the layout hold a group
+  static constexpr int SUMS = NG < 4 ? 4 : NG;                   // entries of the groups' sums
+  static constexpr int BLOCK = 512 + 16 * SUMS;                  // bytes of a token's block
+  __host__ __device__ static constexpr int k(int t, int c) { return (t / GT) * (W4_CHUNK / NG) + c * (W4_CHUNK / NG / 4) + 8 * (t % GT); }
+};
 
-// x [n, in] -> blocks [chunk][n] of W4_BLOCK bytes: fragments [t][c] (16 bytes: four fp16 pairs), then sums [c] (three pairs of
-// pieces; zero where there is no c-th group); factor [n].  One token, by a CTA of THREADS.
-constexpr int W4_BLOCK = 320;
-template <int NGC, int THREADS>
+// x [n, in] -> blocks [chunk][n] of W4Order::BLOCK bytes: fragments [t][c] (16 bytes: four fp16 pairs), then sums [group] (three
+// pairs of pieces; zero where there is no such group); factor [n].  One token, by a CTA of THREADS.
+template <int NG, int THREADS>
 __device__ __forceinline__ void w4_prepare(const bf16* __restrict__ x, int token, int n, int in, int norm, float eps,
                                            unsigned char* blocks, float* factor) {
+  using L = W4Order<NG>;
   constexpr int WARPS = THREADS / 32;
   __shared__ float red[2][WARPS];
   const int tid = threadIdx.x, lane = tid & 31;
@@ -169,48 +175,44 @@ __device__ __forceinline__ void w4_prepare(const bf16* __restrict__ x, int token
   top = red[0][0]; ss = red[1][0];
 #pragma unroll
   for (int w = 1; w < WARPS; ++w) { top = fmaxf(top, red[0][w]); ss += red[1][w]; }
-  const float xs = scale_to_2_13(top), u = xs * CODE_UNIT;
+  const float xs = scale_to_2_13(top), xo = xs * ODD, u = xs * CODE_UNIT;
   if (tid == 0) factor[token] = (norm ? 1.0f / sqrtf(ss / (float)in + eps) : 1.0f) / u;
-  const int chunks = (in + W4_CHUNK - 1) / W4_CHUNK, total = chunks * 16;
+  const int chunks = (in + W4_CHUNK - 1) / W4_CHUNK;
+  // a warp lays out a chunk at a time: lane 4 t + c
 #pragma unroll 2
-  for (int i0 = tid & ~31; i0 < total; i0 += THREADS) {
-    const int i = i0 + lane, chunk = i >> 4, t = (i >> 2) & 3, c = i & 3;
-    const int k = chunk * W4_CHUNK + w4_k<NGC>(t, c);
+  for (int chunk = tid >> 5; chunk < chunks; chunk += WARPS) {
+    const int k = chunk * W4_CHUNK + L::k(lane >> 2, lane & 3);
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (i < total && k < in) load8(x + k, v);
+    if (k < in) load8(x + k, v);
     float s = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
-    uint4* block = reinterpret_cast<uint4*>(blocks + ((size_t)chunk * n + token) * W4_BLOCK);
-    if (i < total) {
-      const float xo = xs * ODD;
-      block[t * 4 + c] =
-          make_uint4(pack2_f16(v[0] * xs, v[4] * xs), pack2_f16(v[1] * xo, v[5] * xo), pack2_f16(v[2] * xs, v[6] * xs),
-                     pack2_f16(v[3] * xo, v[7] * xo));
-    }
-    constexpr int LANES = 16 / NGC;                // that hold a group
+    uint4* block = reinterpret_cast<uint4*>(blocks + ((size_t)chunk * n + token) * L::BLOCK);
+    block[lane] = make_uint4(pack2_f16(v[0] * xs, v[4] * xs), pack2_f16(v[1] * xo, v[5] * xo), pack2_f16(v[2] * xs, v[6] * xs),
+                             pack2_f16(v[3] * xo, v[7] * xo));
 #pragma unroll
-    for (int o = 1; o < LANES; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (i < total && i % LANES == 0) {
+    for (int o = 1; o < L::LANES; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (lane % L::LANES == 0) {
       const float sm = s * u, a = -8.f * sm;
       const float ah = round_bf16(a), mh = round_bf16(sm), am = round_bf16(a - ah), mm = round_bf16(sm - mh);
-      block[16 + (i % 16) / LANES] = make_uint4(pack2(ah, mh), pack2(am, mm), pack2((a - ah) - am, (sm - mh) - mm), 0u);
+      block[32 + lane / L::LANES] = make_uint4(pack2(ah, mh), pack2(am, mm), pack2((a - ah) - am, (sm - mh) - mm), 0u);
     }
-    if (NGC < 4 && i < total && i % 16 < 4 - NGC) block[16 + NGC + i % 16] = make_uint4(0u, 0u, 0u, 0u);
+    if (lane < L::SUMS - NG) block[32 + NG + lane] = make_uint4(0u, 0u, 0u, 0u);
   }
 }
-template <int NGC>
+template <int NG>
 __global__ void __launch_bounds__(1024)
 w4_prepare_kernel(const bf16* __restrict__ X, int64_t ldx, int in, int n, int norm, float eps, unsigned char* __restrict__ blocks,
                   float* __restrict__ factor) {
   dep_launch();
-  w4_prepare<NGC, 1024>(X + (size_t)blockIdx.x * ldx, blockIdx.x, n, in, norm, eps, blocks, factor);
+  w4_prepare<NG, 1024>(X + (size_t)blockIdx.x * ldx, blockIdx.x, n, in, norm, eps, blocks, factor);
 }
 
-template <int NB, int MT, int NGC, int WK>
+template <int NB, int MT, int NG, int WK>
 struct W4Tile {
   static constexpr int WR = W4_WARPS / WK;
-  static constexpr int STAGES = 3;
-  static constexpr int CSTRIDE = NGC == 1 ? 64 : NGC == 2 ? 96 : 80;      // bytes between rows: a load's lanes lie in distinct banks
-  static constexpr int PARAMS = 16 * MT * CSTRIDE, STAGE = PARAMS + 16 * MT * NGC * 4;
+  static constexpr int STAGES = 2;
+  // A row's 128 bytes of codes lie in pieces of a group, piece p of row r at place p ^ (r % NG), so that the lanes of a fragment's
+  // load (eight rows, one group) lie in distinct banks.
+  static constexpr int PARAMS = 16 * MT * 128, STAGE = PARAMS + 16 * MT * NG * 4;
   static constexpr int RING = W4_WARPS * STAGES * STAGE;
   static constexpr int RED = W4_WARPS * MT * 16 * 4;                      // a token's [wk][wr][mt][row]
 };
@@ -236,34 +238,44 @@ template <int MT, bool TWO> __device__ __forceinline__ int w4_place(int r) {
   return w * MT * 16 + (TWO ? (rw >> 4) * 32 + (rw & 15) : rw);
 }
 
-template <int NB, int MT, int NGC, bool TWO, int WK, bool LOCAL>
+template <int NB, int MT, int NG, bool TWO, int WK, bool LOCAL>
 __global__ void __launch_bounds__(W4_WARPS * 32, NB > 2 ? 1 : 2)
 w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf16* __restrict__ X, int64_t ldx, int norm, float eps,
                const unsigned char* blocks_g, float* factor_g, float* __restrict__ part, W4Out o) {
-  using T = W4Tile<NB, MT, NGC, WK>;
+  using T = W4Tile<NB, MT, NG, WK>;
+  using L = W4Order<NG>;
   constexpr int WR = T::WR, WROWS = TWO ? 8 * MT : 16 * MT, ROWS = WR * WROWS;      // output features of a warp, of a tile
   constexpr int RSTRIDE = WR * MT * 16;
-  constexpr int GT = 4 / NGC;                                 // steps of a group
+  constexpr int GT = L::GT, GB = 128 / NG;                    // words of a lane in a group, bytes of a row's group
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ float sm_factor[8 * NB];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, cc = lane & 3;
   const int wk = warp % WK, wr = warp / WK;
-  const int chunks = (in + W4_CHUNK - 1) / W4_CHUNK, groups = in / (128 / NGC);
+  const int chunks = (in + W4_CHUNK - 1) / W4_CHUNK, groups = in / (W4_CHUNK / NG);
   const size_t row_bytes = in / 2;
   float* red = reinterpret_cast<float*>(smem + T::RING);
   unsigned char* x_local = smem + T::RING + n * T::RED;       // a block of zeros, then LOCAL's blocks
   unsigned char* ring = smem + warp * (T::STAGES * T::STAGE);
   const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
-  const bool whole_chunks = groups % NGC == 0;                // a row's params of a chunk are one aligned copy
   const long u0 = line.begin(blockIdx.x), u1 = line.begin(blockIdx.x + 1);
 
-  // the walk of the copies: tile, chunk, the warp's row pointers in that tile
+  // the walk of the copies: tile, chunk, the lane's pointers in that tile.  Of the codes a lane copies piece lane % 8 of rows
+  // lane / 8, lane / 8 + 4, ... of every 16; of the params those of row `lane` of the warp's 16 MT rows.
+  const int f_row = lane >> 3, f_piece = lane & 7;
+  const bool aligned = groups % (NG < 4 ? NG : 4) == 0;       // rows of params begin on the copies' boundaries
+  uint32_t f_dst[2];                                          // by the parity of the row's number among its four
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int unit = f_piece * 16 / GB, within = f_piece * 16 % GB;
+    f_dst[i] = ring_s + f_row * 128 + (unit ^ ((4 * i + f_row) % NG)) * GB + within;
+  }
   int f_tile = (int)(u0 / line.steps), f_step = (int)(u0 - (long)f_tile * line.steps);
   long f_left = u1 - u0;                                      // steps from here on
   int f_chunk = 0, f_end = 0;
   bool fetching = true;
-  const char* f_codes[MT][2];
-  const uint32_t* f_params = nullptr;                         // lane r: row r of the warp's 16 MT rows
+  const char* f_codes[MT];
+  int f_rows[MT];                                             // how many of the 16 rows there are, less the lane's first
+  const uint32_t* f_params = nullptr;
   uint32_t fetch_at = 0, use_at = 0;
   auto f_open = [&]() {                                       // settles on the next tile in which this warp has a chunk
     while (f_left > 0) {
@@ -278,15 +290,12 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
       const int r0 = tile * ROWS + wr * WROWS;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
-        const bool second = TWO && (mt & 1);
         const int rm = r0 + 16 * (TWO ? mt >> 1 : mt);
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          f_codes[mt][i] = (second ? m2.codes : m1.codes) + min(rm + 8 * i + g, out - 1) * row_bytes + (size_t)f_chunk * 64 + 16 * cc;
+        f_rows[mt] = out - rm - f_row;
+        f_codes[mt] = (TWO && (mt & 1) ? m2.codes : m1.codes) + (size_t)min(rm + f_row, out - 1) * row_bytes + (size_t)f_chunk * 128 + 16 * f_piece;
       }
       const int mt = lane >> 4;
-      const bool second = TWO && (mt & 1);
-      f_params = (second ? m2.params : m1.params) + (size_t)min(r0 + 16 * (TWO ? mt >> 1 : mt) + (lane & 15), out - 1) * groups;
+      f_params = (TWO && (mt & 1) ? m2.params : m1.params) + (size_t)min(r0 + 16 * (TWO ? mt >> 1 : mt) + (lane & 15), out - 1) * groups;
       return;
     }
     fetching = false;
@@ -294,22 +303,25 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
   f_open();
   auto fetch_next = [&]() {
     if (fetching) {
-      const uint32_t dst = ring_s + fetch_at;
-      if (f_chunk * W4_CHUNK + 32 * cc < in) {                // codes behind the end meet x = 0: any bits are finite numbers
+      // rows and features that there are not: their codes stay what they are and meet x = 0 or are not written out
+      if (f_chunk * W4_CHUNK + 32 * f_piece < in) {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) cp_async16(dst + (16 * mt + 8 * i + g) * T::CSTRIDE + 16 * cc, f_codes[mt][i]);
+          for (int i = 0; i < 4; ++i)
+            if (4 * i < f_rows[mt]) cp_async16(f_dst[i & 1] + fetch_at + (16 * mt + 4 * i) * 128, f_codes[mt] + (size_t)(4 * i) * row_bytes);
       }
       if (lane < 16 * MT) {
-        const uint32_t* p = f_params + f_chunk * NGC;
-        const uint32_t pd = dst + T::PARAMS + lane * NGC * 4;
-        if (NGC == 4 && whole_chunks) cp_async16(pd, p);
-        else if (NGC == 2 && whole_chunks) cp_async8(pd, p);
-        else {
+        const uint32_t* p = f_params + f_chunk * NG;
+        const uint32_t pd = ring_s + fetch_at + T::PARAMS + lane * NG * 4;
+        if (aligned && (f_chunk + 1) * NG <= groups) {
+          if (NG == 2) cp_async8(pd, p);
+          else cp_async16(pd, p);
+          if (NG == 8) cp_async16(pd + 16, p + 4);
+        } else {
 #pragma unroll
-          for (int i = 0; i < NGC; ++i) {
-            const bool has = f_chunk * NGC + i < groups;
+          for (int i = 0; i < NG; ++i) {
+            const bool has = f_chunk * NG + i < groups;
             cp_async4(pd + 4 * i, has ? p + i : f_params, has);
           }
         }
@@ -317,9 +329,7 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
       f_chunk += WK;
       if (f_chunk < f_end) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) f_codes[mt][i] += 64 * WK;
+        for (int mt = 0; mt < MT; ++mt) f_codes[mt] += 128 * WK;
       } else {
         f_open();
       }
@@ -329,12 +339,12 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
   };
 #pragma unroll
   for (int i = 0; i < T::STAGES - 1; ++i) fetch_next();
-  if (threadIdx.x < W4_BLOCK / 16) reinterpret_cast<uint4*>(x_local)[threadIdx.x] = make_uint4(0u, 0u, 0u, 0u);
+  if (threadIdx.x < L::BLOCK / 16) reinterpret_cast<uint4*>(x_local)[threadIdx.x] = make_uint4(0u, 0u, 0u, 0u);
   const unsigned char* blocks = blocks_g;
   if (LOCAL) {
     for (int t = 0; t < n; ++t)
-      w4_prepare<NGC, W4_WARPS * 32>(X + (size_t)t * ldx, t, n, in, norm, eps, x_local + W4_BLOCK, sm_factor);
-    blocks = x_local + W4_BLOCK;
+      w4_prepare<NG, W4_WARPS * 32>(X + (size_t)t * ldx, t, n, in, norm, eps, x_local + L::BLOCK, sm_factor);
+    blocks = x_local + L::BLOCK;
     __syncthreads();
     if (blockIdx.x == 0 && threadIdx.x < n) factor_g[threadIdx.x] = sm_factor[threadIdx.x];      // for the join
   } else {
@@ -354,69 +364,54 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[nb][mt][i] = 0.f;
-    // a chunk's x: one chunk ahead of its use where it comes from L1 or L2 and the registers allow.  Lanes of absent tokens read
-    // the block of zeros.
-    constexpr bool AHEAD = !LOCAL && NB == 1;
-    uint4 xf[NB][4], xs[NB], xf2[NB][4], xs2[NB];
+    // lanes of absent tokens read the block of zeros
     const unsigned char* xp[NB];
-    const size_t x_step = (size_t)WK * n * W4_BLOCK;
+    const size_t x_step = (size_t)WK * n * L::BLOCK;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       const int token = 8 * nb + g;
-      xp[nb] = (token < n ? blocks + ((size_t)(step * WK + wk) * n + token) * W4_BLOCK : x_local) + 16 * cc;
+      xp[nb] = (token < n ? blocks + ((size_t)(step * WK + wk) * n + token) * L::BLOCK : x_local) + 16 * cc;
     }
-    auto load_x = [&](uint4 (&f)[NB][4], uint4 (&sm)[NB]) {
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t) f[nb][t] = *reinterpret_cast<const uint4*>(xp[nb] + 64 * t);
-        sm[nb] = *reinterpret_cast<const uint4*>(xp[nb] + 256);
-        if (8 * nb + g < n) xp[nb] += x_step;
-      }
-    };
-    if (AHEAD && step * WK + wk < c1) load_x(xf2, xs2);
     for (int chunk = step * WK + wk; chunk < c1; chunk += WK) {
-      if (AHEAD) {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          xs[nb] = xs2[nb];
-#pragma unroll
-          for (int t = 0; t < 4; ++t) xf[nb][t] = xf2[nb][t];
-        }
-        if (chunk + WK < c1) load_x(xf2, xs2);
-      } else {
-        load_x(xf, xs);
-      }
       fetch_next();
       cp_async_wait<T::STAGES - 1>();
       __syncwarp();
       const unsigned char* st = ring + use_at;
       use_at = use_at + T::STAGE == T::STAGES * T::STAGE ? 0 : use_at + T::STAGE;
-      const unsigned char* row = st + g * T::CSTRIDE + 4 * GT * cc;
-      const unsigned char* prm = st + T::PARAMS + g * NGC * 4;
+      const unsigned char* row = st + g * 128 + 4 * GT * cc;
+      const unsigned char* prm = st + T::PARAMS + g * NG * 4;
       // params words of groups that there are not meet zeros in x's sums (a NaN among them makes the row NaN, as it is)
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        const uint32_t p0 = *reinterpret_cast<const uint32_t*>(prm + 16 * mt * NGC * 4 + 4 * (cc % NGC));
-        const uint32_t p1 = *reinterpret_cast<const uint32_t*>(prm + (16 * mt + 8) * NGC * 4 + 4 * (cc % NGC));
+      for (int p = 0; p < L::SUMS / 4; ++p) {
+        uint4 xs[NB];
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          mma16816(y[nb][mt], p0, p1, p0, p1, xs[nb].x, xs[nb].y);
-          if (o.fp32_out) mma16816(y[nb][mt], p0, p1, 0u, 0u, xs[nb].z, 0u);
+        for (int nb = 0; nb < NB; ++nb) xs[nb] = *reinterpret_cast<const uint4*>(xp[nb] + 512 + 64 * p);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          const uint32_t p0 = *reinterpret_cast<const uint32_t*>(prm + 16 * mt * NG * 4 + 4 * ((4 * p + cc) % NG));
+          const uint32_t p1 = *reinterpret_cast<const uint32_t*>(prm + (16 * mt + 8) * NG * 4 + 4 * ((4 * p + cc) % NG));
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            mma16816(y[nb][mt], p0, p1, p0, p1, xs[nb].x, xs[nb].y);
+            if (o.fp32_out) mma16816(y[nb][mt], p0, p1, 0u, 0u, xs[nb].z, 0u);
+          }
         }
       }
-      uint32_t q[MT][2][NGC];
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
+      for (int gr = 0; gr < NG; ++gr) {
+        uint4 xf[NB][GT];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) load_words<NGC>(prm + (16 * mt + 8 * h) * NGC * 4, q[mt][h]);
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int gr = 0; gr < NGC; ++gr) {
-        uint32_t w[MT][2][GT];
+          for (int tt = 0; tt < GT; ++tt) xf[nb][tt] = *reinterpret_cast<const uint4*>(xp[nb] + 64 * (gr * GT + tt));
+        uint32_t w[MT][2][GT], q[MT][2];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) load_words<GT>(row + (16 * mt + 8 * h) * T::CSTRIDE + (64 / NGC) * gr, w[mt][h]);
+          for (int h = 0; h < 2; ++h) {
+            load_words<GT>(row + (16 * mt + 8 * h) * 128 + (gr ^ (g % NG)) * GB, w[mt][h]);
+            q[mt][h] = *reinterpret_cast<const uint32_t*>(prm + ((16 * mt + 8 * h) * NG + gr) * 4);
+          }
         float acc[NB][MT][4];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
@@ -427,25 +422,24 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
         // the row tiles take turns, so that a product does not wait for the one before it
 #pragma unroll
         for (int tt = 0; tt < GT; ++tt) {
-          const int t = gr * GT + tt;
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt) {
             const uint32_t a0 = code_pair<0>(w[mt][0][tt]), a1 = code_pair<0>(w[mt][1][tt]);
             const uint32_t a2 = code_pair<1>(w[mt][0][tt]), a3 = code_pair<1>(w[mt][1][tt]);
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) mma_f16(acc[nb][mt], a0, a1, a2, a3, xf[nb][t].x, xf[nb][t].y);
+            for (int nb = 0; nb < NB; ++nb) mma_f16(acc[nb][mt], a0, a1, a2, a3, xf[nb][tt].x, xf[nb][tt].y);
           }
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt) {
             const uint32_t a0 = code_pair<2>(w[mt][0][tt]), a1 = code_pair<2>(w[mt][1][tt]);
             const uint32_t a2 = code_pair<3>(w[mt][0][tt]), a3 = code_pair<3>(w[mt][1][tt]);
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) mma_f16(acc[nb][mt], a0, a1, a2, a3, xf[nb][t].z, xf[nb][t].w);
+            for (int nb = 0; nb < NB; ++nb) mma_f16(acc[nb][mt], a0, a1, a2, a3, xf[nb][tt].z, xf[nb][tt].w);
           }
         }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-          const float s0 = lo_bf16(q[mt][0][gr]), s1 = lo_bf16(q[mt][1][gr]);
+          const float s0 = lo_bf16(q[mt][0]), s1 = lo_bf16(q[mt][1]);
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -455,6 +449,9 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
             }
         }
       }
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+        if (8 * nb + g < n) xp[nb] += x_step;
       __syncwarp();                                           // the stage may be filled again
     }
     // ---- the warps' shares meet: red[wk][token][wr][mt][row]
@@ -532,9 +529,9 @@ cudaError_t launch_dep_smem(void (*kernel)(KArgs...), dim3 grid, int threads, si
   return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
 }
 
-template <int NB, int MT, int NGC, bool TWO, int WK, bool LOCAL>
+template <int NB, int MT, int NG, bool TWO, int WK, bool LOCAL>
 spts_status launch_tile(spts_ctx* ctx, const W4GemvArgs& a) {
-  using T = W4Tile<NB, MT, NGC, WK>;
+  using T = W4Tile<NB, MT, NG, WK>;
   const W4Out o{a.residual, a.ldr, a.Y, a.ldy, a.fp32_out};
   const int rows = T::WR * (TWO ? 8 * MT : 16 * MT), chunks = ceil_div(a.in, W4_CHUNK);
   W4Line line;
@@ -543,18 +540,18 @@ spts_status launch_tile(spts_ctx* ctx, const W4GemvArgs& a) {
   const int most = (NB > 2 ? 1 : 2) * (ctx->sm_count < W4_MAX_CTAS / 2 ? ctx->sm_count : W4_MAX_CTAS / 2);
   const long total = (long)line.tiles * line.steps;
   // Whole tiles where there are three for every resident CTA, or between one and two for every SM, or where tiles are too
-  // short for two more launches to pay (16 steps take about 8 us); else equal pieces of the line, whose cut tiles are joined.
-  line.whole = line.tiles >= 3 * most || (line.tiles <= most && (line.tiles >= ctx->sm_count || (LOCAL && line.steps <= 16)));
+  // short for two more launches to pay (8 steps take about 8 us); else equal pieces of the line, whose cut tiles are joined.
+  line.whole = line.tiles >= 3 * most || (line.tiles <= most && (line.tiles >= ctx->sm_count || (LOCAL && line.steps <= 8)));
   line.ctas = line.whole ? (line.tiles < most ? line.tiles : most) : total < most ? (int)total : most;
   const bool cut = !line.whole;
   unsigned char* blocks = (unsigned char*)ctx->ws.w4_x;
-  float* factor = (float*)(blocks + (size_t)chunks * a.n * W4_BLOCK);
+  float* factor = (float*)(blocks + (size_t)chunks * a.n * W4Order<NG>::BLOCK);
   if (!LOCAL) {
-    w4_prepare_kernel<NGC><<<a.n, 1024, 0, ctx->stream>>>((const bf16*)a.X, a.ldx, a.in, a.n, a.norm, ctx->desc.rms_eps, blocks, factor);
+    w4_prepare_kernel<NG><<<a.n, 1024, 0, ctx->stream>>>((const bf16*)a.X, a.ldx, a.in, a.n, a.norm, ctx->desc.rms_eps, blocks, factor);
     SPTS_CUDA_OK(ctx);
   }
-  auto kernel = w4_gemv_kernel<NB, MT, NGC, TWO, WK, LOCAL>;
-  const size_t smem = T::RING + (size_t)a.n * T::RED + W4_BLOCK + (LOCAL ? (size_t)chunks * a.n * W4_BLOCK : 0);
+  auto kernel = w4_gemv_kernel<NB, MT, NG, TWO, WK, LOCAL>;
+  const size_t smem = T::RING + (size_t)a.n * T::RED + W4Order<NG>::BLOCK + (LOCAL ? (size_t)chunks * a.n * W4Order<NG>::BLOCK : 0);
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return SPTS_ERR_CUDA;
   const W4Mat m1{(const char*)a.codes, (const uint32_t*)a.params}, m2{(const char*)a.codes2, (const uint32_t*)a.params2};
   const cudaError_t e = [&]() {
@@ -575,24 +572,24 @@ spts_status launch_tile(spts_ctx* ctx, const W4GemvArgs& a) {
   }
   return SPTS_OK;
 }
-template <int NB, int NGC>
+template <int NB, int NG>
 spts_status launch_rows(spts_ctx* ctx, const W4GemvArgs& a) {
   if constexpr (NB > 1) {
-    if (a.codes2 != nullptr) return launch_tile<NB, 2, NGC, true, 1, false>(ctx, a);
-    return launch_tile<NB, 2, NGC, false, 1, false>(ctx, a);
+    if (a.codes2 != nullptr) return launch_tile<NB, 2, NG, true, 1, false>(ctx, a);
+    return launch_tile<NB, 2, NG, false, 1, false>(ctx, a);
   } else {
     // few elements of x are laid out in the kernel itself; few rows: all eight warps on one tile of 16
     const bool local = (long)a.n * align_up((size_t)a.in, W4_CHUNK) <= W4_LOCAL;
-    if (a.codes2 != nullptr) return local ? launch_tile<1, 2, NGC, true, W4_WK, true>(ctx, a) : launch_tile<1, 2, NGC, true, W4_WK, false>(ctx, a);
+    if (a.codes2 != nullptr) return local ? launch_tile<1, 2, NG, true, W4_WK, true>(ctx, a) : launch_tile<1, 2, NG, true, W4_WK, false>(ctx, a);
     if (ceil_div(a.out, 16) <= 2 * ctx->sm_count)
-      return local ? launch_tile<1, 1, NGC, false, 8, true>(ctx, a) : launch_tile<1, 1, NGC, false, 8, false>(ctx, a);
-    return local ? launch_tile<1, 2, NGC, false, W4_WK, true>(ctx, a) : launch_tile<1, 2, NGC, false, W4_WK, false>(ctx, a);
+      return local ? launch_tile<1, 1, NG, false, 8, true>(ctx, a) : launch_tile<1, 1, NG, false, 8, false>(ctx, a);
+    return local ? launch_tile<1, 2, NG, false, W4_WK, true>(ctx, a) : launch_tile<1, 2, NG, false, W4_WK, false>(ctx, a);
   }
 }
 template <int NB>
 spts_status launch_group(spts_ctx* ctx, const W4GemvArgs& a) {
-  if (a.group == 128) return launch_rows<NB, 1>(ctx, a);
-  return a.group == 64 ? launch_rows<NB, 2>(ctx, a) : launch_rows<NB, 4>(ctx, a);
+  if (a.group == 128) return launch_rows<NB, 2>(ctx, a);
+  return a.group == 64 ? launch_rows<NB, 4>(ctx, a) : launch_rows<NB, 8>(ctx, a);
 }
 
 }  // namespace
