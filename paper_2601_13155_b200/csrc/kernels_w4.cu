@@ -150,18 +150,20 @@ template <int NG> struct W4Order {
   __host__ __device__ static constexpr int k(int t, int c) { return (t / GT) * (W4_CHUNK / NG) + c * (W4_CHUNK / NG / 4) + 8 * (t % GT); }
 };
 
-// x [n, in] -> blocks [chunk][n] of W4Order::BLOCK bytes: fragments [t][c] (16 bytes: four fp16 pairs), then sums [group] (three
-// pairs of pieces; zero where there is no such group); factor [n].  One token, by a CTA of THREADS.
+// x [n, in] -> per chunk and token fragments [t][c] (16 bytes: four fp16 pairs), then sums [group] (three pairs of pieces; zero
+// where there is no such group), in rows of 64 bytes `row` apart, tokens `next` and chunks `stride` apart; factor [n].  One token
+// (with x null: zeros), by a CTA of THREADS.
 template <int NG, int THREADS>
-__device__ __forceinline__ void w4_prepare(const bf16* __restrict__ x, int token, int n, int in, int norm, float eps,
-                                           unsigned char* blocks, float* factor) {
+__device__ __forceinline__ void w4_prepare(const bf16* __restrict__ x, int token, int in, int norm, float eps, unsigned char* blocks,
+                                           int row, int next, size_t stride, float* factor) {
   using L = W4Order<NG>;
   constexpr int WARPS = THREADS / 32;
   __shared__ float red[2][WARPS];
   const int tid = threadIdx.x, lane = tid & 31;
   float top = 0.f, ss = 0.f;
+  const int there = x != nullptr ? in : 0;
 #pragma unroll 4
-  for (int k = 8 * tid; k < in; k += 8 * THREADS) {
+  for (int k = 8 * tid; k < there; k += 8 * THREADS) {
     float v[8];
     load8(x + k, v);
 #pragma unroll
@@ -183,27 +185,32 @@ __device__ __forceinline__ void w4_prepare(const bf16* __restrict__ x, int token
   for (int chunk = tid >> 5; chunk < chunks; chunk += WARPS) {
     const int k = chunk * W4_CHUNK + L::k(lane >> 2, lane & 3);
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (k < in) load8(x + k, v);
+    if (k < there) load8(x + k, v);
     float s = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
-    uint4* block = reinterpret_cast<uint4*>(blocks + ((size_t)chunk * n + token) * L::BLOCK);
-    block[lane] = make_uint4(pack2_f16(v[0] * xs, v[4] * xs), pack2_f16(v[1] * xo, v[5] * xo), pack2_f16(v[2] * xs, v[6] * xs),
+    unsigned char* block = blocks + chunk * stride + (size_t)token * next;
+    const auto at = [&](int i) { return reinterpret_cast<uint4*>(block + (size_t)(i >> 2) * row + 16 * (i & 3)); };
+    *at(lane) = make_uint4(pack2_f16(v[0] * xs, v[4] * xs), pack2_f16(v[1] * xo, v[5] * xo), pack2_f16(v[2] * xs, v[6] * xs),
                              pack2_f16(v[3] * xo, v[7] * xo));
 #pragma unroll
     for (int o = 1; o < L::LANES; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     if (lane % L::LANES == 0) {
       const float sm = s * u, a = -8.f * sm;
       const float ah = round_bf16(a), mh = round_bf16(sm), am = round_bf16(a - ah), mm = round_bf16(sm - mh);
-      block[32 + lane / L::LANES] = make_uint4(pack2(ah, mh), pack2(am, mm), pack2((a - ah) - am, (sm - mh) - mm), 0u);
+      *at(32 + lane / L::LANES) = make_uint4(pack2(ah, mh), pack2(am, mm), pack2((a - ah) - am, (sm - mh) - mm), 0u);
     }
-    if (lane < L::SUMS - NG) block[32 + NG + lane] = make_uint4(0u, 0u, 0u, 0u);
+    if (lane < L::SUMS - NG) *at(32 + NG + lane) = make_uint4(0u, 0u, 0u, 0u);
   }
 }
 template <int NG>
 __global__ void __launch_bounds__(1024)
 w4_prepare_kernel(const bf16* __restrict__ X, int64_t ldx, int in, int n, int norm, float eps, unsigned char* __restrict__ blocks,
                   float* __restrict__ factor) {
+  // a CTA per token, those up to the next multiple of eight too (zeros): tokens lie side by side in each row of fragments, which
+  // a load of eight tokens then reads as whole lines
   dep_launch();
-  w4_prepare<NG, 1024>(X + (size_t)blockIdx.x * ldx, blockIdx.x, n, in, norm, eps, blocks, factor);
+  const int token = blockIdx.x, tokens = gridDim.x;
+  w4_prepare<NG, 1024>(token < n ? X + (size_t)token * ldx : nullptr, token, in, norm, eps, blocks, 64 * tokens, 64,
+                       (size_t)W4Order<NG>::BLOCK * tokens, factor);
 }
 
 template <int NB, int MT, int NG, int WK>
@@ -339,11 +346,11 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
   };
 #pragma unroll
   for (int i = 0; i < T::STAGES - 1; ++i) fetch_next();
-  if (threadIdx.x < L::BLOCK / 16) reinterpret_cast<uint4*>(x_local)[threadIdx.x] = make_uint4(0u, 0u, 0u, 0u);
+  if (LOCAL && threadIdx.x < L::BLOCK / 16) reinterpret_cast<uint4*>(x_local)[threadIdx.x] = make_uint4(0u, 0u, 0u, 0u);
   const unsigned char* blocks = blocks_g;
   if (LOCAL) {
     for (int t = 0; t < n; ++t)
-      w4_prepare<NG, W4_WARPS * 32>(X + (size_t)t * ldx, t, n, in, norm, eps, x_local + L::BLOCK, sm_factor);
+      w4_prepare<NG, W4_WARPS * 32>(X + (size_t)t * ldx, t, in, norm, eps, x_local + L::BLOCK, 64, L::BLOCK, (size_t)n * L::BLOCK, sm_factor);
     blocks = x_local + L::BLOCK;
     __syncthreads();
     if (blockIdx.x == 0 && threadIdx.x < n) factor_g[threadIdx.x] = sm_factor[threadIdx.x];      // for the join
@@ -364,14 +371,12 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[nb][mt][i] = 0.f;
-    // lanes of absent tokens read the block of zeros
-    const unsigned char* xp[NB];
-    const size_t x_step = (size_t)WK * n * L::BLOCK;
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      const int token = 8 * nb + g;
-      xp[nb] = (token < n ? blocks + ((size_t)(step * WK + wk) * n + token) * L::BLOCK : x_local) + 16 * cc;
-    }
+    // absent tokens are zeros: LOCAL's lanes read its block of them
+    constexpr int XROW = LOCAL ? 64 : 64 * 8 * NB;
+    const unsigned char* xp;
+    const size_t x_stride = (size_t)(LOCAL ? n : 8 * NB) * L::BLOCK, x_step = LOCAL && g >= n ? 0 : WK * x_stride;
+    if (LOCAL) xp = (g < n ? blocks + (step * WK + wk) * x_stride + g * L::BLOCK : x_local) + 16 * cc;
+    else xp = blocks + (step * WK + wk) * x_stride + g * 64 + 16 * cc;
     for (int chunk = step * WK + wk; chunk < c1; chunk += WK) {
       fetch_next();
       cp_async_wait<T::STAGES - 1>();
@@ -385,7 +390,7 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
       for (int p = 0; p < L::SUMS / 4; ++p) {
         uint4 xs[NB];
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) xs[nb] = *reinterpret_cast<const uint4*>(xp[nb] + 512 + 64 * p);
+        for (int nb = 0; nb < NB; ++nb) xs[nb] = *reinterpret_cast<const uint4*>(xp + (8 + p) * XROW + 512 * nb);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
           const uint32_t p0 = *reinterpret_cast<const uint32_t*>(prm + 16 * mt * NG * 4 + 4 * ((4 * p + cc) % NG));
@@ -403,7 +408,7 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int tt = 0; tt < GT; ++tt) xf[nb][tt] = *reinterpret_cast<const uint4*>(xp[nb] + 64 * (gr * GT + tt));
+          for (int tt = 0; tt < GT; ++tt) xf[nb][tt] = *reinterpret_cast<const uint4*>(xp + (gr * GT + tt) * XROW + 512 * nb);
         uint32_t w[MT][2][GT], q[MT][2];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
@@ -449,9 +454,7 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
             }
         }
       }
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-        if (8 * nb + g < n) xp[nb] += x_step;
+      xp += x_step;
       __syncwarp();                                           // the stage may be filled again
     }
     // ---- the warps' shares meet: red[wk][token][wr][mt][row]
@@ -545,13 +548,13 @@ spts_status launch_tile(spts_ctx* ctx, const W4GemvArgs& a) {
   line.ctas = line.whole ? (line.tiles < most ? line.tiles : most) : total < most ? (int)total : most;
   const bool cut = !line.whole;
   unsigned char* blocks = (unsigned char*)ctx->ws.w4_x;
-  float* factor = (float*)(blocks + (size_t)chunks * a.n * W4Order<NG>::BLOCK);
+  float* factor = (float*)(blocks + (size_t)chunks * 8 * NB * W4Order<NG>::BLOCK);
   if (!LOCAL) {
-    w4_prepare_kernel<NG><<<a.n, 1024, 0, ctx->stream>>>((const bf16*)a.X, a.ldx, a.in, a.n, a.norm, ctx->desc.rms_eps, blocks, factor);
+    w4_prepare_kernel<NG><<<8 * NB, 1024, 0, ctx->stream>>>((const bf16*)a.X, a.ldx, a.in, a.n, a.norm, ctx->desc.rms_eps, blocks, factor);
     SPTS_CUDA_OK(ctx);
   }
   auto kernel = w4_gemv_kernel<NB, MT, NG, TWO, WK, LOCAL>;
-  const size_t smem = T::RING + (size_t)a.n * T::RED + W4Order<NG>::BLOCK + (LOCAL ? (size_t)chunks * a.n * W4Order<NG>::BLOCK : 0);
+  const size_t smem = T::RING + (size_t)a.n * T::RED + (LOCAL ? ((size_t)chunks * a.n + 1) * W4Order<NG>::BLOCK : 0);
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return SPTS_ERR_CUDA;
   const W4Mat m1{(const char*)a.codes, (const uint32_t*)a.params}, m2{(const char*)a.codes2, (const uint32_t*)a.params2};
   const cudaError_t e = [&]() {
