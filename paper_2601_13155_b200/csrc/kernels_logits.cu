@@ -1,41 +1,40 @@
 // Rules on the logits of a generation (penalties for tokens of the history, biases, grammar mask) and the greedy token,
 // in one launch.
 //
-// A cluster of CTAs owns a row; every CTA owns a slice of the vocabulary and holds, in shared memory, whether and how
-// often each token of its slice occurred and which bias entry counts for it.  Every CTA reads the row's whole history and
-// notes what falls into its slice: that is 16 reads of it from L2, but the alternative (each CTA reads a share and notes it
-// in the owner's distributed shared memory) pays for every repeated token with a remote access to one address, and text
-// repeats (one row of 128256 with a history of 33024: 18 us).  Then every CTA passes over its slice of the logits once, and
-// the slices' best tokens meet in CTA 0.
-// Bound by memory at many rows (logits in and out), by the chain launch - tables - history - logits - argmax at one; so
-// the logits are loaded eight to a thread at a time (one at a time took 31 dependent trips to memory per thread: 31 us for
-// one row of 128256), and the first eight before the tables are even cleared.
-#include <cooperative_groups.h>
-
+// A CTA owns a slice of a row's vocabulary and holds, in shared memory, a word per token of it: whether and how often the token
+// occurred in the row's history, and whether a bias entry names it.  It reads the row's whole history and notes what falls into
+// its slice: that is one read of it per slice from L2, but the alternative (each CTA reads a share and notes it in the owner's
+// distributed shared memory) pays for every repeated token with a remote access to one address, and text repeats.  Then the
+// slice's logits pass through once, four neighbouring tokens to a thread, with only the mask to apply; marked tokens are left
+// out of the maximum and listed, and the listed ones, densely, go through the rules (applied in the pass itself they cost every
+// warp the rules' instructions for its one marked token: 66 us for 64 rows of 152063).
+// The slices' best tokens meet in a 64-bit maximum per row, from which the slice that arrives last takes the token.
+//
+// Bound by memory at many rows (logits in and out), by the chain launch - tables - history - logits - maximum at one row.
 #include "spts_common.cuh"
-
-namespace cg = cooperative_groups;
 
 namespace spts {
 
 namespace {
 
-constexpr int LG_THREADS = 512;
-constexpr int LG_BATCH = 8;             // logits of a thread in flight
-constexpr int LG_HISTORY = 4;           // 16-byte pieces of the history of a thread in flight
-constexpr int LG_BYTES = 6;             // shared memory per token of the slice: its word, and 2 for a bias entry
+constexpr int LG_BATCH = 4;             // groups of four logits of a thread in flight
+constexpr int LG_HISTORY = 2;           // 16-byte pieces of the history of a thread in flight
+constexpr int LG_BYTES = 8;             // shared memory per token of the slice: its word, 2 on the list, 2 for a bias entry
 // tokens of a CTA's slice that are worked on at a time
-constexpr int LG_WINDOW = 36864;
+constexpr int LG_WINDOW = 27648;
 
 struct LogitsArgs {
   const float* x; int64_t ld; int n, vocab;
   spts_logits_rules r;
   float* out; int64_t ldo;
   int32_t* token;
+  unsigned long long* key; int* arrived;       // per row; zero between calls
 };
 
-__device__ __forceinline__ void take(float& best, int& besti, float v, int i) {
-  if (v > best || (v == best && i < besti)) { best = v; besti = i; }
+// Larger value, then lower index, is the larger key; values are not NaN.
+__device__ __forceinline__ unsigned long long key_of(float v, int i) {
+  const uint32_t u = __float_as_uint(v == 0.f ? 0.f : v);
+  return ((unsigned long long)((u & 0x80000000u) ? ~u : (u | 0x80000000u)) << 32) | (uint32_t)(0x7FFFFFFF - i);
 }
 
 // the largest entry number wins
@@ -57,19 +56,16 @@ __device__ __forceinline__ void range(const int32_t* start, int b, int n_all, in
 constexpr uint32_t OCCURRED = 0x80000000u, BIASED = 0x40000000u, TIMES = 0x3FFFFFFFu;       // of a token's word
 
 // E: an entry number of the row's bias list, 16 bits where the list is short enough
-template <typename E>
-__global__ void __launch_bounds__(LG_THREADS) logits_kernel(LogitsArgs a, int per, int window) {
+template <typename E, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) logits_kernel(LogitsArgs a, int slices, int per, int window) {
   extern __shared__ __align__(16) unsigned char smem[];
-  // [window] words: occurred, biased, times generated; [window] last bias entry + 1 (windows are multiples of 32)
+  // [window] words, [window] last bias entry + 1, [window] listed tokens (windows are multiples of 32)
   uint32_t* word = reinterpret_cast<uint32_t*>(smem);
   E* entry = reinterpret_cast<E*>(word + window);
-  __shared__ float bv[32];
-  __shared__ int bi[32];
-  __shared__ float top_v;
-  __shared__ int top_i;
-  cg::cluster_group cl = cg::this_cluster();
-  const int rank = (int)cl.block_rank(), nct = (int)cl.num_blocks();
-  const int b = blockIdx.x / nct, tid = threadIdx.x;
+  uint16_t* list = reinterpret_cast<uint16_t*>(entry + window);
+  __shared__ unsigned long long keys[THREADS / 32];
+  __shared__ int listed;
+  const int b = blockIdx.x / slices, slice = blockIdx.x - b * slices, tid = threadIdx.x;
   const bool hist = a.r.history != nullptr, bias = a.r.bias_token != nullptr, tables = hist || bias;
   const float* x = a.x + (size_t)b * a.ld;
   float* out = a.out != nullptr ? a.out + (size_t)b * a.ldo : nullptr;
@@ -77,150 +73,224 @@ __global__ void __launch_bounds__(LG_THREADS) logits_kernel(LogitsArgs a, int pe
   const float rep = a.r.repetition != nullptr ? a.r.repetition[b] : 1.f;
   const float pre = a.r.presence != nullptr ? a.r.presence[b] : 0.f;
   const float fre = a.r.frequency != nullptr ? a.r.frequency[b] : 0.f;
-  float best = -INFINITY;
-  int besti = 0x7FFFFFFF;
+  // token `base` (up to three before the row) lies on a 16-byte boundary, and so do all slices
+  const int base = -(int)((reinterpret_cast<uintptr_t>(x) >> 2) & 3);
+  const bool out4 = out != nullptr && ((reinterpret_cast<uintptr_t>(out + base) & 15) == 0);
+  // the row's part of the lists: history [i0, i1), generated from g0 on, [p0, p1) of the prompt's part whole 16-byte pieces
+  int i0 = 0, i1 = 0, g0 = 0, p0 = 0, p1 = 0, b0 = 0, b1 = 0;
+  if (hist) {
+    range(a.r.history_start, b, a.r.n_history, i0, i1);
+    i1 = max(i0, i1);
+    g0 = a.r.generated_start != nullptr ? min(max(a.r.generated_start[b], i0), i1) : i0;
+    const bool by4 = (reinterpret_cast<uintptr_t>(a.r.history) & 15) == 0;
+    p0 = by4 ? min((i0 + 3) & ~3, g0) : g0;
+    p1 = by4 ? max(p0, g0 & ~3) : g0;
+    if (p0 & 3) p1 = p0;                          // (no whole piece)
+  }
+  if (bias) range(a.r.bias_start, b, a.r.n_bias, b0, b1);
+  unsigned long long best = 0;                    // (below every key)
   for (int w0 = 0; w0 < per; w0 += window) {
-    const int wn = min(window, per - w0);
-    const int v0 = rank * per + w0, v1 = min(a.vocab, v0 + wn);
-    const uint32_t span = (uint32_t)max(0, v1 - v0);
-    float l[LG_BATCH];
-    uint32_t mw[LG_BATCH];
-    // logits v, v + LG_THREADS, ...; v0 and the steps are multiples of 32, so a thread's bit in a mask word is its lane's
-    auto load = [&](int v) {
+    const int wn = min(window, per - w0), v0 = base + slice * per + w0;           // tokens [v0, v0 + wn), as far as there are such
+    // groups of four tokens [j0, j1) lie in the row; up to three tokens before and behind them are taken one by one
+    const int v1 = min(a.vocab, v0 + wn), j0 = v0 < 0 ? 1 : 0, j1 = v1 > v0 ? (v1 - v0) >> 2 : 0;
+    const float4* x4 = reinterpret_cast<const float4*>(x + v0);
+    float4 l[LG_BATCH];
+    uint32_t m0[LG_BATCH], m1[LG_BATCH];
+    auto load = [&](int j) {
 #pragma unroll
-      for (int k = 0; k < LG_BATCH; ++k) {
-        const int i = v + k * LG_THREADS;
-        l[k] = i < v1 ? __ldcs(x + i) : 0.f;
-        mw[k] = i < v1 && mask != nullptr ? __ldg(mask + (i >> 5)) : 0xFFFFFFFFu;
+      for (int k = 0; k < LG_BATCH; ++k, j += THREADS) {
+        l[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        m0[k] = m1[k] = 0xFFFFFFFFu;
+        if (j < j1) {
+          l[k] = x4[j];
+          if (mask != nullptr) { m0[k] = __ldg(mask + ((v0 + 4 * j) >> 5)); m1[k] = __ldg(mask + ((v0 + 4 * j + 3) >> 5)); }
+        }
       }
     };
-    load(v0 + tid);
-    int b0 = 0, b1 = 0;
-    if (bias) range(a.r.bias_start, b, a.r.n_bias, b0, b1);
+    load(j0 + tid);
+    // the first pieces of the lists are on their way before the tables are cleared
+    const int4* h4 = reinterpret_cast<const int4*>(a.r.history);
+    int4 first[LG_HISTORY];
+    int first_bias = -1, first_made = -1;
+#pragma unroll
+    for (int k = 0; k < LG_HISTORY; ++k) first[k] = p0 / 4 + tid + k * THREADS < p1 / 4 ? __ldg(h4 + p0 / 4 + tid + k * THREADS) : make_int4(-1, -1, -1, -1);
+    if (g0 + tid < i1) first_made = __ldg(a.r.history + g0 + tid);
+    if (b0 + tid < b1) first_bias = __ldg(a.r.bias_token + b0 + tid);
     if (tables) {
+      const uint32_t span = (uint32_t)wn;
       const int n16 = window * (4 + (int)sizeof(E)) / 16;             // a multiple of 32 tokens: whole 16-byte words
-      for (int i = tid; i < n16; i += LG_THREADS) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0u, 0u, 0u, 0u);
-      int i0 = 0, i1 = 0, g0 = 0;
-      if (hist) {
-        range(a.r.history_start, b, a.r.n_history, i0, i1);
-        g0 = a.r.generated_start != nullptr ? min(max(a.r.generated_start[b], i0), i1) : i0;
-      }
+      for (int i = tid; i < n16; i += THREADS) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (tid == 0) listed = 0;
       __syncthreads();
+      // a token's place in the slice; tokens that there are not have none
+      const auto place = [&](int t) { return t < 0 || t >= a.vocab ? 0xFFFFFFFFu : (uint32_t)(t - v0); };
+      const auto mark = [&](int t) {
+        const uint32_t o = place(t);
+        if (o < span) word[o] = OCCURRED;
+      };
       if (hist) {
         // whole 16-byte pieces of the prompt's part, then the ends and the generated part one by one
-        const bool by4 = (reinterpret_cast<uintptr_t>(a.r.history) & 15) == 0;
-        const int p0 = by4 ? min((i0 + 3) & ~3, g0) : g0, p1 = by4 ? max(p0, g0 & ~3) : g0;
-        const int4* h4 = reinterpret_cast<const int4*>(a.r.history);
-        for (int j = p0 / 4 + tid; j < p1 / 4; j += LG_HISTORY * LG_THREADS) {
+        for (int j = p0 / 4 + tid; j < p1 / 4; j += LG_HISTORY * THREADS) {
           int4 t[LG_HISTORY];
 #pragma unroll
-          for (int k = 0; k < LG_HISTORY; ++k) t[k] = j + k * LG_THREADS < p1 / 4 ? __ldg(h4 + j + k * LG_THREADS) : make_int4(-1, -1, -1, -1);
+          for (int k = 0; k < LG_HISTORY; ++k)
+            t[k] = j == p0 / 4 + tid ? first[k] : j + k * THREADS < p1 / 4 ? __ldg(h4 + j + k * THREADS) : make_int4(-1, -1, -1, -1);
 #pragma unroll
           for (int k = 0; k < LG_HISTORY; ++k) {
-            const uint32_t o0 = t[k].x - v0, o1 = t[k].y - v0, o2 = t[k].z - v0, o3 = t[k].w - v0;
-            if (o0 < span) word[o0] = OCCURRED;
-            if (o1 < span) word[o1] = OCCURRED;
-            if (o2 < span) word[o2] = OCCURRED;
-            if (o3 < span) word[o3] = OCCURRED;
+            mark(t[k].x); mark(t[k].y); mark(t[k].z); mark(t[k].w);
           }
         }
-        for (int i = i0 + tid; i < p0; i += LG_THREADS) {
-          const uint32_t o = __ldg(a.r.history + i) - v0;
-          if (o < span) word[o] = OCCURRED;
-        }
-        for (int i = p1 + tid; i < g0; i += LG_THREADS) {
-          const uint32_t o = __ldg(a.r.history + i) - v0;
-          if (o < span) word[o] = OCCURRED;
-        }
+        for (int i = i0 + tid; i < p0; i += THREADS) mark(__ldg(a.r.history + i));
+        for (int i = p1 + tid; i < g0; i += THREADS) mark(__ldg(a.r.history + i));
         __syncthreads();                          // the marks above are plain stores; from here on words change by atomics
-        for (int i = g0 + tid; i < i1; i += LG_THREADS) {
-          const uint32_t o = __ldg(a.r.history + i) - v0;
+        for (int i = g0 + tid; i < i1; i += THREADS) {
+          const uint32_t o = place(i == g0 + tid ? first_made : __ldg(a.r.history + i));
           if (o < span) { atomicOr(word + o, OCCURRED); atomicAdd(word + o, 1u); }
         }
       }
-      if (bias) {
-        for (int i = b0 + tid; i < b1; i += LG_THREADS) {
-          const uint32_t o = __ldg(a.r.bias_token + i) - v0;
-          if (o < span) { atomicOr(word + o, BIASED); last_entry(entry + o, i - b0 + 1); }
-        }
+      for (int i = b0 + tid; i < b1; i += THREADS) {
+        const uint32_t o = place(i == b0 + tid ? first_bias : __ldg(a.r.bias_token + i));
+        if (o < span) { atomicOr(word + o, BIASED); last_entry(entry + o, i - b0 + 1); }
       }
       __syncthreads();
     }
-    const uint32_t bit = 1u << (tid & 31);
-    for (int v = v0 + tid; v < v1; v += LG_BATCH * LG_THREADS) {
-      if (v != v0 + tid) load(v);
-      uint32_t tw[LG_BATCH];
-#pragma unroll
-      for (int k = 0; k < LG_BATCH; ++k) tw[k] = tables && v + k * LG_THREADS < v1 ? word[v - v0 + k * LG_THREADS] : 0u;
+    // ---- the slice's logits, as they are or masked; marked tokens stay out of the maximum and are listed
+    float top = -INFINITY;
+    int topi = 0;
+    const int lane = tid & 31;
+    for (int jb = j0 + tid; jb - lane < j1; jb += LG_BATCH * THREADS) {
+      if (jb != j0 + tid) load(jb);
 #pragma unroll
       for (int k = 0; k < LG_BATCH; ++k) {
-        const int i = v + k * LG_THREADS;
-        float y = l[k];
-        if (tw[k] != 0u) {
-          if (tw[k] & OCCURRED) {
-            y = y > 0.f ? __fdiv_rn(y, rep) : __fmul_rn(y, rep);
-            const uint32_t c = tw[k] & TIMES;
-            if (c > 0) y = __fsub_rn(__fsub_rn(y, __fmul_rn(fre, (float)c)), pre);
-          }
-          if (tw[k] & BIASED) y = __fadd_rn(y, a.r.bias_value[b0 + (int)entry[i - v0] - 1]);
+        const int j = jb + k * THREADS, v = v0 + 4 * j;
+        if (j - lane >= j1) break;                 // the whole warp
+        const bool in = j < j1;
+        const uint32_t allowed = __funnelshift_r(m0[k], m1[k], v & 31);
+        float y[4] = {l[k].x, l[k].y, l[k].z, l[k].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!in || !((allowed >> i) & 1u)) y[i] = -INFINITY;
+        if (in) {
+          if (out4) *reinterpret_cast<float4*>(out + v) = make_float4(y[0], y[1], y[2], y[3]);
+          else if (out != nullptr) { out[v] = y[0]; out[v + 1] = y[1]; out[v + 2] = y[2]; out[v + 3] = y[3]; }
         }
-        if (!(mw[k] & bit)) y = -INFINITY;
-        if (i < v1) {
-          if (out != nullptr) out[i] = y;
-          if (y > best || besti == 0x7FFFFFFF) { if (y == y) { best = y; besti = i; } }        // a thread's indices ascend
+        if (tables) {
+          const uint4 w = in ? reinterpret_cast<const uint4*>(word)[j] : make_uint4(0u, 0u, 0u, 0u);
+          if (__any_sync(0xffffffffu, (w.x | w.y | w.z | w.w) != 0u)) {
+            const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+            uint32_t vote[4];
+            int many = 0, before = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              vote[i] = __ballot_sync(0xffffffffu, ww[i] != 0u);
+              many += __popc(vote[i]);
+            }
+            int at = lane == 0 ? atomicAdd(&listed, many) : 0;
+            at = __shfl_sync(0xffffffffu, at, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if (ww[i]) {
+                list[at + before + __popc(vote[i] & ((1u << lane) - 1u))] = (uint16_t)(4 * j + i);
+                y[i] = -INFINITY;
+              }
+              before += __popc(vote[i]);
+            }
+          }
+        }
+        const float m = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));          // (passes over NaN)
+        if (m > top) {                             // a thread's tokens ascend: the first of equals stays
+          top = m;
+          topi = v + (y[0] == m ? 0 : y[1] == m ? 1 : y[2] == m ? 2 : 3);
         }
       }
     }
-    if (w0 + window < per) __syncthreads();       // the tables are emptied again
+    if (tid < 8) {                                 // the ends: tokens before the first group, then those behind the last
+      const int v = tid < 4 ? v0 + tid : v0 + 4 * max(j0, j1) + tid - 4;
+      if (v >= 0 && v < v1 && (tid >= 4 || j0 == 1)) {
+        float y = x[v];
+        if (mask != nullptr && !((__ldg(mask + (v >> 5)) >> (v & 31)) & 1u)) y = -INFINITY;
+        if (out != nullptr) out[v] = y;
+        if (tables && word[v - v0] != 0u) list[atomicAdd(&listed, 1)] = (uint16_t)(v - v0);
+        else if (y > -INFINITY) best = max(best, key_of(y, v));
+      }
+    }
+    if (top > -INFINITY) best = max(best, key_of(top, topi));
+    // ---- the listed tokens
+    if (tables) {
+      __syncthreads();                            // what was written above is written again
+      const int many = listed;
+      for (int i = tid; i < many; i += THREADS) {
+        const int o = list[i], v = v0 + o;
+        const uint32_t w = word[o];
+        float y = x[v];                            // (in place: the logit itself, or -inf where the mask forbids the token anyway)
+        if (w & OCCURRED) {
+          y = y > 0.f ? __fdiv_rn(y, rep) : __fmul_rn(y, rep);
+          const uint32_t c = w & TIMES;
+          if (c > 0) y = __fsub_rn(__fsub_rn(y, __fmul_rn(fre, (float)c)), pre);
+        }
+        if (w & BIASED) y = __fadd_rn(y, a.r.bias_value[b0 + (int)entry[o] - 1]);
+        if (mask != nullptr && !((__ldg(mask + (v >> 5)) >> (v & 31)) & 1u)) y = -INFINITY;
+        if (out != nullptr) out[v] = y;
+        if (y > -INFINITY) best = max(best, key_of(y, v));
+      }
+      if (w0 + window < per) __syncthreads();     // the tables are emptied again
+    }
   }
   if (a.token == nullptr) return;
-  for (int o = 16; o > 0; o >>= 1) take(best, besti, __shfl_xor_sync(0xffffffffu, best, o), __shfl_xor_sync(0xffffffffu, besti, o));
-  if ((tid & 31) == 0) { bv[tid >> 5] = best; bi[tid >> 5] = besti; }
+  for (int o = 16; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
+  if ((tid & 31) == 0) keys[tid >> 5] = best;
   __syncthreads();
   if (tid < 32) {
-    best = tid < LG_THREADS / 32 ? bv[tid] : -INFINITY;
-    besti = tid < LG_THREADS / 32 ? bi[tid] : 0x7FFFFFFF;
-    for (int o = 16; o > 0; o >>= 1) take(best, besti, __shfl_xor_sync(0xffffffffu, best, o), __shfl_xor_sync(0xffffffffu, besti, o));
-    if (tid == 0) { top_v = best; top_i = besti; }
+    best = tid < THREADS / 32 ? keys[tid] : 0;
+    for (int o = 16; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
+    if (tid == 0) {
+      atomicMax(a.key + b, best);
+      __threadfence();
+      if (atomicAdd(a.arrived + b, 1) == slices - 1) {
+        const unsigned long long k = atomicExch(a.key + b, 0ull);            // ready for the next call
+        a.arrived[b] = 0;
+        a.token[b] = k == 0 ? -1 : 0x7FFFFFFF - (int)(uint32_t)k;
+      }
+    }
   }
-  cl.sync();
-  if (rank == 0 && tid == 0) {
-    for (int r = 0; r < nct; ++r) take(best, besti, *cl.map_shared_rank(&top_v, r), *cl.map_shared_rank(&top_i, r));
-    a.token[b] = best == -INFINITY ? -1 : besti;
-  }
-  cl.sync();                                      // CTA 0 has read the others' shared memory
 }
 
 }  // namespace
 
 spts_status launch_process_logits(spts_ctx* ctx, const float* logits, int64_t ld, int n, int vocab,
                                   const spts_logits_rules& rules, float* out, int64_t ldo, int32_t* token) {
-  const LogitsArgs a{logits, ld, n, vocab, rules, out, ldo, token};
   const bool tables = rules.history != nullptr || rules.bias_token != nullptr;
-  // sixteen CTAs to a row where each still has several logits per thread, else eight (the portable size)
-  const int cluster = vocab > 16 * LG_THREADS * 2 ? 16 : 8;
   const bool wide = rules.n_bias > 65534;                        // a row's entries may not fit 16 bits
-  const int per = (int)align_up((size_t)ceil_div(vocab, cluster), 32);
-  const int most = wide ? LG_WINDOW * LG_BYTES / (LG_BYTES + 2) / 32 * 32 : LG_WINDOW;
-  const int window = !tables || per < most ? per : most;
-  void (*kernel)(LogitsArgs, int, int) = wide ? logits_kernel<uint32_t> : logits_kernel<uint16_t>;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(cluster * n);
-  cfg.blockDim = dim3(LG_THREADS);
-  cfg.dynamicSmemBytes = tables ? (size_t)window * (wide ? LG_BYTES + 2 : LG_BYTES) : 0;
-  cfg.stream = ctx->stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = cluster;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LG_WINDOW * LG_BYTES) != cudaSuccess ||
-      cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
-    return SPTS_ERR_CUDA;
-  if (cudaLaunchKernelEx(&cfg, kernel, a, per, window) != cudaSuccess) return SPTS_ERR_CUDA;
-  SPTS_CUDA_OK(ctx);
+  const int bytes = wide ? LG_BYTES + 2 : LG_BYTES;
+  for (int r0 = 0; r0 < n; r0 += LOGITS_MAX_ROWS) {
+    const int rows = n - r0 < LOGITS_MAX_ROWS ? n - r0 : LOGITS_MAX_ROWS;
+    // A few rows: sixteen large CTAs each (the history is read by every one of them).  More: slices of about 6144 tokens, whose
+    // tables let four small CTAs onto an SM.
+    const bool few = 16 * rows <= ctx->sm_count;
+    int slices = few ? 16 : ceil_div(vocab, 6144);
+    if (slices > ceil_div(vocab, 1024)) slices = ceil_div(vocab, 1024);
+    const int per = (int)align_up((size_t)ceil_div(vocab + 3, slices), 32);
+    const int most = LG_WINDOW * LG_BYTES / bytes / 32 * 32;
+    const int window = !tables || per < most ? per : most;
+    LogitsArgs a{logits + (size_t)r0 * ld, ld, rows, vocab, rules, out != nullptr ? out + (size_t)r0 * ldo : nullptr, ldo,
+                 token != nullptr ? token + r0 : nullptr, ctx->ws.lg_key, ctx->ws.lg_arrived};
+    if (r0 > 0) {
+      spts_logits_rules& r = a.r;
+      if (r.history_start) r.history_start += r0;
+      if (r.generated_start) r.generated_start += r0;
+      if (r.repetition) r.repetition += r0;
+      if (r.presence) r.presence += r0;
+      if (r.frequency) r.frequency += r0;
+      if (r.bias_start) r.bias_start += r0;
+      if (r.mask) r.mask += (size_t)r0 * r.ld_mask;
+    }
+    auto kernel = wide ? (few ? logits_kernel<uint32_t, 1024> : logits_kernel<uint32_t, 256>)
+                       : (few ? logits_kernel<uint16_t, 1024> : logits_kernel<uint16_t, 256>);
+    const size_t smem = tables ? (size_t)window * bytes : 0;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LG_WINDOW * LG_BYTES) != cudaSuccess) return SPTS_ERR_CUDA;
+    kernel<<<slices * rows, few ? 1024 : 256, smem, ctx->stream>>>(a, slices, per, window);
+    SPTS_CUDA_OK(ctx);
+  }
   return SPTS_OK;
 }
 

@@ -115,6 +115,8 @@ size_t carve(const spts_model_desc& d, int Nmax, void* base, Workspace* ws, std:
   // fragments 2 bytes an element; sums 16 bytes per 32; factors
   w.w4_x = c.take<char>(W4_X_ELEMENTS * 2 + W4_X_ELEMENTS / 2 + 256);
   w.w4_part = c.take<float>((size_t)2 * W4_MAX_CTAS * 16 * 256);
+  w.lg_key = c.take<unsigned long long>(LOGITS_MAX_ROWS);
+  w.lg_arrived = c.take<int>(LOGITS_MAX_ROWS);
   w.kv4_part = c.take<float>((size_t)2 * KV4_MAX_CTAS * 16 * (d.head_dim + 2));
   w.kv4_arrived = c.take<int>(KV4_MAX_CTAS);
   w.dec = c.take<float>(decode_scratch_floats(d));
@@ -611,7 +613,9 @@ spts_status spts_create(const spts_model_desc* desc, int max_seq, void* workspac
     spts_destroy(ctx);
     return SPTS_ERR_CUDA;
   }
-  if (cudaMemsetAsync(ctx->ws.kv4_arrived, 0, KV4_MAX_CTAS * sizeof(int), ctx->stream) != cudaSuccess) {
+  if (cudaMemsetAsync(ctx->ws.kv4_arrived, 0, KV4_MAX_CTAS * sizeof(int), ctx->stream) != cudaSuccess ||
+      cudaMemsetAsync(ctx->ws.lg_key, 0, LOGITS_MAX_ROWS * sizeof(unsigned long long), ctx->stream) != cudaSuccess ||
+      cudaMemsetAsync(ctx->ws.lg_arrived, 0, LOGITS_MAX_ROWS * sizeof(int), ctx->stream) != cudaSuccess) {
     spts_destroy(ctx);
     return SPTS_ERR_CUDA;
   }
