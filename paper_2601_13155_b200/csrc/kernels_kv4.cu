@@ -528,21 +528,19 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
             if (16 * rt + g + 8 >= valid) { sc[rt][nb][2] = -INFINITY; sc[rt][nb][3] = -INFINITY; }
           }
       }
-      uint32_t vp0[RT][NG], vp1[RT][NG];
       float top_s = 0.f, top[NB][2];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) top[nb][0] = top[nb][1] = -INFINITY;
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        load_words<NG>(st + T::VP + (16 * rt + g) * NG * 4, vp0[rt]);
-        load_words<NG>(st + T::VP + (16 * rt + g + 8) * NG * 4, vp1[rt]);
-#pragma unroll
-        for (int gr = 0; gr < NG; ++gr) top_s = fmaxf(top_s, fmaxf(lo_bf16(vp0[rt][gr]), lo_bf16(vp1[rt][gr])));
+      for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
           for (int i = 0; i < 2; ++i) top[nb][i] = fmaxf(top[nb][i], fmaxf(sc[rt][nb][i], sc[rt][nb][2 + i]));
-      }
+      // the largest scale of V among the params words, ROWS NG / 32 to a lane
+#pragma unroll
+      for (int i = 0; i < (ROWS * NG + 31) / 32; ++i)
+        if (ROWS * NG % 32 == 0 || lane < ROWS * NG) top_s = fmaxf(top_s, lo_bf16(reinterpret_cast<const uint32_t*>(st + T::VP)[32 * i + lane]));
       bool over = top_s > r_lim;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) over = over || top[nb][0] > thr[nb][0] || top[nb][1] > thr[nb][1];
@@ -581,6 +579,9 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
       // ---- O
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
+        uint32_t vp0[NG], vp1[NG];
+        load_words<NG>(st + T::VP + (16 * rt + g) * NG * 4, vp0);
+        load_words<NG>(st + T::VP + (16 * rt + g + 8) * NG * 4, vp1);
         uint32_t pb[NB][NG][2], pu[NB][2];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -595,7 +596,7 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
           for (int i = 0; i < 4; ++i) p[i] *= r_inv;
 #pragma unroll
           for (int gr = 0; gr < NG; ++gr) {
-            const float s0 = lo_bf16(vp0[rt][gr]), s1 = lo_bf16(vp1[rt][gr]);
+            const float s0 = lo_bf16(vp0[gr]), s1 = lo_bf16(vp1[gr]);
             pb[nb][gr][0] = transpose8x8(pack2_f16(p[0] * s0, p[1] * s0));
             pb[nb][gr][1] = transpose8x8(pack2_f16(p[2] * s1, p[3] * s1));
           }
