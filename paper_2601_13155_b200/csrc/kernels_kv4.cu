@@ -4,6 +4,8 @@
 // into warp-level matrix instructions; see there.
 // kv4_attn_plain_kernel: one CTA per query head and sequence, CUDA cores, fp32 arithmetic, online softmax per warp.
 // fp32 storage and SPTS_REFERENCE_KERNELS.
+#include <cooperative_groups.h>
+
 #include "q4_common.cuh"
 
 namespace spts {
@@ -11,6 +13,7 @@ namespace spts {
 namespace {
 
 using namespace q4;
+namespace cg = cooperative_groups;
 
 struct Kv4Dev {
   char* k_codes; char* v_codes; uint32_t* k_params; uint32_t* v_params;
@@ -110,14 +113,20 @@ __global__ void kv4_len_kernel(int32_t* len, const int32_t* __restrict__ at, con
 }
 
 constexpr int PLAIN_WARPS = 16;
+constexpr int PLAIN_ROWS = 4;                      // rows of a warp's step: their loads and sums over lanes run side by side
+constexpr int PLAIN_SPLIT = 8;                     // CTAs per query head at most (a portable cluster)
 
+// blockIdx.x = a cluster's CTAs, which share the rows of query head blockIdx.y in sequence blockIdx.z
 template <typename T, int D>
 __global__ void __launch_bounds__(PLAIN_WARPS * 32)
 kv4_attn_plain_kernel(Kv4Dev c, const T* __restrict__ Q, int64_t ldq, int H, T* __restrict__ O, int64_t ldo) {
   constexpr int E = D / 32;                        // storage positions per lane
   __shared__ float sm_m[PLAIN_WARPS], sm_l[PLAIN_WARPS];
   __shared__ float sm_o[PLAIN_WARPS][D];
-  const int h = blockIdx.x, b = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  __shared__ float sm_part[D + 2];                 // the CTA's O, sum and maximum
+  cg::cluster_group cluster = cg::this_cluster();
+  const int split = gridDim.x, rank = blockIdx.x;
+  const int h = blockIdx.y, b = blockIdx.z, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int kvh = h / (H / c.Hkv);
   const int len = max(0, min(c.len[b], c.capacity));
   T* out = O + (size_t)b * ldo + (size_t)h * D;
@@ -135,31 +144,50 @@ kv4_attn_plain_kernel(Kv4Dev c, const T* __restrict__ Q, int64_t ldq, int H, T* 
   float m = -INFINITY, l = 0.f;
   const size_t base = ((size_t)b * c.Hkv + kvh) * c.capacity;
   const int ng = D / c.group;
-  for (int j = warp; j < len; j += PLAIN_WARPS) {
-    const size_t r = base + j;
-    uint32_t kw, vw;
-    if (E == 4) {
-      kw = reinterpret_cast<const uint16_t*>(c.k_codes + r * (D / 2))[lane];
-      vw = reinterpret_cast<const uint16_t*>(c.v_codes + r * (D / 2))[lane];
-    } else {
-      kw = reinterpret_cast<const uint8_t*>(c.k_codes + r * (D / 2))[lane];
-      vw = reinterpret_cast<const uint8_t*>(c.v_codes + r * (D / 2))[lane];
-    }
-    float s = 0.f;
+  auto codes = [&](const char* at, size_t r) -> uint32_t {
+    return E == 4 ? reinterpret_cast<const uint16_t*>(at + r * (D / 2))[lane] : reinterpret_cast<const uint8_t*>(at + r * (D / 2))[lane];
+  };
+  const int step = split * PLAIN_WARPS * PLAIN_ROWS;
+  for (int64_t j = (int64_t)(rank * PLAIN_WARPS + warp) * PLAIN_ROWS; j < len; j += step) {
+    uint32_t kw[PLAIN_ROWS], vw[PLAIN_ROWS], kp[PLAIN_ROWS][E], vp[PLAIN_ROWS][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const uint32_t p = c.k_params[r * ng + gk[e]];
-      s = fmaf(q[e], fmaf(lo_bf16(p), (float)((int)((kw >> (4 * e)) & 15) - 8), hi_bf16(p)), s);
+    for (int i = 0; i < PLAIN_ROWS; ++i) {
+      const size_t r = base + (j + i < len ? j + i : j);       // rows behind the end: the step's first one, of weight 0
+      kw[i] = codes(c.k_codes, r);
+      vw[i] = codes(c.v_codes, r);
+#pragma unroll
+      for (int e = 0; e < E; ++e) { kp[i][e] = c.k_params[r * ng + gk[e]]; vp[i][e] = c.v_params[r * ng + gv[e]]; }
     }
-    s = warp_sum(s);
-    const float mn = fmaxf(m, s);
+    float s[PLAIN_ROWS];
+    float mn = m;
+#pragma unroll
+    for (int i = 0; i < PLAIN_ROWS; ++i) {
+      s[i] = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        s[i] = fmaf(q[e], fmaf(lo_bf16(kp[i][e]), (float)((int)((kw[i] >> (4 * e)) & 15) - 8), hi_bf16(kp[i][e])), s[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < PLAIN_ROWS; ++i) {
+      s[i] = warp_sum(s[i]);
+      if (j + i < len) mn = fmaxf(mn, s[i]);
+    }
     // a NaN score (non-finite rows in the cache) goes on as NaN
-    const float corr = m == -INFINITY ? 0.f : expf(m - mn), pr = s == -INFINITY ? 0.f : expf(s - mn);
-    l = l * corr + pr;
+    const float corr = m == -INFINITY ? 0.f : expf(m - mn);
+    float pr[PLAIN_ROWS];
+    l *= corr;
+#pragma unroll
+    for (int i = 0; i < PLAIN_ROWS; ++i) {
+      pr[i] = j + i >= len || s[i] == -INFINITY ? 0.f : expf(s[i] - mn);
+      l += pr[i];
+    }
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const uint32_t p = c.v_params[r * ng + gv[e]];
-      o[e] = fmaf(pr, fmaf(lo_bf16(p), (float)((int)((vw >> (4 * e)) & 15) - 8), hi_bf16(p)), o[e] * corr);
+      o[e] *= corr;
+#pragma unroll
+      for (int i = 0; i < PLAIN_ROWS; ++i)
+        if (j + i < len)
+          o[e] = fmaf(pr[i], fmaf(lo_bf16(vp[i][e]), (float)((int)((vw[i] >> (4 * e)) & 15) - 8), hi_bf16(vp[i][e])), o[e]);
     }
     m = mn;
   }
@@ -167,7 +195,8 @@ kv4_attn_plain_kernel(Kv4Dev c, const T* __restrict__ Q, int64_t ldq, int H, T* 
 #pragma unroll
   for (int e = 0; e < E; ++e) sm_o[warp][dv[e]] = o[e];
   __syncthreads();
-  for (int dim = threadIdx.x; dim < D; dim += PLAIN_WARPS * 32) {
+  if (threadIdx.x < D) {
+    const int dim = threadIdx.x;
     float M = -INFINITY, L = 0.f, a = 0.f;
     for (int w = 0; w < PLAIN_WARPS; ++w) M = fmaxf(M, sm_m[w]);
     for (int w = 0; w < PLAIN_WARPS; ++w) {
@@ -175,8 +204,22 @@ kv4_attn_plain_kernel(Kv4Dev c, const T* __restrict__ Q, int64_t ldq, int H, T* 
       L += sm_l[w] * f;
       a = fmaf(sm_o[w][dim], f, a);
     }
-    out[dim] = from_f32<T>(len > 0 ? a / L : 0.f);
+    sm_part[dim] = a;
+    if (dim == 0) { sm_part[D] = L; sm_part[D + 1] = M; }
   }
+  cluster.sync();
+  if (rank == 0 && threadIdx.x < D) {
+    float M = -INFINITY, L = 0.f, a = 0.f;
+    for (int x = 0; x < split; ++x) M = fmaxf(M, cluster.map_shared_rank(sm_part, x)[D + 1]);
+    for (int x = 0; x < split; ++x) {
+      const float* part = cluster.map_shared_rank(sm_part, x);
+      const float f = part[D + 1] == -INFINITY ? 0.f : expf(part[D + 1] - M);
+      L += part[D] * f;
+      a = fmaf(part[threadIdx.x], f, a);
+    }
+    out[threadIdx.x] = from_f32<T>(len > 0 ? a / L : 0.f);
+  }
+  cluster.sync();                                  // no CTA leaves while its part is being read
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -791,7 +834,20 @@ template <typename T, int D>
 spts_status attn_plain_t(spts_ctx* ctx, const spts_kv4_cache* cache, const void* Q, int64_t ldq, void* O, int64_t ldo) {
   const Kv4Dev c = kv4_dev(ctx, cache);
   const int H = ctx->desc.n_q_heads;
-  kv4_attn_plain_kernel<T, D><<<dim3(H, c.n_seq), PLAIN_WARPS * 32, 0, ctx->stream>>>(c, (const T*)Q, ldq, H, (T*)O, ldo);
+  // CTAs per head: as many as still run at once (one of 512 threads and 95 registers on an SM, two at 64 dims)
+  int split = PLAIN_SPLIT;
+  while (split > 1 && (long)H * c.n_seq * split > 2L * ctx->sm_count) split /= 2;
+  cudaLaunchConfig_t config{};
+  config.gridDim = dim3(split, H, c.n_seq);
+  config.blockDim = dim3(PLAIN_WARPS * 32);
+  config.stream = ctx->stream;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = split;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  config.attrs = &attr;
+  config.numAttrs = 1;
+  if (cudaLaunchKernelEx(&config, kv4_attn_plain_kernel<T, D>, c, (const T*)Q, ldq, H, (T*)O, ldo) != cudaSuccess) return SPTS_ERR_CUDA;
   SPTS_CUDA_OK(ctx);
   return SPTS_OK;
 }
