@@ -34,7 +34,7 @@
  *     spts_layer_prefill_skip() and spts_prefill() use the context's workspace for every intermediate
  *     (K of all candidates, the selected rows' Q, the attention output, the SwiGLU intermediate, scores,
  *     index lists), so the workspace grows with max_seq: about 24 KiB per candidate at the 8B shape plus 0.5 GB (of
- *     which 0.47 GB is the SwiGLU intermediate of one 16384-row chunk): 1.30 GB at 32768 candidates, 3.68 GB at 131072.
+ *     which 0.47 GB is the SwiGLU intermediate of one 16384-row chunk): 1.32 GB at 32768 candidates, 3.70 GB at 131072.
  */
 #ifndef SPTS_H_
 #define SPTS_H_
@@ -416,13 +416,14 @@ enum {
 };
 #define SPTS_W4_MAX_N 32
 #define SPTS_W4_MAX_IN 131072
+#define SPTS_W4_MAX_OUT (1 << 30)
 
 /* Y[t] = X[t] W^T for n tokens, 0 <= n <= SPTS_W4_MAX_N, in_features <= SPTS_W4_MAX_IN (the codes are read once for all
  * tokens up to 32768 features, beyond that once for every 24, 16 or 8).
  *   w2 given: Y[t] = silu(X[t] W^T) * (X[t] W2^T) (gate and up projection; same shape and group)
  *   residual given: Y[t] = residual[t] + X[t] W^T (Y may be the residual itself; not with w2 or SPTS_W4_FP32_OUT)
  * X [n, in], residual and Y [n, out] in the storage type with row strides ldx, ldr, ldy in elements; X 16-byte aligned,
- * ldx a multiple of 8 (n > 1).  Sums in fp32, one rounding at the end. */
+ * ldx a multiple of 8 (n > 1); Y lies apart from X.  Sums in fp32, one rounding at the end. */
 spts_status spts_w4_gemv(spts_ctx* ctx, const spts_w4* w, const spts_w4* w2, const void* X, int64_t ldx, int n,
                          const void* residual, int64_t ldr, uint32_t flags, void* Y, int64_t ldy);
 
@@ -457,8 +458,8 @@ spts_status spts_kv4_append(spts_ctx* ctx, const spts_kv4_cache* cache, const vo
 
 /* Attention of one query per sequence over what its cache holds: O[b, h] = softmax_j(Q[b, h] . K[b, j] / sqrt(d))
  * V[b, j], j < len[b], KV head h / (H / Hkv).  Q [n_seq, H, d] and O [n_seq, H * d] in the storage type, row strides
- * ldq, ldo in elements.  A sequence with len[b] <= 0 gets zeros; len[b] beyond the capacity counts as the capacity.
- * n_seq <= SPTS_KV4_MAX_SEQ. */
+ * ldq, ldo in elements; O lies apart from Q, whose elements are below 2^100.  A sequence with len[b] <= 0 gets zeros;
+ * len[b] beyond the capacity counts as the capacity.  n_seq <= SPTS_KV4_MAX_SEQ. */
 #define SPTS_KV4_MAX_SEQ 1024
 spts_status spts_kv4_attention(spts_ctx* ctx, const spts_kv4_cache* cache, const void* Q, int64_t ldq, void* O_out,
                                int64_t ldo);
@@ -466,7 +467,9 @@ spts_status spts_kv4_attention(spts_ctx* ctx, const spts_kv4_cache* cache, const
 /* Rules for the logits of n rows.  Every pointer is a device pointer and may be NULL (the rule is off).
  * The lists are packed: row b's tokens are history[history_start[b]] .. history[history_start[b + 1] - 1] and of them
  * those from index generated_start[b] on were generated (NULL: all); its biases are the entries bias_start[b] ..
- * bias_start[b + 1] - 1.  Tokens outside [0, vocab) are ignored. */
+ * bias_start[b + 1] - 1.  Tokens outside [0, vocab) are ignored, and so is what a start puts outside its list. */
+#define SPTS_LOGITS_MAX_LIST (1 << 29)   /* entries of a list  */
+#define SPTS_LOGITS_MAX_VOCAB (1 << 30)
 typedef struct {
   const int32_t* history;          /* [n_history]  */
   const int32_t* history_start;    /* [n + 1]      */

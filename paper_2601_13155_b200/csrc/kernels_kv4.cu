@@ -691,7 +691,7 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
         s += __shfl_xor_sync(0xffffffffu, s, 16);
         if (g == 0) { sm_m[warp][8 * nb + 2 * cc + i] = msl[nb][i]; sm_l[warp][8 * nb + 2 * cc + i] = s; }
       }
-      const float even = CODE_UNIT_INV / r_inv, odd = even * ODD;       // back from the codes' units; r_inv holds the boost
+      const float r = 1.f / r_inv;                 // (r_inv holds the boost)
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         // lane (group, cc) of the mids' tile holds queries 2 cc, 2 cc + 1
@@ -701,8 +701,8 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
         for (int j = 0; j < 2; ++j) {
           const float* ov = o[nb][t][j];
           float* dst = sm_o + (size_t)(warp * NQ + 8 * nb + 2 * cc) * T::OSTRIDE + 32 * t + 4 * g + 2 * j;
-          *reinterpret_cast<float2*>(dst) = make_float2(fmaf(ov[0] + oz_t[0], even, z0), fmaf(ov[2] + oz_t[2], odd, z0));
-          *reinterpret_cast<float2*>(dst + T::OSTRIDE) = make_float2(fmaf(ov[1] + oz_t[1], even, z1), fmaf(ov[3] + oz_t[3], odd, z1));
+          *reinterpret_cast<float2*>(dst) = make_float2(fmaf((ov[0] + oz_t[0]) * CODE_UNIT_INV, r, z0), fmaf((ov[2] + oz_t[2]) * (CODE_UNIT_INV * ODD), r, z0));
+          *reinterpret_cast<float2*>(dst + T::OSTRIDE) = make_float2(fmaf((ov[1] + oz_t[1]) * CODE_UNIT_INV, r, z1), fmaf((ov[3] + oz_t[3]) * (CODE_UNIT_INV * ODD), r, z1));
         }
       }
     }

@@ -49,7 +49,7 @@ __device__ __forceinline__ void last_entry(uint16_t* p, int e) {
 }
 
 __device__ __forceinline__ void range(const int32_t* start, int b, int n_all, int& i0, int& i1) {
-  i0 = max(0, start[b]);
+  i0 = min(max(0, start[b]), n_all);
   i1 = min(n_all, start[b + 1]);
 }
 

@@ -178,7 +178,7 @@ __device__ __forceinline__ void w4_prepare(const bf16* __restrict__ x, int token
 #pragma unroll
   for (int w = 1; w < WARPS; ++w) { top = fmaxf(top, red[0][w]); ss += red[1][w]; }
   const float xs = scale_to_2_13(top), xo = xs * ODD, u = xs * CODE_UNIT;
-  if (tid == 0) factor[token] = (norm ? 1.0f / sqrtf(ss / (float)in + eps) : 1.0f) / u;
+  if (tid == 0) factor[token] = (norm ? 1.0f / sqrtf(ss / (float)in + eps) : 1.0f) / xs;
   const int chunks = (in + W4_CHUNK - 1) / W4_CHUNK;
   // a warp lays out a chunk at a time: lane 4 t + c
 #pragma unroll 2
@@ -480,8 +480,8 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
       for (int i = threadIdx.x; i < n * ROWS; i += W4_WARPS * 32) {
         const int t = i / ROWS, r = i - t * ROWS, row = tile * ROWS + r, at = w4_place<MT, TWO>(r);
         if (row >= out) continue;
-        const float f = sm_factor[t], v = sum_wk(t, at) * f;
-        w4_store<bf16>(o, t, row, TWO ? silu_mul(v, sum_wk(t, at + 16) * f) : v);
+        const float f = sm_factor[t], v = sum_wk(t, at) * CODE_UNIT_INV * f;
+        w4_store<bf16>(o, t, row, TWO ? silu_mul(v, sum_wk(t, at + 16) * CODE_UNIT_INV * f) : v);
       }
     } else {
       float* mine = part + (size_t)(2 * blockIdx.x + (step == 0 ? 1 : 0)) * n * RSTRIDE;
@@ -514,6 +514,8 @@ w4_join_kernel(int out, int n, W4Line line, const float* __restrict__ part, cons
     if (TWO) v2 += __ldcg(p + 2 * c * share + 16);
   }
   const float f = __ldg(factor + t);
+  v *= CODE_UNIT_INV;
+  v2 *= CODE_UNIT_INV;
   w4_store<bf16>(o, t, row, TWO ? silu_mul(v * f, v2 * f) : v * f);
 }
 

@@ -66,11 +66,12 @@ template <int J> __device__ __forceinline__ uint32_t code_pair(uint32_t w) {
 constexpr float CODE_UNIT = 5.9604644775390625e-08f;        // 2^-24
 constexpr float CODE_UNIT_INV = 16777216.f;                 // 2^24
 constexpr float ODD = 0.0625f;                              // what a factor of an odd J is multiplied by to be in the same unit
-// The power of two that brings `top` (>= 0) to [2^13, 2^14), held within 2^-100 .. 2^120; 1 for zero, infinity and NaN.
+// The power of two that brings `top` (>= 0) to [2^13, 2^14), 2^120 at most (2^-114 at least, by what fp32 holds); 1 for zero,
+// infinity and NaN.  Times CODE_UNIT it may leave fp32's normal range, so its inverse and CODE_UNIT_INV are applied one by one.
 __device__ __forceinline__ float scale_to_2_13(float top) {
   const int e = (int)(__float_as_uint(top) >> 23);          // biased exponent
   if (e == 0 || e >= 255) return e == 0 && top > 0.f ? 1.329227995784916e36f : 1.f;
-  return __uint_as_float((uint32_t)(127 + max(-100, min(120, 13 + 127 - e))) << 23);
+  return __uint_as_float((uint32_t)(127 + min(120, 13 + 127 - e)) << 23);
 }
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"

@@ -1,6 +1,7 @@
 // C boundary of the SPTS library: argument checks, workspace carving and the per-layer
 // schedule of Algorithm 1.  Everything here is host code that enqueues kernels on the context's
 // stream; no call synchronises except spts_last_device_status().
+#include <initializer_list>
 #include <new>
 #include <cmath>
 #include <cstring>
@@ -1150,7 +1151,12 @@ struct DeviceScope {
 };
 #define ON_DEVICE(ctx) DeviceScope device_scope__(ctx); if (!device_scope__.ok) return SPTS_ERR_CUDA
 bool group_ok(int group) { return group == 32 || group == 64 || group == 128; }
-bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
+bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+bool aligned4(std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if (!aligned_to(p, 4)) return false;
+  return true;
+}
 // rows of 16-byte loads: aligned base, stride a multiple of 16 bytes where there is more than one row
 bool rows_ok(const void* p, int64_t ld, int64_t width, int64_t n, size_t es) {
   return aligned16(p) && (n < 2 || (ld >= width && (ld * (int64_t)es) % 16 == 0));
@@ -1158,7 +1164,7 @@ bool rows_ok(const void* p, int64_t ld, int64_t width, int64_t n, size_t es) {
 spts_status check_w4(const spts_w4* w) {
   if (w->codes == nullptr || w->params == nullptr || !aligned16(w->codes) || !aligned16(w->params)) return SPTS_ERR_INVALID_ARG;
   if (!group_ok(w->group) || w->out_features < 1 || w->in_features < 1 || w->in_features % w->group != 0 ||
-      w->in_features > SPTS_W4_MAX_IN)
+      w->in_features > SPTS_W4_MAX_IN || w->out_features > SPTS_W4_MAX_OUT)
     return SPTS_ERR_SHAPE;
   return SPTS_OK;
 }
@@ -1170,7 +1176,7 @@ spts_status check_kv4(const spts_ctx* ctx, const spts_kv4_cache* c) {
   if (c->n_seq == 0) return SPTS_OK;
   if (c->k_codes == nullptr || c->v_codes == nullptr || c->k_params == nullptr || c->v_params == nullptr || c->len == nullptr)
     return SPTS_ERR_INVALID_ARG;
-  if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || !aligned16(c->k_params) || !aligned16(c->v_params))
+  if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || !aligned16(c->k_params) || !aligned16(c->v_params) || !aligned4({c->pos, c->len}))
     return SPTS_ERR_INVALID_ARG;
   return SPTS_OK;
 }
@@ -1179,7 +1185,9 @@ spts_status check_kv4(const spts_ctx* ctx, const spts_kv4_cache* c) {
 spts_status spts_w4_quantize(spts_ctx* ctx, const void* W, int out_features, int in_features, int group, void* codes, void* params) {
   TRY(check_ctx(ctx));
   if (W == nullptr || codes == nullptr || params == nullptr) return SPTS_ERR_INVALID_ARG;
-  if (!group_ok(group) || out_features < 1 || in_features < 1 || in_features % group != 0) return SPTS_ERR_SHAPE;
+  if (!group_ok(group) || out_features < 1 || in_features < 1 || in_features % group != 0 || in_features > SPTS_W4_MAX_IN ||
+      out_features > SPTS_W4_MAX_OUT)
+    return SPTS_ERR_SHAPE;
   if (!aligned16(W) || !aligned16(codes) || !aligned16(params)) return SPTS_ERR_INVALID_ARG;
   ON_DEVICE(ctx);
   return launch_w4_quantize(ctx, W, out_features, in_features, group, codes, params);
@@ -1201,6 +1209,8 @@ spts_status spts_w4_gemv(spts_ctx* ctx, const spts_w4* w, const spts_w4* w2, con
   if (!rows_ok(X, ldx, w->in_features, n, elt_size(ctx->desc))) return SPTS_ERR_INVALID_ARG;
   if (n > 1 && (ldy < w->out_features || (residual != nullptr && ldr < w->out_features))) return SPTS_ERR_INVALID_ARG;
   if (Y == X || (residual == Y && ldr != ldy && n > 1)) return SPTS_ERR_INVALID_ARG;
+  const size_t es = elt_size(ctx->desc);
+  if (!aligned_to(Y, (flags & SPTS_W4_FP32_OUT) ? 4 : es) || !aligned_to(residual, es)) return SPTS_ERR_INVALID_ARG;
   W4GemvArgs a;
   memset(&a, 0, sizeof(a));
   a.codes = w->codes; a.params = w->params;
@@ -1228,6 +1238,7 @@ spts_status spts_kv4_append(spts_ctx* ctx, const spts_kv4_cache* cache, const vo
     if (!rows_ok(K, ldk, width, n_rows, es) || !rows_ok(V, ldv, width, n_rows, es)) return SPTS_ERR_INVALID_ARG;
     if (!aligned16(K_read) || !aligned16(V_read) || (K_read != nullptr && K_read == V_read)) return SPTS_ERR_INVALID_ARG;
   }
+  if (!aligned4({pos, row_start, at})) return SPTS_ERR_INVALID_ARG;
   if (at == cache->len) at = nullptr;
   ON_DEVICE(ctx);
   return launch_kv4_append(ctx, cache, K, ldk, V, ldv, pos, row_start, at, n_rows, K_read, V_read);
@@ -1249,14 +1260,17 @@ spts_status spts_process_logits(spts_ctx* ctx, const float* logits, int64_t ld, 
                                 float* out, int64_t ldo, int32_t* token_out) {
   TRY(check_ctx(ctx));
   if (rules == nullptr || n < 0) return SPTS_ERR_INVALID_ARG;
-  if (vocab < 1 || n > 65535) return SPTS_ERR_SHAPE;
+  if (vocab < 1 || vocab > SPTS_LOGITS_MAX_VOCAB || n > 65535) return SPTS_ERR_SHAPE;
   if (n == 0) return SPTS_OK;
   if (out == nullptr && token_out == nullptr) return SPTS_ERR_INVALID_ARG;
-  if (logits == nullptr || !aligned4(logits) || !aligned4(out)) return SPTS_ERR_INVALID_ARG;
+  if (logits == nullptr || !aligned4({logits, out, token_out})) return SPTS_ERR_INVALID_ARG;
   if (n > 1 && (ld < vocab || (out != nullptr && ldo < vocab))) return SPTS_ERR_INVALID_ARG;
   if (out == logits && n > 1 && ld != ldo) return SPTS_ERR_INVALID_ARG;
   spts_logits_rules r = *rules;
-  if (r.n_history < 0 || r.n_bias < 0) return SPTS_ERR_INVALID_ARG;
+  if (r.n_history < 0 || r.n_history > SPTS_LOGITS_MAX_LIST || r.n_bias < 0 || r.n_bias > SPTS_LOGITS_MAX_LIST) return SPTS_ERR_INVALID_ARG;
+  if (!aligned4({r.history, r.history_start, r.generated_start, r.repetition, r.presence, r.frequency}) ||
+      !aligned4({r.bias_token, r.bias_value, r.bias_start, r.mask}))
+    return SPTS_ERR_INVALID_ARG;
   if (r.history != nullptr && r.history_start == nullptr) return SPTS_ERR_INVALID_ARG;
   if (r.bias_token != nullptr && (r.bias_value == nullptr || r.bias_start == nullptr)) return SPTS_ERR_INVALID_ARG;
   if (r.mask != nullptr && n > 1 && r.ld_mask < (vocab + 31) / 32) return SPTS_ERR_INVALID_ARG;
@@ -1287,6 +1301,7 @@ spts_status spts_decode_step4(spts_ctx* ctx, const spts_model_weights4* mw, cons
   if (n > SPTS_W4_MAX_N || n > ctx->max_seq) return SPTS_ERR_SHAPE;
   if (n == 0) return SPTS_OK;
   if (pos == nullptr || (x_in == nullptr && (token_in == nullptr || mw->embed == nullptr))) return SPTS_ERR_INVALID_ARG;
+  if (!aligned4({pos, token_in, logits_out, token_out})) return SPTS_ERR_INVALID_ARG;
   if (!aligned16(x_in) || !aligned16(x_out) || !aligned16(mw->embed)) return SPTS_ERR_INVALID_ARG;
   const bool head = logits_out != nullptr || token_out != nullptr;
   if (head) {
