@@ -17,11 +17,12 @@ namespace spts {
 
 namespace {
 
-constexpr int LG_BATCH = 4;             // groups of four logits of a thread in flight
+constexpr int LG_BATCH = 2;             // groups of four logits of a thread in flight
 constexpr int LG_HISTORY = 2;           // 16-byte pieces of the history of a thread in flight
 constexpr int LG_BYTES = 8;             // shared memory per token of the slice: its word, 2 on the list, 2 for a bias entry
 // tokens of a CTA's slice that are worked on at a time
 constexpr int LG_WINDOW = 27648;
+constexpr int LG_SLICE = 14336;         // two CTAs' tables in an SM's shared memory
 
 struct LogitsArgs {
   const float* x; int64_t ld; int n, vocab;
@@ -57,7 +58,7 @@ constexpr uint32_t OCCURRED = 0x80000000u, BIASED = 0x40000000u, TIMES = 0x3FFFF
 
 // E: an entry number of the row's bias list, 16 bits where the list is short enough
 template <typename E, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) logits_kernel(LogitsArgs a, int slices, int per, int window) {
+__global__ void __launch_bounds__(THREADS, THREADS == 512 ? 2 : 1) logits_kernel(LogitsArgs a, int slices, int per, int window) {
   extern __shared__ __align__(16) unsigned char smem[];
   // [window] words, [window] last bias entry + 1, [window] listed tokens (windows are multiples of 32)
   uint32_t* word = reinterpret_cast<uint32_t*>(smem);
@@ -176,25 +177,12 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) logits_kernel
         }
         if (tables) {
           const uint4 w = in ? reinterpret_cast<const uint4*>(word)[j] : make_uint4(0u, 0u, 0u, 0u);
-          if (__any_sync(0xffffffffu, (w.x | w.y | w.z | w.w) != 0u)) {
+          if ((w.x | w.y | w.z | w.w) != 0u) {
             const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-            uint32_t vote[4];
-            int many = 0, before = 0;
+            int at = atomicAdd(&listed, (w.x != 0u) + (w.y != 0u) + (w.z != 0u) + (w.w != 0u));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              vote[i] = __ballot_sync(0xffffffffu, ww[i] != 0u);
-              many += __popc(vote[i]);
-            }
-            int at = lane == 0 ? atomicAdd(&listed, many) : 0;
-            at = __shfl_sync(0xffffffffu, at, 0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if (ww[i]) {
-                list[at + before + __popc(vote[i] & ((1u << lane) - 1u))] = (uint16_t)(4 * j + i);
-                y[i] = -INFINITY;
-              }
-              before += __popc(vote[i]);
-            }
+            for (int i = 0; i < 4; ++i)
+              if (ww[i]) { list[at++] = (uint16_t)(4 * j + i); y[i] = -INFINITY; }
           }
         }
         const float m = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));          // (passes over NaN)
@@ -264,10 +252,12 @@ spts_status launch_process_logits(spts_ctx* ctx, const float* logits, int64_t ld
   const int bytes = wide ? LG_BYTES + 2 : LG_BYTES;
   for (int r0 = 0; r0 < n; r0 += LOGITS_MAX_ROWS) {
     const int rows = n - r0 < LOGITS_MAX_ROWS ? n - r0 : LOGITS_MAX_ROWS;
-    // A few rows: sixteen large CTAs each (the history is read by every one of them).  More: slices of about 6144 tokens, whose
-    // tables let four small CTAs onto an SM.
+    // A few rows: sixteen CTAs of 1024 threads each (the history is read by every one of them).  More: slices of at most LG_SLICE
+    // tokens, whose tables let two CTAs of 512 threads onto an SM (64 rows of 152063: 35 us; four of 256 with 6144 tokens 38, three
+    // of 384 with 8192 38, five of 256 40), as many slices as the rounds of resident CTAs that these take have room for.
     const bool few = 16 * rows <= ctx->sm_count;
-    int slices = few ? 16 : ceil_div(vocab, 6144);
+    const int seats = 2 * ctx->sm_count, least = ceil_div(vocab, LG_SLICE), rounds = ceil_div(rows * least, seats);
+    int slices = few ? 16 : rounds * seats / rows > least ? rounds * seats / rows : least;
     if (slices > ceil_div(vocab, 1024)) slices = ceil_div(vocab, 1024);
     const int per = (int)align_up((size_t)ceil_div(vocab + 3, slices), 32);
     const int most = LG_WINDOW * LG_BYTES / bytes / 32 * 32;
@@ -284,11 +274,11 @@ spts_status launch_process_logits(spts_ctx* ctx, const float* logits, int64_t ld
       if (r.bias_start) r.bias_start += r0;
       if (r.mask) r.mask += (size_t)r0 * r.ld_mask;
     }
-    auto kernel = wide ? (few ? logits_kernel<uint32_t, 1024> : logits_kernel<uint32_t, 256>)
-                       : (few ? logits_kernel<uint16_t, 1024> : logits_kernel<uint16_t, 256>);
+    auto kernel = wide ? (few ? logits_kernel<uint32_t, 1024> : logits_kernel<uint32_t, 512>)
+                       : (few ? logits_kernel<uint16_t, 1024> : logits_kernel<uint16_t, 512>);
     const size_t smem = tables ? (size_t)window * bytes : 0;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LG_WINDOW * LG_BYTES) != cudaSuccess) return SPTS_ERR_CUDA;
-    kernel<<<slices * rows, few ? 1024 : 256, smem, ctx->stream>>>(a, slices, per, window);
+    kernel<<<slices * rows, few ? 1024 : 512, smem, ctx->stream>>>(a, slices, per, window);
     SPTS_CUDA_OK(ctx);
   }
   return SPTS_OK;
