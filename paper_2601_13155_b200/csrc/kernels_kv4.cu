@@ -359,7 +359,11 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
   }
   const Kv4Line line{pre, c.n_seq, heads};
   const long total = (long)pre[c.n_seq] * heads;
-  const long ctas = max(1L, min((long)gridDim.x, (total + WARPS - 1) / WARPS));
+  long ctas = max(1L, min((long)gridDim.x, (total + WARPS - 1) / WARPS));
+  // Few equally long units: whole numbers of CTAs to each where that leaves at most a sixteenth of them idle.  (A CTA with the end
+  // of one unit and the beginning of the next meets, leaves and joins twice.)
+  const long units = (long)c.n_seq * heads, whole_ctas = ctas / units * units;
+  if (16 * whole_ctas >= 15 * ctas && pre[1] * (long)c.n_seq == pre[c.n_seq]) ctas = whole_ctas;
   // sequences without rows
   for (int b = blockIdx.x; b < c.n_seq; b += gridDim.x)
     if (pre[b + 1] == pre[b])
