@@ -261,9 +261,9 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
   return d;
 }
-template <int D, int NG, int NB>
+template <int D, int NG, int NB, int W>
 struct Kv4Tile {
-  static constexpr int WARPS = 8;
+  static constexpr int WARPS = W;
   // row tiles of a step: with one, the dependent chain of a step leaves the issue slots half empty at two warps per
   // scheduler (more warps would need the registers that the accumulators hold)
   static constexpr int RT = NB == 1 ? 2 : 1, ROWS = 16 * RT;
@@ -274,7 +274,8 @@ struct Kv4Tile {
   static constexpr int STAGE_BYTES = VP + ROWS * NG * 4;
   static constexpr int RING_BYTES = WARPS * STAGES * STAGE_BYTES;
   static constexpr int OSTRIDE = D + 4;            // floats between the queries of a warp's partial O
-  static constexpr int O_BYTES = WARPS * NQ * OSTRIDE * 4;
+  static constexpr int JOIN_BYTES = KV4_MAX_CTAS * NQ * 4;         // a factor per part and query, in the same place
+  static constexpr int O_BYTES = WARPS * NQ * OSTRIDE * 4 > JOIN_BYTES ? WARPS * NQ * OSTRIDE * 4 : JOIN_BYTES;
   static constexpr int SMEM = RING_BYTES + O_BYTES;
 };
 
@@ -330,11 +331,11 @@ struct Kv4Walk {
   }
 };
 
-template <int D, int NG, int NB>
-__global__ void __launch_bounds__(Kv4Tile<D, NG, NB>::WARPS * 32, 1)
+template <int D, int NG, int NB, int W>
+__global__ void __launch_bounds__(W * 32, 8 / W)
 kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qblocks, bf16* __restrict__ O, int64_t ldo,
                 float* __restrict__ part, int* __restrict__ arrived) {
-  using T = Kv4Tile<D, NG, NB>;
+  using T = Kv4Tile<D, NG, NB, W>;
   constexpr int WARPS = T::WARPS, NQ = T::NQ, NT = D / 32, RT = T::RT, ROWS = T::ROWS;
   constexpr int GT = NT / NG;                      // 32-dim blocks of a group
   extern __shared__ __align__(128) unsigned char smem[];
@@ -876,18 +877,28 @@ spts_status attn_plain_t(spts_ctx* ctx, const spts_kv4_cache* cache, const void*
   return SPTS_OK;
 }
 
-template <int D, int NG, int NB>
-spts_status attn_t(spts_ctx* ctx, const spts_kv4_cache* cache, const void* Q, int64_t ldq, void* O, int64_t ldo) {
-  using T = Kv4Tile<D, NG, NB>;
+template <int D, int NG, int NB, int W>
+spts_status attn_w(spts_ctx* ctx, const spts_kv4_cache* cache, const void* Q, int64_t ldq, void* O, int64_t ldo) {
+  using T = Kv4Tile<D, NG, NB, W>;
   const Kv4Dev c = kv4_dev(ctx, cache);
   const int H = ctx->desc.n_q_heads, G = H / c.Hkv;
-  const int grid = ctx->sm_count < KV4_MAX_CTAS ? ctx->sm_count : KV4_MAX_CTAS;
-  if (cudaFuncSetAttribute(kv4_attn_kernel<D, NG, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, T::SMEM) != cudaSuccess)
+  const int grid = 8 / W * ctx->sm_count < KV4_MAX_CTAS ? 8 / W * ctx->sm_count : KV4_MAX_CTAS;
+  if (cudaFuncSetAttribute(kv4_attn_kernel<D, NG, NB, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, T::SMEM) != cudaSuccess)
     return SPTS_ERR_CUDA;
-  kv4_attn_kernel<D, NG, NB><<<grid, T::WARPS * 32, T::SMEM, ctx->stream>>>(c, (const bf16*)Q, ldq, H, NB == 1 ? 1 : ceil_div(G, 16),
+  kv4_attn_kernel<D, NG, NB, W><<<grid, T::WARPS * 32, T::SMEM, ctx->stream>>>(c, (const bf16*)Q, ldq, H, NB == 1 ? 1 : ceil_div(G, 16),
                                                                             (bf16*)O, ldo, ctx->ws.kv4_part, ctx->ws.kv4_arrived);
   SPTS_CUDA_OK(ctx);
   return SPTS_OK;
+}
+// Four warps to a CTA and two CTAs to an SM where there are two units for every SM: a CTA's units follow one another, each with
+// the latency of its beginning and its meeting, and then two go side by side (256 sequences of 100 rows, 8 KV heads: 33 us instead
+// of 51; 64 of 2048 rows: 45 instead of 50).  Few long units are cut into half as many pieces by eight warps (one sequence of
+// 131072 rows: 42 instead of 46; 5000, 300, 12000 and 40 rows, 2 KV heads: 23 instead of 35).
+template <int D, int NG, int NB>
+spts_status attn_t(spts_ctx* ctx, const spts_kv4_cache* cache, const void* Q, int64_t ldq, void* O, int64_t ldo) {
+  const int kv = ctx->desc.n_kv_heads, G = ctx->desc.n_q_heads / kv;
+  const long units = (long)cache->n_seq * kv * (NB == 1 ? 1 : ceil_div(G, 16));
+  return units >= 2 * ctx->sm_count ? attn_w<D, NG, NB, 4>(ctx, cache, Q, ldq, O, ldo) : attn_w<D, NG, NB, 8>(ctx, cache, Q, ldq, O, ldo);
 }
 template <int D, int NG>
 spts_status attn_heads(spts_ctx* ctx, const spts_kv4_cache* cache, const void* Q, int64_t ldq, void* O, int64_t ldo) {

@@ -138,7 +138,7 @@ static const int BATCH_MAX_SEQ = 1024;        // sequences per packed batch that
 static const int W4_MAX_CTAS = 320;           // CTAs of a 4-bit product: two per SM
 static const size_t W4_X_ELEMENTS = 1 << 20;  // tokens x features that are prepared at a time
 static const int LOGITS_MAX_ROWS = 1024;      // rows of logits per launch
-static const int KV4_MAX_CTAS = 160;          // CTAs of the attention over a 4-bit cache: one per SM
+static const int KV4_MAX_CTAS = 320;          // CTAs of the attention over a 4-bit cache: one or two per SM
 static const int PAP_MAX_WINDOW = 64;         // largest query window of the probe (the paper ablates 1, 4 and 64)
 
 // top-k scratch size in uint32 words
