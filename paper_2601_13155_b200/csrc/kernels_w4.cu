@@ -581,7 +581,9 @@ template <int NB, int NG>
 spts_status launch_rows(spts_ctx* ctx, const W4GemvArgs& a) {
   if constexpr (NB > 1) {
     if (a.codes2 != nullptr) return launch_tile<NB, 2, NG, true, 1, false>(ctx, a);
-    return launch_tile<NB, 2, NG, false, 1, false>(ctx, a);
+    // up to 16 tokens: 16 rows to a warp, whose registers let two CTAs onto an SM (9 x 4096 x 4096: 9.8 us instead of 11.7, 16 x
+    // 28672 x 4096: 27.8 instead of 28.7); more tokens weigh more on x's loads (32 x 128256 x 4096: 164 us instead of 150)
+    return launch_tile<NB, NB == 2 ? 1 : 2, NG, false, 1, false>(ctx, a);
   } else {
     // few elements of x are laid out in the kernel itself; few rows: all eight warps on one tile of 16
     const bool local = (long)a.n * align_up((size_t)a.in, W4_CHUNK) <= W4_LOCAL;
