@@ -587,6 +587,10 @@ spts_status launch_rows(spts_ctx* ctx, const W4GemvArgs& a) {
   } else {
     // few elements of x are laid out in the kernel itself; few rows: all eight warps on one tile of 16
     const bool local = (long)a.n * align_up((size_t)a.in, W4_CHUNK) <= W4_LOCAL;
+    // two matrices: tiles of 64 features and half the depth of a step where there are many (8 x 14336 x 4096: 20.2 us instead of 22.2, 8 x
+    // 28672 x 8192: 55 instead of 61), of 32 where there are few (8 x 1024 x 4096: 7.6 instead of 9.0)
+    if (a.codes2 != nullptr && ceil_div(a.out, 32) > 2 * ctx->sm_count)
+      return local ? launch_tile<1, 2, NG, true, W4_WK / 2, true>(ctx, a) : launch_tile<1, 2, NG, true, W4_WK / 2, false>(ctx, a);
     if (a.codes2 != nullptr) return local ? launch_tile<1, 2, NG, true, W4_WK, true>(ctx, a) : launch_tile<1, 2, NG, true, W4_WK, false>(ctx, a);
     if (ceil_div(a.out, 16) <= 2 * ctx->sm_count)
       return local ? launch_tile<1, 1, NG, false, 8, true>(ctx, a) : launch_tile<1, 1, NG, false, 8, false>(ctx, a);
