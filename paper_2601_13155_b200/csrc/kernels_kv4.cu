@@ -1,9 +1,11 @@
 // The 4-bit KV cache: rows are quantised into it (kv4_append_kernel) and single tokens attend to it.
 //
-// kv4_attn_kernel (bf16): one persistent CTA per SM, its warps streaming 16-row steps of the cache through shared memory
-// into warp-level matrix instructions; see there.
-// kv4_attn_plain_kernel: one CTA per query head and sequence, CUDA cores, fp32 arithmetic, online softmax per warp.
-// fp32 storage and SPTS_REFERENCE_KERNELS.
+// kv4_attn_kernel (bf16): persistent CTAs, whose warps stream steps of 16 or 32 rows of the cache through shared memory into
+// warp-level matrix instructions; see there.
+// kv4_attn_plain_kernel: a cluster of up to eight CTAs per query head and sequence, CUDA cores, fp32 arithmetic, online softmax per
+// warp, the warps' and CTAs' results joined in their order.  Bound by the latency of a warp's steps (loads, sum over lanes,
+// exponential): 3 sequences of 1000 rows, 4 heads of 64 dims in fp32 6.4 us (one CTA per head, row by row, took 35); one of 32768
+// rows, 32 heads of 128 in bf16 336 us (the matrix kernel: 18).  fp32 storage and SPTS_REFERENCE_KERNELS.
 #include <cooperative_groups.h>
 
 #include "q4_common.cuh"
@@ -24,8 +26,8 @@ struct Kv4Dev {
 // One unit = one (row, KV head) of K or of V: D / 8 lanes, eight dims each, 256 / D units to a warp pass; quantised, its words
 // stored in the cache's order.  A warp takes up to `per` passes of one row (blockIdx.y: which, and of K or V), so that the row's
 // sequence is looked up once and the pointers only move.
-// Memory asks for 27 us at 24,600 rows of 8 heads x 128 (each element read once, codes, params and values written once); the
-// quantiser's instructions bound it instead.
+// 18,442 rows of 8 heads x 128 with their values read back take 65 us, where memory asks for 27 (each element read once, codes, params and
+// values written once): the quantiser's instructions (300 to a pass of 256 elements) bound it.  64 single rows: 4.8 us, two launches.
 template <typename T, int D, int LANES>
 __global__ void __launch_bounds__(256)
 kv4_append_kernel(Kv4Dev c, const T* __restrict__ K, int64_t ldk, const T* __restrict__ V, int64_t ldv,
@@ -242,9 +244,15 @@ kv4_attn_plain_kernel(Kv4Dev c, const T* __restrict__ Q, int64_t ldq, int H, T* 
 // after the first rows is rare, so the steps carry no reduction.
 //
 // Work split: the steps (one or two tiles) of all (sequence, KV head) units form one line that is cut into equal pieces, one per CTA
-// (persistent, one per SM), and a CTA deals its steps to its warps.  A unit that lies in one CTA is finished there; a unit
-// cut between CTAs leaves one partial result (maximum, sum, O) per CTA, and the CTA that arrives last adds them in the
-// order of the CTAs, so results do not depend on the order of arrival.  One launch, lengths read on the device.
+// (persistent), and a CTA deals its steps to its warps.  On the line a unit has its steps and, behind them, a fixed number that stands
+// for its beginning (queries) and end (the warps meet); without it the CTAs with many short units came last.  A unit that lies in
+// one CTA is finished there; a unit cut between CTAs leaves one partial result (maximum, sum, O) per CTA, and the CTA that arrives
+// last adds them in the order of the CTAs, so results do not depend on the order of arrival.  One launch, lengths read on the device.
+//
+// Measured: one sequence of 131072 rows, 8 KV heads x 128 in groups of 32: 42 us, 4.0 TB/s of codes and params; 48 ragged sequences
+// of up to 16384 rows, 4 KV heads: 52 us, 3.6 TB/s; one of 777 rows 9.1 us.  Issue slots are half full (300 instructions per 16
+// rows, two warps per scheduler, ALU pipe 43 %, matrix pipe 29 %); four row tiles a step, twelve warps, two or four stages and
+// products in other orders changed nothing, leaving the loads out neither.
 constexpr int KV4_EXTRA = 32;           // a unit's fixed cost in steps (48 ragged sequences of up to 16384 rows: none 74 us, 8 69, 20 55, 32 52)
 constexpr float KV4_LOG2E = 1.4426950408889634f;
 constexpr float KV4_SLACK = 6.0f;       // weights stay below 2^6 ...

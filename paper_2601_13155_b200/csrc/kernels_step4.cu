@@ -1,6 +1,7 @@
 // What a decode step with 4-bit weights and caches needs besides its products, its attention and the rules on its logits:
 // the tokens' embedding rows, and the rotation of q and k between the q / k / v projection and the cache.  Both are a few
-// kilobytes of work between larger kernels (a launch's latency each).
+// kilobytes of work between larger kernels, a launch's latency each: 4.5 and 2.9 us for 1 to 8 tokens of 4096 features, 32 + 2 x 8 heads
+// (serialised, cold).
 #include "spts_common.cuh"
 
 namespace spts {

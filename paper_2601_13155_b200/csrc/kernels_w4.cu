@@ -3,7 +3,8 @@
 //
 // w4_gemv_kernel (bf16): matrix instructions on the codes; see there.
 // w4_gemv_plain_kernel: one warp per output feature, CUDA cores, fp32 arithmetic; a lane takes eight codes (one word)
-// per step.  fp32 storage and SPTS_REFERENCE_KERNELS.
+// per step.  Bound by its instructions (five for every code): one token, 14336 x 4096: 35 us (the matrix kernel: 11).  fp32
+// storage and SPTS_REFERENCE_KERNELS.
 #include "q4_common.cuh"
 
 namespace spts {
@@ -12,6 +13,8 @@ namespace {
 
 using namespace q4;
 
+// Eight elements to a lane, a group to LANES neighbouring lanes (quantize8).  14336 x 4096 in bf16: 74 us, 2.0 TB/s,
+// bound by its instructions.
 template <typename T, int LANES>
 __global__ void __launch_bounds__(256)
 w4_quantize_kernel(const T* __restrict__ W, long n_words, uint32_t* __restrict__ codes,
@@ -132,6 +135,12 @@ spts_status launch_plain(spts_ctx* ctx, const W4GemvArgs& a) {
 // cut between CTAs each leaves its share, and w4_join_kernel adds them in the order of the CTAs.  (The CTA that arrives last
 // added them at first: one CTA's loads for 21 tokens x 256 rows x 21 shares took 50 us.)  Every warp's ring of asynchronous
 // copies runs on across tiles.
+//
+// Measured: 1 x 128256 x 4096 54 us, 5.1 TB/s of codes and params (a copy's rate asks for 46; deeper rings and three CTAs to an SM were
+// slower); 1 x 4096 x 4096 6.3 us (launch, x, one ring's latency); two matrices 8 x 14336 x 4096 20 us, of which x's layout about
+// 4 and the join 3; 21 x 3584 x 18944 in groups of 32 29 us (the same two launches 4 + 4; the product at two warps per
+// scheduler, 800 instructions to 32 rows x 256 features, matrix pipe 37 %).  L1 prefetches of x, three or four stages and two
+// CTAs of 128 registers made the last one 2 to 8 % slower.
 constexpr int W4_WARPS = 8;
 // 256 features: a row's codes of a chunk are one line of 128 bytes, its params 8 to 32 bytes.  (With chunks of 128 the copies
 // spend twice as many line accesses per byte, and the loop's own instructions weigh twice as much.)
@@ -513,7 +522,7 @@ w4_join_kernel(int out, int n, W4Line line, const float* __restrict__ part, cons
     v += __ldcg(p + 2 * c * share);
     if (TWO) v2 += __ldcg(p + 2 * c * share + 16);
   }
-  const float f = __ldg(factor + t);
+  const float f = __ldcg(factor + t);
   v *= CODE_UNIT_INV;
   v2 *= CODE_UNIT_INV;
   w4_store<bf16>(o, t, row, TWO ? silu_mul(v * f, v2 * f) : v * f);

@@ -70,12 +70,16 @@ def half_step(dtype):
 def gemv(x, w, dtype, norm=False, w2=None, residual=None, fp32_out=False, eps=1e-5):
     """y [n, out] in 64 bits and the bound on its error.
 
-    The kernels hold sums in fp32.  A product of the matrix path is (16 + code) * x, at most 31 |x|, and 24 times the sum
-    of x is taken off per group, so all partial sums of an output stay below A = sum (56 scale + |mid|) |x|.  Roundings
+    The kernels hold sums in fp32.  A product of the matrix path is code * x, at most 15 |x| (codes are exact, x is exact in
+    fp16 after a power of two down to 2^-30 of the token's largest element), and 8 times the sum of x is taken off per group, so
+    all partial sums of an output stay below sum (23 scale + |mid|) |x|; A = sum (56 scale + |mid|) |x| is taken.  Roundings
     follow one another at most r = 8 (matrix steps of a group) + in / group (groups) + 24 (lanes, warps, epilogue) times,
-    each off by at most 2^-23 of A (matrix units may truncate): r 2^-23 A.  The CUDA-core form has in / 256 lane steps of
-    eight terms each of size below A / steps, covered by the same bound with r' = 8 in / 256 < r.  The row norm is a sum of
-    squares of positive terms in fp32: relative error below (in / 32 + 16) 2^-24 / 2 + 2^-22."""
+    each off by at most 2^-23 of A (matrix units may truncate): r 2^-23 A.  For outputs in the storage type -8 sum x and
+    sum x are held in two bf16 pieces, off by 2^-17: (8 scale + |mid|) 2^-17 sum |x| more, which the part of A between 23 and
+    56 covers while |mid| <= 9 scale (r >= 33, and 33 * 33 scale 2^-23 >= 17 scale 2^-17); for fp32 outputs in three (2^-26).
+    The CUDA-core form has in / 256 lane steps of eight terms each of size below A / steps, covered by the same bound with
+    r' = 8 in / 256 < r.  The row norm is a sum of squares of positive terms in fp32: relative error below
+    (in / 32 + 16) 2^-24 / 2 + 2^-22."""
     def one(w):
         v, s, m = values(w.codes, w.params)
         y = x @ v.T
@@ -108,12 +112,13 @@ def gemv(x, w, dtype, norm=False, w2=None, residual=None, fp32_out=False, eps=1e
 def attention(q, k_codes, k_params, v_codes, v_params, length, dtype):
     """O [H, d] in 64 bits for one sequence (codes [Hkv, capacity, d / 2]) and the bound on its error.
 
-    bf16: the weight p * scale of a row is rounded to bf16 (half a step, 2^-8 relative) before it meets the code, and p and
-    mid are rounded to bf16 for the mid term (mid exactly representable or off by half a step): 2^-8 sum p scale |code| +
-    2 * 2^-8 sum p |mid|.  The 16 of the code's bias and its removal leave 2^-23 per step of sum p scale 56, steps = rows / 16 / 8 + 40.
-    Scores: the bias and mid terms 24 scale |sum q| and |mid| |sum q| go through two bf16 pieces of the sum of q (2^-16
-    relative), the rest through fp32 steps; an error of e in a score moves every weight by a factor within exp(+-2 e), which
-    moves an output by at most 2.2 e sum p |v|.  fp32 storage: only the fp32 steps."""
+    bf16: the weight p * scale of a row is rounded once, to fp16 (2^-11 relative; the bound takes bf16's 2^-8), before it meets
+    the code, and the -8 multiplies the same rounded weight; p and mid are rounded to bf16 for the mid term (mid exactly
+    representable or off by half a step): 2^-8 sum p scale |code| + 2 * 2^-8 sum p |mid|.  The fp32 sums leave 2^-23 per step
+    of sum p scale 56 (codes up to 15 and 8 taken off), steps = rows / 16 / 8 + 40.
+    Scores: the -8 and mid terms 8 scale |sum q| and |mid| |sum q| go through two bf16 pieces of the sum of q (2^-17 relative;
+    the bound takes 2^-16 and 24), the rest through fp32 steps; an error of e in a score moves every weight by a factor within
+    exp(+-2 e), which moves an output by at most 2.2 e sum p |v|.  fp32 storage: only the fp32 steps."""
     h, d = q.shape
     hkv = k_codes.shape[0]
     out, bound = np.zeros((h, d)), np.full((h, d), 1e-30)
