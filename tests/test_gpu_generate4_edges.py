@@ -164,6 +164,48 @@ def test_attention_long_rows_of_shared_heads_cut_between_blocks():
         lib.close()
 
 
+@pytest.mark.parametrize("heads,kv_heads,dim,group,lens", [
+    (16, 1, 128, 32, "short"), (20, 1, 128, 64, "mixed"), (10, 1, 128, 128, "short"), (8, 1, 128, 32, "mixed"), (6, 2, 128, 64, "mixed"),
+    (4, 2, 128, 128, "short"), (16, 1, 64, 32, "mixed"), (12, 1, 64, 64, "short"), (5, 1, 64, 64, "mixed"), (2, 2, 64, 32, "equal"),
+])
+def test_attention_of_more_units_than_blocks(heads, kv_heads, dim, group, lens):
+    """340 sequences: of 0 to 40 rows, of which most units lie in one block; with a few of thousands, which are cut; and equal ones."""
+    shape = shape_of(heads, kv_heads, dim)
+    lib = context(shape)
+    rng = np.random.default_rng(heads)
+    n = [int(v) for v in rng.integers(0, 41, 340)]
+    if lens == "mixed":
+        for b, rows in ((0, 3000), (7, 1), (100, 2500), (101, 2111), (339, 1777)):
+            n[b] = rows
+    if lens == "equal":
+        n = [33] * 340
+    cache = random_cache(shape, 340, max(n), group, n, seed=1)
+    q = torch.randn(340, heads, dim, device="cuda", generator=gen(5)).to(lib.dtype)
+    out = Guarded((340, heads * dim), lib.dtype)
+    out.t.fill_(float("nan"))
+    lib.kv4_attention(cache, q, O_out=out.t)
+    for b in [0, 1, 2, 7, 50, 99, 100, 101, 102, 200, 338, 339]:
+        check_attention(lib, cache_of(cache, b, shape), q[b:b + 1], out.t[b:b + 1], n[b:b + 1])
+    assert bool(torch.isfinite(out.t).all()) and bool((out.t[[b for b in range(340) if n[b] == 0]] == 0).all())
+    assert torch.equal(lib.kv4_attention(cache, q), out.t)
+    assert out.intact() and lib.check_guards() == 0
+    lib.close()
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(32, 8, 128), (8, 1, 64), (28, 4, 128)])
+@pytest.mark.parametrize("lens", [[1], [31, 32, 33], [257, 0, 0, 1], [0, 0, 4000], [900, 900, 900], [5000, 1, 1, 1, 1, 1, 1, 1, 2000], [63] * 18, [1, 0, 2]])
+def test_attention_pieces_of_every_kind(heads, kv_heads, dim, lens):
+    """Cuts at units' borders, inside a unit's fixed cost, one step before the end, and units of one step."""
+    shape = shape_of(heads, kv_heads, dim)
+    lib = context(shape)
+    cache = random_cache(shape, len(lens), max(lens), 32, lens, seed=len(lens))
+    q = torch.randn(len(lens), heads, dim, device="cuda", generator=gen(5)).to(lib.dtype)
+    out = lib.kv4_attention(cache, q)
+    check_attention(lib, cache, q, out, lens)
+    assert torch.equal(out, lib.kv4_attention(cache, q))
+    lib.close()
+
+
 # ---------------------------------------------------------------------------------------------- rules on logits
 @pytest.mark.parametrize("n,vocab", [(2100, 53), (1025, 1000)])
 def test_logits_of_many_rows(n, vocab):
