@@ -26,10 +26,11 @@ struct Kv4Dev {
 // One unit = one (row, KV head) of K or of V: D / 8 lanes, eight dims each, 256 / D units to a warp pass; quantised, its words
 // stored in the cache's order.  A warp takes up to `per` passes of one row (blockIdx.y: which, and of K or V), so that the row's
 // sequence is looked up once and the pointers only move.
-// 18,442 rows of 8 heads x 128 with their values read back take 65 us, where memory asks for 27 (each element read once, codes, params and
-// values written once): the quantiser's instructions (300 to a pass of 256 elements) bound it.  64 single rows: 4.8 us, two launches.
+// 18,442 rows of 8 heads x 128 with their values read back take 60 us, where memory asks for 27 (each element read once, codes,
+// params and values written once): the quantiser's instructions (300 to a pass of 256 elements) bound it, at four blocks to an SM
+// (three 65 us, five 67).  64 single rows: 4.8 us, two launches.
 template <typename T, int D, int LANES>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 4)
 kv4_append_kernel(Kv4Dev c, const T* __restrict__ K, int64_t ldk, const T* __restrict__ V, int64_t ldv,
                   const int32_t* __restrict__ pos, const int32_t* __restrict__ row_start, const int32_t* __restrict__ at,
                   int n_rows, int per, T* __restrict__ K_read, T* __restrict__ V_read, int* status) {

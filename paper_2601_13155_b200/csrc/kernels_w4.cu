@@ -13,10 +13,10 @@ namespace {
 
 using namespace q4;
 
-// Eight elements to a lane, a group to LANES neighbouring lanes (quantize8).  14336 x 4096 in bf16: 74 us, 2.0 TB/s,
-// bound by its instructions.
+// Eight elements to a lane, a group to LANES neighbouring lanes (quantize8).  14336 x 4096 in bf16: 72 us, 2.0 TB/s,
+// bound by its instructions, at six blocks to an SM (five 76, four 78).
 template <typename T, int LANES>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 6)
 w4_quantize_kernel(const T* __restrict__ W, long n_words, uint32_t* __restrict__ codes,
                    uint32_t* __restrict__ params, int* status) {
   const long i0 = (long)blockIdx.x * 256 + threadIdx.x, stride = (long)gridDim.x * 256;
@@ -136,9 +136,9 @@ spts_status launch_plain(spts_ctx* ctx, const W4GemvArgs& a) {
 // added them at first: one CTA's loads for 21 tokens x 256 rows x 21 shares took 50 us.)  Every warp's ring of asynchronous
 // copies runs on across tiles.
 //
-// Measured: 1 x 128256 x 4096 54 us, 5.1 TB/s of codes and params (a copy's rate asks for 46; deeper rings and three CTAs to an SM were
-// slower); 1 x 4096 x 4096 6.3 us (launch, x, one ring's latency); two matrices 8 x 14336 x 4096 20 us, of which x's layout about
-// 4 and the join 3; 21 x 3584 x 18944 in groups of 32 29 us (the same two launches 4 + 4; the product at two warps per
+// Measured: 1 x 128256 x 4096 54 us, 5.5 TB/s of codes and params (a copy's rate asks for 46; deeper rings and three CTAs to an SM were
+// slower); 1 x 4096 x 4096 6.3 us (launch, x, one ring's latency); two matrices 8 x 14336 x 4096 20 us, of which x's layout
+// about 4; 21 x 3584 x 18944 in groups of 32 29 us (the same two launches 4 + 4; the product at two warps per
 // scheduler, 800 instructions to 32 rows x 256 features, matrix pipe 37 %).  L1 prefetches of x, three or four stages and two
 // CTAs of 128 registers made the last one 2 to 8 % slower.
 constexpr int W4_WARPS = 8;
