@@ -171,12 +171,28 @@ __device__ __forceinline__ void w4_prepare(const bf16* __restrict__ x, int token
   const int tid = threadIdx.x, lane = tid & 31;
   float top = 0.f, ss = 0.f;
   const int there = x != nullptr ? in : 0;
-#pragma unroll 4
-  for (int k = 8 * tid; k < there; k += 8 * THREADS) {
+  // a warp takes a chunk at a time, lane 4 t + c, and keeps its first ones between the two passes
+  constexpr int KEEP = THREADS == 1024 ? 2 : 4;
+  const int k0 = (tid >> 5) * W4_CHUNK + L::k(lane >> 2, lane & 3);
+  Raw8<bf16> kept[KEEP];
+#pragma unroll
+  for (int i = 0; i < KEEP; ++i) {
+    kept[i].zero();
+    if (k0 + i * WARPS * W4_CHUNK < there) kept[i].load(x + k0 + i * WARPS * W4_CHUNK);
+  }
+  const auto look = [&](const Raw8<bf16>& raw) {
     float v[8];
-    load8(x + k, v);
+    raw.get(v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) { top = fmaxf(top, fabsf(v[i])); ss = fmaf(v[i], v[i], ss); }
+  };
+#pragma unroll
+  for (int i = 0; i < KEEP; ++i)
+    if ((tid >> 5) * W4_CHUNK + i * WARPS * W4_CHUNK < there) look(kept[i]);
+  for (int k = k0 + KEEP * WARPS * W4_CHUNK; k < there; k += WARPS * W4_CHUNK) {
+    Raw8<bf16> raw;
+    raw.load(x + k);
+    look(raw);
   }
   top = warp_max(top);
   ss = warp_sum(ss);
@@ -189,17 +205,14 @@ __device__ __forceinline__ void w4_prepare(const bf16* __restrict__ x, int token
   const float xs = scale_to_2_13(top), xo = xs * ODD, u = xs * CODE_UNIT;
   if (tid == 0) factor[token] = (norm ? 1.0f / sqrtf(ss / (float)in + eps) : 1.0f) / xs;
   const int chunks = (in + W4_CHUNK - 1) / W4_CHUNK;
-  // a warp lays out a chunk at a time: lane 4 t + c
-#pragma unroll 2
-  for (int chunk = tid >> 5; chunk < chunks; chunk += WARPS) {
-    const int k = chunk * W4_CHUNK + L::k(lane >> 2, lane & 3);
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (k < there) load8(x + k, v);
+  const auto lay = [&](int chunk, const Raw8<bf16>& raw) {
+    float v[8];
+    raw.get(v);
     float s = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
     unsigned char* block = blocks + chunk * stride + (size_t)token * next;
     const auto at = [&](int i) { return reinterpret_cast<uint4*>(block + (size_t)(i >> 2) * row + 16 * (i & 3)); };
     *at(lane) = make_uint4(pack2_f16(v[0] * xs, v[4] * xs), pack2_f16(v[1] * xo, v[5] * xo), pack2_f16(v[2] * xs, v[6] * xs),
-                             pack2_f16(v[3] * xo, v[7] * xo));
+                           pack2_f16(v[3] * xo, v[7] * xo));
 #pragma unroll
     for (int o = 1; o < L::LANES; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     if (lane % L::LANES == 0) {
@@ -208,6 +221,16 @@ __device__ __forceinline__ void w4_prepare(const bf16* __restrict__ x, int token
       *at(32 + lane / L::LANES) = make_uint4(pack2(ah, mh), pack2(am, mm), pack2((a - ah) - am, (sm - mh) - mm), 0u);
     }
     if (lane < L::SUMS - NG) *at(32 + NG + lane) = make_uint4(0u, 0u, 0u, 0u);
+  };
+#pragma unroll
+  for (int i = 0; i < KEEP; ++i)
+    if ((tid >> 5) + i * WARPS < chunks) lay((tid >> 5) + i * WARPS, kept[i]);
+  for (int chunk = (tid >> 5) + KEEP * WARPS; chunk < chunks; chunk += WARPS) {
+    Raw8<bf16> raw;
+    raw.zero();
+    const int k = chunk * W4_CHUNK + L::k(lane >> 2, lane & 3);
+    if (k < there) raw.load(x + k);
+    lay(chunk, raw);
   }
 }
 template <int NG>
