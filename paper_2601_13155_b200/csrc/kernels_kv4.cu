@@ -168,7 +168,7 @@ kv4_attn_plain_kernel(Kv4Dev c, const T* __restrict__ Q, int64_t ldq, int H, T* 
       s[i] = 0.f;
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        s[i] = fmaf(q[e], fmaf(lo_bf16(kp[i][e]), (float)((int)((kw[i] >> (4 * e)) & 15) - 8), hi_bf16(kp[i][e])), s[i]);
+        s[i] = fmaf(q[e], fmaf(lo_bf16(kp[i][e]), code_less_8(kw[i], e), hi_bf16(kp[i][e])), s[i]);
     }
 #pragma unroll
     for (int i = 0; i < PLAIN_ROWS; ++i) {
@@ -190,7 +190,7 @@ kv4_attn_plain_kernel(Kv4Dev c, const T* __restrict__ Q, int64_t ldq, int H, T* 
 #pragma unroll
       for (int i = 0; i < PLAIN_ROWS; ++i)
         if (j + i < len)
-          o[e] = fmaf(pr[i], fmaf(lo_bf16(vp[i][e]), (float)((int)((vw[i] >> (4 * e)) & 15) - 8), hi_bf16(vp[i][e])), o[e]);
+          o[e] = fmaf(pr[i], fmaf(lo_bf16(vp[i][e]), code_less_8(vw[i], e), hi_bf16(vp[i][e])), o[e]);
     }
     m = mn;
   }

@@ -2,9 +2,9 @@
 // quantiser that fills them.
 //
 // w4_gemv_kernel (bf16): matrix instructions on the codes; see there.
-// w4_gemv_plain_kernel: one warp per output feature, CUDA cores, fp32 arithmetic; a lane takes eight codes (one word)
-// per step.  Bound by its instructions (five for every code): one token, 14336 x 4096: 35 us (the matrix kernel: 11).  fp32
-// storage and SPTS_REFERENCE_KERNELS.
+// w4_gemv_plain_kernel: one or two output features per warp, CUDA cores, fp32 arithmetic; a lane takes eight codes (one word)
+// per step.  Bound by its instructions (five for every code) and the latency of its loads: one token, 14336 x 4096: 28 us (the matrix
+// kernel: 11).  fp32 storage and SPTS_REFERENCE_KERNELS.
 #include "q4_common.cuh"
 
 namespace spts {
@@ -52,32 +52,51 @@ __device__ __forceinline__ void w4_store(const W4Out& o, int t, int row, float y
 }
 __device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.0f + expf(-g)) * u; }
 
-template <typename T, int NT, bool TWO>
+// R features to a warp, which share its loads of x, and up to NT tokens, which share the decoded weights
+template <typename T, int NT, bool TWO, int R>
 __global__ void __launch_bounds__(256)
 w4_gemv_plain_kernel(const uint32_t* __restrict__ codes, const uint32_t* __restrict__ params,
                      const uint32_t* __restrict__ codes2, const uint32_t* __restrict__ params2, int out, int in, int group,
                      const T* __restrict__ X, int64_t ldx, int n, int norm, float eps, W4Out o) {
-  const int row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (row >= out) return;
+  constexpr int M = TWO ? 2 : 1;
+  const int row0 = (blockIdx.x * 8 + (threadIdx.x >> 5)) * R, lane = threadIdx.x & 31;
+  if (row0 >= out) return;
   const int t0 = blockIdx.y * NT;
-  const int words = in / 8, per_group = group / 8;
-  float acc[NT], acc2[NT], ss[NT];
+  const int words = in / 8, groups = in / group, shift = group == 32 ? 2 : group == 64 ? 3 : 4;       // words to a group
+  float acc[R][M][NT], ss[NT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) { acc[t] = 0.f; acc2[t] = 0.f; ss[t] = 0.f; }
+  for (int t = 0; t < NT; ++t) {
+    ss[t] = 0.f;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int m = 0; m < M; ++m) acc[r][m][t] = 0.f;
+  }
   for (int w = lane; w < words; w += 32) {
-    const uint32_t c = codes[(size_t)row * words + w], p = params[(size_t)row * (words / per_group) + w / per_group];
-    uint32_t c2 = 0, p2 = 0;
-    if (TWO) { c2 = codes2[(size_t)row * words + w]; p2 = params2[(size_t)row * (words / per_group) + w / per_group]; }
+    float v[R][M][8];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int m = 0; m < M; ++m) {
+        const size_t row = min(row0 + r, out - 1);
+        const uint32_t c = (m == 0 ? codes : codes2)[row * words + w], p = (m == 0 ? params : params2)[row * groups + (w >> shift)];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[r][m][i] = fmaf(lo_bf16(p), code_less_8(c, i), hi_bf16(p));
+      }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       if (t0 + t < n) {
         float x[8];
         load8(X + (size_t)(t0 + t) * ldx + 8 * w, x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          acc[t] = fmaf(fmaf(lo_bf16(p), (float)((int)((c >> (4 * i)) & 15) - 8), hi_bf16(p)), x[i], acc[t]);
-          if (TWO) acc2[t] = fmaf(fmaf(lo_bf16(p2), (float)((int)((c2 >> (4 * i)) & 15) - 8), hi_bf16(p2)), x[i], acc2[t]);
-          ss[t] = fmaf(x[i], x[i], ss[t]);
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int m = 0; m < M; ++m)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[r][m][t] = fmaf(v[r][m][i], x[i], acc[r][m][t]);
+        if (norm) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) ss[t] = fmaf(x[i], x[i], ss[t]);
         }
       }
     }
@@ -85,33 +104,34 @@ w4_gemv_plain_kernel(const uint32_t* __restrict__ codes, const uint32_t* __restr
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     if (t0 + t < n) {
-      float y = warp_sum(acc[t]);
-      const float y2 = TWO ? warp_sum(acc2[t]) : 0.f;
-      const float s2 = warp_sum(ss[t]);
-      if (lane == 0) {
-        const float rs = norm ? 1.0f / sqrtf(s2 / (float)in + eps) : 1.0f;
-        y *= rs;
-        if (TWO) y = silu_mul(y, y2 * rs);
-        w4_store<T>(o, t0 + t, row, y);
+      const float s2 = norm ? warp_sum(ss[t]) : 0.f;
+      const float rs = norm ? 1.0f / sqrtf(s2 / (float)in + eps) : 1.0f;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        float y = warp_sum(acc[r][0][t]) * rs;
+        if (TWO) y = silu_mul(y, warp_sum(acc[r][M - 1][t]) * rs);
+        if (lane == 0 && row0 + r < out) w4_store<T>(o, t0 + t, row0 + r, y);
       }
     }
   }
 }
 
-template <typename T, int NT>
-spts_status launch_plain(spts_ctx* ctx, const W4GemvArgs& a) {
+template <typename T, int NT, bool TWO, int R>
+spts_status launch_plain_rows(spts_ctx* ctx, const W4GemvArgs& a) {
   const W4Out o{a.residual, a.ldr, a.Y, a.ldy, a.fp32_out};
-  const dim3 grid(ceil_div(a.out, 8), ceil_div(a.n, NT));
-  const uint32_t* c1 = (const uint32_t*)a.codes; const uint32_t* p1 = (const uint32_t*)a.params;
-  const uint32_t* c2 = (const uint32_t*)a.codes2; const uint32_t* p2 = (const uint32_t*)a.params2;
-  if (c2 != nullptr)
-    w4_gemv_plain_kernel<T, NT, true><<<grid, 256, 0, ctx->stream>>>(c1, p1, c2, p2, a.out, a.in, a.group, (const T*)a.X, a.ldx, a.n,
-                                                                     a.norm, ctx->desc.rms_eps, o);
-  else
-    w4_gemv_plain_kernel<T, NT, false><<<grid, 256, 0, ctx->stream>>>(c1, p1, c2, p2, a.out, a.in, a.group, (const T*)a.X, a.ldx, a.n,
-                                                                      a.norm, ctx->desc.rms_eps, o);
+  w4_gemv_plain_kernel<T, NT, TWO, R><<<dim3(ceil_div(a.out, 8 * R), ceil_div(a.n, NT)), 256, 0, ctx->stream>>>(
+      (const uint32_t*)a.codes, (const uint32_t*)a.params, (const uint32_t*)a.codes2, (const uint32_t*)a.params2, a.out, a.in, a.group,
+      (const T*)a.X, a.ldx, a.n, a.norm, ctx->desc.rms_eps, o);
   SPTS_CUDA_OK(ctx);
   return SPTS_OK;
+}
+template <typename T, int NT>
+spts_status launch_plain(spts_ctx* ctx, const W4GemvArgs& a) {
+  // four tokens: two features to a warp where that leaves a block for every SM (fp32, 4 x 8192 x 4096: 26 us, one feature 42)
+  if constexpr (NT > 1)
+    if (ceil_div(a.out, 16) >= ctx->sm_count)
+      return a.codes2 != nullptr ? launch_plain_rows<T, NT, true, 2>(ctx, a) : launch_plain_rows<T, NT, false, 2>(ctx, a);
+  return a.codes2 != nullptr ? launch_plain_rows<T, NT, true, 1>(ctx, a) : launch_plain_rows<T, NT, false, 1>(ctx, a);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------

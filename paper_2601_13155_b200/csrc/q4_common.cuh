@@ -54,6 +54,11 @@ __device__ __forceinline__ void store8(bf16* p, const float* x) {
   *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// code i of a word, less 8, by a mask and an exact subtraction (a conversion instruction has a quarter of their rate)
+__device__ __forceinline__ float code_less_8(uint32_t w, int i) {
+  return __uint_as_float(((w >> (4 * i)) & 15u) | 0x4B000000u) - 8388616.f;
+}
+
 // ---- matrix instructions on codes
 // A nibble in the low mantissa bits of an fp16 whose other bits are zero IS a number: code * 2^-24 in bits 0..3 and
 // code * 2^-20 in bits 4..7 (subnormals, and exact; the matrix units take them as they are).  So the eight codes of a word
