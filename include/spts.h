@@ -386,7 +386,8 @@ spts_status spts_decode_step(spts_ctx* ctx, const spts_model_weights* mw, spts_k
  * its logits).
  *
  * A 4-bit group is 32, 64 or 128 elements that share a bf16 pair (scale, mid); a code c in 0..15 stands for
- *   scale * (c - 8) + mid.
+ *   scale * (c - 8) + mid
+ * with a scale of either sign (the quantisers here make none below zero).
  * Quantising a group x (all in 64 bits, every stored number rounded once to bf16):
  *   scale = bf16((max x - min x) / 15),  mid = bf16((max x + min x) / 2 + scale / 2),
  *   c = clamp(rint((x - mid) / scale) + 8, 0, 15), ties to even;  scale == 0: c = 8.

@@ -238,7 +238,7 @@ kv4_attn_plain_kernel(Kv4Dev c, const T* __restrict__ Q, int64_t ldq, int H, T* 
 // the query's largest element).  The second sum is one more matrix step, in bf16, whose A registers are the params words as
 // they lie in memory and whose B holds -8 sum q and sum q in two bf16 pieces each (off by 2^-17 relative).
 //   O = sum_rows c p'_g - 8 sum_rows p'_g + sum_rows p mid_g,   p'_g = fp16(p scale_g / r), p in the last sum bf16(p)
-// r is a power of two near the largest scale met, so p' uses fp16's eleven bits down to 2^-20 of the largest weight, and its
+// r is a power of two near the size of the largest scale met, so p' uses fp16's eleven bits down to 2^-20 of the largest weight, and its
 // absolute error below that is 2^-31; the -8 multiplies the rounded p' by a matrix step with a constant A, so it cancels up
 // to fp32 sums.  P changes from the accumulator's layout to the B operand's by 8 x 8 transposes between lanes.
 // The running maximum is a reference, not the maximum: it moves only when a score exceeds it by 2^6 (r likewise by 2), which
@@ -257,7 +257,7 @@ kv4_attn_plain_kernel(Kv4Dev c, const T* __restrict__ Q, int64_t ldq, int H, T* 
 constexpr int KV4_EXTRA = 32;           // a unit's fixed cost in steps (48 ragged sequences of up to 16384 rows: none 74 us, 8 69, 20 55, 32 52)
 constexpr float KV4_LOG2E = 1.4426950408889634f;
 constexpr float KV4_SLACK = 6.0f;       // weights stay below 2^6 ...
-constexpr float KV4_BOOST = 64.f;       // ... and meet the scale 2^6 higher: p' below 2^13, normal fp16 down to 2^-20 of the largest
+constexpr float KV4_BOOST = 64.f;       // ... and meet the scale, at most 4 r, 2^6 higher: p' below 2^14, normal fp16 down to 2^-20 of the largest
 
 // 2^x to two units in the last place (results below the normal range become zero)
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -616,10 +616,11 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
           for (int i = 0; i < 2; ++i) top[nb][i] = fmaxf(top[nb][i], fmaxf(sc[rt][nb][i], sc[rt][nb][2 + i]));
-      // the largest scale of V among the params words, ROWS NG / 32 to a lane
+      // the largest scale of V, by its size (a group may hold its values with a negative one), among the params words, ROWS NG / 32
+      // to a lane
 #pragma unroll
       for (int i = 0; i < (ROWS * NG + 31) / 32; ++i)
-        if (ROWS * NG % 32 == 0 || lane < ROWS * NG) top_s = fmaxf(top_s, lo_bf16(reinterpret_cast<const uint32_t*>(st + T::VP)[32 * i + lane]));
+        if (ROWS * NG % 32 == 0 || lane < ROWS * NG) top_s = fmaxf(top_s, fabsf(lo_bf16(reinterpret_cast<const uint32_t*>(st + T::VP)[32 * i + lane])));
       bool over = top_s > r_lim;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) over = over || top[nb][0] > thr[nb][0] || top[nb][1] > thr[nb][1];

@@ -1,0 +1,71 @@
+"""What a caller of the 4-bit generation operators may do beside the plain calls: options, refused arguments, streams of their
+own, scales of either sign, caches of a skipping prefill; and bounds that see a lost rounding piece."""
+import ctypes as C
+from dataclasses import replace
+
+import numpy as np
+import pytest
+import torch
+
+import generate4_ref as R
+from paper_2601_13155_b200 import synth
+from parity_utils import dev, host, i32, rel_rms_err, up
+from test_gpu_decode4 import WIDE, build, reference_layer
+from test_gpu_generate4 import check_attention, close, context, fill_garbage, gen, rand_w4, random_cache, random_rules, shape_of
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------------------------------------- scales of either sign
+@pytest.mark.parametrize("plain", [False, True])
+@pytest.mark.parametrize("heads,kv_heads,dim,group", [(8, 2, 128, 32), (24, 2, 128, 128), (4, 2, 64, 32)])
+@pytest.mark.parametrize("sign", ["negative", "mixed"])
+def test_attention_with_negative_scales(heads, kv_heads, dim, group, sign, plain):
+    """A group may hold its values with a negative scale (a cache made elsewhere).  Bound: R.attention's, whose terms are absolute
+    values of scale times code; it takes the scales' absolute values with the codes mirrored, which are the same values:
+    s (c - 8) + m = |s| (8 - c) + m, where 8 - c may be 8, one more than its formula's |code| of at most 8."""
+    shape = shape_of(heads, kv_heads, dim)
+    lib = context(shape)
+    if plain:
+        lib.set_reference_kernels(True)
+    lens = [700, 3, 0, 64]
+    cache = random_cache(shape, 4, 704, group, lens, seed=7)
+    for t in (cache.k_params, cache.v_params):
+        flip = -1.0 if sign == "negative" else torch.where(torch.rand(t.shape[:-1], device="cuda", generator=gen(8)) < 0.5, -1.0, 1.0)
+        t[..., 0] = t[..., 0] * flip
+    large = 2.0 ** 17 if sign == "negative" else torch.where(cache.v_params[..., 0] < 0, 2.0 ** 17, 1.0)
+    cache.v_params[..., 0] = cache.v_params[..., 0] * large
+    q = torch.randn(4, heads, dim, device="cuda", generator=gen(5)).to(lib.dtype)
+    out = lib.kv4_attention(cache, q).reshape(4, heads, dim)
+    for b, n in enumerate(lens):
+        if n == 0:
+            assert not out[b].any()
+            continue
+        want, bound = signed_attention(R.f64(q[b]), cache, b, n)
+        close(out[b], want, bound, f"sequence {b}")
+    lib.close()
+
+
+def signed_attention(q, cache, b, length):
+    """R.attention's result and bound (bf16) with the absolute values of the scales in the bound."""
+    h, d = q.shape
+    hkv = cache.k_codes.shape[1]
+    out, bound = np.zeros((h, d)), np.zeros((h, d))
+    half = R.half_step(torch.bfloat16)
+    for kv in range(hkv):
+        k, _, ks, km = R.cache_rows(cache.k_codes[b, kv, :length], cache.k_params[b, kv, :length], R.key_dims(d))
+        v, vc, vs, vm = R.cache_rows(cache.v_codes[b, kv, :length], cache.v_params[b, kv, :length], R.value_dims(d))
+        ks, vs = np.abs(ks), np.abs(vs)
+        g = slice(kv * (h // hkv), (kv + 1) * (h // hkv))
+        s = q[g] @ k.T / np.sqrt(d)
+        es = (d / 16 + 24) * 2.0 ** -23 * (np.abs(q[g]) @ (56 * ks + np.abs(km)).T) / np.sqrt(d)
+        es = es + 2.0 ** -16 * (np.abs(q[g]) @ (24 * ks + np.abs(km)).T) / np.sqrt(d)
+        es = es + 2.0 ** -22 * (np.abs(s) + np.abs(s).max(1, keepdims=True) + 16)
+        p = np.exp(s - s.max(1, keepdims=True))
+        p /= p.sum(1, keepdims=True)
+        e = (length / 128 + 40) * 2.0 ** -23 * (p @ (56 * vs + np.abs(vm)))
+        e = e + half * (p @ (vs * np.abs(vc))) + 2 * half * (p @ np.abs(vm))
+        e = e + 2.2 * np.minimum(es.max(1, keepdims=True), 0.05) * (p @ np.abs(v))
+        out[g] = p @ v
+        bound[g] = e * (1 + half) + half * np.abs(out[g]) + 1e-30
+    return out, bound
