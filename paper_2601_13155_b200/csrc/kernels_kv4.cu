@@ -237,7 +237,9 @@ kv4_attn_plain_kernel(Kv4Dev c, const T* __restrict__ Q, int64_t ldq, int H, T* 
 // q is brought to fp16 by a power of two per query (exact: bf16 has fewer bits, and what falls below fp16's range is 2^-35 of
 // the query's largest element).  The second sum is one more matrix step, in bf16, whose A registers are the params words as
 // they lie in memory and whose B holds -8 sum q and sum q in two bf16 pieces each (off by 2^-17 relative).
-//   O = sum_rows c p'_g - 8 sum_rows p'_g + sum_rows p mid_g,   p'_g = fp16(p scale_g / r), p in the last sum bf16(p)
+//   O = sum_rows c p'_g - 8 sum_rows p'_g + sum_rows p mid_g,   p'_g = fp16(p scale_g / r), p in the last sum in two bf16 pieces
+// (2^-17: mids may be far larger than scales, and the sum of the weights that divides O is that of the unrounded ones; with one
+// piece a constant V came back off by up to 2^-8)
 // r is a power of two near the size of the largest scale met, so p' uses fp16's eleven bits down to 2^-20 of the largest weight, and its
 // absolute error below that is 2^-31; the -8 multiplies the rounded p' by a matrix step with a constant A, so it cancels up
 // to fp32 sums.  P changes from the accumulator's layout to the B operand's by 8 x 8 transposes between lanes.
@@ -662,7 +664,11 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
         uint32_t vp0[NG], vp1[NG];
         load_words<NG>(st + T::VP + (16 * rt + g) * NG * 4, vp0);
         load_words<NG>(st + T::VP + (16 * rt + g + 8) * NG * 4, vp1);
-        uint32_t pb[NB][NG][2], pu[NB][2];
+        // mids: A row r holds group r % NG
+        const uint32_t* vm = reinterpret_cast<const uint32_t*>(st + T::VP) + 16 * rt * NG + (g % NG);
+        const uint32_t m0 = __byte_perm(vm[2 * cc * NG], vm[(2 * cc + 1) * NG], 0x7632);
+        const uint32_t m2 = __byte_perm(vm[(2 * cc + 8) * NG], vm[(2 * cc + 9) * NG], 0x7632);
+        uint32_t pb[NB][NG][2];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           float p[4];
@@ -670,8 +676,12 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
           for (int i = 0; i < 4; ++i) p[i] = exp2_fast(fmaf(sc[rt][nb][i], slq[nb][i & 1], -msl[nb][i & 1]));
           l[nb][0] += p[0] + p[2];
           l[nb][1] += p[1] + p[3];
-          pu[nb][0] = transpose8x8(pack2(p[0], p[1]));
-          pu[nb][1] = transpose8x8(pack2(p[2], p[3]));
+          {
+            const uint32_t h0 = pack2(p[0], p[1]), h1 = pack2(p[2], p[3]);
+            mma16816(om[nb], m0, 0u, m2, 0u, transpose8x8(h0), transpose8x8(h1));
+            mma16816(om[nb], m0, 0u, m2, 0u, transpose8x8(pack2(p[0] - lo_bf16(h0), p[1] - hi_bf16(h0))),
+                     transpose8x8(pack2(p[2] - lo_bf16(h1), p[3] - hi_bf16(h1))));
+          }
 #pragma unroll
           for (int i = 0; i < 4; ++i) p[i] *= r_inv;
 #pragma unroll
@@ -680,14 +690,6 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
             pb[nb][gr][0] = transpose8x8(pack2_f16(p[0] * s0, p[1] * s0));
             pb[nb][gr][1] = transpose8x8(pack2_f16(p[2] * s1, p[3] * s1));
           }
-        }
-        {
-          // mids: A row r holds group r % NG
-          const uint32_t* vm = reinterpret_cast<const uint32_t*>(st + T::VP) + 16 * rt * NG + (g % NG);
-          const uint32_t a0 = __byte_perm(vm[2 * cc * NG], vm[(2 * cc + 1) * NG], 0x7632);
-          const uint32_t a2 = __byte_perm(vm[(2 * cc + 8) * NG], vm[(2 * cc + 9) * NG], 0x7632);
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) mma16816(om[nb], a0, 0u, a2, 0u, pu[nb][0], pu[nb][1]);
         }
         uint32_t vw[4][NT / 2];
 #pragma unroll

@@ -69,3 +69,34 @@ def signed_attention(q, cache, b, length):
         out[g] = p @ v
         bound[g] = e * (1 + half) + half * np.abs(out[g]) + 1e-30
     return out, bound
+
+
+# ---------------------------------------------------------------------------------------------- bounds that see a lost piece
+@pytest.mark.parametrize("dim,group,heads", [(128, 32, 8), (128, 128, 32), (64, 64, 8)])
+@pytest.mark.parametrize("weight", [1.0 + 2.0 ** -8 * 0.97, 1.0 + 2.0 ** -8 * 1.03, 2.0 + 2.0 ** -7 * 0.97])
+def test_attention_of_a_constant_under_weights_that_bf16_cannot_hold(dim, group, heads, weight):
+    """Values that are one constant come back as it: the softmax's weights sum to one, whatever they are.  The scores of the first
+    rows are lower than those of the rest by the logarithm of `weight`, which lies next to the middle between two bf16 numbers, so
+    weights rounded to bf16 on one side of the division only would move the output by up to 2^-8.
+    Bound: the weights of the mids are held to 2^-17 relative, the sums of a unit's 1280 rows in fp32 (2^-23 a step, 50 steps), the
+    division and the exponentials cancel: 2^-17 + 2^-17; and half a step of the output."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    shape = shape_of(heads, 2, dim)
+    lib = context(shape)
+    n, rows, first = sms, 1280, 128                                  # as many units as resident blocks; four warps' first steps
+    from paper_2601_13155_b200 import binding
+    cache = binding.Kv4Cache(shape, n, rows, group=group)
+    for t in (cache.k_codes, cache.v_codes):
+        t.fill_(0x88)                                                # code 8 stands for the mid
+    cache.k_params.zero_()
+    cache.k_params[:, :, first:, :, 1] = float(np.log(weight) / np.sqrt(dim))       # q = 1: score = sqrt(d) mid
+    const = 61.0
+    cache.v_params[..., 0] = 2.0 ** -6
+    cache.v_params[..., 1] = const
+    cache.length.fill_(rows)
+    q = torch.ones(n, heads, dim, dtype=torch.bfloat16, device="cuda")
+    out = lib.kv4_attention(cache, q)
+    # 61 lies between 32 and 64: half a step is 2^-3
+    assert float((out.double() - const).abs().max()) <= 2.0 ** -3 * 0.999
+    assert bool((out == const).all())                                # 61 is a bf16 number, and 2^-16 * 61 is less than half a step
+    lib.close()
