@@ -179,7 +179,10 @@ spts_status spts_create(const spts_model_desc* desc, int max_seq, void* workspac
 void spts_destroy(spts_ctx* ctx);
 
 /* Sets SPTS_REFERENCE_KERNELS, SPTS_FFN_SCORE_PAP_ONLY or SPTS_DEBUG_CHECKS on/off
- * (value 0/1), or SPTS_PAP_WINDOW (value 1..64). */
+ * (value 0/1), or SPTS_PAP_WINDOW (value 1..64).  A context whose shape or storage type has no
+ * tensor-core kernels for the prefill runs it on the plain ones whatever the option says and
+ * answers value 0 with SPTS_ERR_UNSUPPORTED; in bf16 SPTS_REFERENCE_KERNELS still selects the
+ * kernels of its 4-bit calls, and value 0 after 1 takes that back with SPTS_OK. */
 spts_status spts_set_option(spts_ctx* ctx, uint32_t option, int value);
 
 /* Synchronises the context's stream and returns the device status word (then clears it). */

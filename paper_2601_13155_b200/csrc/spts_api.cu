@@ -663,8 +663,10 @@ spts_status spts_profile_end(spts_ctx* ctx, float* ms, int64_t* calls, double* f
 spts_status spts_set_option(spts_ctx* ctx, uint32_t option, int value) {
   TRY(check_ctx(ctx));
   if (option == SPTS_REFERENCE_KERNELS) {
-    if (ctx->desc.dtype == SPTS_FP32 || !tc_shape_ok(ctx->desc)) return value ? SPTS_OK : SPTS_ERR_UNSUPPORTED;
+    if (ctx->desc.dtype == SPTS_FP32) return value ? SPTS_OK : SPTS_ERR_UNSUPPORTED;
+    const bool was = ctx->reference_option;
     ctx->reference_option = value != 0;
+    if (!tc_shape_ok(ctx->desc)) return value || was ? SPTS_OK : SPTS_ERR_UNSUPPORTED;      // only the 4-bit calls have a choice
     if (!value && ctx->encode_tiled == nullptr) TRY(tc_init(ctx));
     ctx->reference_kernels = value != 0;
     return SPTS_OK;

@@ -16,6 +16,65 @@ from test_gpu_generate4 import check_attention, close, context, fill_garbage, ge
 pytestmark = pytest.mark.gpu
 
 
+# ---------------------------------------------------------------------------------------------- options
+def test_plain_kernels_of_heads_of_64_dims():
+    """SPTS_REFERENCE_KERNELS reaches the 4-bit calls of a bf16 context whose shape has no tensor-core prefill: one launch for 16
+    tokens (the matrix route lays x out in a launch of its own), and the plain kernels' fp32 arithmetic, which is that of an fp32
+    context on the same values: its results rounded once are the same bits."""
+    from paper_2601_13155_b200 import binding
+    shape = shape_of(8, 2, 64)
+    lib, full = context(shape), context(replace(shape, dtype="fp32"))
+    w = rand_w4(70, 512, 64, 1)
+    x = torch.randn(16, 512, device="cuda", generator=gen(2)).to(torch.bfloat16)
+    lens = [300, 0, 45]
+    cache = random_cache(shape, 3, 320, 32, lens, seed=3)
+    q = torch.randn(3, 8, 64, device="cuda", generator=gen(4)).to(torch.bfloat16)
+
+    def launches(call):
+        before = lib.launch_count()
+        call()
+        return lib.launch_count() - before
+    with pytest.raises(binding.SptsError):                           # nothing to take back
+        lib.set_reference_kernels(False)
+    assert launches(lambda: lib.w4_gemv(w, x)) > 1
+    matrix = lib.kv4_attention(cache, q)
+    lib.set_reference_kernels(True)
+    assert launches(lambda: lib.w4_gemv(w, x)) == 1
+    assert torch.equal(lib.w4_gemv(w, x, fp32_out=True), full.w4_gemv(w, x.float(), fp32_out=True))
+    assert torch.equal(lib.kv4_attention(cache, q), full.kv4_attention(cache, q.float()).to(torch.bfloat16))
+    lib.set_reference_kernels(False)
+    assert launches(lambda: lib.w4_gemv(w, x)) > 1
+    assert torch.equal(lib.kv4_attention(cache, q), matrix)
+    full.set_reference_kernels(True)
+    with pytest.raises(binding.SptsError):                           # fp32 has no other kernels
+        full.set_reference_kernels(False)
+    lib.close()
+    full.close()
+
+
+@pytest.mark.parametrize("heads,kv_heads,group,lens", [(2, 2, 32, [1]), (4, 2, 64, [0, 96, 33]), (8, 1, 32, [300]), (40, 1, 32, [70]), (6, 2, 64, [1500, 1, 64])])
+def test_plain_attention_of_heads_of_64_dims_in_bf16(heads, kv_heads, group, lens):
+    shape = shape_of(heads, kv_heads, 64)
+    lib = context(shape)
+    lib.set_reference_kernels(True)
+    cache = random_cache(shape, len(lens), max(lens), group, lens, seed=heads)
+    q = torch.randn(len(lens), heads, 64, device="cuda", generator=gen(5)).to(lib.dtype)
+    check_attention(lib, cache, q, lib.kv4_attention(cache, q), lens)
+    assert lib.device_status() == 0 and lib.check_guards() == 0
+    lib.close()
+
+
+@pytest.mark.parametrize("n,out,k,group", [(1, 7, 64, 64), (5, 1030, 160, 32), (21, 129, 2048, 32)])
+def test_plain_products_beside_heads_of_64_dims_in_bf16(n, out, k, group):
+    lib = context(shape_of(8, 2, 64))
+    lib.set_reference_kernels(True)
+    w = rand_w4(out, k, group, n)
+    x = torch.randn(n, k, device="cuda", generator=gen(n + k)).to(lib.dtype)
+    y, e = R.gemv(R.f64(x), w, lib.dtype, norm=True, eps=lib.shape.rms_eps)
+    close(lib.w4_gemv(w, x, norm=True), y, e, "norm")
+    lib.close()
+
+
 # ---------------------------------------------------------------------------------------------- scales of either sign
 @pytest.mark.parametrize("plain", [False, True])
 @pytest.mark.parametrize("heads,kv_heads,dim,group", [(8, 2, 128, 32), (24, 2, 128, 128), (4, 2, 64, 32)])
