@@ -522,9 +522,9 @@ typedef struct {
  * token outside the vocabulary gives a row of zeros and SPTS_ERR_INDEX in the device status word).  pos (DEVICE [n_seq]) are
  * their original positions.  Every layer appends the token's K / V to its cache (len grows on the device) and attends to what
  * the cache then holds.  x_out [n_seq, D] optional.  logits_out [n_seq, vocab] fp32 receives the head's logits, with the rules
- * applied where there are any; token_out [n_seq] (optional, needs logits_out) the largest one's token as in
- * spts_process_logits.  Everything that changes from step to step lies on the device, so one captured step can be replayed:
- * token_out may be the next step's token_in. */
+ * applied where there are any (rules without logits_out are refused); token_out [n_seq] (optional, needs logits_out) the largest
+ * one's token as in spts_process_logits.  A step that is refused leaves the caches as they were.  Everything that changes from
+ * step to step lies on the device, so one captured step can be replayed: token_out may be the next step's token_in. */
 spts_status spts_decode_step4(spts_ctx* ctx, const spts_model_weights4* mw, const spts_kv4_cache* caches, const void* x_in,
                               const int32_t* token_in, const int32_t* pos, const spts_logits_rules* rules, void* x_out,
                               float* logits_out, int32_t* token_out);

@@ -1182,6 +1182,20 @@ spts_status check_kv4(const spts_ctx* ctx, const spts_kv4_cache* c) {
     return SPTS_ERR_INVALID_ARG;
   return SPTS_OK;
 }
+// The rules for n > 0 rows of a vocabulary; what no rule needs is left out of r.
+spts_status check_rules(spts_logits_rules& r, int n, int vocab) {
+  if (r.n_history < 0 || r.n_history > SPTS_LOGITS_MAX_LIST || r.n_bias < 0 || r.n_bias > SPTS_LOGITS_MAX_LIST) return SPTS_ERR_INVALID_ARG;
+  if (!aligned4({r.history, r.history_start, r.generated_start, r.repetition, r.presence, r.frequency}) ||
+      !aligned4({r.bias_token, r.bias_value, r.bias_start, r.mask}))
+    return SPTS_ERR_INVALID_ARG;
+  if (r.history != nullptr && r.history_start == nullptr) return SPTS_ERR_INVALID_ARG;
+  if (r.bias_token != nullptr && (r.bias_value == nullptr || r.bias_start == nullptr)) return SPTS_ERR_INVALID_ARG;
+  if (r.mask != nullptr && n > 1 && r.ld_mask < (vocab + 31) / 32) return SPTS_ERR_INVALID_ARG;
+  if (r.repetition == nullptr && r.presence == nullptr && r.frequency == nullptr) r.history = nullptr;   // nothing to count for
+  if (r.n_history == 0) r.history = nullptr;
+  if (r.n_bias == 0) r.bias_token = nullptr;
+  return SPTS_OK;
+}
 }  // namespace
 
 spts_status spts_w4_quantize(spts_ctx* ctx, const void* W, int out_features, int in_features, int group, void* codes, void* params) {
@@ -1269,16 +1283,7 @@ spts_status spts_process_logits(spts_ctx* ctx, const float* logits, int64_t ld, 
   if (n > 1 && (ld < vocab || (out != nullptr && ldo < vocab))) return SPTS_ERR_INVALID_ARG;
   if (out == logits && n > 1 && ld != ldo) return SPTS_ERR_INVALID_ARG;
   spts_logits_rules r = *rules;
-  if (r.n_history < 0 || r.n_history > SPTS_LOGITS_MAX_LIST || r.n_bias < 0 || r.n_bias > SPTS_LOGITS_MAX_LIST) return SPTS_ERR_INVALID_ARG;
-  if (!aligned4({r.history, r.history_start, r.generated_start, r.repetition, r.presence, r.frequency}) ||
-      !aligned4({r.bias_token, r.bias_value, r.bias_start, r.mask}))
-    return SPTS_ERR_INVALID_ARG;
-  if (r.history != nullptr && r.history_start == nullptr) return SPTS_ERR_INVALID_ARG;
-  if (r.bias_token != nullptr && (r.bias_value == nullptr || r.bias_start == nullptr)) return SPTS_ERR_INVALID_ARG;
-  if (r.mask != nullptr && n > 1 && r.ld_mask < (vocab + 31) / 32) return SPTS_ERR_INVALID_ARG;
-  if (r.repetition == nullptr && r.presence == nullptr && r.frequency == nullptr) r.history = nullptr;   // nothing to count for
-  if (r.n_history == 0) r.history = nullptr;
-  if (r.n_bias == 0) r.bias_token = nullptr;
+  TRY(check_rules(r, n, vocab));
   ON_DEVICE(ctx);
   return launch_process_logits(ctx, logits, ld, n, vocab, r, out, ldo, token_out);
 }
@@ -1305,11 +1310,17 @@ spts_status spts_decode_step4(spts_ctx* ctx, const spts_model_weights4* mw, cons
   if (pos == nullptr || (x_in == nullptr && (token_in == nullptr || mw->embed == nullptr))) return SPTS_ERR_INVALID_ARG;
   if (!aligned4({pos, token_in, logits_out, token_out})) return SPTS_ERR_INVALID_ARG;
   if (!aligned16(x_in) || !aligned16(x_out) || !aligned16(mw->embed)) return SPTS_ERR_INVALID_ARG;
+  // the head and its rules are looked at before anything is launched: a step that is refused leaves the caches as they were
   const bool head = logits_out != nullptr || token_out != nullptr;
+  spts_logits_rules r;
+  memset(&r, 0, sizeof(r));
+  if (rules != nullptr) r = *rules;
+  if (rules != nullptr && !head) return SPTS_ERR_INVALID_ARG;
   if (head) {
     if (logits_out == nullptr || d.vocab < 1) return SPTS_ERR_INVALID_ARG;
     TRY(check_w4(&mw->lm_head));
     if (!fits(mw->lm_head, d.vocab, D)) return SPTS_ERR_SHAPE;
+    TRY(check_rules(r, n, d.vocab));
   }
   ON_DEVICE(ctx);
   Workspace& ws = ctx->ws;
@@ -1339,9 +1350,7 @@ spts_status spts_decode_step4(spts_ctx* ctx, const spts_model_weights4* mw, cons
   if (!head) return SPTS_OK;
   TRY(spts_w4_gemv(ctx, &mw->lm_head, nullptr, ws.s4_x, D, n, nullptr, 0, SPTS_W4_NORM | SPTS_W4_FP32_OUT, logits_out, d.vocab));
   if (rules == nullptr && token_out == nullptr) return SPTS_OK;
-  spts_logits_rules none;
-  memset(&none, 0, sizeof(none));
-  return spts_process_logits(ctx, logits_out, d.vocab, n, d.vocab, rules != nullptr ? rules : &none, logits_out, d.vocab, token_out);
+  return spts_process_logits(ctx, logits_out, d.vocab, n, d.vocab, &r, logits_out, d.vocab, token_out);
 }
 
 }  // extern "C"

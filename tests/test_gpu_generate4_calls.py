@@ -75,6 +75,44 @@ def test_plain_products_beside_heads_of_64_dims_in_bf16(n, out, k, group):
     lib.close()
 
 
+# ---------------------------------------------------------------------------------------------- a step that is refused
+def test_a_step_with_refused_rules_leaves_the_caches():
+    """Rules that spts_process_logits refuses are refused by the step before anything is launched: lengths, codes and logits stay."""
+    from paper_2601_13155_b200 import binding
+    lens = [4, 5]
+    lib, shape, model, q, lm, embed, caches = build(WIDE, 128, 64, lens, seed=2)
+    pos, token = i32([4, 5]), i32([1, 2])
+    logits = torch.full((2, shape.vocab), 3.0, device="cuda")
+    good = binding.LogitsRules(history=i32([1, 2, 3]), history_start=i32([0, 1, 3]), presence=torch.ones(2, device="cuda"),
+                               bias_token=i32([1]), bias_value=torch.ones(1, device="cuda"), bias_start=i32([0, 1, 1]),
+                               mask=torch.full((2, 32), -1, dtype=torch.int32, device="cuda"))
+
+    def with_(**kw):
+        c = binding.LogitsRulesC.from_buffer_copy(good.c)
+        for k, v in kw.items():
+            setattr(c, k, v)
+        return c
+    bad = [with_(history=good.c.history + 1), with_(mask=good.c.mask + 2), with_(history_start=None), with_(bias_value=None),
+           with_(bias_start=None), with_(ld_mask=31), with_(n_history=-1), with_(n_bias=2 ** 29 + 1), with_(presence=good.c.presence + 1)]
+    before = [(c.length.clone(), c.k_codes.clone(), c.v_params.clone()) for c in caches.layers]
+    ptr = lambda t: C.c_void_p(t.data_ptr())
+
+    def step(rules, logits_out, token_out):
+        return lib.lib.spts_decode_step4(lib.h, C.byref(model.c), caches.c, None, ptr(token), ptr(pos), C.byref(rules), None,
+                                         logits_out, token_out)
+    launched = lib.launch_count()
+    for c in bad:
+        assert step(c, ptr(logits), None) == 1
+    assert step(good.c, None, None) == 1                             # rules and nothing that they apply to
+    assert lib.launch_count() == launched
+    for (length, codes, params), c in zip(before, caches.layers):
+        assert torch.equal(c.length, length) and torch.equal(c.k_codes, codes) and torch.equal(c.v_params, params)
+    assert bool((logits == 3.0).all())
+    assert step(good.c, ptr(logits), ptr(token)) == 0
+    assert lib.device_status() == 0 and caches.layers[0].length.tolist() == [5, 6]
+    lib.close()
+
+
 # ---------------------------------------------------------------------------------------------- scales of either sign
 @pytest.mark.parametrize("plain", [False, True])
 @pytest.mark.parametrize("heads,kv_heads,dim,group", [(8, 2, 128, 32), (24, 2, 128, 128), (4, 2, 64, 32)])
