@@ -368,7 +368,8 @@ class LogitsRules:
 
 
 class Spts:
-    """One library context bound to a device and a stream."""
+    """One library context bound to a device and a stream.  Calls run on that stream: a caller whose tensors are made or read on
+    another one orders the two (wait_stream)."""
 
     def __init__(self, shape, max_seq: int, device="cuda:0", stream: Optional[torch.cuda.Stream] = None):
         if not torch.cuda.is_available():
@@ -666,11 +667,14 @@ class Spts:
 
     def quantize_layer4(self, tensors: Dict[str, torch.Tensor], group: int = 128) -> Dict[str, W4Weight]:
         """The 4-bit form of one layer's matrices (wq, wk, wv, wo, w_gate, w_up, w_down in the storage type)."""
-        qkv = torch.cat([tensors["wq"], tensors["wk"], tensors["wv"]], 0).contiguous()
-        out = {"wqkv": self.w4_quantize(qkv, group)}
-        for name in ("wo", "w_gate", "w_up", "w_down"):
-            out[name] = self.w4_quantize(tensors[name], group)
-        self.stream.synchronize()                                  # qkv is released on return
+        # the stacked matrix is made here, so only here can its making be ordered before the kernels that read it
+        self.stream.wait_stream(torch.cuda.current_stream(self.device))
+        with torch.cuda.stream(self.stream):
+            qkv = torch.cat([tensors["wq"], tensors["wk"], tensors["wv"]], 0).contiguous()
+            out = {"wqkv": self.w4_quantize(qkv, group)}
+            for name in ("wo", "w_gate", "w_up", "w_down"):
+                out[name] = self.w4_quantize(tensors[name], group)
+        self.stream.synchronize()                                  # qkv is released on return, and the codes are for any stream
         return out
 
     def decode_step4(self, model: "Model4", caches: "Kv4Caches", pos, x_in=None, token_in=None, rules: Optional[LogitsRules] = None,

@@ -113,6 +113,27 @@ def test_a_step_with_refused_rules_leaves_the_caches():
     lib.close()
 
 
+# ---------------------------------------------------------------------------------------------- streams
+def test_a_layer_quantised_on_a_stream_of_its_own():
+    """The stacked q / k / v matrix is made inside the call: the context's stream waits for it, whatever torch's stream still does."""
+    from paper_2601_13155_b200 import binding
+    tensors = {k: up(v, "bf16") for k, v in synth.layer_weights(WIDE, 9).items()}
+    lib = binding.Spts(WIDE, max_seq=64)
+    want = lib.quantize_layer4(tensors, 64)
+    lib.close()
+    lib = binding.Spts(WIDE, max_seq=64, stream=torch.cuda.Stream())
+    torch.cuda.synchronize()
+    for _ in range(3):
+        late = {k: torch.zeros_like(v) for k, v in tensors.items()}
+        torch.cuda._sleep(100_000_000)                              # the matrices arrive some 50 ms from now
+        for k, v in tensors.items():
+            late[k].copy_(v)
+        got = lib.quantize_layer4(late, 64)
+        for name, w in want.items():
+            assert torch.equal(got[name].codes, w.codes) and torch.equal(got[name].params, w.params), name
+    lib.close()
+
+
 # ---------------------------------------------------------------------------------------------- scales of either sign
 @pytest.mark.parametrize("plain", [False, True])
 @pytest.mark.parametrize("heads,kv_heads,dim,group", [(8, 2, 128, 32), (24, 2, 128, 128), (4, 2, 64, 32)])
