@@ -685,6 +685,13 @@ class Spts:
             raise ValueError(f"{s.n_layers} layers of weights and caches are needed")
         for cache in caches.layers:
             self._kv4_shape(cache)
+        if model.devices - {dev}:
+            raise ValueError(f"the weights are on cuda:{model.devices}, the context is on cuda:{dev}")
+        table = model.embed
+        if x_in is None and table is not None and (table.dtype is not self.dtype or table.get_device() != dev or table.shape[0] < s.vocab or
+                                                   table.shape[1] != s.hidden):
+            raise ValueError(f"embed: a {self.dtype} table [{s.vocab}, {s.hidden}] on cuda:{dev} is needed, got {table.dtype} "
+                             f"{tuple(table.shape)} on {table.device}")
         if rules is not None:
             rules.check(n, s.vocab, dev)
         code = self.lib.spts_decode_step4(self.h, model.c, caches.c, _vec(x_in, n * s.hidden, self.dtype, "x_in", dev),
@@ -710,8 +717,13 @@ class Model4:
 
     def __init__(self, layers: List[Dict[str, W4Weight]], lm_head: Optional[W4Weight] = None, embed: Optional[torch.Tensor] = None):
         self.layers, self.lm_head, self.embed = layers, lm_head, embed
-        self._arr = (LayerWeights4C * len(layers))(*[LayerWeights4C(*[w[n].c for n in ("wqkv", "wo", "w_gate", "w_up", "w_down")])
-                                                     for w in layers])
+        if embed is not None:
+            _vec(embed, None, embed.dtype, "embed")
+            if embed.dim() != 2:
+                raise ValueError(f"embed: a table [vocab, hidden] is needed, got {tuple(embed.shape)}")
+        names = [n for n, _ in LayerWeights4C._fields_]
+        self.devices = {w[n].device_index for w in layers for n in names} | ({lm_head.device_index} if lm_head is not None else set())
+        self._arr = (LayerWeights4C * len(layers))(*[LayerWeights4C(*[w[n].c for n in names]) for w in layers])
         self.c = ModelWeights4C(self._arr, lm_head.c if lm_head is not None else W4C(), embed.data_ptr() if embed is not None else None)
 
 
