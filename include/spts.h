@@ -452,7 +452,9 @@ typedef struct {
 /* Quantises n_rows rows of K and V [n_rows, Hkv, d] (K after RoPE; row strides ldk, ldv in elements) into the cache.
  * Sequence b owns rows [row_start[b], row_start[b + 1]) (device [n_seq + 1]; NULL: n_rows == n_seq, one row each);
  * they go to slots at[b], at[b] + 1, ... (device [n_seq]; NULL: behind the rows held, at = len), and len[b] becomes
- * at[b] + the sequence's number of rows.  Rows behind row_start[n_seq] (padding) are ignored.  A slot outside
+ * at[b] + the sequence's number of rows.  Rows behind row_start[n_seq] (padding) are ignored.  Starts ascend within
+ * [0, n_rows]; of a sequence that claims rows outside only those that there are count, and starts that break the rule
+ * put SPTS_ERR_INDEX into the device status word.  A slot outside
  * [0, capacity) is not written, len is clipped to the capacity, and SPTS_ERR_WORKSPACE goes to the device status word.
  * pos [n_rows] is stored where the cache has positions.  K_read, V_read [n_rows, Hkv, d] (storage type, optional):
  * the values that the cache now stands for; padding rows of them are left as they were. */

@@ -58,7 +58,7 @@ kv4_append_kernel(Kv4Dev c, const T* __restrict__ K, int64_t ldk, const T* __res
         if (__ldg(&row_start[mid]) <= row) lo = mid; else hi = mid;
       }
       b = lo;
-      first_row = __ldg(&row_start[b]);
+      first_row = max(0, __ldg(&row_start[b]));
       if (row < first_row || row >= __ldg(&row_start[b + 1])) continue;
     }
     const long slot = (long)(at != nullptr ? __ldg(&at[b]) : __ldg(&c.len[b])) + (row - first_row);
@@ -105,12 +105,18 @@ kv4_append_kernel(Kv4Dev c, const T* __restrict__ K, int64_t ldk, const T* __res
   }
 }
 
-// len[b] = at[b] + rows of b, clipped; a kernel of its own behind the append, whose blocks still read the old lengths
+// len[b] = at[b] + rows of b, clipped; a kernel of its own behind the append, whose blocks still read the old lengths.  Only rows
+// that there are count: what a start claims outside [0, n_rows) was never written.
 __global__ void kv4_len_kernel(int32_t* len, const int32_t* __restrict__ at, const int32_t* __restrict__ row_start, int n_seq,
-                               int capacity) {
+                               int capacity, int n_rows, int* status) {
   const int b = blockIdx.x * blockDim.x + threadIdx.x;
   if (b >= n_seq) return;
-  const long n = row_start != nullptr ? max(0, row_start[b + 1] - row_start[b]) : 1;
+  long n = 1;
+  if (row_start != nullptr) {
+    const int r0 = row_start[b], r1 = row_start[b + 1];
+    if (r0 < 0 || r1 < r0 || r1 > n_rows) set_status(status, SPTS_ERR_INDEX);
+    n = max(0L, (long)min(r1, n_rows) - max(r0, 0));
+  }
   const long v = (long)(at != nullptr ? at[b] : len[b]) + n;
   len[b] = (int32_t)(v < 0 ? 0 : v > capacity ? capacity : v);
 }
@@ -862,7 +868,7 @@ spts_status append_t(spts_ctx* ctx, const spts_kv4_cache* cache, const void* K, 
                                                          (T*)K_read, (T*)V_read, ctx->ws.status);
     SPTS_CUDA_OK(ctx);
   }
-  kv4_len_kernel<<<ceil_div(c.n_seq, 256), 256, 0, ctx->stream>>>(c.len, at, row_start, c.n_seq, c.capacity);
+  kv4_len_kernel<<<ceil_div(c.n_seq, 256), 256, 0, ctx->stream>>>(c.len, at, row_start, c.n_seq, c.capacity, n_rows, ctx->ws.status);
   SPTS_CUDA_OK(ctx);
   return SPTS_OK;
 }

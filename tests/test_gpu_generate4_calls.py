@@ -218,3 +218,31 @@ def test_attention_of_a_constant_under_weights_that_bf16_cannot_hold(dim, group,
     assert float((out.double() - const).abs().max()) <= 2.0 ** -3 * 0.999
     assert bool((out == const).all())                                # 61 is a bf16 number, and 2^-16 * 61 is less than half a step
     lib.close()
+
+
+# ---------------------------------------------------------------------------------------------- cache append
+@pytest.mark.parametrize("start,want,code", [
+    ([0, 3, 12], [3, 15], 8),            # the last sequence claims four rows more than there are
+    ([0, 9, 9], [8, 10], 8),
+    ([0, 20, 30], [8, 10], 8),           # a sequence that begins behind the last row
+    ([0, 3, 8], [3, 15], 0),
+    ([2, 3, 5], [1, 12], 0),             # rows before the first and behind the last sequence are nobody's
+    ([5, 3, 8], [0, 15], 8),             # starts that descend
+    ([-2, 3, 8], [3, 15], 8),            # rows before the first row
+])
+def test_append_counts_the_rows_that_there_are(start, want, code):
+    from paper_2601_13155_b200 import binding
+    lib = context()
+    cache = binding.Kv4Cache(shape_of(), 2, 32, group=64)
+    fill_garbage(cache, 1)
+    before = cache.k_codes.clone()
+    K = torch.randn(8, 2, 128, device="cuda", generator=gen(2)).to(torch.bfloat16)
+    lib.kv4_append(cache, K, K, row_start=i32(start), at=i32([0, 10]))
+    assert lib.device_status() == code
+    assert cache.length.tolist() == want
+    changed = (cache.k_codes != before).any(-1).any(1)
+    held = torch.zeros(2, 32, dtype=torch.bool, device="cuda")
+    held[0, :want[0]] = True
+    held[1, 10:want[1]] = True
+    assert torch.equal(changed, held)                                # every row that the length counts was written, and no other
+    lib.close()
