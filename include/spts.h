@@ -457,7 +457,8 @@ typedef struct {
  * put SPTS_ERR_INDEX into the device status word.  A slot outside
  * [0, capacity) is not written, len is clipped to the capacity, and SPTS_ERR_WORKSPACE goes to the device status word.
  * pos [n_rows] is stored where the cache has positions.  K_read, V_read [n_rows, Hkv, d] (storage type, optional):
- * the values that the cache now stands for; padding rows of them are left as they were. */
+ * the values that the cache now stands for; padding rows of them are left as they were.  K_read may be K and V_read V, where
+ * their rows are packed; they overlap nothing else. */
 spts_status spts_kv4_append(spts_ctx* ctx, const spts_kv4_cache* cache, const void* K, int64_t ldk, const void* V,
                             int64_t ldv, const int32_t* pos, const int32_t* row_start, const int32_t* at, int n_rows,
                             void* K_read, void* V_read);

@@ -1253,6 +1253,8 @@ spts_status spts_kv4_append(spts_ctx* ctx, const spts_kv4_cache* cache, const vo
     if (K == nullptr || V == nullptr) return SPTS_ERR_INVALID_ARG;
     if (!rows_ok(K, ldk, width, n_rows, es) || !rows_ok(V, ldv, width, n_rows, es)) return SPTS_ERR_INVALID_ARG;
     if (!aligned16(K_read) || !aligned16(V_read) || (K_read != nullptr && K_read == V_read)) return SPTS_ERR_INVALID_ARG;
+    // values may take the place of the rows that they come from, element by element, and no other's
+    if (K_read == V || V_read == K || (n_rows > 1 && ((K_read == K && ldk != width) || (V_read == V && ldv != width)))) return SPTS_ERR_INVALID_ARG;
   }
   if (!aligned4({pos, row_start, at})) return SPTS_ERR_INVALID_ARG;
   if (at == cache->len) at = nullptr;

@@ -246,3 +246,22 @@ def test_append_counts_the_rows_that_there_are(start, want, code):
     held[1, 10:want[1]] = True
     assert torch.equal(changed, held)                                # every row that the length counts was written, and no other
     lib.close()
+
+
+def test_append_refuses_values_that_take_the_other_matrix_s_place():
+    """K_out may be K and V_out V where their rows are packed; anything else would be read and written in no order."""
+    from paper_2601_13155_b200 import binding
+    lib = context()
+    cache = binding.Kv4Cache(shape_of(), 3, 32, group=64)
+    wide = torch.randn(3, 2 * 256, device="cuda", generator=gen(2)).to(torch.bfloat16)
+    K, V = torch.randn(3, 2, 128, device="cuda").to(torch.bfloat16), torch.randn(3, 2, 128, device="cuda").to(torch.bfloat16)
+    ptr = lambda t: C.c_void_p(t.data_ptr())
+    call = lambda k, ldk, v, ldv, kr, vr: lib.lib.spts_kv4_append(lib.h, C.byref(cache.c), ptr(k), ldk, ptr(v), ldv, None, None, None, 3, kr, vr)
+    assert call(K, 256, V, 256, ptr(V), None) == 1
+    assert call(K, 256, V, 256, None, ptr(K)) == 1
+    assert call(wide, 512, V, 256, ptr(wide), None) == 1
+    assert call(K, 256, wide, 512, None, ptr(wide)) == 1
+    assert cache.length.tolist() == [0, 0, 0]
+    assert call(K, 256, V, 256, ptr(K), ptr(V)) == 0
+    assert cache.length.tolist() == [1, 1, 1] and lib.device_status() == 0
+    lib.close()
