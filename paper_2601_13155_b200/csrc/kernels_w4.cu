@@ -141,10 +141,11 @@ spts_status launch_plain(spts_ctx* ctx, const W4GemvArgs& a) {
 // codes for five instructions, and
 //   y = sum_groups scale_g sum_i c_i x_i + sum_g (mid_g - 8 scale_g) (sum_i x_i)
 // has its second part in one more matrix step per four groups, in bf16, whose A registers are the params words as they lie in
-// memory and whose B holds -8 sum x and sum x in bf16 pieces (two of them, 2^-17 relative; three for fp32 outputs).
+// memory and whose B holds -8 sum x and sum x in three bf16 pieces each (2^-26 relative; with two, 2^-17, 0.08 % of the
+// bf16 outputs differed from the rounded exact ones; the third costs 2 % of 21 x 3584 x 18944).
 //
-// x is laid out for that once per call: brought to fp16 by a power of two (exact: bf16 has fewer bits, and what falls below
-// fp16's range is 2^-35 of the token's largest element), in the order of the B fragments, with the groups' sums and the factor
+// x is laid out for that once per call: brought to fp16 by a power of two (exact: bf16 has fewer bits; only elements below 2^-26 of
+// the token's largest are rounded, off by up to 2^-34 of it), in the order of the B fragments, with the groups' sums and the factor
 // that takes the power of two back (and the row norm with it).  Few elements (LOCAL) every CTA lays out for itself in shared
 // memory while its first weights are on their way; more are laid out once by w4_prepare_kernel (a CTA per token), whose
 // programmatic dependent the product kernel is: it fills its rings with weights meanwhile.
@@ -450,7 +451,7 @@ w4_gemv_kernel(W4Mat m1, W4Mat m2, int out, int in, int n, W4Line line, const bf
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) {
             mma16816(y[nb][mt], p0, p1, p0, p1, xs[nb].x, xs[nb].y);
-            if (o.fp32_out) mma16816(y[nb][mt], p0, p1, 0u, 0u, xs[nb].z, 0u);
+            mma16816(y[nb][mt], p0, p1, 0u, 0u, xs[nb].z, 0u);
           }
         }
       }

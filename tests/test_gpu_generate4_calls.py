@@ -220,6 +220,44 @@ def test_attention_of_a_constant_under_weights_that_bf16_cannot_hold(dim, group,
     lib.close()
 
 
+@pytest.mark.parametrize("n,out,k,group", [(1, 1000, 4096, 64), (8, 500, 4096, 128), (20, 300, 8192, 32)])
+def test_fp32_outputs_hold_fp32_sums(n, out, k, group):
+    """The root mean square of the error, where the element by element bound is too wide to see a lost piece of the groups' sums.
+
+    With s the scale, x ~ N(0, 1) and g groups of m elements, an output's RMS is 4.6 sqrt(g m) s.  A group's sum of x, about sqrt(m),
+    in two bf16 pieces instead of three would be off by 2^-17 * 0.436 of a number in [1, 2) (the second piece rounds what is left,
+    uniform below 2^-8, to eight bits), 2.3e-6 of the sum: 8 s sqrt(m) 2.3e-6 sqrt(g), 4.0e-6 of the RMS.
+    In three pieces what is left are fp32 steps, of matrix units that may truncate (2^-24 of the partial sum on average): m / 16
+    steps of a group, whose partial sums are about 8.8 sqrt(m) s and of either sign: m / 16 2^-24 8.8 sqrt(m) sqrt(g) s, 9e-7 of the
+    RMS for m = 128; and here at most 18 steps of a warp's outputs: 18 * 2^-24 = 1.1e-6 if all erred to one side at the output's
+    full size, of which they have half on average.  The root of the squares' sum is below 1.1e-6; 2e-6 lies between it and 4.0e-6."""
+    lib = context()
+    w = rand_w4(out, k, group, 21, mids=False)
+    x = torch.randn(n, k, device="cuda", generator=gen(4)).to(lib.dtype)
+    want = R.f64(x) @ R.values(w.codes, w.params)[0].T
+    err = R.f64(lib.w4_gemv(w, x, fp32_out=True)) - want
+    assert np.sqrt((err ** 2).mean()) <= 2e-6 * np.sqrt((want ** 2).mean())
+    lib.close()
+
+
+@pytest.mark.parametrize("n,out", [(8, 60000), (12, 40000)])
+def test_bf16_outputs_are_those_of_fp32_sums(n, out):
+    """How many outputs round to another bf16 number than the exact ones do.  An output that is off by e rounds differently with the
+    probability |e| / ulp; of outputs of a normal distribution of RMS 1 above a quarter, the mean of 1 / ulp is 2^7 * 1.44 * 1.45 =
+    267.  With the errors of the test above (in three pieces below 1.1e-6 in the root mean square, in two 4.0e-6; the mean size is
+    0.8 of it) that are at most 2.3e-4 of the outputs, or 8.5e-4; 5e-4 lies between."""
+    lib = context()
+    k, group = 1024, 64
+    w = rand_w4(out, k, group, 21, mids=False)
+    x = torch.randn(n, k, device="cuda", generator=gen(4)).to(lib.dtype)
+    c = torch.stack([w.codes & 15, w.codes >> 4], -1).reshape(out, k).double() - 8
+    want = x.double() @ (c * w.params[..., 0].double().repeat_interleave(group, -1)).T
+    got = lib.w4_gemv(w, x)
+    seen = want.abs() > 0.25 * want.square().mean().sqrt()
+    assert float((got != want.to(torch.bfloat16))[seen].double().mean()) <= 5e-4
+    lib.close()
+
+
 # ---------------------------------------------------------------------------------------------- cache append
 @pytest.mark.parametrize("start,want,code", [
     ([0, 3, 12], [3, 15], 8),            # the last sequence claims four rows more than there are
