@@ -258,6 +258,56 @@ def test_bf16_outputs_are_those_of_fp32_sums(n, out):
     lib.close()
 
 
+# ---------------------------------------------------------------------------------------------- from the prefill to the 4-bit step
+@pytest.mark.parametrize("shape", [replace(WIDE, n_layers=3, vocab=1024), replace(synth.TINY, hidden=256, ffn_dim=672, n_layers=3)], ids=["bf16", "fp32"])
+def test_from_a_skipping_prefill_to_generation(shape):
+    """A prompt goes through the skipping prefill, whose caches differ in length and positions from layer to layer; they enter the
+    4-bit caches layer by layer, and two tokens are generated.  Each step against the plain 64-bit layers on what the 4-bit caches
+    and weights stand for, within the bounds of the other decode tests."""
+    from paper_2601_13155_b200 import binding, schedule
+    seed, N, L = 31, 300, shape.n_layers
+    lib = binding.Spts(shape, max_seq=N)
+    arrays = [synth.layer_weights(shape, seed, l) for l in range(L)]
+    hw = synth.head_weights(shape, seed)
+    embed = up(hw["embed"], shape.dtype)
+    model = binding.Model([binding.LayerWeights(a, shape.dtype) for a in arrays], up(hw["lm_head"], shape.dtype), embed)
+    ids = np.random.default_rng(seed).integers(0, shape.vocab, N)
+    X = embed[torch.from_numpy(ids).cuda()].clone()
+    plan = [(N, N, 200), (120, 90, 0), (77, 64, 0)]
+    cache = binding.KvCache(shape, L, [p[0] for p in plan])
+    pos, orig = i32(np.arange(N)), i32(np.arange(N))
+    token = torch.empty(1, dtype=torch.int32, device="cuda")
+    lib.prefill(model, plan, X, pos, orig, torch.empty_like(X), torch.empty_like(pos), torch.empty_like(orig), cache, token_out=token)
+    lens = [cache.length(l) for l in range(L)]
+    assert lens == [300, 120, 77]
+
+    caches = binding.Kv4Caches(shape, L, 1, max(lens) + 8, group=32)
+    for l in range(L):
+        k, v, at = cache.k[l][:lens[l]], cache.v[l][:lens[l]], i32([0])
+        lib.kv4_append(caches.layers[l], k, v, pos=cache.pos[l][:lens[l]], row_start=i32([0, lens[l]]), at=at)
+        assert caches.layers[l].length.tolist() == [lens[l]]
+        assert torch.equal(caches.layers[l].pos[0, :lens[l]], cache.pos[l][:lens[l]])
+        held = R.cache_rows(caches.layers[l].k_codes[0, 0, :lens[l]], caches.layers[l].k_params[0, 0, :lens[l]], R.key_dims(shape.head_dim))[0]
+        assert np.array_equal(held, R.quantise(R.f64(k[:, 0]), 32)[3])
+    q = [lib.quantize_layer4({n: up(a[n], shape.dtype) for n in a}, 32) for a in arrays]
+    lm = lib.w4_quantize(up(hw["lm_head"], shape.dtype), 32)
+    model4 = binding.Model4(q, lm, embed)
+    x_out, logits = torch.empty(1, shape.hidden, dtype=lib.dtype, device="cuda"), torch.empty(1, shape.vocab, device="cuda")
+    tol = 4e-2 if shape.dtype == "bf16" else 2e-4
+    for step in range(2):
+        before, at = int(token), i32([N + step])
+        assert 0 <= before < shape.vocab
+        lib.decode_step4(model4, caches, at, token_in=token, x_out=x_out, logits_out=logits, token_out=token)
+        assert lib.device_status() == 0 and lib.check_guards() == 0
+        x = host(embed[before])
+        for l in range(L):
+            x = reference_layer(x, N + step, q[l], shape, caches.layers[l], 0, lens[l] + step + 1, shape.dtype)
+        assert rel_rms_err(host(x_out[0]), x) <= tol * L
+        assert int(token) == int(np.argmax(host(logits[0])))
+        assert [c.length.tolist() for c in caches.layers] == [[n + step + 1] for n in lens]
+    lib.close()
+
+
 # ---------------------------------------------------------------------------------------------- cache append
 @pytest.mark.parametrize("start,want,code", [
     ([0, 3, 12], [3, 15], 8),            # the last sequence claims four rows more than there are
