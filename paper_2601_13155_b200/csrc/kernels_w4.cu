@@ -595,7 +595,11 @@ spts_status launch_tile(spts_ctx* ctx, const W4GemvArgs& a) {
   W4Line line;
   line.tiles = ceil_div(a.out, rows);
   line.steps = ceil_div(chunks, WK);
-  const int most = (NB > 2 ? 1 : 2) * (ctx->sm_count < W4_MAX_CTAS / 2 ? ctx->sm_count : W4_MAX_CTAS / 2);
+  constexpr int SEATS = NB > 2 ? 1 : 2;            // CTAs to an SM
+  const int most = SEATS * (ctx->sm_count < W4_MAX_CTAS / 2 ? ctx->sm_count : W4_MAX_CTAS / 2);
+  // what the workspace holds of shares (two to a CTA), and of x by W4_X_ELEMENTS
+  static_assert((size_t)2 * SEATS * (W4_MAX_CTAS / 2) * 8 * NB * T::WR * MT * 16 <= W4_PART_FLOATS, "shares");
+  static_assert(2 * W4Order<NG>::BLOCK <= 5 * W4_CHUNK && 8 * NB * sizeof(float) <= 256, "x");
   const long total = (long)line.tiles * line.steps;
   // Whole tiles where there are three for every resident CTA, or between one and two for every SM, or where tiles are too
   // short for two more launches to pay (8 steps take about 8 us); else equal pieces of the line, whose cut tiles are joined.

@@ -113,9 +113,8 @@ size_t carve(const spts_model_desc& d, int Nmax, void* base, Workspace* ws, std:
     w.s4_att = c.take<char>(n * HD * es);
     w.s4_hm = c.take<char>(n * d.ffn_dim * es);
   }
-  // fragments 2 bytes an element; sums 16 bytes per 32; factors
-  w.w4_x = c.take<char>(W4_X_ELEMENTS * 2 + W4_X_ELEMENTS / 2 + 256);
-  w.w4_part = c.take<float>((size_t)2 * W4_MAX_CTAS * 16 * 256);
+  w.w4_x = c.take<char>(W4_X_BYTES);
+  w.w4_part = c.take<float>(W4_PART_FLOATS);
   w.lg_key = c.take<unsigned long long>(LOGITS_MAX_ROWS);
   w.lg_arrived = c.take<int>(LOGITS_MAX_ROWS);
   w.kv4_part = c.take<float>((size_t)2 * KV4_MAX_CTAS * 16 * (d.head_dim + 2));

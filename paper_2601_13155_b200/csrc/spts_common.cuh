@@ -95,8 +95,8 @@ struct Workspace {
   void* s4_qkv;         // the same behind it
   void* s4_att;         // [SPTS_W4_MAX_N, H d]
   void* s4_hm;          // [SPTS_W4_MAX_N, Dff]
-  void* w4_x;           // tokens prepared for a 4-bit product: fragments, group sums, factors
-  float* w4_part;       // [2 W4_MAX_CTAS, 32, 256] shares of CTAs that split a product's input axis
+  void* w4_x;           // [W4_X_BYTES] tokens prepared for a 4-bit product: fragments, group sums, factors
+  float* w4_part;       // [W4_PART_FLOATS] shares of CTAs that split a product's input axis
   unsigned long long* lg_key;   // [LOGITS_MAX_ROWS] best token of a row so far; zero between calls
   int* lg_arrived;              // [LOGITS_MAX_ROWS] slices of it that are done; zero between calls
   float* kv4_part;      // [2 * KV4_MAX_CTAS, 16, d + 2] partial results of the attention over a 4-bit cache
@@ -137,6 +137,9 @@ namespace spts {
 static const int BATCH_MAX_SEQ = 1024;        // sequences per packed batch that take the one-launch-per-step route
 static const int W4_MAX_CTAS = 320;           // CTAs of a 4-bit product: two per SM
 static const size_t W4_X_ELEMENTS = 1 << 20;  // tokens x features that are prepared at a time
+static const size_t W4_X_BYTES = W4_X_ELEMENTS * 2 + W4_X_ELEMENTS / 2 + 256;   // fragments 2 bytes an element, sums 16 per 32, factors
+// two shares of a CTA, of 16 tokens by 256 rows, or of 32 where there is one CTA to an SM
+static const size_t W4_PART_FLOATS = (size_t)2 * W4_MAX_CTAS * 16 * 256;
 static const int LOGITS_MAX_ROWS = 1024;      // rows of logits per launch
 static const int KV4_MAX_CTAS = 320;          // CTAs of the attention over a 4-bit cache: one or two per SM
 static const int PAP_MAX_WINDOW = 64;         // largest query window of the probe (the paper ablates 1, 4 and 64)
