@@ -1,6 +1,9 @@
 """What a caller of the 4-bit generation operators may do beside the plain calls: options, refused arguments, streams of their
 own, scales of either sign, caches of a skipping prefill; and bounds that see a lost rounding piece."""
 import ctypes as C
+import os
+import subprocess
+import sys
 from dataclasses import replace
 
 import numpy as np
@@ -132,6 +135,79 @@ def test_a_layer_quantised_on_a_stream_of_its_own():
         for name, w in want.items():
             assert torch.equal(got[name].codes, w.codes) and torch.equal(got[name].params, w.params), name
     lib.close()
+
+
+def test_products_of_several_launches_replayed():
+    """Layout, product and join are dependents of one another: captured, the same bits as called, call after call over one workspace."""
+    from paper_2601_13155_b200 import binding
+    st = torch.cuda.Stream()
+    lib = binding.Spts(shape_of(), max_seq=64, stream=st)
+    cases = [(12, 3000, 8192, 128), (32, 300, 14336, 32), (5, 1030, 4096, 64), (20, 65, 40000, 32)]
+    ws = [rand_w4(out, k, g, i) for i, (_, out, k, g) in enumerate(cases)]
+    xs = [torch.randn(n, k, device="cuda", generator=gen(i)).to(torch.bfloat16) for i, (n, _, k, _) in enumerate(cases)]
+    w2 = rand_w4(1030, 4096, 64, 9)
+
+    def run():
+        return [lib.w4_gemv(w, x, norm=i % 2 == 0, w2=w2 if i == 2 else None) for i, (w, x) in enumerate(zip(ws, xs))]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        want = run()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=st):
+        got = run()
+    for _ in range(5):
+        for y in got:
+            y.fill_(float("nan"))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+    assert lib.device_status() == 0 and lib.check_guards() == 0
+    del g
+    lib.close()
+
+
+FIRST_CAPTURED = """
+import sys, torch
+sys.path[:0] = [{root!r}, {root!r} + "/tests"]
+import test_gpu_decode4 as T
+from paper_2601_13155_b200 import binding
+from parity_utils import i32
+lib, shape, model, q, lm, embed, caches = T.build(T.WIDE, 128, 64, [9, 30], seed=11)
+lib.close()
+st = torch.cuda.Stream()
+lib = binding.Spts(shape, max_seq=64, stream=st)
+pos, token = i32([9, 30]), i32([3, 4])
+logits = torch.empty(2, shape.vocab, device="cuda")
+rules = binding.LogitsRules(bias_token=i32([5]), bias_value=torch.ones(1, device="cuda"), bias_start=i32([0, 1, 1]))
+torch.cuda.synchronize()
+step = lambda: lib.decode_step4(model, caches, pos, token_in=token, rules=rules, logits_out=logits, token_out=token)
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g, stream=st):
+    step()
+g.replay()
+torch.cuda.synchronize()
+assert lib.device_status() == 0 and caches.layers[0].length.tolist() == [10, 31]
+first = logits.clone()
+for c in caches.layers:
+    c.length.copy_(i32([9, 30]))
+token.copy_(i32([3, 4]))
+torch.cuda.synchronize()
+step()
+torch.cuda.synchronize()
+assert torch.equal(first, logits)
+del g
+print("same")
+"""
+
+
+def test_a_step_whose_first_call_is_captured():
+    """In a process of its own, where no kernel of the step has been loaded before."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CAPTURED.format(root=root)], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip().endswith("same"), r.stderr[-2000:]
 
 
 # ---------------------------------------------------------------------------------------------- scales of either sign
