@@ -391,7 +391,7 @@ spts_status spts_decode_step(spts_ctx* ctx, const spts_model_weights* mw, spts_k
  * A 4-bit group is 32, 64 or 128 elements that share a bf16 pair (scale, mid); a code c in 0..15 stands for
  *   scale * (c - 8) + mid
  * with a scale of either sign (the quantisers here make none below zero).
- * Quantising a group x (all in 64 bits, every stored number rounded once to bf16):
+ * Quantising a group x (all in 64 bits; bf16() rounds to fp32 and from there to bf16, to nearest even both times):
  *   scale = bf16((max x - min x) / 15),  mid = bf16((max x + min x) / 2 + scale / 2),
  *   c = clamp(rint((x - mid) / scale) + 8, 0, 15), ties to even;  scale == 0: c = 8.
  * A group with a NaN or an infinity in it is stored as scale 0, mid NaN, and SPTS_ERR_NONFINITE goes to the device

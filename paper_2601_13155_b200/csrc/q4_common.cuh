@@ -121,8 +121,9 @@ template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile(
 // Quantises the eight elements of this lane; the group is LANES (4, 8 or 16) neighbouring lanes of the warp, aligned
 // to their number, and every lane of the warp calls.  Returns the eight codes, element i in bits 4i .. 4i + 3; `params`
 // = scale | mid << 16; read (if not null) the values that the codes stand for.
-// The stored numbers are those of 64-bit arithmetic, at the price of 32-bit arithmetic: each is computed in fp32 with a
-// bound on its error, and only where the bound reaches a border between two results the border is decided exactly.  Borders
+// The stored numbers are those of 64-bit arithmetic (scale and mid rounded to bf16 by way of fp32), at the price of 32-bit
+// arithmetic: each is computed in fp32 with a bound on its error, and only where the bound reaches a border between two results the
+// border is decided exactly.  Borders
 // are common, not rare: differences of bf16 numbers have few bits, so a quotient that ends in exactly one half turns up in
 // every other warp, and a mid that needs nine bits in every group; both are decided in fp32 with error-free sums.
 //   scale  three roundings, off by less than 4 in the 16 bits that bf16 drops: near their middle, 64 bits (rare)

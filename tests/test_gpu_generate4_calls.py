@@ -384,6 +384,24 @@ def test_from_a_skipping_prefill_to_generation(shape):
     lib.close()
 
 
+# ---------------------------------------------------------------------------------------------- quantiser
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_stored_numbers_are_rounded_by_way_of_fp32(dtype):
+    """Scale and mid are 64-bit numbers rounded to fp32 and from there to bf16.  A largest element far below half a step of
+    the sum shows it: (-248 + tiny + 16.5) / 2 rounds to -115.75 in fp32, a tie that goes to -116, where one rounding gives -115.5."""
+    lib = context(shape_of(dtype=dtype))
+    x = torch.full((4, 32), -100.0)
+    x[:, 3] = -248.0
+    x[:, 9] = torch.tensor([2.0 ** -20, 2.0 ** -30, 0.0, 2.0 ** -10])
+    W = x.to(lib.dtype).cuda()
+    w = lib.w4_quantize(W, 32)
+    codes, scale, mid, _ = R.quantise(R.f64(W), 32)
+    s, m = R.split_params(w.params)
+    assert np.array_equal(s, scale) and np.array_equal(m, mid) and np.array_equal(R.nibbles(w.codes), codes)
+    assert m[:, 0].tolist() == [-116.0, -116.0, -116.0, -115.5]
+    lib.close()
+
+
 # ---------------------------------------------------------------------------------------------- cache append
 @pytest.mark.parametrize("start,want,code", [
     ([0, 3, 12], [3, 15], 8),            # the last sequence claims four rows more than there are
