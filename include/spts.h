@@ -423,11 +423,13 @@ enum {
 #define SPTS_W4_MAX_OUT (1 << 30)
 
 /* Y[t] = X[t] W^T for n tokens, 0 <= n <= SPTS_W4_MAX_N, in_features <= SPTS_W4_MAX_IN (the codes are read once for all
- * tokens up to 32768 features, beyond that once for every 24, 16 or 8).
+ * tokens up to 32768 features, beyond that once for every 24, 16 or 8; the plain kernels read them once for every four tokens).
  *   w2 given: Y[t] = silu(X[t] W^T) * (X[t] W2^T) (gate and up projection; same shape and group)
  *   residual given: Y[t] = residual[t] + X[t] W^T (Y may be the residual itself; not with w2 or SPTS_W4_FP32_OUT)
  * X [n, in], residual and Y [n, out] in the storage type with row strides ldx, ldr, ldy in elements; X 16-byte aligned,
- * ldx a multiple of 8 (n > 1); Y lies apart from X.  Sums in fp32, one rounding at the end. */
+ * ldx a multiple of 8 (n > 1); Y lies apart from X.  Sums in fp32, one rounding at the end; in bf16 storage an element of x below
+ * 2^-26 of its token's largest one is rounded first, by up to 2^-34 of that one (not by the plain kernels).  A token that holds an
+ * infinity or a NaN gets outputs that are infinite or NaN; the other tokens' are what they are without it. */
 spts_status spts_w4_gemv(spts_ctx* ctx, const spts_w4* w, const spts_w4* w2, const void* X, int64_t ldx, int n,
                          const void* residual, int64_t ldr, uint32_t flags, void* Y, int64_t ldy);
 
@@ -465,8 +467,9 @@ spts_status spts_kv4_append(spts_ctx* ctx, const spts_kv4_cache* cache, const vo
 
 /* Attention of one query per sequence over what its cache holds: O[b, h] = softmax_j(Q[b, h] . K[b, j] / sqrt(d))
  * V[b, j], j < len[b], KV head h / (H / Hkv).  Q [n_seq, H, d] and O [n_seq, H * d] in the storage type, row strides
- * ldq, ldo in elements; O lies apart from Q, whose elements are below 2^100.  A sequence with len[b] <= 0 gets zeros;
- * len[b] beyond the capacity counts as the capacity.  n_seq <= SPTS_KV4_MAX_SEQ. */
+ * ldq, ldo in elements; O lies apart from Q, whose elements are below 2^100 (small ones beside large ones of a query are rounded as
+ * in spts_w4_gemv).  In bf16 storage the weights meet V's scales in fp16 and V's mids in two bf16 pieces (2^-12 and 2^-17 relative).
+ * A sequence with len[b] <= 0 gets zeros; len[b] beyond the capacity counts as the capacity.  n_seq <= SPTS_KV4_MAX_SEQ. */
 #define SPTS_KV4_MAX_SEQ 1024
 spts_status spts_kv4_attention(spts_ctx* ctx, const spts_kv4_cache* cache, const void* Q, int64_t ldq, void* O_out,
                                int64_t ldo);

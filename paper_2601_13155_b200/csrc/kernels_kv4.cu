@@ -27,7 +27,7 @@ struct Kv4Dev {
 // stored in the cache's order.  A warp takes up to `per` passes of one row (blockIdx.y: which, and of K or V), so that the row's
 // sequence is looked up once and the pointers only move.
 // 18,442 rows of 8 heads x 128 with their values read back take 60 us, where memory asks for 27 (each element read once, codes,
-// params and values written once): the quantiser's instructions (300 to a pass of 256 elements) bound it, at four blocks to an SM
+// params and values written once; in fp32 61 us, where it asks for 50): the quantiser's instructions (300 to a pass of 256 elements) bound it, at four blocks to an SM
 // (three 65 us, five 67).  64 single rows: 4.8 us, two launches.
 template <typename T, int D, int LANES>
 __global__ void __launch_bounds__(256, 4)
@@ -240,8 +240,8 @@ kv4_attn_plain_kernel(Kv4Dev c, const T* __restrict__ Q, int64_t ldq, int H, T* 
 // the instructions between the codes and the matrix units, so they are few: codes enter as fp16 by masks alone (code_pair),
 // scales and mids stay outside in fp32:
 //   S = sum_groups scale_g (sum_i c_i q_i) + sum_g (mid_g - 8 scale_g) (sum_i q_i)
-// q is brought to fp16 by a power of two per query (exact: bf16 has fewer bits, and what falls below fp16's range is 2^-35 of
-// the query's largest element).  The second sum is one more matrix step, in bf16, whose A registers are the params words as
+// q is brought to fp16 by a power of two per query (exact: bf16 has fewer bits; only elements below 2^-26 of the query's largest are
+// rounded, off by up to 2^-34 of it).  The second sum is one more matrix step, in bf16, whose A registers are the params words as
 // they lie in memory and whose B holds -8 sum q and sum q in two bf16 pieces each (off by 2^-17 relative).
 //   O = sum_rows c p'_g - 8 sum_rows p'_g + sum_rows p mid_g,   p'_g = fp16(p scale_g / r), p in the last sum in two bf16 pieces
 // (2^-17: mids may be far larger than scales, and the sum of the weights that divides O is that of the unrounded ones; with one
@@ -258,10 +258,11 @@ kv4_attn_plain_kernel(Kv4Dev c, const T* __restrict__ Q, int64_t ldq, int H, T* 
 // one CTA is finished there; a unit cut between CTAs leaves one partial result (maximum, sum, O) per CTA, and the CTA that arrives
 // last adds them in the order of the CTAs, so results do not depend on the order of arrival.  One launch, lengths read on the device.
 //
-// Measured: one sequence of 131072 rows, 8 KV heads x 128 in groups of 32: 42 us, 4.0 TB/s of codes and params; 48 ragged sequences
-// of up to 16384 rows, 4 KV heads: 52 us, 3.6 TB/s; one of 777 rows 9.1 us.  Issue slots are half full (300 instructions per 16
+// Measured: one sequence of 131072 rows, 8 KV heads x 128 in groups of 32: 44 us, 3.8 TB/s of codes and params; 48 ragged sequences
+// of up to 16384 rows, 4 KV heads: 54 us, 3.5 TB/s; one of 777 rows 9.3 us.  Issue slots are half full (310 instructions per 16
 // rows, two warps per scheduler, ALU pipe 43 %, matrix pipe 29 %); four row tiles a step, twelve warps, two or four stages and
-// products in other orders changed nothing, leaving the loads out neither.
+// products in other orders changed nothing, leaving the loads out neither.  (The figures beside the rules below were taken, either
+// side, before the mids' weights had their second piece, which takes 1 to 2 us of these.)
 constexpr int KV4_EXTRA = 32;           // a unit's fixed cost in steps (48 ragged sequences of up to 16384 rows: none 74 us, 8 69, 20 55, 32 52)
 constexpr float KV4_LOG2E = 1.4426950408889634f;
 constexpr float KV4_SLACK = 6.0f;       // weights stay below 2^6 ...
@@ -392,8 +393,10 @@ kv4_attn_kernel(Kv4Dev c, const bf16* __restrict__ Q, int64_t ldq, int H, int qb
   Kv4Line line{pre, held, c.n_seq, heads, KV4_EXTRA};
   long total = line.start(c.n_seq);
   long ctas = max(1L, min((long)gridDim.x, total / (KV4_EXTRA + 1)));
-  // Few equally long units: whole numbers of CTAs to each where that leaves at most a sixteenth of them idle.  (A CTA with the end
-  // of one unit and the beginning of the next meets, leaves and joins twice: 45.8 instead of 42.4 us for 8 x 131072 rows.)
+  // Few units, as long on average as those of the first sequence (equally long ones above all): whole numbers of CTAs to each where
+  // that leaves at most a sixteenth of them idle.  (A CTA with the end of one unit and the beginning of the next meets, leaves and
+  // joins twice: 45.8 instead of 42.4 us for 8 x 131072 rows.)  Units of other lengths that pass the test are cut all the same,
+  // evenly and without the fixed cost.
   {
     const long units = (long)c.n_seq * heads, most = min((long)gridDim.x, units * ((pre[1] + WARPS - 1) / WARPS)), whole = most / units * units;
     if (pre[1] > 0 && pre[1] * (long)c.n_seq == pre[c.n_seq] && 16 * whole >= 15 * most) {

@@ -13,8 +13,8 @@ namespace {
 
 using namespace q4;
 
-// Eight elements to a lane, a group to LANES neighbouring lanes (quantize8).  14336 x 4096 in bf16: 72 us, 2.0 TB/s,
-// bound by its instructions, at six blocks to an SM (five 76, four 78).
+// Eight elements to a lane, a group to LANES neighbouring lanes (quantize8).  14336 x 4096 in bf16: 70 us, 2.1 TB/s (in fp32 64 us,
+// 4.1 TB/s), bound by its instructions as the append is, at six blocks to an SM (72 us; five 76, four 78).
 template <typename T, int LANES>
 __global__ void __launch_bounds__(256, 6)
 w4_quantize_kernel(const T* __restrict__ W, long n_words, uint32_t* __restrict__ codes,
@@ -158,10 +158,11 @@ spts_status launch_plain(spts_ctx* ctx, const W4GemvArgs& a) {
 // copies runs on across tiles.
 //
 // Measured: 1 x 128256 x 4096 54 us, 5.5 TB/s of codes and params (a copy's rate asks for 46; deeper rings and three CTAs to an SM were
-// slower); 1 x 4096 x 4096 6.3 us (launch, x, one ring's latency); two matrices 8 x 14336 x 4096 20 us, of which x's layout
-// about 4; 21 x 3584 x 18944 in groups of 32 29 us (the same two launches 4 + 4; the product at two warps per
+// slower); 1 x 4096 x 4096 6.3 us (launch, x, one ring's latency); two matrices 8 x 14336 x 4096 19.5 us, of which x's layout
+// about 4; 21 x 3584 x 18944 in groups of 32 30 us (the same two launches 4 + 4; the product at two warps per
 // scheduler, 800 instructions to 32 rows x 256 features, matrix pipe 37 %).  L1 prefetches of x, three or four stages and two
-// CTAs of 128 registers made the last one 2 to 8 % slower.
+// CTAs of 128 registers made the last one 2 to 8 % slower.  (The figures beside the rules below were taken, either side, before bf16
+// outputs had the sums' third piece.)
 constexpr int W4_WARPS = 8;
 // 256 features: a row's codes of a chunk are one line of 128 bytes, its params 8 to 32 bytes.  (With chunks of 128 the copies
 // spend twice as many line accesses per byte, and the loop's own instructions weigh twice as much.)
