@@ -469,6 +469,7 @@ spts_status spts_kv4_append(spts_ctx* ctx, const spts_kv4_cache* cache, const vo
  * V[b, j], j < len[b], KV head h / (H / Hkv).  Q [n_seq, H, d] and O [n_seq, H * d] in the storage type, row strides
  * ldq, ldo in elements; O lies apart from Q, whose elements are below 2^100 (small ones beside large ones of a query are rounded as
  * in spts_w4_gemv).  In bf16 storage the weights meet V's scales in fp16 and V's mids in two bf16 pieces (2^-12 and 2^-17 relative).
+ * Infinities and NaN in the params of a row held make the outputs that they reach infinite or NaN.
  * A sequence with len[b] <= 0 gets zeros; len[b] beyond the capacity counts as the capacity.  n_seq <= SPTS_KV4_MAX_SEQ. */
 #define SPTS_KV4_MAX_SEQ 1024
 spts_status spts_kv4_attention(spts_ctx* ctx, const spts_kv4_cache* cache, const void* Q, int64_t ldq, void* O_out,

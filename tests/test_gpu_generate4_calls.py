@@ -12,9 +12,9 @@ import torch
 
 import generate4_ref as R
 from paper_2601_13155_b200 import synth
-from parity_utils import dev, host, i32, rel_rms_err, up
+from parity_utils import host, i32, rel_rms_err, up
 from test_gpu_decode4 import WIDE, build, reference_layer
-from test_gpu_generate4 import check_attention, close, context, fill_garbage, gen, rand_w4, random_cache, random_rules, shape_of
+from test_gpu_generate4 import check_attention, close, context, fill_garbage, gen, rand_w4, random_cache, shape_of
 
 pytestmark = pytest.mark.gpu
 
