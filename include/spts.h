@@ -536,6 +536,84 @@ spts_status spts_decode_step4(spts_ctx* ctx, const spts_model_weights4* mw, cons
                               const int32_t* token_in, const int32_t* pos, const spts_logits_rules* rules, void* x_out,
                               float* logits_out, int32_t* token_out);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Serving over a paged KV cache in the storage type (the paper keeps one contiguous cache per layer, of another length in every
+ * layer; pages let many sequences and layers of different lengths share one pool), with chunks of new tokens: the next turn of a
+ * conversation, drafted tokens that are verified, or one token each.
+ *
+ * As in the calls above nothing is read back and everything that changes from call to call lies on the device, so the calls can be
+ * captured into a CUDA graph; two captured graphs of one context must not run at the same time. */
+
+#define SPTS_PAGED_MAX_SEQ 1024
+#define SPTS_PAGED_MAX_ROWS (1 << 25)    /* rows of one sequence: max_pages * page_size */
+
+/* One layer's cache.  Row j of sequence b lies in page table[b, j / page_size] at j % page_size; len[b] rows are held (a length
+ * beyond max_pages * page_size counts as that, one below 0 as 0).  What lies behind a sequence's rows and in pages of no sequence may
+ * hold anything.  Sequences may share pages that no call writes: an append writes the pages of the new rows, spts_paged_weights and
+ * spts_paged_evict those of all rows.  An entry of the table that a held or new row needs and that is outside [0, n_pages) puts
+ * SPTS_ERR_INDEX into the device status word; its rows read as zeros and are not written. */
+typedef struct {
+  void* k;                /* [n_pages, page_size, Hkv, d] in the storage type (K after RoPE), 16-byte aligned */
+  void* v;
+  int32_t* pos;           /* [n_pages, page_size] original positions, optional      */
+  float* weight;          /* [n_pages, page_size] gathered attention weight, optional */
+  const int32_t* table;   /* [n_seq, max_pages]                                     */
+  int32_t* len;           /* DEVICE [n_seq]                                         */
+  int32_t n_pages;
+  int32_t page_size;      /* 16, 32, 64, 128 or 256                                 */
+  int32_t max_pages;
+  int32_t n_seq;          /* at most SPTS_PAGED_MAX_SEQ                             */
+} spts_paged_kv;
+
+/* Copies n_rows rows of K and V [n_rows, Hkv, d] (row strides ldk, ldv in elements) into the cache; they overlap none of its
+ * buffers.  Sequence b owns rows [row_start[b], row_start[b + 1]) (device [n_seq + 1]; NULL: n_rows == n_seq, one row each); they
+ * become its rows at[b], at[b] + 1, ... (device [n_seq]; NULL: behind the rows held), and len[b] becomes at[b] + their number.
+ * Rows behind row_start[n_seq] (padding) are ignored.  Starts ascend within [0, n_rows]; of a sequence that claims rows outside only
+ * those that there are count, and starts that break the rule put SPTS_ERR_INDEX into the device status word.  A row that would lie
+ * outside [0, max_pages * page_size) is not written, len is clipped to that range, and SPTS_ERR_WORKSPACE goes to the device status
+ * word.  pos [n_rows] is stored where the cache has positions; the weight of a new row is 0. */
+spts_status spts_paged_append(spts_ctx* ctx, const spts_paged_kv* cache, const void* K, int64_t ldk, const void* V, int64_t ldv,
+                              const int32_t* pos, const int32_t* row_start, const int32_t* at, int n_rows);
+
+/* Attention of a chunk of new tokens over the cache that holds them already (append first).  Sequence b owns the queries
+ * [row_start[b], row_start[b + 1]) (as in spts_paged_append); they are its last n rows, and query i of n sees the rows j <= len[b] - n + i:
+ *   O[i, h] = softmax_j(Q[i, h] . K[j, h / (H / Hkv)] / sqrt(d)) V[j, h / (H / Hkv)],   lse[i, h] = log sum_j exp(Q[i, h] . K[j] / sqrt(d)).
+ * Q [n_rows, H, d] and O [n_rows, H * d] in the storage type, row strides ldq, ldo in elements, O apart from Q; lse_out fp32
+ * [n_rows, H], optional.  A query that sees no row gets zeros and -inf; queries behind row_start[n_seq] (padding) are left as they were.
+ * What a query does not see does not reach it, whatever it holds.  In bf16 storage the weights are rounded to bf16 before they meet V. */
+spts_status spts_paged_attention(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start,
+                                 int n_rows, void* O_out, int64_t ldo, float* lse_out);
+
+/* The attention weight that the rows of the cache get from the queries of spts_paged_attention, gathered in cache->weight:
+ *   weight[j] = decay * weight[j] + 1 / H sum_i sum_h exp(Q[i, h] . K[j, h / (H / Hkv)] / sqrt(d) - lse[i, h])
+ * over the queries i that see row j (the mean over heads of Eq. 4, summed over the queries), for all rows held by all sequences.
+ * lse is what spts_paged_attention gave for these queries.  decay >= 0: 1 adds up over calls, 0 forgets what was there (whatever it
+ * was).  The last rows of a prompt are a window of queries as well: row_start then counts those alone. */
+spts_status spts_paged_weights(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start,
+                               int n_rows, const float* lse, float decay);
+
+/* Cuts every sequence that holds more than keep[b] rows (DEVICE [n_seq]; below 0: the sequence is left alone) down to keep[b].
+ * The rows at positions pos < n_sink and pos > p - n_recent, p being the largest position that the sequence holds, stay before all
+ * others, the others by the largest weight; ties go to the row that comes first in the cache, a weight that is NaN ranks last
+ * (SPTS_ERR_NONFINITE in the device status word).  Rows that stay and lie among the first keep[b] are not moved: the r-th place among those that
+ * an evicted row leaves takes the r-th of the staying rows that lie behind, with its K, V, position and weight.  So the rows
+ * are no longer in the order of their positions, which attention does not ask for.  len[b] becomes keep[b]; the pages behind the
+ * rows left are free.  cache->weight is needed, cache->pos where n_sink > 0 or n_recent > 0. */
+spts_status spts_paged_evict(spts_ctx* ctx, const spts_paged_kv* cache, const int32_t* keep, int n_sink, int n_recent);
+
+/* What a row of logits says about a token: for each of n rows, l = logits[row] (fp32, row stride ld),
+ *   logprob = l[target] - log sum_v exp(l[v]),   entropy = - sum_v p[v] log p[v],   rank = number of tokens before the target,
+ *   top_logprob, top_token [n, n_top] = the n_top largest tokens in order
+ * where a token comes before another if its logit is larger, or equal and its index lower.  targets and all outputs are device pointers; each
+ * output may be NULL (logprob_out and rank_out need targets).  A token at -inf has no share and is no alternative: places that are left get -inf and
+ * token -1.  A row with no token above -inf: logprob -inf, entropy 0.  A target outside [0, vocab) (padding): logprob 0,
+ * rank -1.  A row that holds a NaN or +inf: logprob, entropy and the log probabilities of its alternatives are NaN; NaN is never an alternative and
+ * never before a target. */
+#define SPTS_LOGPROBS_MAX_TOP 32
+spts_status spts_token_logprobs(spts_ctx* ctx, const float* logits, int64_t ld, int n, int vocab, const int32_t* targets, int n_top,
+                                float* logprob_out, int32_t* rank_out, float* entropy_out, float* top_logprob_out,
+                                int32_t* top_token_out);
+
 #ifdef __cplusplus
 }
 #endif

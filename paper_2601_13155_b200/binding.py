@@ -24,6 +24,8 @@ OPT_PAP_WINDOW = 8
 OPT_FFN_SCORE_PAP_ONLY = 16
 OPT_DEBUG_CHECKS = 32
 W4_NORM, W4_FP32_OUT, W4_MAX_N = 1, 2, 32
+PAGED_MAX_SEQ, PAGED_MAX_ROWS, PAGE_SIZES = 1024, 1 << 25, (16, 32, 64, 128, 256)
+LOGPROBS_MAX_TOP = 32
 
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "SHAPE", 3: "WORKSPACE", 4: "CUDA", 5: "TIMEOUT",
                 6: "NONFINITE", 7: "UNSUPPORTED", 8: "INDEX"}
@@ -80,6 +82,11 @@ class ModelWeights4C(C.Structure):
     _fields_ = [("layers", C.POINTER(LayerWeights4C)), ("lm_head", W4C), ("embed", C.c_void_p)]
 
 
+class PagedKvC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "pos", "weight", "table", "len")] + \
+               [(n, C.c_int32) for n in ("n_pages", "page_size", "max_pages", "n_seq")]
+
+
 LOGITS_RULES = ("history", "history_start", "generated_start", "repetition", "presence", "frequency", "bias_token",
                 "bias_value", "bias_start", "mask")
 
@@ -101,7 +108,8 @@ EXPORTS = ("spts_workspace_bytes", "spts_create", "spts_destroy", "spts_set_opti
            "spts_layer_prefill_skip_batch", "spts_msdp_plan", "spts_check_guards", "spts_selftest_wait_timeout",
            "spts_debug_check_index_list", "spts_reduced_attention", "spts_prepared_bytes", "spts_prepare_layer",
            "spts_w4_quantize", "spts_w4_gemv", "spts_kv4_append", "spts_kv4_attention", "spts_process_logits",
-           "spts_decode_step4")
+           "spts_decode_step4", "spts_paged_append", "spts_paged_attention", "spts_paged_weights", "spts_paged_evict",
+           "spts_token_logprobs")
 
 OP_NAMES = {1: "prep", 2: "kproj_pap", 3: "pap_softmax", 4: "topk", 5: "kv_gather", 6: "qv_proj", 7: "attention",
             8: "o_proj", 9: "ltp", 10: "gate_up", 11: "down", 12: "compact", 13: "head", 14: "decode"}
@@ -163,6 +171,12 @@ def load_library() -> C.CDLL:
     lib.spts_decode_step4.argtypes = [vp, C.POINTER(ModelWeights4C), C.POINTER(Kv4CacheC), vp, vp, vp, C.POINTER(LogitsRulesC),
                                       vp, vp, vp]
     lib.spts_process_logits.argtypes = [vp, vp, i64, i32, i32, C.POINTER(LogitsRulesC), vp, i64, vp]
+    paged = C.POINTER(PagedKvC)
+    lib.spts_paged_append.argtypes = [vp, paged, vp, i64, vp, i64, vp, vp, vp, i32]
+    lib.spts_paged_attention.argtypes = [vp, paged, vp, i64, vp, i32, vp, i64, vp]
+    lib.spts_paged_weights.argtypes = [vp, paged, vp, i64, vp, i32, vp, C.c_float]
+    lib.spts_paged_evict.argtypes = [vp, paged, vp, i32, i32]
+    lib.spts_token_logprobs.argtypes = [vp, vp, i64, i32, i32, vp, i32, vp, vp, vp, vp, vp]
     for n in EXPORTS:
         if n not in ("spts_workspace_bytes", "spts_destroy", "spts_launch_count", "spts_proxy_scratch_bytes",
                      "spts_prepared_bytes"):
@@ -326,6 +340,46 @@ class Kv4Cache:
         self.c = Kv4CacheC(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_params.data_ptr(),
                            self.v_params.data_ptr(), self.pos.data_ptr() if self.pos is not None else None,
                            self.length.data_ptr(), n_seq, cap, group)
+
+
+class PagedKv:
+    """One layer's paged cache in the storage type (spts_paged_kv): row j of sequence b lies in page table[b, j // page_size].
+    `table` is device int32 [n_seq, max_pages], `length` device int32 [n_seq].  Existing buffers can be handed in; k and v are made with
+    n_pages pages where they are not, positions and weights where they are asked for."""
+
+    def __init__(self, shape, table: torch.Tensor, page_size: int = 64, n_pages: Optional[int] = None, length=None, k=None, v=None, pos=None,
+                 weight=None, positions: bool = False, weights: bool = False):
+        if page_size not in PAGE_SIZES:
+            raise ValueError(f"pages of {PAGE_SIZES} rows, got {page_size}")
+        _vec(table, None, torch.int32, "table")
+        if table.dim() != 2 or table.shape[0] > PAGED_MAX_SEQ or not 1 <= table.shape[1] <= PAGED_MAX_ROWS // page_size:
+            raise ValueError(f"table: [up to {PAGED_MAX_SEQ}, 1 to {PAGED_MAX_ROWS // page_size}] is needed, got {tuple(table.shape)}")
+        device, dev = table.device, table.get_device()
+        n_seq, max_pages = table.shape
+        hkv, d = shape.n_kv_heads, shape.head_dim
+        if k is not None:
+            n_pages = k.shape[0]
+        if not n_pages or n_pages < 1:
+            raise ValueError("n_pages is needed where k is not given")
+
+        def buf(t, size, dtype, what):
+            if t is None:
+                return torch.zeros(size, dtype=dtype, device=device)
+            _vec(t, None, dtype, what, dev)
+            if tuple(t.shape) != size:
+                raise ValueError(f"{what}: {size} is needed, got {tuple(t.shape)}")
+            return t
+        dt = torch_dtype(shape.dtype)
+        self.k = buf(k, (n_pages, page_size, hkv, d), dt, "k")
+        self.v = buf(v, (n_pages, page_size, hkv, d), dt, "v")
+        self.length = buf(length, (n_seq,), torch.int32, "length")
+        self.pos = buf(pos, (n_pages, page_size), torch.int32, "pos") if pos is not None or positions else None
+        self.weight = buf(weight, (n_pages, page_size), torch.float32, "weight") if weight is not None or weights else None
+        self.table, self.n_seq, self.n_pages, self.page_size, self.max_pages = table, n_seq, n_pages, page_size, max_pages
+        self.heads, self.dtype, self.device_index = (hkv, d), dt, dev
+        ptr = lambda t: t.data_ptr() if t is not None else None
+        self.c = PagedKvC(ptr(self.k), ptr(self.v), ptr(self.pos), ptr(self.weight), ptr(table), ptr(self.length), n_pages, page_size,
+                          max_pages, n_seq)
 
 
 class LogitsRules:
@@ -701,6 +755,90 @@ class Spts:
                                           _vec(token_out, n, i32, "token_out", dev))
         if code:
             raise SptsError(code, "spts_decode_step4")
+
+
+    # ------------------------------------------------------------------ serving over a paged cache
+    def _paged_shape(self, cache: PagedKv):
+        if cache.heads != (self.shape.n_kv_heads, self.shape.head_dim) or cache.dtype is not self.dtype:
+            raise ValueError("the cache was made for other heads or another storage type than this context's")
+        if cache.device_index != self.dev:
+            raise ValueError(f"the cache is not on cuda:{self.dev}")
+
+    def paged_append(self, cache: PagedKv, K: torch.Tensor, V: torch.Tensor, pos=None, row_start=None, at=None):
+        """spts_paged_append: rows of K, V [n, Hkv, d] (K after RoPE) become rows of the cache; row_start [n_seq + 1] and at [n_seq]
+        are device int32."""
+        n, w, dev, i32 = K.shape[0], self.shape.n_kv_heads * self.shape.head_dim, self.dev, torch.int32
+        self._paged_shape(cache)
+        if V.shape[0] != n:
+            raise ValueError("as many rows of V as of K are needed")
+        kp, ldk = _rows(K, w, self.dtype, "K", dev)
+        vp, ldv = _rows(V, w, self.dtype, "V", dev)
+        code = self.lib.spts_paged_append(self.h, cache.c, kp, ldk, vp, ldv, _vec(pos, n, i32, "pos", dev),
+                                          _vec(row_start, cache.n_seq + 1, i32, "row_start", dev), _vec(at, cache.n_seq, i32, "at", dev), n)
+        if code:
+            raise SptsError(code, "spts_paged_append")
+
+    def paged_attention(self, cache: PagedKv, Q: torch.Tensor, row_start=None, O_out=None, lse_out=None, want_lse: bool = False):
+        """spts_paged_attention: Q [n, H, d] (or [n, H * d]), the last rows of their sequences -> O [n, H * d]; with want_lse or lse_out
+        (O, lse [n, H])."""
+        n, w, dev = Q.shape[0], self.shape.n_q_heads * self.shape.head_dim, self.dev
+        self._paged_shape(cache)
+        if O_out is None:
+            O_out = torch.empty((n, w), dtype=self.dtype, device=self.device)
+        if O_out.shape[0] != n:
+            raise ValueError("as many rows of O_out as of Q are needed")
+        if lse_out is None and want_lse:
+            lse_out = torch.empty((n, self.shape.n_q_heads), dtype=torch.float32, device=self.device)
+        qp, ldq = _rows(Q, w, self.dtype, "Q", dev)
+        op, ldo = _rows(O_out, w, self.dtype, "O_out", dev)
+        code = self.lib.spts_paged_attention(self.h, cache.c, qp, ldq, _vec(row_start, cache.n_seq + 1, torch.int32, "row_start", dev), n, op,
+                                             ldo, _vec(lse_out, n * self.shape.n_q_heads, torch.float32, "lse_out", dev))
+        if code:
+            raise SptsError(code, "spts_paged_attention")
+        return O_out if lse_out is None else (O_out, lse_out)
+
+    def paged_weights(self, cache: PagedKv, Q: torch.Tensor, lse: torch.Tensor, row_start=None, decay: float = 1.0):
+        """spts_paged_weights: cache.weight = decay * cache.weight + the weight that the rows get from these queries."""
+        n, dev = Q.shape[0], self.dev
+        self._paged_shape(cache)
+        if cache.weight is None:
+            raise ValueError("the cache was made without weights")
+        qp, ldq = _rows(Q, self.shape.n_q_heads * self.shape.head_dim, self.dtype, "Q", dev)
+        code = self.lib.spts_paged_weights(self.h, cache.c, qp, ldq, _vec(row_start, cache.n_seq + 1, torch.int32, "row_start", dev), n,
+                                           _vec(lse, n * self.shape.n_q_heads, torch.float32, "lse", dev), float(decay))
+        if code:
+            raise SptsError(code, "spts_paged_weights")
+
+    def paged_evict(self, cache: PagedKv, keep: torch.Tensor, n_sink: int = 0, n_recent: int = 0):
+        """spts_paged_evict: every sequence down to keep[b] rows (device int32 [n_seq])."""
+        self._paged_shape(cache)
+        if cache.weight is None or (cache.pos is None and (n_sink or n_recent)):
+            raise ValueError("the cache was made without weights, or without the positions that n_sink and n_recent go by")
+        code = self.lib.spts_paged_evict(self.h, cache.c, _vec(keep, cache.n_seq, torch.int32, "keep", self.dev), int(n_sink), int(n_recent))
+        if code:
+            raise SptsError(code, "spts_paged_evict")
+
+    def token_logprobs(self, logits: torch.Tensor, targets: Optional[torch.Tensor] = None, n_top: int = 0, entropy: bool = True):
+        """spts_token_logprobs: a dict of logprob and rank [n] (with targets, device int32), entropy [n], top_logprob and top_token
+        [n, n_top] (n_top > 0)."""
+        n, v = logits.shape
+        if not 0 <= n_top <= LOGPROBS_MAX_TOP:
+            raise ValueError(f"up to {LOGPROBS_MAX_TOP} alternatives, got {n_top}")
+        lp, ld = _rows(logits, v, torch.float32, "logits", self.dev)
+        tp = _vec(targets, n, torch.int32, "targets", self.dev)
+        f32, i32, new, out = torch.float32, torch.int32, torch.empty, {}
+        if targets is not None:
+            out["logprob"], out["rank"] = new(n, dtype=f32, device=self.device), new(n, dtype=i32, device=self.device)
+        if entropy:
+            out["entropy"] = new(n, dtype=f32, device=self.device)
+        if n_top:
+            out["top_logprob"], out["top_token"] = new(n, n_top, dtype=f32, device=self.device), new(n, n_top, dtype=i32, device=self.device)
+        ptr = lambda name: out[name].data_ptr() if name in out else None
+        code = self.lib.spts_token_logprobs(self.h, lp, ld, n, v, tp, n_top, ptr("logprob"), ptr("rank"), ptr("entropy"), ptr("top_logprob"),
+                                            ptr("top_token"))
+        if code:
+            raise SptsError(code, "spts_token_logprobs")
+        return out
 
 
 class Kv4Caches:

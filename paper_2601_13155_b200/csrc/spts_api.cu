@@ -119,6 +119,13 @@ size_t carve(const spts_model_desc& d, int Nmax, void* base, Workspace* ws, std:
   w.lg_arrived = c.take<int>(LOGITS_MAX_ROWS);
   w.kv4_part = c.take<float>((size_t)2 * KV4_MAX_CTAS * 16 * (d.head_dim + 2));
   w.kv4_arrived = c.take<int>(KV4_MAX_CTAS);
+  w.paged_part = c.take<float>(paged_part_floats(d));
+  w.paged_arrived = c.take<int>(64);
+  w.evict_bits = c.take<uint32_t>(SPTS_PAGED_MAX_ROWS / 32);
+  w.evict_before = c.take<int2>(EVICT_CHUNKS);
+  w.evict_total = c.take<int2>((size_t)SPTS_PAGED_MAX_SEQ * EVICT_SPLIT);
+  w.lp_part = c.take<float>((size_t)LP_MAX_SHARES * LP_PART_FLOATS);
+  w.lp_arrived = c.take<int>(LOGITS_MAX_ROWS);
   w.dec = c.take<float>(decode_scratch_floats(d));
   w.logits_v = c.take<float>((size_t)(d.vocab > 0 ? d.vocab : 1));
   w.xrow = c.take<char>((size_t)d.hidden * es);
@@ -613,7 +620,10 @@ spts_status spts_create(const spts_model_desc* desc, int max_seq, void* workspac
     spts_destroy(ctx);
     return SPTS_ERR_CUDA;
   }
-  if (cudaMemsetAsync(ctx->ws.kv4_arrived, 0, KV4_MAX_CTAS * sizeof(int), ctx->stream) != cudaSuccess ||
+  if (spts_status s = paged_init(ctx); s != SPTS_OK) { spts_destroy(ctx); return s; }
+  if (cudaMemsetAsync(ctx->ws.paged_arrived, 0, 64 * sizeof(int), ctx->stream) != cudaSuccess ||
+      cudaMemsetAsync(ctx->ws.lp_arrived, 0, LOGITS_MAX_ROWS * sizeof(int), ctx->stream) != cudaSuccess ||
+      cudaMemsetAsync(ctx->ws.kv4_arrived, 0, KV4_MAX_CTAS * sizeof(int), ctx->stream) != cudaSuccess ||
       cudaMemsetAsync(ctx->ws.lg_key, 0, LOGITS_MAX_ROWS * sizeof(unsigned long long), ctx->stream) != cudaSuccess ||
       cudaMemsetAsync(ctx->ws.lg_arrived, 0, LOGITS_MAX_ROWS * sizeof(int), ctx->stream) != cudaSuccess) {
     spts_destroy(ctx);
@@ -1352,6 +1362,108 @@ spts_status spts_decode_step4(spts_ctx* ctx, const spts_model_weights4* mw, cons
   TRY(spts_w4_gemv(ctx, &mw->lm_head, nullptr, ws.s4_x, D, n, nullptr, 0, SPTS_W4_NORM | SPTS_W4_FP32_OUT, logits_out, d.vocab));
   if (rules == nullptr && token_out == nullptr) return SPTS_OK;
   return spts_process_logits(ctx, logits_out, d.vocab, n, d.vocab, &r, logits_out, d.vocab, token_out);
+}
+
+// ---- serving over a paged cache
+namespace {
+spts_status check_paged(const spts_paged_kv* c) {
+  if (c == nullptr) return SPTS_ERR_INVALID_ARG;
+  const bool page_ok = c->page_size == 16 || c->page_size == 32 || c->page_size == 64 || c->page_size == 128 || c->page_size == 256;
+  if (!page_ok || c->n_seq < 0 || c->n_seq > SPTS_PAGED_MAX_SEQ || c->max_pages < 1 || c->max_pages > SPTS_PAGED_MAX_ROWS / c->page_size ||
+      c->n_pages < 1 || (int64_t)c->n_pages * c->page_size > (int64_t)1 << 30)
+    return SPTS_ERR_SHAPE;
+  if (c->n_seq == 0) return SPTS_OK;
+  if (c->k == nullptr || c->v == nullptr || c->table == nullptr || c->len == nullptr) return SPTS_ERR_INVALID_ARG;
+  if (!aligned16(c->k) || !aligned16(c->v) || c->k == c->v || !aligned4({c->pos, c->weight, c->table, c->len})) return SPTS_ERR_INVALID_ARG;
+  return SPTS_OK;
+}
+// Whether a call of n_rows rows of the cache's sequences can be made; *none: nothing is to be done.
+spts_status check_chunk(const spts_paged_kv* c, const int32_t* row_start, int n_rows, bool* none) {
+  if (n_rows < 0 || !aligned4({row_start})) return SPTS_ERR_INVALID_ARG;
+  *none = c->n_seq == 0;
+  if (c->n_seq == 0) return n_rows == 0 || row_start != nullptr ? SPTS_OK : SPTS_ERR_INVALID_ARG;
+  if (row_start == nullptr && n_rows != c->n_seq) return SPTS_ERR_INVALID_ARG;
+  return n_rows > SPTS_PAGED_MAX_ROWS ? SPTS_ERR_SHAPE : SPTS_OK;
+}
+}  // namespace
+
+spts_status spts_paged_append(spts_ctx* ctx, const spts_paged_kv* cache, const void* K, int64_t ldk, const void* V, int64_t ldv,
+                              const int32_t* pos, const int32_t* row_start, const int32_t* at, int n_rows) {
+  TRY(check_ctx(ctx));
+  TRY(check_paged(cache));
+  bool none = false;
+  TRY(check_chunk(cache, row_start, n_rows, &none));
+  if (none) return SPTS_OK;
+  const int64_t width = (int64_t)ctx->desc.n_kv_heads * ctx->desc.head_dim;
+  const size_t es = elt_size(ctx->desc);
+  if (n_rows > 0) {
+    if (K == nullptr || V == nullptr || K == cache->k || K == cache->v || V == cache->k || V == cache->v) return SPTS_ERR_INVALID_ARG;
+    if (!rows_ok(K, ldk, width, n_rows, es) || !rows_ok(V, ldv, width, n_rows, es)) return SPTS_ERR_INVALID_ARG;
+  }
+  if (!aligned4({pos, at})) return SPTS_ERR_INVALID_ARG;
+  if (at == cache->len) at = nullptr;
+  ON_DEVICE(ctx);
+  return launch_paged_append(ctx, cache, K, ldk, V, ldv, pos, row_start, at, n_rows);
+}
+
+spts_status spts_paged_attention(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start,
+                                 int n_rows, void* O_out, int64_t ldo, float* lse_out) {
+  TRY(check_ctx(ctx));
+  TRY(check_paged(cache));
+  bool none = false;
+  TRY(check_chunk(cache, row_start, n_rows, &none));
+  if (none || n_rows == 0) return SPTS_OK;
+  if (Q == nullptr || O_out == nullptr || Q == O_out || !aligned4({lse_out})) return SPTS_ERR_INVALID_ARG;
+  const int64_t width = (int64_t)ctx->desc.n_q_heads * ctx->desc.head_dim;
+  const size_t es = elt_size(ctx->desc);
+  if (!rows_ok(Q, ldq, width, n_rows, es) || !rows_ok(O_out, ldo, width, n_rows, es)) return SPTS_ERR_INVALID_ARG;
+  ON_DEVICE(ctx);
+  return launch_paged_attention(ctx, cache, Q, ldq, row_start, n_rows, O_out, ldo, lse_out);
+}
+
+spts_status spts_paged_weights(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start,
+                               int n_rows, const float* lse, float decay) {
+  TRY(check_ctx(ctx));
+  TRY(check_paged(cache));
+  bool none = false;
+  TRY(check_chunk(cache, row_start, n_rows, &none));
+  if (none) return SPTS_OK;
+  if (cache->weight == nullptr || !(decay >= 0.0f) || std::isinf(decay)) return SPTS_ERR_INVALID_ARG;
+  if (n_rows > 0) {
+    if (Q == nullptr || lse == nullptr || !aligned4({lse})) return SPTS_ERR_INVALID_ARG;
+    if (!rows_ok(Q, ldq, (int64_t)ctx->desc.n_q_heads * ctx->desc.head_dim, n_rows, elt_size(ctx->desc))) return SPTS_ERR_INVALID_ARG;
+  }
+  ON_DEVICE(ctx);
+  return launch_paged_weights(ctx, cache, Q, ldq, row_start, n_rows, lse, decay);
+}
+
+spts_status spts_paged_evict(spts_ctx* ctx, const spts_paged_kv* cache, const int32_t* keep, int n_sink, int n_recent) {
+  TRY(check_ctx(ctx));
+  TRY(check_paged(cache));
+  if (n_sink < 0 || n_recent < 0) return SPTS_ERR_INVALID_ARG;
+  if (cache->n_seq == 0) return SPTS_OK;
+  if (keep == nullptr || cache->weight == nullptr || (cache->pos == nullptr && (n_sink > 0 || n_recent > 0)) || !aligned4({keep}))
+    return SPTS_ERR_INVALID_ARG;
+  ON_DEVICE(ctx);
+  return launch_paged_evict(ctx, cache, keep, n_sink, n_recent);
+}
+
+spts_status spts_token_logprobs(spts_ctx* ctx, const float* logits, int64_t ld, int n, int vocab, const int32_t* targets, int n_top,
+                                float* logprob_out, int32_t* rank_out, float* entropy_out, float* top_logprob_out,
+                                int32_t* top_token_out) {
+  TRY(check_ctx(ctx));
+  if (n < 0 || n_top < 0 || n_top > SPTS_LOGPROBS_MAX_TOP) return SPTS_ERR_INVALID_ARG;
+  if (vocab < 1 || vocab > SPTS_LOGITS_MAX_VOCAB || n > SPTS_PAGED_MAX_ROWS) return SPTS_ERR_SHAPE;
+  if (n == 0) return SPTS_OK;
+  if (logits == nullptr || (targets == nullptr && (logprob_out != nullptr || rank_out != nullptr))) return SPTS_ERR_INVALID_ARG;
+  if (n_top == 0) { top_logprob_out = nullptr; top_token_out = nullptr; }
+  if (logprob_out == nullptr && rank_out == nullptr && entropy_out == nullptr && top_logprob_out == nullptr && top_token_out == nullptr)
+    return SPTS_ERR_INVALID_ARG;
+  if (n > 1 && ld < vocab) return SPTS_ERR_INVALID_ARG;
+  if (!aligned4({logits, targets, logprob_out, rank_out}) || !aligned4({entropy_out, top_logprob_out, top_token_out})) return SPTS_ERR_INVALID_ARG;
+  ON_DEVICE(ctx);
+  return launch_token_logprobs(ctx, logits, ld, n, vocab, targets, top_logprob_out == nullptr && top_token_out == nullptr ? 0 : n_top,
+                               logprob_out, rank_out, entropy_out, top_logprob_out, top_token_out);
 }
 
 }  // extern "C"

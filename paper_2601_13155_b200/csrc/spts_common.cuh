@@ -101,6 +101,13 @@ struct Workspace {
   int* lg_arrived;              // [LOGITS_MAX_ROWS] slices of it that are done; zero between calls
   float* kv4_part;      // [2 * KV4_MAX_CTAS, 16, d + 2] partial results of the attention over a 4-bit cache
   int* kv4_arrived;     // [KV4_MAX_CTAS] CTAs that have left theirs; zero between calls
+  float* paged_part;    // [2 * PAGED_MAX_CTAS] shares of attention units that several CTAs work on
+  int* paged_arrived;   // [64] blocks of a call that are done; zero between calls
+  uint32_t* evict_bits; // [SPTS_PAGED_MAX_ROWS / 32] rows that stay
+  int2* evict_before;   // [EVICT_CHUNKS] holes and movers before each chunk of rows, within the part of a sequence that one CTA ranked
+  int2* evict_total;    // [SPTS_PAGED_MAX_SEQ, EVICT_SPLIT] holes and movers of each part
+  float* lp_part;       // shares of slices of logits
+  int* lp_arrived;      // [LOGITS_MAX_ROWS] slices of a row that are done; zero between calls
   int4* attn_tiles;     // [Nmax / 128 + BATCH_MAX_SEQ] query tiles of a packed batch's attention launch
 };
 
@@ -142,6 +149,13 @@ static const size_t W4_X_BYTES = W4_X_ELEMENTS * 2 + W4_X_ELEMENTS / 2 + 256;   
 static const size_t W4_PART_FLOATS = (size_t)2 * W4_MAX_CTAS * 16 * 256;
 static const int LOGITS_MAX_ROWS = 1024;      // rows of logits per launch
 static const int KV4_MAX_CTAS = 320;          // CTAs of the attention over a 4-bit cache: one or two per SM
+static const int PAGED_MAX_CTAS = 160;        // CTAs of the attention over a paged cache: one per SM
+static const int EVICT_CHUNK = 256;           // rows of a chunk of the eviction
+static const int EVICT_SPLIT = 8;             // CTAs that rank one sequence's rows at most (a portable cluster)
+static const int EVICT_CHUNKS = SPTS_PAGED_MAX_ROWS / EVICT_CHUNK;
+static const int LP_MAX_SLICES = 64;          // slices of a row of logits at most
+static const int LP_PART_FLOATS = 8 + 2 * SPTS_LOGPROBS_MAX_TOP;   // statistics and alternatives of a slice
+static const int LP_MAX_SHARES = 4096;        // slices of a launch that share rows
 static const int PAP_MAX_WINDOW = 64;         // largest query window of the probe (the paper ablates 1, 4 and 64)
 
 // top-k scratch size in uint32 words
@@ -286,6 +300,22 @@ spts_status launch_kv4_append(spts_ctx* ctx, const spts_kv4_cache* cache, const 
 spts_status launch_kv4_attention(spts_ctx* ctx, const spts_kv4_cache* cache, const void* Q, int64_t ldq, void* O, int64_t ldo);
 spts_status launch_process_logits(spts_ctx* ctx, const float* logits, int64_t ld, int n, int vocab,
                                   const spts_logits_rules& rules, float* out, int64_t ldo, int32_t* token);
+
+// ---- kernels_paged.cu, kernels_paged_tc.cu, kernels_logprobs.cu : serving over a paged cache
+inline bool paged_tc(const spts_ctx* ctx) {   // heads the tensor-core kernels cover
+  return !plain4(ctx) && ctx->desc.n_q_heads / ctx->desc.n_kv_heads <= 128;
+}
+size_t paged_part_floats(const spts_model_desc& d);
+spts_status paged_init(spts_ctx* ctx);        // kernel attributes, the tensor-map encoder
+spts_status launch_paged_append(spts_ctx* ctx, const spts_paged_kv* cache, const void* K, int64_t ldk, const void* V, int64_t ldv,
+                                const int32_t* pos, const int32_t* row_start, const int32_t* at, int n_rows);
+spts_status launch_paged_attention(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start,
+                                   int n_rows, void* O, int64_t ldo, float* lse);
+spts_status launch_paged_weights(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start,
+                                 int n_rows, const float* lse, float decay);
+spts_status launch_paged_evict(spts_ctx* ctx, const spts_paged_kv* cache, const int32_t* keep, int n_sink, int n_recent);
+spts_status launch_token_logprobs(spts_ctx* ctx, const float* logits, int64_t ld, int n, int vocab, const int32_t* targets, int n_top,
+                                  float* logprob, int32_t* rank, float* entropy, float* top_logprob, int32_t* top_token);
 
 // ---- kernels_step4.cu
 spts_status launch_embed_rows(spts_ctx* ctx, const void* embed, const int32_t* token, int n, void* x);
