@@ -671,13 +671,11 @@ bool plain_attr() {
 }  // namespace
 
 spts_status paged_init(spts_ctx* ctx) {
-  (void)ctx;
   const bool ok = plain_attr<float, 64>() && plain_attr<float, 128>() && plain_attr<bf16, 64>() && plain_attr<bf16, 128>() &&
                   cudaFuncSetAttribute(evict_rank_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, RANK_KEYS * 8) == cudaSuccess;
-  return ok ? SPTS_OK : SPTS_ERR_CUDA;
+  if (!ok) return SPTS_ERR_CUDA;
+  return ctx->desc.dtype == SPTS_BF16 ? paged_tc_init(ctx) : SPTS_OK;
 }
-
-size_t paged_part_floats(const spts_model_desc& d) { (void)d; return 64; }
 
 spts_status launch_paged_append(spts_ctx* ctx, const spts_paged_kv* cache, const void* K, int64_t ldk, const void* V, int64_t ldv,
                                 const int32_t* pos, const int32_t* row_start, const int32_t* at, int n_rows) {
@@ -693,6 +691,7 @@ spts_status launch_paged_append(spts_ctx* ctx, const spts_paged_kv* cache, const
 spts_status launch_paged_attention(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start,
                                    int n_rows, void* O, int64_t ldo, float* lse) {
   if (n_rows == 1) { ldq = 0; ldo = 0; }      // one row has no stride
+  if (paged_tc(ctx)) return launch_paged_attention_tc(ctx, cache, Q, ldq, row_start, n_rows, O, ldo, lse);
   const bool d64 = ctx->desc.head_dim == 64;
   if (ctx->desc.dtype == SPTS_BF16)
     return d64 ? attn_plain_t<bf16, 64>(ctx, cache, Q, ldq, row_start, n_rows, O, ldo, lse)

@@ -1,0 +1,858 @@
+// Attention of chunks of new tokens over a paged KV cache on tcgen05 (bf16 storage, head dims 64 and 128).
+//
+// Rows of a score tile are packed: token x head of one KV head's group, heads inside, floor(128 / G) tokens to a tile of 128 rows, so one
+// drafted token or a long chunk fill as much of a tile as they can and K and V are read once for the whole group.  A unit of work is
+// (sequence, KV head, one tile of tokens or two neighbouring ones); its cost is the number of 128-row blocks of the cache that its last token
+// sees.  All units laid end to end make a line of blocks, which is cut into as many equal pieces as there are CTAs (one per SM): every
+// CTA has the same number of blocks, whatever the batch.  A unit that several CTAs work on leaves shares (O, maximum, sum) in the
+// workspace, joined by paged_attn_join_kernel.  Lengths and starts are read on the device; nothing depends on the host's view.
+//
+//   warp 0      TMA producer: Q tiles (boxes of G heads x tokens), then the blocks of K and V in the order in which they are needed, page
+//               by page, into a ring of five tiles
+//   warp 1      TMEM owner and single-thread MMA issuer; columns S_0 | S_1 | O_0 | O_1
+//   warp 2      clears, in shared memory, the rows of V behind a sequence's last one (they may hold anything, and 0 * NaN is NaN)
+//   warps 4-7   softmax of slot 0, warps 8-11 of slot 1, one row per thread
+// The two slots are the unit's two tiles, which share every block of K and V, or, where it has one tile, two neighbouring blocks of the cache
+// (joined at the end of the unit): either way the tensor core has the other slot's products while one slot's softmax runs.
+// P V reads V as it lies in the pages (row = token): its operand is the transposed one, 128-byte swizzled with the head dims along the row.
+#include "paged_common.cuh"
+#include "tc_ptx.cuh"
+
+namespace spts {
+
+namespace {
+
+using namespace paged;
+using namespace ptx;
+
+constexpr int BLOCK = 128;                     // rows of the cache to a block, rows of a score tile
+constexpr int SLAB = BLOCK * 128;              // [128 rows x 64 bf16], 128-byte swizzle
+constexpr int RING = 5;                        // tiles of K or V in flight
+constexpr int PA_THREADS = 384;
+constexpr int PA_COLS = 512;
+constexpr int REGS_LIGHT = 72, REGS_SOFTMAX = 216;   // 128 * 72 + 256 * 216 = 384 * 168, the launch's total
+constexpr float RESCALE = 8.0f;                // log2 units the running maximum may lag behind
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+template <int D> constexpr int tile_bytes() { return D / 64 * SLAB; }
+template <int D> constexpr int pa_smem() { return 1024 + (2 + RING) * tile_bytes<D>() + 512 + 1024 + 128; }
+template <int D> constexpr int share_floats() { return BLOCK * (D + 2); }       // O, then (maximum, sum) of each row
+
+struct AttnArgs {
+  Cache c;
+  const int32_t* row_start; int n_rows;
+  int H, Hkv, G;
+  int tile_tokens, unit_tokens;                // floor(128 / G); that or twice that
+  const bf16* Q; int64_t ldq;
+  bf16* O; int64_t ldo; float* lse;
+  float* share;
+  int* status;
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<uint32_t*>(&v);
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1, int c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(dst), "l"(tm), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+      : "memory");
+}
+// Operand whose rows run along K (tokens) and whose 128-byte rows hold 64 of the N (head dims): 8-row groups 1024 bytes apart, the next
+// 64 of N one slab behind; a K step of 16 is two groups.
+__device__ __forceinline__ uint64_t smem_desc_rows_along_k(uint32_t saddr) {
+  return smem_desc_sw128(saddr) | ((uint64_t)(SLAB >> 4) << 16);
+}
+constexpr uint32_t B_ALONG_N = 1u << 16;       // instruction descriptor: B is stored N-contiguous
+
+// A wait whose limit counts from its own beginning.
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  if (mbar_test_wait(bar, parity)) return true;
+  uint64_t t0 = 0;
+  for (uint32_t it = 0;; ++it) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if ((it & 0xFFu) == 0xFFu) {
+      if (*abort_flag) return false;
+      const uint64_t now = globaltimer_ns();
+      if (t0 == 0) t0 = now;
+      else if (now - t0 > WAIT_LIMIT_NS) {
+        *abort_flag = 1;
+        return false;
+      }
+    }
+  }
+}
+
+// The same for a whole warp: all lanes or none go on.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, wait(bar, parity, abort_flag));
+}
+
+// ------------------------------------------------------------------------------------------------ the line of blocks
+// sum of floor((a i + b) / m), i < n, by the Euclidean recursion on (m, a)
+__device__ unsigned long long floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
+  unsigned long long sum = 0;
+  while (true) {
+    if (a >= m) { sum += (unsigned long long)n * (n - 1) / 2 * (a / m); a %= m; }
+    if (b >= m) { sum += (unsigned long long)n * (b / m); b %= m; }
+    const unsigned long long y = (unsigned long long)a * n + b;
+    if (y < m) return sum;
+    n = (uint32_t)(y / m);
+    b = (uint32_t)(y % m);
+    const uint32_t t = m;
+    m = a;
+    a = t;
+  }
+}
+// Blocks of unit g of a sequence whose n queries see off + 1, off + 2, ... rows: one at least (the unit's rows are written even where
+// they see nothing).
+__device__ __forceinline__ int unit_blocks(int n, int off, int R, int g) {
+  const int seen = off + min(n, (g + 1) * R);
+  return max(1, (seen + BLOCK - 1) / BLOCK);
+}
+// of the units before g
+__device__ long long blocks_before(int n, int off, int R, int g) {
+  const int whole = min(g, n / R);
+  const int blind = off < 0 ? min(whole, -off / R) : 0;            // units that see nothing
+  long long sum = blind;
+  if (whole > blind) sum += (long long)floor_sum(whole - blind, BLOCK, R, off + (blind + 1) * R + BLOCK - 1);
+  if (g > whole) sum += unit_blocks(n, off, R, whole);
+  return sum;
+}
+
+struct Place { int b, h, g, j; };              // block j of unit (b, h, g)
+
+struct Line {
+  long long* pre;                              // [n_seq + 1] blocks before each sequence
+  long long total;
+  template <int NT> __device__ __forceinline__ void make(const AttnArgs& a, long long* scratch, bool check) {
+    pre = scratch + 32;
+    total = block_prefix<NT>(a.c.n_seq, pre, scratch, [&](int b) {
+      int first, n;
+      call_rows(a.row_start, a.n_rows, b, first, n);
+      if (check) check_starts(a.row_start, a.n_rows, b, a.status);
+      const int R = a.unit_tokens;
+      return n == 0 ? 0LL : a.Hkv * blocks_before(n, held_rows(a.c, b) - n, R, (n + R - 1) / R);
+    });
+  }
+  // a block to each of the first CTAs where there are fewer blocks than CTAs: no CTA between two others is without one
+  __device__ __forceinline__ long long cut(int cta, int ctas) const { return total >= ctas ? total * cta / ctas : min((long long)cta, total); }
+  __device__ __forceinline__ Place find(const AttnArgs& a, long long x) const {
+    Place p;
+    p.b = find_share(pre, a.c.n_seq, x);
+    int first, n;
+    call_rows(a.row_start, a.n_rows, p.b, first, n);
+    const int off = held_rows(a.c, p.b) - n, R = a.unit_tokens;
+    const long long head = (pre[p.b + 1] - pre[p.b]) / a.Hkv;
+    x -= pre[p.b];
+    p.h = (int)(x / head);
+    x -= p.h * head;
+    int lo = 0, hi = (n + R - 1) / R;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (blocks_before(n, off, R, mid) <= x) lo = mid; else hi = mid;
+    }
+    p.g = lo;
+    p.j = (int)(x - blocks_before(n, off, R, lo));
+    return p;
+  }
+};
+
+// A CTA's share of one unit: blocks [j0, j1) of `cost`.
+struct Segment {
+  int b, h, j0, j1, cost;
+  int held, n, off;                            // the sequence's rows, its queries, rows before the first query
+  int token, tokens;                           // first token of the unit (in its sequence), how many
+  int row;                                     // first row of the unit in Q and O
+  bool two;                                    // two tiles
+};
+
+// Each role of a CTA walks over the CTA's segments by itself.
+struct Walk {
+  Place p;
+  long long left;
+  int first, n, off, held;
+  __device__ __forceinline__ void sequence(const AttnArgs& a) {
+    call_rows(a.row_start, a.n_rows, p.b, first, n);
+    held = held_rows(a.c, p.b);
+    off = held - n;
+  }
+  __device__ __forceinline__ bool next(const AttnArgs& a, Segment& s) {
+    if (left <= 0) return false;
+    const int R = a.unit_tokens;
+    s.b = p.b; s.h = p.h; s.held = held; s.n = n; s.off = off;
+    s.cost = unit_blocks(n, off, R, p.g);
+    s.j0 = p.j;
+    s.j1 = (int)min((long long)s.cost, p.j + left);
+    s.token = p.g * R;
+    s.tokens = min(R, n - s.token);
+    s.row = first + s.token;
+    s.two = s.tokens > a.tile_tokens;
+    left -= s.j1 - s.j0;
+    p.j = 0;
+    if ((p.g + 1) * R < n) { ++p.g; return true; }
+    p.g = 0;
+    if (++p.h < a.Hkv) return true;
+    p.h = 0;
+    while (left > 0 && ++p.b < a.c.n_seq) {
+      sequence(a);
+      if (n > 0) break;
+    }
+    return true;
+  }
+};
+
+// ------------------------------------------------------------------------------------------------ rows that came out not finite
+// A weight of zero does not keep an infinity or NaN of V out of a product of matrices.  A row that came out not finite is computed
+// again, by its warp, over the rows [k0, k1) of the cache that it sees: D / 32 dims to a lane.  (m in log2 units; o not divided by l.)
+template <int D>
+__device__ __noinline__ void plain_row(const AttnArgs& a, int b, int kvh, const bf16* q, int k0, int k1, float& m, float& l, float* o) {
+  constexpr int PER = D / 32;
+  const int lane = threadIdx.x & 31;
+  float qf[PER];
+#pragma unroll
+  for (int e = 0; e < PER; ++e) { qf[e] = __bfloat162float(q[lane * PER + e]); o[e] = 0.f; }
+  m = -INFINITY;
+  l = 0.f;
+  const float sc = LOG2E * rsqrtf((float)D);
+  for (int j = k0; j < k1; ++j) {
+    const int64_t slot = slot_of(a.c, b, j);
+    float kf[PER], vf[PER], s = 0.f;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      const int64_t at = (slot * a.Hkv + kvh) * D + lane * PER + e;
+      kf[e] = slot < 0 ? 0.f : __bfloat162float(reinterpret_cast<const bf16*>(a.c.k)[at]);
+      vf[e] = slot < 0 ? 0.f : __bfloat162float(reinterpret_cast<const bf16*>(a.c.v)[at]);
+      s = fmaf(qf[e], kf[e], s);
+    }
+    s = warp_sum(s) * sc;
+    const float now = fmaxf(m, s), base = now == -INFINITY ? 0.f : now;
+    const float alpha = m == -INFINITY ? 0.f : ex2(m - base), p = ex2(s - base);
+    l = l * alpha + p;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) o[e] = p == 0.f ? o[e] * alpha : fmaf(p, vf[e], o[e] * alpha);
+    m = now;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ the kernel
+template <int D>
+__global__ void __launch_bounds__(PA_THREADS, 1)
+paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                  const __grid_constant__ AttnArgs a) {
+  constexpr int TILE = tile_bytes<D>(), SLABS = D / 64;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t sQ = base, sR = sQ + 2 * TILE, bars = sR + RING * TILE;
+  const uint32_t q_full = bars, q_free = bars + 16;            // [2]
+  const uint32_t s_full = bars + 32, o_full = bars + 48;       // [2] slots
+  const uint32_t p_full = bars + 64;                           // [2 slots][2 halves]
+  const uint32_t full = bars + 96, free_ = full + 8 * RING;    // [RING]
+  // [RING] a tile of V with rows behind the last one was asked for; is cleared.  One for each place, since several short segments' tails may
+  // be in the ring at a time
+  const uint32_t v_tail = free_ + 8 * RING, v_clean = v_tail + 8 * RING;
+  const uint32_t x_full = v_clean + 8 * RING, x_free = x_full + 8;   // slot 1's maximum and sum are there; its O has been read
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + (bars - base) + 384);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  float2* ml = reinterpret_cast<float2*>(gen + (bars - base) + 512);
+  Walk* start = reinterpret_cast<Walk*>(gen + (bars - base) + 512 + 1024);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    *abort_flag = 0;
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(q_full + 8 * s, 1); mbar_init(q_free + 8 * s, 1);
+      mbar_init(s_full + 8 * s, 1); mbar_init(o_full + 8 * s, 1);
+      for (int h = 0; h < 2; ++h) mbar_init(p_full + 8 * (2 * s + h), 128);
+    }
+    for (int s = 0; s < RING; ++s) {
+      mbar_init(full + 8 * s, 1); mbar_init(free_ + 8 * s, 1);
+      mbar_init(v_tail + 8 * s, 1); mbar_init(v_clean + 8 * s, 32);
+    }
+    mbar_init(x_full, 128); mbar_init(x_free, 128);
+    fence_mbar_init();
+    prefetch_tensormap(&tmQ); prefetch_tensormap(&tmK); prefetch_tensormap(&tmV);
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32((const void*)tmem_slot), PA_COLS);
+    tmem_relinquish();
+  }
+  // this CTA's piece of the line; the prefix sums lie where K and V will
+  {
+    Line line;
+    line.make<PA_THREADS>(a, reinterpret_cast<long long*>(gen + (sR - base)), blockIdx.x == 0);
+    if (threadIdx.x == 0) {
+      const long long from = line.cut(blockIdx.x, gridDim.x), to = line.cut(blockIdx.x + 1, gridDim.x);
+      Walk w;
+      w.left = to - from;
+      if (w.left > 0) { w.p = line.find(a, from); w.sequence(a); }
+      *start = w;
+    }
+    fence_proxy_async_smem();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  Walk walk = *start;
+  Segment s;
+
+  // The order of the ring's tiles within a segment of nb blocks: with two tiles K_0, V_0, K_1, V_1, ...; with one (slots on neighbouring
+  // blocks) K_0, K_1, V_0, K_2, V_1, ...: `ahead` tiles of K before the first of V, then V_i and K_{i + ahead} in turn, V last.
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_LIGHT));
+    if (warp == 0) {
+      const int shift = a.c.shift, page = 1 << shift, box = min(page, BLOCK);     // rows of a box
+      const uint32_t q_bytes = (uint32_t)(a.G * a.tile_tokens * 128 * SLABS);
+      uint32_t slot = 0, phase = 1, q_used[2] = {0, 0}, q_next = 0;
+      bool ok = true;
+      while (ok && walk.next(a, s)) {
+        const int nb = s.j1 - s.j0, ahead = s.two ? 1 : 2;
+        // where this lane's box of block j lies; rows behind the last one and entries that name no page: a place behind the last page
+        const int32_t* table = a.c.table + (int64_t)s.b * a.c.max_pages;
+        const int nowhere = a.c.n_pages << shift;
+        auto place = [&](int j) {
+          const int row = j * BLOCK + lane * box;
+          if (j >= s.j1 || lane * box >= BLOCK || row >= s.held) return -1;
+          const int p = __ldg(table + (row >> shift));
+          if (p < 0 || p >= a.c.n_pages) { set_status(a.status, SPTS_ERR_INDEX); return nowhere; }
+          return (p << shift) + (row & (page - 1));
+        };
+        int y0 = place(s.j0), y1 = place(s.j0 + 1), y2 = place(s.j0 + 2);
+        for (int t = 0; t < (s.two ? 2 : 1); ++t) {
+          const int buf = s.two ? t : (int)q_next;
+          ok = ok && wait_warp(q_free + 8 * buf, (q_used[buf] & 1) ^ 1, abort_flag);
+          ++q_used[buf];
+          if (ok && lane == 0) {
+            mbar_expect_tx(q_full + 8 * buf, q_bytes);
+            for (int h = 0; h < SLABS; ++h)
+              tma_load_3d(sQ + buf * TILE + h * SLAB, &tmQ, q_full + 8 * buf, 64 * h, s.h * a.G, s.row + t * a.tile_tokens);
+          }
+        }
+        if (!s.two) q_next ^= 1;
+        auto load = [&](bool is_v, int j, int y) {
+          ok = ok && wait_warp(free_ + 8 * slot, phase, abort_flag);
+          if (!ok) return;
+          const int rows = max(0, min(BLOCK, s.held - j * BLOCK)), boxes = (rows + box - 1) / box;
+          const uint32_t bar = full + 8 * slot, dst = sR + slot * TILE + lane * box * 128;
+          if (lane == 0) {
+            if (boxes > 0) mbar_expect_tx(bar, (uint32_t)(boxes * box * 128 * SLABS));
+            else mbar_arrive(bar);
+            if (is_v && rows < BLOCK) mbar_arrive(v_tail + 8 * slot);
+          }
+          __syncwarp();
+          if (y >= 0)
+            for (int h = 0; h < SLABS; ++h) tma_load_2d(dst + h * SLAB, is_v ? &tmV : &tmK, bar, s.h * D + 64 * h, y);
+          if (++slot == RING) { slot = 0; phase ^= 1; }
+        };
+        load(false, s.j0, y0);
+        if (ahead == 2 && nb > 1) load(false, s.j0 + 1, y1);
+        for (int j = s.j0; j < s.j1 && ok; ++j) {
+          load(true, j, y0);
+          if (j + ahead < s.j1) load(false, j + ahead, ahead == 1 ? y1 : y2);
+          y0 = y1; y1 = y2; y2 = place(j + 3);
+        }
+      }
+    } else if (warp == 1) {
+      if (lane == 0) {
+        constexpr uint32_t idesc_s = idesc_bf16(BLOCK, BLOCK), idesc_o = idesc_bf16(BLOCK, D) | B_ALONG_N;
+        uint32_t slot = 0, phase = 0, q_used[2] = {0, 0}, q_next = 0, pv[2] = {0, 0}, clean = 0, turn = 0;   // (clean: a phase for each place)
+        bool ok = true;
+        auto take = [&]() -> uint32_t {          // the ring's next tile
+          ok = ok && wait(full + 8 * slot, phase, abort_flag);
+          const uint32_t at = slot;
+          if (++slot == RING) { slot = 0; phase ^= 1; }
+          return at;
+        };
+        auto take_v = [&](bool tail) -> uint32_t {
+          if (!tail) return take();
+          ok = ok && wait(v_clean + 8 * slot, (clean >> slot) & 1, abort_flag);
+          clean ^= 1u << slot;
+          const uint32_t at = slot;
+          if (++slot == RING) { slot = 0; phase ^= 1; }
+          return at;
+        };
+        auto qk = [&](int t, int buf, uint32_t at) {
+          const uint32_t kb = sR + at * TILE, qb = sQ + buf * TILE;
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            const uint32_t off = (k >> 2) * SLAB + (k & 3) * 32;
+            mma_bf16(tmem_base + t * BLOCK, smem_desc_sw128(qb + off), smem_desc_sw128(kb + off), idesc_s, k > 0 ? 1u : 0u);
+          }
+          mma_commit(s_full + 8 * t);
+        };
+        // O_t += P_t V, P_t read from the columns of S_t, in the halves in which the softmax warps hand it over
+        auto pv_mma = [&](int t, uint32_t at, bool first) {
+          const uint32_t vb = sR + at * TILE;
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            ok = ok && wait(p_full + 8 * (2 * t + half), pv[t] & 1, abort_flag);
+            if (!ok) return;
+            tc_fence_after();
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+              const int k = 4 * half + kk;
+              mma_bf16_tmem_a(tmem_base + 2 * BLOCK + t * BLOCK, tmem_base + t * BLOCK + 8 * k, smem_desc_rows_along_k(vb + k * 2048), idesc_o,
+                              first && k == 0 ? 0u : 1u);
+            }
+          }
+          ++pv[t];
+        };
+        while (ok && walk.next(a, s)) {
+          const int nb = s.j1 - s.j0;
+          const bool tail = s.j1 * BLOCK > s.held;
+          if (s.two) {
+            for (int t = 0; t < 2; ++t) { ok = ok && wait(q_full + 8 * t, q_used[t] & 1, abort_flag); ++q_used[t]; }
+            const uint32_t k0 = take();
+            if (!ok) break;
+            tc_fence_after();
+            qk(0, 0, k0);
+            qk(1, 1, k0);
+            mma_commit(free_ + 8 * k0);
+            if (nb == 1) { mma_commit(q_free); mma_commit(q_free + 8); }
+            for (int i = 0; i < nb && ok; ++i) {
+              const bool more = i + 1 < nb;
+              const uint32_t v = take_v(tail && !more), k = more ? take() : 0;
+              if (!ok) break;
+              for (int t = 0; t < 2 && ok; ++t) {
+                pv_mma(t, v, i == 0);
+                if (!ok) break;
+                if (more) qk(t, t, k);           // (its commit also covers P_t V: O_t rests when S_t arrives)
+                else mma_commit(o_full + 8 * t);
+              }
+              if (!ok) break;
+              mma_commit(free_ + 8 * v);
+              if (more) mma_commit(free_ + 8 * k);
+              if (i + 2 == nb) { mma_commit(q_free); mma_commit(q_free + 8); }
+            }
+          } else {
+            const int buf = (int)q_next;
+            q_next ^= 1;
+            ok = ok && wait(q_full + 8 * buf, q_used[buf] & 1, abort_flag);
+            ++q_used[buf];
+            for (int i = 0; i < 2 && i < nb; ++i) {
+              const uint32_t k = take();
+              if (!ok) break;
+              tc_fence_after();
+              qk((i + turn) & 1, buf, k);
+              mma_commit(free_ + 8 * k);
+            }
+            if (!ok) break;
+            if (nb <= 2) mma_commit(q_free + 8 * buf);
+            for (int i = 0; i < nb && ok; ++i) {
+              const int t = (i + turn) & 1;
+              const bool more = i + 2 < nb;
+              const uint32_t v = take_v(tail && i + 1 == nb);
+              if (!ok) break;
+              pv_mma(t, v, i < 2);
+              if (!ok) break;
+              mma_commit(free_ + 8 * v);
+              if (more) {
+                const uint32_t k = take();
+                if (!ok) break;
+                tc_fence_after();
+                qk(t, buf, k);
+                mma_commit(free_ + 8 * k);
+                if (i + 3 == nb) mma_commit(q_free + 8 * buf);
+              } else {
+                mma_commit(o_full + 8 * t);
+              }
+            }
+            turn = (turn + nb) & 1;
+          }
+        }
+      }
+    } else if (warp == 2) {
+      uint32_t at = 0, tails = 0;                // tiles of the ring up to this segment's end; a phase for each place
+      bool ok = true;
+      while (ok && walk.next(a, s)) {
+        at += 2 * (s.j1 - s.j0);
+        if (s.j1 * BLOCK <= s.held) continue;
+        // the tile was asked for: the one that was in its place before has been used, and it will stay until it is clear
+        const uint32_t slot = (at - 1) % RING;
+        ok = wait_warp(v_tail + 8 * slot, (tails >> slot) & 1, abort_flag) && wait_warp(full + 8 * slot, ((at - 1) / RING) & 1, abort_flag);
+        tails ^= 1u << slot;
+        if (!ok) break;
+        const int rows = max(0, s.held - (s.j1 - 1) * BLOCK);
+        for (int h = 0; h < SLABS; ++h)
+          for (int i = rows * 8 + lane; i < BLOCK * 8; i += 32)
+            *reinterpret_cast<uint4*>(gen + (sR - base) + slot * TILE + h * SLAB + i * 16) = make_uint4(0, 0, 0, 0);
+        fence_proxy_async_smem();
+        mbar_arrive(v_clean + 8 * slot);
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
+    const int t = (warp - 4) >> 2;                     // slot
+    const int quarter = warp & 3;                      // TMEM lanes this warp may access
+    const int row = quarter * 32 + lane;
+    const int row_token = row / a.G, row_head = row % a.G;
+    const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
+    const uint32_t tS = tmem_base + t * BLOCK + lane_off, tO = tmem_base + 2 * BLOCK + t * BLOCK + lane_off;
+    const float sc = LOG2E / (D == 128 ? 11.313708498984761f : 8.0f);
+    const float2 sc2 = make_float2(sc, sc);
+    uint32_t n_s = 0, n_o = 0, n_x = 0, turn = 0;
+    bool ok = true;
+    while (ok && walk.next(a, s)) {
+      const int nb = s.j1 - s.j0, tile = s.two ? t : 0;
+      const int tokens = min(a.tile_tokens, s.tokens - tile * a.tile_tokens);
+      const int token = s.token + tile * a.tile_tokens + row_token;        // in the sequence
+      const bool live = row_token < tokens;
+      const bool any_live = quarter * 32 < tokens * a.G;                   // of this warp
+      const int limit = live ? max(0, s.off + token + 1) : 0;              // rows that this query sees
+      float m_used = -INFINITY, l = 0.f;
+      int done = 0;
+      for (int i = s.two ? 0 : ((t + turn) & 1); i < nb && ok; i += s.two ? 1 : 2) {
+        ok = wait_warp(s_full + 8 * t, n_s & 1, abort_flag);
+        ++n_s;
+        if (!ok) break;
+        if (!any_live) {                                                   // rows of no query: whatever P holds stays in them
+          mbar_arrive(p_full + 16 * t);
+          mbar_arrive(p_full + 16 * t + 8);
+          continue;
+        }
+        tc_fence_after();
+        const int key0 = (s.j0 + i) * BLOCK;
+        uint32_t r[BLOCK];
+#pragma unroll
+        for (int c = 0; c < BLOCK; c += 32) tmem_ld32(tS + c, r + c);
+        tmem_ld_wait();
+        if (__any_sync(0xffffffffu, limit < key0 + BLOCK)) {
+#pragma unroll
+          for (int e = 0; e < BLOCK; ++e)
+            if (key0 + e >= limit) r[e] = 0xFF800000u;                     // -inf
+        }
+        float bm[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int e = 0; e < BLOCK; e += 8) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) bm[u] = max3(bm[u], __uint_as_float(r[e + 2 * u]), __uint_as_float(r[e + 2 * u + 1]));
+        }
+        const float bmax = fmaxf(fmaxf(bm[0], bm[1]), fmaxf(bm[2], bm[3])) * sc;
+        float alpha = 1.0f;                            // for O and l where the running maximum is replaced
+        if (bmax > m_used + RESCALE || m_used == -INFINITY) {
+          alpha = m_used == -INFINITY ? 0.0f : ex2(m_used - bmax);
+          m_used = bmax;
+        }
+        // S_t complete means that the last P_t V has completed, too, and the next cannot start before this thread's P arrives
+        if (done > 0 && __any_sync(0xffffffffu, alpha != 1.0f)) {
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            uint32_t o[32];
+            tmem_ld32(tO + c, o);
+            tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+            tmem_st32(tO + c, o);
+          }
+        }
+        const float shift = m_used == -INFINITY ? 0.f : -m_used;
+        const float2 nm2 = make_float2(shift, shift);
+        float2 ps[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) ps[u] = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          uint32_t pk[32];
+#pragma unroll
+          for (int e = 0; e < 64; e += 2) {
+            const int e0 = 64 * half + e;
+            const float2 x = __ffma2_rn(make_float2(__uint_as_float(r[e0]), __uint_as_float(r[e0 + 1])), sc2, nm2);
+            const float2 p = make_float2(ex2(x.x), ex2(x.y));
+            ps[(e >> 1) & 3] = __fadd2_rn(ps[(e >> 1) & 3], p);
+            pk[e >> 1] = pack2(p.x, p.y);              // rounded once, before it meets V; the sum takes it unrounded
+          }
+#pragma unroll
+          for (int c = 0; c < 32; c += 16) tmem_st16(tS + 32 * half + c, pk + c);
+          tmem_st_wait();
+          tc_fence_before();
+          mbar_arrive(p_full + 8 * (2 * t + half));
+        }
+        const float2 ps0 = __fadd2_rn(ps[0], ps[1]), ps1 = __fadd2_rn(ps[2], ps[3]);
+        l = l * alpha + ((ps0.x + ps0.y) + (ps1.x + ps1.y));
+        ++done;
+      }
+      if (!ok) break;
+      // ---- the end of a segment
+      const bool merge = !s.two && nb > 1, mine = s.two || (merge ? t == 0 : (int)(turn & 1) == t);
+      if (!s.two) turn = (turn + nb) & 1;
+      if (mine || merge) {
+        ok = wait_warp(o_full + 8 * t, n_o & 1, abort_flag);
+        ++n_o;
+        if (!ok) break;
+        tc_fence_after();
+      }
+      float f0 = 1.f, f1 = 0.f;                        // factors of this slot's and of slot 1's O
+      if (merge && t == 1) {
+        ml[row] = make_float2(m_used, l);
+        tc_fence_before();
+        mbar_arrive(x_full);
+        ok = wait_warp(x_free, n_x & 1, abort_flag);
+        ++n_x;
+        continue;
+      }
+      if (!mine) continue;
+      if (merge) {
+        ok = wait_warp(x_full, n_x & 1, abort_flag);
+        ++n_x;
+        if (!ok) break;
+        tc_fence_after();
+        const float2 other = ml[row];
+        const float m = fmaxf(m_used, other.x), b = m == -INFINITY ? 0.f : m;
+        f0 = ex2(m_used - b);
+        f1 = ex2(other.x - b);
+        l = l * f0 + other.y * f1;
+        m_used = m;
+      }
+      const bool direct = s.j0 == 0 && s.j1 == s.cost;
+      const int64_t out_row = (int64_t)s.row + tile * a.tile_tokens + row_token;
+      const int head = s.h * a.G + row_head;
+      bf16* orow = a.O + out_row * a.ldo + (int64_t)head * D;
+      float* share = a.share + ((int64_t)(2 * blockIdx.x + (s.j0 == 0 ? 1 : 0)) * 2 + tile) * share_floats<D>();
+      const float inv = direct ? (l == 0.f ? 0.f : 1.0f / l) : 1.0f;
+      float odd = 0.f;                                 // becomes NaN with a value that is not finite
+      if (any_live) {
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+          uint32_t o[32];
+          tmem_ld32(tO + c, o);
+          tmem_ld_wait();
+          if (merge) {
+            uint32_t o1[32];
+            tmem_ld32(tO + BLOCK + c, o1);
+            tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const float x0 = f0 == 0.f ? 0.f : __uint_as_float(o[e]) * f0, x1 = f1 == 0.f ? 0.f : __uint_as_float(o1[e]) * f1;
+              o[e] = __float_as_uint(x0 + x1);
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            const float x = l == 0.f ? 0.f : __uint_as_float(o[e]) * inv;
+            odd = fmaf(x, 0.f, odd);
+            o[e] = __float_as_uint(x);
+          }
+          if (live && direct) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              uint4 w;
+              w.x = pack2(__uint_as_float(o[g * 8 + 0]), __uint_as_float(o[g * 8 + 1]));
+              w.y = pack2(__uint_as_float(o[g * 8 + 2]), __uint_as_float(o[g * 8 + 3]));
+              w.z = pack2(__uint_as_float(o[g * 8 + 4]), __uint_as_float(o[g * 8 + 5]));
+              w.w = pack2(__uint_as_float(o[g * 8 + 6]), __uint_as_float(o[g * 8 + 7]));
+              *reinterpret_cast<uint4*>(orow + c + g * 8) = w;
+            }
+          } else if (live) {
+#pragma unroll
+            for (int g = 0; g < 8; ++g)
+              *reinterpret_cast<uint4*>(share + row * D + c + g * 4) = make_uint4(o[g * 4], o[g * 4 + 1], o[g * 4 + 2], o[g * 4 + 3]);
+          }
+        }
+        if (live && direct && a.lse != nullptr) a.lse[out_row * a.H + head] = l == 0.f ? -INFINITY : (m_used + log2f(l)) * LN2;
+        if (live && !direct) *reinterpret_cast<float2*>(share + BLOCK * D + 2 * row) = make_float2(m_used, l);
+      }
+      if (merge) {
+        tc_fence_before();
+        mbar_arrive(x_free);
+      }
+      uint32_t again = __ballot_sync(0xffffffffu, live && odd != odd);
+      while (again) {
+        const int who = __ffs(again) - 1;
+        again &= again - 1;
+        const int w_token = __shfl_sync(0xffffffffu, row_token, who), w_head = __shfl_sync(0xffffffffu, head, who), w_row = quarter * 32 + who;
+        const int w_limit = __shfl_sync(0xffffffffu, limit, who);
+        const int64_t w_out = (int64_t)s.row + tile * a.tile_tokens + w_token;
+        float m, sum, o[D / 32];
+        plain_row<D>(a, s.b, s.h, a.Q + w_out * a.ldq + (int64_t)w_head * D, s.j0 * BLOCK, min(s.j1 * BLOCK, w_limit), m, sum, o);
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) {
+          const int col = lane * (D / 32) + e;
+          if (direct) a.O[w_out * a.ldo + (int64_t)w_head * D + col] = __float2bfloat16_rn(sum == 0.f ? 0.f : o[e] / sum);
+          else share[w_row * D + col] = o[e];
+        }
+        if (lane == 0) {
+          if (direct && a.lse != nullptr) a.lse[w_out * a.H + w_head] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * LN2;
+          if (!direct) *reinterpret_cast<float2*>(share + BLOCK * D + 2 * w_row) = make_float2(m, sum);
+        }
+        __syncwarp();
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {
+    if (threadIdx.x == 0) set_status(a.status, SPTS_ERR_TIMEOUT);
+    const uint64_t t1 = globaltimer_ns();
+    while (globaltimer_ns() - t1 < 200000ull) { }
+    __syncthreads();
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, PA_COLS);
+  }
+}
+
+// Joins the shares of units that several CTAs worked on: blockIdx.x = the CTA in which such a unit begins (its last one), blockIdx.y = which of
+// its rows; a warp per row, the shares in the order of the line.
+constexpr int JOIN_THREADS = 256;
+template <int D>
+__global__ void __launch_bounds__(JOIN_THREADS)
+paged_attn_join_kernel(const __grid_constant__ AttnArgs a) {
+  constexpr int PER = D / 32;
+  __shared__ long long scratch[32 + PREFIX_MAX + 1];
+  __shared__ Segment s_seg;
+  __shared__ int s_last;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, cta = blockIdx.x, ctas = gridDim.x;
+  Line line;
+  line.make<JOIN_THREADS>(a, scratch, false);
+  const long long from = line.cut(cta, ctas), to = line.cut(cta + 1, ctas);
+  if (threadIdx.x == 0) s_last = cta;
+  if (threadIdx.x == 0 && from < to) {
+    Walk w;
+    w.p = line.find(a, to - 1);
+    w.left = 1;
+    w.sequence(a);
+    const long long begin = to - 1 - w.p.j;
+    const bool begins_here = begin >= from;
+    w.p.j = 0;
+    w.left = 1LL << 40;
+    w.next(a, s_seg);
+    int last = cta;
+    if (begins_here)
+      while (line.cut(last + 1, ctas) < begin + s_seg.cost) ++last;
+    s_last = last;                               // == cta: nothing to join
+  }
+  __syncthreads();
+  dep_wait();
+  const int last = s_last;
+  if (last == cta) return;
+  const Segment s = s_seg;
+  const int rows0 = min(a.tile_tokens, s.tokens) * a.G, rows1 = (s.tokens - min(a.tile_tokens, s.tokens)) * a.G, parts = last - cta + 1;
+  for (int r = blockIdx.y * (JOIN_THREADS / 32) + warp; r < rows0 + rows1; r += gridDim.y * (JOIN_THREADS / 32)) {
+    const int tile = r >= rows0 ? 1 : 0, row = r - tile * rows0;
+    // share i: of CTA cta, its last segment; of the others their first
+    const auto share = [&](int i) { return a.share + ((int64_t)(2 * (cta + i) + (i == 0 ? 1 : 0)) * 2 + tile) * share_floats<D>(); };
+    float m = -INFINITY;
+    for (int i = lane; i < parts; i += 32) m = fmaxf(m, __ldcg(share(i) + BLOCK * D + 2 * row));
+    m = warp_max(m);
+    const float b = m == -INFINITY ? 0.f : m;
+    float l = 0.f, o[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) o[e] = 0.f;
+    for (int i0 = 0; i0 < parts; i0 += 32) {
+      float f = 0.f, li = 0.f;
+      if (i0 + lane < parts) {
+        const float2 x = __ldcg(reinterpret_cast<const float2*>(share(i0 + lane) + BLOCK * D + 2 * row));
+        f = ex2(x.x - b);
+        li = x.y * f;
+        if (x.x == -INFINITY) li = x.y;          // nothing was seen (0), or NaN alone
+      }
+      l += warp_sum(li);
+#pragma unroll 4
+      for (int i = i0; i < min(parts, i0 + 32); ++i) {
+        const float fi = __shfl_sync(0xffffffffu, f, i - i0);
+        const float* x = share(i) + row * D + lane * PER;
+        if (PER == 4) {
+          const float4 v = __ldcg(reinterpret_cast<const float4*>(x));
+          if (fi != 0.f) { o[0] = fmaf(v.x, fi, o[0]); o[1] = fmaf(v.y, fi, o[1]); o[PER - 2] = fmaf(v.z, fi, o[PER - 2]); o[PER - 1] = fmaf(v.w, fi, o[PER - 1]); }
+        } else {
+          const float2 v = __ldcg(reinterpret_cast<const float2*>(x));
+          if (fi != 0.f) { o[0] = fmaf(v.x, fi, o[0]); o[1] = fmaf(v.y, fi, o[1]); }
+        }
+      }
+    }
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    const int64_t out_row = (int64_t)s.row + tile * a.tile_tokens + row / a.G;
+    const int head = s.h * a.G + row % a.G;
+    uint32_t* to_o = reinterpret_cast<uint32_t*>(a.O + out_row * a.ldo + (int64_t)head * D) + lane * (PER / 2);
+#pragma unroll
+    for (int e = 0; e < PER / 2; ++e) to_o[e] = l == 0.f ? 0u : pack2(o[2 * e] * inv, o[2 * e + 1] * inv);
+    if (lane == 0 && a.lse != nullptr) a.lse[out_row * a.H + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+  }
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+bool encode(spts_ctx* ctx, CUtensorMap* tm, const void* p, int rank, const cuuint64_t* dim, const cuuint64_t* stride, const cuuint32_t* box) {
+  const cuuint32_t step[3] = {1, 1, 1};
+  return reinterpret_cast<EncodeTiledFn>(ctx->paged_encode)(
+             tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(p), dim, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// K or V of all pages as rows of Hkv * d elements; a box is 64 of a head's dims of the rows of a page (of half a page of 256)
+bool map_pages(spts_ctx* ctx, CUtensorMap* tm, const void* p, const spts_paged_kv* c) {
+  const cuuint64_t width = (cuuint64_t)ctx->desc.n_kv_heads * ctx->desc.head_dim;
+  const cuuint64_t dim[2] = {width, (cuuint64_t)c->n_pages * c->page_size}, stride[1] = {width * 2};
+  const cuuint32_t box[2] = {64, (cuuint32_t)(c->page_size < BLOCK ? c->page_size : BLOCK)};
+  return encode(ctx, tm, p, 2, dim, stride, box);
+}
+// Q as [rows, H, d]; a box is 64 dims of `heads` heads of `tokens` rows
+bool map_queries(spts_ctx* ctx, CUtensorMap* tm, const void* p, int64_t ld, int n_rows, int heads, int tokens) {
+  const cuuint64_t H = ctx->desc.n_q_heads, d = ctx->desc.head_dim;
+  const cuuint64_t dim[3] = {d, H, (cuuint64_t)n_rows}, stride[2] = {d * 2, (cuuint64_t)(n_rows == 1 ? H * d : ld) * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)heads, (cuuint32_t)tokens};
+  return encode(ctx, tm, p, 3, dim, stride, box);
+}
+
+template <int D>
+spts_status attention_t(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start, int n_rows, void* O,
+                        int64_t ldo, float* lse) {
+  AttnArgs a;
+  a.c = make_cache(cache); a.row_start = row_start; a.n_rows = n_rows;
+  a.H = ctx->desc.n_q_heads; a.Hkv = ctx->desc.n_kv_heads; a.G = a.H / a.Hkv;
+  a.tile_tokens = BLOCK / a.G;
+  // two tiles to a unit where sequences have more tokens than one holds, on average
+  a.unit_tokens = n_rows > (int64_t)cache->n_seq * a.tile_tokens ? 2 * a.tile_tokens : a.tile_tokens;
+  a.Q = (const bf16*)Q; a.ldq = ldq; a.O = (bf16*)O; a.ldo = ldo; a.lse = lse;
+  a.share = ctx->ws.paged_part; a.status = ctx->ws.status;
+  CUtensorMap tmQ, tmK, tmV;
+  if (!map_queries(ctx, &tmQ, Q, ldq, n_rows, a.G, a.tile_tokens) || !map_pages(ctx, &tmK, cache->k, cache) || !map_pages(ctx, &tmV, cache->v, cache))
+    return SPTS_ERR_CUDA;
+  const int ctas = ctx->sm_count < PAGED_MAX_CTAS ? ctx->sm_count : PAGED_MAX_CTAS;
+  paged_attn_kernel<D><<<ctas, PA_THREADS, pa_smem<D>(), ctx->stream>>>(tmQ, tmK, tmV, a);
+  SPTS_CUDA_OK(ctx);
+  if (launch_dependent(paged_attn_join_kernel<D>, dim3(ctas, 4), dim3(JOIN_THREADS), ctx->stream, a) != cudaSuccess) return SPTS_ERR_CUDA;
+  ctx->launches++;
+  return SPTS_OK;
+}
+
+}  // namespace
+
+size_t paged_part_floats(const spts_model_desc& d) {
+  if (d.dtype != SPTS_BF16) return 64;
+  return (size_t)4 * PAGED_MAX_CTAS * BLOCK * (d.head_dim + 2);
+}
+
+spts_status paged_tc_init(spts_ctx* ctx) {
+  cudaDriverEntryPointQueryResult q;
+  ctx->paged_encode = nullptr;
+  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ctx->paged_encode, cudaEnableDefault, &q) != cudaSuccess || ctx->paged_encode == nullptr)
+    return SPTS_ERR_CUDA;
+  const bool ok = cudaFuncSetAttribute(paged_attn_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, pa_smem<64>()) == cudaSuccess &&
+                  cudaFuncSetAttribute(paged_attn_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, pa_smem<128>()) == cudaSuccess;
+  return ok ? SPTS_OK : SPTS_ERR_CUDA;
+}
+
+spts_status launch_paged_attention_tc(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start, int n_rows,
+                                      void* O, int64_t ldo, float* lse) {
+  return ctx->desc.head_dim == 64 ? attention_t<64>(ctx, cache, Q, ldq, row_start, n_rows, O, ldo, lse)
+                                  : attention_t<128>(ctx, cache, Q, ldq, row_start, n_rows, O, ldo, lse);
+}
+
+}  // namespace spts

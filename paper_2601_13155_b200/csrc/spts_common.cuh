@@ -136,6 +136,7 @@ struct spts_ctx {
   int sm_count;
   int device;               // the device the context was created on
   void* encode_tiled;       // cuTensorMapEncodeTiled entry point (tensor-core mode)
+  void* paged_encode;       // the same for the paged cache's kernels (bf16, whatever the prefill runs on)
   void* prof;               // per-operation CUDA-event timing (host state)
 };
 
@@ -307,6 +308,9 @@ inline bool paged_tc(const spts_ctx* ctx) {   // heads the tensor-core kernels c
 }
 size_t paged_part_floats(const spts_model_desc& d);
 spts_status paged_init(spts_ctx* ctx);        // kernel attributes, the tensor-map encoder
+spts_status paged_tc_init(spts_ctx* ctx);
+spts_status launch_paged_attention_tc(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start, int n_rows,
+                                      void* O, int64_t ldo, float* lse);
 spts_status launch_paged_append(spts_ctx* ctx, const spts_paged_kv* cache, const void* K, int64_t ldk, const void* V, int64_t ldv,
                                 const int32_t* pos, const int32_t* row_start, const int32_t* at, int n_rows);
 spts_status launch_paged_attention(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start,
