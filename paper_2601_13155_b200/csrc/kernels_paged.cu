@@ -703,6 +703,7 @@ spts_status launch_paged_attention(spts_ctx* ctx, const spts_paged_kv* cache, co
 spts_status launch_paged_weights(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start,
                                  int n_rows, const float* lse, float decay) {
   if (n_rows == 1) ldq = 0;
+  if (paged_tc(ctx)) return launch_paged_weights_tc(ctx, cache, Q, ldq, row_start, n_rows, lse, decay);
   const bool d64 = ctx->desc.head_dim == 64;
   if (ctx->desc.dtype == SPTS_BF16)
     return d64 ? weights_plain_t<bf16, 64>(ctx, cache, Q, ldq, row_start, n_rows, lse, decay)

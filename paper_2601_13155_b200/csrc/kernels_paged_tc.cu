@@ -131,6 +131,11 @@ __device__ long long blocks_before(int n, int off, int R, int g) {
   return sum;
 }
 
+// Where the piece of CTA `cta` begins.  Fewer pieces than CTAs: one to each of the first, so that no CTA between two others is without.
+__device__ __forceinline__ long long cut_line(long long total, int cta, int ctas) {
+  return total >= ctas ? total * cta / ctas : min((long long)cta, total);
+}
+
 struct Place { int b, h, g, j; };              // block j of unit (b, h, g)
 
 struct Line {
@@ -146,8 +151,7 @@ struct Line {
       return n == 0 ? 0LL : a.Hkv * blocks_before(n, held_rows(a.c, b) - n, R, (n + R - 1) / R);
     });
   }
-  // a block to each of the first CTAs where there are fewer blocks than CTAs: no CTA between two others is without one
-  __device__ __forceinline__ long long cut(int cta, int ctas) const { return total >= ctas ? total * cta / ctas : min((long long)cta, total); }
+  __device__ __forceinline__ long long cut(int cta, int ctas) const { return cut_line(total, cta, ctas); }
   __device__ __forceinline__ Place find(const AttnArgs& a, long long x) const {
     Place p;
     p.b = find_share(pre, a.c.n_seq, x);
@@ -786,6 +790,357 @@ paged_attn_join_kernel(const __grid_constant__ AttnArgs a) {
   }
 }
 
+// ------------------------------------------------------------------------------------------------ gathered weights
+// The weight that rows of the cache get needs every query's sum of exponentials first, so it is a second pass over K: S^T = K Q^T with the
+// cache's rows along the 128 lanes of the accumulator, so that a thread owns a row and adds up its exponentials over the columns (queries) without
+// meeting another one.  A unit is two blocks of 128 rows of a sequence, its cost the number of (KV head, tile of queries) that see any of
+// them; all units end to end are cut into equal pieces as in the attention.  The warps of a unit that several CTAs work on leave their sums
+// in the workspace; of each 32 rows the warp that comes last adds them up in the order of the line.
+//   warp 0      TMA producer: for every KV head the two blocks of K (two pairs in flight), for every tile of queries its Q (three)
+//   warp 1      TMEM owner and MMA issuer: two accumulators for each of the two blocks
+//   warps 2-3   -lse log2(e) of a tile's queries into shared memory
+//   warps 4-7   the exponentials of the first block, warps 8-11 of the second
+constexpr int PW_Q = 3;                        // tiles of queries in flight
+template <int D> constexpr int pw_smem() { return 1024 + (4 + PW_Q) * tile_bytes<D>() + 256 + PW_Q * BLOCK * 4 + 64; }
+
+static_assert(pw_smem<128>() <= 232448 && pa_smem<128>() <= 232448, "shared memory of a block");
+
+struct WeightArgs {
+  Cache c;
+  const int32_t* row_start; int n_rows;
+  int H, Hkv, G, tile_tokens;
+  const float* lse;
+  float decay;
+  float* share; int* arrived;                  // [2 * CTAs, 256] sums; [CTAs, 8] warps that left theirs, zero between calls
+  int* status;
+};
+
+// Items of the first u units of a sequence: for each KV head, the tiles of queries that see any of its rows; one for each unit where there are
+// no queries (its weights fade).
+__device__ long long items_before(int n, int off, int tt, int Hkv, int u) {
+  if (n == 0) return u;
+  const int tiles = (n + tt - 1) / tt, u0 = off > 0 ? min(u, (off + 2 * BLOCK - 1) / (2 * BLOCK)) : 0;
+  long long sum = (long long)u * tiles;
+  if (u > u0) sum -= (long long)floor_sum(u - u0, tt, 2 * BLOCK, 2 * BLOCK * u0 - off);
+  return sum * Hkv;
+}
+__device__ __forceinline__ int first_tile(int off, int tt, int u) { return max(0, 2 * BLOCK * u - off) / tt; }
+
+struct Unit {
+  int b, u, i0, i1, cost;                      // items [i0, i1) of `cost`
+  int held, n, off, row;                       // the sequence's rows, its queries, rows before the first query, first query in Q
+  int tile0, tiles;                            // tiles of queries that see the unit's rows, for each head (0: no queries)
+  bool two;                                    // it has a second block
+};
+
+struct UnitWalk {
+  int b, u, i, row, n, off, held;
+  long long left;
+  __device__ __forceinline__ void sequence(const WeightArgs& a) {
+    call_rows(a.row_start, a.n_rows, b, row, n);
+    held = held_rows(a.c, b);
+    off = held - n;
+  }
+  __device__ __forceinline__ bool next(const WeightArgs& a, Unit& s) {
+    if (left <= 0) return false;
+    s.b = b; s.u = u; s.held = held; s.n = n; s.off = off; s.row = row;
+    s.tile0 = n == 0 ? 0 : first_tile(off, a.tile_tokens, u);
+    s.tiles = n == 0 ? 0 : (n + a.tile_tokens - 1) / a.tile_tokens - s.tile0;
+    s.cost = n == 0 ? 1 : s.tiles * a.Hkv;
+    s.i0 = i;
+    s.i1 = (int)min((long long)s.cost, i + left);
+    s.two = held - 2 * BLOCK * u > BLOCK;
+    left -= s.i1 - s.i0;
+    i = 0;
+    if (2 * BLOCK * (u + 1) < held) { ++u; return true; }
+    u = 0;
+    while (left > 0 && ++b < a.c.n_seq) {
+      sequence(a);
+      if (held > 0) break;
+    }
+    return true;
+  }
+};
+
+template <int D>
+__global__ void __launch_bounds__(PA_THREADS, 1)
+paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ WeightArgs a) {
+  constexpr int TILE = tile_bytes<D>(), SLABS = D / 64;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t sK = base, sQ = sK + 4 * TILE, bars = sQ + PW_Q * TILE;
+  const uint32_t k_full = bars, k_free = bars + 16;            // [2] pairs of blocks
+  const uint32_t q_full = bars + 32, q_free = q_full + 8 * PW_Q;
+  const uint32_t e_full = q_free + 8 * PW_Q, e_free = e_full + 8 * PW_Q;      // lse of a tile
+  const uint32_t s_full = e_free + 8 * PW_Q, s_free = s_full + 32;            // [2 blocks][2 accumulators]
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + (bars - base) + 208);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  float* s_lse = reinterpret_cast<float*>(gen + (bars - base) + 256);
+  UnitWalk* start = reinterpret_cast<UnitWalk*>(gen + (bars - base) + 256 + PW_Q * BLOCK * 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    *abort_flag = 0;
+    for (int s = 0; s < 2; ++s) { mbar_init(k_full + 8 * s, 1); mbar_init(k_free + 8 * s, 1); }
+    for (int s = 0; s < PW_Q; ++s) {
+      mbar_init(q_full + 8 * s, 1); mbar_init(q_free + 8 * s, 1);
+      mbar_init(e_full + 8 * s, 64); mbar_init(e_free + 8 * s, 256);
+    }
+    for (int s = 0; s < 4; ++s) { mbar_init(s_full + 8 * s, 1); mbar_init(s_free + 8 * s, 128); }
+    fence_mbar_init();
+    prefetch_tensormap(&tmQ); prefetch_tensormap(&tmK);
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32((const void*)tmem_slot), PA_COLS);
+    tmem_relinquish();
+  }
+  long long from = 0, total = 0;
+  {
+    long long* scratch = reinterpret_cast<long long*>(gen);
+    long long* pre = scratch + 32;
+    total = block_prefix<PA_THREADS>(a.c.n_seq, pre, scratch, [&](int b) {
+      int row, n;
+      call_rows(a.row_start, a.n_rows, b, row, n);
+      if (blockIdx.x == 0) check_starts(a.row_start, a.n_rows, b, a.status);
+      const int held = held_rows(a.c, b);
+      return held == 0 ? 0LL : items_before(n, held - n, a.tile_tokens, a.Hkv, (held + 2 * BLOCK - 1) / (2 * BLOCK));
+    });
+    from = cut_line(total, blockIdx.x, gridDim.x);
+    if (threadIdx.x == 0) {
+      UnitWalk w;
+      w.left = cut_line(total, blockIdx.x + 1, gridDim.x) - from;
+      if (w.left > 0) {
+        w.b = find_share(pre, a.c.n_seq, from);
+        w.sequence(a);
+        const long long x = from - pre[w.b];
+        int lo = 0, hi = (w.held + 2 * BLOCK - 1) / (2 * BLOCK);
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (items_before(w.n, w.off, a.tile_tokens, a.Hkv, mid) <= x) lo = mid; else hi = mid;
+        }
+        w.u = lo;
+        w.i = (int)(x - items_before(w.n, w.off, a.tile_tokens, a.Hkv, lo));
+      }
+      *start = w;
+    }
+    fence_proxy_async_smem();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  UnitWalk walk = *start;
+  Unit s;
+  bool ok = true;
+
+  if (warp == 0) {
+    const int shift = a.c.shift, page = 1 << shift, box = min(page, BLOCK);
+    const uint32_t q_bytes = (uint32_t)(a.G * a.tile_tokens * 128 * SLABS);
+    uint32_t n_k = 0, n_q = 0;
+    while (ok && walk.next(a, s)) {
+      const int32_t* table = a.c.table + (int64_t)s.b * a.c.max_pages;
+      // this lane's boxes of the two blocks
+      int y[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int row = (2 * s.u + t) * BLOCK + lane * box;
+        y[t] = -1;
+        if (lane * box < BLOCK && row < s.held) {
+          const int p = __ldg(table + (row >> shift));
+          if (p < 0 || p >= a.c.n_pages) { set_status(a.status, SPTS_ERR_INDEX); y[t] = a.c.n_pages << shift; }
+          else y[t] = (p << shift) + (row & (page - 1));
+        }
+      }
+      if (s.tiles == 0) continue;
+      const int rows = min(2 * BLOCK, s.held - 2 * BLOCK * s.u), boxes = (rows + box - 1) / box;
+      for (int i = s.i0; i < s.i1 && ok; ++i) {
+        const int h = i / s.tiles, q = s.tile0 + i % s.tiles;
+        if (i == s.i0 || q == s.tile0) {
+          const uint32_t st = n_k & 1, bar = k_full + 8 * st;
+          ok = wait_warp(k_free + 8 * st, ((n_k >> 1) & 1) ^ 1, abort_flag);
+          ++n_k;
+          if (!ok) break;
+          if (lane == 0) mbar_expect_tx(bar, (uint32_t)(boxes * box * 128 * SLABS));
+          __syncwarp();
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+            if (y[t] >= 0)
+              for (int l = 0; l < SLABS; ++l)
+                tma_load_2d(sK + (2 * st + t) * TILE + l * SLAB + lane * box * 128, &tmK, bar, h * D + 64 * l, y[t]);
+        }
+        const uint32_t st = n_q % PW_Q;
+        ok = wait_warp(q_free + 8 * st, ((n_q / PW_Q) & 1) ^ 1, abort_flag);
+        ++n_q;
+        if (ok && lane == 0) {
+          mbar_expect_tx(q_full + 8 * st, q_bytes);
+          for (int l = 0; l < SLABS; ++l)
+            tma_load_3d(sQ + st * TILE + l * SLAB, &tmQ, q_full + 8 * st, 64 * l, h * a.G, s.row + q * a.tile_tokens);
+        }
+        __syncwarp();
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      uint32_t n_k = 0, n_q = 0, n_s[2] = {0, 0};
+      while (ok && walk.next(a, s)) {
+        if (s.tiles == 0) continue;
+        for (int i = s.i0; i < s.i1 && ok; ++i) {
+          const int q = s.tile0 + i % s.tiles, tokens = min(a.tile_tokens, s.n - q * a.tile_tokens);
+          if (i == s.i0 || q == s.tile0) { ok = wait(k_full + 8 * (n_k & 1), (n_k >> 1) & 1, abort_flag); ++n_k; }
+          const uint32_t kst = (n_k - 1) & 1, qst = n_q % PW_Q;
+          ok = ok && wait(q_full + 8 * qst, (n_q / PW_Q) & 1, abort_flag);
+          ++n_q;
+          const int cols = (tokens * a.G + 15) & ~15;
+          const uint32_t idesc = idesc_bf16(BLOCK, 0) | ((uint32_t)(cols >> 3) << 17);
+          for (int t = 0; t < (s.two ? 2 : 1) && ok; ++t) {
+            const uint32_t buf = n_s[t] & 1;
+            ok = wait(s_free + 8 * (2 * t + buf), ((n_s[t] >> 1) & 1) ^ 1, abort_flag);
+            ++n_s[t];
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t kb = sK + (2 * kst + t) * TILE, qb = sQ + qst * TILE;
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+              const uint32_t off = (k >> 2) * SLAB + (k & 3) * 32;
+              mma_bf16(tmem_base + (2 * t + buf) * BLOCK, smem_desc_sw128(kb + off), smem_desc_sw128(qb + off), idesc, k > 0 ? 1u : 0u);
+            }
+            mma_commit(s_full + 8 * (2 * t + buf));
+          }
+          if (!ok) break;
+          mma_commit(q_free + 8 * qst);
+          if (i + 1 == s.i1 || q == s.tile0 + s.tiles - 1) mma_commit(k_free + 8 * kst);
+        }
+      }
+    }
+  } else if (warp < 4) {
+    uint32_t n_q = 0;
+    while (ok && walk.next(a, s)) {
+      if (s.tiles == 0) continue;
+      for (int i = s.i0; i < s.i1 && ok; ++i) {
+        const int h = i / s.tiles, q = s.tile0 + i % s.tiles, tokens = min(a.tile_tokens, s.n - q * a.tile_tokens);
+        const uint32_t st = n_q % PW_Q;
+        const int64_t row = (int64_t)s.row + q * a.tile_tokens;
+        float e[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int c = (warp - 2) * 32 + lane + 64 * u;
+          e[u] = c < tokens * a.G ? -__ldg(a.lse + (row + c / a.G) * a.H + h * a.G + c % a.G) * LOG2E : 0.f;
+          if (e[u] == INFINITY) e[u] = 0.f;    // a query that sees nothing: all its scores become -inf, and stay
+        }
+        ok = wait_warp(e_free + 8 * st, ((n_q / PW_Q) & 1) ^ 1, abort_flag);
+        ++n_q;
+        if (!ok) break;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) s_lse[st * BLOCK + (warp - 2) * 32 + lane + 64 * u] = e[u];
+        mbar_arrive(e_full + 8 * st);
+      }
+    }
+  } else {
+    const int t = (warp - 4) >> 2, quarter = warp & 3;
+    const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
+    const float sc = LOG2E / (D == 128 ? 11.313708498984761f : 8.0f);
+    const float2 sc2 = make_float2(sc, sc);
+    uint32_t n_q = 0, n_s = 0;
+    long long at = from;                       // the line's item at which the segment begins
+    while (ok && walk.next(a, s)) {
+      const int key = (2 * s.u + t) * BLOCK + quarter * 32 + lane;
+      const bool work = t == 0 || s.two;
+      float2 sum[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) sum[u] = make_float2(0.f, 0.f);
+      for (int i = s.i0; i < s.i1 && s.tiles > 0 && ok; ++i) {
+        const int q = s.tile0 + i % s.tiles, tokens = min(a.tile_tokens, s.n - q * a.tile_tokens), cols = tokens * a.G;
+        const uint32_t st = n_q % PW_Q;
+        ok = wait_warp(e_full + 8 * st, (n_q / PW_Q) & 1, abort_flag);
+        ++n_q;
+        if (!ok) break;
+        if (work) {
+          const uint32_t buf = n_s & 1;
+          ok = wait_warp(s_full + 8 * (2 * t + buf), (n_s >> 1) & 1, abort_flag);
+          ++n_s;
+          if (!ok) break;
+          tc_fence_after();
+          // column c is query q tile_tokens + c / G, which sees key if key <= off + query
+          const int from_col = min(max(0, key - s.off - q * a.tile_tokens), BLOCK) * a.G;
+          const bool all = !__any_sync(0xffffffffu, from_col > 0);
+          const uint32_t src = tmem_base + (2 * t + buf) * BLOCK + lane_off;
+          const float4* lse4 = reinterpret_cast<const float4*>(s_lse + st * BLOCK);
+#pragma unroll 1
+          for (int c0 = 0; c0 < cols; c0 += 32) {
+            uint32_t r[32];
+            tmem_ld32(src + c0, r);
+            tmem_ld_wait();
+            if (!all || c0 + 32 > cols) {
+#pragma unroll
+              for (int c = 0; c < 32; ++c)
+                if (c0 + c < from_col || c0 + c >= cols) r[c] = 0xFF800000u;      // -inf
+            }
+#pragma unroll
+            for (int c = 0; c < 32; c += 4) {
+              float4 e = lse4[(c0 + c) >> 2];
+              const float2 x = __ffma2_rn(make_float2(__uint_as_float(r[c]), __uint_as_float(r[c + 1])), sc2, make_float2(e.x, e.y));
+              const float2 y = __ffma2_rn(make_float2(__uint_as_float(r[c + 2]), __uint_as_float(r[c + 3])), sc2, make_float2(e.z, e.w));
+              sum[(c >> 1) & 3] = __fadd2_rn(sum[(c >> 1) & 3], make_float2(ex2(x.x), ex2(x.y)));
+              sum[((c >> 1) + 1) & 3] = __fadd2_rn(sum[((c >> 1) + 1) & 3], make_float2(ex2(y.x), ex2(y.y)));
+            }
+          }
+          tc_fence_before();
+          mbar_arrive(s_free + 8 * (2 * t + buf));
+        }
+        mbar_arrive(e_free + 8 * st);
+      }
+      if (!ok) break;
+      const float2 s01 = __fadd2_rn(sum[0], sum[1]), s23 = __fadd2_rn(sum[2], sum[3]);
+      float w = (s01.x + s01.y) + (s23.x + s23.y);
+      bool write = true;
+      if (s.i0 > 0 || s.i1 < s.cost) {
+        // CTAs whose pieces reach into the unit: the first one's share is its last, the others' their first
+        const long long begin = at - s.i0, end = begin + s.cost;
+        const int mine = blockIdx.x, ctas = gridDim.x;
+        int first = mine, last = mine;
+        while (cut_line(total, first, ctas) > begin) --first;
+        while (cut_line(total, last + 1, ctas) < end) ++last;
+        float* share = a.share + (size_t)(2 * mine + (s.i0 == 0 ? 1 : 0)) * 2 * BLOCK;
+        __stcg(share + t * BLOCK + quarter * 32 + lane, w);
+        __threadfence();
+        __syncwarp();
+        int seen = 0;
+        int* arrived = a.arrived + first * 8 + (warp - 4);
+        if (lane == 0) seen = atomicAdd(arrived, 1);
+        seen = __shfl_sync(0xffffffffu, seen, 0);
+        write = seen == last - first;
+        if (write) {
+          __threadfence();
+          if (lane == 0) *arrived = 0;
+          w = 0.f;
+          for (int c = first; c <= last; ++c)
+            w += __ldcg(a.share + (size_t)(2 * c + (c == first ? 1 : 0)) * 2 * BLOCK + t * BLOCK + quarter * 32 + lane);
+        }
+      }
+      if (write && key < s.held) {
+        const int64_t slot = slot_of(a.c, s.b, key);
+        if (slot >= 0) a.c.weight[slot] = (a.decay == 0.f ? 0.f : a.decay * a.c.weight[slot]) + w / (float)a.H;
+        else set_status(a.status, SPTS_ERR_INDEX);
+      }
+      at += s.i1 - s.i0;
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {
+    if (threadIdx.x == 0) set_status(a.status, SPTS_ERR_TIMEOUT);
+    const uint64_t t1 = globaltimer_ns();
+    while (globaltimer_ns() - t1 < 200000ull) { }
+    __syncthreads();
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, PA_COLS);
+  }
+}
+
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                   const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
@@ -832,6 +1187,27 @@ spts_status attention_t(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q
   return SPTS_OK;
 }
 
+template <int D>
+spts_status weights_t(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start, int n_rows,
+                      const float* lse, float decay) {
+  WeightArgs a;
+  a.c = make_cache(cache); a.row_start = row_start; a.n_rows = n_rows;
+  a.H = ctx->desc.n_q_heads; a.Hkv = ctx->desc.n_kv_heads; a.G = a.H / a.Hkv;
+  // tiles of queries as long as the sequences' chunks on average: a box brings in no more queries than that
+  const int most = BLOCK / a.G, mean = ceil_div(n_rows, cache->n_seq);
+  a.tile_tokens = mean < 1 ? 1 : mean < most ? mean : most;
+  a.lse = lse; a.decay = decay;
+  a.share = ctx->ws.paged_part; a.arrived = ctx->ws.paged_arrived + 64; a.status = ctx->ws.status;
+  CUtensorMap tmQ, tmK;
+  // (without a query no box is read; the map still wants a place)
+  if (!map_queries(ctx, &tmQ, n_rows > 0 ? Q : cache->k, ldq, n_rows > 0 ? n_rows : 1, a.G, a.tile_tokens) || !map_pages(ctx, &tmK, cache->k, cache))
+    return SPTS_ERR_CUDA;
+  const int ctas = ctx->sm_count < PAGED_MAX_CTAS ? ctx->sm_count : PAGED_MAX_CTAS;
+  paged_weights_kernel<D><<<ctas, PA_THREADS, pw_smem<D>(), ctx->stream>>>(tmQ, tmK, a);
+  SPTS_CUDA_OK(ctx);
+  return SPTS_OK;
+}
+
 }  // namespace
 
 size_t paged_part_floats(const spts_model_desc& d) {
@@ -845,7 +1221,9 @@ spts_status paged_tc_init(spts_ctx* ctx) {
   if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ctx->paged_encode, cudaEnableDefault, &q) != cudaSuccess || ctx->paged_encode == nullptr)
     return SPTS_ERR_CUDA;
   const bool ok = cudaFuncSetAttribute(paged_attn_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, pa_smem<64>()) == cudaSuccess &&
-                  cudaFuncSetAttribute(paged_attn_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, pa_smem<128>()) == cudaSuccess;
+                  cudaFuncSetAttribute(paged_attn_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, pa_smem<128>()) == cudaSuccess &&
+                  cudaFuncSetAttribute(paged_weights_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, pw_smem<64>()) == cudaSuccess &&
+                  cudaFuncSetAttribute(paged_weights_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, pw_smem<128>()) == cudaSuccess;
   return ok ? SPTS_OK : SPTS_ERR_CUDA;
 }
 
@@ -853,6 +1231,12 @@ spts_status launch_paged_attention_tc(spts_ctx* ctx, const spts_paged_kv* cache,
                                       void* O, int64_t ldo, float* lse) {
   return ctx->desc.head_dim == 64 ? attention_t<64>(ctx, cache, Q, ldq, row_start, n_rows, O, ldo, lse)
                                   : attention_t<128>(ctx, cache, Q, ldq, row_start, n_rows, O, ldo, lse);
+}
+
+spts_status launch_paged_weights_tc(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start, int n_rows,
+                                    const float* lse, float decay) {
+  return ctx->desc.head_dim == 64 ? weights_t<64>(ctx, cache, Q, ldq, row_start, n_rows, lse, decay)
+                                  : weights_t<128>(ctx, cache, Q, ldq, row_start, n_rows, lse, decay);
 }
 
 }  // namespace spts

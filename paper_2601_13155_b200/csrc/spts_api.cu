@@ -120,7 +120,7 @@ size_t carve(const spts_model_desc& d, int Nmax, void* base, Workspace* ws, std:
   w.kv4_part = c.take<float>((size_t)2 * KV4_MAX_CTAS * 16 * (d.head_dim + 2));
   w.kv4_arrived = c.take<int>(KV4_MAX_CTAS);
   w.paged_part = c.take<float>(paged_part_floats(d));
-  w.paged_arrived = c.take<int>(64);
+  w.paged_arrived = c.take<int>(PAGED_COUNTERS);
   w.evict_bits = c.take<uint32_t>(SPTS_PAGED_MAX_ROWS / 32);
   w.evict_before = c.take<int2>(EVICT_CHUNKS);
   w.evict_total = c.take<int2>((size_t)SPTS_PAGED_MAX_SEQ * EVICT_SPLIT);
@@ -621,7 +621,7 @@ spts_status spts_create(const spts_model_desc* desc, int max_seq, void* workspac
     return SPTS_ERR_CUDA;
   }
   if (spts_status s = paged_init(ctx); s != SPTS_OK) { spts_destroy(ctx); return s; }
-  if (cudaMemsetAsync(ctx->ws.paged_arrived, 0, 64 * sizeof(int), ctx->stream) != cudaSuccess ||
+  if (cudaMemsetAsync(ctx->ws.paged_arrived, 0, PAGED_COUNTERS * sizeof(int), ctx->stream) != cudaSuccess ||
       cudaMemsetAsync(ctx->ws.lp_arrived, 0, LOGITS_MAX_ROWS * sizeof(int), ctx->stream) != cudaSuccess ||
       cudaMemsetAsync(ctx->ws.kv4_arrived, 0, KV4_MAX_CTAS * sizeof(int), ctx->stream) != cudaSuccess ||
       cudaMemsetAsync(ctx->ws.lg_key, 0, LOGITS_MAX_ROWS * sizeof(unsigned long long), ctx->stream) != cudaSuccess ||

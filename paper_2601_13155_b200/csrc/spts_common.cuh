@@ -102,7 +102,7 @@ struct Workspace {
   float* kv4_part;      // [2 * KV4_MAX_CTAS, 16, d + 2] partial results of the attention over a 4-bit cache
   int* kv4_arrived;     // [KV4_MAX_CTAS] CTAs that have left theirs; zero between calls
   float* paged_part;    // [2 * PAGED_MAX_CTAS] shares of attention units that several CTAs work on
-  int* paged_arrived;   // [64] blocks of a call that are done; zero between calls
+  int* paged_arrived;   // [PAGED_COUNTERS] blocks of an append that are done, warps that left their share of a sum; zero between calls
   uint32_t* evict_bits; // [SPTS_PAGED_MAX_ROWS / 32] rows that stay
   int2* evict_before;   // [EVICT_CHUNKS] holes and movers before each chunk of rows, within the part of a sequence that one CTA ranked
   int2* evict_total;    // [SPTS_PAGED_MAX_SEQ, EVICT_SPLIT] holes and movers of each part
@@ -151,6 +151,7 @@ static const size_t W4_PART_FLOATS = (size_t)2 * W4_MAX_CTAS * 16 * 256;
 static const int LOGITS_MAX_ROWS = 1024;      // rows of logits per launch
 static const int KV4_MAX_CTAS = 320;          // CTAs of the attention over a 4-bit cache: one or two per SM
 static const int PAGED_MAX_CTAS = 160;        // CTAs of the attention over a paged cache: one per SM
+static const int PAGED_COUNTERS = 64 + 8 * PAGED_MAX_CTAS;
 static const int EVICT_CHUNK = 256;           // rows of a chunk of the eviction
 static const int EVICT_SPLIT = 8;             // CTAs that rank one sequence's rows at most (a portable cluster)
 static const int EVICT_CHUNKS = SPTS_PAGED_MAX_ROWS / EVICT_CHUNK;
@@ -311,6 +312,8 @@ spts_status paged_init(spts_ctx* ctx);        // kernel attributes, the tensor-m
 spts_status paged_tc_init(spts_ctx* ctx);
 spts_status launch_paged_attention_tc(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start, int n_rows,
                                       void* O, int64_t ldo, float* lse);
+spts_status launch_paged_weights_tc(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start, int n_rows,
+                                    const float* lse, float decay);
 spts_status launch_paged_append(spts_ctx* ctx, const spts_paged_kv* cache, const void* K, int64_t ldk, const void* V, int64_t ldv,
                                 const int32_t* pos, const int32_t* row_start, const int32_t* at, int n_rows);
 spts_status launch_paged_attention(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start,
