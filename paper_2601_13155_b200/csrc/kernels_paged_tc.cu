@@ -15,6 +15,8 @@
 // The two slots are the unit's two tiles, which share every block of K and V, or, where it has one tile, two neighbouring blocks of the cache
 // (joined at the end of the unit): either way the tensor core has the other slot's products while one slot's softmax runs.
 // P V reads V as it lies in the pages (row = token): its operand is the transposed one, 128-byte swizzled with the head dims along the row.
+#include <climits>
+
 #include "paged_common.cuh"
 #include "tc_ptx.cuh"
 
@@ -26,11 +28,12 @@ using namespace paged;
 using namespace ptx;
 
 constexpr int BLOCK = 128;                     // rows of the cache to a block, rows of a score tile
-constexpr int SLAB = BLOCK * 128;              // [128 rows x 64 bf16], 128-byte swizzle
+constexpr int SLAB = BLOCK * 128;              // a tile of Q: [128 rows x 64 bf16] for each 64 dims, 128-byte swizzle
 constexpr int RING = 5;                        // tiles of K or V in flight
 constexpr int PA_THREADS = 384;
 constexpr int PA_COLS = 512;
 constexpr int REGS_LIGHT = 72, REGS_SOFTMAX = 216;   // 128 * 72 + 256 * 216 = 384 * 168, the launch's total
+constexpr int SOLO_ROWS = 16;                  // rows of a unit, on average, up to which it is joined within the kernel
 constexpr float RESCALE = 8.0f;                // log2 units the running maximum may lag behind
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
@@ -45,7 +48,8 @@ struct AttnArgs {
   int tile_tokens, unit_tokens;                // floor(128 / G); that or twice that
   const bf16* Q; int64_t ldq;
   bf16* O; int64_t ldo; float* lse;
-  float* share;
+  float* share; int* arrived;
+  int solo;                                    // units are joined by the CTA that is done last instead of a second kernel
   int* status;
 };
 
@@ -69,10 +73,41 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm,
       ::"r"(dst), "l"(tm), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
       : "memory");
 }
-// Operand whose rows run along K (tokens) and whose 128-byte rows hold 64 of the N (head dims): 8-row groups 1024 bytes apart, the next
-// 64 of N one slab behind; a K step of 16 is two groups.
-__device__ __forceinline__ uint64_t smem_desc_rows_along_k(uint32_t saddr) {
-  return smem_desc_sw128(saddr) | ((uint64_t)(SLAB >> 4) << 16);
+// Tiles of K and V in shared memory: [128 / 8 groups of rows][D / 64][8 rows][64 bf16], so that one box brings in all dims of the rows of a
+// page, 128-byte swizzled.  As K-major operand (rows = N or M): the next eight rows are a group further.  As the operand of P V (rows
+// along K, dims along N): the next eight of K are a group further, the next 64 of N 1024 bytes.
+// A descriptor's low word holds the address / 16, so it moves by additions; its high word is constant.
+template <int D> constexpr int group_bytes() { return D / 64 * 1024; }
+constexpr uint32_t desc_high(int stride_bytes) { return (uint32_t)(stride_bytes >> 4) | (1u << 14) | (2u << 29); }
+__device__ __forceinline__ uint32_t desc_low(uint32_t saddr, int leading_bytes) { return ((saddr & 0x3FFFFu) >> 4) | ((uint32_t)(leading_bytes >> 4) << 16); }
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      ".reg .b64 da, db;\n"
+      "mov.b64 da, {%1, %2};\n"
+      "mov.b64 db, {%3, %4};\n"
+      "setp.ne.b32 p, %6, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p;\n"
+      "}\n" ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"((uint32_t)accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      ".reg .b64 db;\n"
+      "mov.b64 db, {%2, %3};\n"
+      "setp.ne.b32 p, %5, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n"
+      "}\n" ::"r"(d), "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"((uint32_t)accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1, int c2, int c3) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+      ::"r"(dst), "l"(tm), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+      : "memory");
 }
 constexpr uint32_t B_ALONG_N = 1u << 16;       // instruction descriptor: B is stored N-contiguous
 
@@ -132,8 +167,17 @@ __device__ long long blocks_before(int n, int off, int R, int g) {
 }
 
 // Where the piece of CTA `cta` begins.  Fewer pieces than CTAs: one to each of the first, so that no CTA between two others is without.
+// (Divisions of 64 bits cost a microsecond together: lines of ordinary length are cut in 32.)
 __device__ __forceinline__ long long cut_line(long long total, int cta, int ctas) {
-  return total >= ctas ? total * cta / ctas : min((long long)cta, total);
+  if (total < ctas) return min((long long)cta, total);
+  if (total < 1 << 23) return (uint32_t)total * (uint32_t)cta / (uint32_t)ctas;
+  return total * cta / ctas;
+}
+// The CTA whose piece holds block x: the largest c with cut_line(c) <= x, that is total c / ctas < x + 1.
+__device__ __forceinline__ int cta_of(long long total, long long x, int ctas) {
+  if (total < ctas) return (int)x;
+  if (total < 1 << 23) return (int)((((uint32_t)x + 1) * (uint32_t)ctas - 1) / (uint32_t)total);
+  return (int)(((x + 1) * ctas - 1) / total);
 }
 
 struct Place { int b, h, g, j; };              // block j of unit (b, h, g)
@@ -158,9 +202,16 @@ struct Line {
     int first, n;
     call_rows(a.row_start, a.n_rows, p.b, first, n);
     const int off = held_rows(a.c, p.b) - n, R = a.unit_tokens;
-    const long long head = (pre[p.b + 1] - pre[p.b]) / a.Hkv;
+    const long long all = pre[p.b + 1] - pre[p.b];
     x -= pre[p.b];
-    p.h = (int)(x / head);
+    long long head;
+    if (all < 1LL << 31) {
+      head = (uint32_t)all / (uint32_t)a.Hkv;
+      p.h = (int)((uint32_t)x / (uint32_t)head);
+    } else {
+      head = all / a.Hkv;
+      p.h = (int)(x / head);
+    }
     x -= p.h * head;
     int lo = 0, hi = (n + R - 1) / R;
     while (hi - lo > 1) {
@@ -168,7 +219,7 @@ struct Line {
       if (blocks_before(n, off, R, mid) <= x) lo = mid; else hi = mid;
     }
     p.g = lo;
-    p.j = (int)(x - blocks_before(n, off, R, lo));
+    p.j = (int)(lo == 0 ? x : x - blocks_before(n, off, R, lo));
     return p;
   }
 };
@@ -250,7 +301,58 @@ __device__ __noinline__ void plain_row(const AttnArgs& a, int b, int kvh, const 
   }
 }
 
+// ------------------------------------------------------------------------------------------------ joining shares
+// Row `row` of a tile of a unit that CTAs first .. last worked on, by one warp: the shares in the order of the line (of the first CTA its last
+// segment, of the others their first).
+template <int D>
+__device__ __forceinline__ void join_row(const AttnArgs& a, const Segment& s, int first, int last, int tile, int row) {
+  constexpr int PER = D / 32;
+  const int lane = threadIdx.x & 31, parts = last - first + 1;
+  const auto share = [&](int i) { return a.share + ((int64_t)(2 * (first + i) + (i == 0 ? 1 : 0)) * 2 + tile) * share_floats<D>(); };
+  float m = -INFINITY;
+  for (int i = lane; i < parts; i += 32) m = fmaxf(m, __ldcg(share(i) + BLOCK * D + 2 * row));
+  m = warp_max(m);
+  const float b = m == -INFINITY ? 0.f : m;
+  float l = 0.f, o[PER];
+#pragma unroll
+  for (int e = 0; e < PER; ++e) o[e] = 0.f;
+  for (int i0 = 0; i0 < parts; i0 += 32) {
+    float f = 0.f, li = 0.f;
+    if (i0 + lane < parts) {
+      const float2 x = __ldcg(reinterpret_cast<const float2*>(share(i0 + lane) + BLOCK * D + 2 * row));
+      f = ex2(x.x - b);
+      li = x.y * f;
+      if (x.x == -INFINITY) li = x.y;          // nothing was seen (0), or NaN alone
+    }
+    l += warp_sum(li);
+#pragma unroll 8
+    for (int i = i0; i < min(parts, i0 + 32); ++i) {
+      const float fi = __shfl_sync(0xffffffffu, f, i - i0);
+      const float* x = share(i) + row * D + lane * PER;
+      float v[PER];
+      if (PER == 4) {
+        const float4 y = __ldcg(reinterpret_cast<const float4*>(x));
+        v[0] = y.x; v[1] = y.y; v[PER - 2] = y.z; v[PER - 1] = y.w;
+      } else {
+        const float2 y = __ldcg(reinterpret_cast<const float2*>(x));
+        v[0] = y.x; v[1] = y.y;
+      }
+#pragma unroll
+      for (int e = 0; e < PER; ++e) o[e] = fi == 0.f ? o[e] : fmaf(v[e], fi, o[e]);
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  const int64_t out_row = (int64_t)s.row + tile * a.tile_tokens + row / a.G;
+  const int head = s.h * a.G + row % a.G;
+  uint32_t* to_o = reinterpret_cast<uint32_t*>(a.O + out_row * a.ldo + (int64_t)head * D) + lane * (PER / 2);
+#pragma unroll
+  for (int e = 0; e < PER / 2; ++e) to_o[e] = l == 0.f ? 0u : pack2(o[2 * e] * inv, o[2 * e + 1] * inv);
+  if (lane == 0 && a.lse != nullptr) a.lse[out_row * a.H + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+}
+
 // ------------------------------------------------------------------------------------------------ the kernel
+struct Start { Walk walk; long long from, total; };      // a CTA's piece
+
 template <int D>
 __global__ void __launch_bounds__(PA_THREADS, 1)
 paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
@@ -271,7 +373,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + (bars - base) + 384);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   float2* ml = reinterpret_cast<float2*>(gen + (bars - base) + 512);
-  Walk* start = reinterpret_cast<Walk*>(gen + (bars - base) + 512 + 1024);
+  const uint32_t g_done = x_free + 8;          // [2 slots] the slot's threads are at the same point
+  volatile int* g_last = abort_flag + 1;       // [2 slots] the slot's share was the last of its unit
+  Start* start = reinterpret_cast<Start*>(gen + (bars - base) + 512 + 1024);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -285,7 +389,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       mbar_init(full + 8 * s, 1); mbar_init(free_ + 8 * s, 1);
       mbar_init(v_tail + 8 * s, 1); mbar_init(v_clean + 8 * s, 32);
     }
-    mbar_init(x_full, 128); mbar_init(x_free, 128);
+    mbar_init(x_full, 128); mbar_init(x_free, 128); mbar_init(g_done, 128); mbar_init(g_done + 8, 128);
     fence_mbar_init();
     prefetch_tensormap(&tmQ); prefetch_tensormap(&tmK); prefetch_tensormap(&tmV);
   }
@@ -302,7 +406,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       Walk w;
       w.left = to - from;
       if (w.left > 0) { w.p = line.find(a, from); w.sequence(a); }
-      *start = w;
+      *start = {w, from, line.total};
     }
     fence_proxy_async_smem();
   }
@@ -310,7 +414,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  Walk walk = *start;
+  Walk walk = start->walk;
   Segment s;
 
   // The order of the ring's tiles within a segment of nb blocks: with two tiles K_0, V_0, K_1, V_1, ...; with one (slots on neighbouring
@@ -320,7 +424,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     if (warp == 0) {
       const int shift = a.c.shift, page = 1 << shift, box = min(page, BLOCK);     // rows of a box
       const uint32_t q_bytes = (uint32_t)(a.G * a.tile_tokens * 128 * SLABS);
-      uint32_t slot = 0, phase = 1, q_used[2] = {0, 0}, q_next = 0;
+      uint32_t slot = 0, phase = 1, q_phase = 3, q_next = 0;     // (q_phase: a bit for each place)
       bool ok = true;
       while (ok && walk.next(a, s)) {
         const int nb = s.j1 - s.j0, ahead = s.two ? 1 : 2;
@@ -337,8 +441,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         int y0 = place(s.j0), y1 = place(s.j0 + 1), y2 = place(s.j0 + 2);
         for (int t = 0; t < (s.two ? 2 : 1); ++t) {
           const int buf = s.two ? t : (int)q_next;
-          ok = ok && wait_warp(q_free + 8 * buf, (q_used[buf] & 1) ^ 1, abort_flag);
-          ++q_used[buf];
+          ok = ok && wait_warp(q_free + 8 * buf, (q_phase >> buf) & 1, abort_flag);
+          q_phase ^= 1u << buf;
           if (ok && lane == 0) {
             mbar_expect_tx(q_full + 8 * buf, q_bytes);
             for (int h = 0; h < SLABS; ++h)
@@ -350,15 +454,14 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           ok = ok && wait_warp(free_ + 8 * slot, phase, abort_flag);
           if (!ok) return;
           const int rows = max(0, min(BLOCK, s.held - j * BLOCK)), boxes = (rows + box - 1) / box;
-          const uint32_t bar = full + 8 * slot, dst = sR + slot * TILE + lane * box * 128;
+          const uint32_t bar = full + 8 * slot;
           if (lane == 0) {
             if (boxes > 0) mbar_expect_tx(bar, (uint32_t)(boxes * box * 128 * SLABS));
             else mbar_arrive(bar);
             if (is_v && rows < BLOCK) mbar_arrive(v_tail + 8 * slot);
           }
           __syncwarp();
-          if (y >= 0)
-            for (int h = 0; h < SLABS; ++h) tma_load_2d(dst + h * SLAB, is_v ? &tmV : &tmK, bar, s.h * D + 64 * h, y);
+          if (y >= 0) tma_load_4d(sR + slot * TILE + lane * box * 128 * SLABS, is_v ? &tmV : &tmK, bar, 0, 0, s.h * SLABS, y >> 3);
           if (++slot == RING) { slot = 0; phase ^= 1; }
         };
         load(false, s.j0, y0);
@@ -371,105 +474,123 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       }
     } else if (warp == 1) {
       if (lane == 0) {
+        // This thread's instructions are what bounds long chunks, so its state is a handful of registers: descriptors advance by additions,
+        // phases are bits.
         constexpr uint32_t idesc_s = idesc_bf16(BLOCK, BLOCK), idesc_o = idesc_bf16(BLOCK, D) | B_ALONG_N;
-        uint32_t slot = 0, phase = 0, q_used[2] = {0, 0}, q_next = 0, pv[2] = {0, 0}, clean = 0, turn = 0;   // (clean: a phase for each place)
+        constexpr uint32_t q_hi = desc_high(1024), k_hi = desc_high(group_bytes<D>());
+        const uint32_t q_lo = desc_low(sQ, 0), k_lo = desc_low(sR, 0), v_lo = desc_low(sR, 1024);
+        uint32_t slot = 0, phase = 0, clean = 0;         // the ring's place; phases of v_clean
+        uint32_t bits = 0;                               // phases: 0, 1 of p_full; 2, 3 of q_full
+        uint32_t turn = 0, q_next = 0;
         bool ok = true;
-        auto take = [&]() -> uint32_t {          // the ring's next tile
-          ok = ok && wait(full + 8 * slot, phase, abort_flag);
-          const uint32_t at = slot;
+        const auto next_slot = [&]() {
           if (++slot == RING) { slot = 0; phase ^= 1; }
-          return at;
         };
-        auto take_v = [&](bool tail) -> uint32_t {
-          if (!tail) return take();
-          ok = ok && wait(v_clean + 8 * slot, (clean >> slot) & 1, abort_flag);
-          clean ^= 1u << slot;
-          const uint32_t at = slot;
-          if (++slot == RING) { slot = 0; phase ^= 1; }
-          return at;
-        };
-        auto qk = [&](int t, int buf, uint32_t at) {
-          const uint32_t kb = sR + at * TILE, qb = sQ + buf * TILE;
-#pragma unroll
-          for (int k = 0; k < D / 16; ++k) {
-            const uint32_t off = (k >> 2) * SLAB + (k & 3) * 32;
-            mma_bf16(tmem_base + t * BLOCK, smem_desc_sw128(qb + off), smem_desc_sw128(kb + off), idesc_s, k > 0 ? 1u : 0u);
+        // the ring's next tile has come (a tail of V: has been cleared)
+        const auto wait_tile = [&]() { ok = ok && wait(full + 8 * slot, phase, abort_flag); };
+        const auto wait_v = [&](bool tail) {
+          if (tail) {
+            ok = ok && wait(v_clean + 8 * slot, (clean >> slot) & 1, abort_flag);
+            clean ^= 1u << slot;
+          } else {
+            wait_tile();
           }
+        };
+        const auto qk = [&](int t, uint32_t q, uint32_t k) {
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i)
+            mma_ss(tmem_base + t * BLOCK, q + (((i >> 2) * SLAB + (i & 3) * 32) >> 4), q_hi, k + (((i >> 2) * 1024 + (i & 3) * 32) >> 4), k_hi, idesc_s, i > 0);
           mma_commit(s_full + 8 * t);
         };
         // O_t += P_t V, P_t read from the columns of S_t, in the halves in which the softmax warps hand it over
-        auto pv_mma = [&](int t, uint32_t at, bool first) {
-          const uint32_t vb = sR + at * TILE;
+        const auto pv = [&](int t, uint32_t v, bool first) {
+          const uint32_t ph = (bits >> t) & 1;
+          bits ^= 1u << t;
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
-            ok = ok && wait(p_full + 8 * (2 * t + half), pv[t] & 1, abort_flag);
+            ok = ok && wait(p_full + 8 * (2 * t + half), ph, abort_flag);
             if (!ok) return;
             tc_fence_after();
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {
-              const int k = 4 * half + kk;
-              mma_bf16_tmem_a(tmem_base + 2 * BLOCK + t * BLOCK, tmem_base + t * BLOCK + 8 * k, smem_desc_rows_along_k(vb + k * 2048), idesc_o,
-                              first && k == 0 ? 0u : 1u);
-            }
+            for (int i = 4 * half; i < 4 * half + 4; ++i)
+              mma_ts(tmem_base + 2 * BLOCK + t * BLOCK, tmem_base + t * BLOCK + 8 * i, v + i * (2 * group_bytes<D>() >> 4), k_hi, idesc_o, !first || i > 0);
           }
-          ++pv[t];
         };
         while (ok && walk.next(a, s)) {
           const int nb = s.j1 - s.j0;
           const bool tail = s.j1 * BLOCK > s.held;
           if (s.two) {
-            for (int t = 0; t < 2; ++t) { ok = ok && wait(q_full + 8 * t, q_used[t] & 1, abort_flag); ++q_used[t]; }
-            const uint32_t k0 = take();
+            ok = ok && wait(q_full, (bits >> 2) & 1, abort_flag) && wait(q_full + 8, (bits >> 3) & 1, abort_flag);
+            bits ^= 12;
+            wait_tile();
             if (!ok) break;
             tc_fence_after();
-            qk(0, 0, k0);
-            qk(1, 1, k0);
-            mma_commit(free_ + 8 * k0);
-            if (nb == 1) { mma_commit(q_free); mma_commit(q_free + 8); }
-            for (int i = 0; i < nb && ok; ++i) {
-              const bool more = i + 1 < nb;
-              const uint32_t v = take_v(tail && !more), k = more ? take() : 0;
+            const uint32_t k0 = k_lo + slot * (TILE >> 4);
+            qk(0, q_lo, k0);
+            qk(1, q_lo + (TILE >> 4), k0);
+            mma_commit(free_ + 8 * slot);
+            next_slot();
+            for (int i = 0; i + 1 < nb; ++i) {
+              wait_v(false);
+              const uint32_t v = v_lo + slot * (TILE >> 4), v_free = free_ + 8 * slot;
+              next_slot();
+              wait_tile();
+              const uint32_t k = k_lo + slot * (TILE >> 4), k_free = free_ + 8 * slot;
+              next_slot();
               if (!ok) break;
-              for (int t = 0; t < 2 && ok; ++t) {
-                pv_mma(t, v, i == 0);
-                if (!ok) break;
-                if (more) qk(t, t, k);           // (its commit also covers P_t V: O_t rests when S_t arrives)
-                else mma_commit(o_full + 8 * t);
-              }
+              pv(0, v, i == 0);
               if (!ok) break;
-              mma_commit(free_ + 8 * v);
-              if (more) mma_commit(free_ + 8 * k);
-              if (i + 2 == nb) { mma_commit(q_free); mma_commit(q_free + 8); }
-            }
-          } else {
-            const int buf = (int)q_next;
-            q_next ^= 1;
-            ok = ok && wait(q_full + 8 * buf, q_used[buf] & 1, abort_flag);
-            ++q_used[buf];
-            for (int i = 0; i < 2 && i < nb; ++i) {
-              const uint32_t k = take();
+              qk(0, q_lo, k);                    // (its commit also covers P_t V: O_t rests when S_t arrives)
+              pv(1, v, i == 0);
               if (!ok) break;
-              tc_fence_after();
-              qk((i + turn) & 1, buf, k);
-              mma_commit(free_ + 8 * k);
+              qk(1, q_lo + (TILE >> 4), k);
+              mma_commit(v_free);
+              mma_commit(k_free);
             }
             if (!ok) break;
-            if (nb <= 2) mma_commit(q_free + 8 * buf);
-            for (int i = 0; i < nb && ok; ++i) {
+            mma_commit(q_free);
+            mma_commit(q_free + 8);
+            wait_v(tail);
+            const uint32_t v = v_lo + slot * (TILE >> 4);
+            if (!ok) break;
+            pv(0, v, nb == 1);
+            mma_commit(o_full);
+            if (!ok) break;
+            pv(1, v, nb == 1);
+            mma_commit(o_full + 8);
+            mma_commit(free_ + 8 * slot);
+            next_slot();
+          } else {
+            const uint32_t q = q_lo + q_next * (TILE >> 4), qf = q_free + 8 * q_next;
+            ok = ok && wait(q_full + 8 * q_next, (bits >> (2 + q_next)) & 1, abort_flag);
+            bits ^= 4u << q_next;
+            q_next ^= 1;
+            for (int i = 0; i < 2 && i < nb; ++i) {
+              wait_tile();
+              if (!ok) break;
+              tc_fence_after();
+              qk((i + turn) & 1, q, k_lo + slot * (TILE >> 4));
+              mma_commit(free_ + 8 * slot);
+              next_slot();
+            }
+            if (!ok) break;
+            if (nb <= 2) mma_commit(qf);
+            for (int i = 0; i < nb; ++i) {
               const int t = (i + turn) & 1;
-              const bool more = i + 2 < nb;
-              const uint32_t v = take_v(tail && i + 1 == nb);
+              wait_v(tail && i + 1 == nb);
               if (!ok) break;
-              pv_mma(t, v, i < 2);
+              pv(t, v_lo + slot * (TILE >> 4), i < 2);
               if (!ok) break;
-              mma_commit(free_ + 8 * v);
-              if (more) {
-                const uint32_t k = take();
+              mma_commit(free_ + 8 * slot);
+              next_slot();
+              if (i + 2 < nb) {
+                wait_tile();
                 if (!ok) break;
                 tc_fence_after();
-                qk(t, buf, k);
-                mma_commit(free_ + 8 * k);
-                if (i + 3 == nb) mma_commit(q_free + 8 * buf);
+                qk(t, q, k_lo + slot * (TILE >> 4));
+                mma_commit(free_ + 8 * slot);
+                next_slot();
+                if (i + 3 == nb) mma_commit(qf);
               } else {
                 mma_commit(o_full + 8 * t);
               }
@@ -491,8 +612,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         if (!ok) break;
         const int rows = max(0, s.held - (s.j1 - 1) * BLOCK);
         for (int h = 0; h < SLABS; ++h)
-          for (int i = rows * 8 + lane; i < BLOCK * 8; i += 32)
-            *reinterpret_cast<uint4*>(gen + (sR - base) + slot * TILE + h * SLAB + i * 16) = make_uint4(0, 0, 0, 0);
+          for (int i = rows * 8 + lane; i < BLOCK * 8; i += 32)      // 16 bytes of row i / 8
+            *reinterpret_cast<uint4*>(gen + (sR - base) + slot * TILE + (i >> 6) * group_bytes<D>() + h * 1024 + (i & 63) * 16) = make_uint4(0, 0, 0, 0);
         fence_proxy_async_smem();
         mbar_arrive(v_clean + 8 * slot);
       }
@@ -507,15 +628,18 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     const uint32_t tS = tmem_base + t * BLOCK + lane_off, tO = tmem_base + 2 * BLOCK + t * BLOCK + lane_off;
     const float sc = LOG2E / (D == 128 ? 11.313708498984761f : 8.0f);
     const float2 sc2 = make_float2(sc, sc);
-    uint32_t n_s = 0, n_o = 0, n_x = 0, turn = 0;
+    uint32_t n_s = 0, n_o = 0, n_x = 0, n_g = 0, turn = 0;
+    long long at = start->from;                        // the line's block at which the segment ends
     bool ok = true;
     while (ok && walk.next(a, s)) {
+      at += s.j1 - s.j0;
       const int nb = s.j1 - s.j0, tile = s.two ? t : 0;
       const int tokens = min(a.tile_tokens, s.tokens - tile * a.tile_tokens);
       const int token = s.token + tile * a.tile_tokens + row_token;        // in the sequence
       const bool live = row_token < tokens;
       const bool any_live = quarter * 32 < tokens * a.G;                   // of this warp
-      const int limit = live ? max(0, s.off + token + 1) : 0;              // rows that this query sees
+      // rows that this query sees (a row of no query is not masked: nothing of it is used, and its warp need not look)
+      const int limit = live ? max(0, s.off + token + 1) : INT_MAX;
       float m_used = -INFINITY, l = 0.f;
       int done = 0;
       for (int i = s.two ? 0 : ((t + turn) & 1); i < nb && ok; i += s.two ? 1 : 2) {
@@ -694,6 +818,29 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
         __syncwarp();
       }
+      if (!direct && a.solo) {
+        // the CTA that leaves the unit's last share joins it, a warp to a row
+        const long long begin = at - s.j1, total = start->total;
+        const int ctas = gridDim.x, first = cta_of(total, begin, ctas), last = cta_of(total, begin + s.cost - 1, ctas);
+        __threadfence();
+        mbar_arrive(g_done + 8 * t);
+        ok = wait_warp(g_done + 8 * t, n_g & 1, abort_flag);
+        ++n_g;
+        if (!ok) break;
+        if (row == 0) {
+          const bool is_last = atomicAdd(a.arrived + 8 * first, 1) == last - first;
+          if (is_last) a.arrived[8 * first] = 0;
+          g_last[t] = is_last;
+        }
+        mbar_arrive(g_done + 8 * t);
+        ok = wait_warp(g_done + 8 * t, n_g & 1, abort_flag);
+        ++n_g;
+        if (!ok) break;
+        if (g_last[t]) {
+          __threadfence();
+          for (int r = quarter; r < s.tokens * a.G; r += 4) join_row<D>(a, s, first, last, 0, r);
+        }
+      }
     }
   }
 
@@ -713,15 +860,14 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 
 // Joins the shares of units that several CTAs worked on: blockIdx.x = the CTA in which such a unit begins (its last one), blockIdx.y = which of
 // its rows; a warp per row, the shares in the order of the line.
-constexpr int JOIN_THREADS = 256;
+constexpr int JOIN_THREADS = 256, JOIN_SPLIT = 16;     // a unit's 256 rows: two to a warp
 template <int D>
 __global__ void __launch_bounds__(JOIN_THREADS)
 paged_attn_join_kernel(const __grid_constant__ AttnArgs a) {
-  constexpr int PER = D / 32;
   __shared__ long long scratch[32 + PREFIX_MAX + 1];
   __shared__ Segment s_seg;
   __shared__ int s_last;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, cta = blockIdx.x, ctas = gridDim.x;
+  const int warp = threadIdx.x >> 5, cta = blockIdx.x, ctas = gridDim.x;
   Line line;
   line.make<JOIN_THREADS>(a, scratch, false);
   const long long from = line.cut(cta, ctas), to = line.cut(cta + 1, ctas);
@@ -736,58 +882,16 @@ paged_attn_join_kernel(const __grid_constant__ AttnArgs a) {
     w.p.j = 0;
     w.left = 1LL << 40;
     w.next(a, s_seg);
-    int last = cta;
-    if (begins_here)
-      while (line.cut(last + 1, ctas) < begin + s_seg.cost) ++last;
-    s_last = last;                               // == cta: nothing to join
+    if (begins_here) s_last = cta_of(line.total, begin + s_seg.cost - 1, ctas);      // == cta: nothing to join
   }
   __syncthreads();
   dep_wait();
   const int last = s_last;
   if (last == cta) return;
   const Segment s = s_seg;
-  const int rows0 = min(a.tile_tokens, s.tokens) * a.G, rows1 = (s.tokens - min(a.tile_tokens, s.tokens)) * a.G, parts = last - cta + 1;
-  for (int r = blockIdx.y * (JOIN_THREADS / 32) + warp; r < rows0 + rows1; r += gridDim.y * (JOIN_THREADS / 32)) {
-    const int tile = r >= rows0 ? 1 : 0, row = r - tile * rows0;
-    // share i: of CTA cta, its last segment; of the others their first
-    const auto share = [&](int i) { return a.share + ((int64_t)(2 * (cta + i) + (i == 0 ? 1 : 0)) * 2 + tile) * share_floats<D>(); };
-    float m = -INFINITY;
-    for (int i = lane; i < parts; i += 32) m = fmaxf(m, __ldcg(share(i) + BLOCK * D + 2 * row));
-    m = warp_max(m);
-    const float b = m == -INFINITY ? 0.f : m;
-    float l = 0.f, o[PER];
-#pragma unroll
-    for (int e = 0; e < PER; ++e) o[e] = 0.f;
-    for (int i0 = 0; i0 < parts; i0 += 32) {
-      float f = 0.f, li = 0.f;
-      if (i0 + lane < parts) {
-        const float2 x = __ldcg(reinterpret_cast<const float2*>(share(i0 + lane) + BLOCK * D + 2 * row));
-        f = ex2(x.x - b);
-        li = x.y * f;
-        if (x.x == -INFINITY) li = x.y;          // nothing was seen (0), or NaN alone
-      }
-      l += warp_sum(li);
-#pragma unroll 4
-      for (int i = i0; i < min(parts, i0 + 32); ++i) {
-        const float fi = __shfl_sync(0xffffffffu, f, i - i0);
-        const float* x = share(i) + row * D + lane * PER;
-        if (PER == 4) {
-          const float4 v = __ldcg(reinterpret_cast<const float4*>(x));
-          if (fi != 0.f) { o[0] = fmaf(v.x, fi, o[0]); o[1] = fmaf(v.y, fi, o[1]); o[PER - 2] = fmaf(v.z, fi, o[PER - 2]); o[PER - 1] = fmaf(v.w, fi, o[PER - 1]); }
-        } else {
-          const float2 v = __ldcg(reinterpret_cast<const float2*>(x));
-          if (fi != 0.f) { o[0] = fmaf(v.x, fi, o[0]); o[1] = fmaf(v.y, fi, o[1]); }
-        }
-      }
-    }
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
-    const int64_t out_row = (int64_t)s.row + tile * a.tile_tokens + row / a.G;
-    const int head = s.h * a.G + row % a.G;
-    uint32_t* to_o = reinterpret_cast<uint32_t*>(a.O + out_row * a.ldo + (int64_t)head * D) + lane * (PER / 2);
-#pragma unroll
-    for (int e = 0; e < PER / 2; ++e) to_o[e] = l == 0.f ? 0u : pack2(o[2 * e] * inv, o[2 * e + 1] * inv);
-    if (lane == 0 && a.lse != nullptr) a.lse[out_row * a.H + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
-  }
+  const int rows0 = min(a.tile_tokens, s.tokens) * a.G, rows1 = (s.tokens - min(a.tile_tokens, s.tokens)) * a.G;
+  for (int r = blockIdx.y * (JOIN_THREADS / 32) + warp; r < rows0 + rows1; r += gridDim.y * (JOIN_THREADS / 32))
+    join_row<D>(a, s, cta, last, r >= rows0 ? 1 : 0, r >= rows0 ? r - rows0 : r);
 }
 
 // ------------------------------------------------------------------------------------------------ gathered weights
@@ -965,9 +1069,7 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
           __syncwarp();
 #pragma unroll
           for (int t = 0; t < 2; ++t)
-            if (y[t] >= 0)
-              for (int l = 0; l < SLABS; ++l)
-                tma_load_2d(sK + (2 * st + t) * TILE + l * SLAB + lane * box * 128, &tmK, bar, h * D + 64 * l, y[t]);
+            if (y[t] >= 0) tma_load_4d(sK + (2 * st + t) * TILE + lane * box * 128 * SLABS, &tmK, bar, 0, 0, h * SLABS, y[t] >> 3);
         }
         const uint32_t st = n_q % PW_Q;
         ok = wait_warp(q_free + 8 * st, ((n_q / PW_Q) & 1) ^ 1, abort_flag);
@@ -999,12 +1101,11 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             ++n_s[t];
             if (!ok) break;
             tc_fence_after();
-            const uint32_t kb = sK + (2 * kst + t) * TILE, qb = sQ + qst * TILE;
+            const uint32_t k = desc_low(sK + (2 * kst + t) * TILE, 0), qd = desc_low(sQ + qst * TILE, 0);
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-              const uint32_t off = (k >> 2) * SLAB + (k & 3) * 32;
-              mma_bf16(tmem_base + (2 * t + buf) * BLOCK, smem_desc_sw128(kb + off), smem_desc_sw128(qb + off), idesc, k > 0 ? 1u : 0u);
-            }
+            for (int e = 0; e < D / 16; ++e)
+              mma_ss(tmem_base + (2 * t + buf) * BLOCK, k + (((e >> 2) * 1024 + (e & 3) * 32) >> 4), desc_high(group_bytes<D>()),
+                     qd + (((e >> 2) * SLAB + (e & 3) * 32) >> 4), desc_high(1024), idesc, e > 0);
             mma_commit(s_full + 8 * (2 * t + buf));
           }
           if (!ok) break;
@@ -1098,9 +1199,7 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         // CTAs whose pieces reach into the unit: the first one's share is its last, the others' their first
         const long long begin = at - s.i0, end = begin + s.cost;
         const int mine = blockIdx.x, ctas = gridDim.x;
-        int first = mine, last = mine;
-        while (cut_line(total, first, ctas) > begin) --first;
-        while (cut_line(total, last + 1, ctas) < end) ++last;
+        const int first = cta_of(total, begin, ctas), last = cta_of(total, end - 1, ctas);
         float* share = a.share + (size_t)(2 * mine + (s.i0 == 0 ? 1 : 0)) * 2 * BLOCK;
         __stcg(share + t * BLOCK + quarter * 32 + lane, w);
         __threadfence();
@@ -1145,17 +1244,18 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 bool encode(spts_ctx* ctx, CUtensorMap* tm, const void* p, int rank, const cuuint64_t* dim, const cuuint64_t* stride, const cuuint32_t* box) {
-  const cuuint32_t step[3] = {1, 1, 1};
+  const cuuint32_t step[4] = {1, 1, 1, 1};
   return reinterpret_cast<EncodeTiledFn>(ctx->paged_encode)(
              tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(p), dim, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// K or V of all pages as rows of Hkv * d elements; a box is 64 of a head's dims of the rows of a page (of half a page of 256)
+// K or V of all pages as [rows / 8][Hkv * d / 64][8 rows][64]; a box is one head's dims of the rows of a page (of half a page of 256), in
+// the order in which they lie in a tile
 bool map_pages(spts_ctx* ctx, CUtensorMap* tm, const void* p, const spts_paged_kv* c) {
   const cuuint64_t width = (cuuint64_t)ctx->desc.n_kv_heads * ctx->desc.head_dim;
-  const cuuint64_t dim[2] = {width, (cuuint64_t)c->n_pages * c->page_size}, stride[1] = {width * 2};
-  const cuuint32_t box[2] = {64, (cuuint32_t)(c->page_size < BLOCK ? c->page_size : BLOCK)};
-  return encode(ctx, tm, p, 2, dim, stride, box);
+  const cuuint64_t dim[4] = {64, 8, width / 64, (cuuint64_t)c->n_pages * c->page_size / 8}, stride[3] = {width * 2, 128, width * 16};
+  const cuuint32_t box[4] = {64, 8, (cuuint32_t)(ctx->desc.head_dim / 64), (cuuint32_t)((c->page_size < BLOCK ? c->page_size : BLOCK) / 8)};
+  return encode(ctx, tm, p, 4, dim, stride, box);
 }
 // Q as [rows, H, d]; a box is 64 dims of `heads` heads of `tokens` rows
 bool map_queries(spts_ctx* ctx, CUtensorMap* tm, const void* p, int64_t ld, int n_rows, int heads, int tokens) {
@@ -1175,14 +1275,17 @@ spts_status attention_t(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q
   // two tiles to a unit where sequences have more tokens than one holds, on average
   a.unit_tokens = n_rows > (int64_t)cache->n_seq * a.tile_tokens ? 2 * a.tile_tokens : a.tile_tokens;
   a.Q = (const bf16*)Q; a.ldq = ldq; a.O = (bf16*)O; a.ldo = ldo; a.lse = lse;
-  a.share = ctx->ws.paged_part; a.status = ctx->ws.status;
+  a.share = ctx->ws.paged_part; a.arrived = ctx->ws.paged_arrived + 64; a.status = ctx->ws.status;
+  // a unit of a few rows is joined in the time that a launch takes; one of many rows wants more warps than one CTA's
+  a.solo = ceil_div(n_rows, cache->n_seq) * a.G <= SOLO_ROWS;
   CUtensorMap tmQ, tmK, tmV;
   if (!map_queries(ctx, &tmQ, Q, ldq, n_rows, a.G, a.tile_tokens) || !map_pages(ctx, &tmK, cache->k, cache) || !map_pages(ctx, &tmV, cache->v, cache))
     return SPTS_ERR_CUDA;
   const int ctas = ctx->sm_count < PAGED_MAX_CTAS ? ctx->sm_count : PAGED_MAX_CTAS;
   paged_attn_kernel<D><<<ctas, PA_THREADS, pa_smem<D>(), ctx->stream>>>(tmQ, tmK, tmV, a);
   SPTS_CUDA_OK(ctx);
-  if (launch_dependent(paged_attn_join_kernel<D>, dim3(ctas, 4), dim3(JOIN_THREADS), ctx->stream, a) != cudaSuccess) return SPTS_ERR_CUDA;
+  if (a.solo) return SPTS_OK;
+  if (launch_dependent(paged_attn_join_kernel<D>, dim3(ctas, JOIN_SPLIT), dim3(JOIN_THREADS), ctx->stream, a) != cudaSuccess) return SPTS_ERR_CUDA;
   ctx->launches++;
   return SPTS_OK;
 }
