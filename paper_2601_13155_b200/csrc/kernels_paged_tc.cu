@@ -39,7 +39,15 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 template <int D> constexpr int tile_bytes() { return D / 64 * SLAB; }
 template <int D> constexpr int pa_smem() { return 1024 + (2 + RING) * tile_bytes<D>() + 512 + 1024 + 128; }
-template <int D> constexpr int share_floats() { return BLOCK * (D + 2); }       // O, then (maximum, sum) of each row
+// A share: O as [D / 8][128 rows][8], so that a warp's rows are written without gaps, then (maximum, sum) of each row.
+template <int D> constexpr int share_floats() { return BLOCK * (D + 2); }
+__device__ __forceinline__ int share_at(int row, int col) { return ((col >> 3) * BLOCK + row) * 8 + (col & 7); }
+// 32 bytes: whole sectors where a warp's lanes write different rows
+__device__ __forceinline__ void store32(void* p, uint4 x, uint4 y) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w), "r"(y.x), "r"(y.y),
+               "r"(y.z), "r"(y.w)
+               : "memory");
+}
 
 struct AttnArgs {
   Cache c;
@@ -48,7 +56,9 @@ struct AttnArgs {
   int tile_tokens, unit_tokens;                // floor(128 / G); that or twice that
   const bf16* Q; int64_t ldq;
   bf16* O; int64_t ldo; float* lse;
+  int wide;                                    // rows of O begin on 32 bytes
   float* share; int* arrived;
+  struct OpenUnit* open;                       // [CTAs]
   int solo;                                    // units are joined by the CTA that is done last instead of a second kernel
   int* status;
 };
@@ -135,16 +145,24 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatil
 }
 
 // ------------------------------------------------------------------------------------------------ the line of blocks
-// sum of floor((a i + b) / m), i < n, by the Euclidean recursion on (m, a)
+// sum of floor((a i + b) / m), i < n, by the Euclidean recursion on (m, a); a, b and m stay small, so 32 bits hold a n + b for all
+// but the longest lines
 __device__ unsigned long long floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
   unsigned long long sum = 0;
   while (true) {
     if (a >= m) { sum += (unsigned long long)n * (n - 1) / 2 * (a / m); a %= m; }
     if (b >= m) { sum += (unsigned long long)n * (b / m); b %= m; }
-    const unsigned long long y = (unsigned long long)a * n + b;
-    if (y < m) return sum;
-    n = (uint32_t)(y / m);
-    b = (uint32_t)(y % m);
+    if (n < 1u << 23) {                        // (a, b < 2^9)
+      const uint32_t y = a * n + b;
+      if (y < m) return sum;
+      n = y / m;
+      b = y % m;
+    } else {
+      const unsigned long long y = (unsigned long long)a * n + b;
+      if (y < m) return sum;
+      n = (uint32_t)(y / m);
+      b = (uint32_t)(y % m);
+    }
     const uint32_t t = m;
     m = a;
     a = t;
@@ -156,14 +174,29 @@ __device__ __forceinline__ int unit_blocks(int n, int off, int R, int g) {
   const int seen = off + min(n, (g + 1) * R);
   return max(1, (seen + BLOCK - 1) / BLOCK);
 }
-// of the units before g
+// What a unit costs beside its blocks (its first products, reading out O), in blocks: places of the line behind its blocks, at which there
+// is nothing to do.
+constexpr int EXTRA = 1;
+// of the units before g, with that
 __device__ long long blocks_before(int n, int off, int R, int g) {
   const int whole = min(g, n / R);
   const int blind = off < 0 ? min(whole, -off / R) : 0;            // units that see nothing
-  long long sum = blind;
+  long long sum = blind + (long long)EXTRA * g;
   if (whole > blind) sum += (long long)floor_sum(whole - blind, BLOCK, R, off + (blind + 1) * R + BLOCK - 1);
   if (g > whole) sum += unit_blocks(n, off, R, whole);
   return sum;
+}
+// The largest g in [0, count) with before(g) <= x, by a warp: 32 guesses at a time.
+template <typename F> __device__ __forceinline__ int warp_find(int count, long long x, F before) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, hi = count;                      // before(lo) <= x, and not at hi
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 31) / 32, g = lo + lane * step;
+    const uint32_t below = __ballot_sync(0xffffffffu, g < hi && (lane == 0 || before(g) <= x));
+    lo += (31 - __clz(below)) * step;
+    hi = min(hi, lo + step);
+  }
+  return lo;
 }
 
 // Where the piece of CTA `cta` begins.  Fewer pieces than CTAs: one to each of the first, so that no CTA between two others is without.
@@ -196,6 +229,7 @@ struct Line {
     });
   }
   __device__ __forceinline__ long long cut(int cta, int ctas) const { return cut_line(total, cta, ctas); }
+  // (by a warp)
   __device__ __forceinline__ Place find(const AttnArgs& a, long long x) const {
     Place p;
     p.b = find_share(pre, a.c.n_seq, x);
@@ -213,13 +247,8 @@ struct Line {
       p.h = (int)(x / head);
     }
     x -= p.h * head;
-    int lo = 0, hi = (n + R - 1) / R;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (blocks_before(n, off, R, mid) <= x) lo = mid; else hi = mid;
-    }
-    p.g = lo;
-    p.j = (int)(lo == 0 ? x : x - blocks_before(n, off, R, lo));
+    p.g = warp_find((n + R - 1) / R, x, [&](int g) { return blocks_before(n, off, R, g); });
+    p.j = (int)(p.g == 0 ? x : x - blocks_before(n, off, R, p.g));
     return p;
   }
 };
@@ -227,7 +256,8 @@ struct Line {
 // A CTA's share of one unit: blocks [j0, j1) of `cost`.
 struct Segment {
   int b, h, j0, j1, cost;
-  int held, n, off;                            // the sequence's rows, its queries, rows before the first query
+  int held, off;                               // the sequence's rows, rows before its first query
+  long long begin;                             // of the unit on the line
   int token, tokens;                           // first token of the unit (in its sequence), how many
   int row;                                     // first row of the unit in Q and O
   bool two;                                    // two tiles
@@ -236,7 +266,7 @@ struct Segment {
 // Each role of a CTA walks over the CTA's segments by itself.
 struct Walk {
   Place p;
-  long long left;
+  long long at, left;                          // place on the line, what is left of the piece
   int first, n, off, held;
   __device__ __forceinline__ void sequence(const AttnArgs& a) {
     call_rows(a.row_start, a.n_rows, p.b, first, n);
@@ -244,27 +274,37 @@ struct Walk {
     off = held - n;
   }
   __device__ __forceinline__ bool next(const AttnArgs& a, Segment& s) {
-    if (left <= 0) return false;
     const int R = a.unit_tokens;
-    s.b = p.b; s.h = p.h; s.held = held; s.n = n; s.off = off;
-    s.cost = unit_blocks(n, off, R, p.g);
-    s.j0 = p.j;
-    s.j1 = (int)min((long long)s.cost, p.j + left);
-    s.token = p.g * R;
-    s.tokens = min(R, n - s.token);
-    s.row = first + s.token;
-    s.two = s.tokens > a.tile_tokens;
-    left -= s.j1 - s.j0;
-    p.j = 0;
-    if ((p.g + 1) * R < n) { ++p.g; return true; }
-    p.g = 0;
-    if (++p.h < a.Hkv) return true;
-    p.h = 0;
-    while (left > 0 && ++p.b < a.c.n_seq) {
-      sequence(a);
-      if (n > 0) break;
+    while (left > 0) {
+      s.cost = unit_blocks(n, off, R, p.g);
+      s.j0 = p.j;
+      const int j1 = (int)min((long long)s.cost + EXTRA, p.j + left);
+      s.j1 = min(j1, s.cost);
+      s.b = p.b; s.h = p.h; s.held = held;
+      s.token = p.g * R;
+      s.tokens = min(R, n - s.token);
+      s.off = off;
+      s.row = first + s.token;
+      s.two = s.tokens > a.tile_tokens;
+      s.begin = at - p.j;
+      left -= j1 - p.j;
+      at += j1 - p.j;
+      p.j = 0;
+      if ((p.g + 1) * R < n) {
+        ++p.g;
+      } else {
+        p.g = 0;
+        if (++p.h == a.Hkv) {
+          p.h = 0;
+          while (left > 0 && ++p.b < a.c.n_seq) {
+            sequence(a);
+            if (n > 0) break;
+          }
+        }
+      }
+      if (s.j0 < s.j1) return true;
     }
-    return true;
+    return false;
   }
 };
 
@@ -302,10 +342,12 @@ __device__ __noinline__ void plain_row(const AttnArgs& a, int b, int kvh, const 
 }
 
 // ------------------------------------------------------------------------------------------------ joining shares
+struct OpenUnit { int last, row, h, tokens; };   // the unit that begins in a CTA and goes on, up to CTA `last` (-1: there is none)
+
 // Row `row` of a tile of a unit that CTAs first .. last worked on, by one warp: the shares in the order of the line (of the first CTA its last
 // segment, of the others their first).
 template <int D>
-__device__ __forceinline__ void join_row(const AttnArgs& a, const Segment& s, int first, int last, int tile, int row) {
+__device__ __forceinline__ void join_row(const AttnArgs& a, int unit_row, int h, int first, int last, int tile, int row) {
   constexpr int PER = D / 32;
   const int lane = threadIdx.x & 31, parts = last - first + 1;
   const auto share = [&](int i) { return a.share + ((int64_t)(2 * (first + i) + (i == 0 ? 1 : 0)) * 2 + tile) * share_floats<D>(); };
@@ -328,7 +370,7 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const Segment& s, in
 #pragma unroll 8
     for (int i = i0; i < min(parts, i0 + 32); ++i) {
       const float fi = __shfl_sync(0xffffffffu, f, i - i0);
-      const float* x = share(i) + row * D + lane * PER;
+      const float* x = share(i) + share_at(row, lane * PER);
       float v[PER];
       if (PER == 4) {
         const float4 y = __ldcg(reinterpret_cast<const float4*>(x));
@@ -342,8 +384,8 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const Segment& s, in
     }
   }
   const float inv = l == 0.f ? 0.f : 1.0f / l;
-  const int64_t out_row = (int64_t)s.row + tile * a.tile_tokens + row / a.G;
-  const int head = s.h * a.G + row % a.G;
+  const int64_t out_row = (int64_t)unit_row + tile * a.tile_tokens + row / a.G;
+  const int head = h * a.G + row % a.G;
   uint32_t* to_o = reinterpret_cast<uint32_t*>(a.O + out_row * a.ldo + (int64_t)head * D) + lane * (PER / 2);
 #pragma unroll
   for (int e = 0; e < PER / 2; ++e) to_o[e] = l == 0.f ? 0u : pack2(o[2 * e] * inv, o[2 * e + 1] * inv);
@@ -351,7 +393,7 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const Segment& s, in
 }
 
 // ------------------------------------------------------------------------------------------------ the kernel
-struct Start { Walk walk; long long from, total; };      // a CTA's piece
+struct Start { Walk walk; long long total; };      // a CTA's piece, the line's length
 
 template <int D>
 __global__ void __launch_bounds__(PA_THREADS, 1)
@@ -401,12 +443,12 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   {
     Line line;
     line.make<PA_THREADS>(a, reinterpret_cast<long long*>(gen + (sR - base)), blockIdx.x == 0);
-    if (threadIdx.x == 0) {
-      const long long from = line.cut(blockIdx.x, gridDim.x), to = line.cut(blockIdx.x + 1, gridDim.x);
+    if (warp == 0) {
       Walk w;
-      w.left = to - from;
-      if (w.left > 0) { w.p = line.find(a, from); w.sequence(a); }
-      *start = {w, from, line.total};
+      w.at = line.cut(blockIdx.x, gridDim.x);
+      w.left = line.cut(blockIdx.x + 1, gridDim.x) - w.at;
+      if (w.left > 0) { w.p = line.find(a, w.at); w.sequence(a); }
+      if (lane == 0) *start = {w, line.total};
     }
     fence_proxy_async_smem();
   }
@@ -629,10 +671,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     const float sc = LOG2E / (D == 128 ? 11.313708498984761f : 8.0f);
     const float2 sc2 = make_float2(sc, sc);
     uint32_t n_s = 0, n_o = 0, n_x = 0, n_g = 0, turn = 0;
-    long long at = start->from;                        // the line's block at which the segment ends
+    bool open = false;                                 // the last segment's unit begins here and goes on in other CTAs
     bool ok = true;
     while (ok && walk.next(a, s)) {
-      at += s.j1 - s.j0;
+      open = s.j0 == 0 && s.j1 < s.cost;
       const int nb = s.j1 - s.j0, tile = s.two ? t : 0;
       const int tokens = min(a.tile_tokens, s.tokens - tile * a.tile_tokens);
       const int token = s.token + tile * a.tile_tokens + row_token;        // in the sequence
@@ -774,19 +816,26 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             o[e] = __float_as_uint(x);
           }
           if (live && direct) {
+            uint4 w[4];
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-              uint4 w;
-              w.x = pack2(__uint_as_float(o[g * 8 + 0]), __uint_as_float(o[g * 8 + 1]));
-              w.y = pack2(__uint_as_float(o[g * 8 + 2]), __uint_as_float(o[g * 8 + 3]));
-              w.z = pack2(__uint_as_float(o[g * 8 + 4]), __uint_as_float(o[g * 8 + 5]));
-              w.w = pack2(__uint_as_float(o[g * 8 + 6]), __uint_as_float(o[g * 8 + 7]));
-              *reinterpret_cast<uint4*>(orow + c + g * 8) = w;
+              w[g].x = pack2(__uint_as_float(o[g * 8 + 0]), __uint_as_float(o[g * 8 + 1]));
+              w[g].y = pack2(__uint_as_float(o[g * 8 + 2]), __uint_as_float(o[g * 8 + 3]));
+              w[g].z = pack2(__uint_as_float(o[g * 8 + 4]), __uint_as_float(o[g * 8 + 5]));
+              w[g].w = pack2(__uint_as_float(o[g * 8 + 6]), __uint_as_float(o[g * 8 + 7]));
+            }
+            if (a.wide) {
+              store32(orow + c, w[0], w[1]);
+              store32(orow + c + 16, w[2], w[3]);
+            } else {
+#pragma unroll
+              for (int g = 0; g < 4; ++g) *reinterpret_cast<uint4*>(orow + c + g * 8) = w[g];
             }
           } else if (live) {
 #pragma unroll
-            for (int g = 0; g < 8; ++g)
-              *reinterpret_cast<uint4*>(share + row * D + c + g * 4) = make_uint4(o[g * 4], o[g * 4 + 1], o[g * 4 + 2], o[g * 4 + 3]);
+            for (int g = 0; g < 4; ++g)
+              store32(share + share_at(row, c + g * 8), make_uint4(o[g * 8], o[g * 8 + 1], o[g * 8 + 2], o[g * 8 + 3]),
+                      make_uint4(o[g * 8 + 4], o[g * 8 + 5], o[g * 8 + 6], o[g * 8 + 7]));
           }
         }
         if (live && direct && a.lse != nullptr) a.lse[out_row * a.H + head] = l == 0.f ? -INFINITY : (m_used + log2f(l)) * LN2;
@@ -810,7 +859,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         for (int e = 0; e < D / 32; ++e) {
           const int col = lane * (D / 32) + e;
           if (direct) a.O[w_out * a.ldo + (int64_t)w_head * D + col] = __float2bfloat16_rn(sum == 0.f ? 0.f : o[e] / sum);
-          else share[w_row * D + col] = o[e];
+          else share[share_at(w_row, col)] = o[e];
         }
         if (lane == 0) {
           if (direct && a.lse != nullptr) a.lse[w_out * a.H + w_head] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * LN2;
@@ -820,8 +869,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       }
       if (!direct && a.solo) {
         // the CTA that leaves the unit's last share joins it, a warp to a row
-        const long long begin = at - s.j1, total = start->total;
-        const int ctas = gridDim.x, first = cta_of(total, begin, ctas), last = cta_of(total, begin + s.cost - 1, ctas);
+        const long long total = start->total;
+        const int ctas = gridDim.x, first = cta_of(total, s.begin, ctas), last = cta_of(total, s.begin + s.cost - 1, ctas);
         __threadfence();
         mbar_arrive(g_done + 8 * t);
         ok = wait_warp(g_done + 8 * t, n_g & 1, abort_flag);
@@ -838,10 +887,12 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         if (!ok) break;
         if (g_last[t]) {
           __threadfence();
-          for (int r = quarter; r < s.tokens * a.G; r += 4) join_row<D>(a, s, first, last, 0, r);
+          for (int r = quarter; r < s.tokens * a.G; r += 4) join_row<D>(a, s.row, s.h, first, last, 0, r);
         }
       }
     }
+    if (threadIdx.x == 128 && !a.solo)
+      a.open[blockIdx.x] = {open && ok ? cta_of(start->total, s.begin + s.cost - 1, gridDim.x) : -1, s.row, s.h, s.tokens};
   }
 
   tc_fence_before();
@@ -864,34 +915,13 @@ constexpr int JOIN_THREADS = 256, JOIN_SPLIT = 16;     // a unit's 256 rows: two
 template <int D>
 __global__ void __launch_bounds__(JOIN_THREADS)
 paged_attn_join_kernel(const __grid_constant__ AttnArgs a) {
-  __shared__ long long scratch[32 + PREFIX_MAX + 1];
-  __shared__ Segment s_seg;
-  __shared__ int s_last;
-  const int warp = threadIdx.x >> 5, cta = blockIdx.x, ctas = gridDim.x;
-  Line line;
-  line.make<JOIN_THREADS>(a, scratch, false);
-  const long long from = line.cut(cta, ctas), to = line.cut(cta + 1, ctas);
-  if (threadIdx.x == 0) s_last = cta;
-  if (threadIdx.x == 0 && from < to) {
-    Walk w;
-    w.p = line.find(a, to - 1);
-    w.left = 1;
-    w.sequence(a);
-    const long long begin = to - 1 - w.p.j;
-    const bool begins_here = begin >= from;
-    w.p.j = 0;
-    w.left = 1LL << 40;
-    w.next(a, s_seg);
-    if (begins_here) s_last = cta_of(line.total, begin + s_seg.cost - 1, ctas);      // == cta: nothing to join
-  }
-  __syncthreads();
   dep_wait();
-  const int last = s_last;
-  if (last == cta) return;
-  const Segment s = s_seg;
-  const int rows0 = min(a.tile_tokens, s.tokens) * a.G, rows1 = (s.tokens - min(a.tile_tokens, s.tokens)) * a.G;
-  for (int r = blockIdx.y * (JOIN_THREADS / 32) + warp; r < rows0 + rows1; r += gridDim.y * (JOIN_THREADS / 32))
-    join_row<D>(a, s, cta, last, r >= rows0 ? 1 : 0, r >= rows0 ? r - rows0 : r);
+  const int4 raw = __ldcg(reinterpret_cast<const int4*>(a.open + blockIdx.x));
+  const OpenUnit u = {raw.x, raw.y, raw.z, raw.w};
+  if (u.last < 0) return;
+  const int rows0 = min(a.tile_tokens, u.tokens) * a.G, rows = u.tokens * a.G, warp = threadIdx.x >> 5;
+  for (int r = blockIdx.y * (JOIN_THREADS / 32) + warp; r < rows; r += JOIN_SPLIT * (JOIN_THREADS / 32))
+    join_row<D>(a, u.row, u.h, blockIdx.x, u.last, r >= rows0 ? 1 : 0, r >= rows0 ? r - rows0 : r);
 }
 
 // ------------------------------------------------------------------------------------------------ gathered weights
@@ -1011,22 +1041,18 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
       return held == 0 ? 0LL : items_before(n, held - n, a.tile_tokens, a.Hkv, (held + 2 * BLOCK - 1) / (2 * BLOCK));
     });
     from = cut_line(total, blockIdx.x, gridDim.x);
-    if (threadIdx.x == 0) {
+    if (warp == 0) {
       UnitWalk w;
       w.left = cut_line(total, blockIdx.x + 1, gridDim.x) - from;
       if (w.left > 0) {
         w.b = find_share(pre, a.c.n_seq, from);
         w.sequence(a);
         const long long x = from - pre[w.b];
-        int lo = 0, hi = (w.held + 2 * BLOCK - 1) / (2 * BLOCK);
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (items_before(w.n, w.off, a.tile_tokens, a.Hkv, mid) <= x) lo = mid; else hi = mid;
-        }
-        w.u = lo;
-        w.i = (int)(x - items_before(w.n, w.off, a.tile_tokens, a.Hkv, lo));
+        const auto before = [&](int u) { return items_before(w.n, w.off, a.tile_tokens, a.Hkv, u); };
+        w.u = warp_find((w.held + 2 * BLOCK - 1) / (2 * BLOCK), x, before);
+        w.i = (int)(x - before(w.u));
       }
-      *start = w;
+      if (lane == 0) *start = w;
     }
     fence_proxy_async_smem();
   }
@@ -1275,7 +1301,9 @@ spts_status attention_t(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q
   // two tiles to a unit where sequences have more tokens than one holds, on average
   a.unit_tokens = n_rows > (int64_t)cache->n_seq * a.tile_tokens ? 2 * a.tile_tokens : a.tile_tokens;
   a.Q = (const bf16*)Q; a.ldq = ldq; a.O = (bf16*)O; a.ldo = ldo; a.lse = lse;
+  a.wide = (reinterpret_cast<uintptr_t>(O) & 31) == 0 && (ldo * 2) % 32 == 0;
   a.share = ctx->ws.paged_part; a.arrived = ctx->ws.paged_arrived + 64; a.status = ctx->ws.status;
+  a.open = reinterpret_cast<OpenUnit*>(ctx->ws.paged_open);
   // a unit of a few rows is joined in the time that a launch takes; one of many rows wants more warps than one CTA's
   a.solo = ceil_div(n_rows, cache->n_seq) * a.G <= SOLO_ROWS;
   CUtensorMap tmQ, tmK, tmV;

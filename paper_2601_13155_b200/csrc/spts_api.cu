@@ -120,6 +120,7 @@ size_t carve(const spts_model_desc& d, int Nmax, void* base, Workspace* ws, std:
   w.kv4_part = c.take<float>((size_t)2 * KV4_MAX_CTAS * 16 * (d.head_dim + 2));
   w.kv4_arrived = c.take<int>(KV4_MAX_CTAS);
   w.paged_part = c.take<float>(paged_part_floats(d));
+  w.paged_open = c.take<int4>(PAGED_MAX_CTAS);
   w.paged_arrived = c.take<int>(PAGED_COUNTERS);
   w.evict_bits = c.take<uint32_t>(SPTS_PAGED_MAX_ROWS / 32);
   w.evict_before = c.take<int2>(EVICT_CHUNKS);

@@ -102,6 +102,7 @@ struct Workspace {
   float* kv4_part;      // [2 * KV4_MAX_CTAS, 16, d + 2] partial results of the attention over a 4-bit cache
   int* kv4_arrived;     // [KV4_MAX_CTAS] CTAs that have left theirs; zero between calls
   float* paged_part;    // [2 * PAGED_MAX_CTAS] shares of attention units that several CTAs work on
+  int4* paged_open;     // [PAGED_MAX_CTAS] units that begin in a CTA and go on in others
   int* paged_arrived;   // [PAGED_COUNTERS] blocks of an append that are done, warps that left their share of a sum; zero between calls
   uint32_t* evict_bits; // [SPTS_PAGED_MAX_ROWS / 32] rows that stay
   int2* evict_before;   // [EVICT_CHUNKS] holes and movers before each chunk of rows, within the part of a sequence that one CTA ranked
