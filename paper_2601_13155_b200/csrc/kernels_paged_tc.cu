@@ -121,6 +121,18 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* tm,
 }
 constexpr uint32_t B_ALONG_N = 1u << 16;       // instruction descriptor: B is stored N-contiguous
 
+__device__ __forceinline__ bool elect_lane() {
+  uint32_t mine;
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "elect.sync _|p, 0xffffffff;\n"
+      "selp.u32 %0, 1, 0, p;\n"
+      "}\n"
+      : "=r"(mine));
+  return mine != 0;
+}
+
 // A wait whose limit counts from its own beginning.
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   if (mbar_test_wait(bar, parity)) return true;
@@ -515,12 +527,15 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
       }
     } else if (warp == 1) {
-      if (lane == 0) {
-        // This thread's instructions are what bounds long chunks, so its state is a handful of registers: descriptors advance by additions,
-        // phases are bits.
+      {
+        // The instructions around the products are what bounds long chunks.  The whole warp runs this role, on values that are the same for
+        // all its lanes (and known to be: shuffles and votes), so that descriptors live in uniform registers; one lane issues.  Descriptors
+        // advance by additions, phases are bits.
+        const bool leader = elect_lane();
         constexpr uint32_t idesc_s = idesc_bf16(BLOCK, BLOCK), idesc_o = idesc_bf16(BLOCK, D) | B_ALONG_N;
         constexpr uint32_t q_hi = desc_high(1024), k_hi = desc_high(group_bytes<D>());
-        const uint32_t q_lo = desc_low(sQ, 0), k_lo = desc_low(sR, 0), v_lo = desc_low(sR, 1024);
+        const uint32_t tm = __shfl_sync(0xffffffffu, tmem_base, 0);
+        const uint32_t q_lo = desc_low(__shfl_sync(0xffffffffu, sQ, 0), 0), k_lo = desc_low(__shfl_sync(0xffffffffu, sR, 0), 0), v_lo = k_lo | (1024 >> 4 << 16);
         uint32_t slot = 0, phase = 0, clean = 0;         // the ring's place; phases of v_clean
         uint32_t bits = 0;                               // phases: 0, 1 of p_full; 2, 3 of q_full
         uint32_t turn = 0, q_next = 0;
@@ -529,19 +544,23 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           if (++slot == RING) { slot = 0; phase ^= 1; }
         };
         // the ring's next tile has come (a tail of V: has been cleared)
-        const auto wait_tile = [&]() { ok = ok && wait(full + 8 * slot, phase, abort_flag); };
+        const auto wait_tile = [&]() { ok = ok && wait_warp(full + 8 * slot, phase, abort_flag); };
         const auto wait_v = [&](bool tail) {
           if (tail) {
-            ok = ok && wait(v_clean + 8 * slot, (clean >> slot) & 1, abort_flag);
+            ok = ok && wait_warp(v_clean + 8 * slot, (clean >> slot) & 1, abort_flag);
             clean ^= 1u << slot;
           } else {
             wait_tile();
           }
         };
+        const auto commit = [&](uint32_t bar) {
+          if (leader) mma_commit(bar);
+        };
         const auto qk = [&](int t, uint32_t q, uint32_t k) {
+          if (!leader) return;
 #pragma unroll
           for (int i = 0; i < D / 16; ++i)
-            mma_ss(tmem_base + t * BLOCK, q + (((i >> 2) * SLAB + (i & 3) * 32) >> 4), q_hi, k + (((i >> 2) * 1024 + (i & 3) * 32) >> 4), k_hi, idesc_s, i > 0);
+            mma_ss(tm + t * BLOCK, q + (((i >> 2) * SLAB + (i & 3) * 32) >> 4), q_hi, k + (((i >> 2) * 1024 + (i & 3) * 32) >> 4), k_hi, idesc_s, i > 0);
           mma_commit(s_full + 8 * t);
         };
         // O_t += P_t V, P_t read from the columns of S_t, in the halves in which the softmax warps hand it over
@@ -550,19 +569,21 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           bits ^= 1u << t;
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
-            ok = ok && wait(p_full + 8 * (2 * t + half), ph, abort_flag);
+            ok = ok && wait_warp(p_full + 8 * (2 * t + half), ph, abort_flag);
             if (!ok) return;
             tc_fence_after();
+            if (leader) {
 #pragma unroll
-            for (int i = 4 * half; i < 4 * half + 4; ++i)
-              mma_ts(tmem_base + 2 * BLOCK + t * BLOCK, tmem_base + t * BLOCK + 8 * i, v + i * (2 * group_bytes<D>() >> 4), k_hi, idesc_o, !first || i > 0);
+              for (int i = 4 * half; i < 4 * half + 4; ++i)
+                mma_ts(tm + 2 * BLOCK + t * BLOCK, tm + t * BLOCK + 8 * i, v + i * (2 * group_bytes<D>() >> 4), k_hi, idesc_o, !first || i > 0);
+            }
           }
         };
-        while (ok && walk.next(a, s)) {
-          const int nb = s.j1 - s.j0;
-          const bool tail = s.j1 * BLOCK > s.held;
-          if (s.two) {
-            ok = ok && wait(q_full, (bits >> 2) & 1, abort_flag) && wait(q_full + 8, (bits >> 3) & 1, abort_flag);
+        while (ok && __any_sync(0xffffffffu, walk.next(a, s))) {
+          const int nb = __shfl_sync(0xffffffffu, s.j1 - s.j0, 0);
+          const bool tail = __any_sync(0xffffffffu, s.j1 * BLOCK > s.held);
+          if (__any_sync(0xffffffffu, s.two)) {
+            ok = ok && wait_warp(q_full, (bits >> 2) & 1, abort_flag) && wait_warp(q_full + 8, (bits >> 3) & 1, abort_flag);
             bits ^= 12;
             wait_tile();
             if (!ok) break;
@@ -570,7 +591,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             const uint32_t k0 = k_lo + slot * (TILE >> 4);
             qk(0, q_lo, k0);
             qk(1, q_lo + (TILE >> 4), k0);
-            mma_commit(free_ + 8 * slot);
+            commit(free_ + 8 * slot);
             next_slot();
             for (int i = 0; i + 1 < nb; ++i) {
               wait_v(false);
@@ -586,25 +607,25 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
               pv(1, v, i == 0);
               if (!ok) break;
               qk(1, q_lo + (TILE >> 4), k);
-              mma_commit(v_free);
-              mma_commit(k_free);
+              commit(v_free);
+              commit(k_free);
             }
             if (!ok) break;
-            mma_commit(q_free);
-            mma_commit(q_free + 8);
+            commit(q_free);
+            commit(q_free + 8);
             wait_v(tail);
             const uint32_t v = v_lo + slot * (TILE >> 4);
             if (!ok) break;
             pv(0, v, nb == 1);
-            mma_commit(o_full);
+            commit(o_full);
             if (!ok) break;
             pv(1, v, nb == 1);
-            mma_commit(o_full + 8);
-            mma_commit(free_ + 8 * slot);
+            commit(o_full + 8);
+            commit(free_ + 8 * slot);
             next_slot();
           } else {
             const uint32_t q = q_lo + q_next * (TILE >> 4), qf = q_free + 8 * q_next;
-            ok = ok && wait(q_full + 8 * q_next, (bits >> (2 + q_next)) & 1, abort_flag);
+            ok = ok && wait_warp(q_full + 8 * q_next, (bits >> (2 + q_next)) & 1, abort_flag);
             bits ^= 4u << q_next;
             q_next ^= 1;
             for (int i = 0; i < 2 && i < nb; ++i) {
@@ -612,29 +633,29 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
               if (!ok) break;
               tc_fence_after();
               qk((i + turn) & 1, q, k_lo + slot * (TILE >> 4));
-              mma_commit(free_ + 8 * slot);
+              commit(free_ + 8 * slot);
               next_slot();
             }
             if (!ok) break;
-            if (nb <= 2) mma_commit(qf);
+            if (nb <= 2) commit(qf);
             for (int i = 0; i < nb; ++i) {
               const int t = (i + turn) & 1;
               wait_v(tail && i + 1 == nb);
               if (!ok) break;
               pv(t, v_lo + slot * (TILE >> 4), i < 2);
               if (!ok) break;
-              mma_commit(free_ + 8 * slot);
+              commit(free_ + 8 * slot);
               next_slot();
               if (i + 2 < nb) {
                 wait_tile();
                 if (!ok) break;
                 tc_fence_after();
                 qk(t, q, k_lo + slot * (TILE >> 4));
-                mma_commit(free_ + 8 * slot);
+                commit(free_ + 8 * slot);
                 next_slot();
-                if (i + 3 == nb) mma_commit(qf);
+                if (i + 3 == nb) commit(qf);
               } else {
-                mma_commit(o_full + 8 * t);
+                commit(o_full + 8 * t);
               }
             }
             turn = (turn + nb) & 1;
