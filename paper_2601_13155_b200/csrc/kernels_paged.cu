@@ -1,6 +1,8 @@
 // The paged KV cache on CUDA cores: rows are appended to it (paged_append_kernel), attention and the weights that its rows gather in
 // either storage type (paged_attn_plain_kernel, paged_weights_plain_kernel: fp32 storage, SPTS_REFERENCE_KERNELS, more than 128 query
 // heads to a KV head), and sequences are cut down to a budget (evict_rank_kernel, evict_move_kernel).
+#include <climits>
+
 #include <cooperative_groups.h>
 
 #include "paged_common.cuh"
@@ -358,7 +360,7 @@ paged_weights_plain_kernel(Cache c, const T* __restrict__ Q, int64_t ldq, const 
 }
 
 // ------------------------------------------------------------------------------------------------ eviction
-constexpr int RANK_THREADS = 512;
+constexpr int RANK_THREADS = 1024;
 constexpr int RANK_KEYS = 24576;               // rows of a CTA whose keys and positions fit shared memory
 constexpr int MOVE_THREADS = 1024;
 
@@ -376,34 +378,35 @@ struct EvictArgs {
   int first_seq;                               // of this launch
   int words;                                   // of evict_bits for each sequence
   uint32_t* bits; int2* before; int2* total;
+  int* arrived;                                // blocks of the moves that are done, zero between calls
   int* status;
 };
 
 // A cluster of CTAs ranks one sequence's rows: each holds the keys of a contiguous part in shared memory; the smallest key that stays is
-// found by a radix select of four digits, whose histograms meet in distributed shared memory; of the rows that have just this key the
-// first ones stay.  What comes out is a bit for each row, and the numbers of holes (rows among the first keep that go) and movers (rows
-// behind them that stay) before each chunk of 256 rows, from which evict_move_kernel finds its copies.  Parts too long for shared
-// memory (capacities beyond 196,608 rows) read their weights again for every digit.
+// found by a radix select of four digits, whose histograms meet in distributed shared memory (a thread for each bin, the CTAs' bins all on
+// their way at once); of the rows that have just this key the first ones stay.  What comes out is a bit for each row, and the numbers of
+// holes (rows among the first keep that go) and movers (rows behind them that stay) before each chunk of 256 rows, from which
+// evict_move_kernel finds its copies.  Parts too long for shared memory (capacities beyond 196,608 rows) read their weights again for every
+// digit.  Bound by the chain of barriers and round trips.
 template <bool SMEM>
 __global__ void __launch_bounds__(RANK_THREADS)
 evict_rank_kernel(EvictArgs a) {
   extern __shared__ __align__(16) uint32_t keys[];                       // [part], then positions [part]
-  __shared__ uint32_t hist[4][256];
-  __shared__ long long newest_all;
-  __shared__ int ties_here, counts[2], warp_n[RANK_THREADS / 32][3];
-  __shared__ uint32_t s_prefix;
-  __shared__ int s_need;
+  __shared__ uint32_t hist[4][256], all[256];
+  __shared__ long long newest_here, newest_all;
+  __shared__ int ties_here, warp_n[RANK_THREADS / 32][3];
   cg::cluster_group cluster = cg::this_cluster();
   const int split = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const Cache& c = a.c;
   const int local = blockIdx.x / split, b = a.first_seq + local, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  dep_launch();
   const int held = held_rows(c, b), keep = a.keep[b];
   if (keep < 0 || held <= keep) return;        // (the same for all CTAs of a cluster)
   const int part = (int)((((int64_t)held + split - 1) / split + EVICT_CHUNK - 1) / EVICT_CHUNK) * EVICT_CHUNK;
   const int j0 = (int)min((int64_t)held, (int64_t)rank * part), n = min(part, held - j0);
   uint32_t* spos = keys + part;
   for (int i = tid; i < 4 * 256; i += RANK_THREADS) (&hist[0][0])[i] = 0;
-  if (tid == 0) { newest_all = LLONG_MIN; ties_here = 0; counts[0] = counts[1] = 0; }
+  if (tid == 0) { newest_here = LLONG_MIN; ties_here = 0; }
   __syncthreads();
   const bool by_pos = a.n_sink > 0 || a.n_recent > 0;
   // the rows' weights and positions, and the largest position that the sequence holds
@@ -430,9 +433,15 @@ evict_rank_kernel(EvictArgs a) {
   if (none) set_status(a.status, SPTS_ERR_INDEX);
   if (a.n_recent > 0) {
     for (int o = 16; o > 0; o >>= 1) newest = max(newest, __shfl_xor_sync(0xffffffffu, newest, o));
-    if (lane == 0) atomicMax(&newest_all, newest);
+    if (lane == 0) atomicMax(&newest_here, newest);
     cluster.sync();
-    for (int s = 0; s < split; ++s) newest = max(newest, *cluster.map_shared_rank(&newest_all, s));
+    if (warp == 0) {
+      newest = lane < split ? *cluster.map_shared_rank(&newest_here, lane) : LLONG_MIN;
+      for (int o = 16; o > 0; o >>= 1) newest = max(newest, __shfl_xor_sync(0xffffffffu, newest, o));
+      if (lane == 0) newest_all = newest;
+    }
+    __syncthreads();
+    newest = newest_all;
   }
   const auto stays_first = [&](int p) { return p < a.n_sink || (a.n_recent > 0 && (long long)p > newest - a.n_recent); };
   const auto key_at = [&](int i) -> uint32_t {
@@ -457,63 +466,63 @@ evict_rank_kernel(EvictArgs a) {
       if (d == 0 || (k >> (shift + 8)) == prefix) atomicAdd(&hist[d][(k >> shift) & 255], 1u);
     }
     cluster.sync();
-    if (warp == 0) {
-      // lane l has digits 255 - 8 l down to 248 - 8 l
+    if (tid < 256) {
+      uint32_t bin[EVICT_SPLIT], sum = 0;
+#pragma unroll
+      for (int s = 0; s < EVICT_SPLIT; ++s) bin[s] = s < split ? cluster.map_shared_rank(&hist[d][0], s)[tid] : 0u;
+#pragma unroll
+      for (int s = 0; s < EVICT_SPLIT; ++s) sum += bin[s];
+      all[tid] = sum;
+    }
+    __syncthreads();
+    {
+      // every warp for itself: lane l has digits 255 - 8 l down to 248 - 8 l
       uint32_t bin[8], sum = 0;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) bin[u] = 0;
-      for (int s = 0; s < split; ++s) {
-        const uint32_t* h = cluster.map_shared_rank(&hist[d][0], s);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) bin[u] += h[255 - 8 * lane - u];
-      }
-#pragma unroll
-      for (int u = 0; u < 8; ++u) sum += bin[u];
+      for (int u = 0; u < 8; ++u) { bin[u] = all[255 - 8 * lane - u]; sum += bin[u]; }
       uint32_t inc = sum;
+#pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const uint32_t other = __shfl_up_sync(0xffffffffu, inc, o);
         if (lane >= o) inc += other;
       }
-      uint32_t above = inc - sum;
-      if (above < (uint32_t)need && inc >= (uint32_t)need) {
+      uint32_t above = inc - sum, digit = 0, left = 0;
+      const bool here = above < (uint32_t)need && inc >= (uint32_t)need;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          if (above < (uint32_t)need && above + bin[u] >= (uint32_t)need) {
-            s_prefix = (prefix << 8) | (uint32_t)(255 - 8 * lane - u);
-            s_need = need - (int)above;
-          }
-          above += bin[u];
-        }
+      for (int u = 0; u < 8; ++u) {
+        if (above < (uint32_t)need && above + bin[u] >= (uint32_t)need) { digit = 255 - 8 * lane - u; left = need - above; }
+        above += bin[u];
       }
+      const int who = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
+      prefix = (prefix << 8) | __shfl_sync(0xffffffffu, digit, who);
+      need = (int)__shfl_sync(0xffffffffu, left, who);
     }
-    __syncthreads();
-    prefix = s_prefix;
-    need = s_need;
-    __syncthreads();
+    __syncthreads();                           // (all[] is written again)
   }
   // ---- rows that have just this key: how many lie in the parts before
   const bool cut = keep > 0;                   // (keep == 0: no row stays)
-  int ties_before = 0;
+  int ties = 0;
   {
     int mine = 0;
     for (int i = tid; i < n; i += RANK_THREADS) mine += cut && key_at(i) == prefix;
-    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    mine = __reduce_add_sync(0xffffffffu, mine);
     if (lane == 0 && mine) atomicAdd(&ties_here, mine);
     cluster.sync();
-    for (int s = 0; s < rank; ++s) ties_before += *cluster.map_shared_rank(&ties_here, s);
+    ties = __reduce_add_sync(0xffffffffu, lane < rank ? *cluster.map_shared_rank(&ties_here, lane) : 0);
   }
   // ---- a bit for every row, holes and movers before each chunk
-  int holes = 0, movers = 0, ties = ties_before;
+  int holes = 0, movers = 0;
   const int64_t word0 = (int64_t)local * a.words;
-  for (int i0 = 0; i0 < part; i0 += RANK_THREADS) {
+  for (int i0 = 0; i0 < n; i0 += RANK_THREADS) {
     const int i = i0 + tid, j = j0 + i;
     const uint32_t k = i < n ? key_at(i) : 0u;
     const bool tie = i < n && cut && k == prefix;
     const uint32_t tie_mask = __ballot_sync(0xffffffffu, tie);
     if (lane == 0) warp_n[warp][0] = __popc(tie_mask);
     __syncthreads();
-    int t = ties;
-    for (int w = 0; w < warp; ++w) t += warp_n[w][0];
+    // (lane w looks at warp w)
+    const int warp_ties = warp_n[lane][0];
+    const int t = ties + __reduce_add_sync(0xffffffffu, lane < warp ? warp_ties : 0);
     const bool stays = i < n && cut && (k > prefix || (tie && t + __popc(tie_mask & ((1u << lane) - 1)) < need));
     const uint32_t bits = __ballot_sync(0xffffffffu, stays);
     const uint32_t hole = __ballot_sync(0xffffffffu, i < n && !stays && j < keep), mover = __ballot_sync(0xffffffffu, stays && j >= keep);
@@ -523,12 +532,15 @@ evict_rank_kernel(EvictArgs a) {
       warp_n[warp][2] = __popc(mover);
     }
     __syncthreads();
-    if (tid % EVICT_CHUNK == 0 && i < n) {
-      int h = holes, m = movers;
-      for (int w = 0; w < warp; ++w) { h += warp_n[w][1]; m += warp_n[w][2]; }
-      a.before[(word0 >> 3) + j / EVICT_CHUNK] = make_int2(h, m);
+    const int warp_holes = warp_n[lane][1], warp_movers = warp_n[lane][2];
+    if (warp % (EVICT_CHUNK / 32) == 0 && i0 + 32 * warp < n) {
+      const int h = holes + __reduce_add_sync(0xffffffffu, lane < warp ? warp_holes : 0);
+      const int m = movers + __reduce_add_sync(0xffffffffu, lane < warp ? warp_movers : 0);
+      if (lane == 0) a.before[(word0 >> 3) + j / EVICT_CHUNK] = make_int2(h, m);
     }
-    for (int w = 0; w < RANK_THREADS / 32; ++w) { ties += warp_n[w][0]; holes += warp_n[w][1]; movers += warp_n[w][2]; }
+    ties += __reduce_add_sync(0xffffffffu, warp_ties);
+    holes += __reduce_add_sync(0xffffffffu, warp_holes);
+    movers += __reduce_add_sync(0xffffffffu, warp_movers);
     __syncthreads();
   }
   if (tid == 0) a.total[local * EVICT_SPLIT + rank] = make_int2(holes, movers);
@@ -536,61 +548,83 @@ evict_rank_kernel(EvictArgs a) {
 }
 
 // Persistent CTAs over the chunks of 256 rows behind the first keep[b] rows of every sequence that is cut.  A chunk's movers are listed,
-// their holes found by the numbers of holes before each chunk, and a warp copies a row's K or V at a time.  Movers lie behind the rows
-// that stay in place and holes among them, so no row is both read and written.
+// their holes found by the numbers of holes before each chunk (in shared memory), and a warp copies a row's K or V at a time.  Movers lie
+// behind the rows that stay in place and holes among them, so no row is both read and written.  The block that is done last sets the lengths,
+// which the others read.  Launched as a dependent of the ranking.
+constexpr int MOVE_BEFORE = 2048;              // chunks whose holes fit shared memory (longer budgets: read where they lie)
 __global__ void __launch_bounds__(MOVE_THREADS)
 evict_move_kernel(EvictArgs a, int n_seq, int split, int row_bytes) {
   __shared__ long long pre[PREFIX_MAX + 1], sums[32];
-  __shared__ int src[EVICT_CHUNK], dst[EVICT_CHUNK], warp_n[EVICT_CHUNK / 32];
+  __shared__ int src[EVICT_CHUNK], dst[EVICT_CHUNK], warp_n[EVICT_CHUNK / 32], hole_before[MOVE_BEFORE];
+  __shared__ bool last;
   const Cache& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const long long items = block_prefix<MOVE_THREADS>(n_seq, pre, sums, [&](int l) {
     const int held = held_rows(c, a.first_seq + l), keep = a.keep[a.first_seq + l];
     return keep < 0 || held <= keep ? 0LL : (long long)(held - 1) / EVICT_CHUNK - keep / EVICT_CHUNK + 1;
   });
+  dep_wait();
+  int noted = -1;                              // the sequence whose holes are in shared memory
   for (long long item = blockIdx.x; item < items; item += gridDim.x) {
     const int l = find_share(pre, n_seq, item), b = a.first_seq + l;
     const int held = held_rows(c, b), keep = a.keep[b];
     const int part = (int)((((int64_t)held + split - 1) / split + EVICT_CHUNK - 1) / EVICT_CHUNK) * EVICT_CHUNK;
     const int chunk = keep / EVICT_CHUNK + (int)(item - pre[l]), per = part / EVICT_CHUNK;
     const int64_t word0 = (int64_t)l * a.words, chunk0 = word0 >> 3;
-    const int2* total = a.total + l * EVICT_SPLIT;
+    const int chunks = (keep + EVICT_CHUNK - 1) / EVICT_CHUNK;       // with holes
+    const bool near = chunks <= MOVE_BEFORE;
+    // holes and movers of the parts, one to a lane
+    const int2 whole = lane < split ? __ldcg(&a.total[l * EVICT_SPLIT + lane]) : make_int2(0, 0);
+    const int movers_before = __ldcg(&a.before[chunk0 + chunk].y);
+    if (near && noted != l) {
+      for (int i = tid; i < chunks; i += MOVE_THREADS) hole_before[i] = __ldcg(&a.before[chunk0 + i].x);
+      noted = l;
+    }
     // the chunk's movers, in order
     uint32_t mine = 0;
     const int j = chunk * EVICT_CHUNK + tid;
     if (tid < EVICT_CHUNK) {
-      const uint32_t bits = chunk * EVICT_CHUNK + 32 * warp < held ? a.bits[word0 + chunk * (EVICT_CHUNK / 32) + warp] : 0u;
+      const uint32_t bits = chunk * EVICT_CHUNK + 32 * warp < held ? __ldcg(&a.bits[word0 + chunk * (EVICT_CHUNK / 32) + warp]) : 0u;
       mine = __ballot_sync(0xffffffffu, ((bits >> lane) & 1u) && j >= keep);
       if (lane == 0) warp_n[warp] = __popc(mine);
     }
     __syncthreads();
     int n = 0, at = 0;
+#pragma unroll
     for (int w = 0; w < EVICT_CHUNK / 32; ++w) { if (w < warp) at += warp_n[w]; n += warp_n[w]; }
     if (tid < EVICT_CHUNK && ((mine >> lane) & 1u)) src[at + __popc(mine & ((1u << lane) - 1))] = j;
     // mover i of the chunk takes hole r of the sequence
-    int r0 = a.before[chunk0 + chunk].y;
-    for (int s = 0; s < chunk / per; ++s) r0 += total[s].y;
-    if (tid < n) {
+    const int r0 = movers_before + __reduce_add_sync(0xffffffffu, lane < chunk / per ? whole.y : 0);
+    if (32 * warp < n) {                       // (whole warps: the parts' holes come by shuffles)
       int r = r0 + tid, s = 0;
-      while (s < split - 1 && r >= total[s].x) { r -= total[s].x; ++s; }
-      // the last chunk of part s with no more than r holes before it
-      int lo = s * per, hi = min((s + 1) * per, (keep + EVICT_CHUNK - 1) / EVICT_CHUNK);
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.before[chunk0 + mid].x <= r) lo = mid; else hi = mid;
+#pragma unroll
+      for (int u = 0; u < EVICT_SPLIT - 1; ++u) {
+        const int holes = __shfl_sync(0xffffffffu, whole.x, u);
+        if (s == u && u < split - 1 && r >= holes) { r -= holes; ++s; }
       }
-      r -= a.before[chunk0 + lo].x;
-      int hole = -1;
-      for (int w = 0; w < EVICT_CHUNK / 32 && hole < 0; ++w) {
-        const int j32 = lo * EVICT_CHUNK + 32 * w;
-        if (j32 >= keep) break;
-        uint32_t free = ~a.bits[word0 + (j32 >> 5)];
-        if (keep - j32 < 32) free &= (1u << (keep - j32)) - 1;
-        const int m = __popc(free);
-        if (r < m) hole = j32 + __fns(free, 0, r + 1);
-        else r -= m;
+      if (tid < n) {
+        // the last chunk of part s with no more than r holes before it
+        int lo = s * per, hi = min((s + 1) * per, chunks);
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if ((near ? hole_before[mid] : __ldcg(&a.before[chunk0 + mid].x)) <= r) lo = mid; else hi = mid;
+        }
+        r -= near ? hole_before[lo] : __ldcg(&a.before[chunk0 + lo].x);
+        const uint4* words = reinterpret_cast<const uint4*>(a.bits + word0 + lo * (EVICT_CHUNK / 32));
+        const uint4 w0 = __ldcg(words), w1 = __ldcg(words + 1);
+        const uint32_t stay[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+        int hole = -1;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+          const int j32 = lo * EVICT_CHUNK + 32 * w;
+          uint32_t free = j32 < keep ? ~stay[w] : 0u;
+          if (j32 < keep && keep - j32 < 32) free &= (1u << (keep - j32)) - 1;
+          const int m = __popc(free);
+          if (hole < 0 && r < m) hole = j32 + __fns(free, 0, r + 1);
+          if (hole < 0) r -= m;
+        }
+        dst[tid] = hole;
       }
-      dst[tid] = hole;
     }
     __syncthreads();
     for (int u = warp; u < 2 * n; u += MOVE_THREADS / 32) {
@@ -618,14 +652,17 @@ evict_move_kernel(EvictArgs a, int n_seq, int split, int row_bytes) {
     }
     __syncthreads();
   }
-}
-
-// behind the moves, whose blocks still read the old lengths
-__global__ void evict_len_kernel(EvictArgs a, int n_seq) {
-  const int b = a.first_seq + blockIdx.x * blockDim.x + threadIdx.x;
-  if (b >= a.first_seq + n_seq) return;
-  const int keep = a.keep[b];
-  if (keep >= 0 && held_rows(a.c, b) > keep) a.c.len[b] = keep;
+  if (tid == 0) {
+    __threadfence();
+    last = atomicAdd(a.arrived, 1) == (int)gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!last) return;
+  if (tid == 0) *a.arrived = 0;
+  for (int l = tid; l < n_seq; l += MOVE_THREADS) {
+    const int keep = a.keep[a.first_seq + l];
+    if (keep >= 0 && held_rows(c, a.first_seq + l) > keep) c.len[a.first_seq + l] = keep;
+  }
 }
 
 template <typename T, int D>
@@ -719,7 +756,8 @@ spts_status launch_paged_evict(spts_ctx* ctx, const spts_paged_kv* cache, const 
   a.c = make_cache(cache); a.keep = keep; a.n_sink = n_sink; a.n_recent = n_recent;
   a.words = (int)align_up((size_t)capacity, EVICT_CHUNK) / 32;
   a.bits = ctx->ws.evict_bits; a.before = ctx->ws.evict_before; a.total = ctx->ws.evict_total; a.status = ctx->ws.status;
-  // one CTA ranks what it can hold in a few rounds of its threads; longer sequences are shared by a cluster
+  a.arrived = ctx->ws.paged_arrived + 1;
+  // one CTA ranks what it holds in a few rounds of its threads; longer sequences are shared by a cluster, whose barriers cost more
   const int split = capacity <= 8 * RANK_THREADS ? 1 : EVICT_SPLIT;
   const int part = (int)align_up((size_t)ceil_div(capacity, split), EVICT_CHUNK);
   const bool smem = part <= RANK_KEYS;
@@ -739,10 +777,9 @@ spts_status launch_paged_evict(spts_ctx* ctx, const spts_paged_kv* cache, const 
     if (cudaLaunchKernelEx(&cfg, smem ? evict_rank_kernel<true> : evict_rank_kernel<false>, a) != cudaSuccess) return SPTS_ERR_CUDA;
     ctx->launches++;
     const int64_t items = (int64_t)n * (a.words / (EVICT_CHUNK / 32));
-    evict_move_kernel<<<(int)(items < 2 * ctx->sm_count ? items : 2 * ctx->sm_count), MOVE_THREADS, 0, ctx->stream>>>(a, n, split, row_bytes);
-    SPTS_CUDA_OK(ctx);
-    evict_len_kernel<<<ceil_div(n, 256), 256, 0, ctx->stream>>>(a, n);
-    SPTS_CUDA_OK(ctx);
+    const int move = (int)(items < 2 * ctx->sm_count ? items : 2 * ctx->sm_count);
+    if (launch_dependent(evict_move_kernel, dim3(move), dim3(MOVE_THREADS), ctx->stream, a, n, split, row_bytes) != cudaSuccess) return SPTS_ERR_CUDA;
+    ctx->launches++;
   }
   return SPTS_OK;
 }
