@@ -362,7 +362,7 @@ paged_weights_plain_kernel(Cache c, const T* __restrict__ Q, int64_t ldq, const 
 // ------------------------------------------------------------------------------------------------ eviction
 constexpr int RANK_THREADS = 1024;
 constexpr int RANK_KEYS = 24576;               // rows of a CTA whose keys and positions fit shared memory
-constexpr int MOVE_THREADS = 1024;
+constexpr int MOVE_THREADS = 512;
 
 // Order of the rows of a sequence: the larger key stays.  Rows that stay before all others have the largest one, NaN the smallest.
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -383,18 +383,41 @@ struct EvictArgs {
 };
 
 // A cluster of CTAs ranks one sequence's rows: each holds the keys of a contiguous part in shared memory; the smallest key that stays is
-// found by a radix select of four digits, whose histograms meet in distributed shared memory (a thread for each bin, the CTAs' bins all on
-// their way at once); of the rows that have just this key the first ones stay.  What comes out is a bit for each row, and the numbers of
+// found by a radix select of three digits (of eleven, eleven and ten bits), whose histograms meet in distributed shared memory (a thread for
+// two bins, the CTAs' bins all on their way at once); of the rows that have just this key the first ones stay.  What comes out is a bit for each row, and the numbers of
 // holes (rows among the first keep that go) and movers (rows behind them that stay) before each chunk of 256 rows, from which
 // evict_move_kernel finds its copies.  Parts too long for shared memory (capacities beyond 196,608 rows) read their weights again for every
 // digit.  Bound by the chain of barriers and round trips.
+constexpr int BINS = 2 * RANK_THREADS;
+static_assert(BINS == 2048, "two bins of a digit of eleven bits to a thread");
+
+// Rows of a CTA's part of a sequence: whole words for each of its warps, whole chunks.
+__host__ __device__ __forceinline__ int part_rows(int held, int split) {
+  return (int)((((int64_t)held + split - 1) / split + RANK_THREADS - 1) / RANK_THREADS) * RANK_THREADS;
+}
+// Sum of v over the threads before this one.
+__device__ __forceinline__ int block_above(int v, int (*warp_n)[3]) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int inc = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int other = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += other;
+  }
+  if (lane == 31) warp_n[warp][0] = inc;
+  __syncthreads();
+  const int w = warp_n[lane][0];
+  return inc - v + __reduce_add_sync(0xffffffffu, lane < warp ? w : 0);
+}
+
 template <bool SMEM>
 __global__ void __launch_bounds__(RANK_THREADS)
 evict_rank_kernel(EvictArgs a) {
   extern __shared__ __align__(16) uint32_t keys[];                       // [part], then positions [part]
-  __shared__ uint32_t hist[4][256], all[256];
+  __shared__ __align__(16) uint32_t hist[3][BINS];
   __shared__ long long newest_here, newest_all;
-  __shared__ int ties_here, warp_n[RANK_THREADS / 32][3];
+  __shared__ int ties_here, warp_n[RANK_THREADS / 32][3], s_need;
+  __shared__ uint32_t s_digit;
   cg::cluster_group cluster = cg::this_cluster();
   const int split = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const Cache& c = a.c;
@@ -402,10 +425,10 @@ evict_rank_kernel(EvictArgs a) {
   dep_launch();
   const int held = held_rows(c, b), keep = a.keep[b];
   if (keep < 0 || held <= keep) return;        // (the same for all CTAs of a cluster)
-  const int part = (int)((((int64_t)held + split - 1) / split + EVICT_CHUNK - 1) / EVICT_CHUNK) * EVICT_CHUNK;
+  const int part = part_rows(held, split);
   const int j0 = (int)min((int64_t)held, (int64_t)rank * part), n = min(part, held - j0);
   uint32_t* spos = keys + part;
-  for (int i = tid; i < 4 * 256; i += RANK_THREADS) (&hist[0][0])[i] = 0;
+  for (int i = tid; i < 3 * BINS; i += RANK_THREADS) (&hist[0][0])[i] = 0;
   if (tid == 0) { newest_here = LLONG_MIN; ties_here = 0; }
   __syncthreads();
   const bool by_pos = a.n_sink > 0 || a.n_recent > 0;
@@ -459,196 +482,191 @@ evict_rank_kernel(EvictArgs a) {
   // ---- the smallest key that stays
   uint32_t prefix = 0;
   int need = keep;                             // rows still to be taken among those with the digits found so far
-  for (int d = 0; d < 4 && keep > 0; ++d) {
-    const int shift = 24 - 8 * d;
+  for (int d = 0; d < 3 && keep > 0; ++d) {
+    const int shift = d == 0 ? 21 : d == 1 ? 10 : 0, known = d == 1 ? 21 : 10;
+    const uint32_t mask = d == 2 ? 1023u : 2047u;
     for (int i = tid; i < n; i += RANK_THREADS) {
       const uint32_t k = key_at(i);
-      if (d == 0 || (k >> (shift + 8)) == prefix) atomicAdd(&hist[d][(k >> shift) & 255], 1u);
+      if (d == 0 || (k >> known) == prefix) atomicAdd(&hist[d][(k >> shift) & mask], 1u);
     }
     cluster.sync();
-    if (tid < 256) {
-      uint32_t bin[EVICT_SPLIT], sum = 0;
-#pragma unroll
-      for (int s = 0; s < EVICT_SPLIT; ++s) bin[s] = s < split ? cluster.map_shared_rank(&hist[d][0], s)[tid] : 0u;
-#pragma unroll
-      for (int s = 0; s < EVICT_SPLIT; ++s) sum += bin[s];
-      all[tid] = sum;
-    }
-    __syncthreads();
+    // thread t has bins BINS - 1 - 2 t and BINS - 2 - 2 t; sums run from the largest digit down
+    uint2 bin = make_uint2(0u, 0u);            // (x: the lower one)
     {
-      // every warp for itself: lane l has digits 255 - 8 l down to 248 - 8 l
-      uint32_t bin[8], sum = 0;
+      uint2 from[EVICT_SPLIT];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) { bin[u] = all[255 - 8 * lane - u]; sum += bin[u]; }
-      uint32_t inc = sum;
+      for (int r = 0; r < EVICT_SPLIT; ++r)
+        from[r] = r < split ? *reinterpret_cast<const uint2*>(cluster.map_shared_rank(&hist[d][0], r) + BINS - 2 - 2 * tid) : make_uint2(0u, 0u);
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t other = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += other;
-      }
-      uint32_t above = inc - sum, digit = 0, left = 0;
-      const bool here = above < (uint32_t)need && inc >= (uint32_t)need;
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        if (above < (uint32_t)need && above + bin[u] >= (uint32_t)need) { digit = 255 - 8 * lane - u; left = need - above; }
-        above += bin[u];
-      }
-      const int who = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
-      prefix = (prefix << 8) | __shfl_sync(0xffffffffu, digit, who);
-      need = (int)__shfl_sync(0xffffffffu, left, who);
+      for (int r = 0; r < EVICT_SPLIT; ++r) { bin.x += from[r].x; bin.y += from[r].y; }
     }
-    __syncthreads();                           // (all[] is written again)
+    const int above = block_above((int)(bin.x + bin.y), warp_n);
+    if (above < need && above + (int)bin.y >= need) { s_digit = BINS - 1 - 2 * tid; s_need = need - above; }
+    else if (above + (int)bin.y < need && above + (int)(bin.x + bin.y) >= need) { s_digit = BINS - 2 - 2 * tid; s_need = need - above - (int)bin.y; }
+    __syncthreads();
+    prefix = (prefix << (d == 2 ? 10 : 11)) | s_digit;
+    need = s_need;
+    __syncthreads();
   }
-  // ---- rows that have just this key: how many lie in the parts before
+  // ---- a warp has part / 32 neighbouring rows from here on
   const bool cut = keep > 0;                   // (keep == 0: no row stays)
+  const int per_warp = part / (RANK_THREADS / 32), w0 = warp * per_warp, w1 = min(n, w0 + per_warp);
+  // rows that have just this key: how many lie in the parts and warps before
   int ties = 0;
   {
     int mine = 0;
-    for (int i = tid; i < n; i += RANK_THREADS) mine += cut && key_at(i) == prefix;
+    for (int i = w0 + lane; i < w1; i += 32) mine += cut && key_at(i) == prefix;
     mine = __reduce_add_sync(0xffffffffu, mine);
     if (lane == 0 && mine) atomicAdd(&ties_here, mine);
+    if (lane == 0) warp_n[warp][0] = mine;
     cluster.sync();
-    ties = __reduce_add_sync(0xffffffffu, lane < rank ? *cluster.map_shared_rank(&ties_here, lane) : 0);
+    ties = __reduce_add_sync(0xffffffffu, (lane < rank ? *cluster.map_shared_rank(&ties_here, lane) : 0) + (lane < warp ? warp_n[lane][0] : 0));
   }
-  // ---- a bit for every row, holes and movers before each chunk
+  // a bit for every row
   int holes = 0, movers = 0;
   const int64_t word0 = (int64_t)local * a.words;
-  for (int i0 = 0; i0 < n; i0 += RANK_THREADS) {
-    const int i = i0 + tid, j = j0 + i;
-    const uint32_t k = i < n ? key_at(i) : 0u;
-    const bool tie = i < n && cut && k == prefix;
+  for (int i0 = w0; i0 < w1; i0 += 32) {
+    const int i = i0 + lane, j = j0 + i;
+    const uint32_t k = i < w1 ? key_at(i) : 0u;
+    const bool tie = i < w1 && cut && k == prefix;
     const uint32_t tie_mask = __ballot_sync(0xffffffffu, tie);
-    if (lane == 0) warp_n[warp][0] = __popc(tie_mask);
-    __syncthreads();
-    // (lane w looks at warp w)
-    const int warp_ties = warp_n[lane][0];
-    const int t = ties + __reduce_add_sync(0xffffffffu, lane < warp ? warp_ties : 0);
-    const bool stays = i < n && cut && (k > prefix || (tie && t + __popc(tie_mask & ((1u << lane) - 1)) < need));
+    const bool stays = i < w1 && cut && (k > prefix || (tie && ties + __popc(tie_mask & ((1u << lane) - 1)) < need));
+    ties += __popc(tie_mask);
     const uint32_t bits = __ballot_sync(0xffffffffu, stays);
-    const uint32_t hole = __ballot_sync(0xffffffffu, i < n && !stays && j < keep), mover = __ballot_sync(0xffffffffu, stays && j >= keep);
-    if (lane == 0) {
-      if (i < n) a.bits[word0 + (j >> 5)] = bits;        // (parts begin on a chunk)
-      warp_n[warp][1] = __popc(hole);
-      warp_n[warp][2] = __popc(mover);
+    holes += __popc(__ballot_sync(0xffffffffu, i < w1 && !stays && j < keep));
+    movers += __popc(__ballot_sync(0xffffffffu, stays && j >= keep));
+    if (lane == 0) a.bits[word0 + (j >> 5)] = bits;      // (parts begin on a chunk, warps on a word)
+    if (SMEM) {
+      __syncwarp();
+      if (lane == 0) keys[w0 + (i0 - w0) / 32] = bits;   // in the place of a row that is done with
     }
-    __syncthreads();
-    const int warp_holes = warp_n[lane][1], warp_movers = warp_n[lane][2];
-    if (warp % (EVICT_CHUNK / 32) == 0 && i0 + 32 * warp < n) {
-      const int h = holes + __reduce_add_sync(0xffffffffu, lane < warp ? warp_holes : 0);
-      const int m = movers + __reduce_add_sync(0xffffffffu, lane < warp ? warp_movers : 0);
-      if (lane == 0) a.before[(word0 >> 3) + j / EVICT_CHUNK] = make_int2(h, m);
-    }
-    ties += __reduce_add_sync(0xffffffffu, warp_ties);
-    holes += __reduce_add_sync(0xffffffffu, warp_holes);
-    movers += __reduce_add_sync(0xffffffffu, warp_movers);
-    __syncthreads();
   }
+  // holes and movers before each chunk
+  if (lane == 0) { warp_n[warp][1] = holes; warp_n[warp][2] = movers; }
+  __syncthreads();
+  const int warp_holes = warp_n[lane][1], warp_movers = warp_n[lane][2];
+  holes = __reduce_add_sync(0xffffffffu, lane < warp ? warp_holes : 0);
+  movers = __reduce_add_sync(0xffffffffu, lane < warp ? warp_movers : 0);
+  __syncwarp();
+  for (int i0 = w0; i0 < w1; i0 += 32) {
+    const int j = j0 + i0;
+    const uint32_t bits = SMEM ? keys[w0 + (i0 - w0) / 32] : a.bits[word0 + (j >> 5)], there = w1 - i0 >= 32 ? 0xFFFFFFFFu : (1u << (w1 - i0)) - 1;
+    const uint32_t front = j + 32 <= keep ? 0xFFFFFFFFu : j >= keep ? 0u : (1u << (keep - j)) - 1;       // rows below keep
+    if (lane == 0 && j % EVICT_CHUNK == 0) a.before[(word0 >> 3) + j / EVICT_CHUNK] = make_int2(holes, movers);
+    holes += __popc(~bits & there & front);
+    movers += __popc(bits & ~front);
+  }
+  holes = __reduce_add_sync(0xffffffffu, warp_holes);
+  movers = __reduce_add_sync(0xffffffffu, warp_movers);
   if (tid == 0) a.total[local * EVICT_SPLIT + rank] = make_int2(holes, movers);
   cluster.sync();                              // the histograms are read by other CTAs of the cluster until here
 }
 
-// Persistent CTAs over the chunks of 256 rows behind the first keep[b] rows of every sequence that is cut.  A chunk's movers are listed,
-// their holes found by the numbers of holes before each chunk (in shared memory), and a warp copies a row's K or V at a time.  Movers lie
-// behind the rows that stay in place and holes among them, so no row is both read and written.  The block that is done last sets the lengths,
-// which the others read.  Launched as a dependent of the ranking.
-constexpr int MOVE_BEFORE = 2048;              // chunks whose holes fit shared memory (longer budgets: read where they lie)
-__global__ void __launch_bounds__(MOVE_THREADS)
+// Persistent CTAs over groups of sixteen movers: mover r of a sequence and its hole r are found by the numbers of movers and holes before
+// each chunk (in shared memory), and all pieces of their rows are copied side by side.  Movers lie behind the rows that stay in place and
+// holes among them, so no row is both read and written.  The block that is done last sets the lengths, which the others read.  Launched as a
+// dependent of the ranking.
+constexpr int MOVE_ROWS = 16;                  // movers of a group
+constexpr int MOVE_AT_ONCE = 8;                // pieces of a thread in flight
+constexpr int MOVE_CHUNKS = 4096;              // chunks of a sequence whose numbers fit shared memory (beyond 1,048,576 rows they are read where they lie)
+
+// The row of `bits` (words of chunk `chunk`, those outside [from, to) left out) that is set for the (r + 1)-th time; -1: there is none.
+__device__ __forceinline__ int nth_row(const uint32_t* bits, bool set, int chunk, int r, int from, int to) {
+  const uint4* words = reinterpret_cast<const uint4*>(bits + (int64_t)chunk * (EVICT_CHUNK / 32));
+  const uint4 w0 = __ldcg(words), w1 = __ldcg(words + 1);
+  const uint32_t word[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+  int found = -1;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) {
+    const int j = chunk * EVICT_CHUNK + 32 * w;
+    uint32_t x = set ? word[w] : ~word[w];
+    if (j < from) x &= from - j >= 32 ? 0u : ~0u << (from - j);
+    if (j + 32 > to) x &= j >= to ? 0u : (1u << (to - j)) - 1;
+    const int m = __popc(x);
+    if (found < 0 && r < m) found = j + __fns(x, 0, r + 1);
+    if (found < 0) r -= m;
+  }
+  return found;
+}
+
+__global__ void __launch_bounds__(MOVE_THREADS, 2)
 evict_move_kernel(EvictArgs a, int n_seq, int split, int row_bytes) {
   __shared__ long long pre[PREFIX_MAX + 1], sums[32];
-  __shared__ int src[EVICT_CHUNK], dst[EVICT_CHUNK], warp_n[EVICT_CHUNK / 32], hole_before[MOVE_BEFORE];
+  __shared__ int64_t src[MOVE_ROWS], dst[MOVE_ROWS];       // places of the rows
+  __shared__ int2 before[MOVE_CHUNKS];
   __shared__ bool last;
   const Cache& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  dep_wait();
   const long long items = block_prefix<MOVE_THREADS>(n_seq, pre, sums, [&](int l) {
     const int held = held_rows(c, a.first_seq + l), keep = a.keep[a.first_seq + l];
-    return keep < 0 || held <= keep ? 0LL : (long long)(held - 1) / EVICT_CHUNK - keep / EVICT_CHUNK + 1;
+    if (keep < 0 || held <= keep) return 0LL;
+    int movers = 0;
+#pragma unroll
+    for (int s = 0; s < EVICT_SPLIT; ++s) movers += s < split ? __ldcg(&a.total[l * EVICT_SPLIT + s].y) : 0;
+    return (long long)(movers + MOVE_ROWS - 1) / MOVE_ROWS;
   });
-  dep_wait();
-  int noted = -1;                              // the sequence whose holes are in shared memory
+  int noted = -1;                              // the sequence whose numbers are in shared memory
   for (long long item = blockIdx.x; item < items; item += gridDim.x) {
     const int l = find_share(pre, n_seq, item), b = a.first_seq + l;
     const int held = held_rows(c, b), keep = a.keep[b];
-    const int part = (int)((((int64_t)held + split - 1) / split + EVICT_CHUNK - 1) / EVICT_CHUNK) * EVICT_CHUNK;
-    const int chunk = keep / EVICT_CHUNK + (int)(item - pre[l]), per = part / EVICT_CHUNK;
+    const int chunks = (held + EVICT_CHUNK - 1) / EVICT_CHUNK, per = part_rows(held, split) / EVICT_CHUNK;
     const int64_t word0 = (int64_t)l * a.words, chunk0 = word0 >> 3;
-    const int chunks = (keep + EVICT_CHUNK - 1) / EVICT_CHUNK;       // with holes
-    const bool near = chunks <= MOVE_BEFORE;
-    // holes and movers of the parts, one to a lane
-    const int2 whole = lane < split ? __ldcg(&a.total[l * EVICT_SPLIT + lane]) : make_int2(0, 0);
-    const int movers_before = __ldcg(&a.before[chunk0 + chunk].y);
+    const bool near = chunks <= MOVE_CHUNKS;
     if (near && noted != l) {
-      for (int i = tid; i < chunks; i += MOVE_THREADS) hole_before[i] = __ldcg(&a.before[chunk0 + i].x);
+      for (int i = tid; i < chunks; i += MOVE_THREADS) before[i] = __ldcg(&a.before[chunk0 + i]);
       noted = l;
     }
-    // the chunk's movers, in order
-    uint32_t mine = 0;
-    const int j = chunk * EVICT_CHUNK + tid;
-    if (tid < EVICT_CHUNK) {
-      const uint32_t bits = chunk * EVICT_CHUNK + 32 * warp < held ? __ldcg(&a.bits[word0 + chunk * (EVICT_CHUNK / 32) + warp]) : 0u;
-      mine = __ballot_sync(0xffffffffu, ((bits >> lane) & 1u) && j >= keep);
-      if (lane == 0) warp_n[warp] = __popc(mine);
-    }
+    // holes and movers of the parts, one to a lane
+    const int2 whole = lane < split ? __ldcg(&a.total[l * EVICT_SPLIT + lane]) : make_int2(0, 0);
+    const int movers = __reduce_add_sync(0xffffffffu, whole.y);
+    const int r0 = (int)(item - pre[l]) * MOVE_ROWS, n = min(MOVE_ROWS, movers - r0);
     __syncthreads();
-    int n = 0, at = 0;
-#pragma unroll
-    for (int w = 0; w < EVICT_CHUNK / 32; ++w) { if (w < warp) at += warp_n[w]; n += warp_n[w]; }
-    if (tid < EVICT_CHUNK && ((mine >> lane) & 1u)) src[at + __popc(mine & ((1u << lane) - 1))] = j;
-    // mover i of the chunk takes hole r of the sequence
-    const int r0 = movers_before + __reduce_add_sync(0xffffffffu, lane < chunk / per ? whole.y : 0);
-    if (32 * warp < n) {                       // (whole warps: the parts' holes come by shuffles)
-      int r = r0 + tid, s = 0;
+    if (warp < 2) {
+      // warp 0 finds the movers, warp 1 their holes
+      const bool hole = warp == 1;
+      int r = r0 + lane, s = 0;
 #pragma unroll
       for (int u = 0; u < EVICT_SPLIT - 1; ++u) {
-        const int holes = __shfl_sync(0xffffffffu, whole.x, u);
-        if (s == u && u < split - 1 && r >= holes) { r -= holes; ++s; }
+        const int here = __shfl_sync(0xffffffffu, hole ? whole.x : whole.y, u);
+        if (s == u && u < split - 1 && r >= here) { r -= here; ++s; }
       }
-      if (tid < n) {
-        // the last chunk of part s with no more than r holes before it
+      if (lane < n) {
+        // the last chunk of part s with no more than r before it
+        const auto number = [&](int chunk) {
+          const int2 x = near ? before[chunk] : __ldcg(&a.before[chunk0 + chunk]);
+          return hole ? x.x : x.y;
+        };
         int lo = s * per, hi = min((s + 1) * per, chunks);
         while (hi - lo > 1) {
           const int mid = (lo + hi) >> 1;
-          if ((near ? hole_before[mid] : __ldcg(&a.before[chunk0 + mid].x)) <= r) lo = mid; else hi = mid;
+          if (number(mid) <= r) lo = mid; else hi = mid;
         }
-        r -= near ? hole_before[lo] : __ldcg(&a.before[chunk0 + lo].x);
-        const uint4* words = reinterpret_cast<const uint4*>(a.bits + word0 + lo * (EVICT_CHUNK / 32));
-        const uint4 w0 = __ldcg(words), w1 = __ldcg(words + 1);
-        const uint32_t stay[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
-        int hole = -1;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) {
-          const int j32 = lo * EVICT_CHUNK + 32 * w;
-          uint32_t free = j32 < keep ? ~stay[w] : 0u;
-          if (j32 < keep && keep - j32 < 32) free &= (1u << (keep - j32)) - 1;
-          const int m = __popc(free);
-          if (hole < 0 && r < m) hole = j32 + __fns(free, 0, r + 1);
-          if (hole < 0) r -= m;
-        }
-        dst[tid] = hole;
+        const int j = nth_row(a.bits + word0, !hole, lo, r - number(lo), hole ? 0 : keep, hole ? keep : held);
+        (hole ? dst : src)[lane] = j < 0 ? -1 : slot_of(c, b, j);
       }
     }
     __syncthreads();
-    for (int u = warp; u < 2 * n; u += MOVE_THREADS / 32) {
-      const int js = src[u >> 1], jd = dst[u >> 1];
-      if (jd < 0) continue;
-      const int64_t from = slot_of(c, b, js), to = slot_of(c, b, jd);
-      if (from < 0 || to < 0) continue;
-      const char* base = (u & 1) ? c.v : c.k;
-      const uint4* s = reinterpret_cast<const uint4*>(base + from * row_bytes);
-      uint4* d = reinterpret_cast<uint4*>(const_cast<char*>(base) + to * row_bytes);
-      const int pieces = row_bytes >> 4;
-      for (int i = lane; i < pieces; i += 128) {
-        uint4 x[4];
+    // all rows' pieces of 16 bytes one after the other, K and V of a row in turn
+    const int pieces = row_bytes >> 4, total = 2 * n * pieces;
+    for (int u0 = tid; u0 < total; u0 += MOVE_AT_ONCE * MOVE_THREADS) {
+      uint4 x[MOVE_AT_ONCE];
 #pragma unroll
-        for (int v = 0; v < 4; ++v)
-          if (i + 32 * v < pieces) x[v] = s[i + 32 * v];
+      for (int v = 0; v < MOVE_AT_ONCE; ++v) {
+        const int u = u0 + v * MOVE_THREADS, r = u / pieces;
+        if (u < total && src[r >> 1] >= 0)
+          x[v] = reinterpret_cast<const uint4*>(((r & 1) ? c.v : c.k) + src[r >> 1] * row_bytes)[u - r * pieces];
+      }
 #pragma unroll
-        for (int v = 0; v < 4; ++v)
-          if (i + 32 * v < pieces) d[i + 32 * v] = x[v];
+      for (int v = 0; v < MOVE_AT_ONCE; ++v) {
+        const int u = u0 + v * MOVE_THREADS, r = u / pieces;
+        if (u < total && src[r >> 1] >= 0 && dst[r >> 1] >= 0)
+          reinterpret_cast<uint4*>(const_cast<char*>((r & 1) ? c.v : c.k) + dst[r >> 1] * row_bytes)[u - r * pieces] = x[v];
       }
-      if (lane == 0) {
-        if (u & 1) c.weight[to] = c.weight[from];
-        else if (c.pos != nullptr) c.pos[to] = c.pos[from];
-      }
+    }
+    if (tid < n && src[tid] >= 0 && dst[tid] >= 0) {
+      c.weight[dst[tid]] = c.weight[src[tid]];
+      if (c.pos != nullptr) c.pos[dst[tid]] = c.pos[src[tid]];
     }
     __syncthreads();
   }
@@ -759,7 +777,7 @@ spts_status launch_paged_evict(spts_ctx* ctx, const spts_paged_kv* cache, const 
   a.arrived = ctx->ws.paged_arrived + 1;
   // one CTA ranks what it holds in a few rounds of its threads; longer sequences are shared by a cluster, whose barriers cost more
   const int split = capacity <= 8 * RANK_THREADS ? 1 : EVICT_SPLIT;
-  const int part = (int)align_up((size_t)ceil_div(capacity, split), EVICT_CHUNK);
+  const int part = part_rows(capacity, split);
   const bool smem = part <= RANK_KEYS;
   const int round = SPTS_PAGED_MAX_ROWS / (a.words * 32);             // sequences whose rows have a bit each in the workspace
   for (a.first_seq = 0; a.first_seq < cache->n_seq; a.first_seq += round) {
@@ -776,7 +794,7 @@ spts_status launch_paged_evict(spts_ctx* ctx, const spts_paged_kv* cache, const 
     cfg.numAttrs = 1;
     if (cudaLaunchKernelEx(&cfg, smem ? evict_rank_kernel<true> : evict_rank_kernel<false>, a) != cudaSuccess) return SPTS_ERR_CUDA;
     ctx->launches++;
-    const int64_t items = (int64_t)n * (a.words / (EVICT_CHUNK / 32));
+    const int64_t items = (int64_t)n * a.words * 32 / (2 * MOVE_ROWS);         // no fewer than there are: at most half of the rows move
     const int move = (int)(items < 2 * ctx->sm_count ? items : 2 * ctx->sm_count);
     if (launch_dependent(evict_move_kernel, dim3(move), dim3(MOVE_THREADS), ctx->stream, a, n, split, row_bytes) != cudaSuccess) return SPTS_ERR_CUDA;
     ctx->launches++;
