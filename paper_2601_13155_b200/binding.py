@@ -271,6 +271,8 @@ def _rows(t: torch.Tensor, width: int, dtype, what: str, dev: int):
     shape = t.shape
     if len(shape) == 2 and shape[1] == width and t.stride(1) == 1:
         return t.data_ptr(), (t.stride(0) if shape[0] > 1 else width)
+    if len(shape) == 3 and shape[1] * shape[2] == width and t.is_contiguous():
+        return t.data_ptr(), width
     if len(shape) < 2 or math.prod(shape[1:]) != width:
         raise ValueError(f"{what}: rows of {width} elements are needed, got {tuple(shape)}")
     inner = 1
@@ -781,18 +783,19 @@ class Spts:
     def paged_attention(self, cache: PagedKv, Q: torch.Tensor, row_start=None, O_out=None, lse_out=None, want_lse: bool = False):
         """spts_paged_attention: Q [n, H, d] (or [n, H * d]), the last rows of their sequences -> O [n, H * d]; with want_lse or lse_out
         (O, lse [n, H])."""
-        n, w, dev = Q.shape[0], self.shape.n_q_heads * self.shape.head_dim, self.dev
+        n, heads, dev = Q.shape[0], self.shape.n_q_heads, self.dev
+        w = heads * self.shape.head_dim
         self._paged_shape(cache)
+        qp, ldq = _rows(Q, w, self.dtype, "Q", dev)
         if O_out is None:
-            O_out = torch.empty((n, w), dtype=self.dtype, device=self.device)
-        if O_out.shape[0] != n:
+            O_out = Q.new_empty((n, w))
+        elif O_out.shape[0] != n:
             raise ValueError("as many rows of O_out as of Q are needed")
         if lse_out is None and want_lse:
-            lse_out = torch.empty((n, self.shape.n_q_heads), dtype=torch.float32, device=self.device)
-        qp, ldq = _rows(Q, w, self.dtype, "Q", dev)
+            lse_out = Q.new_empty((n, heads), dtype=torch.float32)
         op, ldo = _rows(O_out, w, self.dtype, "O_out", dev)
         code = self.lib.spts_paged_attention(self.h, cache.c, qp, ldq, _vec(row_start, cache.n_seq + 1, torch.int32, "row_start", dev), n, op,
-                                             ldo, _vec(lse_out, n * self.shape.n_q_heads, torch.float32, "lse_out", dev))
+                                             ldo, _vec(lse_out, n * heads, torch.float32, "lse_out", dev))
         if code:
             raise SptsError(code, "spts_paged_attention")
         return O_out if lse_out is None else (O_out, lse_out)
@@ -826,16 +829,22 @@ class Spts:
             raise ValueError(f"up to {LOGPROBS_MAX_TOP} alternatives, got {n_top}")
         lp, ld = _rows(logits, v, torch.float32, "logits", self.dev)
         tp = _vec(targets, n, torch.int32, "targets", self.dev)
-        f32, i32, new, out = torch.float32, torch.int32, torch.empty, {}
+        new, i32, out, ptr = logits.new_empty, torch.int32, {}, {}
+
+        def make(name, size, **kw):
+            t = out[name] = new(size, **kw)
+            ptr[name] = t.data_ptr()
         if targets is not None:
-            out["logprob"], out["rank"] = new(n, dtype=f32, device=self.device), new(n, dtype=i32, device=self.device)
+            make("logprob", n)
+            make("rank", n, dtype=i32)
         if entropy:
-            out["entropy"] = new(n, dtype=f32, device=self.device)
+            make("entropy", n)
         if n_top:
-            out["top_logprob"], out["top_token"] = new(n, n_top, dtype=f32, device=self.device), new(n, n_top, dtype=i32, device=self.device)
-        ptr = lambda name: out[name].data_ptr() if name in out else None
-        code = self.lib.spts_token_logprobs(self.h, lp, ld, n, v, tp, n_top, ptr("logprob"), ptr("rank"), ptr("entropy"), ptr("top_logprob"),
-                                            ptr("top_token"))
+            make("top_logprob", (n, n_top))
+            make("top_token", (n, n_top), dtype=i32)
+        get = ptr.get
+        code = self.lib.spts_token_logprobs(self.h, lp, ld, n, v, tp, n_top, get("logprob"), get("rank"), get("entropy"), get("top_logprob"),
+                                            get("top_token"))
         if code:
             raise SptsError(code, "spts_token_logprobs")
         return out

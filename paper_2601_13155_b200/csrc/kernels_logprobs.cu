@@ -225,6 +225,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(LogprobArgs a, 
   // token `base` (up to three before the row) lies on a 16-byte boundary, and so do all slices and pieces
   const int base = -(int)((reinterpret_cast<uintptr_t>(x) >> 2) & 3);
   const int64_t v0 = base + (int64_t)slice * per, v1 = min((int64_t)a.vocab, v0 + per);
+  dep_wait();
   const int target = a.target != nullptr ? a.target[row] : -1;
   const bool scored = target >= 0 && target < a.vocab;
   const float xt = scored ? x[target] : 0.f;
@@ -489,9 +490,10 @@ spts_status launch_token_logprobs(spts_ctx* ctx, const float* logits, int64_t ld
     if (time < least) { least = time; slices = s; }
   }
   const int per = slices == 1 ? vocab + 3 : (int)align_up((size_t)ceil_div(vocab + 3, slices), 4);
-  if (n_top > 0) logprobs_kernel<true><<<(unsigned)((int64_t)n * slices), LP_THREADS, 0, ctx->stream>>>(a, slices, per);
-  else logprobs_kernel<false><<<(unsigned)((int64_t)n * slices), LP_THREADS, 0, ctx->stream>>>(a, slices, per);
-  SPTS_CUDA_OK(ctx);
+  if (launch_dependent(n_top > 0 ? logprobs_kernel<true> : logprobs_kernel<false>, dim3((unsigned)((int64_t)n * slices)), dim3(LP_THREADS), ctx->stream, a,
+                       slices, per) != cudaSuccess)
+    return SPTS_ERR_CUDA;
+  ctx->launches++;
   return SPTS_OK;
 }
 

@@ -25,6 +25,7 @@ paged_append_kernel(Cache c, const char* __restrict__ K, int64_t ldk, const char
                     int* arrived, int* status) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int capacity = c.max_pages << c.shift;
+  dep_wait();
   for (int64_t unit = (int64_t)blockIdx.x * APPEND_WARPS + warp; unit < 2 * (int64_t)n_rows; unit += (int64_t)gridDim.x * APPEND_WARPS) {
     const int row = (int)(unit >> 1);
     const bool is_v = unit & 1;
@@ -173,13 +174,14 @@ paged_attn_plain_kernel(Cache c, const T* __restrict__ Q, int64_t ldq, const int
   const int split = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int G = H / Hkv, kvh = blockIdx.y, tid = threadIdx.x;
   const int64_t tile = blockIdx.x / split;
-  const long long tiles = block_prefix<PL_THREADS>(c.n_seq, pre, sums, [&](int b) {
+  block_prefix<PL_THREADS>(c.n_seq, pre, sums, [&](int b) {
     int f, n;
     call_rows(row_start, n_rows, b, f, n);
     if (kvh == 0 && tile == 0) check_starts(row_start, n_rows, b, status);
     return ((long long)n * G + PL_ROWS - 1) / PL_ROWS;
   });
-  if (tile >= tiles) return;                   // (all CTAs of a cluster have the same tile)
+  __syncthreads();
+  if (tile >= pre[c.n_seq]) return;                   // (all CTAs of a cluster have the same tile)
   const int b = find_share(pre, c.n_seq, tile);
   int first, n;
   call_rows(row_start, n_rows, b, first, n);
@@ -311,10 +313,12 @@ paged_weights_plain_kernel(Cache c, const T* __restrict__ Q, int64_t ldq, const 
   __shared__ long long pre[PREFIX_MAX + 1], sums[32];
   const int G = H / Hkv, tid = threadIdx.x, tr = tid >> 4, tk = tid & 15;
   const float scale = rsqrtf((float)D);
-  const long long items = block_prefix<PL_THREADS>(c.n_seq, pre, sums, [&](int b) {
+  block_prefix<PL_THREADS>(c.n_seq, pre, sums, [&](int b) {
     if (blockIdx.x == 0) check_starts(row_start, n_rows, b, status);
     return (long long)(held_rows(c, b) + PL_KEYS - 1) / PL_KEYS;
   });
+  __syncthreads();
+  const long long items = pre[c.n_seq];
   for (long long item = blockIdx.x; item < items; item += gridDim.x) {
     const int b = find_share(pre, c.n_seq, item);
     int first, n;
@@ -422,13 +426,14 @@ evict_rank_kernel(EvictArgs a) {
   const int split = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const Cache& c = a.c;
   const int local = blockIdx.x / split, b = a.first_seq + local, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  for (int i = tid; i < 3 * BINS; i += RANK_THREADS) (&hist[0][0])[i] = 0;
   dep_launch();
+  dep_wait();
   const int held = held_rows(c, b), keep = a.keep[b];
   if (keep < 0 || held <= keep) return;        // (the same for all CTAs of a cluster)
   const int part = part_rows(held, split);
   const int j0 = (int)min((int64_t)held, (int64_t)rank * part), n = min(part, held - j0);
   uint32_t* spos = keys + part;
-  for (int i = tid; i < 3 * BINS; i += RANK_THREADS) (&hist[0][0])[i] = 0;
   if (tid == 0) { newest_here = LLONG_MIN; ties_here = 0; }
   __syncthreads();
   const bool by_pos = a.n_sink > 0 || a.n_recent > 0;
@@ -598,7 +603,7 @@ evict_move_kernel(EvictArgs a, int n_seq, int split, int row_bytes) {
   const Cache& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   dep_wait();
-  const long long items = block_prefix<MOVE_THREADS>(n_seq, pre, sums, [&](int l) {
+  block_prefix<MOVE_THREADS>(n_seq, pre, sums, [&](int l) {
     const int held = held_rows(c, a.first_seq + l), keep = a.keep[a.first_seq + l];
     if (keep < 0 || held <= keep) return 0LL;
     int movers = 0;
@@ -606,6 +611,8 @@ evict_move_kernel(EvictArgs a, int n_seq, int split, int row_bytes) {
     for (int s = 0; s < EVICT_SPLIT; ++s) movers += s < split ? __ldcg(&a.total[l * EVICT_SPLIT + s].y) : 0;
     return (long long)(movers + MOVE_ROWS - 1) / MOVE_ROWS;
   });
+  __syncthreads();
+  const long long items = pre[n_seq];
   int noted = -1;                              // the sequence whose numbers are in shared memory
   for (long long item = blockIdx.x; item < items; item += gridDim.x) {
     const int l = find_share(pre, n_seq, item), b = a.first_seq + l;
@@ -737,9 +744,10 @@ spts_status launch_paged_append(spts_ctx* ctx, const spts_paged_kv* cache, const
   const int es = ctx->desc.dtype == SPTS_BF16 ? 2 : 4, row_bytes = ctx->desc.n_kv_heads * ctx->desc.head_dim * es;
   const int64_t blocks = (2 * (int64_t)n_rows + APPEND_WARPS - 1) / APPEND_WARPS;
   const int grid = (int)(blocks < 1 ? 1 : blocks < 8 * ctx->sm_count ? blocks : 8 * ctx->sm_count);
-  paged_append_kernel<<<grid, APPEND_WARPS * 32, 0, ctx->stream>>>(make_cache(cache), (const char*)K, ldk * es, (const char*)V, ldv * es, row_bytes,
-                                                                   pos, row_start, at, n_rows, ctx->ws.paged_arrived, ctx->ws.status);
-  SPTS_CUDA_OK(ctx);
+  if (launch_dependent(paged_append_kernel, dim3(grid), dim3(APPEND_WARPS * 32), ctx->stream, make_cache(cache), (const char*)K, ldk * es,
+                       (const char*)V, ldv * es, row_bytes, pos, row_start, at, n_rows, ctx->ws.paged_arrived, ctx->ws.status) != cudaSuccess)
+    return SPTS_ERR_CUDA;
+  ctx->launches++;
   return SPTS_OK;
 }
 
@@ -787,11 +795,13 @@ spts_status launch_paged_evict(spts_ctx* ctx, const spts_paged_kv* cache, const 
     cfg.blockDim = dim3(RANK_THREADS);
     cfg.dynamicSmemBytes = smem ? part * 8 : 0;
     cfg.stream = ctx->stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     if (cudaLaunchKernelEx(&cfg, smem ? evict_rank_kernel<true> : evict_rank_kernel<false>, a) != cudaSuccess) return SPTS_ERR_CUDA;
     ctx->launches++;
     const int64_t items = (int64_t)n * a.words * 32 / (2 * MOVE_ROWS);         // no fewer than there are: at most half of the rows move

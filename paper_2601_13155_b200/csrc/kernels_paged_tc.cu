@@ -454,6 +454,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     tmem_relinquish();
   }
   // this CTA's piece of the line; the prefix sums lie where K and V will
+  dep_wait();
   {
     Line line;
     line.make<PA_THREADS>(a, reinterpret_cast<long long*>(gen + (sR - base)), blockIdx.x == 0);
@@ -992,7 +993,7 @@ struct Unit {
 
 struct UnitWalk {
   int b, u, i, row, n, off, held;
-  long long left;
+  long long left, at, total;                   // left of the piece; where it begins, and the line's length
   __device__ __forceinline__ void sequence(const WeightArgs& a) {
     call_rows(a.row_start, a.n_rows, b, row, n);
     held = held_rows(a.c, b);
@@ -1052,20 +1053,22 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
     tmem_alloc(smem_u32((const void*)tmem_slot), PA_COLS);
     tmem_relinquish();
   }
-  long long from = 0, total = 0;
+  dep_wait();
   {
     long long* scratch = reinterpret_cast<long long*>(gen);
     long long* pre = scratch + 32;
-    total = block_prefix<PA_THREADS>(a.c.n_seq, pre, scratch, [&](int b) {
+    const long long total = block_prefix<PA_THREADS>(a.c.n_seq, pre, scratch, [&](int b) {
       int row, n;
       call_rows(a.row_start, a.n_rows, b, row, n);
       if (blockIdx.x == 0) check_starts(a.row_start, a.n_rows, b, a.status);
       const int held = held_rows(a.c, b);
       return held == 0 ? 0LL : items_before(n, held - n, a.tile_tokens, a.Hkv, (held + 2 * BLOCK - 1) / (2 * BLOCK));
     });
-    from = cut_line(total, blockIdx.x, gridDim.x);
     if (warp == 0) {
+      const long long from = cut_line(total, blockIdx.x, gridDim.x);
       UnitWalk w;
+      w.at = from;
+      w.total = total;
       w.left = cut_line(total, blockIdx.x + 1, gridDim.x) - from;
       if (w.left > 0) {
         w.b = find_share(pre, a.c.n_seq, from);
@@ -1192,7 +1195,8 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
     const float sc = LOG2E / (D == 128 ? 11.313708498984761f : 8.0f);
     const float2 sc2 = make_float2(sc, sc);
     uint32_t n_q = 0, n_s = 0;
-    long long at = from;                       // the line's item at which the segment begins
+    long long at = walk.at;                    // the line's item at which the segment begins
+    const long long total = walk.total;
     while (ok && walk.next(a, s)) {
       const int key = (2 * s.u + t) * BLOCK + quarter * 32 + lane;
       const bool work = t == 0 || s.two;
@@ -1314,6 +1318,22 @@ bool map_queries(spts_ctx* ctx, CUtensorMap* tm, const void* p, int64_t ld, int 
   return encode(ctx, tm, p, 3, dim, stride, box);
 }
 
+// As a dependent of what runs before: a CTA sets up its barriers and tensor memory before it waits for that.
+template <typename... KArgs, typename... Args>
+cudaError_t launch_big(spts_ctx* ctx, void (*kernel)(KArgs...), int ctas, int smem, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ctas);
+  cfg.blockDim = dim3(PA_THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = ctx->stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 template <int D>
 spts_status attention_t(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start, int n_rows, void* O,
                         int64_t ldo, float* lse) {
@@ -1335,8 +1355,8 @@ spts_status attention_t(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q
   if (!map_queries(ctx, &tmQ, Q, ldq, n_rows, a.G, a.tile_tokens) || !map_pages(ctx, &tmK, cache->k, cache) || !map_pages(ctx, &tmV, cache->v, cache))
     return SPTS_ERR_CUDA;
   const int ctas = ctx->sm_count < PAGED_MAX_CTAS ? ctx->sm_count : PAGED_MAX_CTAS;
-  paged_attn_kernel<D><<<ctas, PA_THREADS, pa_smem<D>(), ctx->stream>>>(tmQ, tmK, tmV, a);
-  SPTS_CUDA_OK(ctx);
+  if (launch_big(ctx, paged_attn_kernel<D>, ctas, pa_smem<D>(), tmQ, tmK, tmV, a) != cudaSuccess) return SPTS_ERR_CUDA;
+  ctx->launches++;
   if (a.solo) return SPTS_OK;
   if (launch_dependent(paged_attn_join_kernel<D>, dim3(ctas, JOIN_SPLIT), dim3(JOIN_THREADS), ctx->stream, a) != cudaSuccess) return SPTS_ERR_CUDA;
   ctx->launches++;
@@ -1359,8 +1379,8 @@ spts_status weights_t(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, 
   if (!map_queries(ctx, &tmQ, n_rows > 0 ? Q : cache->k, ldq, n_rows > 0 ? n_rows : 1, a.G, a.tile_tokens) || !map_pages(ctx, &tmK, cache->k, cache))
     return SPTS_ERR_CUDA;
   const int ctas = ctx->sm_count < PAGED_MAX_CTAS ? ctx->sm_count : PAGED_MAX_CTAS;
-  paged_weights_kernel<D><<<ctas, PA_THREADS, pw_smem<D>(), ctx->stream>>>(tmQ, tmK, a);
-  SPTS_CUDA_OK(ctx);
+  if (launch_big(ctx, paged_weights_kernel<D>, ctas, pw_smem<D>(), tmQ, tmK, a) != cudaSuccess) return SPTS_ERR_CUDA;
+  ctx->launches++;
   return SPTS_OK;
 }
 

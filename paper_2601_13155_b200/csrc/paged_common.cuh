@@ -51,12 +51,27 @@ __device__ __forceinline__ int64_t slot_of(const Cache& c, int b, int j) {
 }
 
 // Exclusive prefix sums of up to PREFIX_MAX values by a block of NT threads; value(b) is evaluated once for each b.  pre [n + 1] in
-// shared memory; all threads get the total.  `warp_sums`: 32 entries of shared memory.
+// shared memory; all threads get the total.  `warp_sums`: 32 entries of shared memory.  Up to 32 values are summed by the first warp alone,
+// and only its threads get the total then (others: pre[n] behind the block's next barrier).
 static const int PREFIX_MAX = SPTS_PAGED_MAX_SEQ;
 template <int NT, typename F>
 __device__ __forceinline__ long long block_prefix(int n, long long* pre, long long* warp_sums, F value) {
   constexpr int PER = (PREFIX_MAX + NT - 1) / NT;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (n <= 32) {
+    if (warp > 0) return 0;
+    const long long mine = lane < n ? value(lane) : 0;
+    long long inc = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long other = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += other;
+    }
+    if (lane < n) pre[lane] = inc - mine;
+    if (lane == 31) pre[n] = inc;
+    __syncwarp();
+    return __shfl_sync(0xffffffffu, inc, 31);
+  }
   long long v[PER], sum = 0;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
