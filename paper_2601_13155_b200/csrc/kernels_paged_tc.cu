@@ -957,9 +957,12 @@ paged_attn_join_kernel(const __grid_constant__ AttnArgs a) {
 //   warp 0      TMA producer: for every KV head the two blocks of K (two pairs in flight), for every tile of queries its Q (three)
 //   warp 1      TMEM owner and MMA issuer: two accumulators for each of the two blocks
 //   warps 2-3   -lse log2(e) of a tile's queries into shared memory
-//   warps 4-7   the exponentials of the first block, warps 8-11 of the second
-constexpr int PW_Q = 3;                        // tiles of queries in flight
-template <int D> constexpr int pw_smem() { return 1024 + (4 + PW_Q) * tile_bytes<D>() + 256 + PW_Q * BLOCK * 4 + 64; }
+//   warps 4-11  the exponentials of every second item, warps 12-19 of the others; of the first block warps 4-7 and 12-15
+// (bound by the exponential unit where queries are many: with four warps on each of its quarters instead of two 64 queries over 32768 rows
+// take PLACEHOLDER)
+constexpr int PW_THREADS = 640;
+constexpr int PW_Q = 2, PW_E = 4;              // tiles of queries in flight, of their lse
+template <int D> constexpr int pw_smem() { return 1024 + (4 + PW_Q) * tile_bytes<D>() + 256 + (PW_E + 2) * BLOCK * 4 + 64; }
 
 static_assert(pw_smem<128>() <= 232448 && pa_smem<128>() <= 232448, "shared memory of a block");
 
@@ -1021,7 +1024,7 @@ struct UnitWalk {
 };
 
 template <int D>
-__global__ void __launch_bounds__(PA_THREADS, 1)
+__global__ void __launch_bounds__(PW_THREADS, 1)
 paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ WeightArgs a) {
   constexpr int TILE = tile_bytes<D>(), SLABS = D / 64;
   extern __shared__ uint8_t smem_raw[];
@@ -1030,12 +1033,14 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
   const uint32_t sK = base, sQ = sK + 4 * TILE, bars = sQ + PW_Q * TILE;
   const uint32_t k_full = bars, k_free = bars + 16;            // [2] pairs of blocks
   const uint32_t q_full = bars + 32, q_free = q_full + 8 * PW_Q;
-  const uint32_t e_full = q_free + 8 * PW_Q, e_free = e_full + 8 * PW_Q;      // lse of a tile
-  const uint32_t s_full = e_free + 8 * PW_Q, s_free = s_full + 32;            // [2 blocks][2 accumulators]
-  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + (bars - base) + 208);
+  const uint32_t e_full = q_free + 8 * PW_Q, e_free = e_full + 8 * PW_E;      // lse of a tile
+  const uint32_t s_full = e_free + 8 * PW_E, s_free = s_full + 32;            // [2 blocks][2 accumulators]
+  const uint32_t x_full = s_free + 32, x_free = x_full + 16;                  // [2 blocks] the second warps' sums are there; have been taken
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + (bars - base) + 240);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   float* s_lse = reinterpret_cast<float*>(gen + (bars - base) + 256);
-  UnitWalk* start = reinterpret_cast<UnitWalk*>(gen + (bars - base) + 256 + PW_Q * BLOCK * 4);
+  float* s_sum = s_lse + PW_E * BLOCK;         // [2 blocks][128]
+  UnitWalk* start = reinterpret_cast<UnitWalk*>(gen + (bars - base) + 256 + (PW_E + 2) * BLOCK * 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -1043,9 +1048,10 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
     for (int s = 0; s < 2; ++s) { mbar_init(k_full + 8 * s, 1); mbar_init(k_free + 8 * s, 1); }
     for (int s = 0; s < PW_Q; ++s) {
       mbar_init(q_full + 8 * s, 1); mbar_init(q_free + 8 * s, 1);
-      mbar_init(e_full + 8 * s, 64); mbar_init(e_free + 8 * s, 256);
     }
+    for (int s = 0; s < PW_E; ++s) { mbar_init(e_full + 8 * s, 64); mbar_init(e_free + 8 * s, 256); }
     for (int s = 0; s < 4; ++s) { mbar_init(s_full + 8 * s, 1); mbar_init(s_free + 8 * s, 128); }
+    for (int s = 0; s < 2; ++s) { mbar_init(x_full + 8 * s, 128); mbar_init(x_free + 8 * s, 128); }
     fence_mbar_init();
     prefetch_tensormap(&tmQ); prefetch_tensormap(&tmK);
   }
@@ -1057,7 +1063,7 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
   {
     long long* scratch = reinterpret_cast<long long*>(gen);
     long long* pre = scratch + 32;
-    const long long total = block_prefix<PA_THREADS>(a.c.n_seq, pre, scratch, [&](int b) {
+    const long long total = block_prefix<PW_THREADS>(a.c.n_seq, pre, scratch, [&](int b) {
       int row, n;
       call_rows(a.row_start, a.n_rows, b, row, n);
       if (blockIdx.x == 0) check_starts(a.row_start, a.n_rows, b, a.status);
@@ -1136,7 +1142,7 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
     }
   } else if (warp == 1) {
     if (lane == 0) {
-      uint32_t n_k = 0, n_q = 0, n_s[2] = {0, 0};
+      uint32_t n_k = 0, n_q = 0, used = 0;               // (used: a phase for each accumulator)
       while (ok && walk.next(a, s)) {
         if (s.tiles == 0) continue;
         for (int i = s.i0; i < s.i1 && ok; ++i) {
@@ -1148,9 +1154,9 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
           const int cols = (tokens * a.G + 15) & ~15;
           const uint32_t idesc = idesc_bf16(BLOCK, 0) | ((uint32_t)(cols >> 3) << 17);
           for (int t = 0; t < (s.two ? 2 : 1) && ok; ++t) {
-            const uint32_t buf = n_s[t] & 1;
-            ok = wait(s_free + 8 * (2 * t + buf), ((n_s[t] >> 1) & 1) ^ 1, abort_flag);
-            ++n_s[t];
+            const uint32_t buf = (n_q - 1) & 1;          // items alternate between the accumulators
+            ok = wait(s_free + 8 * (2 * t + buf), ((used >> (2 * t + buf)) & 1) ^ 1, abort_flag);
+            used ^= 1u << (2 * t + buf);
             if (!ok) break;
             tc_fence_after();
             const uint32_t k = desc_low(sK + (2 * kst + t) * TILE, 0), qd = desc_low(sQ + qst * TILE, 0);
@@ -1172,7 +1178,7 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
       if (s.tiles == 0) continue;
       for (int i = s.i0; i < s.i1 && ok; ++i) {
         const int h = i / s.tiles, q = s.tile0 + i % s.tiles, tokens = min(a.tile_tokens, s.n - q * a.tile_tokens);
-        const uint32_t st = n_q % PW_Q;
+        const uint32_t st = n_q % PW_E;
         const int64_t row = (int64_t)s.row + q * a.tile_tokens;
         float e[2];
 #pragma unroll
@@ -1181,7 +1187,7 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
           e[u] = c < tokens * a.G ? -__ldg(a.lse + (row + c / a.G) * a.H + h * a.G + c % a.G) * LOG2E : 0.f;
           if (e[u] == INFINITY) e[u] = 0.f;    // a query that sees nothing: all its scores become -inf, and stay
         }
-        ok = wait_warp(e_free + 8 * st, ((n_q / PW_Q) & 1) ^ 1, abort_flag);
+        ok = wait_warp(e_free + 8 * st, ((n_q / PW_E) & 1) ^ 1, abort_flag);
         ++n_q;
         if (!ok) break;
 #pragma unroll
@@ -1190,11 +1196,11 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
       }
     }
   } else {
-    const int t = (warp - 4) >> 2, quarter = warp & 3;
-    const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
+    const int t = ((warp - 4) >> 2) & 1, group = warp >= 12 ? 1 : 0, quarter = warp & 3;
+    const uint32_t src = tmem_base + (2 * t + group) * BLOCK + ((uint32_t)(quarter * 32) << 16);
     const float sc = LOG2E / (D == 128 ? 11.313708498984761f : 8.0f);
     const float2 sc2 = make_float2(sc, sc);
-    uint32_t n_q = 0, n_s = 0;
+    uint32_t n_q = 0, n_s = 0, n_x = 0;
     long long at = walk.at;                    // the line's item at which the segment begins
     const long long total = walk.total;
     while (ok && walk.next(a, s)) {
@@ -1203,22 +1209,20 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
       float2 sum[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) sum[u] = make_float2(0.f, 0.f);
-      for (int i = s.i0; i < s.i1 && s.tiles > 0 && ok; ++i) {
+      for (int i = s.i0; i < s.i1 && s.tiles > 0 && ok; ++i, ++n_q) {
+        if ((int)(n_q & 1) != group) continue;
         const int q = s.tile0 + i % s.tiles, tokens = min(a.tile_tokens, s.n - q * a.tile_tokens), cols = tokens * a.G;
-        const uint32_t st = n_q % PW_Q;
-        ok = wait_warp(e_full + 8 * st, (n_q / PW_Q) & 1, abort_flag);
-        ++n_q;
+        const uint32_t st = n_q % PW_E;
+        ok = wait_warp(e_full + 8 * st, (n_q / PW_E) & 1, abort_flag);
         if (!ok) break;
         if (work) {
-          const uint32_t buf = n_s & 1;
-          ok = wait_warp(s_full + 8 * (2 * t + buf), (n_s >> 1) & 1, abort_flag);
+          ok = wait_warp(s_full + 8 * (2 * t + group), n_s & 1, abort_flag);
           ++n_s;
           if (!ok) break;
           tc_fence_after();
           // column c is query q tile_tokens + c / G, which sees key if key <= off + query
           const int from_col = min(max(0, key - s.off - q * a.tile_tokens), BLOCK) * a.G;
           const bool all = !__any_sync(0xffffffffu, from_col > 0);
-          const uint32_t src = tmem_base + (2 * t + buf) * BLOCK + lane_off;
           const float4* lse4 = reinterpret_cast<const float4*>(s_lse + st * BLOCK);
 #pragma unroll 1
           for (int c0 = 0; c0 < cols; c0 += 32) {
@@ -1232,7 +1236,7 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             }
 #pragma unroll
             for (int c = 0; c < 32; c += 4) {
-              float4 e = lse4[(c0 + c) >> 2];
+              const float4 e = lse4[(c0 + c) >> 2];
               const float2 x = __ffma2_rn(make_float2(__uint_as_float(r[c]), __uint_as_float(r[c + 1])), sc2, make_float2(e.x, e.y));
               const float2 y = __ffma2_rn(make_float2(__uint_as_float(r[c + 2]), __uint_as_float(r[c + 3])), sc2, make_float2(e.z, e.w));
               sum[(c >> 1) & 3] = __fadd2_rn(sum[(c >> 1) & 3], make_float2(ex2(x.x), ex2(x.y)));
@@ -1240,20 +1244,36 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             }
           }
           tc_fence_before();
-          mbar_arrive(s_free + 8 * (2 * t + buf));
+          mbar_arrive(s_free + 8 * (2 * t + group));
         }
         mbar_arrive(e_free + 8 * st);
       }
       if (!ok) break;
       const float2 s01 = __fadd2_rn(sum[0], sum[1]), s23 = __fadd2_rn(sum[2], sum[3]);
       float w = (s01.x + s01.y) + (s23.x + s23.y);
+      const long long begin = at - s.i0, end = begin + s.cost;
+      at += s.i1 - s.i0;
+      // the second group hands its sums to the first
+      float* mine = s_sum + t * BLOCK + quarter * 32 + lane;
+      if (group == 1) {
+        ok = wait_warp(x_free + 8 * t, (n_x & 1) ^ 1, abort_flag);
+        ++n_x;
+        if (!ok) break;
+        *mine = w;
+        mbar_arrive(x_full + 8 * t);
+        continue;
+      }
+      ok = wait_warp(x_full + 8 * t, n_x & 1, abort_flag);
+      ++n_x;
+      if (!ok) break;
+      w += *mine;
+      mbar_arrive(x_free + 8 * t);
       bool write = true;
       if (s.i0 > 0 || s.i1 < s.cost) {
         // CTAs whose pieces reach into the unit: the first one's share is its last, the others' their first
-        const long long begin = at - s.i0, end = begin + s.cost;
-        const int mine = blockIdx.x, ctas = gridDim.x;
+        const int cta = blockIdx.x, ctas = gridDim.x;
         const int first = cta_of(total, begin, ctas), last = cta_of(total, end - 1, ctas);
-        float* share = a.share + (size_t)(2 * mine + (s.i0 == 0 ? 1 : 0)) * 2 * BLOCK;
+        float* share = a.share + (size_t)(2 * cta + (s.i0 == 0 ? 1 : 0)) * 2 * BLOCK;
         __stcg(share + t * BLOCK + quarter * 32 + lane, w);
         __threadfence();
         __syncwarp();
@@ -1275,7 +1295,6 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         if (slot >= 0) a.c.weight[slot] = (a.decay == 0.f ? 0.f : a.decay * a.c.weight[slot]) + w / (float)a.H;
         else set_status(a.status, SPTS_ERR_INDEX);
       }
-      at += s.i1 - s.i0;
     }
   }
 
@@ -1320,10 +1339,10 @@ bool map_queries(spts_ctx* ctx, CUtensorMap* tm, const void* p, int64_t ld, int 
 
 // As a dependent of what runs before: a CTA sets up its barriers and tensor memory before it waits for that.
 template <typename... KArgs, typename... Args>
-cudaError_t launch_big(spts_ctx* ctx, void (*kernel)(KArgs...), int ctas, int smem, const Args&... args) {
+cudaError_t launch_big(spts_ctx* ctx, void (*kernel)(KArgs...), int ctas, int threads, int smem, const Args&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ctas);
-  cfg.blockDim = dim3(PA_THREADS);
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = ctx->stream;
   cudaLaunchAttribute attr[1];
@@ -1355,7 +1374,7 @@ spts_status attention_t(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q
   if (!map_queries(ctx, &tmQ, Q, ldq, n_rows, a.G, a.tile_tokens) || !map_pages(ctx, &tmK, cache->k, cache) || !map_pages(ctx, &tmV, cache->v, cache))
     return SPTS_ERR_CUDA;
   const int ctas = ctx->sm_count < PAGED_MAX_CTAS ? ctx->sm_count : PAGED_MAX_CTAS;
-  if (launch_big(ctx, paged_attn_kernel<D>, ctas, pa_smem<D>(), tmQ, tmK, tmV, a) != cudaSuccess) return SPTS_ERR_CUDA;
+  if (launch_big(ctx, paged_attn_kernel<D>, ctas, PA_THREADS, pa_smem<D>(), tmQ, tmK, tmV, a) != cudaSuccess) return SPTS_ERR_CUDA;
   ctx->launches++;
   if (a.solo) return SPTS_OK;
   if (launch_dependent(paged_attn_join_kernel<D>, dim3(ctas, JOIN_SPLIT), dim3(JOIN_THREADS), ctx->stream, a) != cudaSuccess) return SPTS_ERR_CUDA;
@@ -1379,7 +1398,7 @@ spts_status weights_t(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, 
   if (!map_queries(ctx, &tmQ, n_rows > 0 ? Q : cache->k, ldq, n_rows > 0 ? n_rows : 1, a.G, a.tile_tokens) || !map_pages(ctx, &tmK, cache->k, cache))
     return SPTS_ERR_CUDA;
   const int ctas = ctx->sm_count < PAGED_MAX_CTAS ? ctx->sm_count : PAGED_MAX_CTAS;
-  if (launch_big(ctx, paged_weights_kernel<D>, ctas, pw_smem<D>(), tmQ, tmK, a) != cudaSuccess) return SPTS_ERR_CUDA;
+  if (launch_big(ctx, paged_weights_kernel<D>, ctas, PW_THREADS, pw_smem<D>(), tmQ, tmK, a) != cudaSuccess) return SPTS_ERR_CUDA;
   ctx->launches++;
   return SPTS_OK;
 }
