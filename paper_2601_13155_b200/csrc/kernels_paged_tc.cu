@@ -1141,35 +1141,45 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      uint32_t n_k = 0, n_q = 0, used = 0;               // (used: a phase for each accumulator)
-      while (ok && walk.next(a, s)) {
-        if (s.tiles == 0) continue;
-        for (int i = s.i0; i < s.i1 && ok; ++i) {
-          const int q = s.tile0 + i % s.tiles, tokens = min(a.tile_tokens, s.n - q * a.tile_tokens);
-          if (i == s.i0 || q == s.tile0) { ok = wait(k_full + 8 * (n_k & 1), (n_k >> 1) & 1, abort_flag); ++n_k; }
-          const uint32_t kst = (n_k - 1) & 1, qst = n_q % PW_Q;
-          ok = ok && wait(q_full + 8 * qst, (n_q / PW_Q) & 1, abort_flag);
-          ++n_q;
-          const int cols = (tokens * a.G + 15) & ~15;
-          const uint32_t idesc = idesc_bf16(BLOCK, 0) | ((uint32_t)(cols >> 3) << 17);
-          for (int t = 0; t < (s.two ? 2 : 1) && ok; ++t) {
-            const uint32_t buf = (n_q - 1) & 1;          // items alternate between the accumulators
-            ok = wait(s_free + 8 * (2 * t + buf), ((used >> (2 * t + buf)) & 1) ^ 1, abort_flag);
-            used ^= 1u << (2 * t + buf);
-            if (!ok) break;
-            tc_fence_after();
-            const uint32_t k = desc_low(sK + (2 * kst + t) * TILE, 0), qd = desc_low(sQ + qst * TILE, 0);
+    // (as in the attention: the whole warp, on uniform values, one lane issues)
+    const bool leader = elect_lane();
+    constexpr uint32_t k_hi = desc_high(group_bytes<D>()), q_hi = desc_high(1024);
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem_base, 0);
+    const uint32_t k_lo = desc_low(__shfl_sync(0xffffffffu, sK, 0), 0), q_lo = desc_low(__shfl_sync(0xffffffffu, sQ, 0), 0);
+    uint32_t n_k = 0, n_q = 0, used = 0;       // (used: a phase for each accumulator)
+    while (ok && __any_sync(0xffffffffu, walk.next(a, s))) {
+      const int tiles = __shfl_sync(0xffffffffu, s.tiles, 0), i0 = __shfl_sync(0xffffffffu, s.i0, 0), i1 = __shfl_sync(0xffffffffu, s.i1, 0);
+      const int left = __shfl_sync(0xffffffffu, s.n - s.tile0 * a.tile_tokens, 0);      // queries from the first tile on
+      const bool two = __any_sync(0xffffffffu, s.two);
+      if (tiles == 0) continue;
+      int q = i0 % tiles;                      // tile of queries, counted from the first
+      for (int i = i0; i < i1 && ok; ++i) {
+        if (i == i0 || q == 0) { ok = wait_warp(k_full + 8 * (n_k & 1), (n_k >> 1) & 1, abort_flag); ++n_k; }
+        const uint32_t kst = (n_k - 1) & 1, qst = n_q % PW_Q, buf = n_q & 1;      // items alternate between the accumulators
+        ok = ok && wait_warp(q_full + 8 * qst, (n_q / PW_Q) & 1, abort_flag);
+        ++n_q;
+        const int cols = (min(a.tile_tokens, left - q * a.tile_tokens) * a.G + 15) & ~15;
+        const uint32_t idesc = idesc_bf16(BLOCK, 0) | ((uint32_t)(cols >> 3) << 17), qd = q_lo + qst * (TILE >> 4);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if (!ok || (t == 1 && !two)) break;
+          ok = wait_warp(s_free + 8 * (2 * t + buf), ((used >> (2 * t + buf)) & 1) ^ 1, abort_flag);
+          used ^= 1u << (2 * t + buf);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t k = k_lo + (2 * kst + t) * (TILE >> 4);
+          if (leader) {
 #pragma unroll
             for (int e = 0; e < D / 16; ++e)
-              mma_ss(tmem_base + (2 * t + buf) * BLOCK, k + (((e >> 2) * 1024 + (e & 3) * 32) >> 4), desc_high(group_bytes<D>()),
-                     qd + (((e >> 2) * SLAB + (e & 3) * 32) >> 4), desc_high(1024), idesc, e > 0);
+              mma_ss(tm + (2 * t + buf) * BLOCK, k + (((e >> 2) * 1024 + (e & 3) * 32) >> 4), k_hi, qd + (((e >> 2) * SLAB + (e & 3) * 32) >> 4), q_hi, idesc,
+                     e > 0);
             mma_commit(s_full + 8 * (2 * t + buf));
           }
-          if (!ok) break;
-          mma_commit(q_free + 8 * qst);
-          if (i + 1 == s.i1 || q == s.tile0 + s.tiles - 1) mma_commit(k_free + 8 * kst);
         }
+        if (!ok) break;
+        if (leader) mma_commit(q_free + 8 * qst);
+        if (++q == tiles) q = 0;
+        if (leader && (i + 1 == i1 || q == 0)) mma_commit(k_free + 8 * kst);
       }
     }
   } else if (warp < 4) {
