@@ -829,22 +829,18 @@ class Spts:
             raise ValueError(f"up to {LOGPROBS_MAX_TOP} alternatives, got {n_top}")
         lp, ld = _rows(logits, v, torch.float32, "logits", self.dev)
         tp = _vec(targets, n, torch.int32, "targets", self.dev)
-        new, i32, out, ptr = logits.new_empty, torch.int32, {}, {}
-
-        def make(name, size, **kw):
-            t = out[name] = new(size, **kw)
-            ptr[name] = t.data_ptr()
+        new, i32, out = logits.new_empty, torch.int32, {}
+        logprob = rank = ent = top = token = None
         if targets is not None:
-            make("logprob", n)
-            make("rank", n, dtype=i32)
+            out["logprob"], out["rank"] = logprob, rank = new(n), new(n, dtype=i32)
+            logprob, rank = logprob.data_ptr(), rank.data_ptr()
         if entropy:
-            make("entropy", n)
+            out["entropy"] = ent = new(n)
+            ent = ent.data_ptr()
         if n_top:
-            make("top_logprob", (n, n_top))
-            make("top_token", (n, n_top), dtype=i32)
-        get = ptr.get
-        code = self.lib.spts_token_logprobs(self.h, lp, ld, n, v, tp, n_top, get("logprob"), get("rank"), get("entropy"), get("top_logprob"),
-                                            get("top_token"))
+            out["top_logprob"], out["top_token"] = top, token = new((n, n_top)), new((n, n_top), dtype=i32)
+            top, token = top.data_ptr(), token.data_ptr()
+        code = self.lib.spts_token_logprobs(self.h, lp, ld, n, v, tp, n_top, logprob, rank, ent, top, token)
         if code:
             raise SptsError(code, "spts_token_logprobs")
         return out
