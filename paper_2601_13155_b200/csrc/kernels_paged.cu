@@ -1,5 +1,5 @@
 // The paged KV cache on CUDA cores: rows are appended to it (paged_append_kernel), attention and the weights that its rows gather in
-// either storage type (paged_attn_plain_kernel, paged_weights_plain_kernel: fp32 storage, SPTS_REFERENCE_KERNELS, more than 128 query
+// either storage type (paged_attn_*_kernel, paged_weights_*_kernel: fp32 storage, SPTS_REFERENCE_KERNELS, more than 128 query
 // heads to a KV head), and sequences are cut down to a budget (evict_rank_kernel, evict_move_kernel).
 #include <climits>
 
@@ -86,11 +86,20 @@ paged_append_kernel(Cache c, const char* __restrict__ K, int64_t ldk, const char
   }
 }
 
-// ------------------------------------------------------------------------------------------------ attention, plain
-constexpr int PL_THREADS = 256;
-constexpr int PL_ROWS = 32;                    // queries of a tile: token x head of a KV head's group, heads inside
-constexpr int PL_KEYS = 64;                    // rows of the cache in shared memory at a time
-constexpr int PL_SPLIT = 8;                    // CTAs that share a tile's rows of the cache at most (a portable cluster)
+// ------------------------------------------------------------------------------------------------ attention and weights, plain
+// CUDA cores, fp32 arithmetic in either storage type.  Rows of queries are token x head of a KV head's group, heads inside.  Chunks of more
+// than eight such rows to a sequence on average go 64 rows at a time against 64 rows of the cache in shared memory (tile kernels: bound by
+// the multiply-adds and the shared memory that feeds them), shorter ones four at a time, straight from global memory (row kernels: bound by
+// memory where there is enough to do).  Where that makes too few blocks, a cluster of up to eight shares a block's rows of the cache, or
+// its KV heads, and joins what it found in the order of its blocks.
+constexpr int PL_THREADS = 256, PL_WARPS = PL_THREADS / 32;
+constexpr int PL_SPLIT = 8;                    // CTAs that share a block's work at most (a portable cluster)
+constexpr int TILE = 64;                       // tile kernels: rows of queries, rows of the cache
+constexpr int FEW = 4, STEP = 8;               // row kernels: rows of queries, rows of the cache that a warp takes at a time
+constexpr int FEW_MOST = 8;                    // rows of queries to a sequence up to which the row kernels are taken
+constexpr int WARP_KEYS = 32;                  // row kernel of the weights: rows of the cache that belong to a warp
+constexpr float SLACK = 8.0f;                  // log2 units the running maximum may lag behind
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 template <typename T> __device__ __forceinline__ float4 load4(const T* p);
 template <> __device__ __forceinline__ float4 load4<float>(const float* p) { return *reinterpret_cast<const float4*>(p); }
@@ -104,262 +113,571 @@ template <> __device__ __forceinline__ void store4<bf16>(bf16* p, float4 v) {
   __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
   *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
 }
+// the D / 32 dims of a row that belong to a lane
+template <typename T, int PER> __device__ __forceinline__ void load_lane(const T* p, float (&x)[PER]) {
+  if (PER == 4) {
+    const float4 v = load4(p);
+    x[0] = v.x; x[1] = v.y; x[PER - 2] = v.z; x[PER - 1] = v.w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < PER; ++e) x[e] = to_f32(p[e]);
+  }
+}
 
-// Rows [j0, j0 + PL_KEYS) of K or V of one KV head into shared memory, zeros from row `end` on and where the table names no page.
-template <typename T, int D, int LD>
-__device__ __forceinline__ void load_rows(const Cache& c, const T* __restrict__ x, int b, int kvh, int Hkv, int j0, int end, float* to, int* status) {
+struct PlainArgs {
+  Cache c;
+  const int32_t* row_start; int n_rows, H, Hkv;
+  const void* Q; int64_t ldq;
+  void* O; int64_t ldo;
+  float* lse;                                  // of the attention: written; of the weights: read
+  float decay;
+  int* status;
+};
+
+// The tile of queries that a block works on; all threads of a block, whose clusters have one tile.
+struct QueryTile {
+  int b, first, n, held, off;                  // sequence, its first query, how many, its rows, rows before the first query
+  int64_t r0, rows;                            // first row of queries of the tile; of the sequence
+  int seen;                                    // rows of the cache that the tile's last query sees
+};
+template <int ROWS>
+__device__ __forceinline__ bool find_tile(const PlainArgs& a, int64_t tile, bool check, long long* pre, long long* sums, QueryTile& t) {
+  const int G = a.H / a.Hkv;
+  block_prefix<PL_THREADS>(a.c.n_seq, pre, sums, [&](int b) {
+    int f, n;
+    call_rows(a.row_start, a.n_rows, b, f, n);
+    if (check) check_starts(a.row_start, a.n_rows, b, a.status);
+    return ((long long)n * G + ROWS - 1) / ROWS;
+  });
+  __syncthreads();
+  if (tile >= pre[a.c.n_seq]) return false;
+  t.b = find_share(pre, a.c.n_seq, tile);
+  call_rows(a.row_start, a.n_rows, t.b, t.first, t.n);
+  t.held = held_rows(a.c, t.b);
+  t.off = t.held - t.n;
+  t.r0 = (tile - pre[t.b]) * ROWS;
+  t.rows = (int64_t)t.n * G;
+  t.seen = max(0, t.off + (int)min((int64_t)t.n, (t.r0 + ROWS - 1) / G + 1));
+  return true;
+}
+
+// Shares of the CTAs of a cluster, of `rows` rows: maxima (log2 units) and sums in m and l, O [rows][D] in o, all in shared memory.  Row r is
+// joined and written by CTA r % split.
+template <typename T, int D>
+__device__ __forceinline__ void join_cluster(cg::cluster_group& cluster, const PlainArgs& a, const QueryTile& t, int rows, int kvh, float* m, float* l, float* o) {
+  const int split = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), G = a.H / a.Hkv, tid = threadIdx.x;
+  cluster.sync();
+  for (int r = rank + split * (tid / (D / 4)); r < rows; r += split * (PL_THREADS / (D / 4))) {
+    const int e = (tid % (D / 4)) * 4;
+    if (t.r0 + r >= t.rows) continue;
+    float top = -INFINITY;
+    for (int s = 0; s < split; ++s) top = fmaxf(top, *cluster.map_shared_rank(&m[r], s));
+    float sum = 0.f;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = 0; s < split; ++s) {
+      const float ms = *cluster.map_shared_rank(&m[r], s), ls = *cluster.map_shared_rank(&l[r], s);
+      if (ms == -INFINITY && ls == 0.f) continue;        // saw none of its rows
+      const float f = ms == -INFINITY ? 1.f : exp2f(ms - top);
+      const float4 y = *reinterpret_cast<const float4*>(cluster.map_shared_rank(o, s) + r * D + e);
+      sum += ls * f;
+      x.x += y.x * f; x.y += y.y * f; x.z += y.z * f; x.w += y.w * f;
+    }
+    const bool none = sum == 0.f;
+    const float inv = none ? 0.f : 1.0f / sum;
+    const int64_t token = t.first + (t.r0 + r) / G;
+    const int head = kvh * G + (int)((t.r0 + r) % G);
+    store4((T*)a.O + token * a.ldo + (int64_t)head * D + e, none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv));
+    if (e == 0 && a.lse != nullptr) a.lse[token * a.H + head] = none ? -INFINITY : (top + log2f(sum)) * LN2;
+  }
+  cluster.sync();
+}
+
+// ---- tile kernels
+constexpr int PAD = 4;                         // floats between rows in shared memory: neighbouring rows in neighbouring banks
+template <int D> constexpr int tile_floats() { return TILE * (D + PAD); }
+
+// Rows [j0, j0 + TILE) of K or V of one KV head into shared memory, zeros from row `end` on and where the table names no page.
+template <typename T, int D>
+__device__ __forceinline__ void load_rows(const PlainArgs& a, const T* __restrict__ x, int b, int kvh, int j0, int end, float* to) {
   constexpr int PER = D / 4;
-  for (int i = threadIdx.x; i < PL_KEYS * PER; i += PL_THREADS) {
+#pragma unroll 4
+  for (int i = threadIdx.x; i < TILE * PER; i += PL_THREADS) {
     const int r = i / PER, e = (i % PER) * 4, j = j0 + r;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (j < end) {
-      const int64_t slot = slot_of(c, b, j);
-      if (slot >= 0) v = load4(x + (slot * Hkv + kvh) * D + e);
-      else set_status(status, SPTS_ERR_INDEX);
+      const int64_t slot = slot_of(a.c, b, j);
+      if (slot >= 0) v = load4(x + (slot * a.Hkv + kvh) * D + e);
+      else set_status(a.status, SPTS_ERR_INDEX);
     }
-    *reinterpret_cast<float4*>(to + r * LD + e) = v;
+    *reinterpret_cast<float4*>(to + r * (D + PAD) + e) = v;
   }
 }
-
-// Queries [r0, r0 + PL_ROWS) of a sequence's rows x heads, zeros behind the last.
+// Rows of queries [r0, r0 + TILE), zeros behind the last, times `scale`.
 template <typename T, int D>
-__device__ __forceinline__ void load_queries(const T* __restrict__ Q, int64_t ldq, int64_t first, int r0, int64_t rows, int kvh, int G, float* to) {
+__device__ __forceinline__ void load_queries(const PlainArgs& a, int64_t first, int64_t r0, int64_t rows, int kvh, float scale, float* to) {
   constexpr int PER = D / 4;
-  for (int i = threadIdx.x; i < PL_ROWS * PER; i += PL_THREADS) {
+  const int G = a.H / a.Hkv;
+  for (int i = threadIdx.x; i < TILE * PER; i += PL_THREADS) {
     const int r = i / PER, e = (i % PER) * 4;
-    const int64_t q = (int64_t)r0 + r;
+    const int64_t q = r0 + r;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (q < rows) v = load4(Q + (first + q / G) * ldq + (int64_t)(kvh * G + q % G) * D + e);
-    *reinterpret_cast<float4*>(to + r * D + e) = v;
+    if (q < rows) v = load4((const T*)a.Q + (first + q / G) * a.ldq + (int64_t)(kvh * G + q % G) * D + e);
+    *reinterpret_cast<float4*>(to + r * (D + PAD) + e) = make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale);
   }
 }
-
-// Scores of queries tr and tr + 16 with keys tk, tk + 16, tk + 32, tk + 48 of the tiles in shared memory.
-template <int D, int LD>
-__device__ __forceinline__ void tile_scores(const float* sq, const float* sk, int tr, int tk, float (&s)[2][4]) {
+// Products of rows 4 tq .. + 3 of queries and rows tk + 16 k of the cache.
+template <int D>
+__device__ __forceinline__ void tile_scores(const float* sq, const float* sk, int tq, int tk, float (&s)[4][4]) {
 #pragma unroll
-  for (int a = 0; a < 2; ++a)
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) s[a][k] = 0.f;
+    for (int k = 0; k < 4; ++k) s[i][k] = 0.f;
 #pragma unroll 4
   for (int e = 0; e < D; e += 4) {
-    const float4 q0 = *reinterpret_cast<const float4*>(sq + tr * D + e), q1 = *reinterpret_cast<const float4*>(sq + (tr + 16) * D + e);
+    float4 q[4], x[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float4 x = *reinterpret_cast<const float4*>(sk + (tk + 16 * k) * LD + e);
-      s[0][k] += q0.x * x.x + q0.y * x.y + q0.z * x.z + q0.w * x.w;
-      s[1][k] += q1.x * x.x + q1.y * x.y + q1.z * x.z + q1.w * x.w;
-    }
+    for (int i = 0; i < 4; ++i) q[i] = *reinterpret_cast<const float4*>(sq + (4 * tq + i) * (D + PAD) + e);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = *reinterpret_cast<const float4*>(sk + (tk + 16 * k) * (D + PAD) + e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s[i][k] = fmaf(q[i].x, x[k].x, fmaf(q[i].y, x[k].y, fmaf(q[i].z, x[k].z, fmaf(q[i].w, x[k].w, s[i][k]))));
   }
 }
 
-template <int D> constexpr int plain_attn_smem() { return (PL_ROWS * D + PL_KEYS * (D + 4) + PL_KEYS * D + PL_ROWS * (PL_KEYS + 1)) * 4; }
+template <int D> constexpr int attn_tile_smem() { return 3 * tile_floats<D>() * 4; }
 
-// A cluster of CTAs per (tile of 32 queries, KV head): each takes a share of the rows that the tile sees, 64 at a time, online
-// softmax, and the shares are joined in their order through distributed shared memory.  Fewer tiles than SMs are shared by up to
-// eight CTAs (three ragged chunks of up to 37 tokens over up to 1000 rows, 4 heads of 64 dims in fp32).
+// A cluster to (tile of 64 rows of queries, KV head).  A thread has 4 x 4 scores, then 4 rows x D / 16 dims of O; sixteen neighbouring threads
+// share the rows, whose maxima and sums stay in registers.  The weights take K's place in shared memory.
 template <typename T, int D>
-__global__ void __launch_bounds__(PL_THREADS)
-paged_attn_plain_kernel(Cache c, const T* __restrict__ Q, int64_t ldq, const int32_t* __restrict__ row_start, int n_rows, int H, int Hkv,
-                        T* __restrict__ O, int64_t ldo, float* __restrict__ lse, int* status) {
-  constexpr int LD = D + 4, PIECES = D / 64;
+__global__ void __launch_bounds__(PL_THREADS, 2)
+paged_attn_tile_kernel(const __grid_constant__ PlainArgs a) {
+  constexpr int LD = D + PAD, PIECES = D / 64, LP = TILE + PAD;
   extern __shared__ __align__(16) float smem_f[];
   float* sq = smem_f;
-  float* sk = sq + PL_ROWS * D;
-  float* sv = sk + PL_KEYS * LD;
-  float* sp = sv + PL_KEYS * D;
-  __shared__ float sm[PL_ROWS], sl[PL_ROWS], salpha[PL_ROWS];
+  float* sk = sq + tile_floats<D>();
+  float* sv = sk + tile_floats<D>();
+  float* sp = sk;                              // [TILE][LP]
+  __shared__ float sm[TILE], sl[TILE];
   __shared__ long long pre[PREFIX_MAX + 1], sums[32];
   cg::cluster_group cluster = cg::this_cluster();
   const int split = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-  const int G = H / Hkv, kvh = blockIdx.y, tid = threadIdx.x;
-  const int64_t tile = blockIdx.x / split;
-  block_prefix<PL_THREADS>(c.n_seq, pre, sums, [&](int b) {
-    int f, n;
-    call_rows(row_start, n_rows, b, f, n);
-    if (kvh == 0 && tile == 0) check_starts(row_start, n_rows, b, status);
-    return ((long long)n * G + PL_ROWS - 1) / PL_ROWS;
-  });
-  __syncthreads();
-  if (tile >= pre[c.n_seq]) return;                   // (all CTAs of a cluster have the same tile)
-  const int b = find_share(pre, c.n_seq, tile);
-  int first, n;
-  call_rows(row_start, n_rows, b, first, n);
-  const int held = held_rows(c, b), off = held - n;
-  const int r0 = (int)(tile - pre[b]) * PL_ROWS;
-  const int64_t rows = (int64_t)n * G;
-  const int seen = max(0, off + (int)min((int64_t)n, ((int64_t)r0 + PL_ROWS - 1) / G + 1));   // rows that the tile's last query sees
-  load_queries<T, D>(Q, ldq, first, r0, rows, kvh, G, sq);
-  if (tid < PL_ROWS) { sm[tid] = -INFINITY; sl[tid] = 0.f; }
-  const float scale = rsqrtf((float)D);
-  const int tr = tid >> 4, tk = tid & 15;
-  // limit of a query: the rows that it sees
-  int limit[2];
+  const int G = a.H / a.Hkv, kvh = blockIdx.y, tid = threadIdx.x, tq = tid >> 4, tk = tid & 15;
+  QueryTile t;
+  if (!find_tile<TILE>(a, blockIdx.x / split, kvh == 0 && blockIdx.x == 0, pre, sums, t)) return;
+  load_queries<T, D>(a, t.first, t.r0, t.rows, kvh, LOG2E * rsqrtf((float)D), sq);
+  // rows of the cache that a query sees; those that all of the tile's see
+  int limit[4];
 #pragma unroll
-  for (int a = 0; a < 2; ++a) limit[a] = r0 + tr + 16 * a < rows ? off + (r0 + tr + 16 * a) / G + 1 : 0;
-  float4 acc[2][PIECES];
+  for (int i = 0; i < 4; ++i) {
+    const int64_t r = t.r0 + 4 * tq + i;
+    limit[i] = r < t.rows ? t.off + (int)(r / G) + 1 : 0;
+  }
+  const int all = t.r0 + TILE <= t.rows ? t.off + (int)(t.r0 / G) + 1 : 0;
+  float m[4], l[4];
+  float4 acc[4][PIECES];
 #pragma unroll
-  for (int a = 0; a < 2; ++a)
+  for (int i = 0; i < 4; ++i) {
+    m[i] = -INFINITY;
+    l[i] = 0.f;
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) acc[a][p] = make_float4(0.f, 0.f, 0.f, 0.f);
-  const int chunks = (seen + PL_KEYS - 1) / PL_KEYS;
+    for (int p = 0; p < PIECES; ++p) acc[i][p] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  const int chunks = (t.seen + TILE - 1) / TILE;
   for (int ch = (int)((int64_t)chunks * rank / split); ch < (int)((int64_t)chunks * (rank + 1) / split); ++ch) {
-    const int j0 = ch * PL_KEYS;
+    const int j0 = ch * TILE;
+    const bool whole = j0 + TILE <= all;
     __syncthreads();
-    load_rows<T, D, LD>(c, (const T*)c.k, b, kvh, Hkv, j0, seen, sk, status);
-    load_rows<T, D, D>(c, (const T*)c.v, b, kvh, Hkv, j0, seen, sv, status);
+    load_rows<T, D>(a, (const T*)a.c.k, t.b, kvh, j0, t.seen, sk);
+    load_rows<T, D>(a, (const T*)a.c.v, t.b, kvh, j0, t.seen, sv);
     __syncthreads();
-    float s[2][4];
-    tile_scores<D, LD>(sq, sk, tr, tk, s);
+    float s[4][4];
+    tile_scores<D>(sq, sk, tq, tk, s);
+    __syncthreads();                           // K is done with
 #pragma unroll
-    for (int a = 0; a < 2; ++a)
+    for (int i = 0; i < 4; ++i) {
+      if (!whole) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) sp[(tr + 16 * a) * (PL_KEYS + 1) + tk + 16 * k] = j0 + tk + 16 * k < limit[a] ? s[a][k] * scale : -INFINITY;
-    __syncthreads();
-    // eight lanes to a query
-    {
-      const int r = tid >> 3, l8 = tid & 7;
-      float* row = sp + r * (PL_KEYS + 1);
-      float m = -INFINITY;
-#pragma unroll
-      for (int k = 0; k < PL_KEYS / 8; ++k) m = fmaxf(m, row[l8 + 8 * k]);
-#pragma unroll
-      for (int o = 4; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-      const float was = sm[r], now = fmaxf(was, m), base = now == -INFINITY ? 0.f : now;
-      float sum = 0.f;
-#pragma unroll
-      for (int k = 0; k < PL_KEYS / 8; ++k) {
-        const float p = expf(row[l8 + 8 * k] - base);
-        row[l8 + 8 * k] = p;
-        sum += p;
+        for (int k = 0; k < 4; ++k) s[i][k] = j0 + tk + 16 * k < limit[i] ? s[i][k] : -INFINITY;
       }
+      float top = fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3]));
 #pragma unroll
-      for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      __syncwarp();
-      if (l8 == 0) {
-        const float alpha = was == -INFINITY ? 0.f : expf(was - base);
-        salpha[r] = alpha;
-        sm[r] = now;
-        sl[r] = sl[r] * alpha + sum;
+      for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      if (top > m[i] + SLACK || m[i] == -INFINITY) {
+        const float alpha = m[i] == -INFINITY ? 0.f : exp2f(m[i] - top);
+        m[i] = top;
+        l[i] *= alpha;
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) { acc[i][p].x *= alpha; acc[i][p].y *= alpha; acc[i][p].z *= alpha; acc[i][p].w *= alpha; }
+      }
+      const float base = m[i] == -INFINITY ? 0.f : m[i];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float p = exp2f(s[i][k] - base);
+        l[i] += p;
+        sp[(4 * tq + i) * LP + tk + 16 * k] = p;
       }
     }
     __syncthreads();
-    // O = alpha O + P V; a row that a query does not see has p = 0 and is passed over, whatever V holds
+    // O += P V; where a query does not see all of the rows, those of weight zero are passed over, whatever V holds
+    if (whole) {
+#pragma unroll 2
+      for (int k = 0; k < TILE; k += 4) {
+        float4 w[4];
 #pragma unroll
-    for (int a = 0; a < 2; ++a) {
-      const float alpha = salpha[tr + 16 * a];
+        for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float4*>(sp + (4 * tq + i) * LP + k);
 #pragma unroll
-      for (int p = 0; p < PIECES; ++p) { acc[a][p].x *= alpha; acc[a][p].y *= alpha; acc[a][p].z *= alpha; acc[a][p].w *= alpha; }
-    }
-    for (int k = 0; k < PL_KEYS; ++k) {
-      const float w[2] = {sp[tr * (PL_KEYS + 1) + k], sp[(tr + 16) * (PL_KEYS + 1) + k]};
+        for (int p = 0; p < PIECES; ++p) {
+          float4 v[4];
 #pragma unroll
-      for (int p = 0; p < PIECES; ++p) {
-        const float4 v = *reinterpret_cast<const float4*>(sv + k * D + 64 * p + 4 * tk);
+          for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const float4*>(sv + (k + u) * LD + 64 * p + 4 * tk);
 #pragma unroll
-        for (int a = 0; a < 2; ++a) {
-          if (w[a] != 0.f) {
-            acc[a][p].x = fmaf(w[a], v.x, acc[a][p].x); acc[a][p].y = fmaf(w[a], v.y, acc[a][p].y);
-            acc[a][p].z = fmaf(w[a], v.z, acc[a][p].z); acc[a][p].w = fmaf(w[a], v.w, acc[a][p].w);
+          for (int i = 0; i < 4; ++i) {
+            const float ws[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              acc[i][p].x = fmaf(ws[u], v[u].x, acc[i][p].x); acc[i][p].y = fmaf(ws[u], v[u].y, acc[i][p].y);
+              acc[i][p].z = fmaf(ws[u], v[u].z, acc[i][p].z); acc[i][p].w = fmaf(ws[u], v[u].w, acc[i][p].w);
+            }
+          }
+        }
+      }
+    } else {
+      for (int k = 0; k < TILE; ++k) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float w = sp[(4 * tq + i) * LP + k];
+          if (w == 0.f) continue;
+#pragma unroll
+          for (int p = 0; p < PIECES; ++p) {
+            const float4 v = *reinterpret_cast<const float4*>(sv + k * LD + 64 * p + 4 * tk);
+            acc[i][p].x = fmaf(w, v.x, acc[i][p].x); acc[i][p].y = fmaf(w, v.y, acc[i][p].y);
+            acc[i][p].z = fmaf(w, v.z, acc[i][p].z); acc[i][p].w = fmaf(w, v.w, acc[i][p].w);
           }
         }
       }
     }
   }
-  // every CTA leaves its share in its own shared memory; query r is joined by CTA r % split
   __syncthreads();
 #pragma unroll
-  for (int a = 0; a < 2; ++a)
+  for (int i = 0; i < 4; ++i) {
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) *reinterpret_cast<float4*>(sk + (tr + 16 * a) * D + 64 * p + 4 * tk) = acc[a][p];
+    for (int o = 8; o > 0; o >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o);
+    if (tk == 0) { sm[4 * tq + i] = m[i]; sl[4 * tq + i] = l[i]; }
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) *reinterpret_cast<float4*>(sv + (4 * tq + i) * D + 64 * p + 4 * tk) = acc[i][p];
+  }
+  join_cluster<T, D>(cluster, a, t, TILE, kvh, sm, sl, sv);
+}
+
+// Blocks of the cache for the weights: (sequence, ROWS rows of it); all threads.
+template <int ROWS>
+__device__ __forceinline__ long long blocks_of_rows(const PlainArgs& a, bool check, long long* pre, long long* sums) {
+  block_prefix<PL_THREADS>(a.c.n_seq, pre, sums, [&](int b) {
+    if (check) check_starts(a.row_start, a.n_rows, b, a.status);
+    return (long long)(held_rows(a.c, b) + ROWS - 1) / ROWS;
+  });
+  __syncthreads();
+  return pre[a.c.n_seq];
+}
+// The sums [rows] of the CTAs of a cluster, which had different KV heads, are added in their order and become weights.
+__device__ __forceinline__ void write_weights(cg::cluster_group& cluster, const PlainArgs& a, int b, int held, int j0, int rows, float* sum) {
+  const int split = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   cluster.sync();
-  for (int r = rank + split * (tid / (D / 4)); r < PL_ROWS; r += split * (PL_THREADS / (D / 4))) {
-    const int e = (tid % (D / 4)) * 4;
-    if (r0 + r >= rows) continue;
-    float m = -INFINITY;
-    for (int s = 0; s < split; ++s) m = fmaxf(m, *cluster.map_shared_rank(&sm[r], s));
-    float l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = 0; s < split; ++s) {
-      const float ms = *cluster.map_shared_rank(&sm[r], s), ls = *cluster.map_shared_rank(&sl[r], s);
-      if (ms == -INFINITY) continue;                    // saw none of its rows
-      const float f = expf(ms - m);
-      const float4 x = *reinterpret_cast<const float4*>(cluster.map_shared_rank(sk, s) + r * D + e);
-      l += ls * f;
-      o.x += x.x * f; o.y += x.y * f; o.z += x.z * f; o.w += x.w * f;
-    }
-    if (m == -INFINITY) { l = 1.f; o = make_float4(0.f, 0.f, 0.f, 0.f); }
-    const int64_t token = first + (int64_t)(r0 + r) / G;
-    const int head = kvh * G + (int)((r0 + r) % G);
-    store4(O + token * ldo + (int64_t)head * D + e, make_float4(o.x / l, o.y / l, o.z / l, o.w / l));
-    if (e == 0 && lse != nullptr) lse[token * H + head] = m + logf(l);
+  for (int i = rank * PL_THREADS + threadIdx.x; i < rows; i += split * PL_THREADS) {
+    if (j0 + i >= held) continue;
+    float w = 0.f;
+    for (int s = 0; s < split; ++s) w += *cluster.map_shared_rank(&sum[i], s);
+    const int64_t slot = slot_of(a.c, b, j0 + i);
+    if (slot >= 0) a.c.weight[slot] = (a.decay == 0.f ? 0.f : a.decay * a.c.weight[slot]) + w / (float)a.H;
+    else set_status(a.status, SPTS_ERR_INDEX);
   }
   cluster.sync();
 }
 
-template <int D> constexpr int plain_weights_smem() { return (PL_ROWS * D + PL_KEYS * (D + 4) + 16 * PL_KEYS) * 4; }
+template <int D> constexpr int weights_tile_smem() { return (2 * tile_floats<D>() + 16 * TILE) * 4; }
 
-// Persistent CTAs over (sequence, 64 rows of it); for every KV head its K in shared memory and the queries that see any of the rows
-// passing by.  A thread sums its queries' weights of four rows; the sixteen threads of a row meet at the end, in their order.
+// Persistent clusters over (sequence, 64 rows of it); a CTA has every split-th KV head: its K in shared memory and the queries that see any
+// of the rows passing by.  A thread sums its queries' weights of four rows; the sixteen threads of a row meet at the end, in their order.
 template <typename T, int D>
-__global__ void __launch_bounds__(PL_THREADS)
-paged_weights_plain_kernel(Cache c, const T* __restrict__ Q, int64_t ldq, const int32_t* __restrict__ row_start, int n_rows, int H, int Hkv,
-                           const float* __restrict__ lse, float decay, int* status) {
-  constexpr int LD = D + 4;
+__global__ void __launch_bounds__(PL_THREADS, 2)
+paged_weights_tile_kernel(const __grid_constant__ PlainArgs a) {
   extern __shared__ __align__(16) float smem_f[];
   float* sq = smem_f;
-  float* sk = sq + PL_ROWS * D;
-  float* part = sk + PL_KEYS * LD;
+  float* sk = sq + tile_floats<D>();
+  float* part = sk + tile_floats<D>();         // [16][TILE]
+  __shared__ float sum_all[TILE], slse[TILE];
   __shared__ long long pre[PREFIX_MAX + 1], sums[32];
-  const int G = H / Hkv, tid = threadIdx.x, tr = tid >> 4, tk = tid & 15;
-  const float scale = rsqrtf((float)D);
-  block_prefix<PL_THREADS>(c.n_seq, pre, sums, [&](int b) {
-    if (blockIdx.x == 0) check_starts(row_start, n_rows, b, status);
-    return (long long)(held_rows(c, b) + PL_KEYS - 1) / PL_KEYS;
-  });
-  __syncthreads();
-  const long long items = pre[c.n_seq];
-  for (long long item = blockIdx.x; item < items; item += gridDim.x) {
-    const int b = find_share(pre, c.n_seq, item);
+  cg::cluster_group cluster = cg::this_cluster();
+  const int split = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int G = a.H / a.Hkv, tid = threadIdx.x, tq = tid >> 4, tk = tid & 15;
+  const long long items = blocks_of_rows<TILE>(a, blockIdx.x == 0, pre, sums);
+  for (long long item = blockIdx.x / split; item < items; item += gridDim.x / split) {
+    const int b = find_share(pre, a.c.n_seq, item);
     int first, n;
-    call_rows(row_start, n_rows, b, first, n);
-    const int held = held_rows(c, b), off = held - n, j0 = (int)(item - pre[b]) * PL_KEYS;
+    call_rows(a.row_start, a.n_rows, b, first, n);
+    const int held = held_rows(a.c, b), off = held - n, j0 = (int)(item - pre[b]) * TILE;
     const int64_t rows = (int64_t)n * G;
     // query i sees the first of these rows if off + i >= j0
-    const int64_t from = (int64_t)max(0, j0 - off) * G / PL_ROWS * PL_ROWS;
+    const int64_t from = (int64_t)max(0, j0 - off) * G / TILE * TILE;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int kvh = 0; kvh < Hkv && from < rows; ++kvh) {
+    for (int kvh = rank; kvh < a.Hkv && from < rows; kvh += split) {
       __syncthreads();
-      load_rows<T, D, LD>(c, (const T*)c.k, b, kvh, Hkv, j0, held, sk, status);
-      for (int64_t r0 = from; r0 < rows; r0 += PL_ROWS) {
+      load_rows<T, D>(a, (const T*)a.c.k, b, kvh, j0, held, sk);
+      for (int64_t r0 = from; r0 < rows; r0 += TILE) {
         __syncthreads();
-        load_queries<T, D>(Q, ldq, first, (int)r0, rows, kvh, G, sq);
+        load_queries<T, D>(a, first, r0, rows, kvh, LOG2E * rsqrtf((float)D), sq);
+        if (tid < TILE) {
+          const int64_t r = r0 + tid;
+          const float e = r < rows ? a.lse[(first + r / G) * a.H + kvh * G + (int)(r % G)] * LOG2E : 0.f;
+          slse[tid] = e == -INFINITY ? 0.f : e;          // (such a query sees nothing)
+        }
         __syncthreads();
-        float s[2][4];
-        tile_scores<D, LD>(sq, sk, tr, tk, s);
+        float s[4][4];
+        tile_scores<D>(sq, sk, tq, tk, s);
+        const bool whole = r0 + TILE <= rows && j0 + TILE <= off + (int)(r0 / G) + 1;
 #pragma unroll
-        for (int a = 0; a < 2; ++a) {
-          const int64_t r = r0 + tr + 16 * a;
-          if (r >= rows) continue;
-          const int limit = off + (int)(r / G) + 1;
-          const float e = lse[(first + r / G) * H + kvh * G + (int)(r % G)];
+        for (int i = 0; i < 4; ++i) {
+          const int64_t r = r0 + 4 * tq + i;
+          const int limit = whole ? INT_MAX : r < rows ? off + (int)(r / G) + 1 : 0;
+          const float e = slse[4 * tq + i];
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            if (j0 + tk + 16 * k < limit) sum[k] += expf(s[a][k] * scale - e);
+            if (j0 + tk + 16 * k < limit) sum[k] += exp2f(s[i][k] - e);
         }
       }
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 4; ++k) part[tr * PL_KEYS + tk + 16 * k] = sum[k];
+    for (int k = 0; k < 4; ++k) part[tq * TILE + tk + 16 * k] = sum[k];
     __syncthreads();
-    if (tid < PL_KEYS && j0 + tid < held) {
+    if (tid < TILE) {
       float w = 0.f;
-      for (int i = 0; i < 16; ++i) w += part[i * PL_KEYS + tid];
-      const int64_t slot = slot_of(c, b, j0 + tid);
-      if (slot >= 0) c.weight[slot] = (decay == 0.f ? 0.f : decay * c.weight[slot]) + w / (float)H;
-      else set_status(status, SPTS_ERR_INDEX);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w += part[i * TILE + tid];
+      sum_all[tid] = w;
     }
+    write_weights(cluster, a, b, held, j0, TILE, sum_all);
+  }
+}
+
+// ---- row kernels
+// Totals over the lanes of v[32]: lane i gets that of v[i].
+__device__ __forceinline__ float lane_totals(float (&v)[32]) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const bool high = lane & o;
+#pragma unroll
+    for (int i = 0; i < o; ++i) {
+      const float keep = high ? v[i + o] : v[i], give = high ? v[i] : v[i + o];
+      v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+    }
+  }
+  return v[0];
+}
+// Scores of four rows of queries and eight of the cache: lane 8 r + k gets that of row r and k.
+template <int PER>
+__device__ __forceinline__ float few_scores(const float (&q)[FEW][PER], const float (&k)[STEP][PER]) {
+  float v[32];
+#pragma unroll
+  for (int r = 0; r < FEW; ++r)
+#pragma unroll
+    for (int u = 0; u < STEP; ++u) {
+      float x = 0.f;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) x = fmaf(q[r][e], k[u][e], x);
+      v[STEP * r + u] = x;
+    }
+  return lane_totals(v);
+}
+template <typename T, int D>
+__device__ __forceinline__ void load_few(const PlainArgs& a, int64_t first, int64_t r0, int64_t rows, int kvh, float (&q)[FEW][D / 32]) {
+  const int G = a.H / a.Hkv, lane = threadIdx.x & 31;
+  const float scale = LOG2E * rsqrtf((float)D);
+#pragma unroll
+  for (int r = 0; r < FEW; ++r) {
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) q[r][e] = 0.f;
+    const int64_t x = r0 + r;
+    if (x < rows) load_lane<T, D / 32>((const T*)a.Q + (first + x / G) * a.ldq + (int64_t)(kvh * G + x % G) * D + lane * (D / 32), q[r]);
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) q[r][e] *= scale;
+  }
+}
+
+// A cluster to (four rows of queries, KV head); each warp takes every eighth step of eight rows of the cache of the CTA's share, the lanes
+// hold D / 32 dims of everything; the warps' results meet in shared memory.  Where a step's rows lie is looked up a step ahead.
+template <typename T, int D>
+__global__ void __launch_bounds__(PL_THREADS, 2)
+paged_attn_row_kernel(const __grid_constant__ PlainArgs a) {
+  constexpr int PER = D / 32;
+  __shared__ __align__(16) float so[PL_WARPS][FEW * D];
+  __shared__ __align__(16) float sp[PL_WARPS][32];
+  __shared__ float sm[PL_WARPS][FEW], sl[PL_WARPS][FEW], tm[FEW], tl[FEW];
+  __shared__ long long pre[PREFIX_MAX + 1], sums[32];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int split = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int G = a.H / a.Hkv, kvh = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  QueryTile t;
+  if (!find_tile<FEW>(a, blockIdx.x / split, kvh == 0 && blockIdx.x == 0, pre, sums, t)) return;
+  float q[FEW][PER], acc[FEW][PER];
+  load_few<T, D>(a, t.first, t.r0, t.rows, kvh, q);
+#pragma unroll
+  for (int r = 0; r < FEW; ++r)
+#pragma unroll
+    for (int e = 0; e < PER; ++e) acc[r][e] = 0.f;
+  // this lane's row of queries and its place in a step
+  const int64_t mine = t.r0 + lane / STEP;
+  const int limit = mine < t.rows ? t.off + (int)(mine / G) + 1 : 0, at = lane % STEP;
+  const int all = t.r0 + FEW <= t.rows ? t.off + (int)(t.r0 / G) + 1 : 0;      // rows that all of the tile's queries see
+  float m = -INFINITY, l = 0.f;
+  const int steps = (t.seen + STEP - 1) / STEP, s1 = (int)((int64_t)steps * (rank + 1) / split);
+  const auto look_up = [&](int st) -> int64_t {          // where row `at` of a step is
+    const int j = st * STEP + at;
+    if (st >= s1 || j >= t.seen) return -1;
+    const int64_t slot = slot_of(a.c, t.b, j);
+    if (slot < 0) set_status(a.status, SPTS_ERR_INDEX);
+    return slot;
+  };
+  int st = (int)((int64_t)steps * rank / split) + warp;
+  int64_t next = look_up(st);
+  for (; st < s1; st += PL_WARPS) {
+    const int j0 = st * STEP;
+    const int64_t slot = next;
+    float k[STEP][PER], v[STEP][PER];
+#pragma unroll
+    for (int u = 0; u < STEP; ++u) {
+#pragma unroll
+      for (int e = 0; e < PER; ++e) { k[u][e] = 0.f; v[u][e] = 0.f; }
+      const int64_t x = __shfl_sync(0xffffffffu, slot, u);
+      if (x < 0) continue;
+      load_lane<T, PER>((const T*)a.c.k + (x * a.Hkv + kvh) * D + lane * PER, k[u]);
+      load_lane<T, PER>((const T*)a.c.v + (x * a.Hkv + kvh) * D + lane * PER, v[u]);
+    }
+    next = look_up(st + PL_WARPS);
+    float s = few_scores<PER>(q, k);
+    const bool whole = j0 + STEP <= all;
+    if (!whole && j0 + at >= limit) s = -INFINITY;
+    float top = s;
+#pragma unroll
+    for (int o = 1; o < STEP; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    float alpha = 1.f;
+    if (top > m + SLACK || m == -INFINITY) {
+      alpha = m == -INFINITY ? 0.f : exp2f(m - top);
+      m = top;
+    }
+    const float p = exp2f(s - (m == -INFINITY ? 0.f : m));
+    l = l * alpha + p;
+    sp[warp][lane] = p;
+    if (__any_sync(0xffffffffu, alpha != 1.f)) {
+#pragma unroll
+      for (int r = 0; r < FEW; ++r) {
+        const float f = __shfl_sync(0xffffffffu, alpha, STEP * r);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) acc[r][e] *= f;
+      }
+    }
+    __syncwarp();
+#pragma unroll
+    for (int r = 0; r < FEW; ++r) {
+      const float4 w0 = *reinterpret_cast<const float4*>(&sp[warp][STEP * r]), w1 = *reinterpret_cast<const float4*>(&sp[warp][STEP * r + 4]);
+      const float w[STEP] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+#pragma unroll
+      for (int u = 0; u < STEP; ++u)
+        if (whole || w[u] != 0.f) {
+#pragma unroll
+          for (int e = 0; e < PER; ++e) acc[r][e] = fmaf(w[u], v[u][e], acc[r][e]);
+        }
+    }
+    __syncwarp();
+  }
+#pragma unroll
+  for (int o = 1; o < STEP; o *= 2) l += __shfl_xor_sync(0xffffffffu, l, o);
+  if (at == 0) { sm[warp][lane / STEP] = m; sl[warp][lane / STEP] = l; }
+#pragma unroll
+  for (int r = 0; r < FEW; ++r)
+#pragma unroll
+    for (int e = 0; e < PER; ++e) so[warp][r * D + lane * PER + e] = acc[r][e];
+  __syncthreads();
+  // warp r joins row r of the CTA's warps
+  if (warp < FEW) {
+    const int r = warp;
+    float top = -INFINITY, sum = 0.f, o[PER];
+#pragma unroll
+    for (int w = 0; w < PL_WARPS; ++w) top = fmaxf(top, sm[w][r]);
+#pragma unroll
+    for (int e = 0; e < PER; ++e) o[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < PL_WARPS; ++w) {
+      if (sm[w][r] == -INFINITY && sl[w][r] == 0.f) continue;
+      const float f = sm[w][r] == -INFINITY ? 1.f : exp2f(sm[w][r] - top);
+      sum += sl[w][r] * f;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) o[e] += so[w][r * D + lane * PER + e] * f;
+    }
+#pragma unroll
+    for (int e = 0; e < PER; ++e) so[0][r * D + lane * PER + e] = o[e];      // (no other warp reads row r)
+    if (lane == 0) { tm[r] = top; tl[r] = sum; }
+  }
+  join_cluster<T, D>(cluster, a, t, FEW, kvh, tm, tl, so[0]);
+}
+
+// Persistent clusters over (sequence, 256 rows of it), 32 to a warp; a CTA has every split-th KV head, whose queries stay in registers while
+// the warp's rows pass.
+template <typename T, int D>
+__global__ void __launch_bounds__(PL_THREADS, 2)
+paged_weights_row_kernel(const __grid_constant__ PlainArgs a) {
+  constexpr int PER = D / 32, ROWS = PL_WARPS * WARP_KEYS, STEPS = WARP_KEYS / STEP;
+  __shared__ float sum_all[ROWS];
+  __shared__ long long pre[PREFIX_MAX + 1], sums[32];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int split = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int G = a.H / a.Hkv, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, at = lane % STEP;
+  const long long items = blocks_of_rows<ROWS>(a, blockIdx.x == 0, pre, sums);
+  for (long long item = blockIdx.x / split; item < items; item += gridDim.x / split) {
+    const int b = find_share(pre, a.c.n_seq, item);
+    int first, n;
+    call_rows(a.row_start, a.n_rows, b, first, n);
+    const int held = held_rows(a.c, b), off = held - n, block0 = (int)(item - pre[b]) * ROWS, j0 = block0 + warp * WARP_KEYS;
+    const int64_t rows = (int64_t)n * G, from = (int64_t)max(0, j0 - off) * G / FEW * FEW;
+    float sum[STEPS];
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) sum[st] = 0.f;
+    const int64_t slot = j0 + lane < held ? slot_of(a.c, b, j0 + lane) : -1;       // (lane i: of row j0 + i)
+    for (int kvh = rank; kvh < a.Hkv && j0 < held; kvh += split) {
+      for (int64_t r0 = from; r0 < rows; r0 += FEW) {
+        float q[FEW][PER];
+        load_few<T, D>(a, first, r0, rows, kvh, q);
+        const int64_t mine = r0 + lane / STEP;
+        const int limit = mine < rows ? off + (int)(mine / G) + 1 : 0;
+        float e = mine < rows ? a.lse[(first + mine / G) * a.H + kvh * G + (int)(mine % G)] * LOG2E : 0.f;
+        if (e == -INFINITY) e = 0.f;                                   // (such a query sees nothing)
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) {
+          float k[STEP][PER];
+#pragma unroll
+          for (int u = 0; u < STEP; ++u) {
+            const int64_t x = __shfl_sync(0xffffffffu, slot, st * STEP + u);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) k[u][i] = 0.f;
+            if (x >= 0) load_lane<T, PER>((const T*)a.c.k + (x * a.Hkv + kvh) * D + lane * PER, k[u]);
+          }
+          const float s = few_scores<PER>(q, k);
+          if (j0 + st * STEP + at < limit) sum[st] += exp2f(s - e);
+        }
+      }
+    }
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) {
+      float w = sum[st];
+#pragma unroll
+      for (int o = STEP; o < 32; o *= 2) w += __shfl_xor_sync(0xffffffffu, w, o);
+      if (lane < STEP) sum_all[warp * WARP_KEYS + st * STEP + lane] = w;
+    }
+    __syncthreads();
+    write_weights(cluster, a, b, held, block0, ROWS, sum_all);
   }
 }
 
@@ -690,44 +1008,57 @@ evict_move_kernel(EvictArgs a, int n_seq, int split, int row_bytes) {
   }
 }
 
-template <typename T, int D>
-spts_status attn_plain_t(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start, int n_rows,
-                         void* O, int64_t ldo, float* lse) {
-  const int H = ctx->desc.n_q_heads, Hkv = ctx->desc.n_kv_heads, G = H / Hkv;
-  const int64_t tiles = (int64_t)n_rows * G / PL_ROWS + cache->n_seq;          // no fewer than there are
-  const int split = tiles * Hkv <= ctx->sm_count / 2 ? PL_SPLIT : 1;
+// A cluster of `split` CTAs to a block of work.
+spts_status launch_clusters(spts_ctx* ctx, void (*kernel)(PlainArgs), dim3 grid, int split, int smem, const PlainArgs& a) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(tiles * split), Hkv);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(PL_THREADS);
-  cfg.dynamicSmemBytes = plain_attn_smem<D>();
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = ctx->stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, paged_attn_plain_kernel<T, D>, make_cache(cache), (const T*)Q, ldq, row_start, n_rows, H, Hkv, (T*)O, ldo, lse,
-                         ctx->ws.status) != cudaSuccess)
-    return SPTS_ERR_CUDA;
+  if (cudaLaunchKernelEx(&cfg, kernel, a) != cudaSuccess) return SPTS_ERR_CUDA;
   ctx->launches++;
   return SPTS_OK;
 }
+// CTAs that share a block of work: as many as make two blocks to an SM, a power of two.
+int share_of(const spts_ctx* ctx, int64_t blocks, int most) {
+  int split = 1;
+  while (2 * split <= most && blocks * split < 2 * ctx->sm_count) split *= 2;
+  return split;
+}
+bool few_rows(const spts_ctx* ctx, const spts_paged_kv* cache, int n_rows) {
+  return (int64_t)n_rows * (ctx->desc.n_q_heads / ctx->desc.n_kv_heads) <= (int64_t)FEW_MOST * cache->n_seq;
+}
 
 template <typename T, int D>
-spts_status weights_plain_t(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start, int n_rows,
-                            const float* lse, float decay) {
-  const int64_t items = (int64_t)cache->n_seq * ceil_div(cache->max_pages * cache->page_size, PL_KEYS);
-  const int grid = (int)(items < 3 * ctx->sm_count ? items : 3 * ctx->sm_count);
-  paged_weights_plain_kernel<T, D><<<grid, PL_THREADS, plain_weights_smem<D>(), ctx->stream>>>(
-      make_cache(cache), (const T*)Q, ldq, row_start, n_rows, ctx->desc.n_q_heads, ctx->desc.n_kv_heads, lse, decay, ctx->ws.status);
-  SPTS_CUDA_OK(ctx);
-  return SPTS_OK;
+spts_status attn_plain_t(spts_ctx* ctx, const spts_paged_kv* cache, const PlainArgs& a) {
+  const bool few = few_rows(ctx, cache, a.n_rows);
+  const int64_t tiles = (int64_t)a.n_rows * (a.H / a.Hkv) / (few ? FEW : TILE) + cache->n_seq;       // no fewer than there are
+  const int split = share_of(ctx, tiles * a.Hkv, PL_SPLIT);
+  const dim3 grid((unsigned)(tiles * split), a.Hkv);
+  return few ? launch_clusters(ctx, paged_attn_row_kernel<T, D>, grid, split, 0, a)
+             : launch_clusters(ctx, paged_attn_tile_kernel<T, D>, grid, split, attn_tile_smem<D>(), a);
+}
+
+template <typename T, int D>
+spts_status weights_plain_t(spts_ctx* ctx, const spts_paged_kv* cache, const PlainArgs& a) {
+  const bool few = few_rows(ctx, cache, a.n_rows);
+  const int64_t most = (int64_t)cache->n_seq * ceil_div(cache->max_pages * cache->page_size, few ? PL_WARPS * WARP_KEYS : TILE);
+  const int split = share_of(ctx, most, a.Hkv < PL_SPLIT ? a.Hkv : PL_SPLIT);
+  const int64_t resident = 4 * ctx->sm_count / split;
+  const dim3 grid((unsigned)((most < resident ? most : resident) * split));
+  return few ? launch_clusters(ctx, paged_weights_row_kernel<T, D>, grid, split, 0, a)
+             : launch_clusters(ctx, paged_weights_tile_kernel<T, D>, grid, split, weights_tile_smem<D>(), a);
 }
 
 template <typename T, int D>
 bool plain_attr() {
-  return cudaFuncSetAttribute(paged_attn_plain_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, plain_attn_smem<D>()) == cudaSuccess &&
-         cudaFuncSetAttribute(paged_weights_plain_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, plain_weights_smem<D>()) == cudaSuccess;
+  return cudaFuncSetAttribute(paged_attn_tile_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, attn_tile_smem<D>()) == cudaSuccess &&
+         cudaFuncSetAttribute(paged_weights_tile_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, weights_tile_smem<D>()) == cudaSuccess;
 }
 
 }  // namespace
@@ -755,24 +1086,21 @@ spts_status launch_paged_attention(spts_ctx* ctx, const spts_paged_kv* cache, co
                                    int n_rows, void* O, int64_t ldo, float* lse) {
   if (n_rows == 1) { ldq = 0; ldo = 0; }      // one row has no stride
   if (paged_tc(ctx)) return launch_paged_attention_tc(ctx, cache, Q, ldq, row_start, n_rows, O, ldo, lse);
+  const PlainArgs a = {make_cache(cache), row_start, n_rows, ctx->desc.n_q_heads, ctx->desc.n_kv_heads, Q, ldq, O, ldo, lse, 0.f, ctx->ws.status};
   const bool d64 = ctx->desc.head_dim == 64;
-  if (ctx->desc.dtype == SPTS_BF16)
-    return d64 ? attn_plain_t<bf16, 64>(ctx, cache, Q, ldq, row_start, n_rows, O, ldo, lse)
-               : attn_plain_t<bf16, 128>(ctx, cache, Q, ldq, row_start, n_rows, O, ldo, lse);
-  return d64 ? attn_plain_t<float, 64>(ctx, cache, Q, ldq, row_start, n_rows, O, ldo, lse)
-             : attn_plain_t<float, 128>(ctx, cache, Q, ldq, row_start, n_rows, O, ldo, lse);
+  if (ctx->desc.dtype == SPTS_BF16) return d64 ? attn_plain_t<bf16, 64>(ctx, cache, a) : attn_plain_t<bf16, 128>(ctx, cache, a);
+  return d64 ? attn_plain_t<float, 64>(ctx, cache, a) : attn_plain_t<float, 128>(ctx, cache, a);
 }
 
 spts_status launch_paged_weights(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, int64_t ldq, const int32_t* row_start,
                                  int n_rows, const float* lse, float decay) {
   if (n_rows == 1) ldq = 0;
   if (paged_tc(ctx)) return launch_paged_weights_tc(ctx, cache, Q, ldq, row_start, n_rows, lse, decay);
+  const PlainArgs a = {make_cache(cache), row_start, n_rows, ctx->desc.n_q_heads, ctx->desc.n_kv_heads, Q, ldq, nullptr, 0, const_cast<float*>(lse), decay,
+                       ctx->ws.status};
   const bool d64 = ctx->desc.head_dim == 64;
-  if (ctx->desc.dtype == SPTS_BF16)
-    return d64 ? weights_plain_t<bf16, 64>(ctx, cache, Q, ldq, row_start, n_rows, lse, decay)
-               : weights_plain_t<bf16, 128>(ctx, cache, Q, ldq, row_start, n_rows, lse, decay);
-  return d64 ? weights_plain_t<float, 64>(ctx, cache, Q, ldq, row_start, n_rows, lse, decay)
-             : weights_plain_t<float, 128>(ctx, cache, Q, ldq, row_start, n_rows, lse, decay);
+  if (ctx->desc.dtype == SPTS_BF16) return d64 ? weights_plain_t<bf16, 64>(ctx, cache, a) : weights_plain_t<bf16, 128>(ctx, cache, a);
+  return d64 ? weights_plain_t<float, 64>(ctx, cache, a) : weights_plain_t<float, 128>(ctx, cache, a);
 }
 
 spts_status launch_paged_evict(spts_ctx* ctx, const spts_paged_kv* cache, const int32_t* keep, int n_sink, int n_recent) {
