@@ -407,6 +407,10 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, int unit_row, int h,
 }
 
 // ------------------------------------------------------------------------------------------------ the kernel
+// Long chunks are bound by the exponentials and the issue of the softmax warps beside the matrix products (2048 tokens over 34816 rows, 32 heads
+// of 128 dims: 1.01 ms, 1119 TFLOP/s; 8192 fresh ones 1206), decode steps by memory (64 sequences of up to 16384 rows: 5.7 to 6.1 TB/s; 48 of up
+// to nine drafted tokens 127 us, 5.1 TB/s), single short ones by their chain of latencies (777 rows: 11.8 us).  Sixteen softmax warps instead of
+// eight were slower (64 single tokens 188 us against 147; 2048 tokens 1064 against 964).
 struct Start { Walk walk; long long total; };      // a CTA's piece, the line's length
 
 template <int D>
@@ -958,8 +962,9 @@ paged_attn_join_kernel(const __grid_constant__ AttnArgs a) {
 //   warp 1      TMEM owner and MMA issuer: two accumulators for each of the two blocks
 //   warps 2-3   -lse log2(e) of a tile's queries into shared memory
 //   warps 4-11  the exponentials of every second item, warps 12-19 of the others; of the first block warps 4-7 and 12-15
-// (bound by the exponential unit where queries are many: with four warps on each of its quarters instead of two 64 queries over 32768 rows
-// take PLACEHOLDER)
+// Bound by memory where queries are few (16 single tokens over up to 8192 rows: 25.6 us, 4.3 TB/s with the launch and the line's ends), by the
+// exponential unit where they are many: 512 tokens over 32768 rows take 193 us (290 with two warps on each of its quarters instead of four),
+// 64 tokens 33 us (37; with all 128 columns of a row in registers at once 46).
 constexpr int PW_THREADS = 640;
 constexpr int PW_Q = 2, PW_E = 4;              // tiles of queries in flight, of their lse
 template <int D> constexpr int pw_smem() { return 1024 + (4 + PW_Q) * tile_bytes<D>() + 256 + (PW_E + 2) * BLOCK * 4 + 64; }
