@@ -134,18 +134,23 @@ __device__ __forceinline__ bool elect_lane() {
   return mine != 0;
 }
 
-// A wait whose limit counts from its own beginning.
-__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+// A wait whose limit counts from its own beginning.  `flags`: [0] somebody gave up; [1] grows while rows are computed again (plain_row),
+// which may take longer than the limit: it counts from the last sign of that.
+constexpr int ABORT = 0, BUSY = 1;
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* flags) {
   if (mbar_test_wait(bar, parity)) return true;
   uint64_t t0 = 0;
+  int busy = 0;
   for (uint32_t it = 0;; ++it) {
     if (mbar_try_wait(bar, parity)) return true;
     if ((it & 0xFFu) == 0xFFu) {
-      if (*abort_flag) return false;
+      if (flags[ABORT]) return false;
       const uint64_t now = globaltimer_ns();
-      if (t0 == 0) t0 = now;
-      else if (now - t0 > WAIT_LIMIT_NS) {
-        *abort_flag = 1;
+      if (t0 == 0 || flags[BUSY] != busy) {
+        t0 = now;
+        busy = flags[BUSY];
+      } else if (now - t0 > WAIT_LIMIT_NS) {
+        flags[ABORT] = 1;
         return false;
       }
     }
@@ -153,8 +158,8 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int
 }
 
 // The same for a whole warp: all lanes or none go on.
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  return __all_sync(0xffffffffu, wait(bar, parity, abort_flag));
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* flags) {
+  return __all_sync(0xffffffffu, wait(bar, parity, flags));
 }
 
 // ------------------------------------------------------------------------------------------------ the line of blocks
@@ -320,36 +325,67 @@ struct Walk {
 };
 
 // ------------------------------------------------------------------------------------------------ rows that came out not finite
-// A weight of zero does not keep an infinity or NaN of V out of a product of matrices.  A row that came out not finite is computed
-// again, by its warp, over the rows [k0, k1) of the cache that it sees: D / 32 dims to a lane.  (m in log2 units; o not divided by l.)
+// A weight of zero does not keep an infinity or NaN of V out of a product of matrices.  A row with a finite sum of weights that came out not
+// finite, of a segment that holds rows it does not see, is computed again, by its warp, over the rows [k0, k1) of the cache that it sees:
+// D / 32 dims to a lane, eight rows at a time.  (m in log2 units; o not divided by l.)
 template <int D>
-__device__ __noinline__ void plain_row(const AttnArgs& a, int b, int kvh, const bf16* q, int k0, int k1, float& m, float& l, float* o) {
-  constexpr int PER = D / 32;
+__device__ __noinline__ void plain_row(const AttnArgs& a, int b, int kvh, const bf16* q, int k0, int k1, volatile int* busy, float& m_out, float& l_out,
+                                       float* o_out) {
+  constexpr int PER = D / 32, STEP = 8;
   const int lane = threadIdx.x & 31;
-  float qf[PER];
+  const auto load = [&](const char* x, int64_t slot, float (&to)[PER]) {
+    const __nv_bfloat162* at = reinterpret_cast<const __nv_bfloat162*>(reinterpret_cast<const bf16*>(x) + (max(slot, (int64_t)0) * a.Hkv + kvh) * D + lane * PER);
 #pragma unroll
-  for (int e = 0; e < PER; ++e) { qf[e] = __bfloat162float(q[lane * PER + e]); o[e] = 0.f; }
-  m = -INFINITY;
-  l = 0.f;
-  const float sc = LOG2E * rsqrtf((float)D);
-  for (int j = k0; j < k1; ++j) {
-    const int64_t slot = slot_of(a.c, b, j);
-    float kf[PER], vf[PER], s = 0.f;
-#pragma unroll
-    for (int e = 0; e < PER; ++e) {
-      const int64_t at = (slot * a.Hkv + kvh) * D + lane * PER + e;
-      kf[e] = slot < 0 ? 0.f : __bfloat162float(reinterpret_cast<const bf16*>(a.c.k)[at]);
-      vf[e] = slot < 0 ? 0.f : __bfloat162float(reinterpret_cast<const bf16*>(a.c.v)[at]);
-      s = fmaf(qf[e], kf[e], s);
+    for (int e = 0; e < PER / 2; ++e) {
+      const float2 y = __bfloat1622float2(__ldg(at + e));
+      to[2 * e] = slot < 0 ? 0.f : y.x;
+      to[2 * e + 1] = slot < 0 ? 0.f : y.y;
     }
-    s = warp_sum(s) * sc;
-    const float now = fmaxf(m, s), base = now == -INFINITY ? 0.f : now;
-    const float alpha = m == -INFINITY ? 0.f : ex2(m - base), p = ex2(s - base);
-    l = l * alpha + p;
+  };
+  float qf[PER], m = -INFINITY, l = 0.f, o[PER];
+  const float sc = LOG2E * rsqrtf((float)D);
 #pragma unroll
-    for (int e = 0; e < PER; ++e) o[e] = p == 0.f ? o[e] * alpha : fmaf(p, vf[e], o[e] * alpha);
-    m = now;
+  for (int e = 0; e < PER; ++e) { qf[e] = __bfloat162float(q[lane * PER + e]) * sc; o[e] = 0.f; }
+  for (int j0 = k0; j0 < k1; j0 += 32) {
+    if (lane == 0) *busy = *busy + 1;
+    const int64_t slots = j0 + lane < k1 ? slot_of(a.c, b, j0 + lane) : -1;
+    for (int u0 = 0; u0 < 32 && j0 + u0 < k1; u0 += STEP) {
+      float s[STEP], v[STEP][PER];
+#pragma unroll
+      for (int u = 0; u < STEP; ++u) {
+        const int64_t slot = __shfl_sync(0xffffffffu, slots, u0 + u);
+        float kf[PER];
+        load(a.c.k, slot, kf);
+        load(a.c.v, slot, v[u]);
+        s[u] = 0.f;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) s[u] = fmaf(qf[e], kf[e], s[u]);
+      }
+      float now = m;
+#pragma unroll
+      for (int u = 0; u < STEP; ++u) {
+        s[u] = warp_sum(s[u]);
+        if (j0 + u0 + u >= k1) s[u] = -INFINITY;
+        now = fmaxf(now, s[u]);
+      }
+      const float base = now == -INFINITY ? 0.f : now, alpha = m == -INFINITY ? 0.f : ex2(m - base);
+      l *= alpha;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) o[e] *= alpha;
+#pragma unroll
+      for (int u = 0; u < STEP; ++u) {
+        const float p = ex2(s[u] - base);
+        l += p;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) o[e] = p == 0.f ? o[e] : fmaf(p, v[u][e], o[e]);
+      }
+      m = now;
+    }
   }
+  m_out = m;
+  l_out = l;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) o_out[e] = o[e];
 }
 
 // ------------------------------------------------------------------------------------------------ joining shares
@@ -431,15 +467,15 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   const uint32_t v_tail = free_ + 8 * RING, v_clean = v_tail + 8 * RING;
   const uint32_t x_full = v_clean + 8 * RING, x_free = x_full + 8;   // slot 1's maximum and sum are there; its O has been read
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + (bars - base) + 384);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  volatile int* flags = reinterpret_cast<volatile int*>(tmem_slot + 1);        // [2]
   float2* ml = reinterpret_cast<float2*>(gen + (bars - base) + 512);
   const uint32_t g_done = x_free + 8;          // [2 slots] the slot's threads are at the same point
-  volatile int* g_last = abort_flag + 1;       // [2 slots] the slot's share was the last of its unit
+  volatile int* g_last = flags + 2;            // [2 slots] the slot's share was the last of its unit
   Start* start = reinterpret_cast<Start*>(gen + (bars - base) + 512 + 1024);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    *abort_flag = 0;
+    flags[ABORT] = flags[BUSY] = 0;
     for (int s = 0; s < 2; ++s) {
       mbar_init(q_full + 8 * s, 1); mbar_init(q_free + 8 * s, 1);
       mbar_init(s_full + 8 * s, 1); mbar_init(o_full + 8 * s, 1);
@@ -502,7 +538,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         int y0 = place(s.j0), y1 = place(s.j0 + 1), y2 = place(s.j0 + 2);
         for (int t = 0; t < (s.two ? 2 : 1); ++t) {
           const int buf = s.two ? t : (int)q_next;
-          ok = ok && wait_warp(q_free + 8 * buf, (q_phase >> buf) & 1, abort_flag);
+          ok = ok && wait_warp(q_free + 8 * buf, (q_phase >> buf) & 1, flags);
           q_phase ^= 1u << buf;
           if (ok && lane == 0) {
             mbar_expect_tx(q_full + 8 * buf, q_bytes);
@@ -512,7 +548,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
         if (!s.two) q_next ^= 1;
         auto load = [&](bool is_v, int j, int y) {
-          ok = ok && wait_warp(free_ + 8 * slot, phase, abort_flag);
+          ok = ok && wait_warp(free_ + 8 * slot, phase, flags);
           if (!ok) return;
           const int rows = max(0, min(BLOCK, s.held - j * BLOCK)), boxes = (rows + box - 1) / box;
           const uint32_t bar = full + 8 * slot;
@@ -551,10 +587,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           if (++slot == RING) { slot = 0; phase ^= 1; }
         };
         // the ring's next tile has come (a tail of V: has been cleared)
-        const auto wait_tile = [&]() { ok = ok && wait_warp(full + 8 * slot, phase, abort_flag); };
+        const auto wait_tile = [&]() { ok = ok && wait_warp(full + 8 * slot, phase, flags); };
         const auto wait_v = [&](bool tail) {
           if (tail) {
-            ok = ok && wait_warp(v_clean + 8 * slot, (clean >> slot) & 1, abort_flag);
+            ok = ok && wait_warp(v_clean + 8 * slot, (clean >> slot) & 1, flags);
             clean ^= 1u << slot;
           } else {
             wait_tile();
@@ -576,7 +612,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           bits ^= 1u << t;
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
-            ok = ok && wait_warp(p_full + 8 * (2 * t + half), ph, abort_flag);
+            ok = ok && wait_warp(p_full + 8 * (2 * t + half), ph, flags);
             if (!ok) return;
             tc_fence_after();
             if (leader) {
@@ -590,7 +626,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           const int nb = __shfl_sync(0xffffffffu, s.j1 - s.j0, 0);
           const bool tail = __any_sync(0xffffffffu, s.j1 * BLOCK > s.held);
           if (__any_sync(0xffffffffu, s.two)) {
-            ok = ok && wait_warp(q_full, (bits >> 2) & 1, abort_flag) && wait_warp(q_full + 8, (bits >> 3) & 1, abort_flag);
+            ok = ok && wait_warp(q_full, (bits >> 2) & 1, flags) && wait_warp(q_full + 8, (bits >> 3) & 1, flags);
             bits ^= 12;
             wait_tile();
             if (!ok) break;
@@ -632,7 +668,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             next_slot();
           } else {
             const uint32_t q = q_lo + q_next * (TILE >> 4), qf = q_free + 8 * q_next;
-            ok = ok && wait_warp(q_full + 8 * q_next, (bits >> (2 + q_next)) & 1, abort_flag);
+            ok = ok && wait_warp(q_full + 8 * q_next, (bits >> (2 + q_next)) & 1, flags);
             bits ^= 4u << q_next;
             q_next ^= 1;
             for (int i = 0; i < 2 && i < nb; ++i) {
@@ -677,7 +713,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         if (s.j1 * BLOCK <= s.held) continue;
         // the tile was asked for: the one that was in its place before has been used, and it will stay until it is clear
         const uint32_t slot = (at - 1) % RING;
-        ok = wait_warp(v_tail + 8 * slot, (tails >> slot) & 1, abort_flag) && wait_warp(full + 8 * slot, ((at - 1) / RING) & 1, abort_flag);
+        ok = wait_warp(v_tail + 8 * slot, (tails >> slot) & 1, flags) && wait_warp(full + 8 * slot, ((at - 1) / RING) & 1, flags);
         tails ^= 1u << slot;
         if (!ok) break;
         const int rows = max(0, s.held - (s.j1 - 1) * BLOCK);
@@ -713,7 +749,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       float m_used = -INFINITY, l = 0.f;
       int done = 0;
       for (int i = s.two ? 0 : ((t + turn) & 1); i < nb && ok; i += s.two ? 1 : 2) {
-        ok = wait_warp(s_full + 8 * t, n_s & 1, abort_flag);
+        ok = wait_warp(s_full + 8 * t, n_s & 1, flags);
         ++n_s;
         if (!ok) break;
         if (!any_live) {                                                   // rows of no query: whatever P holds stays in them
@@ -787,7 +823,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       const bool merge = !s.two && nb > 1, mine = s.two || (merge ? t == 0 : (int)(turn & 1) == t);
       if (!s.two) turn = (turn + nb) & 1;
       if (mine || merge) {
-        ok = wait_warp(o_full + 8 * t, n_o & 1, abort_flag);
+        ok = wait_warp(o_full + 8 * t, n_o & 1, flags);
         ++n_o;
         if (!ok) break;
         tc_fence_after();
@@ -797,13 +833,13 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         ml[row] = make_float2(m_used, l);
         tc_fence_before();
         mbar_arrive(x_full);
-        ok = wait_warp(x_free, n_x & 1, abort_flag);
+        ok = wait_warp(x_free, n_x & 1, flags);
         ++n_x;
         continue;
       }
       if (!mine) continue;
       if (merge) {
-        ok = wait_warp(x_full, n_x & 1, abort_flag);
+        ok = wait_warp(x_full, n_x & 1, flags);
         ++n_x;
         if (!ok) break;
         tc_fence_after();
@@ -873,7 +909,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         tc_fence_before();
         mbar_arrive(x_free);
       }
-      uint32_t again = __ballot_sync(0xffffffffu, live && odd != odd);
+      uint32_t again = __ballot_sync(0xffffffffu, live && odd != odd && l == l && limit < s.j1 * BLOCK);
       while (again) {
         const int who = __ffs(again) - 1;
         again &= again - 1;
@@ -881,7 +917,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         const int w_limit = __shfl_sync(0xffffffffu, limit, who);
         const int64_t w_out = (int64_t)s.row + tile * a.tile_tokens + w_token;
         float m, sum, o[D / 32];
-        plain_row<D>(a, s.b, s.h, a.Q + w_out * a.ldq + (int64_t)w_head * D, s.j0 * BLOCK, min(s.j1 * BLOCK, w_limit), m, sum, o);
+        plain_row<D>(a, s.b, s.h, a.Q + w_out * a.ldq + (int64_t)w_head * D, s.j0 * BLOCK, min(s.j1 * BLOCK, w_limit), flags + BUSY, m, sum, o);
         __syncwarp();
 #pragma unroll
         for (int e = 0; e < D / 32; ++e) {
@@ -901,7 +937,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         const int ctas = gridDim.x, first = cta_of(total, s.begin, ctas), last = cta_of(total, s.begin + s.cost - 1, ctas);
         __threadfence();
         mbar_arrive(g_done + 8 * t);
-        ok = wait_warp(g_done + 8 * t, n_g & 1, abort_flag);
+        ok = wait_warp(g_done + 8 * t, n_g & 1, flags);
         ++n_g;
         if (!ok) break;
         if (row == 0) {
@@ -910,7 +946,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           g_last[t] = is_last;
         }
         mbar_arrive(g_done + 8 * t);
-        ok = wait_warp(g_done + 8 * t, n_g & 1, abort_flag);
+        ok = wait_warp(g_done + 8 * t, n_g & 1, flags);
         ++n_g;
         if (!ok) break;
         if (g_last[t]) {
@@ -925,7 +961,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 
   tc_fence_before();
   __syncthreads();
-  if (*abort_flag) {
+  if (flags[ABORT]) {
     if (threadIdx.x == 0) set_status(a.status, SPTS_ERR_TIMEOUT);
     const uint64_t t1 = globaltimer_ns();
     while (globaltimer_ns() - t1 < 200000ull) { }
@@ -1042,14 +1078,14 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
   const uint32_t s_full = e_free + 8 * PW_E, s_free = s_full + 32;            // [2 blocks][2 accumulators]
   const uint32_t x_full = s_free + 32, x_free = x_full + 16;                  // [2 blocks] the second warps' sums are there; have been taken
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + (bars - base) + 240);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  volatile int* flags = reinterpret_cast<volatile int*>(tmem_slot + 1);        // [2]
   float* s_lse = reinterpret_cast<float*>(gen + (bars - base) + 256);
   float* s_sum = s_lse + PW_E * BLOCK;         // [2 blocks][128]
   UnitWalk* start = reinterpret_cast<UnitWalk*>(gen + (bars - base) + 256 + (PW_E + 2) * BLOCK * 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    *abort_flag = 0;
+    flags[ABORT] = flags[BUSY] = 0;
     for (int s = 0; s < 2; ++s) { mbar_init(k_full + 8 * s, 1); mbar_init(k_free + 8 * s, 1); }
     for (int s = 0; s < PW_Q; ++s) {
       mbar_init(q_full + 8 * s, 1); mbar_init(q_free + 8 * s, 1);
@@ -1125,7 +1161,7 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         const int h = i / s.tiles, q = s.tile0 + i % s.tiles;
         if (i == s.i0 || q == s.tile0) {
           const uint32_t st = n_k & 1, bar = k_full + 8 * st;
-          ok = wait_warp(k_free + 8 * st, ((n_k >> 1) & 1) ^ 1, abort_flag);
+          ok = wait_warp(k_free + 8 * st, ((n_k >> 1) & 1) ^ 1, flags);
           ++n_k;
           if (!ok) break;
           if (lane == 0) mbar_expect_tx(bar, (uint32_t)(boxes * box * 128 * SLABS));
@@ -1135,7 +1171,7 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             if (y[t] >= 0) tma_load_4d(sK + (2 * st + t) * TILE + lane * box * 128 * SLABS, &tmK, bar, 0, 0, h * SLABS, y[t] >> 3);
         }
         const uint32_t st = n_q % PW_Q;
-        ok = wait_warp(q_free + 8 * st, ((n_q / PW_Q) & 1) ^ 1, abort_flag);
+        ok = wait_warp(q_free + 8 * st, ((n_q / PW_Q) & 1) ^ 1, flags);
         ++n_q;
         if (ok && lane == 0) {
           mbar_expect_tx(q_full + 8 * st, q_bytes);
@@ -1159,16 +1195,16 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
       if (tiles == 0) continue;
       int q = i0 % tiles;                      // tile of queries, counted from the first
       for (int i = i0; i < i1 && ok; ++i) {
-        if (i == i0 || q == 0) { ok = wait_warp(k_full + 8 * (n_k & 1), (n_k >> 1) & 1, abort_flag); ++n_k; }
+        if (i == i0 || q == 0) { ok = wait_warp(k_full + 8 * (n_k & 1), (n_k >> 1) & 1, flags); ++n_k; }
         const uint32_t kst = (n_k - 1) & 1, qst = n_q % PW_Q, buf = n_q & 1;      // items alternate between the accumulators
-        ok = ok && wait_warp(q_full + 8 * qst, (n_q / PW_Q) & 1, abort_flag);
+        ok = ok && wait_warp(q_full + 8 * qst, (n_q / PW_Q) & 1, flags);
         ++n_q;
         const int cols = (min(a.tile_tokens, left - q * a.tile_tokens) * a.G + 15) & ~15;
         const uint32_t idesc = idesc_bf16(BLOCK, 0) | ((uint32_t)(cols >> 3) << 17), qd = q_lo + qst * (TILE >> 4);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           if (!ok || (t == 1 && !two)) break;
-          ok = wait_warp(s_free + 8 * (2 * t + buf), ((used >> (2 * t + buf)) & 1) ^ 1, abort_flag);
+          ok = wait_warp(s_free + 8 * (2 * t + buf), ((used >> (2 * t + buf)) & 1) ^ 1, flags);
           used ^= 1u << (2 * t + buf);
           if (!ok) break;
           tc_fence_after();
@@ -1202,7 +1238,7 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
           e[u] = c < tokens * a.G ? -__ldg(a.lse + (row + c / a.G) * a.H + h * a.G + c % a.G) * LOG2E : 0.f;
           if (e[u] == INFINITY) e[u] = 0.f;    // a query that sees nothing: all its scores become -inf, and stay
         }
-        ok = wait_warp(e_free + 8 * st, ((n_q / PW_E) & 1) ^ 1, abort_flag);
+        ok = wait_warp(e_free + 8 * st, ((n_q / PW_E) & 1) ^ 1, flags);
         ++n_q;
         if (!ok) break;
 #pragma unroll
@@ -1228,10 +1264,10 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         if ((int)(n_q & 1) != group) continue;
         const int q = s.tile0 + i % s.tiles, tokens = min(a.tile_tokens, s.n - q * a.tile_tokens), cols = tokens * a.G;
         const uint32_t st = n_q % PW_E;
-        ok = wait_warp(e_full + 8 * st, (n_q / PW_E) & 1, abort_flag);
+        ok = wait_warp(e_full + 8 * st, (n_q / PW_E) & 1, flags);
         if (!ok) break;
         if (work) {
-          ok = wait_warp(s_full + 8 * (2 * t + group), n_s & 1, abort_flag);
+          ok = wait_warp(s_full + 8 * (2 * t + group), n_s & 1, flags);
           ++n_s;
           if (!ok) break;
           tc_fence_after();
@@ -1271,14 +1307,14 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
       // the second group hands its sums to the first
       float* mine = s_sum + t * BLOCK + quarter * 32 + lane;
       if (group == 1) {
-        ok = wait_warp(x_free + 8 * t, (n_x & 1) ^ 1, abort_flag);
+        ok = wait_warp(x_free + 8 * t, (n_x & 1) ^ 1, flags);
         ++n_x;
         if (!ok) break;
         *mine = w;
         mbar_arrive(x_full + 8 * t);
         continue;
       }
-      ok = wait_warp(x_full + 8 * t, n_x & 1, abort_flag);
+      ok = wait_warp(x_full + 8 * t, n_x & 1, flags);
       ++n_x;
       if (!ok) break;
       w += *mine;
@@ -1315,7 +1351,7 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
 
   tc_fence_before();
   __syncthreads();
-  if (*abort_flag) {
+  if (flags[ABORT]) {
     if (threadIdx.x == 0) set_status(a.status, SPTS_ERR_TIMEOUT);
     const uint64_t t1 = globaltimer_ns();
     while (globaltimer_ns() - t1 < 200000ull) { }

@@ -119,6 +119,32 @@ def test_pools_beyond_32_bit_offsets():
             assert torch.equal(got, want)
 
 
+def test_values_not_seen_at_the_end_of_very_long_caches():
+    """160 sequences share 524,288 rows, the last of which, not finite, only the last of their 16 queries see: what the others get takes longer
+    to compute again than a wait within the kernel may last without a sign of life."""
+    shape = shape_of(8, 1, 128)
+    from test_gpu_paged import context
+    lib = context(shape)
+    n_seq, n, held, page = 160, 16, 524288, 256
+    g = torch.Generator().manual_seed(7)
+    k, v = (torch.randn(held // page, page, 1, 128, generator=g).bfloat16().to("cuda") for _ in range(2))
+    k.view(held, 128)[-1] = float("inf")
+    v.view(held, 128)[-1] = float("nan")
+    table = torch.arange(held // page, dtype=torch.int32, device="cuda").repeat(n_seq, 1)
+    length = torch.full((n_seq,), held, dtype=torch.int32, device="cuda")
+    c = binding.PagedKv(shape, table, page_size=page, k=k, v=v, length=length)
+    q, start = R.queries(shape, [n] * n_seq, seed=7)
+    out, lse = lib.paged_attention(c, q, row_start=start, want_lse=True)
+    assert lib.device_status() == 0
+    for b in (0, 77, 159):
+        r = slice(n * b, n * b + n - 1)
+        o, e, l, el = R.attention(q[r], k.view(held, 1, 128)[:held - 1], v.view(held, 1, 128)[:held - 1], held - n, torch.bfloat16)
+        near(out[r].view(n - 1, 8, 128), o, e)
+        near(lse[r], l, el)
+    out = out.view(n_seq, n, 8, 128)
+    assert bool(torch.isfinite(out[:, :-1]).all()) and bool(torch.isnan(out[:, -1]).all())
+
+
 def test_two_contexts_on_two_streams():
     """Each has its workspace: calls that run at the same time do not meet."""
     shape = shape_of(8, 2, 128)
