@@ -205,20 +205,25 @@ __device__ __forceinline__ void join_cluster(cg::cluster_group& cluster, const P
 constexpr int PAD = 4;                         // floats between rows in shared memory: neighbouring rows in neighbouring banks
 template <int D> constexpr int tile_floats() { return TILE * (D + PAD); }
 
-// Rows [j0, j0 + TILE) of K or V of one KV head into shared memory, zeros from row `end` on and where the table names no page.
-template <typename T, int D>
-__device__ __forceinline__ void load_rows(const PlainArgs& a, const T* __restrict__ x, int b, int kvh, int j0, int end, float* to) {
+// Rows [j0, j0 + TILE) of K (and V) of one KV head into shared memory, zeros from row `end` on and where the table names no page.
+template <typename T, int D, bool BOTH>
+__device__ __forceinline__ void load_rows(const PlainArgs& a, int b, int kvh, int j0, int end, float* to_k, float* to_v) {
   constexpr int PER = D / 4;
 #pragma unroll 4
   for (int i = threadIdx.x; i < TILE * PER; i += PL_THREADS) {
     const int r = i / PER, e = (i % PER) * 4, j = j0 + r;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
     if (j < end) {
       const int64_t slot = slot_of(a.c, b, j);
-      if (slot >= 0) v = load4(x + (slot * a.Hkv + kvh) * D + e);
-      else set_status(a.status, SPTS_ERR_INDEX);
+      if (slot >= 0) {
+        k = load4((const T*)a.c.k + (slot * a.Hkv + kvh) * D + e);
+        if (BOTH) v = load4((const T*)a.c.v + (slot * a.Hkv + kvh) * D + e);
+      } else {
+        set_status(a.status, SPTS_ERR_INDEX);
+      }
     }
-    *reinterpret_cast<float4*>(to + r * (D + PAD) + e) = v;
+    *reinterpret_cast<float4*>(to_k + r * (D + PAD) + e) = k;
+    if (BOTH) *reinterpret_cast<float4*>(to_v + r * (D + PAD) + e) = v;
   }
 }
 // Rows of queries [r0, r0 + TILE), zeros behind the last, times `scale`.
@@ -255,6 +260,33 @@ __device__ __forceinline__ void tile_scores(const float* sq, const float* sk, in
   }
 }
 
+// Adds the weights [TILE][TILE + PAD] of rows 4 tq .. + 3 times V to their dims 64 p + 4 tk .. + 3.
+template <int D, bool PASS_ZEROS>
+__device__ __forceinline__ void tile_pv(const float* sp, const float* sv, int tq, int tk, float4 (&acc)[4][D / 64]) {
+#pragma unroll 2
+  for (int k = 0; k < TILE; k += 4) {
+    float4 w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float4*>(sp + (4 * tq + i) * (TILE + PAD) + k);
+#pragma unroll
+    for (int p = 0; p < D / 64; ++p) {
+      float4 v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const float4*>(sv + (k + u) * (D + PAD) + 64 * p + 4 * tk);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float ws[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (!PASS_ZEROS || ws[u] != 0.f) {
+            acc[i][p].x = fmaf(ws[u], v[u].x, acc[i][p].x); acc[i][p].y = fmaf(ws[u], v[u].y, acc[i][p].y);
+            acc[i][p].z = fmaf(ws[u], v[u].z, acc[i][p].z); acc[i][p].w = fmaf(ws[u], v[u].w, acc[i][p].w);
+          }
+      }
+    }
+  }
+}
+
 template <int D> constexpr int attn_tile_smem() { return 3 * tile_floats<D>() * 4; }
 
 // A cluster to (tile of 64 rows of queries, KV head).  A thread has 4 x 4 scores, then 4 rows x D / 16 dims of O; sixteen neighbouring threads
@@ -263,7 +295,7 @@ template <int D> constexpr int attn_tile_smem() { return 3 * tile_floats<D>() * 
 template <typename T, int D>
 __global__ void __launch_bounds__(PL_THREADS, 2)
 paged_attn_tile_kernel(const __grid_constant__ PlainArgs a) {
-  constexpr int LD = D + PAD, PIECES = D / 64, LP = TILE + PAD;
+  constexpr int PIECES = D / 64, LP = TILE + PAD;
   extern __shared__ __align__(16) float smem_f[];
   float* sq = smem_f;
   float* sk = sq + tile_floats<D>();
@@ -299,8 +331,7 @@ paged_attn_tile_kernel(const __grid_constant__ PlainArgs a) {
     const int j0 = ch * TILE;
     const bool whole = j0 + TILE <= all;
     __syncthreads();
-    load_rows<T, D>(a, (const T*)a.c.k, t.b, kvh, j0, t.seen, sk);
-    load_rows<T, D>(a, (const T*)a.c.v, t.b, kvh, j0, t.seen, sv);
+    load_rows<T, D, true>(a, t.b, kvh, j0, t.seen, sk, sv);
     __syncthreads();
     float s[4][4];
     tile_scores<D>(sq, sk, tq, tk, s);
@@ -331,43 +362,8 @@ paged_attn_tile_kernel(const __grid_constant__ PlainArgs a) {
     }
     __syncthreads();
     // O += P V; where a query does not see all of the rows, those of weight zero are passed over, whatever V holds
-    if (whole) {
-#pragma unroll 2
-      for (int k = 0; k < TILE; k += 4) {
-        float4 w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float4*>(sp + (4 * tq + i) * LP + k);
-#pragma unroll
-        for (int p = 0; p < PIECES; ++p) {
-          float4 v[4];
-#pragma unroll
-          for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const float4*>(sv + (k + u) * LD + 64 * p + 4 * tk);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float ws[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              acc[i][p].x = fmaf(ws[u], v[u].x, acc[i][p].x); acc[i][p].y = fmaf(ws[u], v[u].y, acc[i][p].y);
-              acc[i][p].z = fmaf(ws[u], v[u].z, acc[i][p].z); acc[i][p].w = fmaf(ws[u], v[u].w, acc[i][p].w);
-            }
-          }
-        }
-      }
-    } else {
-      for (int k = 0; k < TILE; ++k) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float w = sp[(4 * tq + i) * LP + k];
-          if (w == 0.f) continue;
-#pragma unroll
-          for (int p = 0; p < PIECES; ++p) {
-            const float4 v = *reinterpret_cast<const float4*>(sv + k * LD + 64 * p + 4 * tk);
-            acc[i][p].x = fmaf(w, v.x, acc[i][p].x); acc[i][p].y = fmaf(w, v.y, acc[i][p].y);
-            acc[i][p].z = fmaf(w, v.z, acc[i][p].z); acc[i][p].w = fmaf(w, v.w, acc[i][p].w);
-          }
-        }
-      }
-    }
+    if (whole) tile_pv<D, false>(sp, sv, tq, tk, acc);
+    else tile_pv<D, true>(sp, sv, tq, tk, acc);
   }
   __syncthreads();
 #pragma unroll
@@ -437,7 +433,7 @@ paged_weights_tile_kernel(const __grid_constant__ PlainArgs a) {
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
     for (int kvh = rank; kvh < a.Hkv && from < rows; kvh += split) {
       __syncthreads();
-      load_rows<T, D>(a, (const T*)a.c.k, b, kvh, j0, held, sk);
+      load_rows<T, D, false>(a, b, kvh, j0, held, sk, nullptr);
       for (int64_t r0 = from; r0 < rows; r0 += TILE) {
         __syncthreads();
         load_queries<T, D>(a, first, r0, rows, kvh, LOG2E * rsqrtf((float)D), sq);
