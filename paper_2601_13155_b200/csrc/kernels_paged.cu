@@ -226,17 +226,27 @@ __device__ __forceinline__ void load_rows(const PlainArgs& a, int b, int kvh, in
     if (BOTH) *reinterpret_cast<float4*>(to_v + r * (D + PAD) + e) = v;
   }
 }
-// Rows of queries [r0, r0 + TILE), zeros behind the last, times `scale`.
+// Rows of queries [r0, r0 + TILE), zeros behind the last: into registers, and from there, times `scale`, into shared memory.
+template <int D> constexpr int query_pieces() { return TILE * D / 4 / PL_THREADS; }
 template <typename T, int D>
-__device__ __forceinline__ void load_queries(const PlainArgs& a, int64_t first, int64_t r0, int64_t rows, int kvh, float scale, float* to) {
+__device__ __forceinline__ void fetch_queries(const PlainArgs& a, int64_t first, int64_t r0, int64_t rows, int kvh, float4 (&v)[query_pieces<D>()]) {
   constexpr int PER = D / 4;
   const int G = a.H / a.Hkv;
-  for (int i = threadIdx.x; i < TILE * PER; i += PL_THREADS) {
-    const int r = i / PER, e = (i % PER) * 4;
-    const int64_t q = r0 + r;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (q < rows) v = load4((const T*)a.Q + (first + q / G) * a.ldq + (int64_t)(kvh * G + q % G) * D + e);
-    *reinterpret_cast<float4*>(to + r * (D + PAD) + e) = make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale);
+#pragma unroll
+  for (int u = 0; u < query_pieces<D>(); ++u) {
+    const int i = threadIdx.x + u * PL_THREADS, e = (i % PER) * 4;
+    const int64_t q = r0 + i / PER;
+    v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (q < rows) v[u] = load4((const T*)a.Q + (first + q / G) * a.ldq + (int64_t)(kvh * G + q % G) * D + e);
+  }
+}
+template <int D>
+__device__ __forceinline__ void store_queries(const float4 (&v)[query_pieces<D>()], float scale, float* to) {
+  constexpr int PER = D / 4;
+#pragma unroll
+  for (int u = 0; u < query_pieces<D>(); ++u) {
+    const int i = threadIdx.x + u * PL_THREADS;
+    *reinterpret_cast<float4*>(to + i / PER * (D + PAD) + (i % PER) * 4) = make_float4(v[u].x * scale, v[u].y * scale, v[u].z * scale, v[u].w * scale);
   }
 }
 // Products of rows 4 tq .. + 3 of queries and rows tk + 16 k of the cache.
@@ -291,7 +301,7 @@ template <int D> constexpr int attn_tile_smem() { return 3 * tile_floats<D>() * 
 
 // A cluster to (tile of 64 rows of queries, KV head).  A thread has 4 x 4 scores, then 4 rows x D / 16 dims of O; sixteen neighbouring threads
 // share the rows, whose maxima and sums stay in registers.  The weights take K's place in shared memory.  fp32 storage, 32 heads of 128 dims:
-// 1024 tokens over 4096 rows 2.2 ms (27 TFLOP/s; with 32 x 64 to a block and 8 scores to a thread 3.7), four chunks of 64 tokens 230 us.
+// 1024 tokens over 4096 rows 1.9 ms (32 TFLOP/s; with 32 x 64 to a block and 8 scores to a thread 3.7), four chunks of 64 tokens 183 us.
 template <typename T, int D>
 __global__ void __launch_bounds__(PL_THREADS, 2)
 paged_attn_tile_kernel(const __grid_constant__ PlainArgs a) {
@@ -308,7 +318,11 @@ paged_attn_tile_kernel(const __grid_constant__ PlainArgs a) {
   const int G = a.H / a.Hkv, kvh = blockIdx.y, tid = threadIdx.x, tq = tid >> 4, tk = tid & 15;
   QueryTile t;
   if (!find_tile<TILE>(a, blockIdx.x / split, kvh == 0 && blockIdx.x == 0, pre, sums, t)) return;
-  load_queries<T, D>(a, t.first, t.r0, t.rows, kvh, LOG2E * rsqrtf((float)D), sq);
+  {
+    float4 q[query_pieces<D>()];
+    fetch_queries<T, D>(a, t.first, t.r0, t.rows, kvh, q);
+    store_queries<D>(q, LOG2E * rsqrtf((float)D), sq);
+  }
   // rows of the cache that a query sees; those that all of the tile's see
   int limit[4];
 #pragma unroll
@@ -408,7 +422,8 @@ template <int D> constexpr int weights_tile_smem() { return (2 * tile_floats<D>(
 
 // Persistent clusters over (sequence, 64 rows of it); a CTA has every split-th KV head: its K in shared memory and the queries that see any
 // of the rows passing by.  A thread sums its queries' weights of four rows; the sixteen threads of a row meet at the end, in their order.
-// 1024 tokens over 4096 rows, 32 heads, fp32: 1.36 ms (22 TFLOP/s; with one CTA to 64 rows and 8 scores to a thread 5.2).
+// 1024 tokens over 4096 rows, 32 heads, fp32: 1.24 ms (24 TFLOP/s; with queries fetched as they are needed 1.36, with one CTA to 64 rows and 8
+// scores to a thread 5.2).
 template <typename T, int D>
 __global__ void __launch_bounds__(PL_THREADS, 2)
 paged_weights_tile_kernel(const __grid_constant__ PlainArgs a) {
@@ -434,15 +449,20 @@ paged_weights_tile_kernel(const __grid_constant__ PlainArgs a) {
     for (int kvh = rank; kvh < a.Hkv && from < rows; kvh += split) {
       __syncthreads();
       load_rows<T, D, false>(a, b, kvh, j0, held, sk, nullptr);
+      float4 q[query_pieces<D>()];             // the next tile of queries, on its way
+      float e = 0.f;
+      const auto fetch = [&](int64_t r0) {
+        fetch_queries<T, D>(a, first, r0, rows, kvh, q);
+        const int64_t r = r0 + tid;
+        if (tid < TILE) e = r < rows ? a.lse[(first + r / G) * a.H + kvh * G + (int)(r % G)] * LOG2E : 0.f;
+      };
+      fetch(from);
       for (int64_t r0 = from; r0 < rows; r0 += TILE) {
         __syncthreads();
-        load_queries<T, D>(a, first, r0, rows, kvh, LOG2E * rsqrtf((float)D), sq);
-        if (tid < TILE) {
-          const int64_t r = r0 + tid;
-          const float e = r < rows ? a.lse[(first + r / G) * a.H + kvh * G + (int)(r % G)] * LOG2E : 0.f;
-          slse[tid] = e == -INFINITY ? 0.f : e;          // (such a query sees nothing)
-        }
+        store_queries<D>(q, LOG2E * rsqrtf((float)D), sq);
+        if (tid < TILE) slse[tid] = e == -INFINITY ? 0.f : e;      // (such a query sees nothing)
         __syncthreads();
+        if (r0 + TILE < rows) fetch(r0 + TILE);
         float s[4][4];
         tile_scores<D>(sq, sk, tq, tk, s);
         const bool whole = r0 + TILE <= rows && j0 + TILE <= off + (int)(r0 / G) + 1;
@@ -450,10 +470,10 @@ paged_weights_tile_kernel(const __grid_constant__ PlainArgs a) {
         for (int i = 0; i < 4; ++i) {
           const int64_t r = r0 + 4 * tq + i;
           const int limit = whole ? INT_MAX : r < rows ? off + (int)(r / G) + 1 : 0;
-          const float e = slse[4 * tq + i];
+          const float base = slse[4 * tq + i];
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            if (j0 + tk + 16 * k < limit) sum[k] += exp2f(s[i][k] - e);
+            if (j0 + tk + 16 * k < limit) sum[k] += exp2f(s[i][k] - base);
         }
       }
     }
@@ -1035,8 +1055,9 @@ spts_status launch_clusters(spts_ctx* ctx, void (*kernel)(PlainArgs), dim3 grid,
   ctx->launches++;
   return SPTS_OK;
 }
-// CTAs that share a block of work: as many as make eight blocks to an SM, a power of two.  (32 single tokens over 4096 rows with two, four and eight
-// to an SM: attention 175, 128, 123 us, weights 88, 93, 101; four chunks of 64: 316, 229, 228 and 140, 112, 106.)
+// CTAs that share a block of work: as many as make eight blocks to an SM, a power of two.  (When this was chosen, 32 single tokens over 4096
+// rows with two, four and eight to an SM: attention 175, 128, 123 us, weights 88, 93, 101; four chunks of
+// 64: 316, 229, 228 and 140, 112, 106.)
 int share_of(const spts_ctx* ctx, int64_t blocks, int most) {
   int split = 1;
   while (2 * split <= most && blocks * split < 8 * ctx->sm_count) split *= 2;
