@@ -769,6 +769,7 @@ evict_rank_kernel(EvictArgs a) {
   __shared__ __align__(16) uint32_t hist[3][BINS];
   __shared__ long long newest_here, newest_all;
   __shared__ int ties_here, warp_n[RANK_THREADS / 32][3], s_need;
+  __shared__ bool s_all;
   __shared__ uint32_t s_digit;
   cg::cluster_group cluster = cg::this_cluster();
   const int split = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -854,21 +855,28 @@ evict_rank_kernel(EvictArgs a) {
       for (int r = 0; r < EVICT_SPLIT; ++r) { bin.x += from[r].x; bin.y += from[r].y; }
     }
     const int above = block_above((int)(bin.x + bin.y), warp_n);
-    if (above < need && above + (int)bin.y >= need) { s_digit = BINS - 1 - 2 * tid; s_need = need - above; }
-    else if (above + (int)bin.y < need && above + (int)(bin.x + bin.y) >= need) { s_digit = BINS - 2 - 2 * tid; s_need = need - above - (int)bin.y; }
+    const int upper = above + (int)bin.y, both = upper + (int)bin.x;
+    if (above < need && upper >= need) { s_digit = BINS - 1 - 2 * tid; s_need = need - above; s_all = upper == need; }
+    else if (upper < need && both >= need) { s_digit = BINS - 2 - 2 * tid; s_need = need - upper; s_all = both == need; }
     __syncthreads();
     prefix = (prefix << (d == 2 ? 10 : 11)) | s_digit;
     need = s_need;
+    const bool all = s_all;
     __syncthreads();
+    if (all) {                                 // all rows with these digits stay: the others do not matter
+      prefix <<= shift;
+      need = INT_MAX;
+      break;
+    }
   }
   // ---- a warp has part / 32 neighbouring rows from here on
   const bool cut = keep > 0;                   // (keep == 0: no row stays)
   const int per_warp = part / (RANK_THREADS / 32), w0 = warp * per_warp, w1 = min(n, w0 + per_warp);
-  // rows that have just this key: how many lie in the parts and warps before
+  // rows that have just this key, where not all of them stay: how many lie in the parts and warps before
   int ties = 0;
-  {
+  if (cut && need != INT_MAX) {
     int mine = 0;
-    for (int i = w0 + lane; i < w1; i += 32) mine += cut && key_at(i) == prefix;
+    for (int i = w0 + lane; i < w1; i += 32) mine += key_at(i) == prefix;
     mine = __reduce_add_sync(0xffffffffu, mine);
     if (lane == 0 && mine) atomicAdd(&ties_here, mine);
     if (lane == 0) warp_n[warp][0] = mine;
