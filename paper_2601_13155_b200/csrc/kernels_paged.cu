@@ -714,6 +714,9 @@ paged_weights_row_kernel(const __grid_constant__ PlainArgs a) {
 // ------------------------------------------------------------------------------------------------ eviction
 constexpr int RANK_THREADS = 1024;
 constexpr int RANK_KEYS = 24576;               // rows of a CTA whose keys and positions fit shared memory
+// Rows that go up to which the ranking kernel moves those that stay.  (48 sequences of 4096 rows and n more, ranked and moved by the second
+// kernel 29.6 us, by the first for n = 1, 16, 32: 22.2, 22.8, 23.6; one of 32768: 29.5 and 23.7, 25.8, 27.7.)
+constexpr int RANK_MOVES = 32;
 constexpr int MOVE_THREADS = 512;
 
 // Order of the rows of a sequence: the larger key stays.  Rows that stay before all others have the largest one, NaN the smallest.
@@ -729,6 +732,7 @@ struct EvictArgs {
   int n_sink, n_recent;
   int first_seq;                               // of this launch
   int words;                                   // of evict_bits for each sequence
+  int row_bytes;                               // of K, of V
   uint32_t* bits; int2* before; int2* total;
   int* arrived;                                // blocks of the moves that are done, zero between calls
   int* status;
@@ -739,7 +743,8 @@ struct EvictArgs {
 // two bins, the CTAs' bins all on their way at once); of the rows that have just this key the first ones stay.  What comes out is a bit for
 // each row, and the numbers of holes (rows among the first keep that go) and movers (rows behind them that stay) before each chunk of 256
 // rows, from which evict_move_kernel finds its copies.  Parts too long for shared memory (capacities beyond 196,608 rows) read their weights again for every
-// digit.  Bound by the chain of barriers and round trips (with the moves 31 us for 32768 rows, 26 for 48 sequences of 4111 and less).
+// digit.  Where no more than RANK_MOVES rows go, as of a sequence that is held at its budget, no more move, and the first CTA moves them.
+// Bound by the chain of barriers and round trips (with the moves 28 us for 32768 rows of which 4096 stay, 20 for 48 sequences of 4111 and less).
 constexpr int BINS = 2 * RANK_THREADS;
 static_assert(BINS == 2048, "two bins of a digit of eleven bits to a thread");
 
@@ -770,6 +775,9 @@ evict_rank_kernel(EvictArgs a) {
   __shared__ long long newest_here, newest_all;
   __shared__ int ties_here, warp_n[RANK_THREADS / 32][3], s_need;
   __shared__ bool s_all;
+  __shared__ int2 s_part;
+  __shared__ int s_src[RANK_MOVES], s_dst[RANK_MOVES];
+  __shared__ int64_t s_from[RANK_MOVES], s_to[RANK_MOVES];
   __shared__ uint32_t s_digit;
   cg::cluster_group cluster = cg::this_cluster();
   const int split = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -780,10 +788,12 @@ evict_rank_kernel(EvictArgs a) {
   dep_wait();
   const int held = held_rows(c, b), keep = a.keep[b];
   if (keep < 0 || held <= keep) return;        // (the same for all CTAs of a cluster)
+  const bool few = held - keep <= RANK_MOVES;  // no more rows move than go: the first CTA moves them itself
   const int part = part_rows(held, split);
   const int j0 = (int)min((int64_t)held, (int64_t)rank * part), n = min(part, held - j0);
   uint32_t* spos = keys + part;
   if (tid == 0) { newest_here = LLONG_MIN; ties_here = 0; }
+  if (tid < RANK_MOVES) { s_src[tid] = -1; s_dst[tid] = -1; }
   __syncthreads();
   const bool by_pos = a.n_sink > 0 || a.n_recent > 0;
   // the rows' weights and positions, and the largest position that the sequence holds
@@ -908,26 +918,72 @@ evict_rank_kernel(EvictArgs a) {
   const int warp_holes = warp_n[lane][1], warp_movers = warp_n[lane][2];
   holes = __reduce_add_sync(0xffffffffu, lane < warp ? warp_holes : 0);
   movers = __reduce_add_sync(0xffffffffu, lane < warp ? warp_movers : 0);
+  const int2 whole = make_int2(__reduce_add_sync(0xffffffffu, warp_holes), __reduce_add_sync(0xffffffffu, warp_movers));
+  int* to_src = s_src;
+  int* to_dst = s_dst;
+  if (few && split > 1) {
+    // the first CTA's lists, and the numbers of the parts before
+    to_src = cluster.map_shared_rank(s_src, 0);
+    to_dst = cluster.map_shared_rank(s_dst, 0);
+    if (tid == 0) s_part = whole;
+    cluster.sync();
+    const int2 other = lane < rank ? *cluster.map_shared_rank(&s_part, lane) : make_int2(0, 0);
+    holes += __reduce_add_sync(0xffffffffu, other.x);
+    movers += __reduce_add_sync(0xffffffffu, other.y);
+  }
   __syncwarp();
   for (int i0 = w0; i0 < w1; i0 += 32) {
     const int j = j0 + i0;
     const uint32_t bits = SMEM ? keys[w0 + (i0 - w0) / 32] : a.bits[word0 + (j >> 5)], there = w1 - i0 >= 32 ? 0xFFFFFFFFu : (1u << (w1 - i0)) - 1;
     const uint32_t front = j + 32 <= keep ? 0xFFFFFFFFu : j >= keep ? 0u : (1u << (keep - j)) - 1;       // rows below keep
-    if (lane == 0 && j % EVICT_CHUNK == 0) a.before[(word0 >> 3) + j / EVICT_CHUNK] = make_int2(holes, movers);
-    holes += __popc(~bits & there & front);
-    movers += __popc(bits & ~front);
+    const uint32_t hole = ~bits & there & front, mover = bits & ~front;
+    if (few) {
+      const uint32_t below = (1u << lane) - 1;
+      const int to_hole = holes + __popc(hole & below), to_mover = movers + __popc(mover & below);
+      if ((hole >> lane & 1) && to_hole < RANK_MOVES) to_dst[to_hole] = j + lane;
+      if ((mover >> lane & 1) && to_mover < RANK_MOVES) to_src[to_mover] = j + lane;
+    } else if (lane == 0 && j % EVICT_CHUNK == 0) {
+      a.before[(word0 >> 3) + j / EVICT_CHUNK] = make_int2(holes, movers);
+    }
+    holes += __popc(hole);
+    movers += __popc(mover);
   }
-  holes = __reduce_add_sync(0xffffffffu, warp_holes);
-  movers = __reduce_add_sync(0xffffffffu, warp_movers);
-  if (tid == 0) a.total[local * EVICT_SPLIT + rank] = make_int2(holes, movers);
-  cluster.sync();                              // the histograms are read by other CTAs of the cluster until here
+  if (tid == 0 && !few) a.total[local * EVICT_SPLIT + rank] = whole;
+  cluster.sync();                              // other CTAs of the cluster read the histograms and write the lists until here
+  if (!few || rank > 0) return;
+  if (tid < 2 * RANK_MOVES) {
+    const int r = tid % RANK_MOVES, src = s_src[r], dst = s_dst[r];
+    const bool there = src >= 0 && dst >= 0;
+    (tid < RANK_MOVES ? s_from : s_to)[r] = there ? slot_of(c, b, tid < RANK_MOVES ? src : dst) : -1;
+  }
+  __syncthreads();
+  const int pieces = a.row_bytes >> 4, n_moves = min(held - keep, RANK_MOVES);
+  for (int u0 = tid; u0 < 2 * n_moves * pieces; u0 += 4 * RANK_THREADS) {
+    uint4 x[4];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const int u = u0 + v * RANK_THREADS, r = u / pieces;
+      if (r < 2 * n_moves && s_from[r >> 1] >= 0)
+        x[v] = reinterpret_cast<const uint4*>(((r & 1) ? c.v : c.k) + s_from[r >> 1] * a.row_bytes)[u - r * pieces];
+    }
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const int u = u0 + v * RANK_THREADS, r = u / pieces;
+      if (r < 2 * n_moves && s_from[r >> 1] >= 0 && s_to[r >> 1] >= 0)
+        reinterpret_cast<uint4*>(const_cast<char*>((r & 1) ? c.v : c.k) + s_to[r >> 1] * a.row_bytes)[u - r * pieces] = x[v];
+    }
+  }
+  if (tid < n_moves && s_from[tid] >= 0 && s_to[tid] >= 0) {
+    c.weight[s_to[tid]] = c.weight[s_from[tid]];
+    if (c.pos != nullptr) c.pos[s_to[tid]] = c.pos[s_from[tid]];
+  }
 }
 
 // Persistent CTAs over groups of sixteen movers: mover r of a sequence and its hole r are found by the numbers of movers and holes before
 // each chunk (in shared memory), and all pieces of their rows are copied side by side.  Movers lie behind the rows that stay in place and
 // holes among them, so no row is both read and written.  The block that is done last sets the lengths, which the others read.  Launched as a
-// dependent of the ranking.  Sixteen movers to a group spread even few of them over the SMs: with whole chunks of 256 rows to a CTA the two
-// kernels took 46 us for 32768 rows of which 4096 stay, now 31.
+// dependent of the ranking, which has moved the rows of sequences that give up 32 or fewer.  Sixteen movers to a group spread even few of them over the SMs: with whole chunks of 256 rows to a CTA the two
+// kernels took 46 us for 32768 rows of which 4096 stay, with groups 31.
 constexpr int MOVE_ROWS = 16;                  // movers of a group
 constexpr int MOVE_AT_ONCE = 8;                // pieces of a thread in flight
 constexpr int MOVE_CHUNKS = 4096;              // chunks of a sequence whose numbers fit shared memory (beyond 1,048,576 rows they are read where they lie)
@@ -952,7 +1008,7 @@ __device__ __forceinline__ int nth_row(const uint32_t* bits, bool set, int chunk
 }
 
 __global__ void __launch_bounds__(MOVE_THREADS, 2)
-evict_move_kernel(EvictArgs a, int n_seq, int split, int row_bytes) {
+evict_move_kernel(EvictArgs a, int n_seq, int split) {
   __shared__ long long pre[PREFIX_MAX + 1], sums[32];
   __shared__ int64_t src[MOVE_ROWS], dst[MOVE_ROWS];       // places of the rows
   __shared__ int2 before[MOVE_CHUNKS];
@@ -962,7 +1018,7 @@ evict_move_kernel(EvictArgs a, int n_seq, int split, int row_bytes) {
   dep_wait();
   block_prefix<MOVE_THREADS>(n_seq, pre, sums, [&](int l) {
     const int held = held_rows(c, a.first_seq + l), keep = a.keep[a.first_seq + l];
-    if (keep < 0 || held <= keep) return 0LL;
+    if (keep < 0 || held - RANK_MOVES <= keep) return 0LL;
     int movers = 0;
 #pragma unroll
     for (int s = 0; s < EVICT_SPLIT; ++s) movers += s < split ? __ldcg(&a.total[l * EVICT_SPLIT + s].y) : 0;
@@ -1012,7 +1068,7 @@ evict_move_kernel(EvictArgs a, int n_seq, int split, int row_bytes) {
     }
     __syncthreads();
     // all rows' pieces of 16 bytes one after the other, K and V of a row in turn
-    const int pieces = row_bytes >> 4, total = 2 * n * pieces;
+    const int row_bytes = a.row_bytes, pieces = row_bytes >> 4, total = 2 * n * pieces;
     for (int u0 = tid; u0 < total; u0 += MOVE_AT_ONCE * MOVE_THREADS) {
       uint4 x[MOVE_AT_ONCE];
 #pragma unroll
@@ -1034,13 +1090,17 @@ evict_move_kernel(EvictArgs a, int n_seq, int split, int row_bytes) {
     }
     __syncthreads();
   }
-  if (tid == 0) {
-    __threadfence();
-    last = atomicAdd(a.arrived, 1) == (int)gridDim.x - 1;
+  if (items > 0) {
+    if (tid == 0) {
+      __threadfence();
+      last = atomicAdd(a.arrived, 1) == (int)gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    if (tid == 0) *a.arrived = 0;
+  } else if (blockIdx.x > 0) {
+    return;                                    // (nothing moves, whatever length the others read)
   }
-  __syncthreads();
-  if (!last) return;
-  if (tid == 0) *a.arrived = 0;
   for (int l = tid; l < n_seq; l += MOVE_THREADS) {
     const int keep = a.keep[a.first_seq + l];
     if (keep >= 0 && held_rows(c, a.first_seq + l) > keep) c.len[a.first_seq + l] = keep;
@@ -1148,7 +1208,7 @@ spts_status launch_paged_evict(spts_ctx* ctx, const spts_paged_kv* cache, const 
   const int es = ctx->desc.dtype == SPTS_BF16 ? 2 : 4, row_bytes = ctx->desc.n_kv_heads * ctx->desc.head_dim * es;
   const int capacity = cache->max_pages * cache->page_size;
   EvictArgs a;
-  a.c = make_cache(cache); a.keep = keep; a.n_sink = n_sink; a.n_recent = n_recent;
+  a.c = make_cache(cache); a.keep = keep; a.n_sink = n_sink; a.n_recent = n_recent; a.row_bytes = row_bytes;
   a.words = (int)align_up((size_t)capacity, EVICT_CHUNK) / 32;
   a.bits = ctx->ws.evict_bits; a.before = ctx->ws.evict_before; a.total = ctx->ws.evict_total; a.status = ctx->ws.status;
   a.arrived = ctx->ws.paged_arrived + 1;
@@ -1175,7 +1235,7 @@ spts_status launch_paged_evict(spts_ctx* ctx, const spts_paged_kv* cache, const 
     ctx->launches++;
     const int64_t items = (int64_t)n * a.words * 32 / (2 * MOVE_ROWS);         // no fewer than there are: at most half of the rows move
     const int move = (int)(items < 2 * ctx->sm_count ? items : 2 * ctx->sm_count);
-    if (launch_dependent(evict_move_kernel, dim3(move), dim3(MOVE_THREADS), ctx->stream, a, n, split, row_bytes) != cudaSuccess) return SPTS_ERR_CUDA;
+    if (launch_dependent(evict_move_kernel, dim3(move), dim3(MOVE_THREADS), ctx->stream, a, n, split) != cudaSuccess) return SPTS_ERR_CUDA;
     ctx->launches++;
   }
   return SPTS_OK;

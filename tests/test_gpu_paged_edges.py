@@ -5,7 +5,7 @@ import torch
 
 import paged_ref as R
 from paper_2601_13155_b200 import binding
-from test_gpu_paged import check_attention, check_evict, near, shape_of
+from test_gpu_paged import check_attention, check_evict, context, near, shape_of
 
 pytestmark = pytest.mark.gpu
 
@@ -201,3 +201,13 @@ def test_evictions_budget_of_nothing_and_everything():
     shape = shape_of(2, 1, 64)
     from test_gpu_paged import context
     check_evict(R.Pages(shape, [5000, 4097, 1], 64, seed=60), context(shape), [0, 4096, 1], 0, 0)
+
+
+@pytest.mark.parametrize("n_sink,n_recent", [(0, 0), (4, 64)])
+@pytest.mark.parametrize("longest", [700, 9000, 200000])
+def test_evictions_of_the_few_rows_that_a_step_brought(longest, n_sink, n_recent):
+    """Up to 32 rows go, or just more: of sequences of one block, of a cluster of blocks and beyond shared memory."""
+    shape = shape_of(2, 1, 64)
+    lens = [longest, longest - 1, longest - 300, 400, 400, 33, 32, 1, 260]
+    gone = [1, 32, 33, 31, 32, 33, 32, 1, 7]
+    check_evict(R.Pages(shape, lens, 64, seed=longest), context(shape), [held - x for held, x in zip(lens, gone)], n_sink, n_recent)
