@@ -982,8 +982,8 @@ evict_rank_kernel(EvictArgs a) {
 // Persistent CTAs over groups of sixteen movers: mover r of a sequence and its hole r are found by the numbers of movers and holes before
 // each chunk (in shared memory), and all pieces of their rows are copied side by side.  Movers lie behind the rows that stay in place and
 // holes among them, so no row is both read and written.  The block that is done last sets the lengths, which the others read.  Launched as a
-// dependent of the ranking, which has moved the rows of sequences that give up 32 or fewer.  Sixteen movers to a group spread even few of them over the SMs: with whole chunks of 256 rows to a CTA the two
-// kernels took 46 us for 32768 rows of which 4096 stay, with groups 31.
+// dependent of the ranking, which has moved the rows of sequences that give up 32 or fewer.  Sixteen movers to a group spread even few of
+// them over the SMs: with whole chunks of 256 rows to a CTA the two kernels took 46 us for 32768 rows of which 4096 stay, with groups 31.
 constexpr int MOVE_ROWS = 16;                  // movers of a group
 constexpr int MOVE_AT_ONCE = 8;                // pieces of a thread in flight
 constexpr int MOVE_CHUNKS = 4096;              // chunks of a sequence whose numbers fit shared memory (beyond 1,048,576 rows they are read where they lie)

@@ -444,9 +444,10 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, int unit_row, int h,
 
 // ------------------------------------------------------------------------------------------------ the kernel
 // Long chunks are bound by the instructions of the softmax warps beside the matrix products (2048 tokens over 34816 rows, 32 heads of 128 dims:
-// 0.96 ms, 1175 TFLOP/s; 16384 fresh ones 1279; with a quarter of the exponentials as polynomials of degree five 7 % slower), decode steps by memory (64 sequences of up to 16384 rows: 5.7 to 6.1 TB/s; 48 of up
-// to nine drafted tokens 127 us, 5.1 TB/s), single short ones by their chain of latencies (777 rows: 11.8 us).  Sixteen softmax warps instead of
-// eight were slower (64 single tokens 188 us against 147; 2048 tokens 1064 against 964).
+// 0.96 ms, 1175 TFLOP/s; 16384 fresh ones 1279; with a quarter of the exponentials as polynomials of degree five 7 % slower), decode steps by
+// memory (64 sequences of up to 16384 rows: 5.7 to 6.1 TB/s; 48 of up to nine drafted tokens 127 us, 5.1 TB/s), single short ones by their chain of
+// latencies (777 rows: 11.8 us).  Sixteen softmax warps instead of eight were slower (64 single tokens 188 us against 147; 2048 tokens 1064
+// against 964).
 struct Start { Walk walk; long long total; };      // a CTA's piece, the line's length
 
 template <int D>
