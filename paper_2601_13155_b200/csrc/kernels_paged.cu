@@ -401,7 +401,7 @@ __device__ __forceinline__ long long blocks_of_rows(const PlainArgs& a, bool che
   __syncthreads();
   return pre[a.c.n_seq];
 }
-// The sums [rows] of the CTAs of a cluster, which had different KV heads, are added in their order and become weights.
+// The sums [rows] of the CTAs of a cluster, which had different heads or queries, are added in their order and become weights.
 __device__ __forceinline__ void write_weights(cg::cluster_group& cluster, const PlainArgs& a, int b, int held, int j0, int rows, float* sum) {
   const int split = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   cluster.sync();
@@ -420,8 +420,8 @@ __device__ __forceinline__ void write_weights(cg::cluster_group& cluster, const 
 
 template <int D> constexpr int weights_tile_smem() { return (2 * tile_floats<D>() + 16 * TILE) * 4; }
 
-// Persistent clusters over (sequence, 64 rows of it); a CTA has every split-th KV head: its K in shared memory and the queries that see any
-// of the rows passing by.  A thread sums its queries' weights of four rows; the sixteen threads of a row meet at the end, in their order.
+// Persistent clusters over (sequence, 64 rows of it); a CTA has a part of the KV heads and tiles of queries that see any of the rows: a head's K in
+// shared memory, the queries passing by.  A thread sums its queries' weights of four rows; the sixteen threads of a row meet at the end, in their order.
 // 1024 tokens over 4096 rows, 32 heads, fp32: 1.24 ms (24 TFLOP/s; with queries fetched as they are needed 1.36, with one CTA to 64 rows and 8
 // scores to a thread 5.2).
 template <typename T, int D>
@@ -446,35 +446,40 @@ paged_weights_tile_kernel(const __grid_constant__ PlainArgs a) {
     // query i sees the first of these rows if off + i >= j0
     const int64_t from = (int64_t)max(0, j0 - off) * G / TILE * TILE;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int kvh = rank; kvh < a.Hkv && from < rows; kvh += split) {
+    // this CTA's part of the pairs (KV head, tile of queries), head by head
+    const int64_t tiles = rows > from ? (rows - from + TILE - 1) / TILE : 0, p1 = tiles * a.Hkv * (rank + 1) / split;
+    int64_t pair = tiles * a.Hkv * rank / split;
+    float4 q[query_pieces<D>()];               // the next tile of queries, on its way
+    float e = 0.f;
+    const auto fetch = [&](int64_t pair) {
+      const int kvh = (int)(pair / tiles);
+      const int64_t r0 = from + pair % tiles * TILE, r = r0 + tid;
+      fetch_queries<T, D>(a, first, r0, rows, kvh, q);
+      if (tid < TILE) e = r < rows ? a.lse[(first + r / G) * a.H + kvh * G + (int)(r % G)] * LOG2E : 0.f;
+    };
+    if (pair < p1) fetch(pair);
+    int in_k = -1;                             // the head whose K is in shared memory
+    for (; pair < p1; ++pair) {
+      const int kvh = (int)(pair / tiles);
+      const int64_t r0 = from + pair % tiles * TILE;
       __syncthreads();
-      load_rows<T, D, false>(a, b, kvh, j0, held, sk, nullptr);
-      float4 q[query_pieces<D>()];             // the next tile of queries, on its way
-      float e = 0.f;
-      const auto fetch = [&](int64_t r0) {
-        fetch_queries<T, D>(a, first, r0, rows, kvh, q);
-        const int64_t r = r0 + tid;
-        if (tid < TILE) e = r < rows ? a.lse[(first + r / G) * a.H + kvh * G + (int)(r % G)] * LOG2E : 0.f;
-      };
-      fetch(from);
-      for (int64_t r0 = from; r0 < rows; r0 += TILE) {
-        __syncthreads();
-        store_queries<D>(q, LOG2E * rsqrtf((float)D), sq);
-        if (tid < TILE) slse[tid] = e == -INFINITY ? 0.f : e;      // (such a query sees nothing)
-        __syncthreads();
-        if (r0 + TILE < rows) fetch(r0 + TILE);
-        float s[4][4];
-        tile_scores<D>(sq, sk, tq, tk, s);
-        const bool whole = r0 + TILE <= rows && j0 + TILE <= off + (int)(r0 / G) + 1;
+      if (kvh != in_k) load_rows<T, D, false>(a, b, kvh, j0, held, sk, nullptr);
+      in_k = kvh;
+      store_queries<D>(q, LOG2E * rsqrtf((float)D), sq);
+      if (tid < TILE) slse[tid] = e == -INFINITY ? 0.f : e;        // (such a query sees nothing)
+      __syncthreads();
+      if (pair + 1 < p1) fetch(pair + 1);
+      float s[4][4];
+      tile_scores<D>(sq, sk, tq, tk, s);
+      const bool whole = r0 + TILE <= rows && j0 + TILE <= off + (int)(r0 / G) + 1;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int64_t r = r0 + 4 * tq + i;
-          const int limit = whole ? INT_MAX : r < rows ? off + (int)(r / G) + 1 : 0;
-          const float base = slse[4 * tq + i];
+      for (int i = 0; i < 4; ++i) {
+        const int64_t r = r0 + 4 * tq + i;
+        const int limit = whole ? INT_MAX : r < rows ? off + (int)(r / G) + 1 : 0;
+        const float base = slse[4 * tq + i];
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (j0 + tk + 16 * k < limit) sum[k] += exp2f(s[i][k] - base);
-        }
+        for (int k = 0; k < 4; ++k)
+          if (j0 + tk + 16 * k < limit) sum[k] += exp2f(s[i][k] - base);
       }
     }
     __syncthreads();
@@ -1139,7 +1144,9 @@ template <typename T, int D>
 spts_status attn_plain_t(spts_ctx* ctx, const spts_paged_kv* cache, const PlainArgs& a) {
   const bool few = few_rows(ctx, cache, a.n_rows);
   const int64_t tiles = (int64_t)a.n_rows * (a.H / a.Hkv) / (few ? FEW : TILE) + cache->n_seq;       // no fewer than there are
-  const int split = share_of(ctx, tiles * a.Hkv, PL_SPLIT);
+  // a share has 64 rows of the cache at least (32 sequences of up to 68 rows: without this limit 74 us)
+  const int chunks = ceil_div(cache->max_pages * cache->page_size, TILE);
+  const int split = share_of(ctx, tiles * a.Hkv, chunks < PL_SPLIT ? chunks : PL_SPLIT);
   const dim3 grid((unsigned)(tiles * split), a.Hkv);
   return few ? launch_clusters(ctx, paged_attn_row_kernel<T, D>, grid, split, 0, a)
              : launch_clusters(ctx, paged_attn_tile_kernel<T, D>, grid, split, attn_tile_smem<D>(), a);
@@ -1149,7 +1156,9 @@ template <typename T, int D>
 spts_status weights_plain_t(spts_ctx* ctx, const spts_paged_kv* cache, const PlainArgs& a) {
   const bool few = few_rows(ctx, cache, a.n_rows);
   const int64_t most = (int64_t)cache->n_seq * ceil_div(cache->max_pages * cache->page_size, few ? PL_WARPS * WARP_KEYS : TILE);
-  const int split = share_of(ctx, most, a.Hkv < PL_SPLIT ? a.Hkv : PL_SPLIT);
+  // a share has one head at least, of the tile kernel one head and tile of queries
+  const int64_t parts = few ? a.Hkv : a.Hkv * ((int64_t)a.n_rows * (a.H / a.Hkv) / TILE + 1);
+  const int split = share_of(ctx, most, parts < PL_SPLIT ? (int)parts : PL_SPLIT);
   const int64_t resident = 4 * ctx->sm_count / split;
   const dim3 grid((unsigned)((most < resident ? most : resident) * split));
   return few ? launch_clusters(ctx, paged_weights_row_kernel<T, D>, grid, split, 0, a)
