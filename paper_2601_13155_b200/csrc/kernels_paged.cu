@@ -92,7 +92,7 @@ paged_append_kernel(Cache c, const char* __restrict__ K, int64_t ldk, const char
 // than eight such rows to a sequence on average go 64 rows at a time against 64 rows of the cache in shared memory (tile kernels: bound by
 // the multiply-adds and the shared memory that feeds them), shorter ones four at a time, straight from global memory (row kernels: bound by
 // memory where there is enough to do).  Where that makes too few blocks, a cluster of up to eight shares a block's rows of the cache, or
-// its KV heads, and joins what it found in the order of its blocks.
+// its heads and queries, and joins what it found in the order of its blocks.
 constexpr int PL_THREADS = 256, PL_WARPS = PL_THREADS / 32;
 constexpr int PL_SPLIT = 8;                    // CTAs that share a block's work at most (a portable cluster)
 constexpr int TILE = 64;                       // tile kernels: rows of queries, rows of the cache
@@ -301,7 +301,7 @@ template <int D> constexpr int attn_tile_smem() { return 3 * tile_floats<D>() * 
 
 // A cluster to (tile of 64 rows of queries, KV head).  A thread has 4 x 4 scores, then 4 rows x D / 16 dims of O; sixteen neighbouring threads
 // share the rows, whose maxima and sums stay in registers.  The weights take K's place in shared memory.  fp32 storage, 32 heads of 128 dims:
-// 1024 tokens over 4096 rows 1.9 ms (32 TFLOP/s; with 32 x 64 to a block and 8 scores to a thread 3.7), four chunks of 64 tokens 183 us.
+// 1024 tokens over 4096 rows 1.9 ms (32 TFLOP/s; with 32 x 64 to a block and 8 scores to a thread 3.7), four chunks of 64 tokens 180 us.
 template <typename T, int D>
 __global__ void __launch_bounds__(PL_THREADS, 2)
 paged_attn_tile_kernel(const __grid_constant__ PlainArgs a) {
@@ -422,7 +422,7 @@ template <int D> constexpr int weights_tile_smem() { return (2 * tile_floats<D>(
 
 // Persistent clusters over (sequence, 64 rows of it); a CTA has a part of the KV heads and tiles of queries that see any of the rows: a head's K in
 // shared memory, the queries passing by.  A thread sums its queries' weights of four rows; the sixteen threads of a row meet at the end, in their order.
-// 1024 tokens over 4096 rows, 32 heads, fp32: 1.24 ms (24 TFLOP/s; with queries fetched as they are needed 1.36, with one CTA to 64 rows and 8
+// 1024 tokens over 4096 rows, 32 heads, fp32: 1.28 ms (23 TFLOP/s; with queries fetched as they are needed 1.36, with one CTA to 64 rows and 8
 // scores to a thread 5.2).
 template <typename T, int D>
 __global__ void __launch_bounds__(PL_THREADS, 2)
