@@ -134,9 +134,11 @@ __device__ __forceinline__ bool elect_lane() {
   return mine != 0;
 }
 
-// A wait whose limit counts from its own beginning.  `flags`: [0] somebody gave up; [1] grows while rows are computed again (plain_row),
-// which may take longer than the limit: it counts from the last sign of that.
+// A wait whose limit counts from its own beginning or from the CTA's last sign of life.  `flags`: [0] somebody gave up; [1] grows with every
+// block of the cache that is asked for and while rows are computed again (plain_row): the warp that clears the rows behind a sequence's last one
+// may have nothing to do until the end of a piece that takes many seconds.
 constexpr int ABORT = 0, BUSY = 1;
+__device__ __forceinline__ void sign_of_life(volatile int* busy) { atomicAdd(const_cast<int*>(busy), 1); }
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* flags) {
   if (mbar_test_wait(bar, parity)) return true;
   uint64_t t0 = 0;
@@ -347,7 +349,7 @@ __device__ __noinline__ void plain_row(const AttnArgs& a, int b, int kvh, const 
 #pragma unroll
   for (int e = 0; e < PER; ++e) { qf[e] = __bfloat162float(q[lane * PER + e]) * sc; o[e] = 0.f; }
   for (int j0 = k0; j0 < k1; j0 += 32) {
-    if (lane == 0) *busy = *busy + 1;
+    if (lane == 0) sign_of_life(busy);
     const int64_t slots = j0 + lane < k1 ? slot_of(a.c, b, j0 + lane) : -1;
     for (int u0 = 0; u0 < 32 && j0 + u0 < k1; u0 += STEP) {
       float s[STEP], v[STEP][PER];
@@ -565,6 +567,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         load(false, s.j0, y0);
         if (ahead == 2 && nb > 1) load(false, s.j0 + 1, y1);
         for (int j = s.j0; j < s.j1 && ok; ++j) {
+          if (lane == 0) sign_of_life(flags + BUSY);
           load(true, j, y0);
           if (j + ahead < s.j1) load(false, j + ahead, ahead == 1 ? y1 : y2);
           y0 = y1; y1 = y2; y2 = place(j + 3);

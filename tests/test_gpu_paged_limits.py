@@ -1,0 +1,58 @@
+"""Calls around a paged cache at the ends of what they allow: kernels that run for seconds, lengths out of range, weights that are not
+numbers in rows that stay whatever they are, a context that goes on after a wait that gave up."""
+import pytest
+import torch
+
+import paged_ref as R
+from paper_2601_13155_b200 import binding
+from test_gpu_paged import context, near, shape_of
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True, scope="module")
+def _close():
+    yield
+    import test_gpu_paged
+    for lib in test_gpu_paged._contexts.values():
+        assert lib.check_guards() == 0
+        lib.close()
+    test_gpu_paged._contexts.clear()
+
+
+def test_an_attention_of_several_seconds_is_no_wait_that_gave_up():
+    """4,194,247 fresh tokens of one head, 8.8e12 pairs: the block whose rows behind the last one are to be cleared comes at the very end of the
+    last CTA's piece, which takes longer than the two seconds that a wait within the kernel may last without a sign of life."""
+    shape = shape_of(1, 1, 128)
+    lib = context(shape)
+    page, n_pages = 256, 16384
+    n = n_pages * page - 57
+    g = torch.Generator(device="cuda").manual_seed(9)
+    held = [torch.randn(n_pages * page, 1, 128, device="cuda", generator=g, dtype=torch.bfloat16) for _ in range(2)]
+    held[1][..., 0] = 1.0                            # a column whose result is known for every query
+    for t in held:
+        t[n:] = float("nan")
+    q = torch.randn(n, 128, device="cuda", generator=g, dtype=torch.bfloat16)
+    table = torch.randperm(n_pages, generator=torch.Generator().manual_seed(9)).to(torch.int32)[None].to("cuda")
+    k, v = (torch.empty(n_pages, page, 1, 128, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    for pool, rows in ((k, held[0]), (v, held[1])):
+        pool[table[0].long()] = rows.view(n_pages, page, 1, 128)
+    c = binding.PagedKv(shape, table, page_size=page, k=k, v=v, length=torch.tensor([n], dtype=torch.int32, device="cuda"))
+    out = torch.full((n, 128), float("nan"), device="cuda", dtype=torch.bfloat16)
+    lse = torch.full((n, 1), float("nan"), device="cuda")
+    start = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    begin.record()
+    lib.paged_attention(c, q, row_start=start, O_out=out, lse_out=lse)
+    end.record()
+    assert lib.device_status() == 0
+    assert begin.elapsed_time(end) > 2000
+    # a weight's rounding and the result's, half a step each, and two sums over the rows in (rows / 8 + 80) steps of 2^-23
+    rows = torch.arange(1, n + 1, device="cuda", dtype=torch.float64)
+    assert bool(((out[:, 0].double() - 1).abs() <= 2.01 * 2.0 ** -8 + 2.01 * (rows / 8 + 80) * 2.0 ** -23).all())
+    assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+    for first in (0, 1000, 70000):
+        m = 40
+        o, e, l, el = R.attention(q[first:first + m].view(m, 1, 128), held[0][:first + m], held[1][:first + m], first, torch.bfloat16)
+        near(out[first:first + m].view(m, 1, 128), o, e)
+        near(lse[first:first + m], l, el)
