@@ -42,7 +42,7 @@ paged_append_kernel(Cache c, const char* __restrict__ K, int64_t ldk, const char
       first = max(0, __ldg(&row_start[b]));
       if (row < first || row >= __ldg(&row_start[b + 1])) continue;
     }
-    const int64_t j = (int64_t)(at != nullptr ? __ldg(&at[b]) : c.len[b]) + (row - first);
+    const int64_t j = (int64_t)(at != nullptr ? __ldg(&at[b]) : held_rows(c, b)) + (row - first);
     if (j < 0 || j >= capacity) {
       if (lane == 0) set_status(status, SPTS_ERR_WORKSPACE);
       continue;
@@ -82,7 +82,7 @@ paged_append_kernel(Cache c, const char* __restrict__ K, int64_t ldk, const char
     int first, n;
     call_rows(row_start, n_rows, b, first, n);
     check_starts(row_start, n_rows, b, status);
-    const int64_t v = (int64_t)(at != nullptr ? at[b] : c.len[b]) + n;
+    const int64_t v = (int64_t)(at != nullptr ? at[b] : held_rows(c, b)) + n;
     c.len[b] = (int32_t)(v < 0 ? 0 : v > capacity ? capacity : v);
   }
 }

@@ -56,3 +56,32 @@ def test_an_attention_of_several_seconds_is_no_wait_that_gave_up():
         o, e, l, el = R.attention(q[first:first + m].view(m, 1, 128), held[0][:first + m], held[1][:first + m], first, torch.bfloat16)
         near(out[first:first + m].view(m, 1, 128), o, e)
         near(lse[first:first + m], l, el)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("by", ["nothing", "lengths", "places"])
+def test_append_behind_lengths_out_of_range(dtype, by):
+    """A length below zero counts as none, so the rows begin at place 0; one beyond the table leaves no room.  A place that is given is taken as
+    it is: rows before place 0 are reported and not written."""
+    shape = shape_of(4, 2, 64, dtype)
+    lib = context(shape)
+    for lens, new in (([-5, 3, -2 ** 31], [8, 2, 1]), ([-5, 3, -1], [3, 0, 0]), ([2 ** 31 - 1, 3, 33], [2, 1, 1])):
+        pages = R.Pages(shape, [0, 3, 0], 16, seed=2, room=29)             # tables of 32 rows
+        kept = pages.held(1)[0].clone()
+        pages.c.length.copy_(torch.tensor(lens, dtype=torch.int32))
+        start = torch.tensor([0, new[0], new[0] + new[1], sum(new)], dtype=torch.int32, device="cuda")
+        K, V = (torch.randn(sum(new), 2, 64, device="cuda").to(lib.dtype) for _ in range(2))
+        at = {"nothing": None, "lengths": pages.c.length, "places": pages.c.length.clone()}[by]
+        lib.paged_append(pages.c, K, V, row_start=start, at=at)
+        begin = [held if by == "places" else min(max(held, 0), 32) for held in lens]
+        lost = any(a < 0 or a + m > 32 for a, m in zip(begin, new) if m)
+        assert lib.device_status() == (3 if lost else 0)                   # SPTS_ERR_WORKSPACE
+        assert pages.c.length.tolist() == [min(max(a + m, 0), 32) for a, m in zip(begin, new)]
+        for b in (0, 1, 2):
+            for i in range(new[b]):
+                if 0 <= begin[b] + i < 32:
+                    slot = int(pages.slots(b, torch.tensor(begin[b] + i)))
+                    assert torch.equal(pages.c.k.view(-1, 2, 64)[slot], K[int(start[b]) + i])
+                    assert torch.equal(pages.c.v.view(-1, 2, 64)[slot], V[int(start[b]) + i])
+        assert torch.equal(pages.c.k.view(-1, 2, 64)[pages.slots(1, torch.arange(3)).to("cuda")], kept)
+        assert lib.check_guards() == 0
