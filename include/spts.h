@@ -595,7 +595,7 @@ spts_status spts_paged_weights(spts_ctx* ctx, const spts_paged_kv* cache, const 
 /* Cuts every sequence that holds more than keep[b] rows (DEVICE [n_seq]; below 0: the sequence is left alone) down to keep[b].
  * The rows at positions pos < n_sink and pos > p - n_recent, p being the largest position that the sequence holds, stay before all
  * others, the others by the largest weight; ties go to the row that comes first in the cache, a weight that is NaN ranks last
- * (SPTS_ERR_NONFINITE in the device status word).  Rows that stay and lie among the first keep[b] are not moved: the r-th place among those that
+ * (SPTS_ERR_NONFINITE in the device status word, also for a row that stays before all others).  Rows that stay and lie among the first keep[b] are not moved: the r-th place among those that
  * an evicted row leaves takes the r-th of the staying rows that lie behind, with its K, V, position and weight.  So the rows
  * are no longer in the order of their positions, which attention does not ask for.  len[b] becomes keep[b]; the pages behind the
  * rows left are free.  cache->weight is needed, cache->pos where n_sink > 0 or n_recent > 0. */

@@ -840,10 +840,9 @@ evict_rank_kernel(EvictArgs a) {
     if (SMEM) return keys[i];
     const int64_t slot = slot_of(c, b, j0 + i);
     if (slot < 0) { set_status(a.status, SPTS_ERR_INDEX); return 0u; }
-    if (by_pos && stays_first(c.pos[slot])) return 0xFFFFFFFFu;
-    const float w = c.weight[slot];
+    const float w = c.weight[slot];            // (a NaN is reported of rows that stay whatever they weigh, too, as above)
     if (w != w) set_status(a.status, SPTS_ERR_NONFINITE);
-    return weight_key(w);
+    return by_pos && stays_first(c.pos[slot]) ? 0xFFFFFFFFu : weight_key(w);
   };
   if (SMEM && by_pos)
     for (int i = tid; i < n; i += RANK_THREADS)

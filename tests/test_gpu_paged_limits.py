@@ -5,7 +5,7 @@ import torch
 
 import paged_ref as R
 from paper_2601_13155_b200 import binding
-from test_gpu_paged import context, near, shape_of
+from test_gpu_paged import check_evict, context, near, shape_of
 
 pytestmark = pytest.mark.gpu
 
@@ -85,3 +85,19 @@ def test_append_behind_lengths_out_of_range(dtype, by):
                     assert torch.equal(pages.c.v.view(-1, 2, 64)[slot], V[int(start[b]) + i])
         assert torch.equal(pages.c.k.view(-1, 2, 64)[pages.slots(1, torch.arange(3)).to("cuda")], kept)
         assert lib.check_guards() == 0
+
+
+@pytest.mark.parametrize("capacity", [640, 9600, 200704])
+@pytest.mark.parametrize("n_sink,n_recent", [(9, 0), (0, 9), (9, 9)])
+def test_weights_that_are_no_numbers_in_rows_that_stay_before_all_others(capacity, n_sink, n_recent):
+    """Reported whatever room the table has (one block, a cluster, keys beyond shared memory), and the same rows stay."""
+    shape = shape_of(2, 1, 64)
+    lib = context(shape)
+    for bad, status in ((0, 6 if n_sink else 0), (599, 6 if n_recent else 0), (None, 0)):      # SPTS_ERR_NONFINITE
+        pages = R.Pages(shape, [600, 50], 64, seed=capacity + n_sink)
+        wide = torch.full((2, capacity // 64), -1, dtype=torch.int32, device="cuda")
+        wide[:, : pages.c.max_pages] = pages.c.table
+        pages.c = binding.PagedKv(shape, wide, page_size=64, k=pages.c.k, v=pages.c.v, pos=pages.c.pos, weight=pages.c.weight, length=pages.c.length)
+        if bad is not None and status:
+            pages.c.weight.view(-1)[int(pages.slots(0, torch.tensor(bad)))] = float("nan")
+        check_evict(pages, lib, [300, 50], n_sink, n_recent, status=status)
