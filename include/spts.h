@@ -185,7 +185,10 @@ void spts_destroy(spts_ctx* ctx);
  * kernels of its 4-bit calls, and value 0 after 1 takes that back with SPTS_OK. */
 spts_status spts_set_option(spts_ctx* ctx, uint32_t option, int value);
 
-/* Synchronises the context's stream and returns the device status word (then clears it). */
+/* Synchronises the context's stream and returns the device status word (then clears it).  The word holds the first problem since it was
+ * read last.  After SPTS_ERR_TIMEOUT outputs of that call are incomplete, and calls that are joined by the block that comes last (those of
+ * spts_paged_*, spts_token_logprobs, spts_kv4_attention, spts_process_logits) can go wrong until the word is read: reading a word that is not
+ * SPTS_OK also clears what they count on, so the context is as before. */
 spts_status spts_last_device_status(spts_ctx* ctx);
 
 /* Guard bands (the paper has no counterpart: a stand-in for a memory checker).  Every slice the library carves out
@@ -205,7 +208,8 @@ spts_status spts_debug_check_index_list(spts_ctx* ctx, const int32_t* idx, int n
  * and return from their own waits, the CTA lets copies in flight land, records SPTS_ERR_TIMEOUT in the device
  * status word and exits normally.  This call launches one tiny CTA that runs exactly that code on two barriers
  * nobody ever arrives on, with the limit shortened to limit_us microseconds (1..100000), so a test can see the
- * status come back and the context stay usable.  The production kernels are not involved. */
+ * status come back and the context stay usable.  The production kernels are not involved; what those of spts_paged_* and
+ * spts_token_logprobs count on is left as by a call that gave up, until the status is read. */
 spts_status spts_selftest_wait_timeout(spts_ctx* ctx, uint32_t limit_us);
 
 /* Number of kernels the library has launched on this context so far. */

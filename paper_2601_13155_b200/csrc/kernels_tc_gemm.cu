@@ -538,14 +538,17 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 
 // The give-up path of the bounded waits on its own: two roles wait on barriers nobody arrives on.  Warp 0's wait
 // runs into the (shortened) limit and raises the abort flag; warp 1's wait has a limit far away and must return
-// because of the flag.  Then the same teardown as the kernels above: status word, drain delay, normal exit.
-__global__ void __launch_bounds__(64, 1) wait_selftest_kernel(uint64_t limit_ns, int* status, int* observed) {
+// because of the flag.  Then the same teardown as the kernels above: status word, drain delay, normal exit.  What it counted before
+// (one arrival in each of the counters at `paged` and `rows`) stays, as where one CTA of several gives up.
+__global__ void __launch_bounds__(64, 1) wait_selftest_kernel(uint64_t limit_ns, int* status, int* observed, int* paged, int n_paged, int* rows, int n_rows) {
   __shared__ __align__(8) uint64_t bar_store[2];
   __shared__ int abort_store;
   volatile int* abort_flag = &abort_store;
   const uint32_t bar0 = smem_u32(&bar_store[0]), bar1 = smem_u32(&bar_store[1]);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint64_t t0 = globaltimer_ns();
+  for (int i = threadIdx.x; i < n_paged; i += 64) atomicAdd(paged + i, 1);
+  for (int i = threadIdx.x; i < n_rows; i += 64) atomicAdd(rows + i, 1);
   if (threadIdx.x == 0) {
     *abort_flag = 0;
     mbar_init(bar0, 1);
@@ -655,7 +658,8 @@ int tc_sumsq_parts(int n_out) { return ceil_div(n_out, 256); }
 
 spts_status launch_wait_selftest(spts_ctx* ctx, uint32_t limit_us) {
   // observed[] lives behind the status word: ws.status has 64 ints, the first is the status itself
-  wait_selftest_kernel<<<1, 64, 0, ctx->stream>>>((uint64_t)limit_us * 1000ull, ctx->ws.status, ctx->ws.status + 8);
+  wait_selftest_kernel<<<1, 64, 0, ctx->stream>>>((uint64_t)limit_us * 1000ull, ctx->ws.status, ctx->ws.status + 8,
+                                                 ctx->ws.paged_arrived, PAGED_COUNTERS, ctx->ws.lp_arrived, LOGITS_MAX_ROWS);
   SPTS_CUDA_OK(ctx);
   return SPTS_OK;
 }

@@ -562,6 +562,28 @@ spts_status batch_attention_blocks(spts_ctx* ctx, const spts_layer_weights* w, v
   return SPTS_OK;
 }
 
+// The calls around 4-bit generation and paged caches, and the device status, may be asked for while another device is current.
+struct DeviceScope {
+  int back = -1;
+  bool ok;
+  explicit DeviceScope(const spts_ctx* ctx) {
+    int cur = -1;
+    ok = cudaGetDevice(&cur) == cudaSuccess;
+    if (ok && cur != ctx->device) { back = cur; ok = cudaSetDevice(ctx->device) == cudaSuccess; }
+  }
+  ~DeviceScope() { if (back >= 0) cudaSetDevice(back); }
+};
+#define ON_DEVICE(ctx) DeviceScope device_scope__(ctx); if (!device_scope__.ok) return SPTS_ERR_CUDA
+
+// What kernels leave at zero for the next call, unless one gave up a wait: counts of those that are done, running maxima.
+bool clear_counters(spts_ctx* ctx) {
+  return cudaMemsetAsync(ctx->ws.paged_arrived, 0, PAGED_COUNTERS * sizeof(int), ctx->stream) == cudaSuccess &&
+         cudaMemsetAsync(ctx->ws.lp_arrived, 0, LOGITS_MAX_ROWS * sizeof(int), ctx->stream) == cudaSuccess &&
+         cudaMemsetAsync(ctx->ws.kv4_arrived, 0, KV4_MAX_CTAS * sizeof(int), ctx->stream) == cudaSuccess &&
+         cudaMemsetAsync(ctx->ws.lg_key, 0, LOGITS_MAX_ROWS * sizeof(unsigned long long), ctx->stream) == cudaSuccess &&
+         cudaMemsetAsync(ctx->ws.lg_arrived, 0, LOGITS_MAX_ROWS * sizeof(int), ctx->stream) == cudaSuccess;
+}
+
 spts_status check_ctx(const spts_ctx* ctx) { return ctx == nullptr ? SPTS_ERR_INVALID_ARG : SPTS_OK; }
 
 }  // namespace
@@ -622,14 +644,7 @@ spts_status spts_create(const spts_model_desc* desc, int max_seq, void* workspac
     return SPTS_ERR_CUDA;
   }
   if (spts_status s = paged_init(ctx); s != SPTS_OK) { spts_destroy(ctx); return s; }
-  if (cudaMemsetAsync(ctx->ws.paged_arrived, 0, PAGED_COUNTERS * sizeof(int), ctx->stream) != cudaSuccess ||
-      cudaMemsetAsync(ctx->ws.lp_arrived, 0, LOGITS_MAX_ROWS * sizeof(int), ctx->stream) != cudaSuccess ||
-      cudaMemsetAsync(ctx->ws.kv4_arrived, 0, KV4_MAX_CTAS * sizeof(int), ctx->stream) != cudaSuccess ||
-      cudaMemsetAsync(ctx->ws.lg_key, 0, LOGITS_MAX_ROWS * sizeof(unsigned long long), ctx->stream) != cudaSuccess ||
-      cudaMemsetAsync(ctx->ws.lg_arrived, 0, LOGITS_MAX_ROWS * sizeof(int), ctx->stream) != cudaSuccess) {
-    spts_destroy(ctx);
-    return SPTS_ERR_CUDA;
-  }
+  if (!clear_counters(ctx)) { spts_destroy(ctx); return SPTS_ERR_CUDA; }
   *out = ctx;
   return SPTS_OK;
 }
@@ -699,10 +714,14 @@ spts_status spts_set_option(spts_ctx* ctx, uint32_t option, int value) {
 
 spts_status spts_last_device_status(spts_ctx* ctx) {
   TRY(check_ctx(ctx));
+  ON_DEVICE(ctx);
   if (cudaStreamSynchronize(ctx->stream) != cudaSuccess) return SPTS_ERR_CUDA;
   int st = 0;
   if (cudaMemcpy(&st, ctx->ws.status, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) return SPTS_ERR_CUDA;
-  if (st != 0 && cudaMemset(ctx->ws.status, 0, sizeof(int)) != cudaSuccess) return SPTS_ERR_CUDA;
+  if (st == 0) return SPTS_OK;
+  if (cudaMemset(ctx->ws.status, 0, sizeof(int)) != cudaSuccess) return SPTS_ERR_CUDA;
+  // the word holds the first problem alone: a wait may have been given up behind any
+  if (!clear_counters(ctx) || cudaStreamSynchronize(ctx->stream) != cudaSuccess) return SPTS_ERR_CUDA;
   return (spts_status)st;
 }
 
@@ -1150,18 +1169,6 @@ spts_status spts_decode_step(spts_ctx* ctx, const spts_model_weights* mw, spts_k
 
 // ---- generation with 4-bit weights and caches
 namespace {
-// The calls of this part may be made while another device is current.
-struct DeviceScope {
-  int back = -1;
-  bool ok;
-  explicit DeviceScope(const spts_ctx* ctx) {
-    int cur = -1;
-    ok = cudaGetDevice(&cur) == cudaSuccess;
-    if (ok && cur != ctx->device) { back = cur; ok = cudaSetDevice(ctx->device) == cudaSuccess; }
-  }
-  ~DeviceScope() { if (back >= 0) cudaSetDevice(back); }
-};
-#define ON_DEVICE(ctx) DeviceScope device_scope__(ctx); if (!device_scope__.ok) return SPTS_ERR_CUDA
 bool group_ok(int group) { return group == 32 || group == 64 || group == 128; }
 bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 bool aligned4(std::initializer_list<const void*> ps) {

@@ -101,3 +101,32 @@ def test_weights_that_are_no_numbers_in_rows_that_stay_before_all_others(capacit
         if bad is not None and status:
             pages.c.weight.view(-1)[int(pages.slots(0, torch.tensor(bad)))] = float("nan")
         check_evict(pages, lib, [300, 50], n_sink, n_recent, status=status)
+
+
+def test_calls_after_a_wait_that_gave_up():
+    """A CTA that gives up leaves what others have counted: reading the status puts that in order for everything that is joined by the one that
+    comes last, single tokens and chunks over long caches, weights, appends, evictions and long rows of logits."""
+    shape = shape_of(8, 2, 128)
+    lib = binding.Spts(shape, max_seq=64)
+    want = None
+    for gave_up in (False, True, False):
+        if gave_up:
+            lib.selftest_wait_timeout(1000)
+            assert lib.device_status() == 5                                # SPTS_ERR_TIMEOUT
+        got = []
+        for rows in (1, 90):
+            pages = R.Pages(shape, [9000, 700], 64, seed=rows, room=100)
+            q, start = R.queries(shape, [rows, rows], seed=rows)
+            K, V = (torch.randn(2 * rows, 2, 128, generator=torch.Generator().manual_seed(rows)).to(torch.bfloat16).to("cuda") for _ in range(2))
+            lib.paged_append(pages.c, K, V, row_start=start)
+            out, lse = lib.paged_attention(pages.c, q, row_start=start, want_lse=True)
+            lib.paged_weights(pages.c, q, lse, row_start=start, decay=0.0)
+            lib.paged_evict(pages.c, torch.tensor([4000, 690], dtype=torch.int32, device="cuda"))
+            got += [out, lse, pages.c.weight.nan_to_num(-1.0), pages.c.length, pages.c.k.nan_to_num(-1.0)]
+        x = torch.randn(2, 128256, generator=torch.Generator().manual_seed(3)).to("cuda")
+        got += list(lib.token_logprobs(x, torch.tensor([5, 128000], dtype=torch.int32, device="cuda"), n_top=6).values())
+        assert lib.device_status() == 0 and lib.check_guards() == 0
+        want = want or got
+        assert got[3].tolist() == [4000, 690]
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    lib.close()
