@@ -86,7 +86,8 @@ struct TopShared {
   unsigned long long list[LP_LIST];            // order << 32 | ~token: the larger key comes first
   unsigned long long best[SPTS_LOGPROBS_MAX_TOP];
   unsigned long long warp_best[LP_WARPS];
-  uint32_t warp_floor[LP_WARPS];
+  uint32_t warp_floor[LP_WARPS];               // of find_floor
+  uint32_t stretch_floor;                      // (a word of its own: slower warps may still be reading the others)
   int n;                                       // candidates asked for, of which those below LP_LIST are there
   uint32_t most[LP_STRETCHES];                 // order of the largest token of a stretch
   int reach, reaching[LP_STRETCHES];           // stretches that reach the floor
@@ -315,7 +316,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(LogprobArgs a, 
           const uint32_t mine = t.most[i];
           int above = 0;
           for (int j = 0; j < stretches; ++j) above += t.most[j] > mine || (t.most[j] == mine && j < i);
-          if (above == k - 1) t.warp_floor[0] = mine;
+          if (above == k - 1) t.stretch_floor = mine;
         }
       } else if (warp == 0) {
         // the largest number of twenty bits (and twelve zeros) that k stretches reach, bit by bit
@@ -329,10 +330,10 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(LogprobArgs a, 
             if (32 * u < stretches) reach += mine[u] >= (floor | bit);
           if (__reduce_add_sync(0xffffffffu, reach) >= k) floor |= bit;
         }
-        if (lane == 0) t.warp_floor[0] = floor;
+        if (lane == 0) t.stretch_floor = floor;
       }
       __syncthreads();
-      from = max(from, t.warp_floor[0]);
+      from = max(from, t.stretch_floor);
     }
     for (int i = tid; i < stretches; i += LP_THREADS)
       if (t.most[i] >= from) t.reaching[atomicAdd(&t.reach, 1)] = i;
