@@ -377,12 +377,10 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(LogprobArgs a, 
       reinterpret_cast<uint32_t*>(mine)[8 + 2 * tid] = tid < listed ? (uint32_t)(t.list[tid] >> 32) : 0u;
       reinterpret_cast<uint32_t*>(mine)[9 + 2 * tid] = tid < listed ? (uint32_t)t.list[tid] : 0u;
     }
-    __threadfence();
     __syncthreads();
-    if (tid == 0) last = atomicAdd(&a.arrived[row], 1) == slices - 1;
+    if (tid == 0) last = count_arrival(&a.arrived[row]) == slices - 1;
     __syncthreads();
     if (!last) return;
-    __threadfence();
     if (tid == 0) a.arrived[row] = 0;
     const float* all = a.part + (int64_t)row * slices * LP_PART_FLOATS;
     if (warp == 0) {

@@ -71,10 +71,7 @@ paged_append_kernel(Cache c, const char* __restrict__ K, int64_t ldk, const char
   }
   __shared__ bool last;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    __threadfence();
-    last = atomicAdd(arrived, 1) == (int)gridDim.x - 1;
-  }
+  if (threadIdx.x == 0) last = count_arrival(arrived) == (int)gridDim.x - 1;
   __syncthreads();
   if (!last) return;
   if (threadIdx.x == 0) *arrived = 0;
@@ -1095,10 +1092,7 @@ evict_move_kernel(EvictArgs a, int n_seq, int split) {
     __syncthreads();
   }
   if (items > 0) {
-    if (tid == 0) {
-      __threadfence();
-      last = atomicAdd(a.arrived, 1) == (int)gridDim.x - 1;
-    }
+    if (tid == 0) last = count_arrival(a.arrived) == (int)gridDim.x - 1;
     __syncthreads();
     if (!last) return;
     if (tid == 0) *a.arrived = 0;

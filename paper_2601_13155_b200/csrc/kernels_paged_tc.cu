@@ -939,13 +939,12 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         // the CTA that leaves the unit's last share joins it, a warp to a row
         const long long total = start->total;
         const int ctas = gridDim.x, first = cta_of(total, s.begin, ctas), last = cta_of(total, s.begin + s.cost - 1, ctas);
-        __threadfence();
         mbar_arrive(g_done + 8 * t);
         ok = wait_warp(g_done + 8 * t, n_g & 1, flags);
         ++n_g;
         if (!ok) break;
         if (row == 0) {
-          const bool is_last = atomicAdd(a.arrived + 8 * first, 1) == last - first;
+          const bool is_last = count_arrival(a.arrived + 8 * first) == last - first;
           if (is_last) a.arrived[8 * first] = 0;
           g_last[t] = is_last;
         }
@@ -954,7 +953,6 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         ++n_g;
         if (!ok) break;
         if (g_last[t]) {
-          __threadfence();
           for (int r = quarter; r < s.tokens * a.G; r += 4) join_row<D>(a, s.row, s.h, first, last, 0, r);
         }
       }
@@ -1330,15 +1328,14 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         const int first = cta_of(total, begin, ctas), last = cta_of(total, end - 1, ctas);
         float* share = a.share + (size_t)(2 * cta + (s.i0 == 0 ? 1 : 0)) * 2 * BLOCK;
         __stcg(share + t * BLOCK + quarter * 32 + lane, w);
-        __threadfence();
         __syncwarp();
         int seen = 0;
         int* arrived = a.arrived + first * 8 + (warp - 4);
-        if (lane == 0) seen = atomicAdd(arrived, 1);
+        if (lane == 0) seen = count_arrival(arrived);
+        __syncwarp();
         seen = __shfl_sync(0xffffffffu, seen, 0);
         write = seen == last - first;
         if (write) {
-          __threadfence();
           if (lane == 0) *arrived = 0;
           w = 0.f;
           for (int c = first; c <= last; ++c)

@@ -336,6 +336,15 @@ spts_status launch_rope_rows(spts_ctx* ctx, const float* in, const float2* cs, i
 __device__ __forceinline__ void dep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// One thread counts its block (or warp) as done, for "the one that comes last goes on"; how many there were before.  A release and an acquire of
+// this thread: what the threads wrote that it has met at a barrier is visible before the count, and what others counted before it is
+// visible after it, to this thread and to those that it meets at the next barrier.
+__device__ __forceinline__ int count_arrival(int* counter) {
+  int before;
+  asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
+  return before;
+}
+
 template <typename... KArgs, typename... Args>
 cudaError_t launch_dependent(void (*kernel)(KArgs...), dim3 grid, dim3 block, cudaStream_t st, Args... args) {
   cudaLaunchConfig_t cfg = {};

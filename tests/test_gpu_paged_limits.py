@@ -130,3 +130,34 @@ def test_calls_after_a_wait_that_gave_up():
         assert got[3].tolist() == [4000, 690]
         assert all(torch.equal(a, b) for a, b in zip(got, want))
     lib.close()
+
+
+def test_joined_results_never_hold_another_calls_shares():
+    """Two calls in turn, many times over: a share that was read before it was written would be the other call's."""
+    shape = shape_of(8, 2, 128)
+    lib = context(shape)
+    made = []
+    for seed in (1, 2):
+        pages = R.Pages(shape, [30000, 9000, 700], 64, seed=seed, room=64)
+        q, start = R.queries(shape, [1, 1, 1], seed=seed)
+        x = torch.randn(3, 128256, generator=torch.Generator().manual_seed(seed)).to("cuda")
+        K, V = (torch.randn(3, 2, 128, generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16).to("cuda") for _ in range(2))
+        made.append((pages, q, x, K, V, pages.c.length.clone(), []))
+    for _ in range(60):
+        for pages, q, x, K, V, lens, seen in made:
+            lib.paged_append(pages.c, K, V, at=lens)
+            out, lse = lib.paged_attention(pages.c, q, want_lse=True)
+            lib.paged_weights(pages.c, q, lse, decay=0.0)
+            got = [out, lse, pages.c.weight.nan_to_num(-1.0), pages.c.length.clone()]
+            got += list(lib.token_logprobs(x, torch.arange(3, dtype=torch.int32, device="cuda"), n_top=4).values())
+            seen.append(got)
+    assert lib.device_status() == 0
+    for pages, q, x, K, V, lens, seen in made:
+        assert seen[0][3].tolist() == [30001, 9001, 701]
+        for got in seen[1:]:
+            assert all(torch.equal(a, b) for a, b in zip(got, seen[0]))
+        for b, held in enumerate([30001, 9001, 701]):
+            k, v = pages.held(b)[:2]
+            o, e, l, el = R.attention(q[b:b + 1], k, v, held - 1, torch.bfloat16)
+            near(seen[0][0][b:b + 1].view(1, 8, 128), o, e)
+            near(seen[0][1][b:b + 1], l, el)
