@@ -33,3 +33,25 @@ def test_alternatives_whichever_floor_is_the_higher(vocab, n, where):
             assert bool(((out["top_logprob"].double() - want).abs() <= bound).all())
     assert lib.device_status() == 0 and lib.check_guards() == 0
     lib.close()
+
+
+@pytest.mark.parametrize("n", [2, 700])
+def test_stretches_of_several_pieces(n):
+    """The longest rows: a stretch whose largest token is noted is several pieces' 512 where a row is not shared."""
+    vocab = 1 << 20
+    lib = binding.Spts(synth.ModelShape(hidden=256, n_q_heads=4, n_kv_heads=2, head_dim=64, ffn_dim=256, ltp_dlow=64, ltp_rank=16, n_layers=1, vocab=64,
+                                        dtype="bf16"), max_seq=64)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    x = torch.randn(n, vocab, device="cuda", generator=g)
+    target = torch.randint(0, vocab, (n,), device="cuda", generator=g, dtype=torch.int32)
+    out = lib.token_logprobs(x, target, n_top=32)
+    assert lib.device_status() == 0 and lib.check_guards() == 0
+    for i in range(0, n, max(1, n // 7)):
+        value, index = torch.sort(x[i], descending=True, stable=True)
+        assert torch.equal(out["top_token"][i], index[:32].to(torch.int32))
+        xt = x[i, int(target[i])]
+        assert int(out["rank"][i]) == int((x[i] > xt).sum() + ((x[i] == xt) & (torch.arange(vocab, device="cuda") < int(target[i]))).sum())
+        want = xt.double() - torch.logsumexp(x[i].double(), -1)
+        bound = 2 * (2.0 ** -21 + 16 * 2.0 ** -23) + (vocab / 512 + 60) * 2.0 ** -24 + 2.0 ** -22 * (1 + want.abs() + 16)
+        assert abs(float(out["logprob"][i]) - float(want)) <= float(bound)
+    lib.close()

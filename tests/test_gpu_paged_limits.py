@@ -5,7 +5,7 @@ import torch
 
 import paged_ref as R
 from paper_2601_13155_b200 import binding
-from test_gpu_paged import check_evict, context, near, shape_of
+from test_gpu_paged import check_attention, check_evict, context, near, shape_of
 
 pytestmark = pytest.mark.gpu
 
@@ -161,3 +161,21 @@ def test_joined_results_never_hold_another_calls_shares():
             o, e, l, el = R.attention(q[b:b + 1], k, v, held - 1, torch.bfloat16)
             near(seen[0][0][b:b + 1].view(1, 8, 128), o, e)
             near(seen[0][1][b:b + 1], l, el)
+
+
+@pytest.mark.parametrize("dtype,plain", [("bf16", False), ("bf16", True), ("fp32", False)])
+@pytest.mark.parametrize("heads,kv,dim", [(2, 2, 64), (4, 4, 128), (14, 2, 64), (32, 4, 128)])
+@pytest.mark.parametrize("chunk,others", [(512, 63), (300, 40), (33, 200)])
+def test_one_long_chunk_beside_many_single_tokens(dtype, plain, heads, kv, dim, chunk, others):
+    """What goes by the batch's average chunk (tiles of one or two, who joins, boxes of queries, rows or tiles) holds for those far from it."""
+    lens = [9000] + [1 + 37 * i % 900 for i in range(others)]
+    rows = [chunk] + [1] * others
+    check_attention(shape_of(heads, kv, dim, dtype), lens, rows, 64, plain, seed=chunk + heads)
+    check_attention(shape_of(heads, kv, dim, dtype), lens[::-1], rows[::-1], 16, plain, seed=others)
+
+
+@pytest.mark.parametrize("n_sink,n_recent", [(0, 0), (4, 64)])
+def test_evict_more_rows_than_have_their_numbers_in_shared_memory(n_sink, n_recent):
+    """Beyond 1,048,576 rows; a sequence beside it that gives up a few."""
+    shape = shape_of(1, 1, 64)
+    check_evict(R.Pages(shape, [1100003, 5000], 256, seed=3), context(shape), [400001, 4990], n_sink, n_recent)
