@@ -182,7 +182,7 @@ void spts_destroy(spts_ctx* ctx);
  * (value 0/1), or SPTS_PAP_WINDOW (value 1..64).  A context whose shape or storage type has no
  * tensor-core kernels for the prefill runs it on the plain ones whatever the option says and
  * answers value 0 with SPTS_ERR_UNSUPPORTED; in bf16 SPTS_REFERENCE_KERNELS still selects the
- * kernels of its 4-bit calls, and value 0 after 1 takes that back with SPTS_OK. */
+ * kernels of its 4-bit calls and of spts_paged_*, and value 0 after 1 takes that back with SPTS_OK. */
 spts_status spts_set_option(spts_ctx* ctx, uint32_t option, int value);
 
 /* Synchronises the context's stream and returns the device status word (then clears it).  The word holds the first problem since it was
@@ -555,7 +555,7 @@ spts_status spts_decode_step4(spts_ctx* ctx, const spts_model_weights4* mw, cons
  * beyond max_pages * page_size counts as that, one below 0 as 0).  What lies behind a sequence's rows and in pages of no sequence may
  * hold anything.  Sequences may share pages that no call writes: an append writes the pages of the new rows, spts_paged_weights and
  * spts_paged_evict those of all rows.  An entry of the table that a held or new row needs and that is outside [0, n_pages) puts
- * SPTS_ERR_INDEX into the device status word; its rows read as zeros and are not written. */
+ * SPTS_ERR_INDEX into the device status word; its rows read as zeros and are not written, and an eviction ranks them last. */
 typedef struct {
   void* k;                /* [n_pages, page_size, Hkv, d] in the storage type (K after RoPE), 16-byte aligned */
   void* v;
@@ -575,7 +575,7 @@ typedef struct {
  * Rows behind row_start[n_seq] (padding) are ignored.  Starts ascend within [0, n_rows]; of a sequence that claims rows outside only
  * those that there are count, and starts that break the rule put SPTS_ERR_INDEX into the device status word.  A row that would lie
  * outside [0, max_pages * page_size) is not written, len is clipped to that range, and SPTS_ERR_WORKSPACE goes to the device status
- * word.  pos [n_rows] is stored where the cache has positions; the weight of a new row is 0. */
+ * word.  pos [n_rows] is stored where the cache has positions (NULL: they stay as they were); the weight of a new row is 0. */
 spts_status spts_paged_append(spts_ctx* ctx, const spts_paged_kv* cache, const void* K, int64_t ldk, const void* V, int64_t ldv,
                               const int32_t* pos, const int32_t* row_start, const int32_t* at, int n_rows);
 

@@ -11,7 +11,7 @@
 // list in shared memory, and of that the best are taken.  Where the list runs over (equal logits), the slice is gone through piece by piece.
 // A row is shared by slices where rows are few; the slice that arrives last joins what the others left, in their order.
 // Bound by memory where rows are many: 509 rows of 152063 take 69 us with 20 alternatives (4.5 TB/s), 54 without (5.8 TB/s); one row of 128256
-// 10 us, a chain of latencies.  Lists kept piece by piece and threads that search their own tokens again took 157 and 100 us for the former.
+// 9.6 us, a chain of latencies.  Lists kept piece by piece and threads that search their own tokens again took 157 and 100 us for the former.
 #include "spts_common.cuh"
 
 namespace spts {

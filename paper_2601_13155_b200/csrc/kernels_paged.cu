@@ -19,7 +19,7 @@ constexpr int APPEND_WARPS = 8;
 
 // One warp copies a row's K, another its V, in 16-byte pieces, four in flight to a lane.  Lengths grow only once no block reads the old ones
 // any more: the block that is done last sets them (one launch).  Bound by memory where rows are many (eight chunks of up to 4099 tokens,
-// 118 MB: 22 us, 5.4 TB/s), else by the launch (one row of 64 sequences: 3.2 us).
+// 118 MB: 22 us, 5.4 TB/s), else by the launch (one row of 64 sequences: 3.3 us).
 __global__ void __launch_bounds__(APPEND_WARPS * 32)
 paged_append_kernel(Cache c, const char* __restrict__ K, int64_t ldk, const char* __restrict__ V, int64_t ldv, int row_bytes,
                     const int32_t* __restrict__ pos, const int32_t* __restrict__ row_start, const int32_t* __restrict__ at, int n_rows,
@@ -657,7 +657,7 @@ paged_attn_row_kernel(const __grid_constant__ PlainArgs a) {
 }
 
 // Persistent clusters over (sequence, 256 rows of it), 32 to a warp; a CTA has every split-th KV head, whose queries stay in registers while
-// the warp's rows pass.  32 single tokens over up to 4096 rows, 32 heads, fp32: 101 us, 2.1 TB/s.
+// the warp's rows pass.  32 single tokens over up to 4096 rows, 32 heads, fp32: 104 us, 2.1 TB/s.
 template <typename T, int D>
 __global__ void __launch_bounds__(PL_THREADS, 2)
 paged_weights_row_kernel(const __grid_constant__ PlainArgs a) {
@@ -1129,6 +1129,8 @@ int share_of(const spts_ctx* ctx, int64_t blocks, int most) {
   while (2 * split <= most && blocks * split < 8 * ctx->sm_count) split *= 2;
   return split;
 }
+// (By the batch's average: 63 single tokens beside a chunk of 512, 2048 rows each, go by tiles as well and take 1590 us, weights 2120, where
+// the two by themselves take 212 + 586 and 239 + 327.)
 bool few_rows(const spts_ctx* ctx, const spts_paged_kv* cache, int n_rows) {
   return (int64_t)n_rows * (ctx->desc.n_q_heads / ctx->desc.n_kv_heads) <= (int64_t)FEW_MOST * cache->n_seq;
 }
@@ -1214,7 +1216,9 @@ spts_status launch_paged_evict(spts_ctx* ctx, const spts_paged_kv* cache, const 
   a.words = (int)align_up((size_t)capacity, EVICT_CHUNK) / 32;
   a.bits = ctx->ws.evict_bits; a.before = ctx->ws.evict_before; a.total = ctx->ws.evict_total; a.status = ctx->ws.status;
   a.arrived = ctx->ws.paged_arrived + 1;
-  // one CTA ranks what it holds in a few rounds of its threads; longer sequences are shared by a cluster, whose barriers cost more
+  // one CTA ranks what it holds in a few rounds of its threads; longer sequences are shared by a cluster, whose barriers cost more.  The lengths
+  // lie on the device, so this goes by the room that the table has: 48 sequences of up to 4111 rows take 19.4 us in tables of 4128 rows, 23.3 in
+  // tables of 32768, 26.4 in tables of 262144, whose parts would not fit shared memory (one of 32768 rows: 28.0, 28.2 and 34.4).
   const int split = capacity <= 8 * RANK_THREADS ? 1 : EVICT_SPLIT;
   const int part = part_rows(capacity, split);
   const bool smem = part <= RANK_KEYS;

@@ -165,7 +165,7 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatil
 }
 
 // ------------------------------------------------------------------------------------------------ the line of blocks
-// sum of floor((a i + b) / m), i < n, by the Euclidean recursion on (m, a); a, b and m stay small, so 32 bits hold a n + b for all
+// sum of floor((a i + b) / m), i < n, by the well-known recursion of such sums that follows Euclid's algorithm on (m, a); a, b and m stay small, so 32 bits hold a n + b for all
 // but the longest lines
 __device__ unsigned long long floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
   unsigned long long sum = 0;
@@ -445,10 +445,12 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, int unit_row, int h,
 }
 
 // ------------------------------------------------------------------------------------------------ the kernel
-// Long chunks are bound by the instructions of the softmax warps beside the matrix products (2048 tokens over 34816 rows, 32 heads of 128 dims:
-// 0.96 ms, 1175 TFLOP/s; 16384 fresh ones 1279; with a quarter of the exponentials as polynomials of degree five 7 % slower), decode steps by
-// memory (64 sequences of up to 16384 rows: 5.7 to 6.1 TB/s; 48 of up to nine drafted tokens 127 us, 5.1 TB/s), single short ones by their chain of
-// latencies (777 rows: 11.8 us).  Sixteen softmax warps instead of eight were slower (64 single tokens 188 us against 147; 2048 tokens 1064
+// Long chunks fill no unit (2048 tokens over 34816 rows, 32 heads of 128 dims, replayed: 0.96 to 1.07 ms, 1060 to 1180 TFLOP/s; tensor pipe busy
+// 64 %, issue slots 38 %, and 2.27 GB read where K and V hold 143 MB, which the L2 does not): what is left is the two softmax warpgroups' chain of
+// loads, maxima, exponentials and stores beside the products, and blocks that miss the L2 (16384 fresh tokens, whose K and V fit it: 1225 to 1279
+// TFLOP/s).  With a quarter of the exponentials as polynomials of degree five 7 % slower.  Decode steps are bound by memory (64 sequences of up to
+// 16384 rows: 280 us, 6.2 TB/s; 48 of up to nine drafted tokens 129 us, 5.0 TB/s), single short ones by their chain of latencies (777
+// rows: 11.9 us).  Sixteen softmax warps instead of eight were slower (64 single tokens 188 us against 147; 2048 tokens 1064
 // against 964).
 struct Start { Walk walk; long long total; };      // a CTA's piece, the line's length
 
@@ -810,7 +812,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             const float2 x = __ffma2_rn(make_float2(__uint_as_float(r[e0]), __uint_as_float(r[e0 + 1])), sc2, nm2);
             const float2 p = make_float2(ex2(x.x), ex2(x.y));
             ps[(e >> 1) & 3] = __fadd2_rn(ps[(e >> 1) & 3], p);
-            pk[e >> 1] = pack2(p.x, p.y);              // rounded once, before it meets V; the sum takes it unrounded
+            // rounded to bf16 once, since the product takes both operands in V's type; the sum takes it unrounded.  That adds as much to
+            // the error as the result's own rounding (0.0017 -> 0.0022 to 0.0024 of the RMS); a second product for what the rounding
+            // leaves would double P V.
+            pk[e >> 1] = pack2(p.x, p.y);
           }
 #pragma unroll
           for (int c = 0; c < 32; c += 16) tmem_st16(tS + 32 * half + c, pk + c);
@@ -996,11 +1001,11 @@ paged_attn_join_kernel(const __grid_constant__ AttnArgs a) {
 // meeting another one.  A unit is two blocks of 128 rows of a sequence, its cost the number of (KV head, tile of queries) that see any of
 // them; all units end to end are cut into equal pieces as in the attention.  The warps of a unit that several CTAs work on leave their sums
 // in the workspace; of each 32 rows the warp that comes last adds them up in the order of the line.
-//   warp 0      TMA producer: for every KV head the two blocks of K (two pairs in flight), for every tile of queries its Q (three)
+//   warp 0      TMA producer: for every KV head the two blocks of K (two pairs in flight), for every tile of queries its Q (two)
 //   warp 1      TMEM owner and MMA issuer: two accumulators for each of the two blocks
 //   warps 2-3   -lse log2(e) of a tile's queries into shared memory
 //   warps 4-11  the exponentials of every second item, warps 12-19 of the others; of the first block warps 4-7 and 12-15
-// Bound by memory where queries are few (16 single tokens over up to 8192 rows: 25.6 us, 4.3 TB/s with the launch and the line's ends), by the
+// Bound by memory where queries are few (16 single tokens over up to 8192 rows: 26.3 us, 4.2 TB/s with the launch and the line's ends), by the
 // exponential unit where they are many: 512 tokens over 32768 rows take 193 us (290 with two warps on each of its quarters instead of four),
 // 64 tokens 33 us (37; with all 128 columns of a row in registers at once 46).
 constexpr int PW_THREADS = 640;
@@ -1412,7 +1417,8 @@ spts_status attention_t(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q
   a.c = make_cache(cache); a.row_start = row_start; a.n_rows = n_rows;
   a.H = ctx->desc.n_q_heads; a.Hkv = ctx->desc.n_kv_heads; a.G = a.H / a.Hkv;
   a.tile_tokens = BLOCK / a.G;
-  // two tiles to a unit where sequences have more tokens than one holds, on average
+  // two tiles to a unit where sequences have more tokens than one holds, on average (63 single tokens and a chunk of 512, 8192 rows each,
+  // which take one: 410 us together, 327 and 86 by themselves)
   a.unit_tokens = n_rows > (int64_t)cache->n_seq * a.tile_tokens ? 2 * a.tile_tokens : a.tile_tokens;
   // (measured: with 1, 2, 3 blocks 64 single tokens over up to 8192 rows take 151, 144, 145 us, 8192 fresh tokens 495, 461, 456 us)
   a.extra = a.unit_tokens > a.tile_tokens ? 3 : 2;
@@ -1440,7 +1446,8 @@ spts_status weights_t(spts_ctx* ctx, const spts_paged_kv* cache, const void* Q, 
   WeightArgs a;
   a.c = make_cache(cache); a.row_start = row_start; a.n_rows = n_rows;
   a.H = ctx->desc.n_q_heads; a.Hkv = ctx->desc.n_kv_heads; a.G = a.H / a.Hkv;
-  // tiles of queries as long as the sequences' chunks on average: a box brings in no more queries than that
+  // tiles of queries as long as the sequences' chunks on average: a box brings in no more queries than that.  (Chunks far from the average pay
+  // for it: 63 single tokens and a chunk of 512, 8192 rows each, take 270 us together, 171 and 61 by themselves.)
   const int most = BLOCK / a.G, mean = ceil_div(n_rows, cache->n_seq);
   a.tile_tokens = mean < 1 ? 1 : mean < most ? mean : most;
   a.lse = lse; a.decay = decay;
